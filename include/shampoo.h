@@ -373,6 +373,115 @@ int shampoo_root_inverse_newton(const float *a, int32_t n, int32_t batch, float 
  * Host only, no device work; SHAMPOO_ERR_NULL / SHAMPOO_ERR_SHAPE on bad arguments. */
 int shampoo_jacobi_pair(int32_t s, int32_t halves, int32_t round, int32_t k, int32_t *p, int32_t *q);
 
+/* ------------------------------------------------------------------------------------------
+ * Operators of a training pass that make the gradients of a step.  Each is asynchronous on `stream` and works on the
+ * current device; pointers are device pointers unless a line says otherwise; argument errors are returned before any work
+ * is enqueued.  Matrices are row-major, a leading dimension (ld..., in elements) is the distance of their rows.  dtype codes
+ * are SHAMPOO_GRAD_F32 and SHAMPOO_GRAD_BF16.  Sums, norms and softmax statistics are float32.  The same call on the
+ * same inputs gives the same bits.
+ * ------------------------------------------------------------------------------------------ */
+
+/* How a weight lies in memory: rows of inputs for every output, or the other way round. */
+enum { SHAMPOO_OUT_IN = 0, SHAMPOO_IN_OUT = 1 };
+
+/*
+ * Softmax cross entropy of a linear layer over many classes, and its gradients:
+ *   z = x w^T + bias,  lse_i = log sum_v exp z_iv,  loss_i = lse_i - z_{i,t_i},
+ *   g_iv = scale weight_i (exp(z_iv - lse_i) - [v = t_i]),  dx = g w,  dw = g^T x,  dbias_v = sum_i g_iv
+ * (the gradients of scale sum_i weight_i loss_i).  The logits of a piece of the rows at a time lie in the workspace,
+ * at most 4 GiB of them (or 256 rows), never all of them.
+ * A row whose target is outside 0 ... classes - 1 is ignored: loss 0 and g_i = 0 whatever its logits are (its row of x
+ * still is a factor of dw: 0 times a value that is not finite is not 0).  bias may mask classes by -infinity: their
+ * probability and gradient are 0; a masked target has loss +infinity; a row with every class masked has g_i = 0.
+ */
+typedef struct {
+  int64_t rows;           /* >= 0                                                              */
+  int32_t features;       /* 1 ... 65536                                                       */
+  int32_t classes;        /* 1 ... 4194304                                                     */
+  int32_t dtype;          /* of x, w and dx.  bf16: z from exact products; g is rounded to bf16 for the products of dx
+                             and bf16 dw, to 16 bits for those of float32 dw.  float32: all products to float32 accuracy
+                             (three bf16 terms per value, six products)                       */
+  int32_t grad_dtype;     /* of dw; float32 x: float32                                         */
+  int32_t w_layout;       /* of w and dw: SHAMPOO_OUT_IN [classes][features], SHAMPOO_IN_OUT [features][classes] */
+  int32_t has_bias;       /* != 0: bias is given                                              */
+  int32_t gradients;      /* != 0: dx, dw (and dbias) are wanted; 0: the loss alone             */
+  int64_t ldx, ldw, lddx, lddw;
+} shampoo_cross_entropy;
+/* bytes of workspace; 0 if c is invalid */
+size_t shampoo_linear_cross_entropy_workspace_bytes(const shampoo_cross_entropy *c);
+/*
+ * x [rows][features], w per w_layout: 16-byte aligned (else SHAMPOO_ERR_UNSUPPORTED); bias [classes] float32 or NULL;
+ * targets [rows] int64; weight [rows] float32 or NULL (all 1); loss [rows] float32, not weighted;
+ * dx [rows][features], dw like w, dbias [classes] float32: overwritten; each may be NULL where it is not wanted.
+ * workspace: 256-byte aligned.
+ */
+int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, const void *w, const float *bias,
+                                 const int64_t *targets, const float *weight, float scale, float *loss,
+                                 void *dx, void *dw, float *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Activation checkpoints in 8 bits.  A matrix is kept as codes q (int8) and one exponent s per row and group of 32
+ * neighbouring columns: x ~ q 2^s with q = rint(x 2^-s) and the smallest s for which the group's largest |x| rounds to at
+ * most 127.  Groups below 2^-100 are kept as zeros; a group with an infinity, a NaN or a value from 255 2^120 on
+ * reads NaN as a whole.  33 bytes per 32 values (columns are padded to a multiple of 32).
+ * `packed` is opaque: 256-byte aligned memory of shampoo_checkpoint_bytes(rows, cols) bytes (0 if they are invalid:
+ * rows < 0, cols < 1 or above 1048576).
+ */
+enum { SHAMPOO_ACT_NONE = 0, SHAMPOO_ACT_RELU = 1, SHAMPOO_ACT_GELU = 2 /* with erf */, SHAMPOO_ACT_SILU = 3 };
+size_t shampoo_checkpoint_bytes(int64_t rows, int32_t cols);
+int shampoo_checkpoint_pack(const void *x, int32_t dtype, int64_t rows, int32_t cols, int64_t ldx,
+                            void *packed, size_t packed_bytes, void *stream);
+/* y = a(x) of what the checkpoint holds */
+int shampoo_checkpoint_unpack(const void *packed, size_t packed_bytes, int64_t rows, int32_t cols, int32_t activation,
+                              void *y, int32_t dtype, int64_t ldy, void *stream);
+/* dx = dy a'(x) (ReLU: 0 at 0); dx may be dy */
+int shampoo_checkpoint_activation_grad(const void *packed, size_t packed_bytes, int64_t rows, int32_t cols, int32_t activation,
+                                       const void *dy, int32_t dtype, int64_t lddy, void *dx, int64_t lddx, void *stream);
+/*
+ * Gradient of a linear layer y = a(x) W + b from the checkpoint of x [rows][in] and dy [rows][out]:
+ *   dW = a(x)^T dy (SHAMPOO_IN_OUT; SHAMPOO_OUT_IN: transposed),  db = column sums of dy (float32; NULL: not wanted).
+ * dtype: of dy (16-byte aligned, else SHAMPOO_ERR_UNSUPPORTED).  Float32 dy: products to float32 accuracy, dw float32.
+ * bf16 dy: x and dy enter as they are; a(x), where an activation is given, rounded to bf16 for bf16 dw and to 16 bits for
+ * float32 dw.  in <= 65536, out <= 4194304.
+ */
+size_t shampoo_checkpoint_weight_grad_workspace_bytes(int64_t rows, int32_t in, int32_t out, int32_t activation, int32_t dtype,
+                                                      int64_t lddy, int32_t grad_dtype, int32_t want_bias);
+int shampoo_checkpoint_weight_grad(const void *packed, size_t packed_bytes, int64_t rows, int32_t in, int32_t activation,
+                                   const void *dy, int32_t dtype, int32_t out, int64_t lddy, void *dw, int32_t grad_dtype,
+                                   int32_t w_layout, int64_t lddw, float *db, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Residual sum with the norms after and before a block, its gate and its scale:
+ *   u = norm_post(f),  r_out = r + scale gate u,  h = norm_pre(r_out),
+ *   norm(x) = (x - mean) / sqrt(mean of its squares + epsilon) w + b   (SHAMPOO_NORM_RMS: without mean and b).
+ * Sums and norms in float32 on values that are not rounded between the steps.
+ */
+enum { SHAMPOO_NORM_NONE = 0, SHAMPOO_NORM_RMS = 1, SHAMPOO_NORM_LAYER = 2 };
+typedef struct {
+  int64_t rows;            /* >= 0                                                             */
+  int32_t cols;            /* 1 ... 16384                                                       */
+  int32_t dtype;           /* of r, f, r_out, h and their gradients                              */
+  int32_t post, pre;       /* SHAMPOO_NORM_*; NONE: u = f, no h                                  */
+  int64_t gates;           /* 0: no gate; otherwise gate is [gates][cols] and every rows / gates rows share one (gates divides rows) */
+  float epsilon, scale;    /* epsilon >= 0                                                       */
+  const float *w_post, *b_post, *gate, *w_pre, *b_pre; /* [cols] float32; w of every norm that is there, b of a layer norm or NULL */
+} shampoo_residual_norm;
+/* r, f, r_out, h: [rows][cols], dense (ld = cols unless ld is given); r_out may be r.  packed_r, packed_f: where checkpoints of r and f are written
+ * (both or neither), as by shampoo_checkpoint_pack. */
+int shampoo_residual_norm_forward(const shampoo_residual_norm *c, const void *r, int64_t ldr, const void *f, int64_t ldf,
+                                  void *r_out, int64_t ld_r_out, void *h, int64_t ldh,
+                                  void *packed_r, void *packed_f, size_t packed_bytes, void *stream);
+/*
+ * Gradients from those of r_out (dr_out, NULL: 0) and of h (dh; NULL where there is no h).  r and f as the forward call had them: packed != 0:
+ * their checkpoints (ldr, ldf ignored), otherwise the matrices.  dr may be dr_out, df may be dh.  dgate [gates][cols], dw_post, db_post,
+ * dw_pre, db_pre [cols]: float32, each NULL where it is not wanted.
+ */
+size_t shampoo_residual_norm_backward_workspace_bytes(const shampoo_residual_norm *c);
+int shampoo_residual_norm_backward(const shampoo_residual_norm *c, int32_t packed, const void *r, int64_t ldr, const void *f, int64_t ldf,
+                                   const void *dr_out, int64_t ld_dr_out, const void *dh, int64_t ld_dh,
+                                   void *dr, int64_t ld_dr, void *df, int64_t ld_df, float *dgate, float *dw_post, float *db_post,
+                                   float *dw_pre, float *db_pre, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Static, NUL-terminated description of a return code. */
 const char *shampoo_strerror(int code);
 

@@ -22,6 +22,9 @@ ROOT_EIGH, ROOT_NEWTON = 0, 1
 LARGE_DIM_BLOCKING, LARGE_DIM_ADAGRAD, LARGE_DIM_DIAGONAL = 0, 1, 2
 MATRIX_CORES_AUTO, MATRIX_CORES_FP32 = 0, 1
 STAGE_FACTOR, STAGE_GRAFT, STAGE_ROOT, STAGE_PRECOND, STAGE_UPDATE, STAGE_DIAG, STAGE_FUSED, STAGE_PRECOND2 = range(8)
+OUT_IN, IN_OUT = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 STAGE_NAMES = ("factor", "graft", "root", "precond", "update", "diag", "fused", "precond2")
 
 EXPORTS = (
@@ -30,6 +33,10 @@ EXPORTS = (
     "shampoo_root_inverse_workspace_bytes", "shampoo_root_inverse", "shampoo_root_inverse_static",
     "shampoo_root_inverse_warm_workspace_bytes", "shampoo_root_inverse_warm",
     "shampoo_root_inverse_newton_workspace_bytes", "shampoo_root_inverse_newton", "shampoo_jacobi_pair",
+    "shampoo_linear_cross_entropy_workspace_bytes", "shampoo_linear_cross_entropy",
+    "shampoo_checkpoint_bytes", "shampoo_checkpoint_pack", "shampoo_checkpoint_unpack", "shampoo_checkpoint_activation_grad",
+    "shampoo_checkpoint_weight_grad_workspace_bytes", "shampoo_checkpoint_weight_grad",
+    "shampoo_residual_norm_forward", "shampoo_residual_norm_backward_workspace_bytes", "shampoo_residual_norm_backward",
     "shampoo_strerror",
 )
 
@@ -63,6 +70,18 @@ class ShampooConfig(ctypes.Structure):
         ("grad_dtype", ctypes.c_int32),
         ("device", ctypes.c_int32),
     ]
+
+
+class CrossEntropy(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in (
+        "features", "classes", "dtype", "grad_dtype", "w_layout", "has_bias", "gradients")] + [
+        (n, ctypes.c_int64) for n in ("ldx", "ldw", "lddx", "lddw")]
+
+
+class ResidualNorm(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("cols", "dtype", "post", "pre")] + [
+        ("gates", ctypes.c_int64), ("epsilon", ctypes.c_float), ("scale", ctypes.c_float)] + [
+        (n, ctypes.c_void_p) for n in ("w_post", "b_post", "gate", "w_pre", "b_pre")]
 
 
 _lib = None
@@ -112,6 +131,29 @@ def lib():
     L.shampoo_root_inverse_newton.restype = ctypes.c_int
     L.shampoo_jacobi_pair.argtypes = [ctypes.c_int32] * 4 + [ctypes.POINTER(ctypes.c_int32)] * 2
     L.shampoo_jacobi_pair.restype = ctypes.c_int
+    cep, rnp = ctypes.POINTER(CrossEntropy), ctypes.POINTER(ResidualNorm)
+    L.shampoo_linear_cross_entropy_workspace_bytes.argtypes = [cep]
+    L.shampoo_linear_cross_entropy_workspace_bytes.restype = sz
+    L.shampoo_linear_cross_entropy.argtypes = [cep, vp, vp, vp, vp, vp, f32, vp, vp, vp, vp, vp, sz, vp]
+    L.shampoo_linear_cross_entropy.restype = ctypes.c_int
+    L.shampoo_checkpoint_bytes.argtypes = [i64, i32]
+    L.shampoo_checkpoint_bytes.restype = sz
+    L.shampoo_checkpoint_pack.argtypes = [vp, i32, i64, i32, i64, vp, sz, vp]
+    L.shampoo_checkpoint_pack.restype = ctypes.c_int
+    L.shampoo_checkpoint_unpack.argtypes = [vp, sz, i64, i32, i32, vp, i32, i64, vp]
+    L.shampoo_checkpoint_unpack.restype = ctypes.c_int
+    L.shampoo_checkpoint_activation_grad.argtypes = [vp, sz, i64, i32, i32, vp, i32, i64, vp, i64, vp]
+    L.shampoo_checkpoint_activation_grad.restype = ctypes.c_int
+    L.shampoo_checkpoint_weight_grad_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i64, i32, i32]
+    L.shampoo_checkpoint_weight_grad_workspace_bytes.restype = sz
+    L.shampoo_checkpoint_weight_grad.argtypes = [vp, sz, i64, i32, i32, vp, i32, i32, i64, vp, i32, i32, i64, vp, vp, sz, vp]
+    L.shampoo_checkpoint_weight_grad.restype = ctypes.c_int
+    L.shampoo_residual_norm_forward.argtypes = [rnp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]
+    L.shampoo_residual_norm_forward.restype = ctypes.c_int
+    L.shampoo_residual_norm_backward_workspace_bytes.argtypes = [rnp]
+    L.shampoo_residual_norm_backward_workspace_bytes.restype = sz
+    L.shampoo_residual_norm_backward.argtypes = [rnp, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64] + [vp] * 5 + [vp, sz, vp]
+    L.shampoo_residual_norm_backward.restype = ctypes.c_int
     L.shampoo_strerror.argtypes = [ctypes.c_int]
     L.shampoo_strerror.restype = ctypes.c_char_p
     _lib = L
@@ -387,3 +429,207 @@ def shampoo_root_inverse_newton(a, epsilon, p, tolerance=1e-6, max_iterations=10
     if want_failed:
         res.append(failed)
     return res[0] if len(res) == 1 else tuple(res)
+
+
+# ----------------------------------------------------------------------------
+# Operators of a training pass
+# ----------------------------------------------------------------------------
+def _dtype_code(dtype):
+    import torch
+    assert dtype in (torch.float32, torch.bfloat16), f"float32 or bfloat16, not {dtype}"
+    return GRAD_BF16 if dtype == torch.bfloat16 else GRAD_F32
+
+
+def _rows(x, dtype=None, align=1):
+    """A CUDA matrix whose rows are contiguous, as the library reads it (a copy where it is not, or not aligned to `align` bytes)."""
+    assert x.is_cuda and x.dim() == 2 and (dtype is None or x.dtype == dtype), "a CUDA matrix of the right type is needed"
+    if (x.shape[1] > 1 and x.stride(1) != 1) or (x.shape[0] > 1 and x.stride(0) < x.shape[1]):
+        x = x.contiguous()
+    return x.new_empty(x.shape).copy_(x) if x.data_ptr() % align else x
+
+
+def _ld(x):
+    return x.stride(0) if x.shape[0] > 1 else max(x.shape[1], 1)
+
+
+def _ptr(x):
+    return ctypes.c_void_p(x.data_ptr()) if x is not None else None
+
+
+def _vector(x, shape, device):
+    """A float32 operand of exactly this shape, or None"""
+    import torch
+    if x is None:
+        return None
+    assert x.device == device and x.dtype == torch.float32 and tuple(x.shape) == tuple(shape), "a float32 tensor of the right shape is needed"
+    return x.contiguous()
+
+
+def _workspace(nbytes, device):
+    import torch
+    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+
+
+def shampoo_linear_cross_entropy(x, w, targets, bias=None, weight=None, scale=1.0, grad_dtype=None, gradients=True):
+    """Loss of every row, lse(x w^T + bias) - (x w^T + bias)[target], and the gradients of scale * sum(weight * loss).
+
+    x [n, d] and w [v, d]: CUDA, both float32 or both bfloat16; w may be the transposed view of a [d, v] matrix, dw then is one
+    too.  targets [n] int64 (outside 0 ... v - 1: ignored), bias [v] and weight [n] float32.  Returns (loss, dx, dw, dbias),
+    dbias None without a bias, dw of grad_dtype (default: the type of w); with gradients=False the loss alone."""
+    import torch
+    code = _dtype_code(x.dtype)
+    assert w.is_cuda and w.dim() == 2 and w.dtype == x.dtype and w.device == x.device and w.shape[1] == x.shape[1]
+    n, d, v = x.shape[0], x.shape[1], w.shape[0]
+    assert targets.device == x.device and targets.dtype == torch.int64 and tuple(targets.shape) == (n,)
+    grad_dtype = grad_dtype or w.dtype
+    in_out = v > 1 and w.stride(0) == 1 and (d > 1 or w.stride(1) != 1)      # the view of a matrix [d, v]
+    x, wm = _rows(x, align=16), _rows(w.t() if in_out else w, align=16)
+    targets, bias, weight = targets.contiguous(), _vector(bias, (v,), x.device), _vector(weight, (n,), x.device)
+    loss = torch.empty((n,), dtype=torch.float32, device=x.device)
+    dx = dw = dbias = None
+    if gradients:
+        dx = torch.empty((n, d), dtype=x.dtype, device=x.device)
+        dw = torch.empty(tuple(wm.shape), dtype=grad_dtype, device=x.device)
+        dbias = torch.empty((v,), dtype=torch.float32, device=x.device) if bias is not None else None
+    c = CrossEntropy(n, d, v, code, _dtype_code(grad_dtype), IN_OUT if in_out else OUT_IN, 1 if bias is not None else 0,
+                     1 if gradients else 0, _ld(x), _ld(wm), d, wm.shape[1])
+    ws = _workspace(lib().shampoo_linear_cross_entropy_workspace_bytes(ctypes.byref(c)), x.device)
+    with torch.cuda.device(x.device):
+        _check(lib().shampoo_linear_cross_entropy(ctypes.byref(c), _ptr(x), _ptr(wm), _ptr(bias), _ptr(targets), _ptr(weight), scale,
+                                                  _ptr(loss), _ptr(dx), _ptr(dw), _ptr(dbias), _ptr(ws), ws.numel(), _stream_ptr()))
+    if not gradients:
+        return loss
+    return loss, dx, dw.t() if in_out else dw, dbias
+
+
+class Checkpoint:
+    """An activation [rows, cols] in 8 bits (codes and shared exponents in one CUDA tensor)."""
+
+    def __init__(self, packed, rows, cols, dtype):
+        self.packed, self.rows, self.cols, self.dtype = packed, rows, cols, dtype
+
+    @classmethod
+    def empty(cls, rows, cols, dtype, device):
+        nbytes = lib().shampoo_checkpoint_bytes(rows, cols)
+        if nbytes == 0 and rows > 0:
+            raise ShampooError(-7)
+        return cls(_workspace(nbytes, device), rows, cols, dtype)
+
+
+def shampoo_checkpoint_pack(x):
+    """Checkpoint of a CUDA matrix [rows, cols], float32 or bfloat16."""
+    import torch
+    code, x = _dtype_code(x.dtype), _rows(x)
+    c = Checkpoint.empty(x.shape[0], x.shape[1], x.dtype, x.device)
+    with torch.cuda.device(x.device):
+        _check(lib().shampoo_checkpoint_pack(_ptr(x), code, c.rows, c.cols, _ld(x), _ptr(c.packed), c.packed.numel(), _stream_ptr()))
+    return c
+
+
+def shampoo_checkpoint_unpack(c, activation=ACT_NONE, dtype=None):
+    """activation(x) [rows, cols] of what a checkpoint holds, in `dtype` (default: that of the packed matrix)."""
+    import torch
+    y = torch.empty((c.rows, c.cols), dtype=dtype or c.dtype, device=c.packed.device)
+    with torch.cuda.device(y.device):
+        _check(lib().shampoo_checkpoint_unpack(_ptr(c.packed), c.packed.numel(), c.rows, c.cols, activation, _ptr(y),
+                                               _dtype_code(y.dtype), c.cols, _stream_ptr()))
+    return y
+
+
+def shampoo_checkpoint_activation_grad(c, dy, activation):
+    """dy * activation'(x) for the x that a checkpoint holds."""
+    import torch
+    assert tuple(dy.shape) == (c.rows, c.cols) and dy.device == c.packed.device
+    code, dy = _dtype_code(dy.dtype), _rows(dy)
+    dx = torch.empty((c.rows, c.cols), dtype=dy.dtype, device=dy.device)
+    with torch.cuda.device(dy.device):
+        _check(lib().shampoo_checkpoint_activation_grad(_ptr(c.packed), c.packed.numel(), c.rows, c.cols, activation, _ptr(dy), code,
+                                                        _ld(dy), _ptr(dx), c.cols, _stream_ptr()))
+    return dx
+
+
+def shampoo_checkpoint_weight_grad(c, dy, activation=ACT_NONE, grad_dtype=None, out_in=False, bias=False):
+    """Gradient of the weight of y = activation(x) W from a checkpoint of x [rows, in] and dy [rows, out]: [in, out], or [out, in]
+    with out_in; of grad_dtype (default: the type of dy).  With bias also the column sums of dy, float32."""
+    import torch
+    assert dy.dim() == 2 and dy.shape[0] == c.rows and dy.device == c.packed.device
+    code, dy = _dtype_code(dy.dtype), _rows(dy, align=16)
+    out = dy.shape[1]
+    dw = torch.empty((out, c.cols) if out_in else (c.cols, out), dtype=grad_dtype or dy.dtype, device=dy.device)
+    db = torch.empty((out,), dtype=torch.float32, device=dy.device) if bias else None
+    grad = _dtype_code(dw.dtype)
+    nbytes = lib().shampoo_checkpoint_weight_grad_workspace_bytes(c.rows, c.cols, out, activation, code, _ld(dy), grad, 1 if bias else 0)
+    ws = _workspace(nbytes, dy.device)
+    with torch.cuda.device(dy.device):
+        _check(lib().shampoo_checkpoint_weight_grad(_ptr(c.packed), c.packed.numel(), c.rows, c.cols, activation, _ptr(dy), code, out,
+                                                    _ld(dy), _ptr(dw), grad, OUT_IN if out_in else IN_OUT, dw.shape[1], _ptr(db),
+                                                    _ptr(ws), ws.numel(), _stream_ptr()))
+    return (dw, db) if bias else dw
+
+
+def _residual_norm(rows, cols, dtype, device, post, pre, w_post, b_post, gate, w_pre, b_pre, epsilon, scale):
+    if gate is not None and gate.dim() == 1:
+        gate = gate[None]
+    keep = [_vector(w_post, (cols,), device), _vector(b_post, (cols,), device),
+            _vector(gate, (gate.shape[0], cols), device) if gate is not None else None,
+            _vector(w_pre, (cols,), device), _vector(b_pre, (cols,), device)]
+    c = ResidualNorm(rows, cols, _dtype_code(dtype), post, pre, gate.shape[0] if gate is not None else 0, epsilon, scale,
+                     *[k.data_ptr() if k is not None else None for k in keep])
+    c._keep = keep
+    return c
+
+
+def shampoo_residual_norm_forward(r, f, post=NORM_RMS, pre=NORM_RMS, w_post=None, b_post=None, gate=None, w_pre=None, b_pre=None,
+                                  epsilon=1e-5, scale=1.0, checkpoint=False):
+    """r_out = r + scale * gate * norm_post(f) and h = norm_pre(r_out) (None where pre is NORM_NONE).  r, f [rows, cols], float32 or
+    bfloat16; weights [cols] and gate [cols] or [gates, cols] (every rows / gates rows share one) float32.  With
+    checkpoint also those of r and f, for the backward pass: (r_out, h, r8, f8)."""
+    import torch
+    assert r.dim() == 2 and r.shape == f.shape and r.dtype == f.dtype and r.device == f.device
+    r, f = _rows(r), _rows(f)
+    rows, cols = r.shape
+    c = _residual_norm(rows, cols, r.dtype, r.device, post, pre, w_post, b_post, gate, w_pre, b_pre, epsilon, scale)
+    r_out = torch.empty((rows, cols), dtype=r.dtype, device=r.device)
+    h = torch.empty_like(r_out) if pre != NORM_NONE else None
+    r8, f8 = (Checkpoint.empty(rows, cols, r.dtype, r.device) for _ in range(2)) if checkpoint else (None, None)
+    with torch.cuda.device(r.device):
+        _check(lib().shampoo_residual_norm_forward(
+            ctypes.byref(c), _ptr(r), _ld(r), _ptr(f), _ld(f), _ptr(r_out), cols, _ptr(h), cols,
+            _ptr(r8.packed) if checkpoint else None, _ptr(f8.packed) if checkpoint else None, r8.packed.numel() if checkpoint else 0,
+            _stream_ptr()))
+    return (r_out, h, r8, f8) if checkpoint else (r_out, h)
+
+
+def shampoo_residual_norm_backward(r, f, dr_out, dh, post=NORM_RMS, pre=NORM_RMS, w_post=None, b_post=None, gate=None, w_pre=None,
+                                   b_pre=None, epsilon=1e-5, scale=1.0):
+    """Gradients of shampoo_residual_norm_forward from those of r_out (None: zero) and h (None where there is no h); r and f: the
+    matrices, or the checkpoints that the forward pass wrote.  Returns a dict of dr, df, and float32 dgate, dw_post, db_post,
+    dw_pre, db_pre, None for those of what is not there."""
+    import torch
+    packed = isinstance(r, Checkpoint)
+    assert packed == isinstance(f, Checkpoint)
+    dtype, device = r.dtype, (r.packed.device if packed else r.device)
+    rows, cols = (r.rows, r.cols) if packed else r.shape
+    if packed:
+        assert (f.rows, f.cols, f.packed.device) == (rows, cols, device)
+    else:
+        assert f.shape == r.shape and f.dtype == dtype and f.device == device
+        r, f = _rows(r), _rows(f)
+    for d in (dr_out, dh):
+        assert d is None or (d.device == device and d.dtype == dtype and tuple(d.shape) == (rows, cols))
+    dr_out, dh = (None if d is None else _rows(d) for d in (dr_out, dh))
+    c = _residual_norm(rows, cols, dtype, device, post, pre, w_post, b_post, gate, w_pre, b_pre, epsilon, scale)
+    out = {"dr": torch.empty((rows, cols), dtype=dtype, device=device), "df": torch.empty((rows, cols), dtype=dtype, device=device)}
+    vector = lambda wanted, shape: torch.empty(shape, dtype=torch.float32, device=device) if wanted else None
+    out["dgate"] = vector(gate is not None, gate.shape if gate is not None else ())
+    out["dw_post"], out["db_post"] = vector(post != NORM_NONE, (cols,)), vector(b_post is not None and post == NORM_LAYER, (cols,))
+    out["dw_pre"], out["db_pre"] = vector(pre != NORM_NONE, (cols,)), vector(b_pre is not None and pre == NORM_LAYER, (cols,))
+    ws = _workspace(lib().shampoo_residual_norm_backward_workspace_bytes(ctypes.byref(c)), device)
+    with torch.cuda.device(device):
+        _check(lib().shampoo_residual_norm_backward(
+            ctypes.byref(c), 1 if packed else 0, _ptr(r.packed if packed else r), cols if packed else _ld(r),
+            _ptr(f.packed if packed else f), cols if packed else _ld(f),
+            _ptr(dr_out), _ld(dr_out) if dr_out is not None else 0, _ptr(dh), _ld(dh) if dh is not None else 0,
+            _ptr(out["dr"]), cols, _ptr(out["df"]), cols, *[_ptr(out[k]) for k in ("dgate", "dw_post", "db_post", "dw_pre", "db_pre")],
+            _ptr(ws), ws.numel(), _stream_ptr()))
+    return out

@@ -6,13 +6,14 @@ import os
 import subprocess
 import sys
 import sysconfig
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB = os.path.join(HERE, "libshampoo.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
-SOURCES = [os.path.join(HERE, "csrc", "shampoo.hip")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("shampoo.hip", "training.hip")]
 FLAGS = [
-    "-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950",
+    "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
     # packed fp32 instructions are kept out of the generated code
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
@@ -31,16 +32,23 @@ def marshal_command():
                "-L" + os.path.join(root, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"])
 
 
-def build(verbose=True):
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmds = [[hipcc] + FLAGS + SOURCES + ["-o", LIB], marshal_command()]
-    for cmd in cmds:
-        if verbose:
+def _run(cmds, verbose):
+    """All of them side by side"""
+    if verbose:
+        for cmd in cmds:
             print(" ".join(cmd), flush=True)
-    running = [subprocess.Popen(cmd) for cmd in cmds]     # side by side
+    running = [subprocess.Popen(cmd) for cmd in cmds]
     failed = [cmd for cmd, p in zip(cmds, running) if p.wait() != 0]
     if failed:
         raise subprocess.CalledProcessError(1, failed[0])
+
+
+def build(verbose=True):
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.basename(f) + ".o") for f in SOURCES]
+        _run([[hipcc] + FLAGS + ["-c", f, "-o", o] for f, o in zip(SOURCES, objects)] + [marshal_command()], verbose)
+        _run([[hipcc, "-shared", "--offload-arch=gfx950"] + objects + ["-o", LIB]], verbose)
     return LIB
 
 

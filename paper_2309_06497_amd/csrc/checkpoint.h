@@ -1,0 +1,207 @@
+// Activation checkpoints in 8 bits.
+//
+// A matrix [rows][cols] is kept as codes q (int8) and one exponent s per row and group of 32 neighbouring features:
+// x ~ q 2^s, q = rint(x 2^-s), with the smallest s for which the group's largest |x| rounds to at most 127.  A power of two
+// for the scale makes every step of both directions exact but the one rounding (x 2^-s is exact, q 2^s is a bf16 value), so
+// that the products that read a checkpoint (train_gemm.h) lose nothing more, and the codes do not depend on how a
+// kernel orders its work.  The error of an element is at most half a step: 1/255 ... 1/127.5 of the largest of its group.
+// Groups whose largest element is below 2^-100 are zero; a group with an infinity, a NaN or an element from 255 2^120
+// on is NaN as a whole.
+//
+// In memory: codes [rows][pitch], pitch = cols rounded up to 32 (zeros at the end of a row), then, from the next multiple of
+// 256 bytes on, the exponents [rows][pitch / 32], one byte each: s + 133 (0: zero group, 255: not finite).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include "vectors.h"
+
+namespace shampoo {
+
+enum { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
+
+struct Packed {
+  int8_t *codes; uint8_t *exps;
+  int64_t rows;
+  int32_t cols, pitch;
+};
+
+// The exponent byte of a group from the bits of its largest |x|: x in [1, 2) 2^e gives s = e - 6, or e - 5 where x 2^(6 - e)
+// would round to 128 (from 127.5 on: the upper seven mantissa bits all ones, which the addition carries into the exponent).
+__device__ __forceinline__ uint32_t exponent_byte(uint32_t largest) {
+  if (largest >= 0x7f7f0000u) return 255u;                  // would carry into the exponent of infinity
+  if (largest < (27u << 23)) return 0u;                     // 2^-100
+  return (largest + 0x10000u) >> 23;                        // e + 127 = s + 133
+}
+// 2^-s and 2^s of an exponent byte (27 ... 254); for byte 0 the codes are zero, for 255 the scale makes them NaN
+__device__ __forceinline__ float code_per_value(uint32_t byte) { return __uint_as_float((260u - byte) << 23); }
+__device__ __forceinline__ float value_per_code(uint32_t byte) {
+  return byte == 255u ? __uint_as_float(0x7fc00000u) : byte < 27u ? 0.f : __uint_as_float((byte - 6u) << 23);
+}
+
+// Eight neighbouring values of a lane, four neighbouring lanes a group: their codes, and the group's byte in `byte`
+__device__ __forceinline__ uint2 pack8(const f32x8 &x, uint32_t &byte) {
+  uint32_t largest = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) largest = max(largest, __float_as_uint(x.v[e]) & 0x7fffffffu);
+  largest = max(largest, (uint32_t)__shfl_xor((int)largest, 1, 64));
+  largest = max(largest, (uint32_t)__shfl_xor((int)largest, 2, 64));
+  byte = exponent_byte(largest);
+  uint32_t w[2] = {0u, 0u};
+  if (byte == 255u) { w[0] = w[1] = 0x01010101u; }           // 1 x NaN
+  else if (byte != 0u) {
+    const float per = code_per_value(byte);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e >> 2] |= ((uint32_t)(int)rintf(x.v[e] * per) & 255u) << (8 * (e & 3));
+  }
+  return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ f32x8 unpack8(uint2 w, float scale) {
+  f32x8 r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r.v[e] = (float)(int8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3))) * scale;
+  return r;
+}
+// eight values at column c (a multiple of 8 below pitch) of row i
+__device__ __forceinline__ f32x8 packed_load8(const Packed &p, int64_t i, int c) {
+  const uint2 w = *reinterpret_cast<const uint2 *>(p.codes + i * p.pitch + c);
+  return unpack8(w, value_per_code(p.exps[i * (p.pitch >> 5) + (c >> 5)]));
+}
+// all 64 lanes have to take part; lanes past the row's end with zeros
+__device__ __forceinline__ void packed_store8(const Packed &p, int64_t i, int c, const f32x8 &x) {
+  uint32_t byte;
+  const uint2 w = pack8(x, byte);
+  if (c >= p.pitch) return;
+  *reinterpret_cast<uint2 *>(p.codes + i * p.pitch + c) = w;
+  if ((c & 31) == 0) p.exps[i * (p.pitch >> 5) + (c >> 5)] = (uint8_t)byte;
+}
+
+__device__ __forceinline__ float activate(float z, int kind) {
+  switch (kind) {
+    case ACT_RELU: return z > 0.f ? z : z != z ? z : 0.f;
+    case ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    case ACT_SILU: return z / (1.f + expf(-z));
+    default: return z;
+  }
+}
+__device__ __forceinline__ float slope(float z, int kind) {
+  switch (kind) {
+    case ACT_RELU: return z > 0.f ? 1.f : z != z ? z : 0.f;
+    case ACT_GELU: return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+    case ACT_SILU: { const float s = 1.f / (1.f + expf(-z)); return s * (1.f + z * (1.f - s)); }
+    default: return 1.f;
+  }
+}
+
+// Pieces of eight in row order: a thread takes one piece, a grid at most 2^30 of them; row0: the grid's first row.
+// One pass, 16 bytes (8 for codes) per lane: bound by memory.
+struct PackArgs {
+  const void *x; int64_t ldx;
+  Packed p;
+  int64_t row0; uint32_t pieces, per_row;      // pieces of this grid; pitch / 8
+  int32_t vec;
+};
+template <typename T> __global__ __launch_bounds__(256) void checkpoint_pack_kernel(const PackArgs g) {
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+  const uint32_t r = min(i, g.pieces - 1) / g.per_row;
+  const int c = (int)(min(i, g.pieces - 1) - r * g.per_row) * 8;
+  const int64_t row = g.row0 + r;
+  const f32x8 x = load8(static_cast<const T *>(g.x) + row * g.ldx, c, g.p.cols, g.vec);
+  uint32_t byte;
+  const uint2 w = pack8(x, byte);                // per_row is a multiple of 4: a group never straddles rows or wavefronts
+  if (i >= g.pieces) return;
+  *reinterpret_cast<uint2 *>(g.p.codes + row * g.p.pitch + c) = w;
+  if ((c & 31) == 0) g.p.exps[row * (g.p.pitch >> 5) + (c >> 5)] = (uint8_t)byte;
+}
+
+// y = a(x), or dx = dy a'(x)
+struct UnpackArgs {
+  Packed p;
+  const void *dy; int64_t lddy;                // GRAD
+  void *y; int64_t ldy;
+  int64_t row0; uint32_t pieces, per_row;
+  int32_t vec, activation;
+};
+template <typename T, bool GRAD> __global__ __launch_bounds__(256) void checkpoint_unpack_kernel(const UnpackArgs g) {
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+  if (i >= g.pieces) return;
+  const uint32_t r = i / g.per_row;
+  const int c = (int)(i - r * g.per_row) * 8;
+  const int64_t row = g.row0 + r;
+  if (c >= g.p.cols) return;
+  f32x8 x = packed_load8(g.p, row, c);
+  if constexpr (GRAD) {
+    const f32x8 d = load8(static_cast<const T *>(g.dy) + row * g.lddy, c, g.p.cols, g.vec);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x.v[e] = d.v[e] * slope(x.v[e], g.activation);
+  } else if (g.activation != ACT_NONE) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x.v[e] = activate(x.v[e], g.activation);
+  }
+  store8(static_cast<T *>(g.y) + row * g.ldy, c, g.p.cols, g.vec, x);
+}
+
+// a(x) of a checkpoint, or a matrix in memory (float32 or bf16, any alignment), as PLANES bf16 planes [plane][rows][ld], ld a
+// multiple of 8, zeros from cols to ld.
+struct PlanesArgs {
+  Packed p; const void *x; int64_t ldx;        // one of the two
+  uint16_t *out; int64_t plane, ld;
+  int64_t row0; uint32_t pieces, per_row;      // ld / 8
+  int32_t cols, vec, activation;
+};
+enum { FROM_PACKED = 0, FROM_F32 = 1, FROM_BF16 = 2 };
+template <int FROM, int PLANES> __global__ __launch_bounds__(256) void planes_kernel(const PlanesArgs g) {
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+  if (i >= g.pieces) return;
+  const uint32_t r = i / g.per_row;
+  const int c = (int)(i - r * g.per_row) * 8;
+  const int64_t row = g.row0 + r;
+  f32x8 x = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+  if constexpr (FROM == FROM_PACKED) {
+    if (c < g.p.pitch) x = packed_load8(g.p, row, c);
+    if (g.activation != ACT_NONE) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x.v[e] = c + e < g.cols ? activate(x.v[e], g.activation) : 0.f;
+    } else {                                     // a group that is not finite reads NaN in the padding too
+#pragma unroll
+      for (int e = 0; e < 8; ++e) if (c + e >= g.cols) x.v[e] = 0.f;
+    }
+  } else if constexpr (FROM == FROM_F32) {
+    x = load8(static_cast<const float *>(g.x) + row * g.ldx, c, g.cols, g.vec);
+  } else {
+    x = load8(static_cast<const uint16_t *>(g.x) + row * g.ldx, c, g.cols, g.vec);
+  }
+  uint16_t q[8][PLANES];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) bf16_planes_of<PLANES>(x.v[e], q[e]);
+#pragma unroll
+  for (int t = 0; t < PLANES; ++t) {
+    uint4 w;
+    w.x = q[0][t] | (uint32_t)q[1][t] << 16; w.y = q[2][t] | (uint32_t)q[3][t] << 16;
+    w.z = q[4][t] | (uint32_t)q[5][t] << 16; w.w = q[6][t] | (uint32_t)q[7][t] << 16;
+    *reinterpret_cast<uint4 *>(g.out + t * g.plane + row * g.ld + c) = w;
+  }
+}
+
+// out[j] = sum over rows of x[i][j], in an order that does not depend on the launch: workgroup (j / 256, part) sums its rows,
+// partial_sum_kernel the parts.
+template <typename T> __global__ __launch_bounds__(256) void column_sums_kernel(const T *x, int64_t ldx, int64_t rows, int32_t cols, int64_t per_part, float *out) {
+  const int j = blockIdx.x * 256 + threadIdx.x;
+  if (j >= cols) return;
+  const int64_t i0 = blockIdx.y * per_part, i1 = min(rows, i0 + per_part);
+  float s = 0.f;
+  for (int64_t i = i0; i < i1; ++i) {
+    if constexpr (sizeof(T) == 4) s += x[i * ldx + j]; else s += bf16_value(x[i * ldx + j]);
+  }
+  out[(int64_t)blockIdx.y * cols + j] = s;
+}
+// out[o][j] = sum over p < parts of in[o][p][j]
+__global__ __launch_bounds__(256) void partial_sum_kernel(const float *in, int32_t parts, int32_t cols, int64_t in_stride, int64_t part_stride, float *out, int64_t out_stride) {
+  const int j = blockIdx.x * 256 + threadIdx.x;
+  if (j >= cols) return;
+  const float *p = in + blockIdx.y * in_stride + j;
+  float s = 0.f;
+  for (int i = 0; i < parts; ++i) s += p[i * part_stride];
+  out[blockIdx.y * out_stride + j] = s;
+}
+
+}  // namespace shampoo

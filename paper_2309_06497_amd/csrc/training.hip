@@ -1,0 +1,580 @@
+// libshampoo, the operators of a training pass: argument checks, workspace layout, kernel launches and the extern "C"
+// boundary of their part of shampoo.h.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "../../include/shampoo.h"
+#include "checkpoint.h"
+#include "cross_entropy.h"
+#include "residual_norm.h"
+#include "train_gemm.h"
+#include "vectors.h"
+
+using namespace shampoo;
+
+namespace {
+
+constexpr size_t ALIGN = 256;
+constexpr int64_t MAX_ROWS = 0x7fffffff;
+constexpr int32_t MAX_FEATURES = 65536, MAX_OUT = 1 << 22, MAX_PACKED_COLS = 1 << 20, MAX_NORM_COLS = 16384;
+constexpr int64_t MAX_LD = 1 << 22;                        // of an operand as it lies: offsets inside a tile have 32 bits
+constexpr size_t LOGIT_BYTES = (size_t)4 << 30;            // scratch of a piece of the rows
+constexpr size_t PLANE_BYTES = (size_t)1 << 30;
+constexpr int64_t PIECE_ROWS = 256;                        // rows of a piece are a multiple of this
+
+inline size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
+inline int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+inline bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+inline bool dtype_ok(int32_t d) { return d == SHAMPOO_GRAD_F32 || d == SHAMPOO_GRAD_BF16; }
+inline int64_t size_of(int32_t d) { return d == SHAMPOO_GRAD_F32 ? 4 : 2; }
+// rows of `ld` elements from p on start on multiples of 16 bytes
+inline bool vec_ok(const void *p, int64_t ld, int32_t dtype) { return aligned(p, 16) && ld * size_of(dtype) % 16 == 0; }
+
+#define HIP_TRY(expr)                          \
+  do {                                         \
+    hipError_t e_ = (expr);                    \
+    if (e_ != hipSuccess) return SHAMPOO_ERR_HIP; \
+  } while (0)
+#define TRY(...)                               \
+  do {                                         \
+    const int rc_ = (__VA_ARGS__);             \
+    if (rc_ != SHAMPOO_OK) return rc_;         \
+  } while (0)
+
+// ---------------------------------------------------------------------------
+// Workspaces: arrays one behind the other
+// ---------------------------------------------------------------------------
+struct Arena {
+  unsigned char *base; size_t used = 0;
+  explicit Arena(void *p) : base(static_cast<unsigned char *>(p)) {}
+  template <typename T> T *take(size_t count) {
+    T *p = reinterpret_cast<T *>(base + used);
+    used += align_up(count * sizeof(T));
+    return p;
+  }
+};
+inline int workspace_ok(const void *p, size_t have, size_t want) {
+  return want > 0 && (!p || !aligned(p, ALIGN) || have < want) ? SHAMPOO_ERR_WORKSPACE : SHAMPOO_OK;
+}
+
+// ---------------------------------------------------------------------------
+// Elementwise launches
+// ---------------------------------------------------------------------------
+// Rows of `per_row` pieces each, at most 2^30 pieces in a launch.
+template <typename Launch> int by_rows(int64_t rows, uint32_t per_row, Launch &&launch) {
+  const int64_t at_once = std::max<int64_t>(1, ((int64_t)1 << 30) / per_row);
+  for (int64_t r = 0; r < rows; r += at_once) {
+    const uint32_t pieces = (uint32_t)(std::min(at_once, rows - r) * per_row);
+    launch(r, pieces, dim3((pieces + 255) / 256));
+    HIP_TRY(hipGetLastError());
+  }
+  return SHAMPOO_OK;
+}
+
+Packed packed_view(const void *p, int64_t rows, int32_t cols) {
+  Packed v;
+  v.rows = rows; v.cols = cols; v.pitch = (int32_t)round_up(cols, 32);
+  v.codes = static_cast<int8_t *>(const_cast<void *>(p));
+  v.exps = p ? reinterpret_cast<uint8_t *>(v.codes) + align_up((size_t)rows * v.pitch) : nullptr;
+  return v;
+}
+
+// bf16 planes of a matrix or of a(checkpoint)
+template <int FROM> int launch_planes(PlanesArgs g, int planes, int64_t rows, hipStream_t s) {
+  g.per_row = (uint32_t)(g.ld / 8);
+  return by_rows(rows, g.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
+    g.row0 = r; g.pieces = pieces;
+    switch (planes) {
+      case 1: planes_kernel<FROM, 1><<<grid, 256, 0, s>>>(g); break;
+      case 2: planes_kernel<FROM, 2><<<grid, 256, 0, s>>>(g); break;
+      default: planes_kernel<FROM, 3><<<grid, 256, 0, s>>>(g);
+    }
+  });
+}
+
+// out[o][j] = sum of `parts` rows of in
+int launch_partial_sums(const float *in, int32_t parts, int32_t cols, int32_t outputs, int64_t in_stride, int64_t part_stride, float *out,
+                        int64_t out_stride, hipStream_t s) {
+  for (int32_t o = 0; o < outputs; o += 65535) {
+    partial_sum_kernel<<<dim3((cols + 255) / 256, std::min(outputs - o, 65535)), 256, 0, s>>>(in + o * in_stride, parts, cols, in_stride, part_stride,
+                                                                                             out + o * out_stride, out_stride);
+    HIP_TRY(hipGetLastError());
+  }
+  return SHAMPOO_OK;
+}
+
+__global__ __launch_bounds__(256) void zero_rows_kernel(unsigned char *p, int64_t row_bytes, int64_t ld_bytes) {
+  for (int64_t j = blockIdx.x * 256 + threadIdx.x; j < row_bytes; j += (int64_t)gridDim.x * 256) p[(int64_t)blockIdx.y * ld_bytes + j] = 0;
+}
+// gradients of no rows at all
+int launch_zero(void *p, int64_t rows, int64_t cols, int64_t ld, int64_t elem, hipStream_t s) {
+  for (int64_t r = 0; r < rows; r += 65535) {
+    zero_rows_kernel<<<dim3((unsigned)std::min<int64_t>(1024, (cols * elem + 255) / 256), (unsigned)std::min<int64_t>(65535, rows - r)), 256, 0, s>>>(
+        static_cast<unsigned char *>(p) + r * ld * elem, cols * elem, ld * elem);
+    HIP_TRY(hipGetLastError());
+  }
+  return SHAMPOO_OK;
+}
+
+// ---------------------------------------------------------------------------
+// Matrix products
+// ---------------------------------------------------------------------------
+struct Operand {
+  const uint16_t *p; int64_t ld, plane; int planes, lie;
+};
+struct Result {
+  void *c; int64_t ldc; int store; const float *add; int64_t ldadd;
+};
+
+// the pairs of planes that a product needs, smallest first: of terms of 8 bits each, those that reach 24 bits
+int plane_pairs(int na, int nb, uint32_t &pa, uint32_t &pb) {
+  int n = 0;
+  const int most = std::max(na, nb) - 1;
+  pa = pb = 0;
+  for (int sum = most; sum >= 0; --sum)
+    for (int a = std::min(sum, na - 1); a >= 0 && sum - a < nb; --a) { pa |= (uint32_t)a << (4 * n); pb |= (uint32_t)(sum - a) << (4 * n); ++n; }
+  return n;
+}
+
+int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const Result &c, hipStream_t s) {
+  TrainGemmArgs g;
+  g.a = a.p; g.b = b.p; g.lda = a.ld; g.ldb = b.ld; g.a_plane = a.plane; g.b_plane = b.plane;
+  g.M = (int32_t)M; g.N = (int32_t)N; g.K = (int32_t)K;
+  g.products = plane_pairs(a.planes, b.planes, g.plane_a, g.plane_b);
+  g.c = c.c; g.ldc = c.ldc; g.add = c.add; g.ldadd = c.ldadd; g.store = c.store;
+  const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
+  if (tiles > ((int64_t)1 << 23)) return SHAMPOO_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)tiles);
+  if (a.lie == LIE_K && b.lie == LIE_K) train_gemm_kernel<LIE_K, LIE_K><<<grid, 256, 0, s>>>(g);
+  else if (a.lie == LIE_K) train_gemm_kernel<LIE_K, LIE_ROWS><<<grid, 256, 0, s>>>(g);
+  else train_gemm_kernel<LIE_ROWS, LIE_ROWS><<<grid, 256, 0, s>>>(g);
+  HIP_TRY(hipGetLastError());
+  return SHAMPOO_OK;
+}
+
+// A matrix of the caller as an operand: as it lies, or as planes in scratch (float32; rows that the products cannot read 16 bytes at
+// a time without passing their end).
+inline bool lies_well(int32_t dtype, int64_t cols, int64_t ld) { return dtype == SHAMPOO_GRAD_BF16 && cols % 8 == 0 && ld % 8 == 0 && ld <= MAX_LD; }
+struct Source {
+  int32_t dtype; int64_t rows, cols, ld;
+  bool copy() const { return !lies_well(dtype, cols, ld); }
+  int planes() const { return dtype == SHAMPOO_GRAD_F32 ? 3 : 1; }
+  int64_t ldp() const { return round_up(cols, 64); }
+  uint16_t *take(Arena &a) const { return copy() ? a.take<uint16_t>((size_t)planes() * rows * ldp()) : nullptr; }
+  int operand(const void *p, uint16_t *scratch, int lie, Operand &o, hipStream_t s) const {
+    if (!copy()) { o = {static_cast<const uint16_t *>(p), ld, 0, 1, lie}; return SHAMPOO_OK; }
+    o = {scratch, ldp(), rows * ldp(), planes(), lie};
+    PlanesArgs g = {};
+    g.x = p; g.ldx = ld; g.out = scratch; g.plane = o.plane; g.ld = o.ld; g.cols = (int32_t)cols; g.vec = vec_ok(p, ld, dtype);
+    return dtype == SHAMPOO_GRAD_F32 ? launch_planes<FROM_F32>(g, 3, rows, s) : launch_planes<FROM_BF16>(g, 1, rows, s);
+  }
+};
+
+// ---------------------------------------------------------------------------
+// Cross entropy
+// ---------------------------------------------------------------------------
+struct CrossEntropyPlan {
+  Source x, w;
+  int planes = 1;            // of g
+  int64_t ldz = 0, piece = 0, pieces = 0, ranges = 1, range_rows = 1;
+  bool sum = false;          // bf16 dw of several pieces: summed in scratch
+  size_t bytes = 0;
+  uint16_t *xp, *wp, *g;
+  float *z, *lse, *coef, *acc, *sums, *db;
+};
+int cross_entropy_plan(const shampoo_cross_entropy &c, void *workspace, CrossEntropyPlan &p) {
+  if (c.rows < 0 || c.features < 1 || c.classes < 1) return SHAMPOO_ERR_SHAPE;
+  if (c.rows > MAX_ROWS || c.features > MAX_FEATURES || c.classes > MAX_OUT) return SHAMPOO_ERR_UNSUPPORTED;
+  if (!dtype_ok(c.dtype) || !dtype_ok(c.grad_dtype) || (c.w_layout != SHAMPOO_OUT_IN && c.w_layout != SHAMPOO_IN_OUT)) return SHAMPOO_ERR_HYPER;
+  if (c.gradients && c.dtype == SHAMPOO_GRAD_F32 && c.grad_dtype != SHAMPOO_GRAD_F32) return SHAMPOO_ERR_HYPER;
+  const bool out_in = c.w_layout == SHAMPOO_OUT_IN;
+  const int64_t wcols = out_in ? c.features : c.classes;
+  if (c.ldx < c.features || c.ldw < wcols || (c.gradients && (c.lddx < c.features || c.lddw < wcols))) return SHAMPOO_ERR_SHAPE;
+  p.x = {c.dtype, c.rows, c.features, c.ldx};
+  p.w = {c.dtype, out_in ? c.classes : c.features, wcols, c.ldw};
+  p.planes = c.dtype == SHAMPOO_GRAD_F32 ? 3 : c.grad_dtype == SHAMPOO_GRAD_F32 ? 2 : 1;
+  p.ldz = round_up(c.classes, 64);
+  const size_t per_row = (size_t)p.ldz * (4 + (c.gradients ? 2 * p.planes : 0));
+  p.piece = std::min<int64_t>(round_up(std::max<int64_t>(c.rows, 1), PIECE_ROWS),
+                              std::max<int64_t>(PIECE_ROWS, (int64_t)(LOGIT_BYTES / per_row) / PIECE_ROWS * PIECE_ROWS));
+  p.pieces = (c.rows + p.piece - 1) / p.piece;
+  p.sum = c.gradients && p.pieces > 1 && c.grad_dtype == SHAMPOO_GRAD_BF16;
+  p.range_rows = 64;
+  p.ranges = p.piece / p.range_rows;
+  Arena a(workspace);
+  p.xp = p.x.take(a); p.wp = p.w.take(a);
+  p.z = a.take<float>((size_t)p.piece * p.ldz);
+  p.lse = a.take<float>(p.piece); p.coef = a.take<float>(p.piece);
+  if (c.gradients) {
+    p.g = a.take<uint16_t>((size_t)p.planes * p.piece * p.ldz);
+    if (p.sum) p.acc = a.take<float>((size_t)p.w.rows * p.w.cols);
+    if (c.has_bias) { p.sums = a.take<float>((size_t)p.ranges * c.classes * p.pieces); }
+  }
+  p.bytes = a.used;
+  return SHAMPOO_OK;
+}
+
+// ---------------------------------------------------------------------------
+// Weight gradient from a checkpoint
+// ---------------------------------------------------------------------------
+struct WeightGradPlan {
+  Source dy;
+  int planes = 1;            // of a(x)
+  int64_t ldp = 0, piece = 0, pieces = 0, parts = 1, part_rows = 1;
+  bool sum = false;
+  size_t bytes = 0;
+  uint16_t *xp, *dyp;
+  float *acc, *sums;
+};
+int weight_grad_plan(int64_t rows, int32_t in, int32_t out, int32_t activation, int32_t dtype, int64_t lddy, int32_t grad_dtype, bool bias,
+                     void *workspace, WeightGradPlan &p) {
+  if (rows < 0 || in < 1 || out < 1 || lddy < out) return SHAMPOO_ERR_SHAPE;
+  if (rows > MAX_ROWS || in > MAX_FEATURES || out > MAX_OUT) return SHAMPOO_ERR_UNSUPPORTED;
+  if (!dtype_ok(dtype) || !dtype_ok(grad_dtype) || activation < ACT_NONE || activation > ACT_SILU) return SHAMPOO_ERR_HYPER;
+  if (dtype == SHAMPOO_GRAD_F32 && grad_dtype != SHAMPOO_GRAD_F32) return SHAMPOO_ERR_HYPER;
+  p.dy = {dtype, rows, out, lddy};
+  p.planes = activation == ACT_NONE ? 1 : dtype == SHAMPOO_GRAD_F32 ? 3 : grad_dtype == SHAMPOO_GRAD_F32 ? 2 : 1;
+  p.ldp = round_up(in, 64);
+  p.piece = std::min<int64_t>(round_up(std::max<int64_t>(rows, 1), PIECE_ROWS),
+                              std::max<int64_t>(PIECE_ROWS, (int64_t)(PLANE_BYTES / ((size_t)p.ldp * 2 * p.planes)) / PIECE_ROWS * PIECE_ROWS));
+  p.pieces = (rows + p.piece - 1) / p.piece;
+  p.sum = p.pieces > 1 && grad_dtype == SHAMPOO_GRAD_BF16;
+  p.part_rows = std::max<int64_t>(64, (rows + 255) / 256);
+  p.parts = std::max<int64_t>(1, (rows + p.part_rows - 1) / p.part_rows);
+  Arena a(workspace);
+  p.xp = a.take<uint16_t>((size_t)p.planes * p.piece * p.ldp);
+  p.dyp = p.dy.take(a);
+  if (p.sum) p.acc = a.take<float>((size_t)in * out);
+  if (bias) p.sums = a.take<float>((size_t)p.parts * out);
+  p.bytes = a.used;
+  return SHAMPOO_OK;
+}
+
+// where the sum over pieces of a weight gradient goes: float32 ones add up in place, bf16 ones in scratch until the last
+Result piece_result(void *dw, int64_t lddw, int32_t grad_dtype, float *acc, int64_t cols, bool first, bool last) {
+  if (grad_dtype == SHAMPOO_GRAD_F32) return {dw, lddw, STORE_F32, first ? nullptr : static_cast<const float *>(dw), lddw};
+  if (last) return {dw, lddw, STORE_BF16, first ? nullptr : acc, cols};
+  return {acc, cols, STORE_F32, first ? nullptr : acc, cols};
+}
+
+// ---------------------------------------------------------------------------
+// Residual norm
+// ---------------------------------------------------------------------------
+constexpr int64_t NORM_CHUNKS = 1024;                      // workgroups of the backward pass
+int residual_norm_ok(const shampoo_residual_norm &c) {
+  if (c.rows < 0 || c.cols < 1 || c.gates < 0) return SHAMPOO_ERR_SHAPE;
+  if (c.rows > MAX_ROWS || c.cols > MAX_NORM_COLS) return SHAMPOO_ERR_UNSUPPORTED;
+  if (c.gates > 0 && c.rows % c.gates != 0) return SHAMPOO_ERR_SHAPE;
+  if (!dtype_ok(c.dtype) || c.post < NORM_NONE || c.post > NORM_LAYER || c.pre < NORM_NONE || c.pre > NORM_LAYER) return SHAMPOO_ERR_HYPER;
+  if (!(c.epsilon >= 0.f) || !std::isfinite(c.epsilon) || !std::isfinite(c.scale)) return SHAMPOO_ERR_HYPER;
+  if ((c.post != NORM_NONE && !c.w_post) || (c.pre != NORM_NONE && !c.w_pre) || (c.gates > 0 && !c.gate)) return SHAMPOO_ERR_NULL;
+  return SHAMPOO_OK;
+}
+ResidualNormArgs residual_norm_args(const shampoo_residual_norm &c) {
+  ResidualNormArgs g = {};
+  g.w_post = c.w_post; g.b_post = c.post == NORM_LAYER ? c.b_post : nullptr;
+  g.w_pre = c.w_pre; g.b_pre = c.pre == NORM_LAYER ? c.b_pre : nullptr;
+  g.gate = c.gates > 0 ? c.gate : nullptr;
+  g.rows = c.rows; g.cols = c.cols; g.post = c.post; g.pre = c.pre; g.epsilon = c.epsilon; g.alpha = c.scale;
+  g.group_rows = c.gates > 0 ? c.rows / c.gates : c.rows;
+  return g;
+}
+struct NormChunks { int64_t rows, chunks; int32_t per_group; };
+// A workgroup of the backward pass has rows of one group, or several whole groups where there are more than workgroups.
+NormChunks norm_chunks(const shampoo_residual_norm &c) {
+  const int64_t groups = std::max<int64_t>(1, c.gates), group_rows = c.rows / groups;
+  if (groups >= NORM_CHUNKS) {
+    const int64_t each = (groups + NORM_CHUNKS - 1) / NORM_CHUNKS;
+    return {each * group_rows, (groups + each - 1) / each, 0};
+  }
+  const int64_t want = std::max<int64_t>(1, std::min(NORM_CHUNKS / groups, group_rows));
+  const int64_t rows = std::max<int64_t>(1, (group_rows + want - 1) / want), per = std::max<int64_t>(1, (group_rows + rows - 1) / rows);
+  return {rows, per * groups, (int32_t)per};
+}
+
+template <typename T> int launch_norm_forward(const ResidualNormArgs &g, hipStream_t s) {
+#define FORWARD(TPR, NJ) residual_norm_forward_kernel<T, TPR, NJ><<<dim3((unsigned)((g.rows + 256 / TPR - 1) / (256 / TPR))), 256, 0, s>>>(g)
+  if (g.cols <= 512) FORWARD(64, 1);
+  else if (g.cols <= 1024) FORWARD(64, 2);
+  else if (g.cols <= 2048) FORWARD(64, 4);
+  else if (g.cols <= 4096) FORWARD(256, 2);
+  else if (g.cols <= 8192) FORWARD(256, 4);
+  else FORWARD(256, 8);
+#undef FORWARD
+  HIP_TRY(hipGetLastError());
+  return SHAMPOO_OK;
+}
+template <typename T, bool PACKED> int launch_norm_backward(const ResidualNormArgs &g, int64_t chunks, hipStream_t s) {
+  const dim3 grid((unsigned)chunks);
+  if (g.cols <= 2048) residual_norm_backward_kernel<T, PACKED, 1><<<grid, 256, 0, s>>>(g);
+  else if (g.cols <= 4096) residual_norm_backward_kernel<T, PACKED, 2><<<grid, 256, 0, s>>>(g);
+  else if (g.cols <= 8192) residual_norm_backward_kernel<T, PACKED, 4><<<grid, 256, 0, s>>>(g);
+  else residual_norm_backward_kernel<T, PACKED, 8><<<grid, 256, 0, s>>>(g);
+  HIP_TRY(hipGetLastError());
+  return SHAMPOO_OK;
+}
+
+int checkpoint_ok(int64_t rows, int32_t cols, const void *packed, size_t bytes) {
+  if (rows < 0 || cols < 1) return SHAMPOO_ERR_SHAPE;
+  if (rows > MAX_ROWS || cols > MAX_PACKED_COLS) return SHAMPOO_ERR_UNSUPPORTED;
+  return workspace_ok(packed, bytes, shampoo_checkpoint_bytes(rows, cols));
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------------------
+// extern "C" boundary
+// ---------------------------------------------------------------------------
+extern "C" {
+
+size_t shampoo_linear_cross_entropy_workspace_bytes(const shampoo_cross_entropy *c) {
+  CrossEntropyPlan p;
+  return c && cross_entropy_plan(*c, nullptr, p) == SHAMPOO_OK ? p.bytes : 0;
+}
+
+int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, const void *w, const float *bias, const int64_t *targets,
+                                 const float *weight, float scale, float *loss, void *dx, void *dw, float *dbias, void *workspace,
+                                 size_t workspace_bytes, void *stream) {
+  if (!c) return SHAMPOO_ERR_NULL;
+  CrossEntropyPlan p;
+  TRY(cross_entropy_plan(*c, workspace, p));
+  if (!w || (c->rows > 0 && (!x || !targets || !loss)) || (c->has_bias && !bias)) return SHAMPOO_ERR_NULL;
+  if (!std::isfinite(scale)) return SHAMPOO_ERR_HYPER;
+  if (!aligned(x, 16) || !aligned(w, 16)) return SHAMPOO_ERR_UNSUPPORTED;
+  TRY(workspace_ok(workspace, workspace_bytes, p.bytes));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int64_t d = c->features, v = c->classes;
+  const bool out_in = c->w_layout == SHAMPOO_OUT_IN;
+  if (!c->gradients) { dx = dw = nullptr; dbias = nullptr; }
+  if (!c->has_bias) { bias = nullptr; dbias = nullptr; }
+  if (c->rows == 0) {
+    if (dw) TRY(launch_zero(dw, p.w.rows, p.w.cols, c->lddw, size_of(c->grad_dtype), s));
+    if (dbias) TRY(launch_zero(dbias, 1, v, v, 4, s));
+    return SHAMPOO_OK;
+  }
+  Operand xo, wo;
+  TRY(p.x.operand(x, p.xp, LIE_K, xo, s));
+  TRY(p.w.operand(w, p.wp, out_in ? LIE_K : LIE_ROWS, wo, s));
+  for (int64_t k = 0; k < p.pieces; ++k) {
+    const int64_t i0 = k * p.piece, n = std::min(p.piece, c->rows - i0);
+    Operand xk = xo;
+    xk.p += i0 * xo.ld;
+    TRY(gemm(xk, wo, n, v, d, {p.z, p.ldz, STORE_F32, nullptr, 0}, s));
+    RowLossArgs r = {p.z, p.ldz, bias, targets + i0, weight ? weight + i0 : nullptr, scale, p.lse, p.coef, loss + i0, (int32_t)v};
+    row_loss_kernel<<<dim3((unsigned)n), 256, 0, s>>>(r);
+    HIP_TRY(hipGetLastError());
+    if (!c->gradients) continue;
+    const int64_t ranges = (n + p.range_rows - 1) / p.range_rows;
+    SoftmaxGradArgs q = {p.z, p.ldz, p.lse, p.coef, targets + i0, p.g, p.piece * p.ldz, p.ldz, dbias ? p.sums + k * p.ranges * v : nullptr,
+                         (int32_t)n, (int32_t)v, (int32_t)p.range_rows};
+    const dim3 grid((unsigned)((p.ldz / 8 + 255) / 256), (unsigned)ranges);
+    switch (p.planes) {
+      case 1: softmax_grad_kernel<1><<<grid, 256, 0, s>>>(q); break;
+      case 2: softmax_grad_kernel<2><<<grid, 256, 0, s>>>(q); break;
+      default: softmax_grad_kernel<3><<<grid, 256, 0, s>>>(q);
+    }
+    HIP_TRY(hipGetLastError());
+    if (dx) {
+      const Operand go = {p.g, p.ldz, p.piece * p.ldz, c->dtype == SHAMPOO_GRAD_BF16 ? 1 : p.planes, LIE_K};
+      Operand wt = wo;
+      wt.lie = out_in ? LIE_ROWS : LIE_K;
+      TRY(gemm(go, wt, n, d, v, {static_cast<char *>(dx) + i0 * c->lddx * size_of(c->dtype), c->lddx, c->dtype == SHAMPOO_GRAD_F32 ? STORE_F32 : STORE_BF16, nullptr, 0}, s));
+    }
+    if (dw) {
+      const Operand gt = {p.g, p.ldz, p.piece * p.ldz, p.planes, LIE_ROWS};
+      xk.lie = LIE_ROWS;
+      const Result out = piece_result(dw, c->lddw, c->grad_dtype, p.acc, p.w.cols, k == 0, k == p.pieces - 1);
+      TRY(out_in ? gemm(gt, xk, v, d, n, out, s) : gemm(xk, gt, d, v, n, out, s));
+    }
+  }
+  if (dbias) {
+    const int64_t last = c->rows - (p.pieces - 1) * p.piece, parts = (p.pieces - 1) * p.ranges + (last + p.range_rows - 1) / p.range_rows;
+    TRY(launch_partial_sums(p.sums, (int32_t)parts, (int32_t)v, 1, 0, v, dbias, v, s));
+  }
+  return SHAMPOO_OK;
+}
+
+size_t shampoo_checkpoint_bytes(int64_t rows, int32_t cols) {
+  if (rows < 0 || rows > MAX_ROWS || cols < 1 || cols > MAX_PACKED_COLS) return 0;
+  const size_t pitch = (size_t)round_up(cols, 32);
+  return align_up((size_t)rows * pitch) + align_up((size_t)rows * (pitch / 32));
+}
+
+int shampoo_checkpoint_pack(const void *x, int32_t dtype, int64_t rows, int32_t cols, int64_t ldx, void *packed, size_t packed_bytes,
+                            void *stream) {
+  if (rows > 0 && (!x || !packed)) return SHAMPOO_ERR_NULL;
+  if (!dtype_ok(dtype)) return SHAMPOO_ERR_HYPER;
+  TRY(checkpoint_ok(rows, cols, packed, packed_bytes));
+  if (ldx < cols) return SHAMPOO_ERR_SHAPE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  PackArgs g = {};
+  g.x = x; g.ldx = ldx; g.p = packed_view(packed, rows, cols); g.vec = vec_ok(x, ldx, dtype);
+  g.per_row = (uint32_t)g.p.pitch / 8;
+  return by_rows(rows, g.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
+    g.row0 = r; g.pieces = pieces;
+    if (dtype == SHAMPOO_GRAD_F32) checkpoint_pack_kernel<float><<<grid, 256, 0, s>>>(g);
+    else checkpoint_pack_kernel<uint16_t><<<grid, 256, 0, s>>>(g);
+  });
+}
+
+int shampoo_checkpoint_unpack(const void *packed, size_t packed_bytes, int64_t rows, int32_t cols, int32_t activation, void *y, int32_t dtype,
+                              int64_t ldy, void *stream) {
+  if (rows > 0 && (!packed || !y)) return SHAMPOO_ERR_NULL;
+  if (!dtype_ok(dtype) || activation < ACT_NONE || activation > ACT_SILU) return SHAMPOO_ERR_HYPER;
+  TRY(checkpoint_ok(rows, cols, packed, packed_bytes));
+  if (ldy < cols) return SHAMPOO_ERR_SHAPE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  UnpackArgs g = {};
+  g.p = packed_view(packed, rows, cols); g.y = y; g.ldy = ldy; g.activation = activation; g.vec = vec_ok(y, ldy, dtype);
+  g.per_row = (uint32_t)g.p.pitch / 8;
+  return by_rows(rows, g.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
+    g.row0 = r; g.pieces = pieces;
+    if (dtype == SHAMPOO_GRAD_F32) checkpoint_unpack_kernel<float, false><<<grid, 256, 0, s>>>(g);
+    else checkpoint_unpack_kernel<uint16_t, false><<<grid, 256, 0, s>>>(g);
+  });
+}
+
+int shampoo_checkpoint_activation_grad(const void *packed, size_t packed_bytes, int64_t rows, int32_t cols, int32_t activation, const void *dy,
+                                       int32_t dtype, int64_t lddy, void *dx, int64_t lddx, void *stream) {
+  if (rows > 0 && (!packed || !dy || !dx)) return SHAMPOO_ERR_NULL;
+  if (!dtype_ok(dtype) || activation < ACT_NONE || activation > ACT_SILU) return SHAMPOO_ERR_HYPER;
+  TRY(checkpoint_ok(rows, cols, packed, packed_bytes));
+  if (lddy < cols || lddx < cols) return SHAMPOO_ERR_SHAPE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  UnpackArgs g = {};
+  g.p = packed_view(packed, rows, cols); g.dy = dy; g.lddy = lddy; g.y = dx; g.ldy = lddx; g.activation = activation;
+  g.vec = vec_ok(dy, lddy, dtype) && vec_ok(dx, lddx, dtype);
+  g.per_row = (uint32_t)g.p.pitch / 8;
+  return by_rows(rows, g.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
+    g.row0 = r; g.pieces = pieces;
+    if (dtype == SHAMPOO_GRAD_F32) checkpoint_unpack_kernel<float, true><<<grid, 256, 0, s>>>(g);
+    else checkpoint_unpack_kernel<uint16_t, true><<<grid, 256, 0, s>>>(g);
+  });
+}
+
+size_t shampoo_checkpoint_weight_grad_workspace_bytes(int64_t rows, int32_t in, int32_t out, int32_t activation, int32_t dtype, int64_t lddy,
+                                                      int32_t grad_dtype, int32_t want_bias) {
+  WeightGradPlan p;
+  return weight_grad_plan(rows, in, out, activation, dtype, lddy, grad_dtype, want_bias != 0, nullptr, p) == SHAMPOO_OK ? p.bytes : 0;
+}
+
+int shampoo_checkpoint_weight_grad(const void *packed, size_t packed_bytes, int64_t rows, int32_t in, int32_t activation, const void *dy,
+                                   int32_t dtype, int32_t out, int64_t lddy, void *dw, int32_t grad_dtype, int32_t w_layout, int64_t lddw,
+                                   float *db, void *workspace, size_t workspace_bytes, void *stream) {
+  if ((rows > 0 && (!packed || !dy)) || !dw) return SHAMPOO_ERR_NULL;
+  WeightGradPlan p;
+  TRY(weight_grad_plan(rows, in, out, activation, dtype, lddy, grad_dtype, db != nullptr, workspace, p));
+  if (w_layout != SHAMPOO_OUT_IN && w_layout != SHAMPOO_IN_OUT) return SHAMPOO_ERR_HYPER;
+  const bool out_in = w_layout == SHAMPOO_OUT_IN;
+  if (lddw < (out_in ? in : out)) return SHAMPOO_ERR_SHAPE;
+  if (!aligned(dy, 16)) return SHAMPOO_ERR_UNSUPPORTED;
+  TRY(checkpoint_ok(rows, in, packed, packed_bytes));
+  TRY(workspace_ok(workspace, workspace_bytes, p.bytes));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (rows == 0) {
+    TRY(launch_zero(dw, out_in ? out : in, out_in ? in : out, lddw, size_of(grad_dtype), s));
+    if (db) TRY(launch_zero(db, 1, out, out, 4, s));
+    return SHAMPOO_OK;
+  }
+  Operand dyo;
+  TRY(p.dy.operand(dy, p.dyp, LIE_ROWS, dyo, s));
+  PlanesArgs g = {};
+  g.out = p.xp; g.ld = p.ldp; g.cols = in; g.activation = activation;
+  for (int64_t k = 0; k < p.pieces; ++k) {
+    const int64_t i0 = k * p.piece, n = std::min(p.piece, rows - i0);
+    const Operand xo = {p.xp, p.ldp, p.piece * p.ldp, p.planes, LIE_ROWS};
+    Operand dk = dyo;
+    dk.p += i0 * dyo.ld;
+    g.p = packed_view(packed, rows, in);
+    g.p.codes += i0 * g.p.pitch; g.p.exps += i0 * (g.p.pitch / 32);
+    g.plane = xo.plane;
+    TRY(launch_planes<FROM_PACKED>(g, p.planes, n, s));
+    const Result r = piece_result(dw, lddw, grad_dtype, p.acc, out_in ? in : out, k == 0, k == p.pieces - 1);
+    TRY(out_in ? gemm(dk, xo, out, in, n, r, s) : gemm(xo, dk, in, out, n, r, s));
+  }
+  if (db) {
+    const dim3 grid((out + 255) / 256, (unsigned)p.parts);
+    if (dtype == SHAMPOO_GRAD_F32) column_sums_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float *>(dy), lddy, rows, out, p.part_rows, p.sums);
+    else column_sums_kernel<uint16_t><<<grid, 256, 0, s>>>(static_cast<const uint16_t *>(dy), lddy, rows, out, p.part_rows, p.sums);
+    HIP_TRY(hipGetLastError());
+    TRY(launch_partial_sums(p.sums, (int32_t)p.parts, out, 1, 0, out, db, out, s));
+  }
+  return SHAMPOO_OK;
+}
+
+int shampoo_residual_norm_forward(const shampoo_residual_norm *c, const void *r, int64_t ldr, const void *f, int64_t ldf, void *r_out,
+                                  int64_t ld_r_out, void *h, int64_t ldh, void *packed_r, void *packed_f, size_t packed_bytes, void *stream) {
+  if (!c) return SHAMPOO_ERR_NULL;
+  TRY(residual_norm_ok(*c));
+  if (c->rows == 0) return SHAMPOO_OK;
+  if (!r || !f || !r_out || (c->pre != NORM_NONE && !h) || !packed_r != !packed_f) return SHAMPOO_ERR_NULL;
+  if (ldr < c->cols || ldf < c->cols || ld_r_out < c->cols || (c->pre != NORM_NONE && ldh < c->cols)) return SHAMPOO_ERR_SHAPE;
+  if (packed_r) {
+    TRY(checkpoint_ok(c->rows, c->cols, packed_r, packed_bytes));
+    TRY(checkpoint_ok(c->rows, c->cols, packed_f, packed_bytes));
+  }
+  ResidualNormArgs g = residual_norm_args(*c);
+  g.r = r; g.ldr = ldr; g.f = f; g.ldf = ldf; g.r_out = r_out; g.ld_r_out = ld_r_out; g.h = h; g.ldh = ldh;
+  g.r8 = packed_view(packed_r, c->rows, c->cols); g.f8 = packed_view(packed_f, c->rows, c->cols);
+  g.vec = vec_ok(r, ldr, c->dtype) && vec_ok(f, ldf, c->dtype) && vec_ok(r_out, ld_r_out, c->dtype) && (c->pre == NORM_NONE || vec_ok(h, ldh, c->dtype));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return c->dtype == SHAMPOO_GRAD_F32 ? launch_norm_forward<float>(g, s) : launch_norm_forward<uint16_t>(g, s);
+}
+
+size_t shampoo_residual_norm_backward_workspace_bytes(const shampoo_residual_norm *c) {
+  if (!c || residual_norm_ok(*c) != SHAMPOO_OK) return 0;
+  return align_up((size_t)norm_chunks(*c).chunks * 5 * c->cols * sizeof(float));
+}
+
+int shampoo_residual_norm_backward(const shampoo_residual_norm *c, int32_t packed, const void *r, int64_t ldr, const void *f, int64_t ldf,
+                                   const void *dr_out, int64_t ld_dr_out, const void *dh, int64_t ld_dh, void *dr, int64_t ld_dr, void *df,
+                                   int64_t ld_df, float *dgate, float *dw_post, float *db_post, float *dw_pre, float *db_pre, void *workspace,
+                                   size_t workspace_bytes, void *stream) {
+  if (!c) return SHAMPOO_ERR_NULL;
+  TRY(residual_norm_ok(*c));
+  if (c->gates == 0) dgate = nullptr;
+  if (c->post == NORM_NONE) dw_post = nullptr;
+  if (c->post != NORM_LAYER) db_post = nullptr;
+  if (c->pre == NORM_NONE) { dw_pre = nullptr; dh = nullptr; }
+  if (c->pre != NORM_LAYER) db_pre = nullptr;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int32_t cols = c->cols;
+  if (c->rows == 0) {
+    if (dgate) TRY(launch_zero(dgate, c->gates, cols, cols, 4, s));
+    for (float *p : {dw_post, db_post, dw_pre, db_pre})
+      if (p) TRY(launch_zero(p, 1, cols, cols, 4, s));
+    return SHAMPOO_OK;
+  }
+  if (!r || !f || !dr || !df || (c->pre != NORM_NONE && !dh)) return SHAMPOO_ERR_NULL;
+  if ((!packed && (ldr < cols || ldf < cols)) || (dr_out && ld_dr_out < cols) || (dh && ld_dh < cols) || ld_dr < cols || ld_df < cols)
+    return SHAMPOO_ERR_SHAPE;
+  if (packed && (!aligned(r, ALIGN) || !aligned(f, ALIGN))) return SHAMPOO_ERR_WORKSPACE;
+  const NormChunks k = norm_chunks(*c);
+  TRY(workspace_ok(workspace, workspace_bytes, shampoo_residual_norm_backward_workspace_bytes(c)));
+  ResidualNormArgs g = residual_norm_args(*c);
+  g.vec = vec_ok(dr, ld_dr, c->dtype) && vec_ok(df, ld_df, c->dtype) && (!dr_out || vec_ok(dr_out, ld_dr_out, c->dtype)) &&
+          (!dh || vec_ok(dh, ld_dh, c->dtype)) && (packed || (vec_ok(r, ldr, c->dtype) && vec_ok(f, ldf, c->dtype)));
+  g.r = r; g.f = f; g.ldr = ldr; g.ldf = ldf;
+  if (packed) { g.r8 = packed_view(r, c->rows, cols); g.f8 = packed_view(f, c->rows, cols); }
+  g.dr_out = dr_out; g.ld_dr_out = ld_dr_out; g.dh = dh; g.ld_dh = ld_dh; g.dr = dr; g.ld_dr = ld_dr; g.df = df; g.ld_df = ld_df;
+  g.dgate = k.per_group ? nullptr : dgate;
+  g.partial = static_cast<float *>(workspace);
+  g.chunk_rows = k.rows; g.chunks_per_group = k.per_group;
+  if (c->dtype == SHAMPOO_GRAD_F32) {
+    TRY(packed ? launch_norm_backward<float, true>(g, k.chunks, s) : launch_norm_backward<float, false>(g, k.chunks, s));
+  } else {
+    TRY(packed ? launch_norm_backward<uint16_t, true>(g, k.chunks, s) : launch_norm_backward<uint16_t, false>(g, k.chunks, s));
+  }
+  const int64_t stride = 5 * (int64_t)cols;
+  if (dgate && k.per_group)
+    TRY(launch_partial_sums(g.partial, k.per_group, cols, (int32_t)c->gates, k.per_group * stride, stride, dgate, cols, s));
+  float *outs[4] = {dw_post, db_post, dw_pre, db_pre};
+  for (int q = 0; q < 4; ++q)
+    if (outs[q]) TRY(launch_partial_sums(g.partial + (q + 1) * cols, (int32_t)k.chunks, cols, 1, 0, stride, outs[q], cols, s));
+  return SHAMPOO_OK;
+}
+
+}  // extern "C"
