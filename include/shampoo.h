@@ -399,8 +399,8 @@ typedef struct {
   int32_t features;       /* 1 ... 65536                                                       */
   int32_t classes;        /* 1 ... 4194304                                                     */
   int32_t dtype;          /* of x, w and dx.  bf16: z from exact products; g is rounded to bf16 for the products of dx
-                             and bf16 dw, to 16 bits for those of float32 dw.  float32: all products to float32 accuracy
-                             (three bf16 terms per value, six products)                       */
+                             and bf16 dw, and has float32 accuracy (three bf16 terms) for float32 dw.  float32: all
+                             products to float32 accuracy (three terms per value, six products) */
   int32_t grad_dtype;     /* of dw; float32 x: float32                                         */
   int32_t w_layout;       /* of w and dw: SHAMPOO_OUT_IN [classes][features], SHAMPOO_IN_OUT [features][classes] */
   int32_t has_bias;       /* != 0: bias is given                                              */
@@ -441,7 +441,7 @@ int shampoo_checkpoint_activation_grad(const void *packed, size_t packed_bytes, 
  * Gradient of a linear layer y = a(x) W + b from the checkpoint of x [rows][in] and dy [rows][out]:
  *   dW = a(x)^T dy (SHAMPOO_IN_OUT; SHAMPOO_OUT_IN: transposed),  db = column sums of dy (float32; NULL: not wanted).
  * dtype: of dy (16-byte aligned, else SHAMPOO_ERR_UNSUPPORTED).  Float32 dy: products to float32 accuracy, dw float32.
- * bf16 dy: x and dy enter as they are; a(x), where an activation is given, rounded to bf16 for bf16 dw and to 16 bits for
+ * bf16 dy: x and dy enter as they are; a(x), where an activation is given, rounded to bf16 for bf16 dw, with float32 accuracy for
  * float32 dw.  in <= 65536, out <= 4194304.
  */
 size_t shampoo_checkpoint_weight_grad_workspace_bytes(int64_t rows, int32_t in, int32_t out, int32_t activation, int32_t dtype,

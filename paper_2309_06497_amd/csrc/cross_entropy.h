@@ -3,92 +3,105 @@
 //   lse_i = log sum_v exp z_iv        loss_i = lse_i - z_{i,t_i}        g_iv = c_i (exp(z_iv - lse_i) - [v = t_i])
 //   dx = g w        dw = g^T x        db = column sums of g
 //
-// c_i = scale weight_i, zero where the target is ignored.  Logits of a piece of the rows at a time lie in scratch.
+// c_i = scale weight_i, zero where the target is ignored.  The product that makes z (train_gemm.h) leaves, for every row
+// and span of 64 or 128 classes, the largest z and the sum of exp(z - largest), and of a piece of the rows
+//   bf16 x, bf16 dw, no bias: the distance of z from the largest of its span in 16 bits, steps of 2^-10 in the exponent of 2
+//     (2 bytes per logit; exp(z) is off by 3.4e-4 of itself at most where the rounding of g to bf16 is 3.9e-3; what is further than 64
+//     steps of 1 away, 5e-20 of the largest, counts as zero).  g takes its place.
+//   otherwise: z in float32, beside it g as the bf16 planes that float32 results need.
+// The three products are 6 rows features classes operations; what lies between them is bound by memory.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include "train_gemm.h"
 #include "vectors.h"
 
 namespace shampoo {
 
-// lse, loss and c of a row of float32 logits; a workgroup per row.  z += bias on the way.
+// lse, loss and c of every row from the largest logits and sums of its spans: 16 rows per workgroup, 16 threads a row.
 struct RowLossArgs {
-  float *z; int64_t ldz;
-  const float *bias; const int64_t *targets; const float *weight;
+  const float2 *stats; int64_t stats_ld;
+  const float *target_z; const int64_t *targets; const float *weight;
   float scale;
   float *lse, *coef, *loss;
-  int32_t classes;
+  int32_t rows, classes, spans;
 };
+// exp sums (m, s) and (n, t) together; s is 0 or NaN where m is -infinity
+__device__ __forceinline__ void join_exp(float &m, float &s, float n, float t) {
+  const float top = fmaxf(m, n);
+  const float a = m == -INFINITY ? s : s * __builtin_amdgcn_exp2f((m - top) * LOG2_E), b = n == -INFINITY ? t : t * __builtin_amdgcn_exp2f((n - top) * LOG2_E);
+  m = top; s = a + b;
+}
 __global__ __launch_bounds__(256) void row_loss_kernel(const RowLossArgs g) {
-  __shared__ float red[8];
-  const int64_t i = blockIdx.x;
-  float *z = g.z + i * g.ldz;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  float m = -INFINITY;
-  bool nan = false;
-  for (int v = tid; v < g.classes; v += 256) {
-    float x = z[v];
-    if (g.bias) { x += g.bias[v]; z[v] = x; }
-    nan |= x != x;
-    m = fmaxf(m, x);
-  }
-  if (nan) m = NAN;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) { const float y = __shfl_xor(m, o, 64); m = m != m || y != y ? NAN : fmaxf(m, y); }
-  if (lane == 0) red[wave] = m;
+  __shared__ float2 part[16][16];
+  const int r = threadIdx.x & 15, k = threadIdx.x >> 4, i = blockIdx.x * 16 + r;
+  float m = -INFINITY, s = 0.f;
+  if (i < g.rows)
+    for (int p = k; p < g.spans; p += 16) {
+      const float2 x = g.stats[p * g.stats_ld + i];
+      join_exp(m, s, x.x, x.y);
+    }
+  part[k][r] = make_float2(m, s);
   __syncthreads();
-#pragma unroll
-  for (int k = 0; k < 4; ++k) { const float y = red[k]; m = m != m || y != y ? NAN : fmaxf(m, y); }
-  float s = 0.f;
-  const float base = m == -INFINITY ? 0.f : m;
-  for (int v = tid; v < g.classes; v += 256) s += expf(z[v] - base);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-  if (lane == 0) red[4 + wave] = s;
-  __syncthreads();
-  if (tid != 0) return;
-  s = (red[4] + red[5]) + (red[6] + red[7]);
-  const float lse = base + logf(s);
+  if (k != 0 || i >= g.rows) return;
+  for (int p = 1; p < 16; ++p) join_exp(m, s, part[p][r].x, part[p][r].y);
+  const float lse = (m == -INFINITY ? 0.f : m) + logf(s);       // no class left: -infinity
   const int64_t t = g.targets[i];
   const bool valid = t >= 0 && t < g.classes;
   g.lse[i] = lse;
   g.coef[i] = valid ? g.scale * (g.weight ? g.weight[i] : 1.f) : 0.f;
-  const float zt = valid ? z[t] : 0.f;
+  const float zt = valid ? g.target_z[i] : 0.f;
   g.loss[i] = !valid ? 0.f : zt == -INFINITY ? INFINITY : lse - zt;
 }
 
-// g of a piece of the rows as PLANES bf16 planes [plane][rows][ldg] (ldg: classes rounded up, zeros there), and the column
-// sums of every range of rows for the bias.  A thread has eight columns of the rows of its range.
+// g of a piece of the rows, zeros from classes to ldg.  A thread has eight columns of the rows of its range.
 struct SoftmaxGradArgs {
-  const float *z; int64_t ldz;
+  const float *z; int64_t ldg;       // float32 logits
+  const float2 *stats; int64_t stats_ld; int32_t span;
   const float *lse, *coef; const int64_t *targets;
-  uint16_t *out; int64_t plane, ldg;
-  float *sums;                       // [ranges][classes], or nullptr
+  uint16_t *out; int64_t plane;      // [plane][rows][ldg]; 16-bit logits are read here
+  float *sums;                       // [ranges][classes] column sums of g, or nullptr
   int32_t rows, classes, per_range;
 };
+// PLANES = 0: one plane, in the place of 16-bit logits
 template <int PLANES> __global__ __launch_bounds__(256) void softmax_grad_kernel(const SoftmaxGradArgs g) {
+  constexpr int OUT = PLANES ? PLANES : 1;
   const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
   if (c >= g.ldg) return;
   const int i0 = blockIdx.y * g.per_range, i1 = min(g.rows, i0 + g.per_range);
   f32x8 sum = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
   for (int i = i0; i < i1; ++i) {
     const float lse = g.lse[i], k = g.coef[i];
-    const int64_t t = g.targets[i] - c;
-    const f32x8 z = load8(g.z + i * g.ldz, c, g.classes, true);
-    uint16_t q[8][PLANES];
+    const int64_t t = g.targets[i] - c, at = (int64_t)i * g.ldg + c;
+    f32x8 p;
+    if constexpr (PLANES == 0) {
+      const uint4 u = *reinterpret_cast<const uint4 *>(g.out + at);
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+      const float top = (g.stats[(int64_t)(c / g.span) * g.stats_ld + i].x - lse) * LOG2_E;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t q = (w[e >> 1] >> (16 * (e & 1))) & 0xffffu;
+        p.v[e] = q == 65535u ? 0.f : __builtin_amdgcn_exp2f(top - (float)q * (1.f / LOGIT_STEPS));
+      }
+    } else {
+      p = load8(g.z + at, 0, 8, true);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p.v[e] = expf(p.v[e] - lse);
+    }
+    uint16_t q[8][OUT];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       float x = 0.f;
-      if (k != 0.f && c + e < g.classes && lse != -INFINITY) x = k * (expf(z.v[e] - lse) - (t == e ? 1.f : 0.f));
+      if (k != 0.f && c + e < g.classes && lse != -INFINITY) x = k * (p.v[e] - (t == e ? 1.f : 0.f));
       sum.v[e] += x;
-      bf16_planes_of<PLANES>(x, q[e]);
+      bf16_planes_of<OUT>(x, q[e]);
     }
 #pragma unroll
-    for (int s = 0; s < PLANES; ++s) {
+    for (int s = 0; s < OUT; ++s) {
       uint4 w;
       w.x = q[0][s] | (uint32_t)q[1][s] << 16; w.y = q[2][s] | (uint32_t)q[3][s] << 16;
       w.z = q[4][s] | (uint32_t)q[5][s] << 16; w.w = q[6][s] | (uint32_t)q[7][s] << 16;
-      *reinterpret_cast<uint4 *>(g.out + s * g.plane + (int64_t)i * g.ldg + c) = w;
+      *reinterpret_cast<uint4 *>(g.out + s * g.plane + at) = w;
     }
   }
   if (!g.sums) return;

@@ -3,18 +3,36 @@
 //   C[m][n] = sum over pairs (s, t) of planes, sum over k: A_s(m, k) B_t(n, k)
 //
 // Operands are bf16 planes in memory: one for a bf16 matrix, up to three for a float32 one (x = h + l + m, 8 bits each), whose
-// products (s, t) are all that float32 accuracy needs, smallest first.  An operand lies along k (ptr[row * ld + k]) or along
-// rows (ptr[k * ld + row]).  Contract, which the host keeps: 16-byte aligned, ld % 8 == 0, the contiguous extent readable up to a
-// multiple of 8, and zero there where that extent is k.
+// products (s, t) are all that float32 accuracy needs, smallest first: one loop over k behind the other.  An operand lies along
+// k (ptr[row * ld + k]) or along rows (ptr[k * ld + row]).  Contract, which the host keeps: 16-byte aligned, ld % 8 == 0, the
+// contiguous extent readable up to a multiple of 8, and zero there where that extent is k.
+//
+// Tile of 64 TI x 64 TI per workgroup of four wavefronts, 32 TI x 32 TI each as TI x TI tiles of v_mfma_f32_32x32x16_bf16.  TI = 4:
+// 256 accumulator registers, one wavefront per SIMD; 8 KB of operands from LDS per 16 products of 32 cycles, half of what LDS
+// delivers (with 128 x 64 per wavefront it would be three quarters, and the loads into LDS take another quarter).  TI = 2 where that gives too
+// few workgroups.
+//
+// Slabs of 64 values of k go straight into LDS (global_load_lds_dwordx4), the next one in flight while one is multiplied.  Such a
+// load fills 1 KiB of consecutive LDS, so bank conflicts are kept away by which 16 bytes a lane asks for:
+//   along k:    LDS rows of 128 bytes; chunk c of row r at position c ^ (r / 2 % 8).  16 lanes that are served together read one
+//               chunk of 16 rows: two rows a 256-byte line, each pair of rows another position.
+//   along rows: LDS rows of one k; chunk c (8 rows of the operand) of k at position c ^ 4 (k % 4).  ds_read_b64_tr_b16 hands
+//               four values of k of one row to a lane: 16 lanes read 4 k of 16 rows, the four k in four quarters of the banks.
+// What lies past the end of the operand (rows or k) is read from a page of zeros.
+//
+// The MFMA operands are handed over swapped, so that a lane has one row of C and runs of four columns: softmax statistics are sums over
+// registers, and stores go through LDS in whole rows.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <utility>
 #include "lds_dma.h"
+#include "vectors.h"
 
 namespace shampoo {
 
 enum { LIE_K = 0, LIE_ROWS = 1 };          // which index of an operand is contiguous
-enum { STORE_F32 = 0, STORE_BF16 = 1 };
+enum { STORE_F32 = 0, STORE_BF16 = 1, STORE_LOGITS_F32 = 2, STORE_LOGITS_U16 = 3, STORE_NO_LOGITS = 4 };
 
 struct TrainGemmArgs {
   const uint16_t *a, *b;
@@ -22,57 +40,350 @@ struct TrainGemmArgs {
   int32_t M, N, K;
   int32_t products;                        // pairs of planes
   uint32_t plane_a, plane_b;               // four bits each: the planes of product i
-  void *c; int64_t ldc;
+  int32_t tiles_m, tiles_n, splits, per_split;   // slabs of the whole sequence (products x ceil(K / 64)) per split
+  void *c; int64_t ldc, c_split;           // c_split: from the result of a split to the next
   const float *add; int64_t ldadd;         // C += add (float32; may be c itself) or nullptr
-  int32_t store;                           // STORE_F32 / STORE_BF16
+  int32_t store, vec;                      // vec: rows of c (and add) start on multiples of 16 bytes
+  // logits: z = C + bias; per row and span (32 TI columns): the largest z and sum of exp(z - largest); the target's z
+  const float *bias; const int64_t *targets;
+  float2 *stats; int64_t stats_ld;         // [span][row]
+  float *target_z;
 };
 
-typedef float train_f16 __attribute__((ext_vector_type(16)));
+typedef float train_f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// One 64 x 64 tile per workgroup of four wavefronts (32 x 32 each), 32 values of k at a time through LDS.
-template <int ALIE, int BLIE>
-__global__ __launch_bounds__(256) void train_gemm_kernel(const TrainGemmArgs g) {
-  __shared__ __align__(16) uint16_t as[64][40], bs[64][40];
-  const int tiles_n = (g.N + 63) / 64, tm = blockIdx.x / tiles_n, tn = blockIdx.x - tm * tiles_n;
-  const int row0 = tm * 64, col0 = tn * 64, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
-  train_f16 acc;
+constexpr int TG_BK = 64;
+// distance of a logit from the largest of its span in 16 bits: steps of 2^-10 in the exponent of 2
+constexpr float LOGIT_STEPS = 1024.f, LOG2_E = 1.4426950408889634f;
+
+static __device__ __align__(256) unsigned char tg_zeros[256];
+
+// LDS accesses of one wavefront that depend on one another: LDS keeps their order, the compiler must
+__device__ __forceinline__ void tg_wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// How a lane fills and reads the slab of one operand of 64 TI rows.
+template <int LIE, int TI> struct SlabSide {
+  static constexpr int ROWS = 64 * TI, BYTES = ROWS * TG_BK * 2, PIECES = BYTES / 4096;   // 1 KiB pieces per wavefront
+  static constexpr int CHUNKS = LIE == LIE_K ? 8 : ROWS / 8;        // 16-byte chunks of an LDS row
+  static constexpr int STEP_READS = LIE == LIE_K ? TI : 2 * TI;     // LDS reads for 16 values of k
+  uint32_t off[PIECES];        // bytes from the tile's corner
+  uint32_t kc[PIECES];         // first k of the lane's 16 bytes (all are one k along rows)
+  uint32_t valid;              // bit q: the rows of piece q are there
+  uint32_t addr[4];            // LDS: along k, one for each 16 values of k; along rows, one for each 32 rows
+
+  __device__ __forceinline__ void init(int64_t ld, int rows_left, int wave, int side, int lane, uint32_t lds) {
+    valid = 0;
 #pragma unroll
-  for (int v = 0; v < 16; ++v) acc[v] = 0.f;
-  for (int q = 0; q < g.products; ++q) {
-    const uint16_t *pa = g.a + (int64_t)((g.plane_a >> (4 * q)) & 15) * g.a_plane, *pb = g.b + (int64_t)((g.plane_b >> (4 * q)) & 15) * g.b_plane;
-    for (int k0 = 0; k0 < g.K; k0 += 32) {
-      __syncthreads();
-      for (int e = tid; e < 64 * 32; e += 256) {
-        const int i = ALIE == LIE_K ? e >> 5 : e & 63, k = ALIE == LIE_K ? e & 31 : e >> 6;
-        uint16_t v = 0;
-        if (row0 + i < g.M && k0 + k < g.K) v = ALIE == LIE_K ? pa[(int64_t)(row0 + i) * g.lda + k0 + k] : pa[(int64_t)(k0 + k) * g.lda + row0 + i];
-        as[i][k] = v;
+    for (int q = 0; q < PIECES; ++q) {
+      const int p = (wave * PIECES + q) * 64 + lane, r = p / CHUNKS, pos = p % CHUNKS;
+      if (LIE == LIE_K) {
+        const int ch = pos ^ ((r >> 1) & 7);
+        off[q] = (uint32_t)(r * ld * 2) + ch * 16;
+        kc[q] = ch * 8;
+        valid |= (r < rows_left ? 1u : 0u) << q;
+      } else {
+        const int ch = pos ^ (4 * (r & 3));
+        off[q] = (uint32_t)(r * ld * 2) + ch * 16;
+        kc[q] = r;
+        valid |= (ch * 8 < rows_left ? 1u : 0u) << q;
       }
-      for (int e = tid; e < 64 * 32; e += 256) {
-        const int i = BLIE == LIE_K ? e >> 5 : e & 63, k = BLIE == LIE_K ? e & 31 : e >> 6;
-        uint16_t v = 0;
-        if (col0 + i < g.N && k0 + k < g.K) v = BLIE == LIE_K ? pb[(int64_t)(col0 + i) * g.ldb + k0 + k] : pb[(int64_t)(k0 + k) * g.ldb + col0 + i];
-        bs[i][k] = v;
-      }
-      __syncthreads();
+    }
+    if (LIE == LIE_K) {
+      const int f = lane & 31, q = lane >> 5;
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const bf16x8 x = *reinterpret_cast<const bf16x8 *>(&as[wm * 32 + (lane & 31)][16 * s + 8 * (lane >> 5)]);
-        const bf16x8 y = *reinterpret_cast<const bf16x8 *>(&bs[wn * 32 + (lane & 31)][16 * s + 8 * (lane >> 5)]);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, acc, 0, 0, 0);
+      for (int s = 0; s < 4; ++s) addr[s] = lds + (side * 32 * TI + f) * 128 + (((2 * s + q) ^ ((f >> 1) & 7)) * 16);
+    } else {
+      const int b = lane >> 4, t = lane & 15, k = 8 * (b >> 1) + (t >> 2);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int ch = side * 4 * TI + 4 * (i < TI ? i : 0) + 2 * (b & 1) + ((t & 3) >> 1);
+        addr[i] = lds + k * ROWS * 2 + ((ch ^ (4 * (t >> 2))) * 16) + (t & 1) * 8;
       }
     }
   }
-  // accumulator element v: row 8 (v / 4) + 4 (lane / 32) + v % 4, column lane % 32
-#pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    const int i = row0 + wm * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3), j = col0 + wn * 32 + (lane & 31);
-    if (i >= g.M || j >= g.N) continue;
-    float x = acc[v];
-    if (g.add) x += g.add[(int64_t)i * g.ldadd + j];
-    if (g.store == STORE_F32) static_cast<float *>(g.c)[(int64_t)i * g.ldc + j] = x;
-    else static_cast<__bf16 *>(g.c)[(int64_t)i * g.ldc + j] = (__bf16)x;
+};
+
+template <typename F, int... I> __device__ __forceinline__ void tg_each(std::integer_sequence<int, I...>, F &&f) { (f(std::integral_constant<int, I>()), ...); }
+
+#define TG_READ128(dst, addr, imm) asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(imm) : "memory")
+#define TG_READ_TR(dst, addr, imm) asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(imm) : "memory")
+
+// One operand of 16 values of k of 32 TI rows: what the matrix cores take.
+template <int LIE, int TI> struct SlabRegs {
+  u32x4 f[LIE == LIE_K ? TI : 1];
+  u32x2 t[LIE == LIE_K ? 1 : TI][2];
+  // LDS read number R of step S from the stage at byte `st`
+  template <int R, int S> __device__ __forceinline__ void read(const SlabSide<LIE, TI> &side, uint32_t st) {
+    if constexpr (LIE == LIE_K) TG_READ128(f[R], side.addr[S] + st, R * 4096);
+    else TG_READ_TR(t[R >> 1][R & 1], side.addr[R >> 1] + st, (16 * S + 4 * (R & 1)) * 128 * TI);
   }
+  // behind the wait: the compiler may use them from here on
+  __device__ __forceinline__ void arrived() {
+#pragma unroll
+    for (int i = 0; i < TI; ++i) {
+      if constexpr (LIE == LIE_K) asm volatile("" : "+v"(f[i])); else asm volatile("" : "+v"(t[i][0]), "+v"(t[i][1]));
+    }
+  }
+  __device__ __forceinline__ bf16x8 operand(int i) const {
+    if constexpr (LIE == LIE_K) return __builtin_bit_cast(bf16x8, f[i]);
+    else return __builtin_bit_cast(bf16x8, __builtin_shufflevector(t[i][0], t[i][1], 0, 1, 2, 3));
+  }
+};
+
+template <int TI, int ALIE, int BLIE, bool LOGITS>
+__global__ __launch_bounds__(256, TI == 4 ? 1 : 2) void train_gemm_kernel(const TrainGemmArgs g) {
+  typedef SlabSide<ALIE, TI> SideA;
+  typedef SlabSide<BLIE, TI> SideB;
+  constexpr int TILE = 64 * TI, SPAN = 32 * TI, STAGE = SideA::BYTES + SideB::BYTES, PIECES = SideA::PIECES, NMM = TI * TI;
+  __shared__ __align__(256) unsigned char smem[2 * STAGE];
+  const int tiles = g.tiles_m * g.tiles_n, total = tiles * g.splits;
+  // an XCD (workgroup index modulo 8) has neighbouring tiles, in columns of eight
+  const int per = (total + 7) / 8, logical = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+  if (logical >= total || (int)(blockIdx.x >> 3) >= per) return;
+  const int split = logical / tiles, tile = logical - split * tiles;
+  const int group = tile / (8 * g.tiles_n), in_group = tile - group * 8 * g.tiles_n, rows_of = min(8, g.tiles_m - 8 * group);
+  const int tm = 8 * group + in_group % rows_of, tn = in_group / rows_of;
+  const int row0 = tm * TILE, col0 = tn * TILE;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
+  const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)smem;
+
+  SideA sa; SideB sb;
+  sa.init(g.lda, g.M - row0, wave, wm, lane, lds);
+  sb.init(g.ldb, g.N - col0, wave, wn, lane, lds + SideA::BYTES);
+  const uint16_t *corner_a = g.a + (ALIE == LIE_K ? (int64_t)row0 * g.lda : row0), *corner_b = g.b + (BLIE == LIE_K ? (int64_t)col0 * g.ldb : col0);
+  const int64_t step_a = ALIE == LIE_K ? TG_BK : TG_BK * g.lda, step_b = BLIE == LIE_K ? TG_BK : TG_BK * g.ldb;
+  const int slabs_k = (g.K + TG_BK - 1) / TG_BK, all = slabs_k * g.products;
+  const int first = split * g.per_split, count = min(g.per_split, all - first);
+
+  // the slab that is loaded next
+  int in_q = first / slabs_k, in_s = first - in_q * slabs_k, in_left = count;
+  const char *in_a, *in_b;
+  uint32_t ok_a, ok_b;
+  auto locate = [&]() {
+    const int pa = (g.plane_a >> (4 * in_q)) & 15, pb = (g.plane_b >> (4 * in_q)) & 15;
+    in_a = uniform_ptr(corner_a + pa * g.a_plane + in_s * step_a);
+    in_b = uniform_ptr(corner_b + pb * g.b_plane + in_s * step_b);
+  };
+  auto mask = [&]() {
+    const int left = in_left > 0 ? g.K - in_s * TG_BK : 0;
+    ok_a = sa.valid; ok_b = sb.valid;
+    if (left < TG_BK) {
+#pragma unroll
+      for (int q = 0; q < PIECES; ++q) {
+        if ((int)sa.kc[q] >= left) ok_a &= ~(1u << q);
+        if ((int)sb.kc[q] >= left) ok_b &= ~(1u << q);
+      }
+    }
+  };
+  auto next_slab = [&]() {
+    --in_left;
+    if (++in_s == slabs_k) { in_s = 0; ++in_q; }
+    if (in_left > 0) locate();
+    mask();
+  };
+  auto load_a = [&](int q, int stage) {
+    const char *p = (ok_a >> q) & 1 ? in_a + sa.off[q] : reinterpret_cast<const char *>(tg_zeros);
+    __builtin_amdgcn_global_load_lds((glb_void *)p, (lds_void *)(smem + stage + (wave * PIECES + q) * 1024), 16, 0, 0);
+  };
+  auto load_b = [&](int q, int stage) {
+    const char *p = (ok_b >> q) & 1 ? in_b + sb.off[q] : reinterpret_cast<const char *>(tg_zeros);
+    __builtin_amdgcn_global_load_lds((glb_void *)p, (lds_void *)(smem + stage + SideA::BYTES + (wave * PIECES + q) * 1024), 16, 0, 0);
+  };
+
+  train_f32x16 acc[TI][TI];
+#pragma unroll
+  for (int i = 0; i < TI; ++i)
+#pragma unroll
+    for (int j = 0; j < TI; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+
+  // two sets that take turns
+  SlabRegs<ALIE, TI> ra[2];
+  SlabRegs<BLIE, TI> rb[2];
+  constexpr int READS = SideA::STEP_READS + SideB::STEP_READS;
+  auto read = [&](auto rc, auto sc, uint32_t from) {
+    constexpr int R = decltype(rc)::value, S = decltype(sc)::value, B0 = SideA::STEP_READS;
+    if constexpr (R < B0) ra[S & 1].template read<R, S>(sa, from);
+    else if constexpr (R < READS) rb[S & 1].template read<R - B0, S>(sb, from);
+  };
+
+  // One step: the products of 16 values of k, and between them, one at a time, so that the matrix cores do not wait for the wavefront
+  // to issue something else, the LDS reads of the next step (in its first half) and loads of slabs to come (in its second).  A slab's loads
+  // begin with step 3, behind the barrier after which nobody reads its stage any more, and end with step 0 of the slab before it.
+  constexpr int HALF = NMM / 2, PER_SLOT = (READS + HALF - 1) / HALF, LOADS_PER_SLOT = (PIECES + HALF - 1) / HALF;
+  auto step = [&](auto sc, uint32_t st, uint32_t st_next) {
+    constexpr int S = decltype(sc)::value, X = S & 1, LEAD = S == 3 ? NMM / 8 + (NMM < 8) : 0;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    ra[X].arrived(); rb[X].arrived();
+    LDS_SCHED_BARRIER();
+    tg_each(std::make_integer_sequence<int, NMM>(), [&](auto mc) {
+      constexpr int P = decltype(mc)::value, I = P / TI, J = P % TI;
+      acc[I][J] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rb[X].operand(J), ra[X].operand(I), acc[I][J], 0, 0, 0);
+      if constexpr (S == 3 && P == LEAD - 1) {
+        LDS_SCHED_BARRIER();
+        LDS_DMA_WAIT_VM(0);
+        __builtin_amdgcn_s_barrier();
+      }
+      LDS_SCHED_BARRIER();
+      if constexpr (P >= LEAD && P < LEAD + HALF) {
+        tg_each(std::make_integer_sequence<int, PER_SLOT>(), [&](auto rc) {
+          read(std::integral_constant<int, (P - LEAD) * PER_SLOT + decltype(rc)::value>(), std::integral_constant<int, (S + 1) & 3>(), S == 3 ? st_next : st);
+        });
+      }
+      if constexpr (P >= HALF && (S == 3 || S == 0)) {
+#pragma unroll
+        for (int q = (P - HALF) * LOADS_PER_SLOT; q < (P - HALF + 1) * LOADS_PER_SLOT && q < PIECES; ++q) {
+          if constexpr (S == 3) load_a(q, st); else load_b(q, st_next);
+        }
+      }
+      LDS_SCHED_BARRIER();
+    });
+  };
+
+  in_left = count;
+  locate();
+  mask();
+#pragma unroll
+  for (int q = 0; q < PIECES; ++q) { load_a(q, 0); load_b(q, 0); }
+  next_slab();
+#pragma unroll
+  for (int q = 0; q < PIECES; ++q) load_a(q, STAGE);
+  LDS_DMA_WAIT_VM(PIECES);
+  __builtin_amdgcn_s_barrier();
+  tg_each(std::make_integer_sequence<int, READS>(), [&](auto rc) { read(rc, std::integral_constant<int, 0>(), 0); });
+  uint32_t st = 0;
+  for (int t = 0; t < count; ++t) {
+    const uint32_t other = STAGE - st;
+    step(std::integral_constant<int, 0>(), st, other);
+    next_slab();
+    step(std::integral_constant<int, 1>(), st, other);
+    step(std::integral_constant<int, 2>(), st, other);
+    step(std::integral_constant<int, 3>(), st, other);
+    st = other;
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  ra[0].arrived(); rb[0].arrived();
+  LDS_DMA_WAIT_VM(0);
+  __syncthreads();
+
+  // A lane has row lane % 32 of every tile, columns 8 (v / 4) + 4 (lane / 32) + v % 4.  32 rows at a time go through LDS, which only
+  // this wavefront touches.
+  constexpr int PITCH = SPAN + 4;                 // floats: rows are 16-byte aligned and four banks apart
+  static_assert(4 * 32 * PITCH * 4 + (LOGITS ? 4 * SPAN * 4 : 0) <= 2 * STAGE, "LDS");
+  float *buf = reinterpret_cast<float *>(smem) + wave * 32 * PITCH;
+  const int half = lane >> 5, colw = col0 + wn * SPAN, roww = row0 + wm * SPAN;
+  [[maybe_unused]] float *bias = reinterpret_cast<float *>(smem) + 4 * 32 * PITCH + wave * SPAN;
+  if constexpr (LOGITS) {
+    for (int j = lane; j < SPAN; j += 64) bias[j] = colw + j >= g.N ? -INFINITY : g.bias ? g.bias[colw + j] : 0.f;   // no class there: probability 0
+  }
+#pragma unroll
+  for (int i = 0; i < TI; ++i) {
+    const int row = roww + 32 * i + (lane & 31);
+    [[maybe_unused]] float largest = -INFINITY;
+    if constexpr (LOGITS) {
+      tg_wave_order();
+#pragma unroll
+      for (int j = 0; j < TI; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float4 b = *reinterpret_cast<const float4 *>(bias + 32 * j + 8 * q + 4 * half);
+          const float add[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            acc[i][j][4 * q + e] += add[e];
+            largest = fmaxf(largest, acc[i][j][4 * q + e]);
+          }
+        }
+      largest = fmaxf(largest, __shfl_xor(largest, 32, 64));
+      const float base = largest == -INFINITY ? 0.f : largest;
+      float sum = 0.f;
+      const int64_t t = row < g.M ? g.targets[row] - colw : -1;
+      if (__any(t >= 0 && t < SPAN && colw + t < g.N)) {
+        float zt = 0.f;
+#pragma unroll
+        for (int j = 0; j < TI; ++j)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) zt = (int)t == 32 * j + 8 * (v >> 2) + 4 * half + (v & 3) ? acc[i][j][v] : zt;
+        if (t >= 0 && t < SPAN && colw + t < g.N && (((int)t >> 2) & 1) == half) g.target_z[row] = zt;
+      }
+#pragma unroll
+      for (int j = 0; j < TI; ++j)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const float e = (acc[i][j][v] - base) * LOG2_E;
+          sum += __builtin_amdgcn_exp2f(e);
+          if (g.store == STORE_LOGITS_U16) acc[i][j][v] = fminf(-e * LOGIT_STEPS, 65535.f);
+        }
+      sum += __shfl_xor(sum, 32, 64);
+      if (half == 0 && row < g.M) g.stats[(int64_t)(colw / SPAN) * g.stats_ld + row] = make_float2(largest, sum);
+    }
+    if (LOGITS && g.store == STORE_NO_LOGITS) continue;
+    tg_wave_order();
+#pragma unroll
+    for (int j = 0; j < TI; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4 *>(buf + (lane & 31) * PITCH + 32 * j + 8 * q + 4 * half) =
+            make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+    tg_wave_order();
+    constexpr int LANES = SPAN / 8, ROWS_AT_ONCE = 64 / LANES;      // eight columns a lane
+    const int c = (lane % LANES) * 8, col = colw + c, limit = LOGITS ? (int)g.ldc : g.N;
+#pragma unroll
+    for (int r = lane / LANES; r < 32; r += ROWS_AT_ONCE) {
+      const int out = roww + 32 * i + r;
+      if (out < g.M && col < limit) {
+        const float4 x = *reinterpret_cast<const float4 *>(buf + r * PITCH + c), y = *reinterpret_cast<const float4 *>(buf + r * PITCH + c + 4);
+        f32x8 z = {{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w}};
+        if (LOGITS && g.store == STORE_LOGITS_U16) {
+          uint32_t w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = (uint32_t)(z.v[2 * e] + 0.5f) | (uint32_t)(z.v[2 * e + 1] + 0.5f) << 16;
+          *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(g.c) + (int64_t)out * g.ldc + col) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+          if (!LOGITS && g.add) {
+            const f32x8 old = load8(g.add + (int64_t)out * g.ldadd, col, g.N, g.vec);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z.v[e] += old.v[e];
+          }
+          if (!LOGITS && g.store == STORE_BF16) store8(static_cast<uint16_t *>(g.c) + (int64_t)out * g.ldc, col, limit, g.vec, z);
+          else store8(static_cast<float *>(g.c) + split * g.c_split + (int64_t)out * g.ldc, col, limit, g.vec, z);
+        }
+      }
+    }
+  }
+}
+
+// The results of several splits, float32 [split][rows][cols], added up in order.
+struct JoinArgs {
+  const float *part; int64_t stride; int32_t splits;
+  void *c; int64_t ldc; const float *add; int64_t ldadd;
+  int64_t row0; uint32_t pieces, per_row;
+  int32_t cols, pitch, store, vec;
+};
+__global__ __launch_bounds__(256) void train_join_kernel(const JoinArgs g) {
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+  if (i >= g.pieces) return;
+  const uint32_t r = i / g.per_row;
+  const int c = (int)(i - r * g.per_row) * 8;
+  const int64_t row = g.row0 + r;
+  f32x8 s = load8(g.part + row * g.pitch, c, g.pitch, true);
+  for (int k = 1; k < g.splits; ++k) {
+    const f32x8 x = load8(g.part + k * g.stride + row * g.pitch, c, g.pitch, true);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s.v[e] += x.v[e];
+  }
+  if (g.add) {
+    const f32x8 x = load8(g.add + row * g.ldadd, c, g.cols, g.vec);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s.v[e] += x.v[e];
+  }
+  if (g.store == STORE_BF16) store8(static_cast<uint16_t *>(g.c) + row * g.ldc, c, g.cols, g.vec, s);
+  else store8(static_cast<float *>(g.c) + row * g.ldc, c, g.cols, g.vec, s);
 }
 
 }  // namespace shampoo

@@ -87,11 +87,8 @@ template <int FROM> int launch_planes(PlanesArgs g, int planes, int64_t rows, hi
   g.per_row = (uint32_t)(g.ld / 8);
   return by_rows(rows, g.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
     g.row0 = r; g.pieces = pieces;
-    switch (planes) {
-      case 1: planes_kernel<FROM, 1><<<grid, 256, 0, s>>>(g); break;
-      case 2: planes_kernel<FROM, 2><<<grid, 256, 0, s>>>(g); break;
-      default: planes_kernel<FROM, 3><<<grid, 256, 0, s>>>(g);
-    }
+    if (planes == 1) planes_kernel<FROM, 1><<<grid, 256, 0, s>>>(g);
+    else planes_kernel<FROM, 3><<<grid, 256, 0, s>>>(g);
   });
 }
 
@@ -139,20 +136,58 @@ int plane_pairs(int na, int nb, uint32_t &pa, uint32_t &pb) {
   return n;
 }
 
-int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const Result &c, hipStream_t s) {
-  TrainGemmArgs g;
+// How a product is cut: tiles of 256 or 128 (TI), and splits of the sequence of slabs where there are few tiles.
+struct GemmCut { int ti, splits, per_split; size_t bytes; };
+GemmCut gemm_cut(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, bool logits) {
+  uint32_t unused_a, unused_b;
+  const int64_t all = (K + TG_BK - 1) / TG_BK * plane_pairs(planes_a, planes_b, unused_a, unused_b);
+  const int64_t large = ((M + 255) / 256) * ((N + 255) / 256);
+  GemmCut c = {large >= 128 ? 4 : 2, 1, (int)all, 0};
+  if (logits) return c;
+  const int64_t tile = 64 * c.ti, tiles = ((M + tile - 1) / tile) * ((N + tile - 1) / tile), want = c.ti == 4 ? 256 : 512;
+  const int64_t splits = std::max<int64_t>(1, std::min(want / tiles, all / 4));
+  c.per_split = (int)((all + splits - 1) / splits);
+  c.splits = (int)((all + c.per_split - 1) / c.per_split);
+  if (c.splits > 1) c.bytes = align_up((size_t)c.splits * M * round_up(N, 8) * sizeof(float));
+  return c;
+}
+template <int TI, bool LOGITS> void gemm_launch(const TrainGemmArgs &g, int alie, int blie, hipStream_t s) {
+  const int64_t total = (int64_t)g.tiles_m * g.tiles_n * g.splits;
+  const dim3 grid((unsigned)((total + 7) / 8 * 8));
+  if (alie == LIE_K && blie == LIE_K) train_gemm_kernel<TI, LIE_K, LIE_K, LOGITS><<<grid, 256, 0, s>>>(g);
+  else if (alie == LIE_K) train_gemm_kernel<TI, LIE_K, LIE_ROWS, LOGITS><<<grid, 256, 0, s>>>(g);
+  else if constexpr (!LOGITS) train_gemm_kernel<TI, LIE_ROWS, LIE_ROWS, LOGITS><<<grid, 256, 0, s>>>(g);
+}
+int gemm_args(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const GemmCut &cut, TrainGemmArgs &g) {
+  g = {};
   g.a = a.p; g.b = b.p; g.lda = a.ld; g.ldb = b.ld; g.a_plane = a.plane; g.b_plane = b.plane;
   g.M = (int32_t)M; g.N = (int32_t)N; g.K = (int32_t)K;
   g.products = plane_pairs(a.planes, b.planes, g.plane_a, g.plane_b);
-  g.c = c.c; g.ldc = c.ldc; g.add = c.add; g.ldadd = c.ldadd; g.store = c.store;
-  const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
-  if (tiles > ((int64_t)1 << 23)) return SHAMPOO_ERR_UNSUPPORTED;
-  const dim3 grid((unsigned)tiles);
-  if (a.lie == LIE_K && b.lie == LIE_K) train_gemm_kernel<LIE_K, LIE_K><<<grid, 256, 0, s>>>(g);
-  else if (a.lie == LIE_K) train_gemm_kernel<LIE_K, LIE_ROWS><<<grid, 256, 0, s>>>(g);
-  else train_gemm_kernel<LIE_ROWS, LIE_ROWS><<<grid, 256, 0, s>>>(g);
+  g.tiles_m = (int32_t)((M + 64 * cut.ti - 1) / (64 * cut.ti)); g.tiles_n = (int32_t)((N + 64 * cut.ti - 1) / (64 * cut.ti));
+  g.splits = cut.splits; g.per_split = cut.per_split;
+  return (int64_t)g.tiles_m * g.tiles_n > ((int64_t)1 << 23) ? SHAMPOO_ERR_UNSUPPORTED : SHAMPOO_OK;
+}
+// C = A B^T; `part`: scratch of gemm_cut's size
+int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const Result &c, float *part, hipStream_t s) {
+  const GemmCut cut = gemm_cut(M, N, K, a.planes, b.planes, false);
+  TrainGemmArgs g;
+  TRY(gemm_args(a, b, M, N, K, cut, g));
+  const bool vec = vec_ok(c.c, c.ldc, c.store == STORE_F32 ? SHAMPOO_GRAD_F32 : SHAMPOO_GRAD_BF16) && (!c.add || vec_ok(c.add, c.ldadd, SHAMPOO_GRAD_F32));
+  if (cut.splits == 1) {
+    g.c = c.c; g.ldc = c.ldc; g.add = c.add; g.ldadd = c.ldadd; g.store = c.store; g.vec = vec;
+  } else {
+    g.c = part; g.ldc = round_up(N, 8); g.c_split = M * g.ldc; g.store = STORE_F32; g.vec = 1;
+  }
+  if (cut.ti == 4) gemm_launch<4, false>(g, a.lie, b.lie, s); else gemm_launch<2, false>(g, a.lie, b.lie, s);
   HIP_TRY(hipGetLastError());
-  return SHAMPOO_OK;
+  if (cut.splits == 1) return SHAMPOO_OK;
+  JoinArgs j = {};
+  j.part = part; j.stride = g.c_split; j.splits = cut.splits; j.c = c.c; j.ldc = c.ldc; j.add = c.add; j.ldadd = c.ldadd;
+  j.cols = (int32_t)N; j.pitch = (int32_t)g.ldc; j.store = c.store; j.vec = vec; j.per_row = (uint32_t)(g.ldc / 8);
+  return by_rows(M, j.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
+    j.row0 = r; j.pieces = pieces;
+    train_join_kernel<<<grid, 256, 0, s>>>(j);
+  });
 }
 
 // A matrix of the caller as an operand: as it lies, or as planes in scratch (float32; rows that the products cannot read 16 bytes at
@@ -178,12 +213,14 @@ struct Source {
 // ---------------------------------------------------------------------------
 struct CrossEntropyPlan {
   Source x, w;
-  int planes = 1;            // of g
-  int64_t ldz = 0, piece = 0, pieces = 0, ranges = 1, range_rows = 1;
+  int planes = 0;            // of g beside float32 logits; 0: in the place of 16-bit ones
+  int64_t ldz = 0, spans = 0, piece = 0, pieces = 0, range_rows = 1, ranges = 1;
   bool sum = false;          // bf16 dw of several pieces: summed in scratch
   size_t bytes = 0;
   uint16_t *xp, *wp, *g;
-  float *z, *lse, *coef, *acc, *sums, *db;
+  float *z, *lse, *coef, *target_z, *acc, *sums, *part;
+  float2 *stats;
+  int grad_planes() const { return std::max(planes, 1); }
 };
 int cross_entropy_plan(const shampoo_cross_entropy &c, void *workspace, CrossEntropyPlan &p) {
   if (c.rows < 0 || c.features < 1 || c.classes < 1) return SHAMPOO_ERR_SHAPE;
@@ -191,27 +228,38 @@ int cross_entropy_plan(const shampoo_cross_entropy &c, void *workspace, CrossEnt
   if (!dtype_ok(c.dtype) || !dtype_ok(c.grad_dtype) || (c.w_layout != SHAMPOO_OUT_IN && c.w_layout != SHAMPOO_IN_OUT)) return SHAMPOO_ERR_HYPER;
   if (c.gradients && c.dtype == SHAMPOO_GRAD_F32 && c.grad_dtype != SHAMPOO_GRAD_F32) return SHAMPOO_ERR_HYPER;
   const bool out_in = c.w_layout == SHAMPOO_OUT_IN;
-  const int64_t wcols = out_in ? c.features : c.classes;
-  if (c.ldx < c.features || c.ldw < wcols || (c.gradients && (c.lddx < c.features || c.lddw < wcols))) return SHAMPOO_ERR_SHAPE;
-  p.x = {c.dtype, c.rows, c.features, c.ldx};
-  p.w = {c.dtype, out_in ? c.classes : c.features, wcols, c.ldw};
-  p.planes = c.dtype == SHAMPOO_GRAD_F32 ? 3 : c.grad_dtype == SHAMPOO_GRAD_F32 ? 2 : 1;
-  p.ldz = round_up(c.classes, 64);
-  const size_t per_row = (size_t)p.ldz * (4 + (c.gradients ? 2 * p.planes : 0));
+  const int64_t wcols = out_in ? c.features : c.classes, d = c.features, v = c.classes;
+  if (c.ldx < d || c.ldw < wcols || (c.gradients && (c.lddx < d || c.lddw < wcols))) return SHAMPOO_ERR_SHAPE;
+  p.x = {c.dtype, c.rows, d, c.ldx};
+  p.w = {c.dtype, out_in ? v : d, wcols, c.ldw};
+  // a float32 result needs g to float32 accuracy, and that needs the logits so
+  p.planes = c.grad_dtype == SHAMPOO_GRAD_F32 ? 3 : c.has_bias ? 1 : 0;
+  p.ldz = round_up(v, 64);
+  p.spans = round_up(v, 256) / 64;
+  const size_t per_row = (size_t)p.spans * sizeof(float2) + (c.gradients ? (size_t)p.ldz * (p.planes ? 4 + 2 * p.planes : 2) : 0);
   p.piece = std::min<int64_t>(round_up(std::max<int64_t>(c.rows, 1), PIECE_ROWS),
                               std::max<int64_t>(PIECE_ROWS, (int64_t)(LOGIT_BYTES / per_row) / PIECE_ROWS * PIECE_ROWS));
   p.pieces = (c.rows + p.piece - 1) / p.piece;
   p.sum = c.gradients && p.pieces > 1 && c.grad_dtype == SHAMPOO_GRAD_BF16;
-  p.range_rows = 64;
-  p.ranges = p.piece / p.range_rows;
+  // rows of a thread of softmax_grad_kernel: 64 where that leaves a thousand workgroups
+  p.range_rows = std::min<int64_t>(64, std::max<int64_t>(1, std::min(p.piece, c.rows) * ((p.ldz + 2047) / 2048) / 1024));
+  p.ranges = (p.piece + p.range_rows - 1) / p.range_rows;
   Arena a(workspace);
   p.xp = p.x.take(a); p.wp = p.w.take(a);
-  p.z = a.take<float>((size_t)p.piece * p.ldz);
-  p.lse = a.take<float>(p.piece); p.coef = a.take<float>(p.piece);
+  p.lse = a.take<float>(p.piece); p.coef = a.take<float>(p.piece); p.target_z = a.take<float>(p.piece);
+  p.stats = a.take<float2>((size_t)p.spans * p.piece);
   if (c.gradients) {
-    p.g = a.take<uint16_t>((size_t)p.planes * p.piece * p.ldz);
+    if (p.planes) p.z = a.take<float>((size_t)p.piece * p.ldz);
+    p.g = a.take<uint16_t>((size_t)p.grad_planes() * p.piece * p.ldz);
     if (p.sum) p.acc = a.take<float>((size_t)p.w.rows * p.w.cols);
-    if (c.has_bias) { p.sums = a.take<float>((size_t)p.ranges * c.classes * p.pieces); }
+    if (c.has_bias) p.sums = a.take<float>((size_t)p.ranges * p.pieces * v);
+    size_t part = 0;
+    for (int64_t n : {p.piece, c.rows - std::max<int64_t>(0, p.pieces - 1) * p.piece, c.rows}) {      // all pieces, the last one, a single one
+      if (n < 1 || n > p.piece) continue;
+      part = std::max(part, gemm_cut(n, d, v, c.dtype == SHAMPOO_GRAD_F32 ? 3 : 1, p.w.planes(), false).bytes);
+      part = std::max(part, out_in ? gemm_cut(v, d, n, p.grad_planes(), p.x.planes(), false).bytes : gemm_cut(d, v, n, p.x.planes(), p.grad_planes(), false).bytes);
+    }
+    if (part) p.part = a.take<float>(part / sizeof(float));
   }
   p.bytes = a.used;
   return SHAMPOO_OK;
@@ -227,7 +275,7 @@ struct WeightGradPlan {
   bool sum = false;
   size_t bytes = 0;
   uint16_t *xp, *dyp;
-  float *acc, *sums;
+  float *acc, *sums, *part;
 };
 int weight_grad_plan(int64_t rows, int32_t in, int32_t out, int32_t activation, int32_t dtype, int64_t lddy, int32_t grad_dtype, bool bias,
                      void *workspace, WeightGradPlan &p) {
@@ -236,7 +284,7 @@ int weight_grad_plan(int64_t rows, int32_t in, int32_t out, int32_t activation, 
   if (!dtype_ok(dtype) || !dtype_ok(grad_dtype) || activation < ACT_NONE || activation > ACT_SILU) return SHAMPOO_ERR_HYPER;
   if (dtype == SHAMPOO_GRAD_F32 && grad_dtype != SHAMPOO_GRAD_F32) return SHAMPOO_ERR_HYPER;
   p.dy = {dtype, rows, out, lddy};
-  p.planes = activation == ACT_NONE ? 1 : dtype == SHAMPOO_GRAD_F32 ? 3 : grad_dtype == SHAMPOO_GRAD_F32 ? 2 : 1;
+  p.planes = activation == ACT_NONE ? 1 : grad_dtype == SHAMPOO_GRAD_F32 ? 3 : 1;
   p.ldp = round_up(in, 64);
   p.piece = std::min<int64_t>(round_up(std::max<int64_t>(rows, 1), PIECE_ROWS),
                               std::max<int64_t>(PIECE_ROWS, (int64_t)(PLANE_BYTES / ((size_t)p.ldp * 2 * p.planes)) / PIECE_ROWS * PIECE_ROWS));
@@ -249,6 +297,12 @@ int weight_grad_plan(int64_t rows, int32_t in, int32_t out, int32_t activation, 
   p.dyp = p.dy.take(a);
   if (p.sum) p.acc = a.take<float>((size_t)in * out);
   if (bias) p.sums = a.take<float>((size_t)p.parts * out);
+  size_t part = 0;
+  for (int64_t n : {p.piece, rows - std::max<int64_t>(0, p.pieces - 1) * p.piece, rows}) {
+    if (n < 1 || n > p.piece) continue;
+    part = std::max(part, std::max(gemm_cut(out, in, n, p.dy.planes(), p.planes, false).bytes, gemm_cut(in, out, n, p.planes, p.dy.planes(), false).bytes));
+  }
+  if (part) p.part = a.take<float>(part / sizeof(float));
   p.bytes = a.used;
   return SHAMPOO_OK;
 }
@@ -362,32 +416,40 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
     const int64_t i0 = k * p.piece, n = std::min(p.piece, c->rows - i0);
     Operand xk = xo;
     xk.p += i0 * xo.ld;
-    TRY(gemm(xk, wo, n, v, d, {p.z, p.ldz, STORE_F32, nullptr, 0}, s));
-    RowLossArgs r = {p.z, p.ldz, bias, targets + i0, weight ? weight + i0 : nullptr, scale, p.lse, p.coef, loss + i0, (int32_t)v};
-    row_loss_kernel<<<dim3((unsigned)n), 256, 0, s>>>(r);
+    const GemmCut cut = gemm_cut(n, v, d, xk.planes, wo.planes, true);
+    const int32_t span = 32 * cut.ti;
+    TrainGemmArgs z;
+    TRY(gemm_args(xk, wo, n, v, d, cut, z));
+    z.c = p.planes ? static_cast<void *>(p.z) : p.g; z.ldc = p.ldz; z.vec = 1;
+    z.store = !c->gradients ? STORE_NO_LOGITS : p.planes ? STORE_LOGITS_F32 : STORE_LOGITS_U16;
+    z.bias = bias; z.targets = targets + i0; z.stats = p.stats; z.stats_ld = p.piece; z.target_z = p.target_z;
+    if (cut.ti == 4) gemm_launch<4, true>(z, xk.lie, wo.lie, s); else gemm_launch<2, true>(z, xk.lie, wo.lie, s);
     HIP_TRY(hipGetLastError());
-    if (!c->gradients) continue;
-    const int64_t ranges = (n + p.range_rows - 1) / p.range_rows;
-    SoftmaxGradArgs q = {p.z, p.ldz, p.lse, p.coef, targets + i0, p.g, p.piece * p.ldz, p.ldz, dbias ? p.sums + k * p.ranges * v : nullptr,
-                         (int32_t)n, (int32_t)v, (int32_t)p.range_rows};
-    const dim3 grid((unsigned)((p.ldz / 8 + 255) / 256), (unsigned)ranges);
+    const RowLossArgs r = {p.stats, p.piece, p.target_z, targets + i0, weight ? weight + i0 : nullptr, scale, p.lse, p.coef, loss + i0,
+                           (int32_t)n, (int32_t)v, z.tiles_n * 2};
+    row_loss_kernel<<<dim3((unsigned)((n + 15) / 16)), 256, 0, s>>>(r);
+    HIP_TRY(hipGetLastError());
+    if (!dx && !dw && !dbias) continue;
+    const SoftmaxGradArgs q = {p.z, p.ldz, p.stats, p.piece, span, p.lse, p.coef, targets + i0, p.g, p.piece * p.ldz,
+                               dbias ? p.sums + k * p.ranges * v : nullptr, (int32_t)n, (int32_t)v, (int32_t)p.range_rows};
+    const dim3 grid((unsigned)((p.ldz / 8 + 255) / 256), (unsigned)((n + p.range_rows - 1) / p.range_rows));
     switch (p.planes) {
+      case 0: softmax_grad_kernel<0><<<grid, 256, 0, s>>>(q); break;
       case 1: softmax_grad_kernel<1><<<grid, 256, 0, s>>>(q); break;
-      case 2: softmax_grad_kernel<2><<<grid, 256, 0, s>>>(q); break;
       default: softmax_grad_kernel<3><<<grid, 256, 0, s>>>(q);
     }
     HIP_TRY(hipGetLastError());
     if (dx) {
-      const Operand go = {p.g, p.ldz, p.piece * p.ldz, c->dtype == SHAMPOO_GRAD_BF16 ? 1 : p.planes, LIE_K};
+      const Operand go = {p.g, p.ldz, p.piece * p.ldz, c->dtype == SHAMPOO_GRAD_F32 ? 3 : 1, LIE_K};
       Operand wt = wo;
       wt.lie = out_in ? LIE_ROWS : LIE_K;
-      TRY(gemm(go, wt, n, d, v, {static_cast<char *>(dx) + i0 * c->lddx * size_of(c->dtype), c->lddx, c->dtype == SHAMPOO_GRAD_F32 ? STORE_F32 : STORE_BF16, nullptr, 0}, s));
+      TRY(gemm(go, wt, n, d, v, {static_cast<char *>(dx) + i0 * c->lddx * size_of(c->dtype), c->lddx, c->dtype == SHAMPOO_GRAD_F32 ? STORE_F32 : STORE_BF16, nullptr, 0}, p.part, s));
     }
     if (dw) {
-      const Operand gt = {p.g, p.ldz, p.piece * p.ldz, p.planes, LIE_ROWS};
+      const Operand gt = {p.g, p.ldz, p.piece * p.ldz, p.grad_planes(), LIE_ROWS};
       xk.lie = LIE_ROWS;
       const Result out = piece_result(dw, c->lddw, c->grad_dtype, p.acc, p.w.cols, k == 0, k == p.pieces - 1);
-      TRY(out_in ? gemm(gt, xk, v, d, n, out, s) : gemm(xk, gt, d, v, n, out, s));
+      TRY(out_in ? gemm(gt, xk, v, d, n, out, p.part, s) : gemm(xk, gt, d, v, n, out, p.part, s));
     }
   }
   if (dbias) {
@@ -493,7 +555,7 @@ int shampoo_checkpoint_weight_grad(const void *packed, size_t packed_bytes, int6
     g.plane = xo.plane;
     TRY(launch_planes<FROM_PACKED>(g, p.planes, n, s));
     const Result r = piece_result(dw, lddw, grad_dtype, p.acc, out_in ? in : out, k == 0, k == p.pieces - 1);
-    TRY(out_in ? gemm(dk, xo, out, in, n, r, s) : gemm(xo, dk, in, out, n, r, s));
+    TRY(out_in ? gemm(dk, xo, out, in, n, r, p.part, s) : gemm(xo, dk, in, out, n, r, p.part, s));
   }
   if (db) {
     const dim3 grid((out + 255) / 256, (unsigned)p.parts);
