@@ -141,11 +141,11 @@ template <typename T, bool GRAD> __global__ __launch_bounds__(256) void checkpoi
 }
 
 // a(x) of a checkpoint, or a matrix in memory (float32 or bf16, any alignment), as PLANES bf16 planes [plane][rows][ld], ld a
-// multiple of 8, zeros from cols to ld.
+// multiple of 8, zeros from cols to ld and in rows from `rows` on.
 struct PlanesArgs {
   Packed p; const void *x; int64_t ldx;        // one of the two
   uint16_t *out; int64_t plane, ld;
-  int64_t row0; uint32_t pieces, per_row;      // ld / 8
+  int64_t rows, row0; uint32_t pieces, per_row;      // ld / 8
   int32_t cols, vec, activation;
 };
 enum { FROM_PACKED = 0, FROM_F32 = 1, FROM_BF16 = 2 };
@@ -156,7 +156,8 @@ template <int FROM, int PLANES> __global__ __launch_bounds__(256) void planes_ke
   const int c = (int)(i - r * g.per_row) * 8;
   const int64_t row = g.row0 + r;
   f32x8 x = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
-  if constexpr (FROM == FROM_PACKED) {
+  if (row >= g.rows) {
+  } else if constexpr (FROM == FROM_PACKED) {
     if (c < g.p.pitch) x = packed_load8(g.p, row, c);
     if (g.activation != ACT_NONE) {
 #pragma unroll

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(256) void row_loss_kernel(const RowLossArgs g) {
   g.loss[i] = !valid ? 0.f : zt == -INFINITY ? INFINITY : lse - zt;
 }
 
-// g of a piece of the rows, zeros from classes to ldg.  A thread has eight columns of the rows of its range.
+// g of a piece of the rows, zeros from classes to ldg and in the rows from `rows` to the next multiple of 64.  A thread has eight columns of the rows of its range.
 struct SoftmaxGradArgs {
   const float *z; int64_t ldg;       // float32 logits
   const float2 *stats; int64_t stats_ld; int32_t span;
@@ -68,11 +68,12 @@ template <int PLANES> __global__ __launch_bounds__(256) void softmax_grad_kernel
   constexpr int OUT = PLANES ? PLANES : 1;
   const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
   if (c >= g.ldg) return;
-  const int i0 = blockIdx.y * g.per_range, i1 = min(g.rows, i0 + g.per_range);
+  const int i0 = blockIdx.y * g.per_range, i1 = min((g.rows + 63) & ~63, i0 + g.per_range);
   f32x8 sum = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
   for (int i = i0; i < i1; ++i) {
-    const float lse = g.lse[i], k = g.coef[i];
-    const int64_t t = g.targets[i] - c, at = (int64_t)i * g.ldg + c;
+    const bool there = i < g.rows;
+    const float lse = there ? g.lse[i] : 0.f, k = there ? g.coef[i] : 0.f;
+    const int64_t t = (there ? g.targets[i] : 0) - c, at = (int64_t)i * g.ldg + c;
     f32x8 p;
     if constexpr (PLANES == 0) {
       const uint4 u = *reinterpret_cast<const uint4 *>(g.out + at);

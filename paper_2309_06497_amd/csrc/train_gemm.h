@@ -4,8 +4,9 @@
 //
 // Operands are bf16 planes in memory: one for a bf16 matrix, up to three for a float32 one (x = h + l + m, 8 bits each), whose
 // products (s, t) are all that float32 accuracy needs, smallest first: one loop over k behind the other.  An operand lies along
-// k (ptr[row * ld + k]) or along rows (ptr[k * ld + row]).  Contract, which the host keeps: 16-byte aligned, ld % 8 == 0, the
-// contiguous extent readable up to a multiple of 8, and zero there where that extent is k.
+// k (ptr[row * ld + k]) or along rows (ptr[k * ld + row]).  Contract, which the host keeps: 16-byte aligned, ld % 8 == 0; along k
+// readable up to the next multiple of 64 of K and zero there, along rows readable up to a multiple of 8 of the rows; and where both
+// lie along rows, one of them has zeros for k from K to the next multiple of 64.
 //
 // Tile of 64 TI x 64 TI per workgroup of four wavefronts, 32 TI x 32 TI each as TI x TI tiles of v_mfma_f32_32x32x16_bf16.  TI = 4:
 // 256 accumulator registers, one wavefront per SIMD; 8 KB of operands from LDS per 16 products of 32 cycles, half of what LDS
@@ -18,7 +19,8 @@
 //               chunk of 16 rows: two rows a 256-byte line, each pair of rows another position.
 //   along rows: LDS rows of one k; chunk c (8 rows of the operand) of k at position c ^ 4 (k % 4).  ds_read_b64_tr_b16 hands
 //               four values of k of one row to a lane: 16 lanes read 4 k of 16 rows, the four k in four quarters of the banks.
-// What lies past the end of the operand (rows or k) is read from a page of zeros.
+// Past the end of an operand its last row, or last k, is read again: rows for results that nobody keeps, k for products with the
+// other operand's zeros.  So every load is one instruction: a scalar base that moves on by a slab, and an offset per lane.
 //
 // The MFMA operands are handed over swapped, so that a lane has one row of C and runs of four columns: softmax statistics are sums over
 // registers, and stores go through LDS in whole rows.
@@ -39,6 +41,7 @@ struct TrainGemmArgs {
   int64_t lda, ldb, a_plane, b_plane;      // elements
   int32_t M, N, K;
   int32_t products;                        // pairs of planes
+  int32_t padded;                          // both along rows: 1 where A, 2 where B has the zeros
   uint32_t plane_a, plane_b;               // four bits each: the planes of product i
   int32_t tiles_m, tiles_n, splits, per_split;   // slabs of the whole sequence (products x ceil(K / 64)) per split
   void *c; int64_t ldc, c_split;           // c_split: from the result of a split to the next
@@ -57,8 +60,6 @@ constexpr int TG_BK = 64;
 // distance of a logit from the largest of its span in 16 bits: steps of 2^-10 in the exponent of 2
 constexpr float LOGIT_STEPS = 1024.f, LOG2_E = 1.4426950408889634f;
 
-static __device__ __align__(256) unsigned char tg_zeros[256];
-
 // LDS accesses of one wavefront that depend on one another: LDS keeps their order, the compiler must
 __device__ __forceinline__ void tg_wave_order() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -71,27 +72,18 @@ template <int LIE, int TI> struct SlabSide {
   static constexpr int CHUNKS = LIE == LIE_K ? 8 : ROWS / 8;        // 16-byte chunks of an LDS row
   static constexpr int STEP_READS = LIE == LIE_K ? TI : 2 * TI;     // LDS reads for 16 values of k
   uint32_t off[PIECES];        // bytes from the tile's corner
-  uint32_t kc[PIECES];         // first k of the lane's 16 bytes (all are one k along rows)
-  uint32_t valid;              // bit q: the rows of piece q are there
   uint32_t addr[4];            // LDS: along k, one for each 16 values of k; along rows, one for each 32 rows
 
-  __device__ __forceinline__ void init(int64_t ld, int rows_left, int wave, int side, int lane, uint32_t lds) {
-    valid = 0;
+  // k_left: values of k that are there
+  __device__ __forceinline__ void offsets(int64_t ld, int rows_left, int k_left, int wave, int lane) {
 #pragma unroll
     for (int q = 0; q < PIECES; ++q) {
       const int p = (wave * PIECES + q) * 64 + lane, r = p / CHUNKS, pos = p % CHUNKS;
-      if (LIE == LIE_K) {
-        const int ch = pos ^ ((r >> 1) & 7);
-        off[q] = (uint32_t)(r * ld * 2) + ch * 16;
-        kc[q] = ch * 8;
-        valid |= (r < rows_left ? 1u : 0u) << q;
-      } else {
-        const int ch = pos ^ (4 * (r & 3));
-        off[q] = (uint32_t)(r * ld * 2) + ch * 16;
-        kc[q] = r;
-        valid |= (ch * 8 < rows_left ? 1u : 0u) << q;
-      }
+      if (LIE == LIE_K) off[q] = (uint32_t)(min(r, rows_left - 1) * ld * 2) + (pos ^ ((r >> 1) & 7)) * 16;
+      else off[q] = (uint32_t)(min(r, k_left - 1) * ld * 2) + min(pos ^ (4 * (r & 3)), (rows_left - 1) >> 3) * 16;
     }
+  }
+  __device__ __forceinline__ void addresses(int side, int lane, uint32_t lds) {
     if (LIE == LIE_K) {
       const int f = lane & 31, q = lane >> 5;
 #pragma unroll
@@ -152,46 +144,39 @@ __global__ __launch_bounds__(256, TI == 4 ? 1 : 2) void train_gemm_kernel(const 
   const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)smem;
 
   SideA sa; SideB sb;
-  sa.init(g.lda, g.M - row0, wave, wm, lane, lds);
-  sb.init(g.ldb, g.N - col0, wave, wn, lane, lds + SideA::BYTES);
+  sa.addresses(wm, lane, lds);
+  sb.addresses(wn, lane, lds + SideA::BYTES);
   const uint16_t *corner_a = g.a + (ALIE == LIE_K ? (int64_t)row0 * g.lda : row0), *corner_b = g.b + (BLIE == LIE_K ? (int64_t)col0 * g.ldb : col0);
   const int64_t step_a = ALIE == LIE_K ? TG_BK : TG_BK * g.lda, step_b = BLIE == LIE_K ? TG_BK : TG_BK * g.ldb;
   const int slabs_k = (g.K + TG_BK - 1) / TG_BK, all = slabs_k * g.products;
   const int first = split * g.per_split, count = min(g.per_split, all - first);
 
-  // the slab that is loaded next
-  int in_q = first / slabs_k, in_s = first - in_q * slabs_k, in_left = count;
+  // the slab that is loaded next: where it begins, and how much of k is left there; behind the last one that one again
+  int in_q = first / slabs_k, in_s = first - in_q * slabs_k, in_left = count, in_k;
   const char *in_a, *in_b;
-  uint32_t ok_a, ok_b;
   auto locate = [&]() {
     const int pa = (g.plane_a >> (4 * in_q)) & 15, pb = (g.plane_b >> (4 * in_q)) & 15;
     in_a = uniform_ptr(corner_a + pa * g.a_plane + in_s * step_a);
     in_b = uniform_ptr(corner_b + pb * g.b_plane + in_s * step_b);
+    in_k = g.K - in_s * TG_BK;
+    sa.offsets(g.lda, g.M - row0, g.padded == 1 ? TG_BK : in_k, wave, lane);
+    sb.offsets(g.ldb, g.N - col0, g.padded == 2 ? TG_BK : in_k, wave, lane);
   };
-  auto mask = [&]() {
-    const int left = in_left > 0 ? g.K - in_s * TG_BK : 0;
-    ok_a = sa.valid; ok_b = sb.valid;
-    if (left < TG_BK) {
-#pragma unroll
-      for (int q = 0; q < PIECES; ++q) {
-        if ((int)sa.kc[q] >= left) ok_a &= ~(1u << q);
-        if ((int)sb.kc[q] >= left) ok_b &= ~(1u << q);
+  auto next_slab = [&]() {
+    if (--in_left > 0) {
+      in_a += 2 * step_a; in_b += 2 * step_b;
+      in_k -= TG_BK;
+      if (in_k < TG_BK) {                          // the end of k, or the next pair of planes
+        if (in_k <= 0) { ++in_q; in_s = 0; } else { in_s = slabs_k - 1; }
+        locate();
       }
     }
   };
-  auto next_slab = [&]() {
-    --in_left;
-    if (++in_s == slabs_k) { in_s = 0; ++in_q; }
-    if (in_left > 0) locate();
-    mask();
-  };
   auto load_a = [&](int q, int stage) {
-    const char *p = (ok_a >> q) & 1 ? in_a + sa.off[q] : reinterpret_cast<const char *>(tg_zeros);
-    __builtin_amdgcn_global_load_lds((glb_void *)p, (lds_void *)(smem + stage + (wave * PIECES + q) * 1024), 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((glb_void *)(in_a + sa.off[q]), (lds_void *)(smem + stage + (wave * PIECES + q) * 1024), 16, 0, 0);
   };
   auto load_b = [&](int q, int stage) {
-    const char *p = (ok_b >> q) & 1 ? in_b + sb.off[q] : reinterpret_cast<const char *>(tg_zeros);
-    __builtin_amdgcn_global_load_lds((glb_void *)p, (lds_void *)(smem + stage + SideA::BYTES + (wave * PIECES + q) * 1024), 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((glb_void *)(in_b + sb.off[q]), (lds_void *)(smem + stage + SideA::BYTES + (wave * PIECES + q) * 1024), 16, 0, 0);
   };
 
   train_f32x16 acc[TI][TI];
@@ -245,9 +230,7 @@ __global__ __launch_bounds__(256, TI == 4 ? 1 : 2) void train_gemm_kernel(const 
     });
   };
 
-  in_left = count;
   locate();
-  mask();
 #pragma unroll
   for (int q = 0; q < PIECES; ++q) { load_a(q, 0); load_b(q, 0); }
   next_slab();
@@ -260,8 +243,8 @@ __global__ __launch_bounds__(256, TI == 4 ? 1 : 2) void train_gemm_kernel(const 
   for (int t = 0; t < count; ++t) {
     const uint32_t other = STAGE - st;
     step(std::integral_constant<int, 0>(), st, other);
-    next_slab();
     step(std::integral_constant<int, 1>(), st, other);
+    next_slab();
     step(std::integral_constant<int, 2>(), st, other);
     step(std::integral_constant<int, 3>(), st, other);
     st = other;

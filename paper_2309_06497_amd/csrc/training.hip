@@ -121,6 +121,7 @@ int launch_zero(void *p, int64_t rows, int64_t cols, int64_t ld, int64_t elem, h
 // ---------------------------------------------------------------------------
 struct Operand {
   const uint16_t *p; int64_t ld, plane; int planes, lie;
+  bool padded = false;       // along rows: zeros behind the last k
 };
 struct Result {
   void *c; int64_t ldc; int store; const float *add; int64_t ldadd;
@@ -165,6 +166,7 @@ int gemm_args(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t 
   g.products = plane_pairs(a.planes, b.planes, g.plane_a, g.plane_b);
   g.tiles_m = (int32_t)((M + 64 * cut.ti - 1) / (64 * cut.ti)); g.tiles_n = (int32_t)((N + 64 * cut.ti - 1) / (64 * cut.ti));
   g.splits = cut.splits; g.per_split = cut.per_split;
+  g.padded = a.padded ? 1 : b.padded ? 2 : 0;
   return (int64_t)g.tiles_m * g.tiles_n > ((int64_t)1 << 23) ? SHAMPOO_ERR_UNSUPPORTED : SHAMPOO_OK;
 }
 // C = A B^T; `part`: scratch of gemm_cut's size
@@ -190,12 +192,11 @@ int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, co
   });
 }
 
-// A matrix of the caller as an operand: as it lies, or as planes in scratch (float32; rows that the products cannot read 16 bytes at
-// a time without passing their end).
-inline bool lies_well(int32_t dtype, int64_t cols, int64_t ld) { return dtype == SHAMPOO_GRAD_BF16 && cols % 8 == 0 && ld % 8 == 0 && ld <= MAX_LD; }
+// A matrix of the caller as an operand: as it lies, or as planes in scratch (float32; rows that the products cannot read to their
+// slabs' end: `along`, 64 where the columns are k in some product, otherwise 8).
 struct Source {
-  int32_t dtype; int64_t rows, cols, ld;
-  bool copy() const { return !lies_well(dtype, cols, ld); }
+  int32_t dtype; int64_t rows, cols, ld; int along;
+  bool copy() const { return dtype != SHAMPOO_GRAD_BF16 || cols % along != 0 || ld % 8 != 0 || ld > MAX_LD; }
   int planes() const { return dtype == SHAMPOO_GRAD_F32 ? 3 : 1; }
   int64_t ldp() const { return round_up(cols, 64); }
   uint16_t *take(Arena &a) const { return copy() ? a.take<uint16_t>((size_t)planes() * rows * ldp()) : nullptr; }
@@ -203,7 +204,7 @@ struct Source {
     if (!copy()) { o = {static_cast<const uint16_t *>(p), ld, 0, 1, lie}; return SHAMPOO_OK; }
     o = {scratch, ldp(), rows * ldp(), planes(), lie};
     PlanesArgs g = {};
-    g.x = p; g.ldx = ld; g.out = scratch; g.plane = o.plane; g.ld = o.ld; g.cols = (int32_t)cols; g.vec = vec_ok(p, ld, dtype);
+    g.rows = rows; g.x = p; g.ldx = ld; g.out = scratch; g.plane = o.plane; g.ld = o.ld; g.cols = (int32_t)cols; g.vec = vec_ok(p, ld, dtype);
     return dtype == SHAMPOO_GRAD_F32 ? launch_planes<FROM_F32>(g, 3, rows, s) : launch_planes<FROM_BF16>(g, 1, rows, s);
   }
 };
@@ -230,8 +231,8 @@ int cross_entropy_plan(const shampoo_cross_entropy &c, void *workspace, CrossEnt
   const bool out_in = c.w_layout == SHAMPOO_OUT_IN;
   const int64_t wcols = out_in ? c.features : c.classes, d = c.features, v = c.classes;
   if (c.ldx < d || c.ldw < wcols || (c.gradients && (c.lddx < d || c.lddw < wcols))) return SHAMPOO_ERR_SHAPE;
-  p.x = {c.dtype, c.rows, d, c.ldx};
-  p.w = {c.dtype, out_in ? v : d, wcols, c.ldw};
+  p.x = {c.dtype, c.rows, d, c.ldx, TG_BK};
+  p.w = {c.dtype, out_in ? v : d, wcols, c.ldw, TG_BK};
   // a float32 result needs g to float32 accuracy, and that needs the logits so
   p.planes = c.grad_dtype == SHAMPOO_GRAD_F32 ? 3 : c.has_bias ? 1 : 0;
   p.ldz = round_up(v, 64);
@@ -283,7 +284,7 @@ int weight_grad_plan(int64_t rows, int32_t in, int32_t out, int32_t activation, 
   if (rows > MAX_ROWS || in > MAX_FEATURES || out > MAX_OUT) return SHAMPOO_ERR_UNSUPPORTED;
   if (!dtype_ok(dtype) || !dtype_ok(grad_dtype) || activation < ACT_NONE || activation > ACT_SILU) return SHAMPOO_ERR_HYPER;
   if (dtype == SHAMPOO_GRAD_F32 && grad_dtype != SHAMPOO_GRAD_F32) return SHAMPOO_ERR_HYPER;
-  p.dy = {dtype, rows, out, lddy};
+  p.dy = {dtype, rows, out, lddy, 8};
   p.planes = activation == ACT_NONE ? 1 : grad_dtype == SHAMPOO_GRAD_F32 ? 3 : 1;
   p.ldp = round_up(in, 64);
   p.piece = std::min<int64_t>(round_up(std::max<int64_t>(rows, 1), PIECE_ROWS),
@@ -432,7 +433,7 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
     if (!dx && !dw && !dbias) continue;
     const SoftmaxGradArgs q = {p.z, p.ldz, p.stats, p.piece, span, p.lse, p.coef, targets + i0, p.g, p.piece * p.ldz,
                                dbias ? p.sums + k * p.ranges * v : nullptr, (int32_t)n, (int32_t)v, (int32_t)p.range_rows};
-    const dim3 grid((unsigned)((p.ldz / 8 + 255) / 256), (unsigned)((n + p.range_rows - 1) / p.range_rows));
+    const dim3 grid((unsigned)((p.ldz / 8 + 255) / 256), (unsigned)((round_up(n, TG_BK) + p.range_rows - 1) / p.range_rows));   // zeros behind the last row
     switch (p.planes) {
       case 0: softmax_grad_kernel<0><<<grid, 256, 0, s>>>(q); break;
       case 1: softmax_grad_kernel<1><<<grid, 256, 0, s>>>(q); break;
@@ -446,14 +447,14 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
       TRY(gemm(go, wt, n, d, v, {static_cast<char *>(dx) + i0 * c->lddx * size_of(c->dtype), c->lddx, c->dtype == SHAMPOO_GRAD_F32 ? STORE_F32 : STORE_BF16, nullptr, 0}, p.part, s));
     }
     if (dw) {
-      const Operand gt = {p.g, p.ldz, p.piece * p.ldz, p.grad_planes(), LIE_ROWS};
+      const Operand gt = {p.g, p.ldz, p.piece * p.ldz, p.grad_planes(), LIE_ROWS, true};
       xk.lie = LIE_ROWS;
       const Result out = piece_result(dw, c->lddw, c->grad_dtype, p.acc, p.w.cols, k == 0, k == p.pieces - 1);
       TRY(out_in ? gemm(gt, xk, v, d, n, out, p.part, s) : gemm(xk, gt, d, v, n, out, p.part, s));
     }
   }
   if (dbias) {
-    const int64_t last = c->rows - (p.pieces - 1) * p.piece, parts = (p.pieces - 1) * p.ranges + (last + p.range_rows - 1) / p.range_rows;
+    const int64_t last = c->rows - (p.pieces - 1) * p.piece, parts = (p.pieces - 1) * p.ranges + (round_up(last, TG_BK) + p.range_rows - 1) / p.range_rows;
     TRY(launch_partial_sums(p.sums, (int32_t)parts, (int32_t)v, 1, 0, v, dbias, v, s));
   }
   return SHAMPOO_OK;
@@ -547,13 +548,14 @@ int shampoo_checkpoint_weight_grad(const void *packed, size_t packed_bytes, int6
   g.out = p.xp; g.ld = p.ldp; g.cols = in; g.activation = activation;
   for (int64_t k = 0; k < p.pieces; ++k) {
     const int64_t i0 = k * p.piece, n = std::min(p.piece, rows - i0);
-    const Operand xo = {p.xp, p.ldp, p.piece * p.ldp, p.planes, LIE_ROWS};
+    const Operand xo = {p.xp, p.ldp, p.piece * p.ldp, p.planes, LIE_ROWS, true};
     Operand dk = dyo;
     dk.p += i0 * dyo.ld;
     g.p = packed_view(packed, rows, in);
     g.p.codes += i0 * g.p.pitch; g.p.exps += i0 * (g.p.pitch / 32);
     g.plane = xo.plane;
-    TRY(launch_planes<FROM_PACKED>(g, p.planes, n, s));
+    g.rows = n;
+    TRY(launch_planes<FROM_PACKED>(g, p.planes, round_up(n, TG_BK), s));     // zeros behind the last row
     const Result r = piece_result(dw, lddw, grad_dtype, p.acc, out_in ? in : out, k == 0, k == p.pieces - 1);
     TRY(out_in ? gemm(dk, xo, out, in, n, r, p.part, s) : gemm(xo, dk, in, out, n, r, p.part, s));
   }
