@@ -98,14 +98,13 @@ struct PackArgs {
   const void *x; int64_t ldx;
   Packed p;
   int64_t row0; uint32_t pieces, per_row;      // pieces of this grid; pitch / 8
-  int32_t vec;
 };
 template <typename T> __global__ __launch_bounds__(256) void checkpoint_pack_kernel(const PackArgs g) {
   const uint32_t i = blockIdx.x * 256u + threadIdx.x;
   const uint32_t r = min(i, g.pieces - 1) / g.per_row;
   const int c = (int)(min(i, g.pieces - 1) - r * g.per_row) * 8;
   const int64_t row = g.row0 + r;
-  const f32x8 x = load8(static_cast<const T *>(g.x) + row * g.ldx, c, g.p.cols, g.vec);
+  const f32x8 x = load8(static_cast<const T *>(g.x) + row * g.ldx, c, g.p.cols);
   uint32_t byte;
   const uint2 w = pack8(x, byte);                // per_row is a multiple of 4: a group never straddles rows or wavefronts
   if (i >= g.pieces) return;
@@ -119,7 +118,7 @@ struct UnpackArgs {
   const void *dy; int64_t lddy;                // GRAD
   void *y; int64_t ldy;
   int64_t row0; uint32_t pieces, per_row;
-  int32_t vec, activation;
+  int32_t activation;
 };
 template <typename T, bool GRAD> __global__ __launch_bounds__(256) void checkpoint_unpack_kernel(const UnpackArgs g) {
   const uint32_t i = blockIdx.x * 256u + threadIdx.x;
@@ -130,14 +129,14 @@ template <typename T, bool GRAD> __global__ __launch_bounds__(256) void checkpoi
   if (c >= g.p.cols) return;
   f32x8 x = packed_load8(g.p, row, c);
   if constexpr (GRAD) {
-    const f32x8 d = load8(static_cast<const T *>(g.dy) + row * g.lddy, c, g.p.cols, g.vec);
+    const f32x8 d = load8(static_cast<const T *>(g.dy) + row * g.lddy, c, g.p.cols);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x.v[e] = d.v[e] * slope(x.v[e], g.activation);
   } else if (g.activation != ACT_NONE) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x.v[e] = activate(x.v[e], g.activation);
   }
-  store8(static_cast<T *>(g.y) + row * g.ldy, c, g.p.cols, g.vec, x);
+  store8(static_cast<T *>(g.y) + row * g.ldy, c, g.p.cols, x);
 }
 
 // a(x) of a checkpoint, or a matrix in memory (float32 or bf16, any alignment), as PLANES bf16 planes [plane][rows][ld], ld a
@@ -146,7 +145,7 @@ struct PlanesArgs {
   Packed p; const void *x; int64_t ldx;        // one of the two
   uint16_t *out; int64_t plane, ld;
   int64_t rows, row0; uint32_t pieces, per_row;      // ld / 8
-  int32_t cols, vec, activation;
+  int32_t cols, activation;
 };
 enum { FROM_PACKED = 0, FROM_F32 = 1, FROM_BF16 = 2 };
 template <int FROM, int PLANES> __global__ __launch_bounds__(256) void planes_kernel(const PlanesArgs g) {
@@ -167,9 +166,9 @@ template <int FROM, int PLANES> __global__ __launch_bounds__(256) void planes_ke
       for (int e = 0; e < 8; ++e) if (c + e >= g.cols) x.v[e] = 0.f;
     }
   } else if constexpr (FROM == FROM_F32) {
-    x = load8(static_cast<const float *>(g.x) + row * g.ldx, c, g.cols, g.vec);
+    x = load8(static_cast<const float *>(g.x) + row * g.ldx, c, g.cols);
   } else {
-    x = load8(static_cast<const uint16_t *>(g.x) + row * g.ldx, c, g.cols, g.vec);
+    x = load8(static_cast<const uint16_t *>(g.x) + row * g.ldx, c, g.cols);
   }
   uint16_t q[8][PLANES];
 #pragma unroll
@@ -184,7 +183,7 @@ template <int FROM, int PLANES> __global__ __launch_bounds__(256) void planes_ke
 }
 
 // out[j] = sum over rows of x[i][j], in an order that does not depend on the launch: workgroup (j / 256, part) sums its rows,
-// partial_sum_kernel the parts.
+// join_sums_kernel the parts.
 template <typename T> __global__ __launch_bounds__(256) void column_sums_kernel(const T *x, int64_t ldx, int64_t rows, int32_t cols, int64_t per_part, float *out) {
   const int j = blockIdx.x * 256 + threadIdx.x;
   if (j >= cols) return;
@@ -194,15 +193,6 @@ template <typename T> __global__ __launch_bounds__(256) void column_sums_kernel(
     if constexpr (sizeof(T) == 4) s += x[i * ldx + j]; else s += bf16_value(x[i * ldx + j]);
   }
   out[(int64_t)blockIdx.y * cols + j] = s;
-}
-// out[o][j] = sum over p < parts of in[o][p][j]
-__global__ __launch_bounds__(256) void partial_sum_kernel(const float *in, int32_t parts, int32_t cols, int64_t in_stride, int64_t part_stride, float *out, int64_t out_stride) {
-  const int j = blockIdx.x * 256 + threadIdx.x;
-  if (j >= cols) return;
-  const float *p = in + blockIdx.y * in_stride + j;
-  float s = 0.f;
-  for (int i = 0; i < parts; ++i) s += p[i * part_stride];
-  out[blockIdx.y * out_stride + j] = s;
 }
 
 }  // namespace shampoo

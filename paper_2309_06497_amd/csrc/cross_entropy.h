@@ -85,7 +85,7 @@ template <int PLANES> __global__ __launch_bounds__(256) void softmax_grad_kernel
         p.v[e] = q == 65535u ? 0.f : __builtin_amdgcn_exp2f(top - (float)q * (1.f / LOGIT_STEPS));
       }
     } else {
-      p = load8(g.z + at, 0, 8, true);
+      p = load8(g.z + at, 0, 8);
 #pragma unroll
       for (int e = 0; e < 8; ++e) p.v[e] = expf(p.v[e] - lse);
     }

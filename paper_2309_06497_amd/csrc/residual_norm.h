@@ -8,7 +8,10 @@
 //   dr = dr' + inv (g - n mean(g n) - mean(g)),  g = dh w_pre, n the normalised r'  (RMS: without mean(g))
 //   du = alpha gate dr,  df the same of norm_post,  dgate = sum alpha u dr,  dw = sum dy n,  db = sum dy
 //
-// A row is held in registers, in pieces of eight neighbouring features per thread, so that memory is read and written once.
+// A team of 64, 256 or 512 threads holds a row in registers, in pieces of eight neighbouring features per thread, so that memory
+// is read and written once: bound by memory (about 30 vector operations per element against 10 ... 20 bytes).  Up to 2048 features a
+// team is one wavefront and its sums need no barrier.  Backward a team has several rows, the next one on its way while
+// one is worked on, and keeps the sums for the weights in registers; the teams' sums are joined in order by a second launch.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -26,31 +29,50 @@ struct ResidualNormArgs {
   void *r_out, *h; int64_t ld_r_out, ldh;              // forward
   const void *dr_out, *dh; int64_t ld_dr_out, ld_dh;   // backward
   void *dr, *df; int64_t ld_dr, ld_df;
-  float *dgate;                                        // written here where a workgroup has whole groups
-  float *partial;                                      // [workgroups][5][cols]: dgate, dw_post, db_post, dw_pre, db_pre
-  int64_t rows, group_rows, chunk_rows;                // rows per gate, per workgroup
-  int32_t chunks_per_group;                            // 0: a workgroup has whole groups
+  float *dgate;                                        // written here where a team has whole groups
+  float *partial;                                      // [teams][5][cols]: dgate, dw_post, dw_pre, db_post, db_pre
+  int64_t rows, group_rows, chunk_rows, teams;         // rows per gate, per team of the backward pass
+  int32_t chunks_per_group;                            // 0: a team has whole groups
   int32_t cols, post, pre;
   float epsilon, alpha;
-  int32_t vec;                                         // rows start on multiples of 16 bytes
 };
+enum { SUM_GATE = 0, SUM_W_POST = 1, SUM_W_PRE = 2, SUM_B_POST = 3, SUM_B_PRE = 4, SUMS = 5 };
 
+// The sum over a wavefront, in every lane: within rows of 16 lanes, then across them.
+__device__ __forceinline__ float wave_sum(float x) {
+#define ADD_DPP(CTRL, ROWS) x += __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), CTRL, ROWS, 0xf, false))
+  ADD_DPP(0x111, 0xf); ADD_DPP(0x112, 0xf); ADD_DPP(0x114, 0xf); ADD_DPP(0x118, 0xf);      // row_shr 1, 2, 4, 8
+  ADD_DPP(0x142, 0xa); ADD_DPP(0x143, 0xc);                                                // row_bcast 15, 31
+#undef ADD_DPP
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 63));
+}
 // sums over the threads of a row, for all of them; `slot` (two floats per wavefront): one that no other sum uses at the time
 template <int TPR> __device__ __forceinline__ void row_sums(float &x, float &y, float *slot) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) { x += __shfl_xor(x, o, 64); y += __shfl_xor(y, o, 64); }
-  if constexpr (TPR == 256) {
+  x = wave_sum(x); y = wave_sum(y);
+  if constexpr (TPR > 64) {
     const int wave = threadIdx.x >> 6;
     if ((threadIdx.x & 63) == 0) { slot[2 * wave] = x; slot[2 * wave + 1] = y; }
     __syncthreads();
     x = (slot[0] + slot[2]) + (slot[4] + slot[6]);
     y = (slot[1] + slot[3]) + (slot[5] + slot[7]);
+    if constexpr (TPR == 512) {
+      x += (slot[8] + slot[10]) + (slot[12] + slot[14]);
+      y += (slot[9] + slot[11]) + (slot[13] + slot[15]);
+    }
   }
 }
+constexpr int NORM_SLOT = 16;       // floats of a slot
 
-// x becomes (x - mean) / sqrt(...), the returned value one over the root.  Padding stays zero.
-template <int TPR, int NJ> __device__ __forceinline__ float normalise(f32x8 (&x)[NJ], int kind, int cols, float eps, int at, float *slot) {
-  const float per = 1.f / (float)cols;
+// Where a thread's pieces of a row are: piece j at column (at + TPR j) 8.
+template <int TPR, int NJ> struct RowPieces {
+  int at, cols;
+  __device__ __forceinline__ int column(int j) const { return (at + TPR * j) * 8; }
+  __device__ __forceinline__ bool has(int j, int e) const { return column(j) + e < cols; }
+};
+
+// x becomes (x - mean) / sqrt(...), the returned value one over the root.  Padding stays zero.  Uses slots 0 and 1.
+template <int TPR, int NJ> __device__ __forceinline__ float normalise(f32x8 (&x)[NJ], const RowPieces<TPR, NJ> &at, int kind, float eps, float *slot) {
+  const float per = 1.f / (float)at.cols;
   float s = 0.f, unused = 0.f;
   if (kind == NORM_LAYER) {
 #pragma unroll
@@ -62,14 +84,14 @@ template <int TPR, int NJ> __device__ __forceinline__ float normalise(f32x8 (&x)
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[j].v[e] = (at + TPR * j) * 8 + e < cols ? x[j].v[e] - mean : 0.f;
+      for (int e = 0; e < 8; ++e) x[j].v[e] = at.has(j, e) ? x[j].v[e] - mean : 0.f;
     s = 0.f;
   }
 #pragma unroll
   for (int j = 0; j < NJ; ++j)
 #pragma unroll
     for (int e = 0; e < 8; ++e) s += x[j].v[e] * x[j].v[e];
-  row_sums<TPR>(s, unused, slot + 8);
+  row_sums<TPR>(s, unused, slot + NORM_SLOT);
   const float inv = rsqrtf(s * per + eps);
 #pragma unroll
   for (int j = 0; j < NJ; ++j)
@@ -78,135 +100,210 @@ template <int TPR, int NJ> __device__ __forceinline__ float normalise(f32x8 (&x)
   return inv;
 }
 
-template <typename T, int TPR, int NJ> __global__ __launch_bounds__(256) void residual_norm_forward_kernel(const ResidualNormArgs g) {
-  __shared__ float red[32];
-  const int at = threadIdx.x % TPR;
-  const int64_t i = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-  if (i >= g.rows) return;                             // a whole wavefront; workgroups of one row have one
+template <typename T, int TPR, int NJ>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void residual_norm_forward_kernel(const ResidualNormArgs g) {
+  constexpr int TEAMS = TPR > 256 ? 1 : 256 / TPR;
+  __shared__ float red[4 * NORM_SLOT];
+  const RowPieces<TPR, NJ> at = {(int)threadIdx.x % TPR, g.cols};
+  const int64_t i = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TPR;
+  if (i >= g.rows) return;                             // a whole team
   f32x8 f[NJ], r[NJ];
   const T *pr = static_cast<const T *>(g.r) + i * g.ldr, *pf = static_cast<const T *>(g.f) + i * g.ldf;
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) f[j] = load8(pf, (at + TPR * j) * 8, g.cols, g.vec);
+  for (int j = 0; j < NJ; ++j) f[j] = load8(pf, at.column(j), g.cols);
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) r[j] = load8(pr, (at + TPR * j) * 8, g.cols, g.vec);
+  for (int j = 0; j < NJ; ++j) r[j] = load8(pr, at.column(j), g.cols);
   if (g.f8.codes) {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) { packed_store8(g.f8, i, (at + TPR * j) * 8, f[j]); packed_store8(g.r8, i, (at + TPR * j) * 8, r[j]); }
+    for (int j = 0; j < NJ; ++j) { packed_store8(g.f8, i, at.column(j), f[j]); packed_store8(g.r8, i, at.column(j), r[j]); }
   }
-  if (g.post != NORM_NONE) normalise<TPR, NJ>(f, g.post, g.cols, g.epsilon, at, red);
-  const float *gate = g.gate ? g.gate + i / g.group_rows * g.cols : nullptr;
+  if (g.post != NORM_NONE) {
+    normalise(f, at, g.post, g.epsilon, red);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const f32x8 w = load8(g.w_post, at.column(j), g.cols);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[j].v[e] *= w.v[e];
+    }
+    if (g.b_post) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const f32x8 b = load8(g.b_post, at.column(j), g.cols);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[j].v[e] += b.v[e];
+      }
+    }
+  }
+  if (g.gate) {
+    const float *gate = g.gate + i / g.group_rows * g.cols;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const f32x8 w = load8(gate, at.column(j), g.cols);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[j].v[e] *= w.v[e];
+    }
+  }
   T *po = static_cast<T *>(g.r_out) + i * g.ld_r_out;
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
-    const int c = (at + TPR * j) * 8;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (c + e >= g.cols) continue;
-      float u = f[j].v[e];
-      if (g.post != NORM_NONE) { u *= g.w_post[c + e]; if (g.b_post) u += g.b_post[c + e]; }
-      if (gate) u *= gate[c + e];
-      r[j].v[e] += g.alpha * u;
-    }
-    store8(po, c, g.cols, g.vec, r[j]);
+    for (int e = 0; e < 8; ++e) r[j].v[e] += g.alpha * f[j].v[e];
+    store8(po, at.column(j), g.cols, r[j]);
   }
   if (g.pre == NORM_NONE) return;
-  normalise<TPR, NJ>(r, g.pre, g.cols, g.epsilon, at, red + 16);
+  normalise(r, at, g.pre, g.epsilon, red + 2 * NORM_SLOT);
   T *ph = static_cast<T *>(g.h) + i * g.ldh;
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
-    const int c = (at + TPR * j) * 8;
+    const f32x8 w = load8(g.w_pre, at.column(j), g.cols);
+    f32x8 b = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+    if (g.b_pre) b = load8(g.b_pre, at.column(j), g.cols);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (c + e >= g.cols) continue;
-      r[j].v[e] *= g.w_pre[c + e];
-      if (g.b_pre) r[j].v[e] += g.b_pre[c + e];
-    }
-    store8(ph, c, g.cols, g.vec, r[j]);
+    for (int e = 0; e < 8; ++e) r[j].v[e] = r[j].v[e] * w.v[e] + b.v[e];
+    store8(ph, at.column(j), g.cols, r[j]);
   }
 }
 
-// dx of a norm in place of dy w (in `d`): inv (d - n mean(d n) - mean(d))
-template <int NJ> __device__ __forceinline__ void norm_gradient(f32x8 (&d)[NJ], const f32x8 (&n)[NJ], float inv, int kind, int cols, float *slot) {
+// dx of a norm in place of dy w (in `d`): inv (d - n mean(d n) - mean(d)).  Padding of d may become anything.
+template <int TPR, int NJ> __device__ __forceinline__ void norm_gradient(f32x8 (&d)[NJ], const f32x8 (&n)[NJ], float inv, int kind, int cols, float *slot) {
   float sn = 0.f, s = 0.f;
 #pragma unroll
   for (int j = 0; j < NJ; ++j)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) { sn += d[j].v[e] * n[j].v[e]; s += d[j].v[e]; }
-  row_sums<256>(sn, s, slot);
+    for (int e = 0; e < 8; ++e) sn += d[j].v[e] * n[j].v[e];
+  if (kind == NORM_LAYER) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += d[j].v[e];
+  }
+  row_sums<TPR>(sn, s, slot);
   const float per = 1.f / (float)cols;
-  sn *= per; s = kind == NORM_LAYER ? s * per : 0.f;
+  sn *= -per * inv; s *= -per * inv;
 #pragma unroll
   for (int j = 0; j < NJ; ++j)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) d[j].v[e] = inv * (d[j].v[e] - n[j].v[e] * sn - s);
+    for (int e = 0; e < 8; ++e) d[j].v[e] = inv * d[j].v[e] + (n[j].v[e] * sn + s);
 }
 
-// A workgroup has chunk_rows rows of one group, or of whole groups, and their sums for the weights.
-template <typename T, bool PACKED, int NJ> __global__ __launch_bounds__(256) void residual_norm_backward_kernel(const ResidualNormArgs g) {
-  __shared__ float red[2][56];
-  const int at = threadIdx.x;
+// What a row brings, as it comes from memory: r and f as eight values, or eight codes and their exponent byte in the same registers.
+template <typename T, int NJ> struct RawRow {
+  Raw8<T> r[NJ], f[NJ], dr_out[NJ], dh[NJ];
+  uint32_t r_byte[NJ], f_byte[NJ];
+  template <typename At> __device__ __forceinline__ void load(const ResidualNormArgs &g, const At &at, int64_t i) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int c = at.column(j);
+      if (g.r8.codes) { codes(g.f8, i, c, f[j], f_byte[j]); codes(g.r8, i, c, r[j], r_byte[j]); }
+      else {
+        f[j] = raw_load8(static_cast<const T *>(g.f) + i * g.ldf, c, g.cols);
+        r[j] = raw_load8(static_cast<const T *>(g.r) + i * g.ldr, c, g.cols);
+      }
+      if (g.dh) dh[j] = raw_load8(static_cast<const T *>(g.dh) + i * g.ld_dh, c, g.cols);
+      if (g.dr_out) dr_out[j] = raw_load8(static_cast<const T *>(g.dr_out) + i * g.ld_dr_out, c, g.cols);
+    }
+  }
+  __device__ __forceinline__ void codes(const Packed &p, int64_t i, int c, Raw8<T> &x, uint32_t &byte) {
+    uint2 w = make_uint2(0u, 0u);
+    byte = 0u;
+    if (c < p.cols) {
+      w = *reinterpret_cast<const uint2 *>(p.codes + i * p.pitch + c);
+      byte = p.exps[i * (p.pitch >> 5) + (c >> 5)];
+    }
+    x.u[0][0] = w.x; x.u[0][1] = w.y;
+  }
+  // a group that is not finite reads NaN in the padding too
+  template <typename At> static __device__ __forceinline__ f32x8 values(const Raw8<T> &x, uint32_t byte, bool packed, const At &at, int j) {
+    if (!packed) return expand8(x);
+    f32x8 v = unpack8(make_uint2(x.u[0][0], x.u[0][1]), value_per_code(byte));
+    if (at.column(j) + 8 > at.cols) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v.v[e] = at.has(j, e) ? v.v[e] : 0.f;
+    }
+    return v;
+  }
+};
+
+// A team has chunk_rows rows of one group, or of whole groups, and their sums for the weights.  BIAS: of biases too.
+template <typename T, int TPR, int NJ, bool BIAS>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void residual_norm_backward_kernel(const ResidualNormArgs g) {
+  constexpr int TEAMS = TPR > 256 ? 1 : 256 / TPR, NSUM = BIAS ? 5 : 3;
+  __shared__ float red[2][6 * NORM_SLOT];
+  const RowPieces<TPR, NJ> at = {(int)threadIdx.x % TPR, g.cols};
+  const int64_t team = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TPR;
+  if (team >= g.teams) return;
   int64_t i0, i1;
   if (g.chunks_per_group) {
-    const int64_t group = blockIdx.x / g.chunks_per_group, k = blockIdx.x - group * g.chunks_per_group;
+    const int64_t group = team / g.chunks_per_group, k = team - group * g.chunks_per_group;
     i0 = group * g.group_rows + k * g.chunk_rows;
     i1 = min(i0 + g.chunk_rows, (group + 1) * g.group_rows);
   } else {
-    i0 = (int64_t)blockIdx.x * g.chunk_rows;
+    i0 = team * g.chunk_rows;
     i1 = min(i0 + g.chunk_rows, g.rows);
   }
-  f32x8 sum[5][NJ];
+  f32x8 sum[NSUM][NJ];
 #pragma unroll
-  for (int q = 0; q < 5; ++q)
+  for (int q = 0; q < NSUM; ++q)
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[q][j].v[e] = 0.f;
   int64_t left = g.chunks_per_group ? 0 : g.group_rows, group = g.gate ? i0 / g.group_rows : 0;   // rows until the group's sum is written
+  RawRow<T, NJ> raw;
+  if (i0 < i1) raw.load(g, at, i0);
   for (int64_t i = i0; i < i1; ++i) {
     float *slot = red[i & 1];
-    f32x8 r[NJ], f[NJ], u[NJ], d[NJ];
     const float *gate = g.gate ? g.gate + group * g.cols : nullptr;
+    f32x8 r[NJ], f[NJ], d[NJ], over[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const int c = (at + 256 * j) * 8;
-      if constexpr (PACKED) {
-        f32x8 zero = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
-        f[j] = c < g.cols ? packed_load8(g.f8, i, c) : zero;
-        r[j] = c < g.cols ? packed_load8(g.r8, i, c) : zero;
-        // a group that is not finite reads NaN in the padding too
-#pragma unroll
-        for (int e = 0; e < 8; ++e) if (c + e >= g.cols) { f[j].v[e] = 0.f; r[j].v[e] = 0.f; }
-      } else {
-        f[j] = load8(static_cast<const T *>(g.f) + i * g.ldf, c, g.cols, g.vec);
-        r[j] = load8(static_cast<const T *>(g.r) + i * g.ldr, c, g.cols, g.vec);
-      }
+      f[j] = raw.values(raw.f[j], raw.f_byte[j], g.r8.codes != nullptr, at, j);
+      r[j] = raw.values(raw.r[j], raw.r_byte[j], g.r8.codes != nullptr, at, j);
+      if (g.dh) d[j] = expand8(raw.dh[j]);
+      if (g.dr_out) over[j] = expand8(raw.dr_out[j]);
     }
-    const float inv_f = g.post != NORM_NONE ? normalise<256, NJ>(f, g.post, g.cols, g.epsilon, at, slot) : 1.f;
+    if (i + 1 < i1) raw.load(g, at, i + 1);
+    const float inv_f = g.post != NORM_NONE ? normalise(f, at, g.post, g.epsilon, slot) : 1.f;
+    // u = norm_post(f), formed again where it is needed
+    auto block = [&](int j) {
+      f32x8 u = f[j];
+      if (g.post != NORM_NONE) {
+        const f32x8 w = load8(g.w_post, at.column(j), g.cols);
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int c = (at + 256 * j) * 8;
+        for (int e = 0; e < 8; ++e) u.v[e] *= w.v[e];
+        if (BIAS && g.b_post) {
+          const f32x8 b = load8(g.b_post, at.column(j), g.cols);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        u[j].v[e] = f[j].v[e];
-        if (c + e >= g.cols) continue;
-        if (g.post != NORM_NONE) { u[j].v[e] *= g.w_post[c + e]; if (g.b_post) u[j].v[e] += g.b_post[c + e]; }
-        r[j].v[e] += g.alpha * (gate ? gate[c + e] * u[j].v[e] : u[j].v[e]);
-      }
-    }
-    if (g.pre != NORM_NONE) {
-      const float inv = normalise<256, NJ>(r, g.pre, g.cols, g.epsilon, at, slot + 16);
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        const int c = (at + 256 * j) * 8;
-        d[j] = load8(static_cast<const T *>(g.dh) + i * g.ld_dh, c, g.cols, g.vec);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          sum[3][j].v[e] += d[j].v[e] * r[j].v[e];
-          sum[4][j].v[e] += d[j].v[e];
-          d[j].v[e] *= c + e < g.cols ? g.w_pre[c + e] : 0.f;
+          for (int e = 0; e < 8; ++e) u.v[e] += b.v[e];
         }
       }
-      norm_gradient<NJ>(d, r, inv, g.pre, g.cols, slot + 32);
+      return u;
+    };
+    if (g.pre != NORM_NONE) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const f32x8 u = block(j);
+        if (gate) {
+          const f32x8 w = load8(gate, at.column(j), g.cols);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) r[j].v[e] += g.alpha * w.v[e] * u.v[e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) r[j].v[e] += g.alpha * u.v[e];
+        }
+      }
+      const float inv = normalise(r, at, g.pre, g.epsilon, slot + 2 * NORM_SLOT);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const f32x8 w = load8(g.w_pre, at.column(j), g.cols);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          sum[SUM_W_PRE][j].v[e] += d[j].v[e] * r[j].v[e];
+          if constexpr (BIAS) sum[SUM_B_PRE][j].v[e] += d[j].v[e];
+          d[j].v[e] *= w.v[e];
+        }
+      }
+      norm_gradient<TPR, NJ>(d, r, inv, g.pre, g.cols, slot + 4 * NORM_SLOT);
     } else {
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
@@ -215,54 +312,81 @@ template <typename T, bool PACKED, int NJ> __global__ __launch_bounds__(256) voi
     }
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const int c = (at + 256 * j) * 8;
       if (g.dr_out) {
-        const f32x8 x = load8(static_cast<const T *>(g.dr_out) + i * g.ld_dr_out, c, g.cols, g.vec);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[j].v[e] += x.v[e];
+        for (int e = 0; e < 8; ++e) d[j].v[e] += over[j].v[e];
       }
-      if (g.dr) store8(static_cast<T *>(g.dr) + i * g.ld_dr, c, g.cols, g.vec, d[j]);
+      store8(static_cast<T *>(g.dr) + i * g.ld_dr, at.column(j), g.cols, d[j]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (c + e >= g.cols) { d[j].v[e] = 0.f; continue; }
-        d[j].v[e] *= g.alpha;
-        sum[0][j].v[e] += d[j].v[e] * u[j].v[e];
-        if (gate) d[j].v[e] *= gate[c + e];
-        if (g.post != NORM_NONE) {
-          sum[1][j].v[e] += d[j].v[e] * f[j].v[e];
-          sum[2][j].v[e] += d[j].v[e];
-          d[j].v[e] *= g.w_post[c + e];
+      for (int e = 0; e < 8; ++e) d[j].v[e] = at.has(j, e) ? d[j].v[e] * g.alpha : 0.f;
+      if (gate) {
+        const f32x8 w = load8(gate, at.column(j), g.cols), u = block(j);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { sum[SUM_GATE][j].v[e] += d[j].v[e] * u.v[e]; d[j].v[e] *= w.v[e]; }
+      }
+      if (g.post != NORM_NONE) {
+        const f32x8 w = load8(g.w_post, at.column(j), g.cols);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          sum[SUM_W_POST][j].v[e] += d[j].v[e] * f[j].v[e];
+          if constexpr (BIAS) sum[SUM_B_POST][j].v[e] += d[j].v[e];
+          d[j].v[e] *= w.v[e];
         }
       }
     }
-    if (g.post != NORM_NONE) norm_gradient<NJ>(d, f, inv_f, g.post, g.cols, slot + 40);
+    if (g.post != NORM_NONE) norm_gradient<TPR, NJ>(d, f, inv_f, g.post, g.cols, slot + 5 * NORM_SLOT);
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) store8(static_cast<T *>(g.df) + i * g.ld_df, (at + 256 * j) * 8, g.cols, g.vec, d[j]);
-    if (g.dgate && left && --left == 0) {
+    for (int j = 0; j < NJ; ++j) store8(static_cast<T *>(g.df) + i * g.ld_df, at.column(j), g.cols, d[j]);
+    if (left && --left == 0) {
+      if (g.dgate) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) store8(g.dgate + group * g.cols, at.column(j), g.cols, sum[SUM_GATE][j]);
+      }
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int c = (at + 256 * j) * 8 + e;
-          if (c < g.cols) g.dgate[group * g.cols + c] = sum[0][j].v[e];
-          sum[0][j].v[e] = 0.f;
-        }
+        for (int e = 0; e < 8; ++e) sum[SUM_GATE][j].v[e] = 0.f;
       left = g.group_rows;
       ++group;
     }
   }
-  float *out = g.partial + (int64_t)blockIdx.x * 5 * g.cols;
+  float *out = g.partial + team * SUMS * g.cols;
 #pragma unroll
-  for (int q = 0; q < 5; ++q) {
-    if (q == 0 ? !g.gate || !g.chunks_per_group : q == 1 ? g.post == NORM_NONE : q == 2 ? g.post != NORM_LAYER : q == 3 ? g.pre == NORM_NONE : g.pre != NORM_LAYER) continue;
+  for (int q = 0; q < NSUM; ++q) {
+    const bool wanted = q == SUM_GATE ? g.gate && g.chunks_per_group : q == SUM_W_POST ? g.post != NORM_NONE : q == SUM_W_PRE ? g.pre != NORM_NONE : true;
+    if (!wanted) continue;
 #pragma unroll
-    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int c = (at + 256 * j) * 8 + e;
-        if (c < g.cols) out[q * g.cols + c] = sum[q][j].v[e];
-      }
+    for (int j = 0; j < NJ; ++j) store8(out + q * g.cols, at.column(j), g.cols, sum[q][j]);
   }
+}
+
+// Sums over teams or parts: out_k[o][j] = sum over p < parts of in[k][o][p][j], k = blockIdx.z, o = blockIdx.y, in an order that
+// does not depend on the launch.  A workgroup has 64 columns and 16 threads for each.
+struct JoinSumsArgs {
+  const float *in[SUMS]; float *out[SUMS];
+  int64_t output_stride, part_stride, out_stride;
+  int32_t parts, cols;
+};
+__global__ __launch_bounds__(1024) void join_sums_kernel(const JoinSumsArgs g) {
+  __shared__ float part[16][64];
+  const int c = threadIdx.x & 63, k = threadIdx.x >> 6, j = blockIdx.x * 64 + c;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (j < g.cols) {
+    const float *p = g.in[blockIdx.z] + blockIdx.y * g.output_stride + j;
+    int i = k;
+    for (; i + 48 < g.parts; i += 64) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) s[q] += p[(i + 16 * q) * g.part_stride];
+    }
+    for (; i < g.parts; i += 16) s[0] += p[i * g.part_stride];
+  }
+  part[k][c] = (s[0] + s[1]) + (s[2] + s[3]);
+  __syncthreads();
+  if (k != 0 || j >= g.cols) return;
+  float t = 0.f;
+#pragma unroll
+  for (int q = 0; q < 16; ++q) t += part[q][c];
+  g.out[blockIdx.z][blockIdx.y * g.out_stride + j] = t;
 }
 
 }  // namespace shampoo

@@ -46,7 +46,7 @@ struct TrainGemmArgs {
   int32_t tiles_m, tiles_n, splits, per_split;   // slabs of the whole sequence (products x ceil(K / 64)) per split
   void *c; int64_t ldc, c_split;           // c_split: from the result of a split to the next
   const float *add; int64_t ldadd;         // C += add (float32; may be c itself) or nullptr
-  int32_t store, vec;                      // vec: rows of c (and add) start on multiples of 16 bytes
+  int32_t store;
   // logits: z = C + bias; per row and span (32 TI columns): the largest z and sum of exp(z - largest); the target's z
   const float *bias; const int64_t *targets;
   float2 *stats; int64_t stats_ld;         // [span][row]
@@ -329,12 +329,12 @@ __global__ __launch_bounds__(256, TI == 4 ? 1 : 2) void train_gemm_kernel(const 
           *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(g.c) + (int64_t)out * g.ldc + col) = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
           if (!LOGITS && g.add) {
-            const f32x8 old = load8(g.add + (int64_t)out * g.ldadd, col, g.N, g.vec);
+            const f32x8 old = load8(g.add + (int64_t)out * g.ldadd, col, g.N);
 #pragma unroll
             for (int e = 0; e < 8; ++e) z.v[e] += old.v[e];
           }
-          if (!LOGITS && g.store == STORE_BF16) store8(static_cast<uint16_t *>(g.c) + (int64_t)out * g.ldc, col, limit, g.vec, z);
-          else store8(static_cast<float *>(g.c) + split * g.c_split + (int64_t)out * g.ldc, col, limit, g.vec, z);
+          if (!LOGITS && g.store == STORE_BF16) store8(static_cast<uint16_t *>(g.c) + (int64_t)out * g.ldc, col, limit, z);
+          else store8(static_cast<float *>(g.c) + split * g.c_split + (int64_t)out * g.ldc, col, limit, z);
         }
       }
     }
@@ -346,7 +346,7 @@ struct JoinArgs {
   const float *part; int64_t stride; int32_t splits;
   void *c; int64_t ldc; const float *add; int64_t ldadd;
   int64_t row0; uint32_t pieces, per_row;
-  int32_t cols, pitch, store, vec;
+  int32_t cols, pitch, store;
 };
 __global__ __launch_bounds__(256) void train_join_kernel(const JoinArgs g) {
   const uint32_t i = blockIdx.x * 256u + threadIdx.x;
@@ -354,19 +354,19 @@ __global__ __launch_bounds__(256) void train_join_kernel(const JoinArgs g) {
   const uint32_t r = i / g.per_row;
   const int c = (int)(i - r * g.per_row) * 8;
   const int64_t row = g.row0 + r;
-  f32x8 s = load8(g.part + row * g.pitch, c, g.pitch, true);
+  f32x8 s = load8(g.part + row * g.pitch, c, g.pitch);
   for (int k = 1; k < g.splits; ++k) {
-    const f32x8 x = load8(g.part + k * g.stride + row * g.pitch, c, g.pitch, true);
+    const f32x8 x = load8(g.part + k * g.stride + row * g.pitch, c, g.pitch);
 #pragma unroll
     for (int e = 0; e < 8; ++e) s.v[e] += x.v[e];
   }
   if (g.add) {
-    const f32x8 x = load8(g.add + row * g.ldadd, c, g.cols, g.vec);
+    const f32x8 x = load8(g.add + row * g.ldadd, c, g.cols);
 #pragma unroll
     for (int e = 0; e < 8; ++e) s.v[e] += x.v[e];
   }
-  if (g.store == STORE_BF16) store8(static_cast<uint16_t *>(g.c) + row * g.ldc, c, g.cols, g.vec, s);
-  else store8(static_cast<float *>(g.c) + row * g.ldc, c, g.cols, g.vec, s);
+  if (g.store == STORE_BF16) store8(static_cast<uint16_t *>(g.c) + row * g.ldc, c, g.cols, s);
+  else store8(static_cast<float *>(g.c) + row * g.ldc, c, g.cols, s);
 }
 
 }  // namespace shampoo

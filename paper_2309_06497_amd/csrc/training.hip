@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "../../include/shampoo.h"
 #include "checkpoint.h"
@@ -30,8 +31,6 @@ inline int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; 
 inline bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 inline bool dtype_ok(int32_t d) { return d == SHAMPOO_GRAD_F32 || d == SHAMPOO_GRAD_BF16; }
 inline int64_t size_of(int32_t d) { return d == SHAMPOO_GRAD_F32 ? 4 : 2; }
-// rows of `ld` elements from p on start on multiples of 16 bytes
-inline bool vec_ok(const void *p, int64_t ld, int32_t dtype) { return aligned(p, 16) && ld * size_of(dtype) % 16 == 0; }
 
 #define HIP_TRY(expr)                          \
   do {                                         \
@@ -92,12 +91,15 @@ template <int FROM> int launch_planes(PlanesArgs g, int planes, int64_t rows, hi
   });
 }
 
-// out[o][j] = sum of `parts` rows of in
-int launch_partial_sums(const float *in, int32_t parts, int32_t cols, int32_t outputs, int64_t in_stride, int64_t part_stride, float *out,
-                        int64_t out_stride, hipStream_t s) {
-  for (int32_t o = 0; o < outputs; o += 65535) {
-    partial_sum_kernel<<<dim3((cols + 255) / 256, std::min(outputs - o, 65535)), 256, 0, s>>>(in + o * in_stride, parts, cols, in_stride, part_stride,
-                                                                                             out + o * out_stride, out_stride);
+// outs[k][o][j] = sum of `parts` rows of ins[k][o], for `count` of them
+int launch_join_sums(const float *const *ins, float *const *outs, int count, int32_t parts, int32_t cols, int64_t outputs, int64_t output_stride,
+                     int64_t part_stride, int64_t out_stride, hipStream_t s) {
+  if (count == 0) return SHAMPOO_OK;
+  JoinSumsArgs g = {};
+  g.output_stride = output_stride; g.part_stride = part_stride; g.out_stride = out_stride; g.parts = parts; g.cols = cols;
+  for (int64_t o = 0; o < outputs; o += 65535) {
+    for (int k = 0; k < count; ++k) { g.in[k] = ins[k] + o * output_stride; g.out[k] = outs[k] + o * out_stride; }
+    join_sums_kernel<<<dim3((cols + 63) / 64, (unsigned)std::min<int64_t>(outputs - o, 65535), count), 1024, 0, s>>>(g);
     HIP_TRY(hipGetLastError());
   }
   return SHAMPOO_OK;
@@ -174,18 +176,17 @@ int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, co
   const GemmCut cut = gemm_cut(M, N, K, a.planes, b.planes, false);
   TrainGemmArgs g;
   TRY(gemm_args(a, b, M, N, K, cut, g));
-  const bool vec = vec_ok(c.c, c.ldc, c.store == STORE_F32 ? SHAMPOO_GRAD_F32 : SHAMPOO_GRAD_BF16) && (!c.add || vec_ok(c.add, c.ldadd, SHAMPOO_GRAD_F32));
   if (cut.splits == 1) {
-    g.c = c.c; g.ldc = c.ldc; g.add = c.add; g.ldadd = c.ldadd; g.store = c.store; g.vec = vec;
+    g.c = c.c; g.ldc = c.ldc; g.add = c.add; g.ldadd = c.ldadd; g.store = c.store;
   } else {
-    g.c = part; g.ldc = round_up(N, 8); g.c_split = M * g.ldc; g.store = STORE_F32; g.vec = 1;
+    g.c = part; g.ldc = round_up(N, 8); g.c_split = M * g.ldc; g.store = STORE_F32;
   }
   if (cut.ti == 4) gemm_launch<4, false>(g, a.lie, b.lie, s); else gemm_launch<2, false>(g, a.lie, b.lie, s);
   HIP_TRY(hipGetLastError());
   if (cut.splits == 1) return SHAMPOO_OK;
   JoinArgs j = {};
   j.part = part; j.stride = g.c_split; j.splits = cut.splits; j.c = c.c; j.ldc = c.ldc; j.add = c.add; j.ldadd = c.ldadd;
-  j.cols = (int32_t)N; j.pitch = (int32_t)g.ldc; j.store = c.store; j.vec = vec; j.per_row = (uint32_t)(g.ldc / 8);
+  j.cols = (int32_t)N; j.pitch = (int32_t)g.ldc; j.store = c.store; j.per_row = (uint32_t)(g.ldc / 8);
   return by_rows(M, j.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
     j.row0 = r; j.pieces = pieces;
     train_join_kernel<<<grid, 256, 0, s>>>(j);
@@ -204,7 +205,7 @@ struct Source {
     if (!copy()) { o = {static_cast<const uint16_t *>(p), ld, 0, 1, lie}; return SHAMPOO_OK; }
     o = {scratch, ldp(), rows * ldp(), planes(), lie};
     PlanesArgs g = {};
-    g.rows = rows; g.x = p; g.ldx = ld; g.out = scratch; g.plane = o.plane; g.ld = o.ld; g.cols = (int32_t)cols; g.vec = vec_ok(p, ld, dtype);
+    g.rows = rows; g.x = p; g.ldx = ld; g.out = scratch; g.plane = o.plane; g.ld = o.ld; g.cols = (int32_t)cols;
     return dtype == SHAMPOO_GRAD_F32 ? launch_planes<FROM_F32>(g, 3, rows, s) : launch_planes<FROM_BF16>(g, 1, rows, s);
   }
 };
@@ -318,7 +319,7 @@ Result piece_result(void *dw, int64_t lddw, int32_t grad_dtype, float *acc, int6
 // ---------------------------------------------------------------------------
 // Residual norm
 // ---------------------------------------------------------------------------
-constexpr int64_t NORM_CHUNKS = 1024;                      // workgroups of the backward pass
+constexpr int64_t NORM_CHUNKS = 1024;                      // teams of the backward pass
 int residual_norm_ok(const shampoo_residual_norm &c) {
   if (c.rows < 0 || c.cols < 1 || c.gates < 0) return SHAMPOO_ERR_SHAPE;
   if (c.rows > MAX_ROWS || c.cols > MAX_NORM_COLS) return SHAMPOO_ERR_UNSUPPORTED;
@@ -338,7 +339,7 @@ ResidualNormArgs residual_norm_args(const shampoo_residual_norm &c) {
   return g;
 }
 struct NormChunks { int64_t rows, chunks; int32_t per_group; };
-// A workgroup of the backward pass has rows of one group, or several whole groups where there are more than workgroups.
+// A team of the backward pass has rows of one group, or several whole groups where there are more than teams.
 NormChunks norm_chunks(const shampoo_residual_norm &c) {
   const int64_t groups = std::max<int64_t>(1, c.gates), group_rows = c.rows / groups;
   if (groups >= NORM_CHUNKS) {
@@ -350,24 +351,32 @@ NormChunks norm_chunks(const shampoo_residual_norm &c) {
   return {rows, per * groups, (int32_t)per};
 }
 
+// Threads for a row: a wavefront up to 2048 features (32 a lane, sums without barriers), above that as many as keep a row in registers.
+template <typename F> void norm_variant(int32_t cols, F &&launch) {
+#define VARIANT(TPR, NJ) launch(std::integral_constant<int, TPR>(), std::integral_constant<int, NJ>())
+  if (cols <= 512) VARIANT(64, 1);
+  else if (cols <= 1024) VARIANT(64, 2);
+  else if (cols <= 2048) VARIANT(64, 4);
+  else if (cols <= 4096) VARIANT(256, 2);
+  else if (cols <= 8192) VARIANT(256, 4);
+  else VARIANT(512, 4);
+#undef VARIANT
+}
 template <typename T> int launch_norm_forward(const ResidualNormArgs &g, hipStream_t s) {
-#define FORWARD(TPR, NJ) residual_norm_forward_kernel<T, TPR, NJ><<<dim3((unsigned)((g.rows + 256 / TPR - 1) / (256 / TPR))), 256, 0, s>>>(g)
-  if (g.cols <= 512) FORWARD(64, 1);
-  else if (g.cols <= 1024) FORWARD(64, 2);
-  else if (g.cols <= 2048) FORWARD(64, 4);
-  else if (g.cols <= 4096) FORWARD(256, 2);
-  else if (g.cols <= 8192) FORWARD(256, 4);
-  else FORWARD(256, 8);
-#undef FORWARD
+  norm_variant(g.cols, [&](auto tpr, auto nj) {
+    constexpr int TPR = decltype(tpr)::value, TEAMS = TPR > 256 ? 1 : 256 / TPR;
+    residual_norm_forward_kernel<T, TPR, decltype(nj)::value><<<dim3((unsigned)((g.rows + TEAMS - 1) / TEAMS)), TEAMS * TPR, 0, s>>>(g);
+  });
   HIP_TRY(hipGetLastError());
   return SHAMPOO_OK;
 }
-template <typename T, bool PACKED> int launch_norm_backward(const ResidualNormArgs &g, int64_t chunks, hipStream_t s) {
-  const dim3 grid((unsigned)chunks);
-  if (g.cols <= 2048) residual_norm_backward_kernel<T, PACKED, 1><<<grid, 256, 0, s>>>(g);
-  else if (g.cols <= 4096) residual_norm_backward_kernel<T, PACKED, 2><<<grid, 256, 0, s>>>(g);
-  else if (g.cols <= 8192) residual_norm_backward_kernel<T, PACKED, 4><<<grid, 256, 0, s>>>(g);
-  else residual_norm_backward_kernel<T, PACKED, 8><<<grid, 256, 0, s>>>(g);
+template <typename T> int launch_norm_backward(const ResidualNormArgs &g, bool bias, hipStream_t s) {
+  norm_variant(g.cols, [&](auto tpr, auto nj) {
+    constexpr int TPR = decltype(tpr)::value, NJ = decltype(nj)::value, TEAMS = TPR > 256 ? 1 : 256 / TPR;
+    const dim3 grid((unsigned)((g.teams + TEAMS - 1) / TEAMS));
+    if (bias) residual_norm_backward_kernel<T, TPR, NJ, true><<<grid, TEAMS * TPR, 0, s>>>(g);
+    else residual_norm_backward_kernel<T, TPR, NJ, false><<<grid, TEAMS * TPR, 0, s>>>(g);
+  });
   HIP_TRY(hipGetLastError());
   return SHAMPOO_OK;
 }
@@ -421,7 +430,7 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
     const int32_t span = 32 * cut.ti;
     TrainGemmArgs z;
     TRY(gemm_args(xk, wo, n, v, d, cut, z));
-    z.c = p.planes ? static_cast<void *>(p.z) : p.g; z.ldc = p.ldz; z.vec = 1;
+    z.c = p.planes ? static_cast<void *>(p.z) : p.g; z.ldc = p.ldz;
     z.store = !c->gradients ? STORE_NO_LOGITS : p.planes ? STORE_LOGITS_F32 : STORE_LOGITS_U16;
     z.bias = bias; z.targets = targets + i0; z.stats = p.stats; z.stats_ld = p.piece; z.target_z = p.target_z;
     if (cut.ti == 4) gemm_launch<4, true>(z, xk.lie, wo.lie, s); else gemm_launch<2, true>(z, xk.lie, wo.lie, s);
@@ -455,7 +464,8 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
   }
   if (dbias) {
     const int64_t last = c->rows - (p.pieces - 1) * p.piece, parts = (p.pieces - 1) * p.ranges + (round_up(last, TG_BK) + p.range_rows - 1) / p.range_rows;
-    TRY(launch_partial_sums(p.sums, (int32_t)parts, (int32_t)v, 1, 0, v, dbias, v, s));
+    const float *in = p.sums;
+    TRY(launch_join_sums(&in, &dbias, 1, (int32_t)parts, (int32_t)v, 1, 0, v, v, s));
   }
   return SHAMPOO_OK;
 }
@@ -474,7 +484,7 @@ int shampoo_checkpoint_pack(const void *x, int32_t dtype, int64_t rows, int32_t 
   if (ldx < cols) return SHAMPOO_ERR_SHAPE;
   hipStream_t s = static_cast<hipStream_t>(stream);
   PackArgs g = {};
-  g.x = x; g.ldx = ldx; g.p = packed_view(packed, rows, cols); g.vec = vec_ok(x, ldx, dtype);
+  g.x = x; g.ldx = ldx; g.p = packed_view(packed, rows, cols);
   g.per_row = (uint32_t)g.p.pitch / 8;
   return by_rows(rows, g.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
     g.row0 = r; g.pieces = pieces;
@@ -491,7 +501,7 @@ int shampoo_checkpoint_unpack(const void *packed, size_t packed_bytes, int64_t r
   if (ldy < cols) return SHAMPOO_ERR_SHAPE;
   hipStream_t s = static_cast<hipStream_t>(stream);
   UnpackArgs g = {};
-  g.p = packed_view(packed, rows, cols); g.y = y; g.ldy = ldy; g.activation = activation; g.vec = vec_ok(y, ldy, dtype);
+  g.p = packed_view(packed, rows, cols); g.y = y; g.ldy = ldy; g.activation = activation;
   g.per_row = (uint32_t)g.p.pitch / 8;
   return by_rows(rows, g.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
     g.row0 = r; g.pieces = pieces;
@@ -509,7 +519,6 @@ int shampoo_checkpoint_activation_grad(const void *packed, size_t packed_bytes, 
   hipStream_t s = static_cast<hipStream_t>(stream);
   UnpackArgs g = {};
   g.p = packed_view(packed, rows, cols); g.dy = dy; g.lddy = lddy; g.y = dx; g.ldy = lddx; g.activation = activation;
-  g.vec = vec_ok(dy, lddy, dtype) && vec_ok(dx, lddx, dtype);
   g.per_row = (uint32_t)g.p.pitch / 8;
   return by_rows(rows, g.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
     g.row0 = r; g.pieces = pieces;
@@ -564,7 +573,8 @@ int shampoo_checkpoint_weight_grad(const void *packed, size_t packed_bytes, int6
     if (dtype == SHAMPOO_GRAD_F32) column_sums_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float *>(dy), lddy, rows, out, p.part_rows, p.sums);
     else column_sums_kernel<uint16_t><<<grid, 256, 0, s>>>(static_cast<const uint16_t *>(dy), lddy, rows, out, p.part_rows, p.sums);
     HIP_TRY(hipGetLastError());
-    TRY(launch_partial_sums(p.sums, (int32_t)p.parts, out, 1, 0, out, db, out, s));
+    const float *in = p.sums;
+    TRY(launch_join_sums(&in, &db, 1, (int32_t)p.parts, out, 1, 0, out, out, s));
   }
   return SHAMPOO_OK;
 }
@@ -583,14 +593,13 @@ int shampoo_residual_norm_forward(const shampoo_residual_norm *c, const void *r,
   ResidualNormArgs g = residual_norm_args(*c);
   g.r = r; g.ldr = ldr; g.f = f; g.ldf = ldf; g.r_out = r_out; g.ld_r_out = ld_r_out; g.h = h; g.ldh = ldh;
   g.r8 = packed_view(packed_r, c->rows, c->cols); g.f8 = packed_view(packed_f, c->rows, c->cols);
-  g.vec = vec_ok(r, ldr, c->dtype) && vec_ok(f, ldf, c->dtype) && vec_ok(r_out, ld_r_out, c->dtype) && (c->pre == NORM_NONE || vec_ok(h, ldh, c->dtype));
   hipStream_t s = static_cast<hipStream_t>(stream);
   return c->dtype == SHAMPOO_GRAD_F32 ? launch_norm_forward<float>(g, s) : launch_norm_forward<uint16_t>(g, s);
 }
 
 size_t shampoo_residual_norm_backward_workspace_bytes(const shampoo_residual_norm *c) {
   if (!c || residual_norm_ok(*c) != SHAMPOO_OK) return 0;
-  return align_up((size_t)norm_chunks(*c).chunks * 5 * c->cols * sizeof(float));
+  return align_up((size_t)norm_chunks(*c).chunks * SUMS * c->cols * sizeof(float));
 }
 
 int shampoo_residual_norm_backward(const shampoo_residual_norm *c, int32_t packed, const void *r, int64_t ldr, const void *f, int64_t ldf,
@@ -619,25 +628,25 @@ int shampoo_residual_norm_backward(const shampoo_residual_norm *c, int32_t packe
   const NormChunks k = norm_chunks(*c);
   TRY(workspace_ok(workspace, workspace_bytes, shampoo_residual_norm_backward_workspace_bytes(c)));
   ResidualNormArgs g = residual_norm_args(*c);
-  g.vec = vec_ok(dr, ld_dr, c->dtype) && vec_ok(df, ld_df, c->dtype) && (!dr_out || vec_ok(dr_out, ld_dr_out, c->dtype)) &&
-          (!dh || vec_ok(dh, ld_dh, c->dtype)) && (packed || (vec_ok(r, ldr, c->dtype) && vec_ok(f, ldf, c->dtype)));
   g.r = r; g.f = f; g.ldr = ldr; g.ldf = ldf;
   if (packed) { g.r8 = packed_view(r, c->rows, cols); g.f8 = packed_view(f, c->rows, cols); }
   g.dr_out = dr_out; g.ld_dr_out = ld_dr_out; g.dh = dh; g.ld_dh = ld_dh; g.dr = dr; g.ld_dr = ld_dr; g.df = df; g.ld_df = ld_df;
   g.dgate = k.per_group ? nullptr : dgate;
   g.partial = static_cast<float *>(workspace);
-  g.chunk_rows = k.rows; g.chunks_per_group = k.per_group;
-  if (c->dtype == SHAMPOO_GRAD_F32) {
-    TRY(packed ? launch_norm_backward<float, true>(g, k.chunks, s) : launch_norm_backward<float, false>(g, k.chunks, s));
-  } else {
-    TRY(packed ? launch_norm_backward<uint16_t, true>(g, k.chunks, s) : launch_norm_backward<uint16_t, false>(g, k.chunks, s));
+  g.chunk_rows = k.rows; g.chunks_per_group = k.per_group; g.teams = k.chunks;
+  const bool bias = db_post || db_pre || g.b_post;
+  TRY(c->dtype == SHAMPOO_GRAD_F32 ? launch_norm_backward<float>(g, bias, s) : launch_norm_backward<uint16_t>(g, bias, s));
+  const int64_t stride = SUMS * (int64_t)cols;
+  const float *ins[SUMS]; float *outs[SUMS];
+  if (dgate && k.per_group) {
+    ins[0] = g.partial; outs[0] = dgate;
+    TRY(launch_join_sums(ins, outs, 1, k.per_group, cols, c->gates, k.per_group * stride, stride, cols, s));
   }
-  const int64_t stride = 5 * (int64_t)cols;
-  if (dgate && k.per_group)
-    TRY(launch_partial_sums(g.partial, k.per_group, cols, (int32_t)c->gates, k.per_group * stride, stride, dgate, cols, s));
-  float *outs[4] = {dw_post, db_post, dw_pre, db_pre};
-  for (int q = 0; q < 4; ++q)
-    if (outs[q]) TRY(launch_partial_sums(g.partial + (q + 1) * cols, (int32_t)k.chunks, cols, 1, 0, stride, outs[q], cols, s));
+  float *const wanted[SUMS] = {nullptr, dw_post, dw_pre, db_post, db_pre};
+  int count = 0;
+  for (int q = 0; q < SUMS; ++q)
+    if (wanted[q]) { ins[count] = g.partial + q * cols; outs[count++] = wanted[q]; }
+  TRY(launch_join_sums(ins, outs, count, (int32_t)k.chunks, cols, 1, 0, stride, cols, s));
   return SHAMPOO_OK;
 }
 

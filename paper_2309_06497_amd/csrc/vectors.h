@@ -16,41 +16,58 @@ __device__ __forceinline__ uint32_t bf16_pair(float x, float y) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(pair{x, y}, bpair));
 }
 
-// Elements c ... c + 7 of a row of n, zeros past its end.  vec: the row starts on a multiple of 16 bytes (c % 8 == 0), so that
-// a whole piece is read or written 16 bytes at a time.
-template <typename T> __device__ __forceinline__ f32x8 load8(const T *row, int c, int n, bool vec) {
-  f32x8 r;
-  if (vec && c + 8 <= n) {
-    if constexpr (sizeof(T) == 4) {
-      const float4 a = *reinterpret_cast<const float4 *>(row + c), b = *reinterpret_cast<const float4 *>(row + c + 4);
-      r = {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
-    } else {
-      const uint4 u = *reinterpret_cast<const uint4 *>(row + c);
-      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+// Rows may start at any multiple of their element: the memory takes 16-byte accesses that are not aligned (a row that is costs
+// a cache line less per 64 lanes).
+typedef uint32_t rows_u32x4 __attribute__((ext_vector_type(4)));
+template <typename T> struct RowVector;
+template <> struct RowVector<float> { typedef rows_u32x4 type __attribute__((aligned(4))); };
+template <> struct RowVector<uint16_t> { typedef rows_u32x4 type __attribute__((aligned(2))); };
+
+// Elements c ... c + 7 of a row of n as they are in memory, zeros past its end.
+template <typename T> struct Raw8 { rows_u32x4 u[sizeof(T) / 2]; };
+template <typename T> __device__ __forceinline__ Raw8<T> raw_load8(const T *row, int c, int n) {
+  Raw8<T> r;
+  if (c + 8 <= n) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) { r.v[2 * e] = __uint_as_float(w[e] << 16); r.v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u); }
-    }
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k) r.u[k] = reinterpret_cast<const typename RowVector<T>::type *>(row + c)[k];
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      r.v[e] = 0.f;
-      if (c + e < n) { if constexpr (sizeof(T) == 4) r.v[e] = row[c + e]; else r.v[e] = bf16_value(row[c + e]); }
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k) r.u[k] = rows_u32x4{0u, 0u, 0u, 0u};
+    if (c < n) {
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (c + e < n) {
+          if constexpr (sizeof(T) == 4) r.u[e >> 2][e & 3] = __float_as_uint(row[c + e]);
+          else r.u[0][e >> 1] |= (uint32_t)row[c + e] << (16 * (e & 1));
+        }
     }
   }
   return r;
 }
-template <typename T> __device__ __forceinline__ void store8(T *row, int c, int n, bool vec, const f32x8 &x) {
-  if (vec && c + 8 <= n) {
-    if constexpr (sizeof(T) == 4) {
-      *reinterpret_cast<float4 *>(row + c) = make_float4(x.v[0], x.v[1], x.v[2], x.v[3]);
-      *reinterpret_cast<float4 *>(row + c + 4) = make_float4(x.v[4], x.v[5], x.v[6], x.v[7]);
-    } else {
-      *reinterpret_cast<uint4 *>(row + c) = make_uint4(bf16_pair(x.v[0], x.v[1]), bf16_pair(x.v[2], x.v[3]),
-                                                       bf16_pair(x.v[4], x.v[5]), bf16_pair(x.v[6], x.v[7]));
-    }
+template <typename T> __device__ __forceinline__ f32x8 expand8(const Raw8<T> &r) {
+  f32x8 x;
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x.v[e] = __uint_as_float(r.u[e >> 2][e & 3]);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < 4; ++e) { x.v[2 * e] = __uint_as_float(r.u[0][e] << 16); x.v[2 * e + 1] = __uint_as_float(r.u[0][e] & 0xffff0000u); }
+  }
+  return x;
+}
+template <typename T> __device__ __forceinline__ f32x8 load8(const T *row, int c, int n) { return expand8(raw_load8(row, c, n)); }
+template <typename T> __device__ __forceinline__ void store8(T *row, int c, int n, const f32x8 &x) {
+  if (c + 8 <= n) {
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+      rows_u32x4 u;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { if constexpr (sizeof(T) == 4) u[e] = __float_as_uint(x.v[4 * k + e]); else u[e] = bf16_pair(x.v[2 * e], x.v[2 * e + 1]); }
+      reinterpret_cast<typename RowVector<T>::type *>(row + c)[k] = u;
+    }
+  } else if (c < n) {
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
       if (c + e < n) { if constexpr (sizeof(T) == 4) row[c + e] = x.v[e]; else row[c + e] = bf16_bits(x.v[e]); }
   }
 }
