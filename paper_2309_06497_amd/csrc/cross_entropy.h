@@ -63,46 +63,59 @@ struct SoftmaxGradArgs {
   float *sums;                       // [ranges][classes] column sums of g, or nullptr
   int32_t rows, classes, per_range;
 };
-// PLANES = 0: one plane, in the place of 16-bit logits
+// PLANES = 0: one plane, in the place of 16-bit logits.  Four rows are on their way together.
 template <int PLANES> __global__ __launch_bounds__(256) void softmax_grad_kernel(const SoftmaxGradArgs g) {
-  constexpr int OUT = PLANES ? PLANES : 1;
+  constexpr int OUT = PLANES ? PLANES : 1, AHEAD = 4;
   const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
   if (c >= g.ldg) return;
-  const int i0 = blockIdx.y * g.per_range, i1 = min((g.rows + 63) & ~63, i0 + g.per_range);
+  const int end = (g.rows + 63) & ~63, i0 = blockIdx.y * g.per_range, i1 = min(end, i0 + g.per_range);
+  const int64_t span = (int64_t)(c / g.span) * g.stats_ld;
   f32x8 sum = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
-  for (int i = i0; i < i1; ++i) {
-    const bool there = i < g.rows;
-    const float lse = there ? g.lse[i] : 0.f, k = there ? g.coef[i] : 0.f;
-    const int64_t t = (there ? g.targets[i] : 0) - c, at = (int64_t)i * g.ldg + c;
-    f32x8 p;
-    if constexpr (PLANES == 0) {
-      const uint4 u = *reinterpret_cast<const uint4 *>(g.out + at);
-      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-      const float top = (g.stats[(int64_t)(c / g.span) * g.stats_ld + i].x - lse) * LOG2_E;
+  for (int first = i0; first < i1; first += AHEAD) {
+    Raw8<float> z[PLANES ? AHEAD : 1];
+    Raw8<uint16_t> q16[PLANES ? 1 : AHEAD];
+    float lse[AHEAD], k[AHEAD], top[AHEAD];
+    int64_t t[AHEAD];
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      const int i = min(first + a, i1 - 1);
+      const int64_t at = (int64_t)i * g.ldg + c;
+      const bool there = i < g.rows;
+      lse[a] = there ? g.lse[i] : 0.f; k[a] = there ? g.coef[i] : 0.f; t[a] = (there ? g.targets[i] : 0) - c;
+      if constexpr (PLANES == 0) { q16[a] = raw_load8(g.out + at, 0, 8); top[a] = there ? g.stats[span + i].x : 0.f; }
+      else z[a] = raw_load8(g.z + at, 0, 8);
+    }
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      if (first + a >= i1) break;
+      f32x8 p;
+      if constexpr (PLANES == 0) {
+        const float from = (top[a] - lse[a]) * LOG2_E;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t q = (q16[a].u[0][e >> 1] >> (16 * (e & 1))) & 0xffffu;
+          p.v[e] = q == 65535u ? 0.f : __builtin_amdgcn_exp2f(from - (float)q * (1.f / LOGIT_STEPS));
+        }
+      } else {
+        p = expand8(z[a]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p.v[e] = expf(p.v[e] - lse[a]);
+      }
+      uint16_t q[8][OUT];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const uint32_t q = (w[e >> 1] >> (16 * (e & 1))) & 0xffffu;
-        p.v[e] = q == 65535u ? 0.f : __builtin_amdgcn_exp2f(top - (float)q * (1.f / LOGIT_STEPS));
+        float x = 0.f;
+        if (k[a] != 0.f && c + e < g.classes && lse[a] != -INFINITY) x = k[a] * (p.v[e] - (t[a] == e ? 1.f : 0.f));
+        sum.v[e] += x;
+        bf16_planes_of<OUT>(x, q[e]);
       }
-    } else {
-      p = load8(g.z + at, 0, 8);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p.v[e] = expf(p.v[e] - lse);
-    }
-    uint16_t q[8][OUT];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float x = 0.f;
-      if (k != 0.f && c + e < g.classes && lse != -INFINITY) x = k * (p.v[e] - (t == e ? 1.f : 0.f));
-      sum.v[e] += x;
-      bf16_planes_of<OUT>(x, q[e]);
-    }
-#pragma unroll
-    for (int s = 0; s < OUT; ++s) {
-      uint4 w;
-      w.x = q[0][s] | (uint32_t)q[1][s] << 16; w.y = q[2][s] | (uint32_t)q[3][s] << 16;
-      w.z = q[4][s] | (uint32_t)q[5][s] << 16; w.w = q[6][s] | (uint32_t)q[7][s] << 16;
-      *reinterpret_cast<uint4 *>(g.out + s * g.plane + at) = w;
+      for (int s = 0; s < OUT; ++s) {
+        uint4 w;
+        w.x = q[0][s] | (uint32_t)q[1][s] << 16; w.y = q[2][s] | (uint32_t)q[3][s] << 16;
+        w.z = q[4][s] | (uint32_t)q[5][s] << 16; w.w = q[6][s] | (uint32_t)q[7][s] << 16;
+        *reinterpret_cast<uint4 *>(g.out + s * g.plane + (int64_t)(first + a) * g.ldg + c) = w;
+      }
     }
   }
   if (!g.sums) return;

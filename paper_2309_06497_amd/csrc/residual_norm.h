@@ -8,10 +8,13 @@
 //   dr = dr' + inv (g - n mean(g n) - mean(g)),  g = dh w_pre, n the normalised r'  (RMS: without mean(g))
 //   du = alpha gate dr,  df the same of norm_post,  dgate = sum alpha u dr,  dw = sum dy n,  db = sum dy
 //
-// A team of 64, 256 or 512 threads holds a row in registers, in pieces of eight neighbouring features per thread, so that memory
-// is read and written once: bound by memory (about 30 vector operations per element against 10 ... 20 bytes).  Up to 2048 features a
-// team is one wavefront and its sums need no barrier.  Backward a team has several rows, the next one on its way while
-// one is worked on, and keeps the sums for the weights in registers; the teams' sums are joined in order by a second launch.
+// A team of threads holds a row in registers, in pieces of eight neighbouring features per thread, so that memory is read and
+// written once: bound by memory, beside about 35 vector operations per element.  Forward a team is one wavefront up to
+// 2048 features: its sums need no barrier, and other wavefronts hide its latency.  Backward a team has several rows, the next one on its way
+// while one is worked on, and keeps weights and the sums for their gradients in registers, so a thread has one piece
+// (up to 4096 features): 16384 x 2048 in bf16 from checkpoints 90 us, 223 with a wavefront per row and four pieces a thread (477 registers), 141 with the
+// weights read for every row; 768 teams of 256 threads, three per CU, and 111 us with 1024.  The teams' sums are joined in order by a second launch.
+// 16384 x 2048, bf16: forward with checkpoints 68 us (337 MB, 5.0 TB/s), backward 90 + 7 us (337 MB, 3.7 TB/s).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -53,8 +56,9 @@ template <int TPR> __device__ __forceinline__ void row_sums(float &x, float &y, 
     const int wave = threadIdx.x >> 6;
     if ((threadIdx.x & 63) == 0) { slot[2 * wave] = x; slot[2 * wave + 1] = y; }
     __syncthreads();
-    x = (slot[0] + slot[2]) + (slot[4] + slot[6]);
-    y = (slot[1] + slot[3]) + (slot[5] + slot[7]);
+    x = slot[0] + slot[2];
+    y = slot[1] + slot[3];
+    if constexpr (TPR >= 256) { x += slot[4] + slot[6]; y += slot[5] + slot[7]; }
     if constexpr (TPR == 512) {
       x += (slot[8] + slot[10]) + (slot[12] + slot[14]);
       y += (slot[9] + slot[11]) + (slot[13] + slot[15]);
@@ -224,10 +228,24 @@ template <typename T, int NJ> struct RawRow {
   }
 };
 
+// Rows of weights, kept in registers over a team's rows where a thread has one piece, and otherwise read where they are used.
+template <int NJ> struct NormWeight {
+  static constexpr bool KEEP = NJ == 1;
+  f32x8 kept;
+  const float *p;
+  template <typename At> __device__ __forceinline__ void set(const float *w, const At &at) {
+    p = w;
+    if constexpr (KEEP) { if (w) kept = load8(w, at.column(0), at.cols); }
+  }
+  template <typename At> __device__ __forceinline__ f32x8 get(const At &at, int j) const {
+    if constexpr (KEEP) return kept; else return load8(p, at.column(j), at.cols);
+  }
+};
+
 // A team has chunk_rows rows of one group, or of whole groups, and their sums for the weights.  BIAS: of biases too.
 template <typename T, int TPR, int NJ, bool BIAS>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void residual_norm_backward_kernel(const ResidualNormArgs g) {
-  constexpr int TEAMS = TPR > 256 ? 1 : 256 / TPR, NSUM = BIAS ? 5 : 3;
+__global__ __launch_bounds__(TPR == 64 ? 256 : TPR, NJ == 1 && TPR <= 256 && sizeof(T) == 2 && !BIAS ? 3 : 1) void residual_norm_backward_kernel(const ResidualNormArgs g) {
+  constexpr int TEAMS = TPR == 64 ? 4 : 1, NSUM = BIAS ? 5 : 3;
   __shared__ float red[2][6 * NORM_SLOT];
   const RowPieces<TPR, NJ> at = {(int)threadIdx.x % TPR, g.cols};
   const int64_t team = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TPR;
@@ -249,18 +267,22 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void residual_norm_backward_
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[q][j].v[e] = 0.f;
   int64_t left = g.chunks_per_group ? 0 : g.group_rows, group = g.gate ? i0 / g.group_rows : 0;   // rows until the group's sum is written
+  NormWeight<NJ> w_post, b_post, w_pre, gate;
+  w_post.set(g.post != NORM_NONE ? g.w_post : nullptr, at); w_pre.set(g.pre != NORM_NONE ? g.w_pre : nullptr, at);
+  b_post.set(BIAS ? g.b_post : nullptr, at);
+  gate.set(g.gate ? g.gate + group * g.cols : nullptr, at);
   RawRow<T, NJ> raw;
   if (i0 < i1) raw.load(g, at, i0);
   for (int64_t i = i0; i < i1; ++i) {
     float *slot = red[i & 1];
-    const float *gate = g.gate ? g.gate + group * g.cols : nullptr;
-    f32x8 r[NJ], f[NJ], d[NJ], over[NJ];
+    f32x8 r[NJ], f[NJ], d[NJ];
+    Raw8<T> over[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       f[j] = raw.values(raw.f[j], raw.f_byte[j], g.r8.codes != nullptr, at, j);
       r[j] = raw.values(raw.r[j], raw.r_byte[j], g.r8.codes != nullptr, at, j);
       if (g.dh) d[j] = expand8(raw.dh[j]);
-      if (g.dr_out) over[j] = expand8(raw.dr_out[j]);
+      over[j] = raw.dr_out[j];
     }
     if (i + 1 < i1) raw.load(g, at, i + 1);
     const float inv_f = g.post != NORM_NONE ? normalise(f, at, g.post, g.epsilon, slot) : 1.f;
@@ -268,11 +290,11 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void residual_norm_backward_
     auto block = [&](int j) {
       f32x8 u = f[j];
       if (g.post != NORM_NONE) {
-        const f32x8 w = load8(g.w_post, at.column(j), g.cols);
+        const f32x8 w = w_post.get(at, j);
 #pragma unroll
         for (int e = 0; e < 8; ++e) u.v[e] *= w.v[e];
         if (BIAS && g.b_post) {
-          const f32x8 b = load8(g.b_post, at.column(j), g.cols);
+          const f32x8 b = b_post.get(at, j);
 #pragma unroll
           for (int e = 0; e < 8; ++e) u.v[e] += b.v[e];
         }
@@ -283,8 +305,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void residual_norm_backward_
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         const f32x8 u = block(j);
-        if (gate) {
-          const f32x8 w = load8(gate, at.column(j), g.cols);
+        if (g.gate) {
+          const f32x8 w = gate.get(at, j);
 #pragma unroll
           for (int e = 0; e < 8; ++e) r[j].v[e] += g.alpha * w.v[e] * u.v[e];
         } else {
@@ -295,7 +317,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void residual_norm_backward_
       const float inv = normalise(r, at, g.pre, g.epsilon, slot + 2 * NORM_SLOT);
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        const f32x8 w = load8(g.w_pre, at.column(j), g.cols);
+        const f32x8 w = w_pre.get(at, j);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           sum[SUM_W_PRE][j].v[e] += d[j].v[e] * r[j].v[e];
@@ -313,19 +335,20 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void residual_norm_backward_
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       if (g.dr_out) {
+        const f32x8 x = expand8(over[j]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[j].v[e] += over[j].v[e];
+        for (int e = 0; e < 8; ++e) d[j].v[e] += x.v[e];
       }
       store8(static_cast<T *>(g.dr) + i * g.ld_dr, at.column(j), g.cols, d[j]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) d[j].v[e] = at.has(j, e) ? d[j].v[e] * g.alpha : 0.f;
-      if (gate) {
-        const f32x8 w = load8(gate, at.column(j), g.cols), u = block(j);
+      if (g.gate) {
+        const f32x8 w = gate.get(at, j), u = block(j);
 #pragma unroll
         for (int e = 0; e < 8; ++e) { sum[SUM_GATE][j].v[e] += d[j].v[e] * u.v[e]; d[j].v[e] *= w.v[e]; }
       }
       if (g.post != NORM_NONE) {
-        const f32x8 w = load8(g.w_post, at.column(j), g.cols);
+        const f32x8 w = w_post.get(at, j);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           sum[SUM_W_POST][j].v[e] += d[j].v[e] * f[j].v[e];
@@ -348,6 +371,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void residual_norm_backward_
         for (int e = 0; e < 8; ++e) sum[SUM_GATE][j].v[e] = 0.f;
       left = g.group_rows;
       ++group;
+      if (g.gate && i + 1 < i1) gate.set(g.gate + group * g.cols, at);
     }
   }
   float *out = g.partial + team * SUMS * g.cols;

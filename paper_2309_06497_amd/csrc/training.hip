@@ -319,7 +319,13 @@ Result piece_result(void *dw, int64_t lddw, int32_t grad_dtype, float *acc, int6
 // ---------------------------------------------------------------------------
 // Residual norm
 // ---------------------------------------------------------------------------
-constexpr int64_t NORM_CHUNKS = 1024;                      // teams of the backward pass
+// Teams of the backward pass: what the GPU holds at a time (two or three wavefronts per SIMD by registers; 512 threads: one team per CU),
+// and at least four rows each, since every team leaves a row of sums.
+inline int norm_threads(int32_t cols) { return cols <= 512 ? 64 : cols <= 1024 ? 128 : cols <= 2048 ? 256 : 512; }
+inline int64_t norm_teams(const shampoo_residual_norm &c) {
+  const int64_t held = c.cols <= 2048 ? 3 * 256 * 256 / norm_threads(c.cols) : 256;
+  return std::max<int64_t>(1, std::min(held, c.rows / 4));
+}
 int residual_norm_ok(const shampoo_residual_norm &c) {
   if (c.rows < 0 || c.cols < 1 || c.gates < 0) return SHAMPOO_ERR_SHAPE;
   if (c.rows > MAX_ROWS || c.cols > MAX_NORM_COLS) return SHAMPOO_ERR_UNSUPPORTED;
@@ -342,17 +348,18 @@ struct NormChunks { int64_t rows, chunks; int32_t per_group; };
 // A team of the backward pass has rows of one group, or several whole groups where there are more than teams.
 NormChunks norm_chunks(const shampoo_residual_norm &c) {
   const int64_t groups = std::max<int64_t>(1, c.gates), group_rows = c.rows / groups;
-  if (groups >= NORM_CHUNKS) {
-    const int64_t each = (groups + NORM_CHUNKS - 1) / NORM_CHUNKS;
+  const int64_t teams = norm_teams(c);
+  if (groups >= teams) {
+    const int64_t each = (groups + teams - 1) / teams;
     return {each * group_rows, (groups + each - 1) / each, 0};
   }
-  const int64_t want = std::max<int64_t>(1, std::min(NORM_CHUNKS / groups, group_rows));
+  const int64_t want = std::max<int64_t>(1, std::min(teams / groups, group_rows));
   const int64_t rows = std::max<int64_t>(1, (group_rows + want - 1) / want), per = std::max<int64_t>(1, (group_rows + rows - 1) / rows);
   return {rows, per * groups, (int32_t)per};
 }
 
-// Threads for a row: a wavefront up to 2048 features (32 a lane, sums without barriers), above that as many as keep a row in registers.
-template <typename F> void norm_variant(int32_t cols, F &&launch) {
+// Threads and pieces of eight features per thread for a row (residual_norm.h)
+template <typename F> void norm_forward_variant(int32_t cols, F &&launch) {
 #define VARIANT(TPR, NJ) launch(std::integral_constant<int, TPR>(), std::integral_constant<int, NJ>())
   if (cols <= 512) VARIANT(64, 1);
   else if (cols <= 1024) VARIANT(64, 2);
@@ -360,10 +367,18 @@ template <typename F> void norm_variant(int32_t cols, F &&launch) {
   else if (cols <= 4096) VARIANT(256, 2);
   else if (cols <= 8192) VARIANT(256, 4);
   else VARIANT(512, 4);
+}
+template <typename F> void norm_backward_variant(int32_t cols, F &&launch) {
+  if (cols <= 512) VARIANT(64, 1);
+  else if (cols <= 1024) VARIANT(128, 1);
+  else if (cols <= 2048) VARIANT(256, 1);
+  else if (cols <= 4096) VARIANT(512, 1);
+  else if (cols <= 8192) VARIANT(512, 2);
+  else VARIANT(512, 4);
 #undef VARIANT
 }
 template <typename T> int launch_norm_forward(const ResidualNormArgs &g, hipStream_t s) {
-  norm_variant(g.cols, [&](auto tpr, auto nj) {
+  norm_forward_variant(g.cols, [&](auto tpr, auto nj) {
     constexpr int TPR = decltype(tpr)::value, TEAMS = TPR > 256 ? 1 : 256 / TPR;
     residual_norm_forward_kernel<T, TPR, decltype(nj)::value><<<dim3((unsigned)((g.rows + TEAMS - 1) / TEAMS)), TEAMS * TPR, 0, s>>>(g);
   });
@@ -371,8 +386,8 @@ template <typename T> int launch_norm_forward(const ResidualNormArgs &g, hipStre
   return SHAMPOO_OK;
 }
 template <typename T> int launch_norm_backward(const ResidualNormArgs &g, bool bias, hipStream_t s) {
-  norm_variant(g.cols, [&](auto tpr, auto nj) {
-    constexpr int TPR = decltype(tpr)::value, NJ = decltype(nj)::value, TEAMS = TPR > 256 ? 1 : 256 / TPR;
+  norm_backward_variant(g.cols, [&](auto tpr, auto nj) {
+    constexpr int TPR = decltype(tpr)::value, NJ = decltype(nj)::value, TEAMS = TPR == 64 ? 4 : 1;
     const dim3 grid((unsigned)((g.teams + TEAMS - 1) / TEAMS));
     if (bias) residual_norm_backward_kernel<T, TPR, NJ, true><<<grid, TEAMS * TPR, 0, s>>>(g);
     else residual_norm_backward_kernel<T, TPR, NJ, false><<<grid, TEAMS * TPR, 0, s>>>(g);
@@ -638,11 +653,12 @@ int shampoo_residual_norm_backward(const shampoo_residual_norm *c, int32_t packe
   TRY(c->dtype == SHAMPOO_GRAD_F32 ? launch_norm_backward<float>(g, bias, s) : launch_norm_backward<uint16_t>(g, bias, s));
   const int64_t stride = SUMS * (int64_t)cols;
   const float *ins[SUMS]; float *outs[SUMS];
-  if (dgate && k.per_group) {
+  const bool one_gate = c->gates == 1 && k.per_group;      // joined like the weights
+  if (dgate && k.per_group && !one_gate) {
     ins[0] = g.partial; outs[0] = dgate;
     TRY(launch_join_sums(ins, outs, 1, k.per_group, cols, c->gates, k.per_group * stride, stride, cols, s));
   }
-  float *const wanted[SUMS] = {nullptr, dw_post, dw_pre, db_post, db_pre};
+  float *const wanted[SUMS] = {one_gate ? dgate : nullptr, dw_post, dw_pre, db_post, db_pre};
   int count = 0;
   for (int q = 0; q < SUMS; ++q)
     if (wanted[q]) { ins[count] = g.partial + q * cols; outs[count++] = wanted[q]; }
