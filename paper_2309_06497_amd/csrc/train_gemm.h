@@ -256,7 +256,7 @@ __global__ __launch_bounds__(256, TI == 4 ? 1 : 2) void train_gemm_kernel(const 
 
   // A lane has row lane % 32 of every tile, columns 8 (v / 4) + 4 (lane / 32) + v % 4.  32 rows at a time go through LDS, which only
   // this wavefront touches.
-  constexpr int PITCH = SPAN + 4;                 // floats: rows are 16-byte aligned and four banks apart
+  constexpr int PITCH = SPAN + 4, PITCH16 = SPAN + 8;      // floats, 16-bit logits: rows are 16-byte aligned and four banks apart
   static_assert(4 * 32 * PITCH * 4 + (LOGITS ? 4 * SPAN * 4 : 0) <= 2 * STAGE, "LDS");
   float *buf = reinterpret_cast<float *>(smem) + wave * 32 * PITCH;
   const int half = lane >> 5, colw = col0 + wn * SPAN, roww = row0 + wm * SPAN;
@@ -264,70 +264,81 @@ __global__ __launch_bounds__(256, TI == 4 ? 1 : 2) void train_gemm_kernel(const 
   if constexpr (LOGITS) {
     for (int j = lane; j < SPAN; j += 64) bias[j] = colw + j >= g.N ? -INFINITY : g.bias ? g.bias[colw + j] : 0.f;   // no class there: probability 0
   }
+  [[maybe_unused]] const bool biased = g.bias || colw + SPAN > g.N;
 #pragma unroll
   for (int i = 0; i < TI; ++i) {
     const int row = roww + 32 * i + (lane & 31);
-    [[maybe_unused]] float largest = -INFINITY;
+    tg_wave_order();
     if constexpr (LOGITS) {
-      tg_wave_order();
+      if (biased) {
+#pragma unroll
+        for (int j = 0; j < TI; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float4 b = *reinterpret_cast<const float4 *>(bias + 32 * j + 8 * q + 4 * half);
+            acc[i][j][4 * q] += b.x; acc[i][j][4 * q + 1] += b.y; acc[i][j][4 * q + 2] += b.z; acc[i][j][4 * q + 3] += b.w;
+          }
+      }
+      float largest = -INFINITY;
 #pragma unroll
       for (int j = 0; j < TI; ++j)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float4 b = *reinterpret_cast<const float4 *>(bias + 32 * j + 8 * q + 4 * half);
-          const float add[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            acc[i][j][4 * q + e] += add[e];
-            largest = fmaxf(largest, acc[i][j][4 * q + e]);
-          }
-        }
+        for (int v = 0; v < 16; v += 2) largest = fmaxf(largest, fmaxf(acc[i][j][v], acc[i][j][v + 1]));
       largest = fmaxf(largest, __shfl_xor(largest, 32, 64));
       const float base = largest == -INFINITY ? 0.f : largest;
-      float sum = 0.f;
       const int64_t t = row < g.M ? g.targets[row] - colw : -1;
-      if (__any(t >= 0 && t < SPAN && colw + t < g.N)) {
+      const bool here = t >= 0 && t < SPAN && colw + t < g.N;
+      if (__any(here)) {
         float zt = 0.f;
 #pragma unroll
         for (int j = 0; j < TI; ++j)
 #pragma unroll
           for (int v = 0; v < 16; ++v) zt = (int)t == 32 * j + 8 * (v >> 2) + 4 * half + (v & 3) ? acc[i][j][v] : zt;
-        if (t >= 0 && t < SPAN && colw + t < g.N && (((int)t >> 2) & 1) == half) g.target_z[row] = zt;
+        if (here && (((int)t >> 2) & 1) == half) g.target_z[row] = zt;
       }
+      // exp of the distance from the largest, and that in 16 bits, one conversion for two
+      float sum = 0.f;
 #pragma unroll
       for (int j = 0; j < TI; ++j)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const float e = (acc[i][j][v] - base) * LOG2_E;
-          sum += __builtin_amdgcn_exp2f(e);
-          if (g.store == STORE_LOGITS_U16) acc[i][j][v] = fminf(-e * LOGIT_STEPS, 65535.f);
+        for (int q = 0; q < 4; ++q) {
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float d = acc[i][j][4 * q + e] - base;
+            sum += __builtin_amdgcn_exp2f(d * LOG2_E);
+            x[e] = d * (-LOG2_E * LOGIT_STEPS / 65535.f);
+          }
+          if (g.store == STORE_LOGITS_U16) {
+            const u32x2 w = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(x[0], x[1])), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(x[2], x[3]))};
+            *reinterpret_cast<u32x2 *>(reinterpret_cast<uint16_t *>(buf) + (lane & 31) * PITCH16 + 32 * j + 8 * q + 4 * half) = w;
+          }
         }
       sum += __shfl_xor(sum, 32, 64);
       if (half == 0 && row < g.M) g.stats[(int64_t)(colw / SPAN) * g.stats_ld + row] = make_float2(largest, sum);
     }
     if (LOGITS && g.store == STORE_NO_LOGITS) continue;
-    tg_wave_order();
-#pragma unroll
-    for (int j = 0; j < TI; ++j)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<float4 *>(buf + (lane & 31) * PITCH + 32 * j + 8 * q + 4 * half) =
-            make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-    tg_wave_order();
     constexpr int LANES = SPAN / 8, ROWS_AT_ONCE = 64 / LANES;      // eight columns a lane
     const int c = (lane % LANES) * 8, col = colw + c, limit = LOGITS ? (int)g.ldc : g.N;
+    if (!LOGITS || g.store != STORE_LOGITS_U16) {
+#pragma unroll
+      for (int j = 0; j < TI; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<float4 *>(buf + (lane & 31) * PITCH + 32 * j + 8 * q + 4 * half) =
+              make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+    }
+    tg_wave_order();
 #pragma unroll
     for (int r = lane / LANES; r < 32; r += ROWS_AT_ONCE) {
       const int out = roww + 32 * i + r;
       if (out < g.M && col < limit) {
-        const float4 x = *reinterpret_cast<const float4 *>(buf + r * PITCH + c), y = *reinterpret_cast<const float4 *>(buf + r * PITCH + c + 4);
-        f32x8 z = {{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w}};
         if (LOGITS && g.store == STORE_LOGITS_U16) {
-          uint32_t w[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = (uint32_t)(z.v[2 * e] + 0.5f) | (uint32_t)(z.v[2 * e + 1] + 0.5f) << 16;
-          *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(g.c) + (int64_t)out * g.ldc + col) = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(g.c) + (int64_t)out * g.ldc + col) =
+              *reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(buf) + r * PITCH16 + c);
         } else {
+          const float4 x = *reinterpret_cast<const float4 *>(buf + r * PITCH + c), y = *reinterpret_cast<const float4 *>(buf + r * PITCH + c + 4);
+          f32x8 z = {{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w}};
           if (!LOGITS && g.add) {
             const f32x8 old = load8(g.add + (int64_t)out * g.ldadd, col, g.N);
 #pragma unroll
