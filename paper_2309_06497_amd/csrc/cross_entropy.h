@@ -18,6 +18,59 @@
 
 namespace shampoo {
 
+// Logits from the float32 results of several splits of their product, where that has too few tiles to fill the GPU otherwise: what
+// the logits' product leaves (train_gemm.h), in spans of 64 classes.  A thread has eight classes of a row, eight threads a span.
+struct LogitsJoinArgs {
+  const float *part; int64_t stride, pitch; int32_t splits;
+  void *z; int64_t ldz; int32_t store;
+  const float *bias; const int64_t *targets;
+  float2 *stats; int64_t stats_ld; float *target_z;
+  int32_t rows, classes;
+  uint32_t pieces, per_row;          // ldz / 8, a multiple of 8
+};
+__global__ __launch_bounds__(256) void logits_join_kernel(const LogitsJoinArgs g) {
+  const uint32_t at = min(blockIdx.x * 256u + threadIdx.x, g.pieces - 1);       // the last one again: whole spans, whole wavefronts
+  const int i = at / g.per_row, c = (at - i * g.per_row) * 8;
+  f32x8 z = load8(g.part + (int64_t)i * g.pitch, c, (int)g.pitch);
+  for (int k = 1; k < g.splits; ++k) {
+    const f32x8 x = load8(g.part + k * g.stride + (int64_t)i * g.pitch, c, (int)g.pitch);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z.v[e] += x.v[e];
+  }
+  if (g.bias) {
+    const f32x8 b = load8(g.bias, c, g.classes);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z.v[e] += b.v[e];
+  }
+  float largest = -INFINITY;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (c + e >= g.classes) z.v[e] = -INFINITY;
+    largest = fmaxf(largest, z.v[e]);
+  }
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) largest = fmaxf(largest, __shfl_xor(largest, o, 64));
+  const float base = largest == -INFINITY ? 0.f : largest;
+  const int64_t t = g.targets[i] - c;
+  float sum = 0.f;
+  uint32_t w[4];
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const float d = z.v[e] - base, d1 = z.v[e + 1] - base;
+    sum += __builtin_amdgcn_exp2f(d * LOG2_E) + __builtin_amdgcn_exp2f(d1 * LOG2_E);
+    w[e >> 1] = logit_pair(d, d1);
+  }
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor(sum, o, 64);
+  if (blockIdx.x * 256u + threadIdx.x >= g.pieces) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (t == e && c + e < g.classes) g.target_z[i] = z.v[e];
+  if ((c & 63) == 0) g.stats[(int64_t)(c >> 6) * g.stats_ld + i] = make_float2(largest, sum);
+  if (g.store == STORE_LOGITS_U16) *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(g.z) + (int64_t)i * g.ldz + c) = make_uint4(w[0], w[1], w[2], w[3]);
+  else if (g.store == STORE_LOGITS_F32) store8(static_cast<float *>(g.z) + (int64_t)i * g.ldz, c, (int)g.ldz, z);
+}
+
 // lse, loss and c of every row from the largest logits and sums of its spans: 16 rows per workgroup, 16 threads a row.
 struct RowLossArgs {
   const float2 *stats; int64_t stats_ld;

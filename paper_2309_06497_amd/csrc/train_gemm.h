@@ -60,6 +60,12 @@ constexpr int TG_BK = 64;
 // distance of a logit from the largest of its span in 16 bits: steps of 2^-10 in the exponent of 2
 constexpr float LOGIT_STEPS = 1024.f, LOG2_E = 1.4426950408889634f;
 
+// two of them, from z - largest
+__device__ __forceinline__ uint32_t logit_pair(float d, float e) {
+  constexpr float C = -LOG2_E * LOGIT_STEPS / 65535.f;
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(d * C, e * C));
+}
+
 // LDS accesses of one wavefront that depend on one another: LDS keeps their order, the compiler must
 __device__ __forceinline__ void tg_wave_order() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -307,10 +313,10 @@ __global__ __launch_bounds__(256, TI == 4 ? 1 : 2) void train_gemm_kernel(const 
           for (int e = 0; e < 4; ++e) {
             const float d = acc[i][j][4 * q + e] - base;
             sum += __builtin_amdgcn_exp2f(d * LOG2_E);
-            x[e] = d * (-LOG2_E * LOGIT_STEPS / 65535.f);
+            x[e] = d;
           }
           if (g.store == STORE_LOGITS_U16) {
-            const u32x2 w = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(x[0], x[1])), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(x[2], x[3]))};
+            const u32x2 w = {logit_pair(x[0], x[1]), logit_pair(x[2], x[3])};
             *reinterpret_cast<u32x2 *>(reinterpret_cast<uint16_t *>(buf) + (lane & 31) * PITCH16 + 32 * j + 8 * q + 4 * half) = w;
           }
         }

@@ -141,12 +141,11 @@ int plane_pairs(int na, int nb, uint32_t &pa, uint32_t &pb) {
 
 // How a product is cut: tiles of 256 or 128 (TI), and splits of the sequence of slabs where there are few tiles.
 struct GemmCut { int ti, splits, per_split; size_t bytes; };
-GemmCut gemm_cut(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, bool logits) {
+GemmCut gemm_cut(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b) {
   uint32_t unused_a, unused_b;
   const int64_t all = (K + TG_BK - 1) / TG_BK * plane_pairs(planes_a, planes_b, unused_a, unused_b);
   const int64_t large = ((M + 255) / 256) * ((N + 255) / 256);
   GemmCut c = {large >= 128 ? 4 : 2, 1, (int)all, 0};
-  if (logits) return c;
   const int64_t tile = 64 * c.ti, tiles = ((M + tile - 1) / tile) * ((N + tile - 1) / tile), want = c.ti == 4 ? 256 : 512;
   const int64_t splits = std::max<int64_t>(1, std::min(want / tiles, all / 4));
   c.per_split = (int)((all + splits - 1) / splits);
@@ -171,19 +170,24 @@ int gemm_args(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t 
   g.padded = a.padded ? 1 : b.padded ? 2 : 0;
   return (int64_t)g.tiles_m * g.tiles_n > ((int64_t)1 << 23) ? SHAMPOO_ERR_UNSUPPORTED : SHAMPOO_OK;
 }
+// the splits' results one behind the other in `part`
+void gemm_partial(TrainGemmArgs &g, const GemmCut &cut, int alie, int blie, float *part, hipStream_t s) {
+  g.c = part; g.ldc = round_up(g.N, 8); g.c_split = g.M * g.ldc; g.store = STORE_F32;
+  if (cut.ti == 4) gemm_launch<4, false>(g, alie, blie, s); else gemm_launch<2, false>(g, alie, blie, s);
+}
 // C = A B^T; `part`: scratch of gemm_cut's size
 int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const Result &c, float *part, hipStream_t s) {
-  const GemmCut cut = gemm_cut(M, N, K, a.planes, b.planes, false);
+  const GemmCut cut = gemm_cut(M, N, K, a.planes, b.planes);
   TrainGemmArgs g;
   TRY(gemm_args(a, b, M, N, K, cut, g));
   if (cut.splits == 1) {
     g.c = c.c; g.ldc = c.ldc; g.add = c.add; g.ldadd = c.ldadd; g.store = c.store;
-  } else {
-    g.c = part; g.ldc = round_up(N, 8); g.c_split = M * g.ldc; g.store = STORE_F32;
+    if (cut.ti == 4) gemm_launch<4, false>(g, a.lie, b.lie, s); else gemm_launch<2, false>(g, a.lie, b.lie, s);
+    HIP_TRY(hipGetLastError());
+    return SHAMPOO_OK;
   }
-  if (cut.ti == 4) gemm_launch<4, false>(g, a.lie, b.lie, s); else gemm_launch<2, false>(g, a.lie, b.lie, s);
+  gemm_partial(g, cut, a.lie, b.lie, part, s);
   HIP_TRY(hipGetLastError());
-  if (cut.splits == 1) return SHAMPOO_OK;
   JoinArgs j = {};
   j.part = part; j.stride = g.c_split; j.splits = cut.splits; j.c = c.c; j.ldc = c.ldc; j.add = c.add; j.ldadd = c.ldadd;
   j.cols = (int32_t)N; j.pitch = (int32_t)g.ldc; j.store = c.store; j.per_row = (uint32_t)(g.ldc / 8);
@@ -255,14 +259,16 @@ int cross_entropy_plan(const shampoo_cross_entropy &c, void *workspace, CrossEnt
     p.g = a.take<uint16_t>((size_t)p.grad_planes() * p.piece * p.ldz);
     if (p.sum) p.acc = a.take<float>((size_t)p.w.rows * p.w.cols);
     if (c.has_bias) p.sums = a.take<float>((size_t)p.ranges * p.pieces * v);
-    size_t part = 0;
-    for (int64_t n : {p.piece, c.rows - std::max<int64_t>(0, p.pieces - 1) * p.piece, c.rows}) {      // all pieces, the last one, a single one
-      if (n < 1 || n > p.piece) continue;
-      part = std::max(part, gemm_cut(n, d, v, c.dtype == SHAMPOO_GRAD_F32 ? 3 : 1, p.w.planes(), false).bytes);
-      part = std::max(part, out_in ? gemm_cut(v, d, n, p.grad_planes(), p.x.planes(), false).bytes : gemm_cut(d, v, n, p.x.planes(), p.grad_planes(), false).bytes);
-    }
-    if (part) p.part = a.take<float>(part / sizeof(float));
   }
+  size_t part = 0;
+  for (int64_t n : {p.piece, c.rows - std::max<int64_t>(0, p.pieces - 1) * p.piece, c.rows}) {      // all pieces, the last one, a single one
+    if (n < 1 || n > p.piece) continue;
+    part = std::max(part, gemm_cut(n, v, d, p.x.planes(), p.w.planes()).bytes);
+    if (!c.gradients) continue;
+    part = std::max(part, gemm_cut(n, d, v, c.dtype == SHAMPOO_GRAD_F32 ? 3 : 1, p.w.planes()).bytes);
+    part = std::max(part, out_in ? gemm_cut(v, d, n, p.grad_planes(), p.x.planes()).bytes : gemm_cut(d, v, n, p.x.planes(), p.grad_planes()).bytes);
+  }
+  if (part) p.part = a.take<float>(part / sizeof(float));
   p.bytes = a.used;
   return SHAMPOO_OK;
 }
@@ -302,7 +308,7 @@ int weight_grad_plan(int64_t rows, int32_t in, int32_t out, int32_t activation, 
   size_t part = 0;
   for (int64_t n : {p.piece, rows - std::max<int64_t>(0, p.pieces - 1) * p.piece, rows}) {
     if (n < 1 || n > p.piece) continue;
-    part = std::max(part, std::max(gemm_cut(out, in, n, p.dy.planes(), p.planes, false).bytes, gemm_cut(in, out, n, p.planes, p.dy.planes(), false).bytes));
+    part = std::max(part, std::max(gemm_cut(out, in, n, p.dy.planes(), p.planes).bytes, gemm_cut(in, out, n, p.planes, p.dy.planes()).bytes));
   }
   if (part) p.part = a.take<float>(part / sizeof(float));
   p.bytes = a.used;
@@ -441,17 +447,26 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
     const int64_t i0 = k * p.piece, n = std::min(p.piece, c->rows - i0);
     Operand xk = xo;
     xk.p += i0 * xo.ld;
-    const GemmCut cut = gemm_cut(n, v, d, xk.planes, wo.planes, true);
-    const int32_t span = 32 * cut.ti;
+    const GemmCut cut = gemm_cut(n, v, d, xk.planes, wo.planes);
+    const int32_t span = cut.splits > 1 ? 64 : 32 * cut.ti;
+    const int store = !c->gradients ? STORE_NO_LOGITS : p.planes ? STORE_LOGITS_F32 : STORE_LOGITS_U16;
+    void *const logits = p.planes ? static_cast<void *>(p.z) : p.g;
     TrainGemmArgs z;
     TRY(gemm_args(xk, wo, n, v, d, cut, z));
-    z.c = p.planes ? static_cast<void *>(p.z) : p.g; z.ldc = p.ldz;
-    z.store = !c->gradients ? STORE_NO_LOGITS : p.planes ? STORE_LOGITS_F32 : STORE_LOGITS_U16;
-    z.bias = bias; z.targets = targets + i0; z.stats = p.stats; z.stats_ld = p.piece; z.target_z = p.target_z;
-    if (cut.ti == 4) gemm_launch<4, true>(z, xk.lie, wo.lie, s); else gemm_launch<2, true>(z, xk.lie, wo.lie, s);
+    if (cut.splits > 1) {
+      gemm_partial(z, cut, xk.lie, wo.lie, p.part, s);
+      HIP_TRY(hipGetLastError());
+      LogitsJoinArgs j = {p.part, z.c_split, z.ldc, cut.splits, logits, p.ldz, store, bias, targets + i0, p.stats, p.piece, p.target_z,
+                          (int32_t)n, (int32_t)v, (uint32_t)(n * (p.ldz / 8)), (uint32_t)(p.ldz / 8)};
+      logits_join_kernel<<<dim3((j.pieces + 255) / 256), 256, 0, s>>>(j);
+    } else {
+      z.c = logits; z.ldc = p.ldz; z.store = store;
+      z.bias = bias; z.targets = targets + i0; z.stats = p.stats; z.stats_ld = p.piece; z.target_z = p.target_z;
+      if (cut.ti == 4) gemm_launch<4, true>(z, xk.lie, wo.lie, s); else gemm_launch<2, true>(z, xk.lie, wo.lie, s);
+    }
     HIP_TRY(hipGetLastError());
     const RowLossArgs r = {p.stats, p.piece, p.target_z, targets + i0, weight ? weight + i0 : nullptr, scale, p.lse, p.coef, loss + i0,
-                           (int32_t)n, (int32_t)v, z.tiles_n * 2};
+                           (int32_t)n, (int32_t)v, (int32_t)((v + span - 1) / span)};
     row_loss_kernel<<<dim3((unsigned)((n + 15) / 16)), 256, 0, s>>>(r);
     HIP_TRY(hipGetLastError());
     if (!dx && !dw && !dbias) continue;

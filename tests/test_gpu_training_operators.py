@@ -176,6 +176,32 @@ def test_head_with_masked_classes_and_rows_that_are_not_finite():
         assert torch.isfinite(out[0][rest]).all() and torch.isfinite(out[1][rest]).all()
 
 
+def test_head_where_every_class_is_masked_by_the_lowest_value():
+    """The softmax of equal logits, however low: 1 / classes each (z + lowest is lowest: nothing of z is left)."""
+    torch = torch_()
+    g = gen(12)
+    for n, d, v in ((40, 64, 300), (200, 1024, 300), (600, 64, 16500)):          # one product, several splits, large tiles
+        for dt in (torch.bfloat16, torch.float32):
+            x, w = normal(g, n, d).to(dt), normal(g, v, d, sigma=0.1).to(dt)
+            t = torch.randint(0, v, (n,), generator=g, device="cuda")
+            low = torch.full((v,), torch.finfo(torch.float32).min, device="cuda")
+            loss, dx, dw, db = B.shampoo_linear_cross_entropy(x, w, t, bias=low)
+            # lse = lowest + log(classes) rounds to lowest, and so does z: the loss is what float32 leaves, 0
+            assert not loss.any() and torch.isfinite(dx).all() and torch.isfinite(dw).all() and torch.isfinite(db).all()
+
+
+def test_head_whose_logits_span_the_whole_range():
+    """Differences beyond 64 powers of two, and beyond float32's exponents, next to ordinary ones."""
+    torch = torch_()
+    g = gen(13)
+    for n, d, v in ((40, 64, 300), (600, 64, 16500)):
+        x, w = normal(g, n, d, sigma=3.0).bfloat16(), normal(g, v, d, sigma=3.0).bfloat16()
+        t = torch.randint(0, v, (n,), generator=g, device="cuda")
+        want = head_reference(x, w, t, None, None, 1.0)
+        out = B.shampoo_linear_cross_entropy(x, w, t)
+        check_head(out, want, d, True, False)
+
+
 def test_head_of_large_logits_does_not_overflow():
     torch = torch_()
     g = gen(9)
