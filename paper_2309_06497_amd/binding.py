@@ -436,14 +436,27 @@ def shampoo_root_inverse_newton(a, epsilon, p, tolerance=1e-6, max_iterations=10
 # ----------------------------------------------------------------------------
 def _dtype_code(dtype):
     import torch
-    assert dtype in (torch.float32, torch.bfloat16), f"float32 or bfloat16, not {dtype}"
-    return GRAD_BF16 if dtype == torch.bfloat16 else GRAD_F32
+    if dtype is torch.bfloat16:
+        return GRAD_BF16
+    assert dtype is torch.float32, f"float32 or bfloat16, not {dtype}"
+    return GRAD_F32
+
+
+def _launch(fn, device, *args):
+    """fn(*args, stream) on a device and its current stream.  Addresses go as integers: these calls are often shorter than a
+    microsecond per argument would allow."""
+    import torch
+    index = device.index
+    if index == torch._C._cuda_getDevice():
+        return _check(fn(*args, torch._C._cuda_getCurrentRawStream(index)))
+    with torch.cuda.device(index):
+        _check(fn(*args, torch._C._cuda_getCurrentRawStream(index)))
 
 
 def _rows(x, dtype=None, align=1):
     """A CUDA matrix whose rows are contiguous, as the library reads it (a copy where it is not, or not aligned to `align` bytes)."""
     assert x.is_cuda and x.dim() == 2 and (dtype is None or x.dtype == dtype), "a CUDA matrix of the right type is needed"
-    if (x.shape[1] > 1 and x.stride(1) != 1) or (x.shape[0] > 1 and x.stride(0) < x.shape[1]):
+    if not x.is_contiguous() and ((x.shape[1] > 1 and x.stride(1) != 1) or (x.shape[0] > 1 and x.stride(0) < x.shape[1])):
         x = x.contiguous()
     return x.new_empty(x.shape).copy_(x) if x.data_ptr() % align else x
 
@@ -453,7 +466,7 @@ def _ld(x):
 
 
 def _ptr(x):
-    return ctypes.c_void_p(x.data_ptr()) if x is not None else None
+    return x.data_ptr() if x is not None else None
 
 
 def _vector(x, shape, device):
@@ -494,9 +507,8 @@ def shampoo_linear_cross_entropy(x, w, targets, bias=None, weight=None, scale=1.
     c = CrossEntropy(n, d, v, code, _dtype_code(grad_dtype), IN_OUT if in_out else OUT_IN, 1 if bias is not None else 0,
                      1 if gradients else 0, _ld(x), _ld(wm), d, wm.shape[1])
     ws = _workspace(lib().shampoo_linear_cross_entropy_workspace_bytes(ctypes.byref(c)), x.device)
-    with torch.cuda.device(x.device):
-        _check(lib().shampoo_linear_cross_entropy(ctypes.byref(c), _ptr(x), _ptr(wm), _ptr(bias), _ptr(targets), _ptr(weight), scale,
-                                                  _ptr(loss), _ptr(dx), _ptr(dw), _ptr(dbias), _ptr(ws), ws.numel(), _stream_ptr()))
+    _launch(lib().shampoo_linear_cross_entropy, x.device, ctypes.byref(c), _ptr(x), _ptr(wm), _ptr(bias), _ptr(targets), _ptr(weight),
+            scale, _ptr(loss), _ptr(dx), _ptr(dw), _ptr(dbias), _ptr(ws), ws.numel())
     if not gradients:
         return loss
     return loss, dx, dw.t() if in_out else dw, dbias
@@ -521,8 +533,7 @@ def shampoo_checkpoint_pack(x):
     import torch
     code, x = _dtype_code(x.dtype), _rows(x)
     c = Checkpoint.empty(x.shape[0], x.shape[1], x.dtype, x.device)
-    with torch.cuda.device(x.device):
-        _check(lib().shampoo_checkpoint_pack(_ptr(x), code, c.rows, c.cols, _ld(x), _ptr(c.packed), c.packed.numel(), _stream_ptr()))
+    _launch(lib().shampoo_checkpoint_pack, x.device, _ptr(x), code, c.rows, c.cols, _ld(x), _ptr(c.packed), c.packed.numel())
     return c
 
 
@@ -530,9 +541,8 @@ def shampoo_checkpoint_unpack(c, activation=ACT_NONE, dtype=None):
     """activation(x) [rows, cols] of what a checkpoint holds, in `dtype` (default: that of the packed matrix)."""
     import torch
     y = torch.empty((c.rows, c.cols), dtype=dtype or c.dtype, device=c.packed.device)
-    with torch.cuda.device(y.device):
-        _check(lib().shampoo_checkpoint_unpack(_ptr(c.packed), c.packed.numel(), c.rows, c.cols, activation, _ptr(y),
-                                               _dtype_code(y.dtype), c.cols, _stream_ptr()))
+    _launch(lib().shampoo_checkpoint_unpack, y.device, _ptr(c.packed), c.packed.numel(), c.rows, c.cols, activation, _ptr(y),
+            _dtype_code(y.dtype), c.cols)
     return y
 
 
@@ -542,9 +552,8 @@ def shampoo_checkpoint_activation_grad(c, dy, activation):
     assert tuple(dy.shape) == (c.rows, c.cols) and dy.device == c.packed.device
     code, dy = _dtype_code(dy.dtype), _rows(dy)
     dx = torch.empty((c.rows, c.cols), dtype=dy.dtype, device=dy.device)
-    with torch.cuda.device(dy.device):
-        _check(lib().shampoo_checkpoint_activation_grad(_ptr(c.packed), c.packed.numel(), c.rows, c.cols, activation, _ptr(dy), code,
-                                                        _ld(dy), _ptr(dx), c.cols, _stream_ptr()))
+    _launch(lib().shampoo_checkpoint_activation_grad, dy.device, _ptr(c.packed), c.packed.numel(), c.rows, c.cols, activation, _ptr(dy),
+            code, _ld(dy), _ptr(dx), c.cols)
     return dx
 
 
@@ -560,10 +569,8 @@ def shampoo_checkpoint_weight_grad(c, dy, activation=ACT_NONE, grad_dtype=None, 
     grad = _dtype_code(dw.dtype)
     nbytes = lib().shampoo_checkpoint_weight_grad_workspace_bytes(c.rows, c.cols, out, activation, code, _ld(dy), grad, 1 if bias else 0)
     ws = _workspace(nbytes, dy.device)
-    with torch.cuda.device(dy.device):
-        _check(lib().shampoo_checkpoint_weight_grad(_ptr(c.packed), c.packed.numel(), c.rows, c.cols, activation, _ptr(dy), code, out,
-                                                    _ld(dy), _ptr(dw), grad, OUT_IN if out_in else IN_OUT, dw.shape[1], _ptr(db),
-                                                    _ptr(ws), ws.numel(), _stream_ptr()))
+    _launch(lib().shampoo_checkpoint_weight_grad, dy.device, _ptr(c.packed), c.packed.numel(), c.rows, c.cols, activation, _ptr(dy), code,
+            out, _ld(dy), _ptr(dw), grad, OUT_IN if out_in else IN_OUT, dw.shape[1], _ptr(db), _ptr(ws), ws.numel())
     return (dw, db) if bias else dw
 
 
@@ -592,11 +599,8 @@ def shampoo_residual_norm_forward(r, f, post=NORM_RMS, pre=NORM_RMS, w_post=None
     r_out = torch.empty((rows, cols), dtype=r.dtype, device=r.device)
     h = torch.empty_like(r_out) if pre != NORM_NONE else None
     r8, f8 = (Checkpoint.empty(rows, cols, r.dtype, r.device) for _ in range(2)) if checkpoint else (None, None)
-    with torch.cuda.device(r.device):
-        _check(lib().shampoo_residual_norm_forward(
-            ctypes.byref(c), _ptr(r), _ld(r), _ptr(f), _ld(f), _ptr(r_out), cols, _ptr(h), cols,
-            _ptr(r8.packed) if checkpoint else None, _ptr(f8.packed) if checkpoint else None, r8.packed.numel() if checkpoint else 0,
-            _stream_ptr()))
+    _launch(lib().shampoo_residual_norm_forward, r.device, ctypes.byref(c), _ptr(r), _ld(r), _ptr(f), _ld(f), _ptr(r_out), cols, _ptr(h), cols,
+            _ptr(r8.packed) if checkpoint else None, _ptr(f8.packed) if checkpoint else None, r8.packed.numel() if checkpoint else 0)
     return (r_out, h, r8, f8) if checkpoint else (r_out, h)
 
 
@@ -625,11 +629,9 @@ def shampoo_residual_norm_backward(r, f, dr_out, dh, post=NORM_RMS, pre=NORM_RMS
     out["dw_post"], out["db_post"] = vector(post != NORM_NONE, (cols,)), vector(b_post is not None and post == NORM_LAYER, (cols,))
     out["dw_pre"], out["db_pre"] = vector(pre != NORM_NONE, (cols,)), vector(b_pre is not None and pre == NORM_LAYER, (cols,))
     ws = _workspace(lib().shampoo_residual_norm_backward_workspace_bytes(ctypes.byref(c)), device)
-    with torch.cuda.device(device):
-        _check(lib().shampoo_residual_norm_backward(
-            ctypes.byref(c), 1 if packed else 0, _ptr(r.packed if packed else r), cols if packed else _ld(r),
+    _launch(lib().shampoo_residual_norm_backward, device, ctypes.byref(c), 1 if packed else 0, _ptr(r.packed if packed else r), cols if packed else _ld(r),
             _ptr(f.packed if packed else f), cols if packed else _ld(f),
             _ptr(dr_out), _ld(dr_out) if dr_out is not None else 0, _ptr(dh), _ld(dh) if dh is not None else 0,
             _ptr(out["dr"]), cols, _ptr(out["df"]), cols, *[_ptr(out[k]) for k in ("dgate", "dw_post", "db_post", "dw_pre", "db_pre")],
-            _ptr(ws), ws.numel(), _stream_ptr()))
+            _ptr(ws), ws.numel())
     return out
