@@ -182,17 +182,29 @@ template <int FROM, int PLANES> __global__ __launch_bounds__(256) void planes_ke
   }
 }
 
-// out[j] = sum over rows of x[i][j], in an order that does not depend on the launch: workgroup (j / 256, part) sums its rows,
+// Column sums of x, in an order that does not depend on the launch: workgroup (j / 64, part) sums its rows, 16 threads a column, and
 // join_sums_kernel the parts.
-template <typename T> __global__ __launch_bounds__(256) void column_sums_kernel(const T *x, int64_t ldx, int64_t rows, int32_t cols, int64_t per_part, float *out) {
-  const int j = blockIdx.x * 256 + threadIdx.x;
-  if (j >= cols) return;
-  const int64_t i0 = blockIdx.y * per_part, i1 = min(rows, i0 + per_part);
-  float s = 0.f;
-  for (int64_t i = i0; i < i1; ++i) {
-    if constexpr (sizeof(T) == 4) s += x[i * ldx + j]; else s += bf16_value(x[i * ldx + j]);
+template <typename T> __global__ __launch_bounds__(1024) void column_sums_kernel(const T *x, int64_t ldx, int64_t rows, int32_t cols, int64_t per_part, float *out) {
+  __shared__ float part[16][64];
+  const int c = threadIdx.x & 63, k = threadIdx.x >> 6, j = blockIdx.x * 64 + c;
+  const int64_t i1 = min(rows, (int64_t)(blockIdx.y + 1) * per_part);
+  auto value = [&](int64_t i) { if constexpr (sizeof(T) == 4) return x[i * ldx + j]; else return bf16_value(x[i * ldx + j]); };
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (j < cols) {
+    int64_t i = blockIdx.y * per_part + k;
+    for (; i + 48 < i1; i += 64) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) s[q] += value(i + 16 * q);
+    }
+    for (; i < i1; i += 16) s[0] += value(i);
   }
-  out[(int64_t)blockIdx.y * cols + j] = s;
+  part[k][c] = (s[0] + s[1]) + (s[2] + s[3]);
+  __syncthreads();
+  if (k != 0 || j >= cols) return;
+  float t = 0.f;
+#pragma unroll
+  for (int q = 0; q < 16; ++q) t += part[q][c];
+  out[(int64_t)blockIdx.y * cols + j] = t;
 }
 
 }  // namespace shampoo

@@ -139,19 +139,32 @@ int plane_pairs(int na, int nb, uint32_t &pa, uint32_t &pb) {
   return n;
 }
 
-// How a product is cut: tiles of 256 or 128 (TI), and splits of the sequence of slabs where there are few tiles.
+// How a product is cut: tiles of 256 or 128 (TI), and splits of the sequence of slabs, whose float32 results a second launch adds up.  The
+// shortest by what was measured, in microseconds: a slab takes a tile of 256 alone on its CU 1.7 (1.75 with all CUs at work: the clock gives way),
+// a tile of 128 0.75 alone, 1.0 beside a second one, 0.58 each where they follow one another; 4 ... 11 for a tile's start and end; a join 3 and its traffic at 4 TB/s.
+// Against all cuts of 19 shapes between 256 x 256 x 512 and 8192 x 2048 x 8192 the choice is within 15 % of the best.  For example
+// 2000 x 1000 x 50000: 191 (256, 8 splits), 210 (128, 4), 639 (128, 1); 2048 x 2048 x 2048: 29 (128, 1), 34 (128, 2), 50 (256, 1);
+// 256 x 256 x 4096: 14 (128, 16), 26 (128, 1).
 struct GemmCut { int ti, splits, per_split; size_t bytes; };
 GemmCut gemm_cut(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b) {
   uint32_t unused_a, unused_b;
   const int64_t all = (K + TG_BK - 1) / TG_BK * plane_pairs(planes_a, planes_b, unused_a, unused_b);
-  const int64_t large = ((M + 255) / 256) * ((N + 255) / 256);
-  GemmCut c = {large >= 128 ? 4 : 2, 1, (int)all, 0};
-  const int64_t tile = 64 * c.ti, tiles = ((M + tile - 1) / tile) * ((N + tile - 1) / tile), want = c.ti == 4 ? 256 : 512;
-  const int64_t splits = std::max<int64_t>(1, std::min(want / tiles, all / 4));
-  c.per_split = (int)((all + splits - 1) / splits);
-  c.splits = (int)((all + c.per_split - 1) / c.per_split);
-  if (c.splits > 1) c.bytes = align_up((size_t)c.splits * M * round_up(N, 8) * sizeof(float));
-  return c;
+  GemmCut best = {2, 1, (int)all, 0};
+  double shortest = INFINITY;
+  for (int ti : {2, 4})
+    for (int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+      if (splits > 1 && splits > all / 2) break;
+      const int64_t tile = 64 * ti, tiles = ((M + tile - 1) / tile) * ((N + tile - 1) / tile), per = (all + splits - 1) / splits;
+      const double each = (double)((tiles * splits + 255) / 256);       // workgroups per CU
+      double us = ti == 4 ? 5.0 + each * (6.0 + 1.7 * (double)per) : 4.0 + (double)per * (each <= 1.0 ? 0.75 : each <= 2.0 ? 1.0 : 0.58 * each);
+      if (splits > 1) us += 3.0 + (double)splits * (double)M * (double)N * 2e-6;
+      if (us < shortest) {
+        shortest = us;
+        best = {ti, (int)((all + per - 1) / per), (int)per, 0};
+      }
+    }
+  if (best.splits > 1) best.bytes = align_up((size_t)best.splits * M * round_up(N, 8) * sizeof(float));
+  return best;
 }
 template <int TI, bool LOGITS> void gemm_launch(const TrainGemmArgs &g, int alie, int blie, hipStream_t s) {
   const int64_t total = (int64_t)g.tiles_m * g.tiles_n * g.splits;
@@ -298,7 +311,7 @@ int weight_grad_plan(int64_t rows, int32_t in, int32_t out, int32_t activation, 
                               std::max<int64_t>(PIECE_ROWS, (int64_t)(PLANE_BYTES / ((size_t)p.ldp * 2 * p.planes)) / PIECE_ROWS * PIECE_ROWS));
   p.pieces = (rows + p.piece - 1) / p.piece;
   p.sum = p.pieces > 1 && grad_dtype == SHAMPOO_GRAD_BF16;
-  p.part_rows = std::max<int64_t>(64, (rows + 255) / 256);
+  p.part_rows = std::max<int64_t>(64, (rows + 63) / 64);
   p.parts = std::max<int64_t>(1, (rows + p.part_rows - 1) / p.part_rows);
   Arena a(workspace);
   p.xp = a.take<uint16_t>((size_t)p.planes * p.piece * p.ldp);
@@ -599,9 +612,9 @@ int shampoo_checkpoint_weight_grad(const void *packed, size_t packed_bytes, int6
     TRY(out_in ? gemm(dk, xo, out, in, n, r, p.part, s) : gemm(xo, dk, in, out, n, r, p.part, s));
   }
   if (db) {
-    const dim3 grid((out + 255) / 256, (unsigned)p.parts);
-    if (dtype == SHAMPOO_GRAD_F32) column_sums_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float *>(dy), lddy, rows, out, p.part_rows, p.sums);
-    else column_sums_kernel<uint16_t><<<grid, 256, 0, s>>>(static_cast<const uint16_t *>(dy), lddy, rows, out, p.part_rows, p.sums);
+    const dim3 grid((out + 63) / 64, (unsigned)p.parts);
+    if (dtype == SHAMPOO_GRAD_F32) column_sums_kernel<float><<<grid, 1024, 0, s>>>(static_cast<const float *>(dy), lddy, rows, out, p.part_rows, p.sums);
+    else column_sums_kernel<uint16_t><<<grid, 1024, 0, s>>>(static_cast<const uint16_t *>(dy), lddy, rows, out, p.part_rows, p.sums);
     HIP_TRY(hipGetLastError());
     const float *in = p.sums;
     TRY(launch_join_sums(&in, &db, 1, (int32_t)p.parts, out, 1, 0, out, out, s));
