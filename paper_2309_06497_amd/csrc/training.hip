@@ -24,7 +24,8 @@ constexpr int32_t MAX_FEATURES = 65536, MAX_OUT = 1 << 22, MAX_PACKED_COLS = 1 <
 constexpr int64_t MAX_LD = 1 << 22;                        // of an operand as it lies: offsets inside a tile have 32 bits
 constexpr size_t LOGIT_BYTES = (size_t)4 << 30;            // scratch of a piece of the rows
 constexpr size_t PLANE_BYTES = (size_t)1 << 30;
-constexpr int64_t PIECE_ROWS = 256;                        // rows of a piece are a multiple of this
+constexpr int64_t PIECE_ROWS = 256, MAX_PIECE_ROWS = 1 << 21;   // rows of a piece are a multiple of the first (grids: at most 65535 ranges of 64)
+constexpr int64_t MAX_TILES = 1 << 23;                     // of a product: threads of a launch have 32 bits
 
 inline size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
 inline int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
@@ -173,7 +174,7 @@ template <int TI, bool LOGITS> void gemm_launch(const TrainGemmArgs &g, int alie
   else if (alie == LIE_K) train_gemm_kernel<TI, LIE_K, LIE_ROWS, LOGITS><<<grid, 256, 0, s>>>(g);
   else if constexpr (!LOGITS) train_gemm_kernel<TI, LIE_ROWS, LIE_ROWS, LOGITS><<<grid, 256, 0, s>>>(g);
 }
-int gemm_args(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const GemmCut &cut, TrainGemmArgs &g) {
+void gemm_args(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const GemmCut &cut, TrainGemmArgs &g) {
   g = {};
   g.a = a.p; g.b = b.p; g.lda = a.ld; g.ldb = b.ld; g.a_plane = a.plane; g.b_plane = b.plane;
   g.M = (int32_t)M; g.N = (int32_t)N; g.K = (int32_t)K;
@@ -181,7 +182,6 @@ int gemm_args(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t 
   g.tiles_m = (int32_t)((M + 64 * cut.ti - 1) / (64 * cut.ti)); g.tiles_n = (int32_t)((N + 64 * cut.ti - 1) / (64 * cut.ti));
   g.splits = cut.splits; g.per_split = cut.per_split;
   g.padded = a.padded ? 1 : b.padded ? 2 : 0;
-  return (int64_t)g.tiles_m * g.tiles_n > ((int64_t)1 << 23) ? SHAMPOO_ERR_UNSUPPORTED : SHAMPOO_OK;
 }
 // the splits' results one behind the other in `part`
 void gemm_partial(TrainGemmArgs &g, const GemmCut &cut, int alie, int blie, float *part, hipStream_t s) {
@@ -192,7 +192,7 @@ void gemm_partial(TrainGemmArgs &g, const GemmCut &cut, int alie, int blie, floa
 int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const Result &c, float *part, hipStream_t s) {
   const GemmCut cut = gemm_cut(M, N, K, a.planes, b.planes);
   TrainGemmArgs g;
-  TRY(gemm_args(a, b, M, N, K, cut, g));
+  gemm_args(a, b, M, N, K, cut, g);
   if (cut.splits == 1) {
     g.c = c.c; g.ldc = c.ldc; g.add = c.add; g.ldadd = c.ldadd; g.store = c.store;
     if (cut.ti == 4) gemm_launch<4, false>(g, a.lie, b.lie, s); else gemm_launch<2, false>(g, a.lie, b.lie, s);
@@ -248,6 +248,7 @@ int cross_entropy_plan(const shampoo_cross_entropy &c, void *workspace, CrossEnt
   if (c.gradients && c.dtype == SHAMPOO_GRAD_F32 && c.grad_dtype != SHAMPOO_GRAD_F32) return SHAMPOO_ERR_HYPER;
   const bool out_in = c.w_layout == SHAMPOO_OUT_IN;
   const int64_t wcols = out_in ? c.features : c.classes, d = c.features, v = c.classes;
+  if (((v + 127) / 128) * ((d + 127) / 128) > MAX_TILES) return SHAMPOO_ERR_UNSUPPORTED;
   if (c.ldx < d || c.ldw < wcols || (c.gradients && (c.lddx < d || c.lddw < wcols))) return SHAMPOO_ERR_SHAPE;
   p.x = {c.dtype, c.rows, d, c.ldx, TG_BK};
   p.w = {c.dtype, out_in ? v : d, wcols, c.ldw, TG_BK};
@@ -257,7 +258,7 @@ int cross_entropy_plan(const shampoo_cross_entropy &c, void *workspace, CrossEnt
   p.spans = round_up(v, 256) / 64;
   const size_t per_row = (size_t)p.spans * sizeof(float2) + (c.gradients ? (size_t)p.ldz * (p.planes ? 4 + 2 * p.planes : 2) : 0);
   p.piece = std::min<int64_t>(round_up(std::max<int64_t>(c.rows, 1), PIECE_ROWS),
-                              std::max<int64_t>(PIECE_ROWS, (int64_t)(LOGIT_BYTES / per_row) / PIECE_ROWS * PIECE_ROWS));
+                              std::min(MAX_PIECE_ROWS, std::max<int64_t>(PIECE_ROWS, (int64_t)(LOGIT_BYTES / per_row) / PIECE_ROWS * PIECE_ROWS)));
   p.pieces = (c.rows + p.piece - 1) / p.piece;
   p.sum = c.gradients && p.pieces > 1 && c.grad_dtype == SHAMPOO_GRAD_BF16;
   // rows of a thread of softmax_grad_kernel: 64 where that leaves a thousand workgroups
@@ -301,7 +302,8 @@ struct WeightGradPlan {
 int weight_grad_plan(int64_t rows, int32_t in, int32_t out, int32_t activation, int32_t dtype, int64_t lddy, int32_t grad_dtype, bool bias,
                      void *workspace, WeightGradPlan &p) {
   if (rows < 0 || in < 1 || out < 1 || lddy < out) return SHAMPOO_ERR_SHAPE;
-  if (rows > MAX_ROWS || in > MAX_FEATURES || out > MAX_OUT) return SHAMPOO_ERR_UNSUPPORTED;
+  if (rows > MAX_ROWS || in > MAX_FEATURES || out > MAX_OUT || (((int64_t)in + 127) / 128) * (((int64_t)out + 127) / 128) > MAX_TILES)
+    return SHAMPOO_ERR_UNSUPPORTED;
   if (!dtype_ok(dtype) || !dtype_ok(grad_dtype) || activation < ACT_NONE || activation > ACT_SILU) return SHAMPOO_ERR_HYPER;
   if (dtype == SHAMPOO_GRAD_F32 && grad_dtype != SHAMPOO_GRAD_F32) return SHAMPOO_ERR_HYPER;
   p.dy = {dtype, rows, out, lddy, 8};
@@ -465,7 +467,7 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
     const int store = !c->gradients ? STORE_NO_LOGITS : p.planes ? STORE_LOGITS_F32 : STORE_LOGITS_U16;
     void *const logits = p.planes ? static_cast<void *>(p.z) : p.g;
     TrainGemmArgs z;
-    TRY(gemm_args(xk, wo, n, v, d, cut, z));
+    gemm_args(xk, wo, n, v, d, cut, z);
     if (cut.splits > 1) {
       gemm_partial(z, cut, xk.lie, wo.lie, p.part, s);
       HIP_TRY(hipGetLastError());
