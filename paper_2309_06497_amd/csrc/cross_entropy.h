@@ -8,7 +8,8 @@
 //   bf16 x, bf16 dw, no bias: the distance of z from the largest of its span in 16 bits, steps of 2^-10 in the exponent of 2
 //     (2 bytes per logit; exp(z) is off by 3.4e-4 of itself at most where the rounding of g to bf16 is 3.9e-3; what is further than 64
 //     steps of 1 away, 5e-20 of the largest, counts as zero).  g takes its place.
-//   otherwise: z in float32, beside it g as the bf16 planes that float32 results need.
+//   float32 x or dw, or a bias: z in float32, beside it g as the bf16 planes that float32 results need.
+// Few features (and no sums for a bias): neither; the product runs a second time, once the rows' sums are known, and leaves g itself.
 // The three products are 6 rows features classes operations; what lies between them is bound by memory.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -22,7 +23,7 @@ namespace shampoo {
 // the logits' product leaves (train_gemm.h), in spans of 64 classes.  A thread has eight classes of a row, eight threads a span.
 struct LogitsJoinArgs {
   const float *part; int64_t stride, pitch; int32_t splits;
-  void *z; int64_t ldz; int32_t store;
+  void *z; int64_t ldz; int32_t end, store;
   const float *bias; const int64_t *targets;
   float2 *stats; int64_t stats_ld; float *target_z;
   int32_t rows, classes;
@@ -32,6 +33,7 @@ __global__ __launch_bounds__(256) void logits_join_kernel(const LogitsJoinArgs g
   const uint32_t at = min(blockIdx.x * 256u + threadIdx.x, g.pieces - 1);       // the last one again: whole spans, whole wavefronts
   const int i = at / g.per_row, c = (at - i * g.per_row) * 8;
   f32x8 z = load8(g.part + (int64_t)i * g.pitch, c, (int)g.pitch);
+#pragma unroll 4
   for (int k = 1; k < g.splits; ++k) {
     const f32x8 x = load8(g.part + k * g.stride + (int64_t)i * g.pitch, c, (int)g.pitch);
 #pragma unroll
@@ -67,11 +69,11 @@ __global__ __launch_bounds__(256) void logits_join_kernel(const LogitsJoinArgs g
   for (int e = 0; e < 8; ++e)
     if (t == e && c + e < g.classes) g.target_z[i] = z.v[e];
   if ((c & 63) == 0) g.stats[(int64_t)(c >> 6) * g.stats_ld + i] = make_float2(largest, sum);
-  if (g.store == STORE_LOGITS_U16) *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(g.z) + (int64_t)i * g.ldz + c) = make_uint4(w[0], w[1], w[2], w[3]);
-  else if (g.store == STORE_LOGITS_F32) store8(static_cast<float *>(g.z) + (int64_t)i * g.ldz, c, (int)g.ldz, z);
+  if (g.end == END_LOGITS_U16) *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(g.z) + (int64_t)i * g.ldz + c) = make_uint4(w[0], w[1], w[2], w[3]);
+  else if (g.store != STORE_NOTHING) store8(static_cast<float *>(g.z) + (int64_t)i * g.ldz, c, (int)g.ldz, z);
 }
 
-// lse, loss and c of every row from the largest logits and sums of its spans: 16 rows per workgroup, 16 threads a row.
+// lse, loss and c of every row from the largest logits and sums of its spans: 16 rows per workgroup, 64 threads a row.
 struct RowLossArgs {
   const float2 *stats; int64_t stats_ld;
   const float *target_z; const int64_t *targets; const float *weight;
@@ -85,16 +87,23 @@ __device__ __forceinline__ void join_exp(float &m, float &s, float n, float t) {
   const float a = m == -INFINITY ? s : s * __builtin_amdgcn_exp2f((m - top) * LOG2_E), b = n == -INFINITY ? t : t * __builtin_amdgcn_exp2f((n - top) * LOG2_E);
   m = top; s = a + b;
 }
-__global__ __launch_bounds__(256) void row_loss_kernel(const RowLossArgs g) {
+__global__ __launch_bounds__(1024) void row_loss_kernel(const RowLossArgs g) {
   __shared__ float2 part[16][16];
   const int r = threadIdx.x & 15, k = threadIdx.x >> 4, i = blockIdx.x * 16 + r;
   float m = -INFINITY, s = 0.f;
-  if (i < g.rows)
-    for (int p = k; p < g.spans; p += 16) {
+  if (i < g.rows) {
+#pragma unroll 4
+    for (int p = k; p < g.spans; p += 64) {
       const float2 x = g.stats[p * g.stats_ld + i];
       join_exp(m, s, x.x, x.y);
     }
-  part[k][r] = make_float2(m, s);
+  }
+#pragma unroll
+  for (int o = 16; o < 64; o <<= 1) {            // the four of a wavefront, then the wavefronts in order
+    const float n = __shfl_xor(m, o, 64), t = __shfl_xor(s, o, 64);
+    join_exp(m, s, n, t);
+  }
+  if ((k & 3) == 0) part[k >> 2][r] = make_float2(m, s);
   __syncthreads();
   if (k != 0 || i >= g.rows) return;
   for (int p = 1; p < 16; ++p) join_exp(m, s, part[p][r].x, part[p][r].y);

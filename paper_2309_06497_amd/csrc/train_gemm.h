@@ -27,6 +27,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 #include <utility>
 #include "lds_dma.h"
 #include "vectors.h"
@@ -34,7 +35,9 @@
 namespace shampoo {
 
 enum { LIE_K = 0, LIE_ROWS = 1 };          // which index of an operand is contiguous
-enum { STORE_F32 = 0, STORE_BF16 = 1, STORE_LOGITS_F32 = 2, STORE_LOGITS_U16 = 3, STORE_NO_LOGITS = 4 };
+enum { STORE_F32 = 0, STORE_BF16 = 1, STORE_NOTHING = 2 };
+// What becomes of a tile: C itself; the logits' statistics and the logits in float32 (or not at all) or in 16 bits; the gradient of the logits
+enum { END_PLAIN = 0, END_LOGITS = 1, END_LOGITS_U16 = 2, END_GRAD = 3 };
 
 struct TrainGemmArgs {
   const uint16_t *a, *b;
@@ -47,10 +50,12 @@ struct TrainGemmArgs {
   void *c; int64_t ldc, c_split;           // c_split: from the result of a split to the next
   const float *add; int64_t ldadd;         // C += add (float32; may be c itself) or nullptr
   int32_t store;
-  // logits: z = C + bias; per row and span (32 TI columns): the largest z and sum of exp(z - largest); the target's z
+  // END_LOGITS...: z = C + bias (16 bits: no bias); per row and span (32 TI columns): the largest z and sum of exp(z - largest); the target's z
   const float *bias; const int64_t *targets;
   float2 *stats; int64_t stats_ld;         // [span][row]
   float *target_z;
+  // END_GRAD, from the statistics of a first product: coef (exp(z - lse) - [target]) as bf16 planes
+  const float *lse, *coef; int64_t c_plane; int32_t c_planes;
 };
 
 typedef float train_f32x16 __attribute__((ext_vector_type(16)));
@@ -132,12 +137,12 @@ template <int LIE, int TI> struct SlabRegs {
   }
 };
 
-template <int TI, int ALIE, int BLIE, bool LOGITS>
-__global__ __launch_bounds__(256, TI == 4 ? 1 : 2) void train_gemm_kernel(const TrainGemmArgs g) {
+template <int TI, int STAGES, int ALIE, int BLIE, int END>
+__global__ __launch_bounds__(256, TI == 2 && STAGES == 2 ? 2 : 1) void train_gemm_kernel(const TrainGemmArgs g) {
   typedef SlabSide<ALIE, TI> SideA;
   typedef SlabSide<BLIE, TI> SideB;
   constexpr int TILE = 64 * TI, SPAN = 32 * TI, STAGE = SideA::BYTES + SideB::BYTES, PIECES = SideA::PIECES, NMM = TI * TI;
-  __shared__ __align__(256) unsigned char smem[2 * STAGE];
+  __shared__ __align__(256) unsigned char smem[STAGES * STAGE];
   const int tiles = g.tiles_m * g.tiles_n, total = tiles * g.splits;
   // an XCD (workgroup index modulo 8) has neighbouring tiles, in columns of eight
   const int per = (total + 7) / 8, logical = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
@@ -204,10 +209,11 @@ __global__ __launch_bounds__(256, TI == 4 ? 1 : 2) void train_gemm_kernel(const 
   };
 
   // One step: the products of 16 values of k, and between them, one at a time, so that the matrix cores do not wait for the wavefront
-  // to issue something else, the LDS reads of the next step (in its first half) and loads of slabs to come (in its second).  A slab's loads
-  // begin with step 3, behind the barrier after which nobody reads its stage any more, and end with step 0 of the slab before it.
+  // to issue something else, the LDS reads of the next step (in its first half) and loads of slabs to come (in its second).  The loads of
+  // slab t + STAGES begin with step 3 of slab t, behind the barrier after which nobody reads its stage any more, and end
+  // with step 0 of slab t + 1.  st: the stage of this slab, st_next: of the next one, st_in: of the one that is loaded.
   constexpr int HALF = NMM / 2, PER_SLOT = (READS + HALF - 1) / HALF, LOADS_PER_SLOT = (PIECES + HALF - 1) / HALF;
-  auto step = [&](auto sc, uint32_t st, uint32_t st_next) {
+  auto step = [&](auto sc, uint32_t st, uint32_t st_next, uint32_t st_in) {
     constexpr int S = decltype(sc)::value, X = S & 1, LEAD = S == 3 ? NMM / 8 + (NMM < 8) : 0;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     ra[X].arrived(); rb[X].arrived();
@@ -217,7 +223,7 @@ __global__ __launch_bounds__(256, TI == 4 ? 1 : 2) void train_gemm_kernel(const 
       acc[I][J] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rb[X].operand(J), ra[X].operand(I), acc[I][J], 0, 0, 0);
       if constexpr (S == 3 && P == LEAD - 1) {
         LDS_SCHED_BARRIER();
-        LDS_DMA_WAIT_VM(0);
+        LDS_DMA_WAIT_VM((STAGES - 2) * 2 * PIECES);       // the next slab is there
         __builtin_amdgcn_s_barrier();
       }
       LDS_SCHED_BARRIER();
@@ -229,7 +235,7 @@ __global__ __launch_bounds__(256, TI == 4 ? 1 : 2) void train_gemm_kernel(const 
       if constexpr (P >= HALF && (S == 3 || S == 0)) {
 #pragma unroll
         for (int q = (P - HALF) * LOADS_PER_SLOT; q < (P - HALF + 1) * LOADS_PER_SLOT && q < PIECES; ++q) {
-          if constexpr (S == 3) load_a(q, st); else load_b(q, st_next);
+          if constexpr (S == 3) load_a(q, st_in); else load_b(q, st_in);
         }
       }
       LDS_SCHED_BARRIER();
@@ -238,22 +244,26 @@ __global__ __launch_bounds__(256, TI == 4 ? 1 : 2) void train_gemm_kernel(const 
 
   locate();
 #pragma unroll
-  for (int q = 0; q < PIECES; ++q) { load_a(q, 0); load_b(q, 0); }
-  next_slab();
+  for (int t = 0; t < STAGES; ++t) {
 #pragma unroll
-  for (int q = 0; q < PIECES; ++q) load_a(q, STAGE);
-  LDS_DMA_WAIT_VM(PIECES);
+    for (int q = 0; q < PIECES; ++q) load_a(q, t * STAGE);
+    if (t == STAGES - 1) break;
+#pragma unroll
+    for (int q = 0; q < PIECES; ++q) load_b(q, t * STAGE);
+    next_slab();
+  }
+  LDS_DMA_WAIT_VM((STAGES - 2) * 2 * PIECES + PIECES);
   __builtin_amdgcn_s_barrier();
   tg_each(std::make_integer_sequence<int, READS>(), [&](auto rc) { read(rc, std::integral_constant<int, 0>(), 0); });
   uint32_t st = 0;
   for (int t = 0; t < count; ++t) {
-    const uint32_t other = STAGE - st;
-    step(std::integral_constant<int, 0>(), st, other);
-    step(std::integral_constant<int, 1>(), st, other);
+    const uint32_t next = st + STAGE == STAGES * STAGE ? 0 : st + STAGE, before = st == 0 ? (STAGES - 1) * STAGE : st - STAGE;
+    step(std::integral_constant<int, 0>(), st, next, before);
+    step(std::integral_constant<int, 1>(), st, next, 0);
     next_slab();
-    step(std::integral_constant<int, 2>(), st, other);
-    step(std::integral_constant<int, 3>(), st, other);
-    st = other;
+    step(std::integral_constant<int, 2>(), st, next, 0);
+    step(std::integral_constant<int, 3>(), st, next, st);
+    st = next;
   }
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   ra[0].arrived(); rb[0].arrived();
@@ -263,20 +273,58 @@ __global__ __launch_bounds__(256, TI == 4 ? 1 : 2) void train_gemm_kernel(const 
   // A lane has row lane % 32 of every tile, columns 8 (v / 4) + 4 (lane / 32) + v % 4.  32 rows at a time go through LDS, which only
   // this wavefront touches.
   constexpr int PITCH = SPAN + 4, PITCH16 = SPAN + 8;      // floats, 16-bit logits: rows are 16-byte aligned and four banks apart
-  static_assert(4 * 32 * PITCH * 4 + (LOGITS ? 4 * SPAN * 4 : 0) <= 2 * STAGE, "LDS");
+  static_assert(4 * 32 * PITCH * 4 + 4 * SPAN * 4 <= STAGES * STAGE, "LDS");
   float *buf = reinterpret_cast<float *>(smem) + wave * 32 * PITCH;
   const int half = lane >> 5, colw = col0 + wn * SPAN, roww = row0 + wm * SPAN;
   [[maybe_unused]] float *bias = reinterpret_cast<float *>(smem) + 4 * 32 * PITCH + wave * SPAN;
-  if constexpr (LOGITS) {
+  if constexpr (END == END_LOGITS || END == END_GRAD) {
     for (int j = lane; j < SPAN; j += 64) bias[j] = colw + j >= g.N ? -INFINITY : g.bias ? g.bias[colw + j] : 0.f;   // no class there: probability 0
   }
-  [[maybe_unused]] const bool biased = g.bias || colw + SPAN > g.N;
-#pragma unroll
-  for (int i = 0; i < TI; ++i) {
-    const int row = roww + 32 * i + (lane & 31);
+  constexpr int LANES = SPAN / 8, ROWS_AT_ONCE = 64 / LANES;      // eight columns a lane
+  const int c = (lane % LANES) * 8, col = colw + c, limit = END == END_PLAIN ? g.N : (int)g.ldc;
+  const int row_limit = END == END_GRAD ? (g.M + TG_BK - 1) / TG_BK * TG_BK : g.M;                  // zeros behind the last row
+  // rows r, r + ROWS_AT_ONCE, ... of the 32 that lie in LDS
+  auto put = [&](int i, auto &&store) {
     tg_wave_order();
-    if constexpr (LOGITS) {
-      if (biased) {
+#pragma unroll
+    for (int r = lane / LANES; r < 32; r += ROWS_AT_ONCE) {
+      const int out = roww + 32 * i + r;
+      if (out < row_limit && col < limit) store(r, (int64_t)out);
+    }
+    tg_wave_order();
+  };
+  auto stage = [&](int i) {
+#pragma unroll
+    for (int j = 0; j < TI; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4 *>(buf + (lane & 31) * PITCH + 32 * j + 8 * q + 4 * half) =
+            make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+  };
+  auto staged = [&](int r) { return load8(buf + r * PITCH + c, 0, 8); };
+
+  if constexpr (END == END_PLAIN) {
+#pragma unroll
+    for (int i = 0; i < TI; ++i) {
+      stage(i);
+      put(i, [&](int r, int64_t out) {
+        f32x8 z = staged(r);
+        if (g.add) {
+          const f32x8 old = load8(g.add + out * g.ldadd, col, g.N);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) z.v[e] += old.v[e];
+        }
+        if (g.store == STORE_BF16) store8(static_cast<uint16_t *>(g.c) + out * g.ldc, col, limit, z);
+        else store8(static_cast<float *>(g.c) + split * g.c_split + out * g.ldc, col, limit, z);
+      });
+    }
+  } else {
+    tg_wave_order();
+#pragma unroll
+    for (int i = 0; i < TI; ++i) {
+      const int row = roww + 32 * i + (lane & 31);
+      const int64_t target = row < g.M ? g.targets[row] - colw : -1;
+      if constexpr (END == END_LOGITS || END == END_GRAD) {
 #pragma unroll
         for (int j = 0; j < TI; ++j)
 #pragma unroll
@@ -285,98 +333,118 @@ __global__ __launch_bounds__(256, TI == 4 ? 1 : 2) void train_gemm_kernel(const 
             acc[i][j][4 * q] += b.x; acc[i][j][4 * q + 1] += b.y; acc[i][j][4 * q + 2] += b.z; acc[i][j][4 * q + 3] += b.w;
           }
       }
-      float largest = -INFINITY;
-#pragma unroll
-      for (int j = 0; j < TI; ++j)
-#pragma unroll
-        for (int v = 0; v < 16; v += 2) largest = fmaxf(largest, fmaxf(acc[i][j][v], acc[i][j][v + 1]));
-      largest = fmaxf(largest, __shfl_xor(largest, 32, 64));
-      const float base = largest == -INFINITY ? 0.f : largest;
-      const int64_t t = row < g.M ? g.targets[row] - colw : -1;
-      const bool here = t >= 0 && t < SPAN && colw + t < g.N;
-      if (__any(here)) {
-        float zt = 0.f;
+      if constexpr (END == END_GRAD) {
+        const float lse = row < g.M ? g.lse[row] : 0.f, k = row < g.M && lse != -INFINITY ? g.coef[row] : 0.f;
+        const int at = target >= 0 && target < SPAN ? (int)target - 4 * half : -1;
 #pragma unroll
         for (int j = 0; j < TI; ++j)
 #pragma unroll
-          for (int v = 0; v < 16; ++v) zt = (int)t == 32 * j + 8 * (v >> 2) + 4 * half + (v & 3) ? acc[i][j][v] : zt;
-        if (here && (((int)t >> 2) & 1) == half) g.target_z[row] = zt;
-      }
-      // exp of the distance from the largest, and that in 16 bits, one conversion for two
-      float sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < TI; ++j)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          float x[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float d = acc[i][j][4 * q + e] - base;
-            sum += __builtin_amdgcn_exp2f(d * LOG2_E);
-            x[e] = d;
+          for (int v = 0; v < 16; ++v) {
+            const float p = __builtin_amdgcn_exp2f((acc[i][j][v] - lse) * LOG2_E);
+            acc[i][j][v] = k != 0.f ? k * (at == 32 * j + 8 * (v >> 2) + (v & 3) ? p - 1.f : p) : 0.f;
           }
-          if (g.store == STORE_LOGITS_U16) {
-            const u32x2 w = {logit_pair(x[0], x[1]), logit_pair(x[2], x[3])};
-            *reinterpret_cast<u32x2 *>(reinterpret_cast<uint16_t *>(buf) + (lane & 31) * PITCH16 + 32 * j + 8 * q + 4 * half) = w;
+        stage(i);
+        put(i, [&](int r, int64_t out) {
+          f32x8 z = staged(r);
+          uint16_t *to = static_cast<uint16_t *>(g.c) + out * g.ldc + col;
+          for (int s = 0; s < g.c_planes; ++s) {          // each plane what the ones before it leave
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              w[e] = bf16_pair(z.v[2 * e], z.v[2 * e + 1]);
+              z.v[2 * e] -= __uint_as_float(w[e] << 16); z.v[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
+            }
+            *reinterpret_cast<uint4 *>(to + s * g.c_plane) = make_uint4(w[0], w[1], w[2], w[3]);
           }
-        }
-      sum += __shfl_xor(sum, 32, 64);
-      if (half == 0 && row < g.M) g.stats[(int64_t)(colw / SPAN) * g.stats_ld + row] = make_float2(largest, sum);
-    }
-    if (LOGITS && g.store == STORE_NO_LOGITS) continue;
-    constexpr int LANES = SPAN / 8, ROWS_AT_ONCE = 64 / LANES;      // eight columns a lane
-    const int c = (lane % LANES) * 8, col = colw + c, limit = LOGITS ? (int)g.ldc : g.N;
-    if (!LOGITS || g.store != STORE_LOGITS_U16) {
+        });
+      } else {
+        // ENDS: the span reaches past the last class (float32: the bias has taken care of that)
+        auto statistics = [&](auto ends) {
+          constexpr bool ENDS = decltype(ends)::value;
+          auto z = [&](int j, int v) {
+            const float x = acc[i][j][v];
+            return ENDS && colw + 32 * j + 8 * (v >> 2) + 4 * half + (v & 3) >= g.N ? -INFINITY : x;
+          };
+          float largest = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < TI; ++j)
+          for (int j = 0; j < TI; ++j)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          *reinterpret_cast<float4 *>(buf + (lane & 31) * PITCH + 32 * j + 8 * q + 4 * half) =
-              make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-    }
-    tg_wave_order();
+            for (int v = 0; v < 16; v += 2) largest = fmaxf(largest, fmaxf(z(j, v), z(j, v + 1)));
+          largest = fmaxf(largest, __shfl_xor(largest, 32, 64));
+          const float base = largest == -INFINITY ? 0.f : largest;
+          const bool here = target >= 0 && target < SPAN && colw + target < g.N;
+          if (__any(here)) {
+            float zt = 0.f;
 #pragma unroll
-    for (int r = lane / LANES; r < 32; r += ROWS_AT_ONCE) {
-      const int out = roww + 32 * i + r;
-      if (out < g.M && col < limit) {
-        if (LOGITS && g.store == STORE_LOGITS_U16) {
-          *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(g.c) + (int64_t)out * g.ldc + col) =
-              *reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(buf) + r * PITCH16 + c);
+            for (int j = 0; j < TI; ++j)
+#pragma unroll
+              for (int v = 0; v < 16; ++v) zt = (int)target == 32 * j + 8 * (v >> 2) + 4 * half + (v & 3) ? acc[i][j][v] : zt;
+            if (here && (((int)target >> 2) & 1) == half) g.target_z[row] = zt;
+          }
+          // exp of the distance from the largest, and that in 16 bits, one conversion for two
+          float sum = 0.f;
+#pragma unroll
+          for (int j = 0; j < TI; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              float d[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                d[e] = z(j, 4 * q + e) - base;
+                sum += __builtin_amdgcn_exp2f(d[e] * LOG2_E);
+              }
+              if constexpr (END == END_LOGITS_U16) {
+                const u32x2 w = {logit_pair(d[0], d[1]), logit_pair(d[2], d[3])};
+                *reinterpret_cast<u32x2 *>(reinterpret_cast<uint16_t *>(buf) + (lane & 31) * PITCH16 + 32 * j + 8 * q + 4 * half) = w;
+              }
+            }
+          sum += __shfl_xor(sum, 32, 64);
+          if (half == 0 && row < g.M) g.stats[(int64_t)(colw / SPAN) * g.stats_ld + row] = make_float2(largest, sum);
+        };
+        if constexpr (END == END_LOGITS_U16) {
+          if (colw + SPAN > g.N) statistics(std::true_type()); else statistics(std::false_type());
+          put(i, [&](int r, int64_t out) {
+            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(g.c) + out * g.ldc + col) =
+                *reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(buf) + r * PITCH16 + c);
+          });
         } else {
-          const float4 x = *reinterpret_cast<const float4 *>(buf + r * PITCH + c), y = *reinterpret_cast<const float4 *>(buf + r * PITCH + c + 4);
-          f32x8 z = {{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w}};
-          if (!LOGITS && g.add) {
-            const f32x8 old = load8(g.add + (int64_t)out * g.ldadd, col, g.N);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z.v[e] += old.v[e];
+          statistics(std::false_type());
+          if (g.store != STORE_NOTHING) {
+            stage(i);
+            put(i, [&](int r, int64_t out) { store8(static_cast<float *>(g.c) + out * g.ldc, col, limit, staged(r)); });
           }
-          if (!LOGITS && g.store == STORE_BF16) store8(static_cast<uint16_t *>(g.c) + (int64_t)out * g.ldc, col, limit, z);
-          else store8(static_cast<float *>(g.c) + split * g.c_split + (int64_t)out * g.ldc, col, limit, z);
         }
       }
     }
   }
 }
 
-// The results of several splits, float32 [split][rows][cols], added up in order.
+// The results of several splits, float32 [split][rows][cols], added up in an order that does not depend on the launch.  LANES
+// threads share a piece of eight columns where there are many splits, so that their loads are on their way together.
 struct JoinArgs {
   const float *part; int64_t stride; int32_t splits;
   void *c; int64_t ldc; const float *add; int64_t ldadd;
   int64_t row0; uint32_t pieces, per_row;
   int32_t cols, pitch, store;
 };
-__global__ __launch_bounds__(256) void train_join_kernel(const JoinArgs g) {
-  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
-  if (i >= g.pieces) return;
+template <int LANES> __global__ __launch_bounds__(256) void train_join_kernel(const JoinArgs g) {
+  const uint32_t at = blockIdx.x * (256u / LANES) + threadIdx.x / LANES, i = min(at, g.pieces - 1);
+  const int lane = threadIdx.x % LANES;
   const uint32_t r = i / g.per_row;
   const int c = (int)(i - r * g.per_row) * 8;
   const int64_t row = g.row0 + r;
-  f32x8 s = load8(g.part + row * g.pitch, c, g.pitch);
-  for (int k = 1; k < g.splits; ++k) {
+  f32x8 s = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+#pragma unroll 4
+  for (int k = lane; k < g.splits; k += LANES) {
     const f32x8 x = load8(g.part + k * g.stride + row * g.pitch, c, g.pitch);
 #pragma unroll
     for (int e = 0; e < 8; ++e) s.v[e] += x.v[e];
   }
+#pragma unroll
+  for (int o = 1; o < LANES; o <<= 1)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s.v[e] += __shfl_xor(s.v[e], o, 64);
+  if (at >= g.pieces || lane != 0) return;
   if (g.add) {
     const f32x8 x = load8(g.add + row * g.ldadd, c, g.cols);
 #pragma unroll

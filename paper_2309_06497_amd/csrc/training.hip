@@ -24,6 +24,7 @@ constexpr int32_t MAX_FEATURES = 65536, MAX_OUT = 1 << 22, MAX_PACKED_COLS = 1 <
 constexpr int64_t MAX_LD = 1 << 22;                        // of an operand as it lies: offsets inside a tile have 32 bits
 constexpr size_t LOGIT_BYTES = (size_t)4 << 30;            // scratch of a piece of the rows
 constexpr size_t PLANE_BYTES = (size_t)1 << 30;
+constexpr int LOGIT_SPLITS = 64;
 constexpr int64_t PIECE_ROWS = 256, MAX_PIECE_ROWS = 1 << 21;   // rows of a piece are a multiple of the first (grids: at most 65535 ranges of 64)
 constexpr int64_t MAX_TILES = 1 << 23;                     // of a product: threads of a launch have 32 bits
 
@@ -141,38 +142,44 @@ int plane_pairs(int na, int nb, uint32_t &pa, uint32_t &pb) {
 }
 
 // How a product is cut: tiles of 256 or 128 (TI), and splits of the sequence of slabs, whose float32 results a second launch adds up.  The
-// shortest by what was measured, in microseconds: a slab takes a tile of 256 alone on its CU 1.7 (1.75 with all CUs at work: the clock gives way),
-// a tile of 128 0.75 alone, 1.0 beside a second one, 0.58 each where they follow one another; 4 ... 11 for a tile's start and end; a join 3 and its traffic at 4 TB/s.
+// shortest by what was measured, in microseconds: a slab takes a tile of 256 alone on its CU 1.7 (with all CUs at work; the clock gives way),
+// a tile of 128 0.55 alone (four stages: a slab is asked for three slabs ahead; two stages, 0.8), 1.0 beside a second one (two
+// stages each), 0.58 each where they follow one another; 4 ... 11 for a tile's start and end; a join 3 and its traffic at 4 TB/s.
 // Against all cuts of 19 shapes between 256 x 256 x 512 and 8192 x 2048 x 8192 the choice is within 15 % of the best.  For example
-// 2000 x 1000 x 50000: 191 (256, 8 splits), 210 (128, 4), 639 (128, 1); 2048 x 2048 x 2048: 29 (128, 1), 34 (128, 2), 50 (256, 1);
-// 256 x 256 x 4096: 14 (128, 16), 26 (128, 1).
-struct GemmCut { int ti, splits, per_split; size_t bytes; };
-GemmCut gemm_cut(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b) {
+// 2000 x 1000 x 50000: 186 (256, 8 splits), 206 (128, 4), 637 (128, 1); 2048 x 2048 x 2048: 21 (128, 1; two stages 29), 41 (128, 2),
+// 47 (256, 1); 256 x 256 x 4096: 11 (128, 16), 26 (128, 1).
+struct GemmCut { int ti, splits, per_split; size_t bytes; int stages; };
+GemmCut gemm_cut(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, int most = 512) {
   uint32_t unused_a, unused_b;
   const int64_t all = (K + TG_BK - 1) / TG_BK * plane_pairs(planes_a, planes_b, unused_a, unused_b);
-  GemmCut best = {2, 1, (int)all, 0};
+  GemmCut best = {2, 1, (int)all, 0, 2};
   double shortest = INFINITY;
   for (int ti : {2, 4})
-    for (int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-      if (splits > 1 && splits > all / 2) break;
+    for (int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256, 384, 512}) {
+      if (splits > 1 && (splits > all / 2 || splits > most)) break;
       const int64_t tile = 64 * ti, tiles = ((M + tile - 1) / tile) * ((N + tile - 1) / tile), per = (all + splits - 1) / splits;
       const double each = (double)((tiles * splits + 255) / 256);       // workgroups per CU
-      double us = ti == 4 ? 5.0 + each * (6.0 + 1.7 * (double)per) : 4.0 + (double)per * (each <= 1.0 ? 0.75 : each <= 2.0 ? 1.0 : 0.58 * each);
+      double us = ti == 4 ? 5.0 + each * (6.0 + 1.7 * (double)per) : 4.0 + (double)per * (each <= 1.0 ? 0.55 : each <= 2.0 ? 1.0 : 0.58 * each);
       if (splits > 1) us += 3.0 + (double)splits * (double)M * (double)N * 2e-6;
       if (us < shortest) {
         shortest = us;
-        best = {ti, (int)((all + per - 1) / per), (int)per, 0};
+        best = {ti, (int)((all + per - 1) / per), (int)per, 0, ti == 2 && each <= 1.0 ? 4 : 2};
       }
     }
   if (best.splits > 1) best.bytes = align_up((size_t)best.splits * M * round_up(N, 8) * sizeof(float));
   return best;
 }
-template <int TI, bool LOGITS> void gemm_launch(const TrainGemmArgs &g, int alie, int blie, hipStream_t s) {
+template <int TI, int STAGES, int END> void gemm_launch(const TrainGemmArgs &g, int alie, int blie, hipStream_t s) {
   const int64_t total = (int64_t)g.tiles_m * g.tiles_n * g.splits;
   const dim3 grid((unsigned)((total + 7) / 8 * 8));
-  if (alie == LIE_K && blie == LIE_K) train_gemm_kernel<TI, LIE_K, LIE_K, LOGITS><<<grid, 256, 0, s>>>(g);
-  else if (alie == LIE_K) train_gemm_kernel<TI, LIE_K, LIE_ROWS, LOGITS><<<grid, 256, 0, s>>>(g);
-  else if constexpr (!LOGITS) train_gemm_kernel<TI, LIE_ROWS, LIE_ROWS, LOGITS><<<grid, 256, 0, s>>>(g);
+  if (alie == LIE_K && blie == LIE_K) train_gemm_kernel<TI, STAGES, LIE_K, LIE_K, END><<<grid, 256, 0, s>>>(g);
+  else if (alie == LIE_K) train_gemm_kernel<TI, STAGES, LIE_K, LIE_ROWS, END><<<grid, 256, 0, s>>>(g);
+  else if constexpr (END == END_PLAIN) train_gemm_kernel<TI, STAGES, LIE_ROWS, LIE_ROWS, END><<<grid, 256, 0, s>>>(g);
+}
+template <int END> void gemm_launch(const TrainGemmArgs &g, const GemmCut &cut, int alie, int blie, hipStream_t s) {
+  if (cut.ti == 4) gemm_launch<4, 2, END>(g, alie, blie, s);
+  else if (cut.stages == 4) gemm_launch<2, 4, END>(g, alie, blie, s);
+  else gemm_launch<2, 2, END>(g, alie, blie, s);
 }
 void gemm_args(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const GemmCut &cut, TrainGemmArgs &g) {
   g = {};
@@ -186,7 +193,7 @@ void gemm_args(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t
 // the splits' results one behind the other in `part`
 void gemm_partial(TrainGemmArgs &g, const GemmCut &cut, int alie, int blie, float *part, hipStream_t s) {
   g.c = part; g.ldc = round_up(g.N, 8); g.c_split = g.M * g.ldc; g.store = STORE_F32;
-  if (cut.ti == 4) gemm_launch<4, false>(g, alie, blie, s); else gemm_launch<2, false>(g, alie, blie, s);
+  gemm_launch<END_PLAIN>(g, cut, alie, blie, s);
 }
 // C = A B^T; `part`: scratch of gemm_cut's size
 int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const Result &c, float *part, hipStream_t s) {
@@ -195,7 +202,7 @@ int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, co
   gemm_args(a, b, M, N, K, cut, g);
   if (cut.splits == 1) {
     g.c = c.c; g.ldc = c.ldc; g.add = c.add; g.ldadd = c.ldadd; g.store = c.store;
-    if (cut.ti == 4) gemm_launch<4, false>(g, a.lie, b.lie, s); else gemm_launch<2, false>(g, a.lie, b.lie, s);
+    gemm_launch<END_PLAIN>(g, cut, a.lie, b.lie, s);
     HIP_TRY(hipGetLastError());
     return SHAMPOO_OK;
   }
@@ -206,7 +213,8 @@ int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, co
   j.cols = (int32_t)N; j.pitch = (int32_t)g.ldc; j.store = c.store; j.per_row = (uint32_t)(g.ldc / 8);
   return by_rows(M, j.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
     j.row0 = r; j.pieces = pieces;
-    train_join_kernel<<<grid, 256, 0, s>>>(j);
+    if (cut.splits >= 16 && pieces < (1u << 24)) train_join_kernel<8><<<dim3((pieces + 31) / 32), 256, 0, s>>>(j);
+    else train_join_kernel<1><<<grid, 256, 0, s>>>(j);
   });
 }
 
@@ -232,7 +240,8 @@ struct Source {
 // ---------------------------------------------------------------------------
 struct CrossEntropyPlan {
   Source x, w;
-  int planes = 0;            // of g beside float32 logits; 0: in the place of 16-bit ones
+  int planes = 0;            // of g beside float32 logits (twice: alone); 0: in the place of 16-bit ones
+  bool twice = false;        // the logits' product runs a second time and leaves g
   int64_t ldz = 0, spans = 0, piece = 0, pieces = 0, range_rows = 1, ranges = 1;
   bool sum = false;          // bf16 dw of several pieces: summed in scratch
   size_t bytes = 0;
@@ -254,9 +263,14 @@ int cross_entropy_plan(const shampoo_cross_entropy &c, void *workspace, CrossEnt
   p.w = {c.dtype, out_in ? v : d, wcols, c.ldw, TG_BK};
   // a float32 result needs g to float32 accuracy, and that needs the logits so
   p.planes = c.grad_dtype == SHAMPOO_GRAD_F32 ? 3 : c.has_bias ? 1 : 0;
+  // Once more 2 features operations per logit (six times that in float32), or 4 bytes (16-bit logits) or 8 of traffic.  4096 rows, 32000 classes
+  // (float32: 8000), us with logits kept / made twice: bf16, bf16 dw: 406 / 384 (128 features), 615 / 625 (384); bf16, float32 dw:
+  // 859 / 754 (256), 1078 / 1029 (512), 1479 / 1538 (768); float32: 282 / 239 (64), 345 / 352 (128).
+  p.twice = c.gradients && !c.has_bias && d <= (c.dtype == SHAMPOO_GRAD_F32 ? 96 : p.planes ? 640 : 192);
+  if (p.twice) p.planes = std::max(p.planes, 1);
   p.ldz = round_up(v, 64);
   p.spans = round_up(v, 256) / 64;
-  const size_t per_row = (size_t)p.spans * sizeof(float2) + (c.gradients ? (size_t)p.ldz * (p.planes ? 4 + 2 * p.planes : 2) : 0);
+  const size_t per_row = (size_t)p.spans * sizeof(float2) + (c.gradients ? (size_t)p.ldz * (p.twice ? 2 * p.planes : p.planes ? 4 + 2 * p.planes : 2) : 0);
   p.piece = std::min<int64_t>(round_up(std::max<int64_t>(c.rows, 1), PIECE_ROWS),
                               std::min(MAX_PIECE_ROWS, std::max<int64_t>(PIECE_ROWS, (int64_t)(LOGIT_BYTES / per_row) / PIECE_ROWS * PIECE_ROWS)));
   p.pieces = (c.rows + p.piece - 1) / p.piece;
@@ -269,7 +283,7 @@ int cross_entropy_plan(const shampoo_cross_entropy &c, void *workspace, CrossEnt
   p.lse = a.take<float>(p.piece); p.coef = a.take<float>(p.piece); p.target_z = a.take<float>(p.piece);
   p.stats = a.take<float2>((size_t)p.spans * p.piece);
   if (c.gradients) {
-    if (p.planes) p.z = a.take<float>((size_t)p.piece * p.ldz);
+    if (p.planes && !p.twice) p.z = a.take<float>((size_t)p.piece * p.ldz);
     p.g = a.take<uint16_t>((size_t)p.grad_planes() * p.piece * p.ldz);
     if (p.sum) p.acc = a.take<float>((size_t)p.w.rows * p.w.cols);
     if (c.has_bias) p.sums = a.take<float>((size_t)p.ranges * p.pieces * v);
@@ -277,7 +291,7 @@ int cross_entropy_plan(const shampoo_cross_entropy &c, void *workspace, CrossEnt
   size_t part = 0;
   for (int64_t n : {p.piece, c.rows - std::max<int64_t>(0, p.pieces - 1) * p.piece, c.rows}) {      // all pieces, the last one, a single one
     if (n < 1 || n > p.piece) continue;
-    part = std::max(part, gemm_cut(n, v, d, p.x.planes(), p.w.planes()).bytes);
+    part = std::max(part, gemm_cut(n, v, d, p.x.planes(), p.w.planes(), p.twice ? 1 : LOGIT_SPLITS).bytes);
     if (!c.gradients) continue;
     part = std::max(part, gemm_cut(n, d, v, c.dtype == SHAMPOO_GRAD_F32 ? 3 : 1, p.w.planes()).bytes);
     part = std::max(part, out_in ? gemm_cut(v, d, n, p.grad_planes(), p.x.planes()).bytes : gemm_cut(d, v, n, p.x.planes(), p.grad_planes()).bytes);
@@ -462,36 +476,41 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
     const int64_t i0 = k * p.piece, n = std::min(p.piece, c->rows - i0);
     Operand xk = xo;
     xk.p += i0 * xo.ld;
-    const GemmCut cut = gemm_cut(n, v, d, xk.planes, wo.planes);
+    const GemmCut cut = gemm_cut(n, v, d, xk.planes, wo.planes, p.twice ? 1 : LOGIT_SPLITS);
     const int32_t span = cut.splits > 1 ? 64 : 32 * cut.ti;
-    const int store = !c->gradients ? STORE_NO_LOGITS : p.planes ? STORE_LOGITS_F32 : STORE_LOGITS_U16;
+    const int store = !c->gradients || p.twice ? STORE_NOTHING : STORE_F32, end = store == STORE_NOTHING || p.planes ? END_LOGITS : END_LOGITS_U16;
     void *const logits = p.planes ? static_cast<void *>(p.z) : p.g;
     TrainGemmArgs z;
     gemm_args(xk, wo, n, v, d, cut, z);
     if (cut.splits > 1) {
       gemm_partial(z, cut, xk.lie, wo.lie, p.part, s);
       HIP_TRY(hipGetLastError());
-      LogitsJoinArgs j = {p.part, z.c_split, z.ldc, cut.splits, logits, p.ldz, store, bias, targets + i0, p.stats, p.piece, p.target_z,
+      LogitsJoinArgs j = {p.part, z.c_split, z.ldc, cut.splits, logits, p.ldz, end, store, bias, targets + i0, p.stats, p.piece, p.target_z,
                           (int32_t)n, (int32_t)v, (uint32_t)(n * (p.ldz / 8)), (uint32_t)(p.ldz / 8)};
       logits_join_kernel<<<dim3((j.pieces + 255) / 256), 256, 0, s>>>(j);
     } else {
       z.c = logits; z.ldc = p.ldz; z.store = store;
       z.bias = bias; z.targets = targets + i0; z.stats = p.stats; z.stats_ld = p.piece; z.target_z = p.target_z;
-      if (cut.ti == 4) gemm_launch<4, true>(z, xk.lie, wo.lie, s); else gemm_launch<2, true>(z, xk.lie, wo.lie, s);
+      if (end == END_LOGITS_U16) gemm_launch<END_LOGITS_U16>(z, cut, xk.lie, wo.lie, s); else gemm_launch<END_LOGITS>(z, cut, xk.lie, wo.lie, s);
     }
     HIP_TRY(hipGetLastError());
     const RowLossArgs r = {p.stats, p.piece, p.target_z, targets + i0, weight ? weight + i0 : nullptr, scale, p.lse, p.coef, loss + i0,
                            (int32_t)n, (int32_t)v, (int32_t)((v + span - 1) / span)};
-    row_loss_kernel<<<dim3((unsigned)((n + 15) / 16)), 256, 0, s>>>(r);
+    row_loss_kernel<<<dim3((unsigned)((n + 15) / 16)), 1024, 0, s>>>(r);
     HIP_TRY(hipGetLastError());
     if (!dx && !dw && !dbias) continue;
-    const SoftmaxGradArgs q = {p.z, p.ldz, p.stats, p.piece, span, p.lse, p.coef, targets + i0, p.g, p.piece * p.ldz,
-                               dbias ? p.sums + k * p.ranges * v : nullptr, (int32_t)n, (int32_t)v, (int32_t)p.range_rows};
-    const dim3 grid((unsigned)((p.ldz / 8 + 255) / 256), (unsigned)((round_up(n, TG_BK) + p.range_rows - 1) / p.range_rows));   // zeros behind the last row
-    switch (p.planes) {
-      case 0: softmax_grad_kernel<0><<<grid, 256, 0, s>>>(q); break;
-      case 1: softmax_grad_kernel<1><<<grid, 256, 0, s>>>(q); break;
-      default: softmax_grad_kernel<3><<<grid, 256, 0, s>>>(q);
+    if (p.twice) {
+      z.c = p.g; z.lse = p.lse; z.coef = p.coef; z.c_plane = p.piece * p.ldz; z.c_planes = p.planes;
+      gemm_launch<END_GRAD>(z, cut, xk.lie, wo.lie, s);
+    } else {
+      const SoftmaxGradArgs q = {p.z, p.ldz, p.stats, p.piece, span, p.lse, p.coef, targets + i0, p.g, p.piece * p.ldz,
+                                 dbias ? p.sums + k * p.ranges * v : nullptr, (int32_t)n, (int32_t)v, (int32_t)p.range_rows};
+      const dim3 grid((unsigned)((p.ldz / 8 + 255) / 256), (unsigned)((round_up(n, TG_BK) + p.range_rows - 1) / p.range_rows));   // zeros behind the last row
+      switch (p.planes) {
+        case 0: softmax_grad_kernel<0><<<grid, 256, 0, s>>>(q); break;
+        case 1: softmax_grad_kernel<1><<<grid, 256, 0, s>>>(q); break;
+        default: softmax_grad_kernel<3><<<grid, 256, 0, s>>>(q);
+      }
     }
     HIP_TRY(hipGetLastError());
     if (dx) {
