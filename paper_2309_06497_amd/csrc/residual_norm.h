@@ -384,25 +384,26 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR, NJ == 1 && TPR <= 256 && siz
   }
 }
 
-// Sums over teams or parts: out_k[o][j] = sum over p < parts of in[k][o][p][j], k = blockIdx.z, o = blockIdx.y, in an order that
+// Sums over teams or parts: out_k[o][j] = sum over p < parts_k of in_k[o][p][j], k = blockIdx.z, o = blockIdx.y, in an order that
 // does not depend on the launch.  A workgroup has 64 columns and 16 threads for each.
+constexpr int JOIN_SUMS = 8;
 struct JoinSumsArgs {
-  const float *in[SUMS]; float *out[SUMS];
+  const float *in[JOIN_SUMS]; float *out[JOIN_SUMS]; int32_t parts[JOIN_SUMS];
   int64_t output_stride, part_stride, out_stride;
-  int32_t parts, cols;
+  int32_t cols;
 };
 __global__ __launch_bounds__(1024) void join_sums_kernel(const JoinSumsArgs g) {
   __shared__ float part[16][64];
-  const int c = threadIdx.x & 63, k = threadIdx.x >> 6, j = blockIdx.x * 64 + c;
+  const int c = threadIdx.x & 63, k = threadIdx.x >> 6, j = blockIdx.x * 64 + c, parts = g.parts[blockIdx.z];
   float s[4] = {0.f, 0.f, 0.f, 0.f};
   if (j < g.cols) {
     const float *p = g.in[blockIdx.z] + blockIdx.y * g.output_stride + j;
     int i = k;
-    for (; i + 48 < g.parts; i += 64) {
+    for (; i + 48 < parts; i += 64) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) s[q] += p[(i + 16 * q) * g.part_stride];
     }
-    for (; i < g.parts; i += 16) s[0] += p[i * g.part_stride];
+    for (; i < parts; i += 16) s[0] += p[i * g.part_stride];
   }
   part[k][c] = (s[0] + s[1]) + (s[2] + s[3]);
   __syncthreads();

@@ -93,18 +93,20 @@ template <int FROM> int launch_planes(PlanesArgs g, int planes, int64_t rows, hi
   });
 }
 
-// outs[k][o][j] = sum of `parts` rows of ins[k][o], for `count` of them
-int launch_join_sums(const float *const *ins, float *const *outs, int count, int32_t parts, int32_t cols, int64_t outputs, int64_t output_stride,
-                     int64_t part_stride, int64_t out_stride, hipStream_t s) {
-  if (count == 0) return SHAMPOO_OK;
-  JoinSumsArgs g = {};
-  g.output_stride = output_stride; g.part_stride = part_stride; g.out_stride = out_stride; g.parts = parts; g.cols = cols;
-  for (int64_t o = 0; o < outputs; o += 65535) {
-    for (int k = 0; k < count; ++k) { g.in[k] = ins[k] + o * output_stride; g.out[k] = outs[k] + o * out_stride; }
-    join_sums_kernel<<<dim3((cols + 63) / 64, (unsigned)std::min<int64_t>(outputs - o, 65535), count), 1024, 0, s>>>(g);
+// outputs[o][j] = sum of the parts of each of `count` entries of g
+int launch_join_sums(JoinSumsArgs g, int count, int64_t outputs, hipStream_t s) {
+  for (int64_t o = 0; count > 0 && o < outputs; o += 65535) {
+    join_sums_kernel<<<dim3((g.cols + 63) / 64, (unsigned)std::min<int64_t>(outputs - o, 65535), count), 1024, 0, s>>>(g);
     HIP_TRY(hipGetLastError());
+    for (int k = 0; k < count; ++k) { g.in[k] += 65535 * g.output_stride; g.out[k] += 65535 * g.out_stride; }
   }
   return SHAMPOO_OK;
+}
+// out[j] = sum of `parts` rows of in
+int launch_join_rows(const float *in, int64_t parts, int32_t cols, float *out, hipStream_t s) {
+  JoinSumsArgs g = {};
+  g.in[0] = in; g.out[0] = out; g.parts[0] = (int32_t)parts; g.part_stride = cols; g.cols = cols;
+  return launch_join_sums(g, 1, 1, s);
 }
 
 __global__ __launch_bounds__(256) void zero_rows_kernel(unsigned char *p, int64_t row_bytes, int64_t ld_bytes) {
@@ -528,8 +530,7 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
   }
   if (dbias) {
     const int64_t last = c->rows - (p.pieces - 1) * p.piece, parts = (p.pieces - 1) * p.ranges + (round_up(last, TG_BK) + p.range_rows - 1) / p.range_rows;
-    const float *in = p.sums;
-    TRY(launch_join_sums(&in, &dbias, 1, (int32_t)parts, (int32_t)v, 1, 0, v, v, s));
+    TRY(launch_join_rows(p.sums, parts, (int32_t)v, dbias, s));
   }
   return SHAMPOO_OK;
 }
@@ -637,8 +638,7 @@ int shampoo_checkpoint_weight_grad(const void *packed, size_t packed_bytes, int6
     if (dtype == SHAMPOO_GRAD_F32) column_sums_kernel<float><<<grid, 1024, 0, s>>>(static_cast<const float *>(dy), lddy, rows, out, p.part_rows, p.sums);
     else column_sums_kernel<uint16_t><<<grid, 1024, 0, s>>>(static_cast<const uint16_t *>(dy), lddy, rows, out, p.part_rows, p.sums);
     HIP_TRY(hipGetLastError());
-    const float *in = p.sums;
-    TRY(launch_join_sums(&in, &db, 1, (int32_t)p.parts, out, 1, 0, out, out, s));
+    TRY(launch_join_rows(p.sums, p.parts, out, db, s));
   }
   return SHAMPOO_OK;
 }
@@ -700,18 +700,24 @@ int shampoo_residual_norm_backward(const shampoo_residual_norm *c, int32_t packe
   g.chunk_rows = k.rows; g.chunks_per_group = k.per_group; g.teams = k.chunks;
   const bool bias = db_post || db_pre || g.b_post;
   TRY(c->dtype == SHAMPOO_GRAD_F32 ? launch_norm_backward<float>(g, bias, s) : launch_norm_backward<uint16_t>(g, bias, s));
-  const int64_t stride = SUMS * (int64_t)cols;
-  const float *ins[SUMS]; float *outs[SUMS];
-  const bool one_gate = c->gates == 1 && k.per_group;      // joined like the weights
-  if (dgate && k.per_group && !one_gate) {
-    ins[0] = g.partial; outs[0] = dgate;
-    TRY(launch_join_sums(ins, outs, 1, k.per_group, cols, c->gates, k.per_group * stride, stride, cols, s));
-  }
-  float *const wanted[SUMS] = {one_gate ? dgate : nullptr, dw_post, dw_pre, db_post, db_pre};
+  JoinSumsArgs j = {};
+  j.part_stride = SUMS * (int64_t)cols; j.out_stride = cols; j.cols = cols;
   int count = 0;
+  auto add = [&](const float *in, float *out, int64_t parts) { j.in[count] = in; j.out[count] = out; j.parts[count++] = (int32_t)parts; };
+  float *const sums[SUMS] = {nullptr, dw_post, dw_pre, db_post, db_pre};
   for (int q = 0; q < SUMS; ++q)
-    if (wanted[q]) { ins[count] = g.partial + q * cols; outs[count++] = wanted[q]; }
-  TRY(launch_join_sums(ins, outs, count, (int32_t)k.chunks, cols, 1, 0, stride, cols, s));
+    if (sums[q]) add(g.partial + q * cols, sums[q], k.chunks);
+  if (dgate && k.per_group) {
+    j.output_stride = k.per_group * j.part_stride;
+    if (count + c->gates <= JOIN_SUMS) {                   // few gates: in the same launch
+      for (int64_t o = 0; o < c->gates; ++o) add(g.partial + o * j.output_stride, dgate + o * cols, k.per_group);
+    } else {
+      JoinSumsArgs gates = j;
+      gates.in[0] = g.partial; gates.out[0] = dgate; gates.parts[0] = k.per_group;
+      TRY(launch_join_sums(gates, 1, c->gates, s));
+    }
+  }
+  TRY(launch_join_sums(j, count, 1, s));
   return SHAMPOO_OK;
 }
 
