@@ -1,5 +1,5 @@
 """ctypes binding of libshampoo.so: the same entry points as include/shampoo.h
-(the tensors of a step go through _marshal.so, csrc/marshal.cpp).
+(the tensors of a step and of the training operators go through _marshal.so, csrc/marshal.cpp).
 
 Argument marshalling only -- every step of the optimizer runs in the HIP
 kernels of the library.  PyTorch is used for device memory and streams.
@@ -432,67 +432,38 @@ def shampoo_root_inverse_newton(a, epsilon, p, tolerance=1e-6, max_iterations=10
 
 
 # ----------------------------------------------------------------------------
-# Operators of a training pass
+# Operators of a training pass: checks of tensors, outputs and workspaces are csrc/marshal.cpp's
 # ----------------------------------------------------------------------------
-# Many of these calls take less time on the GPU than their arguments take here, so the module is looked up once and tensors are
-# asked for as little as possible.
-_torch = None
+_ops = None
+_codes = {}            # torch's types and the library's
+_DTYPES = ()
 
 
-def _load():
-    global _torch, _codes
+def _load_ops():
+    global _ops, _codes, _DTYPES
     import torch
+    from . import _marshal
+    L = lib()
+    _marshal.use([ctypes.cast(getattr(L, "shampoo_" + name), ctypes.c_void_p).value for name in (
+        "linear_cross_entropy_workspace_bytes", "linear_cross_entropy", "checkpoint_bytes", "checkpoint_pack", "checkpoint_unpack",
+        "checkpoint_activation_grad", "checkpoint_weight_grad_workspace_bytes", "checkpoint_weight_grad", "residual_norm_forward",
+        "residual_norm_backward_workspace_bytes", "residual_norm_backward")])
     _codes = {torch.float32: GRAD_F32, torch.bfloat16: GRAD_BF16}
-    _torch = torch
-    return lib()
+    _DTYPES = (torch.float32, torch.bfloat16)
+    _ops = _marshal
+    return _marshal
 
 
-def _dtype_code(dtype):
+def _code(dtype):
     assert dtype in _codes, f"float32 or bfloat16, not {dtype}"
     return _codes[dtype]
 
 
-def _launch(fn, device, *args):
-    """fn(*args, stream) on a device and its current stream; addresses are integers"""
-    c, index = _torch._C, device.index
-    if index == c._cuda_getDevice():
-        code = fn(*args, c._cuda_getCurrentRawStream(index))
-    else:
-        with _torch.cuda.device(index):
-            code = fn(*args, c._cuda_getCurrentRawStream(index))
-    if code:
-        raise ShampooError(code)
-
-
-def _rows(x, align=1):
-    """A CUDA matrix whose rows are contiguous, as the library reads it (a copy where it is not, or not aligned to `align` bytes)."""
-    assert x.is_cuda and x.dim() == 2, "a CUDA matrix is needed"
-    if not x.is_contiguous():
-        (n, d), (s, e) = x.shape, x.stride()
-        if (d > 1 and e != 1) or (n > 1 and s < d):
-            x = x.contiguous()
-    return x.new_empty(x.shape).copy_(x) if align > 1 and x.data_ptr() % align else x
-
-
-def _ld(x):
-    n, d = x.shape
-    return x.stride(0) if n > 1 else max(d, 1)
-
-
-def _ptr(x):
-    return x.data_ptr() if x is not None else None
-
-
-def _vector(x, shape, device):
-    """A float32 operand of exactly this shape, or None"""
-    if x is None:
-        return None
-    assert x.dtype is _torch.float32 and x.shape == shape and x.device == device, "a float32 tensor of the right shape is needed"
-    return x.contiguous()
-
-
-def _workspace(nbytes, like):
-    return like.new_empty(max(nbytes, 256), dtype=_torch.uint8)
+def _result(r):
+    """An operator's tensors; instead of them the library's error code"""
+    if r.__class__ is int:
+        raise ShampooError(r)
+    return r
 
 
 def shampoo_linear_cross_entropy(x, w, targets, bias=None, weight=None, scale=1.0, grad_dtype=None, gradients=True):
@@ -501,103 +472,44 @@ def shampoo_linear_cross_entropy(x, w, targets, bias=None, weight=None, scale=1.
     x [n, d] and w [v, d]: CUDA, both float32 or both bfloat16; w may be the transposed view of a [d, v] matrix, dw then is one
     too.  targets [n] int64 (outside 0 ... v - 1: ignored), bias [v] and weight [n] float32.  Returns (loss, dx, dw, dbias),
     dbias None without a bias, dw of grad_dtype (default: the type of w); with gradients=False the loss alone."""
-    L = lib() if _torch else _load()
-    code = _dtype_code(x.dtype)
-    assert w.is_cuda and w.dim() == 2 and w.dtype == x.dtype and w.device == x.device and w.shape[1] == x.shape[1]
-    (n, d), v = x.shape, w.shape[0]
-    assert targets.device == x.device and targets.dtype == _torch.int64 and tuple(targets.shape) == (n,)
-    grad_dtype = grad_dtype or w.dtype
-    in_out = v > 1 and w.stride(0) == 1 and (d > 1 or w.stride(1) != 1)      # the view of a matrix [d, v]
-    x, wm = _rows(x, align=16), _rows(w.t() if in_out else w, align=16)
-    targets, bias, weight = targets.contiguous(), _vector(bias, (v,), x.device), _vector(weight, (n,), x.device)
-    loss = x.new_empty((n,), dtype=_torch.float32)
-    dx = dw = dbias = None
-    if gradients:
-        dx, dw = x.new_empty((n, d)), x.new_empty(wm.shape, dtype=grad_dtype)
-        dbias = loss.new_empty((v,)) if bias is not None else None
-    c = CrossEntropy(n, d, v, code, _dtype_code(grad_dtype), IN_OUT if in_out else OUT_IN, 1 if bias is not None else 0,
-                     1 if gradients else 0, _ld(x), _ld(wm), d, wm.shape[1])
-    ws = _workspace(L.shampoo_linear_cross_entropy_workspace_bytes(ctypes.byref(c)), x)
-    _launch(L.shampoo_linear_cross_entropy, x.device, ctypes.byref(c), _ptr(x), _ptr(wm), _ptr(bias), _ptr(targets), _ptr(weight),
-            scale, _ptr(loss), _ptr(dx), _ptr(dw), _ptr(dbias), _ptr(ws), ws.numel())
-    if not gradients:
-        return loss
-    return loss, dx, dw.t() if in_out else dw, dbias
+    ops = _ops or _load_ops()
+    r = _result(ops.cross_entropy(x, w, targets, bias, weight, scale, None if grad_dtype is None else _code(grad_dtype), gradients))
+    return r if gradients else r[0]
 
 
 class Checkpoint:
     """An activation [rows, cols] in 8 bits (codes and shared exponents in one CUDA tensor)."""
+    __slots__ = ("packed", "rows", "cols", "code")
 
-    def __init__(self, packed, rows, cols, dtype):
-        self.packed, self.rows, self.cols, self.dtype = packed, rows, cols, dtype
+    def __init__(self, packed, shape, code):
+        self.packed, (self.rows, self.cols), self.code = packed, shape, code
 
-    @classmethod
-    def like(cls, x):
-        rows, cols = x.shape
-        nbytes = _lib.shampoo_checkpoint_bytes(rows, cols)
-        if nbytes == 0 and rows > 0:
-            raise ShampooError(-7)
-        return cls(_workspace(nbytes, x), rows, cols, x.dtype)
+    @property
+    def dtype(self):
+        """That of the packed matrix"""
+        return _DTYPES[self.code]
 
 
 def shampoo_checkpoint_pack(x):
     """Checkpoint of a CUDA matrix [rows, cols], float32 or bfloat16."""
-    L = lib() if _torch else _load()
-    code, x = _dtype_code(x.dtype), _rows(x)
-    c = Checkpoint.like(x)
-    _launch(L.shampoo_checkpoint_pack, x.device, _ptr(x), code, c.rows, c.cols, _ld(x), _ptr(c.packed), c.packed.numel())
-    return c
+    return Checkpoint(_result((_ops or _load_ops()).pack(x)), x.shape, _codes[x.dtype])
 
 
 def shampoo_checkpoint_unpack(c, activation=ACT_NONE, dtype=None):
     """activation(x) [rows, cols] of what a checkpoint holds, in `dtype` (default: that of the packed matrix)."""
-    L = lib() if _torch else _load()
-    y = c.packed.new_empty((c.rows, c.cols), dtype=dtype or c.dtype)
-    _launch(L.shampoo_checkpoint_unpack, y.device, _ptr(c.packed), c.packed.numel(), c.rows, c.cols, activation, _ptr(y),
-            _dtype_code(y.dtype), c.cols)
-    return y
+    return _result(_ops.unpack(c.packed, c.rows, c.cols, activation, c.code if dtype is None else _code(dtype)))
 
 
 def shampoo_checkpoint_activation_grad(c, dy, activation):
     """dy * activation'(x) for the x that a checkpoint holds."""
-    L = lib() if _torch else _load()
-    assert dy.shape == (c.rows, c.cols) and dy.device == c.packed.device
-    code, dy = _dtype_code(dy.dtype), _rows(dy)
-    dx = dy.new_empty((c.rows, c.cols))
-    _launch(L.shampoo_checkpoint_activation_grad, dy.device, _ptr(c.packed), c.packed.numel(), c.rows, c.cols, activation, _ptr(dy),
-            code, _ld(dy), _ptr(dx), c.cols)
-    return dx
+    return _result(_ops.activation_grad(c.packed, c.rows, c.cols, dy, activation))
 
 
 def shampoo_checkpoint_weight_grad(c, dy, activation=ACT_NONE, grad_dtype=None, out_in=False, bias=False):
     """Gradient of the weight of y = activation(x) W from a checkpoint of x [rows, in] and dy [rows, out]: [in, out], or [out, in]
     with out_in; of grad_dtype (default: the type of dy).  With bias also the column sums of dy, float32."""
-    L = lib() if _torch else _load()
-    assert dy.dim() == 2 and dy.shape[0] == c.rows and dy.device == c.packed.device
-    code, dy = _dtype_code(dy.dtype), _rows(dy, align=16)
-    out = dy.shape[1]
-    dw = dy.new_empty((out, c.cols) if out_in else (c.cols, out), dtype=grad_dtype or dy.dtype)
-    db = dy.new_empty((out,), dtype=_torch.float32) if bias else None
-    grad = _dtype_code(dw.dtype)
-    nbytes = L.shampoo_checkpoint_weight_grad_workspace_bytes(c.rows, c.cols, out, activation, code, _ld(dy), grad, 1 if bias else 0)
-    ws = _workspace(nbytes, dy)
-    _launch(L.shampoo_checkpoint_weight_grad, dy.device, _ptr(c.packed), c.packed.numel(), c.rows, c.cols, activation, _ptr(dy), code,
-            out, _ld(dy), _ptr(dw), grad, OUT_IN if out_in else IN_OUT, dw.shape[1], _ptr(db), _ptr(ws), ws.numel())
-    return (dw, db) if bias else dw
-
-
-def _residual_norm(rows, cols, dtype, device, post, pre, w_post, b_post, gate, w_pre, b_pre, epsilon, scale):
-    gates = 0
-    if gate is not None:
-        if gate.dim() == 1:
-            gate = gate[None]
-        gates = gate.shape[0]
-    row = (cols,)
-    keep = (_vector(w_post, row, device), _vector(b_post, row, device), _vector(gate, (gates, cols), device),
-            _vector(w_pre, row, device), _vector(b_pre, row, device))
-    c = ResidualNorm(rows, cols, _dtype_code(dtype), post, pre, gates, epsilon, scale, *map(_ptr, keep))
-    c._keep = keep
-    return c
+    r = _result(_ops.weight_grad(c.packed, c.rows, c.cols, dy, activation, None if grad_dtype is None else _code(grad_dtype), out_in, bias))
+    return r if bias else r[0]
 
 
 def shampoo_residual_norm_forward(r, f, post=NORM_RMS, pre=NORM_RMS, w_post=None, b_post=None, gate=None, w_pre=None, b_pre=None,
@@ -605,18 +517,15 @@ def shampoo_residual_norm_forward(r, f, post=NORM_RMS, pre=NORM_RMS, w_post=None
     """r_out = r + scale * gate * norm_post(f) and h = norm_pre(r_out) (None where pre is NORM_NONE).  r, f [rows, cols], float32 or
     bfloat16; weights [cols] and gate [cols] or [gates, cols] (every rows / gates rows share one) float32.  With
     checkpoint also those of r and f, for the backward pass: (r_out, h, r8, f8)."""
-    L = lib() if _torch else _load()
-    device = r.device
-    assert r.dim() == 2 and r.shape == f.shape and r.dtype is f.dtype and device == f.device
-    r, f = _rows(r), _rows(f)
-    rows, cols = r.shape
-    c = _residual_norm(rows, cols, r.dtype, device, post, pre, w_post, b_post, gate, w_pre, b_pre, epsilon, scale)
-    r_out = r.new_empty((rows, cols))
-    h = r.new_empty((rows, cols)) if pre != NORM_NONE else None
-    r8, f8 = (Checkpoint.like(r_out), Checkpoint.like(r_out)) if checkpoint else (None, None)
-    _launch(L.shampoo_residual_norm_forward, device, ctypes.byref(c), _ptr(r), _ld(r), _ptr(f), _ld(f), _ptr(r_out), cols, _ptr(h), cols,
-            _ptr(r8.packed) if checkpoint else None, _ptr(f8.packed) if checkpoint else None, r8.packed.numel() if checkpoint else 0)
-    return (r_out, h, r8, f8) if checkpoint else (r_out, h)
+    ops = _ops or _load_ops()
+    r_out, h, r8, f8 = _result(ops.norm_forward(r, f, post, pre, w_post, b_post, gate, w_pre, b_pre, epsilon, scale, checkpoint))
+    if not checkpoint:
+        return r_out, h
+    code = _codes[r.dtype]
+    return r_out, h, Checkpoint(r8, r.shape, code), Checkpoint(f8, r.shape, code)
+
+
+_NORM_GRADIENTS = ("dr", "df", "dgate", "dw_post", "db_post", "dw_pre", "db_pre")
 
 
 def shampoo_residual_norm_backward(r, f, dr_out, dh, post=NORM_RMS, pre=NORM_RMS, w_post=None, b_post=None, gate=None, w_pre=None,
@@ -624,31 +533,10 @@ def shampoo_residual_norm_backward(r, f, dr_out, dh, post=NORM_RMS, pre=NORM_RMS
     """Gradients of shampoo_residual_norm_forward from those of r_out (None: zero) and h (None where there is no h); r and f: the
     matrices, or the checkpoints that the forward pass wrote.  Returns a dict of dr, df, and float32 dgate, dw_post, db_post,
     dw_pre, db_pre, None for those of what is not there."""
-    L = lib() if _torch else _load()
-    packed = isinstance(r, Checkpoint)
-    assert packed == isinstance(f, Checkpoint)
-    dtype, device = r.dtype, (r.packed.device if packed else r.device)
-    rows, cols = (r.rows, r.cols) if packed else r.shape
-    if packed:
-        assert (f.rows, f.cols, f.packed.device) == (rows, cols, device)
+    ops = _ops or _load_ops()
+    if isinstance(r, Checkpoint):
+        assert (f.rows, f.cols, f.code) == (r.rows, r.cols, r.code), "checkpoints of one shape and type are needed"
+        out = ops.norm_backward(r.packed, f.packed, r.rows, r.cols, r.code, dr_out, dh, post, pre, w_post, b_post, gate, w_pre, b_pre, epsilon, scale)
     else:
-        assert f.shape == r.shape and f.dtype == dtype and f.device == device
-        r, f = _rows(r), _rows(f)
-    for d in (dr_out, dh):
-        assert d is None or (d.device == device and d.dtype is dtype and d.shape == (rows, cols))
-    dr_out, dh = (None if d is None else _rows(d) for d in (dr_out, dh))
-    c = _residual_norm(rows, cols, dtype, device, post, pre, w_post, b_post, gate, w_pre, b_pre, epsilon, scale)
-    like = r.packed if packed else r
-    float32 = _torch.float32
-    vector = lambda wanted, shape=(cols,): like.new_empty(shape, dtype=float32) if wanted else None
-    out = {"dr": like.new_empty((rows, cols), dtype=dtype), "df": like.new_empty((rows, cols), dtype=dtype),
-           "dgate": like.new_empty(gate.shape, dtype=float32) if gate is not None else None,
-           "dw_post": vector(post != NORM_NONE), "db_post": vector(b_post is not None and post == NORM_LAYER),
-           "dw_pre": vector(pre != NORM_NONE), "db_pre": vector(b_pre is not None and pre == NORM_LAYER)}
-    ws = _workspace(L.shampoo_residual_norm_backward_workspace_bytes(ctypes.byref(c)), like)
-    _launch(L.shampoo_residual_norm_backward, device, ctypes.byref(c), 1 if packed else 0, _ptr(r.packed if packed else r), cols if packed else _ld(r),
-            _ptr(f.packed if packed else f), cols if packed else _ld(f),
-            _ptr(dr_out), _ld(dr_out) if dr_out is not None else 0, _ptr(dh), _ld(dh) if dh is not None else 0,
-            _ptr(out["dr"]), cols, _ptr(out["df"]), cols, *[_ptr(v) for v in list(out.values())[2:]],
-            _ptr(ws), ws.numel())
-    return out
+        out = ops.norm_backward(r, f, 0, 0, None, dr_out, dh, post, pre, w_post, b_post, gate, w_pre, b_pre, epsilon, scale)
+    return dict(zip(_NORM_GRADIENTS, _result(out)))
