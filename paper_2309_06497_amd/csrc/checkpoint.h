@@ -33,12 +33,13 @@ __device__ __forceinline__ uint32_t exponent_byte(uint32_t largest) {
   return (largest + 0x10000u) >> 23;                        // e + 127 = s + 133
 }
 // 2^-s and 2^s of an exponent byte (27 ... 254); for byte 0 the codes are zero, for 255 the scale makes them NaN
-__device__ __forceinline__ float code_per_value(uint32_t byte) { return __uint_as_float((260u - byte) << 23); }
+__device__ __forceinline__ float code_per_value(uint32_t byte) { return __uint_as_float((260u - min(max(byte, 27u), 254u)) << 23); }
 __device__ __forceinline__ float value_per_code(uint32_t byte) {
   return byte == 255u ? __uint_as_float(0x7fc00000u) : byte < 27u ? 0.f : __uint_as_float((byte - 6u) << 23);
 }
 
-// Eight neighbouring values of a lane, four neighbouring lanes a group: their codes, and the group's byte in `byte`
+// Eight neighbouring values of a lane, four neighbouring lanes a group: their codes, and the group's byte in `byte`.  Beside
+// 1.5 2^23 the unit of a float32 is 1: adding that rounds x 2^-s to even and leaves the code in the low byte.
 __device__ __forceinline__ uint2 pack8(const f32x8 &x, uint32_t &byte) {
   uint32_t largest = 0;
 #pragma unroll
@@ -46,19 +47,23 @@ __device__ __forceinline__ uint2 pack8(const f32x8 &x, uint32_t &byte) {
   largest = max(largest, (uint32_t)__shfl_xor((int)largest, 1, 64));
   largest = max(largest, (uint32_t)__shfl_xor((int)largest, 2, 64));
   byte = exponent_byte(largest);
-  uint32_t w[2] = {0u, 0u};
-  if (byte == 255u) { w[0] = w[1] = 0x01010101u; }           // 1 x NaN
-  else if (byte != 0u) {
-    const float per = code_per_value(byte);
+  const float per = code_per_value(byte);
+  uint32_t q[8], w[2];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[e >> 2] |= ((uint32_t)(int)rintf(x.v[e] * per) & 255u) << (8 * (e & 3));
-  }
+  for (int e = 0; e < 8; ++e) q[e] = __float_as_uint(fmaf(x.v[e], per, 12582912.f));
+#pragma unroll
+  for (int h = 0; h < 2; ++h)                                // the low bytes of four, first one lowest
+    w[h] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[4 * h + 3], q[4 * h + 2], 0x0c0c0400u), __builtin_amdgcn_perm(q[4 * h + 1], q[4 * h], 0x0c0c0400u), 0x05040100u);
+  if (byte == 0u) w[0] = w[1] = 0u;
+  if (byte == 255u) w[0] = w[1] = 0x01010101u;               // 1 x NaN
   return make_uint2(w[0], w[1]);
 }
+// from q + 128, which a conversion takes out of its word (128 2^s itself may be past float32)
 __device__ __forceinline__ f32x8 unpack8(uint2 w, float scale) {
   f32x8 r;
+  const uint32_t u[2] = {w.x ^ 0x80808080u, w.y ^ 0x80808080u};
 #pragma unroll
-  for (int e = 0; e < 8; ++e) r.v[e] = (float)(int8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3))) * scale;
+  for (int e = 0; e < 8; ++e) r.v[e] = ((float)((u[e >> 2] >> (8 * (e & 3))) & 255u) - 128.f) * scale;
   return r;
 }
 // eight values at column c (a multiple of 8 below pitch) of row i

@@ -49,20 +49,24 @@ __device__ __forceinline__ float wave_sum(float x) {
 #undef ADD_DPP
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 63));
 }
-// sums over the threads of a row, for all of them; `slot` (two floats per wavefront): one that no other sum uses at the time
-template <int TPR> __device__ __forceinline__ void row_sums(float &x, float &y, float *slot) {
-  x = wave_sum(x); y = wave_sum(y);
+// sums over the threads of a row, for all of them; `slot` (two floats per wavefront): one that no other sum uses at the time.  BOTH:
+// of x and y, otherwise of x alone.
+template <int TPR, bool BOTH> __device__ __forceinline__ void row_sums(float &x, float &y, float *slot) {
+  x = wave_sum(x);
+  if constexpr (BOTH) y = wave_sum(y);
   if constexpr (TPR > 64) {
+    constexpr int WAVES = TPR / 64;
     const int wave = threadIdx.x >> 6;
-    if ((threadIdx.x & 63) == 0) { slot[2 * wave] = x; slot[2 * wave + 1] = y; }
+    if ((threadIdx.x & 63) == 0) { slot[wave] = x; if constexpr (BOTH) slot[WAVES + wave] = y; }
     __syncthreads();
-    x = slot[0] + slot[2];
-    y = slot[1] + slot[3];
-    if constexpr (TPR >= 256) { x += slot[4] + slot[6]; y += slot[5] + slot[7]; }
-    if constexpr (TPR == 512) {
-      x += (slot[8] + slot[10]) + (slot[12] + slot[14]);
-      y += (slot[9] + slot[11]) + (slot[13] + slot[15]);
-    }
+    auto all = [](const float *p) {
+      float s = p[0] + p[1];
+      if constexpr (WAVES >= 4) s += p[2] + p[3];
+      if constexpr (WAVES == 8) s += (p[4] + p[5]) + (p[6] + p[7]);
+      return s;
+    };
+    x = all(slot);
+    if constexpr (BOTH) y = all(slot + WAVES);
   }
 }
 constexpr int NORM_SLOT = 16;       // floats of a slot
@@ -83,7 +87,7 @@ template <int TPR, int NJ> __device__ __forceinline__ float normalise(f32x8 (&x)
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 8; ++e) s += x[j].v[e];
-    row_sums<TPR>(s, unused, slot);
+    row_sums<TPR, false>(s, unused, slot);
     const float mean = s * per;
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
@@ -95,7 +99,7 @@ template <int TPR, int NJ> __device__ __forceinline__ float normalise(f32x8 (&x)
   for (int j = 0; j < NJ; ++j)
 #pragma unroll
     for (int e = 0; e < 8; ++e) s += x[j].v[e] * x[j].v[e];
-  row_sums<TPR>(s, unused, slot + NORM_SLOT);
+  row_sums<TPR, false>(s, unused, slot + NORM_SLOT);
   const float inv = rsqrtf(s * per + eps);
 #pragma unroll
   for (int j = 0; j < NJ; ++j)
@@ -168,26 +172,33 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void residual_norm_forward_k
   }
 }
 
-// dx of a norm in place of dy w (in `d`): inv (d - n mean(d n) - mean(d)).  Padding of d may become anything.
-template <int TPR, int NJ> __device__ __forceinline__ void norm_gradient(f32x8 (&d)[NJ], const f32x8 (&n)[NJ], float inv, int kind, int cols, float *slot) {
+// dx of a norm in place of dy w (in `d`): inv (d - n mean(d n) - mean(d)).  Padding stays zero.
+template <int TPR, int NJ> __device__ __forceinline__ void norm_gradient(f32x8 (&d)[NJ], const f32x8 (&n)[NJ], const RowPieces<TPR, NJ> &at, float inv, int kind, float *slot) {
   float sn = 0.f, s = 0.f;
 #pragma unroll
   for (int j = 0; j < NJ; ++j)
 #pragma unroll
     for (int e = 0; e < 8; ++e) sn += d[j].v[e] * n[j].v[e];
+  const float per = -inv / (float)at.cols;
   if (kind == NORM_LAYER) {
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 8; ++e) s += d[j].v[e];
+    row_sums<TPR, true>(sn, s, slot);
+    sn *= per; s *= per;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d[j].v[e] = at.has(j, e) ? inv * d[j].v[e] + (n[j].v[e] * sn + s) : 0.f;
+  } else {
+    row_sums<TPR, false>(sn, s, slot);
+    sn *= per;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d[j].v[e] = inv * d[j].v[e] + n[j].v[e] * sn;
   }
-  row_sums<TPR>(sn, s, slot);
-  const float per = 1.f / (float)cols;
-  sn *= -per * inv; s *= -per * inv;
-#pragma unroll
-  for (int j = 0; j < NJ; ++j)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) d[j].v[e] = inv * d[j].v[e] + (n[j].v[e] * sn + s);
 }
 
 // What a row brings, as it comes from memory: r and f as eight values, or eight codes and their exponent byte in the same registers.
@@ -228,17 +239,28 @@ template <typename T, int NJ> struct RawRow {
   }
 };
 
-// Rows of weights, kept in registers over a team's rows where a thread has one piece, and otherwise read where they are used.
+// Rows of weights (times alpha), kept in registers over a team's rows where a thread has one piece, and otherwise read where they
+// are used.  No weights: ones.
 template <int NJ> struct NormWeight {
   static constexpr bool KEEP = NJ == 1;
   f32x8 kept;
   const float *p;
-  template <typename At> __device__ __forceinline__ void set(const float *w, const At &at) {
-    p = w;
-    if constexpr (KEEP) { if (w) kept = load8(w, at.column(0), at.cols); }
+  float alpha;
+  template <typename At> __device__ __forceinline__ void set(const float *w, const At &at, float by = 1.f) {
+    p = w; alpha = by;
+    if constexpr (KEEP) kept = read(at, 0);
+  }
+  template <typename At> __device__ __forceinline__ f32x8 read(const At &at, int j) const {
+    f32x8 x = {{alpha, alpha, alpha, alpha, alpha, alpha, alpha, alpha}};
+    if (p) {
+      x = load8(p, at.column(j), at.cols);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x.v[e] *= alpha;
+    }
+    return x;
   }
   template <typename At> __device__ __forceinline__ f32x8 get(const At &at, int j) const {
-    if constexpr (KEEP) return kept; else return load8(p, at.column(j), at.cols);
+    if constexpr (KEEP) return kept; else return read(at, j);
   }
 };
 
@@ -270,7 +292,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR, NJ == 1 && TPR <= 256 && siz
   NormWeight<NJ> w_post, b_post, w_pre, gate;
   w_post.set(g.post != NORM_NONE ? g.w_post : nullptr, at); w_pre.set(g.pre != NORM_NONE ? g.w_pre : nullptr, at);
   b_post.set(BIAS ? g.b_post : nullptr, at);
-  gate.set(g.gate ? g.gate + group * g.cols : nullptr, at);
+  gate.set(g.gate ? g.gate + group * g.cols : nullptr, at, g.alpha);
   RawRow<T, NJ> raw;
   if (i0 < i1) raw.load(g, at, i0);
   for (int64_t i = i0; i < i1; ++i) {
@@ -304,15 +326,9 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR, NJ == 1 && TPR <= 256 && siz
     if (g.pre != NORM_NONE) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        const f32x8 u = block(j);
-        if (g.gate) {
-          const f32x8 w = gate.get(at, j);
+        const f32x8 u = block(j), w = gate.get(at, j);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) r[j].v[e] += g.alpha * w.v[e] * u.v[e];
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) r[j].v[e] += g.alpha * u.v[e];
-        }
+        for (int e = 0; e < 8; ++e) r[j].v[e] += w.v[e] * u.v[e];
       }
       const float inv = normalise(r, at, g.pre, g.epsilon, slot + 2 * NORM_SLOT);
 #pragma unroll
@@ -325,7 +341,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR, NJ == 1 && TPR <= 256 && siz
           d[j].v[e] *= w.v[e];
         }
       }
-      norm_gradient<TPR, NJ>(d, r, inv, g.pre, g.cols, slot + 4 * NORM_SLOT);
+      norm_gradient<TPR, NJ>(d, r, at, inv, g.pre, slot + 4 * NORM_SLOT);
     } else {
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
@@ -340,13 +356,14 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR, NJ == 1 && TPR <= 256 && siz
         for (int e = 0; e < 8; ++e) d[j].v[e] += x.v[e];
       }
       store8(static_cast<T *>(g.dr) + i * g.ld_dr, at.column(j), g.cols, d[j]);
+      if (g.gate) {                                     // times alpha at the end
+        const f32x8 u = block(j);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) d[j].v[e] = at.has(j, e) ? d[j].v[e] * g.alpha : 0.f;
-      if (g.gate) {
-        const f32x8 w = gate.get(at, j), u = block(j);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { sum[SUM_GATE][j].v[e] += d[j].v[e] * u.v[e]; d[j].v[e] *= w.v[e]; }
+        for (int e = 0; e < 8; ++e) sum[SUM_GATE][j].v[e] += d[j].v[e] * u.v[e];
       }
+      const f32x8 w = gate.get(at, j);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d[j].v[e] *= w.v[e];
       if (g.post != NORM_NONE) {
         const f32x8 w = w_post.get(at, j);
 #pragma unroll
@@ -357,13 +374,17 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR, NJ == 1 && TPR <= 256 && siz
         }
       }
     }
-    if (g.post != NORM_NONE) norm_gradient<TPR, NJ>(d, f, inv_f, g.post, g.cols, slot + 5 * NORM_SLOT);
+    if (g.post != NORM_NONE) norm_gradient<TPR, NJ>(d, f, at, inv_f, g.post, slot + 5 * NORM_SLOT);
 #pragma unroll
     for (int j = 0; j < NJ; ++j) store8(static_cast<T *>(g.df) + i * g.ld_df, at.column(j), g.cols, d[j]);
     if (left && --left == 0) {
       if (g.dgate) {
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) store8(g.dgate + group * g.cols, at.column(j), g.cols, sum[SUM_GATE][j]);
+        for (int j = 0; j < NJ; ++j) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sum[SUM_GATE][j].v[e] *= g.alpha;
+          store8(g.dgate + group * g.cols, at.column(j), g.cols, sum[SUM_GATE][j]);
+        }
       }
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
@@ -371,7 +392,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR, NJ == 1 && TPR <= 256 && siz
         for (int e = 0; e < 8; ++e) sum[SUM_GATE][j].v[e] = 0.f;
       left = g.group_rows;
       ++group;
-      if (g.gate && i + 1 < i1) gate.set(g.gate + group * g.cols, at);
+      if (g.gate && i + 1 < i1) gate.set(g.gate + group * g.cols, at, g.alpha);
     }
   }
   float *out = g.partial + team * SUMS * g.cols;
@@ -379,6 +400,12 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR, NJ == 1 && TPR <= 256 && siz
   for (int q = 0; q < NSUM; ++q) {
     const bool wanted = q == SUM_GATE ? g.gate && g.chunks_per_group : q == SUM_W_POST ? g.post != NORM_NONE : q == SUM_W_PRE ? g.pre != NORM_NONE : true;
     if (!wanted) continue;
+    if (q == SUM_GATE) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[SUM_GATE][j].v[e] *= g.alpha;
+    }
 #pragma unroll
     for (int j = 0; j < NJ; ++j) store8(out + q * g.cols, at.column(j), g.cols, sum[q][j]);
   }
