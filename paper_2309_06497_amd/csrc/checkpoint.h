@@ -153,8 +153,7 @@ struct PlanesArgs {
   int32_t cols, activation;
 };
 enum { FROM_PACKED = 0, FROM_F32 = 1, FROM_BF16 = 2 };
-template <int FROM, int PLANES> __global__ __launch_bounds__(256) void planes_kernel(const PlanesArgs g) {
-  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+template <int FROM, int PLANES> __device__ __forceinline__ void planes_piece(const PlanesArgs &g, uint32_t i) {
   if (i >= g.pieces) return;
   const uint32_t r = i / g.per_row;
   const int c = (int)(i - r * g.per_row) * 8;
@@ -185,6 +184,13 @@ template <int FROM, int PLANES> __global__ __launch_bounds__(256) void planes_ke
     w.z = q[4][t] | (uint32_t)q[5][t] << 16; w.w = q[6][t] | (uint32_t)q[7][t] << 16;
     *reinterpret_cast<uint4 *>(g.out + t * g.plane + row * g.ld + c) = w;
   }
+}
+template <int FROM, int PLANES> __global__ __launch_bounds__(256) void planes_kernel(const PlanesArgs g) { planes_piece<FROM, PLANES>(g, blockIdx.x * 256u + threadIdx.x); }
+// Both operands of a product in one launch: the first `blocks` workgroups have g, the others h.
+template <int FROM_G, int PLANES_G, int FROM_H, int PLANES_H>
+__global__ __launch_bounds__(256) void planes_pair_kernel(const PlanesArgs g, const PlanesArgs h, uint32_t blocks) {
+  if (blockIdx.x < blocks) planes_piece<FROM_G, PLANES_G>(g, blockIdx.x * 256u + threadIdx.x);
+  else planes_piece<FROM_H, PLANES_H>(h, (blockIdx.x - blocks) * 256u + threadIdx.x);
 }
 
 // Column sums of x, in an order that does not depend on the launch: workgroup (j / 64, part) sums its rows, 16 threads a column, and

@@ -87,6 +87,15 @@ __device__ __forceinline__ void join_exp(float &m, float &s, float n, float t) {
   const float a = m == -INFINITY ? s : s * __builtin_amdgcn_exp2f((m - top) * LOG2_E), b = n == -INFINITY ? t : t * __builtin_amdgcn_exp2f((n - top) * LOG2_E);
   m = top; s = a + b;
 }
+__device__ __forceinline__ void row_end(const RowLossArgs &g, int i, float m, float s, float &lse, float &coef) {
+  const float l = (m == -INFINITY ? 0.f : m) + logf(s);         // no class left: -infinity
+  const int64_t t = g.targets[i];
+  const bool valid = t >= 0 && t < g.classes;
+  lse = l;
+  coef = valid ? g.scale * (g.weight ? g.weight[i] : 1.f) : 0.f;
+  const float zt = valid ? g.target_z[i] : 0.f;
+  g.loss[i] = !valid ? 0.f : zt == -INFINITY ? INFINITY : l - zt;
+}
 __global__ __launch_bounds__(1024) void row_loss_kernel(const RowLossArgs g) {
   __shared__ float2 part[16][16];
   const int r = threadIdx.x & 15, k = threadIdx.x >> 4, i = blockIdx.x * 16 + r;
@@ -107,31 +116,47 @@ __global__ __launch_bounds__(1024) void row_loss_kernel(const RowLossArgs g) {
   __syncthreads();
   if (k != 0 || i >= g.rows) return;
   for (int p = 1; p < 16; ++p) join_exp(m, s, part[p][r].x, part[p][r].y);
-  const float lse = (m == -INFINITY ? 0.f : m) + logf(s);       // no class left: -infinity
-  const int64_t t = g.targets[i];
-  const bool valid = t >= 0 && t < g.classes;
-  g.lse[i] = lse;
-  g.coef[i] = valid ? g.scale * (g.weight ? g.weight[i] : 1.f) : 0.f;
-  const float zt = valid ? g.target_z[i] : 0.f;
-  g.loss[i] = !valid ? 0.f : zt == -INFINITY ? INFINITY : lse - zt;
+  row_end(g, i, m, s, g.lse[i], g.coef[i]);
 }
 
 // g of a piece of the rows, zeros from classes to ldg and in the rows from `rows` to the next multiple of 64.  A thread has eight columns of the rows of its range.
 struct SoftmaxGradArgs {
+  RowLossArgs row;
   const float *z; int64_t ldg;       // float32 logits
-  const float2 *stats; int64_t stats_ld; int32_t span;
-  const float *lse, *coef; const int64_t *targets;
+  int32_t span;
   uint16_t *out; int64_t plane;      // [plane][rows][ldg]; 16-bit logits are read here
   float *sums;                       // [ranges][classes] column sums of g, or nullptr
-  int32_t rows, classes, per_range;
+  int32_t per_range;                 // at most 64
 };
-// PLANES = 0: one plane, in the place of 16-bit logits.  Four rows are on their way together.
+// PLANES = 0: one plane, in the place of 16-bit logits.  Four rows are on their way together.  Where a workgroup has the rows' whole
+// width (up to 2048 classes) it ends the rows' sums too: one launch instead of two.
 template <int PLANES> __global__ __launch_bounds__(256) void softmax_grad_kernel(const SoftmaxGradArgs g) {
   constexpr int OUT = PLANES ? PLANES : 1, AHEAD = 4;
-  const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
+  __shared__ float row_lse[64], row_coef[64];
+  const int c = (blockIdx.x * 256 + threadIdx.x) * 8, rows = g.row.rows, classes = g.row.classes;
+  const int end = (rows + 63) & ~63, i0 = blockIdx.y * g.per_range, i1 = min(end, i0 + g.per_range);
+  {
+    const int r = threadIdx.x >> 2, i = i0 + r;                 // four threads a row
+    float lse = 0.f, coef = 0.f;                                // nothing behind the last row
+    if (gridDim.x == 1) {
+      float m = -INFINITY, s = 0.f;
+      if (i < min(i1, rows))
+        for (int p = threadIdx.x & 3; p < g.row.spans; p += 4) {
+          const float2 x = g.row.stats[p * g.row.stats_ld + i];
+          join_exp(m, s, x.x, x.y);
+        }
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) {
+        const float n = __shfl_xor(m, o, 64), t = __shfl_xor(s, o, 64);
+        join_exp(m, s, n, t);
+      }
+      if ((threadIdx.x & 3) == 0 && i < min(i1, rows)) row_end(g.row, i, m, s, lse, coef);
+    } else if (i < min(i1, rows)) { lse = g.row.lse[i]; coef = g.row.coef[i]; }
+    if ((threadIdx.x & 3) == 0) { row_lse[r] = lse; row_coef[r] = coef; }
+  }
+  __syncthreads();
   if (c >= g.ldg) return;
-  const int end = (g.rows + 63) & ~63, i0 = blockIdx.y * g.per_range, i1 = min(end, i0 + g.per_range);
-  const int64_t span = (int64_t)(c / g.span) * g.stats_ld;
+  const int64_t span = (int64_t)(c / g.span) * g.row.stats_ld;
   f32x8 sum = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
   for (int first = i0; first < i1; first += AHEAD) {
     Raw8<float> z[PLANES ? AHEAD : 1];
@@ -142,9 +167,9 @@ template <int PLANES> __global__ __launch_bounds__(256) void softmax_grad_kernel
     for (int a = 0; a < AHEAD; ++a) {
       const int i = min(first + a, i1 - 1);
       const int64_t at = (int64_t)i * g.ldg + c;
-      const bool there = i < g.rows;
-      lse[a] = there ? g.lse[i] : 0.f; k[a] = there ? g.coef[i] : 0.f; t[a] = (there ? g.targets[i] : 0) - c;
-      if constexpr (PLANES == 0) { q16[a] = raw_load8(g.out + at, 0, 8); top[a] = there ? g.stats[span + i].x : 0.f; }
+      const bool there = i < rows;
+      lse[a] = row_lse[i - i0]; k[a] = row_coef[i - i0]; t[a] = (there ? g.row.targets[i] : 0) - c;
+      if constexpr (PLANES == 0) { q16[a] = raw_load8(g.out + at, 0, 8); top[a] = there ? g.row.stats[span + i].x : 0.f; }
       else z[a] = raw_load8(g.z + at, 0, 8);
     }
 #pragma unroll
@@ -167,7 +192,7 @@ template <int PLANES> __global__ __launch_bounds__(256) void softmax_grad_kernel
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float x = 0.f;
-        if (k[a] != 0.f && c + e < g.classes && lse[a] != -INFINITY) x = k[a] * (p.v[e] - (t[a] == e ? 1.f : 0.f));
+        if (k[a] != 0.f && c + e < classes && lse[a] != -INFINITY) x = k[a] * (p.v[e] - (t[a] == e ? 1.f : 0.f));
         sum.v[e] += x;
         bf16_planes_of<OUT>(x, q[e]);
       }
@@ -183,7 +208,7 @@ template <int PLANES> __global__ __launch_bounds__(256) void softmax_grad_kernel
   if (!g.sums) return;
 #pragma unroll
   for (int e = 0; e < 8; ++e)
-    if (c + e < g.classes) g.sums[(int64_t)blockIdx.y * g.classes + c + e] = sum.v[e];
+    if (c + e < classes) g.sums[(int64_t)blockIdx.y * classes + c + e] = sum.v[e];
 }
 
 }  // namespace shampoo

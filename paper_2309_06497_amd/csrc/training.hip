@@ -83,14 +83,39 @@ Packed packed_view(const void *p, int64_t rows, int32_t cols) {
   return v;
 }
 
-// bf16 planes of a matrix or of a(checkpoint)
-template <int FROM> int launch_planes(PlanesArgs g, int planes, int64_t rows, hipStream_t s) {
-  g.per_row = (uint32_t)(g.ld / 8);
-  return by_rows(rows, g.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
-    g.row0 = r; g.pieces = pieces;
-    if (planes == 1) planes_kernel<FROM, 1><<<grid, 256, 0, s>>>(g);
-    else planes_kernel<FROM, 3><<<grid, 256, 0, s>>>(g);
+// bf16 planes of a matrix or of a(checkpoint): what planes_kernel has to do for it
+struct PlanesTask { PlanesArgs g; int from, planes; int64_t rows; };
+template <typename F> void planes_variant(const PlanesTask &t, F &&f) {
+  if (t.from == FROM_F32) f(std::integral_constant<int, FROM_F32>(), std::integral_constant<int, 3>());
+  else if (t.from == FROM_BF16) f(std::integral_constant<int, FROM_BF16>(), std::integral_constant<int, 1>());
+  else if (t.planes == 1) f(std::integral_constant<int, FROM_PACKED>(), std::integral_constant<int, 1>());
+  else f(std::integral_constant<int, FROM_PACKED>(), std::integral_constant<int, 3>());
+}
+int launch_planes(PlanesTask t, hipStream_t s) {
+  t.g.per_row = (uint32_t)(t.g.ld / 8);
+  return by_rows(t.rows, t.g.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
+    t.g.row0 = r; t.g.pieces = pieces;
+    planes_variant(t, [&](auto from, auto planes) { planes_kernel<decltype(from)::value, decltype(planes)::value><<<grid, 256, 0, s>>>(t.g); });
   });
+}
+// Two of them, in one launch where both are small: up to 2^22 pieces of eight together a launch's latency counts.  g of FROM_F32 with h of the same,
+// FROM_BF16 likewise, or g of FROM_PACKED with either.
+int launch_planes(PlanesTask g, PlanesTask h, hipStream_t s) {
+  g.g.per_row = (uint32_t)(g.g.ld / 8); h.g.per_row = (uint32_t)(h.g.ld / 8);
+  const int64_t pg = g.rows * g.g.per_row, ph = h.rows * h.g.per_row;
+  if (pg + ph > (1 << 22)) { TRY(launch_planes(g, s)); return launch_planes(h, s); }
+  g.g.pieces = (uint32_t)pg; h.g.pieces = (uint32_t)ph;
+  const uint32_t blocks = (uint32_t)((pg + 255) / 256), all = blocks + (uint32_t)((ph + 255) / 256);
+  planes_variant(h, [&](auto from, auto planes) {
+    constexpr int FROM = decltype(from)::value, PLANES = decltype(planes)::value;
+    if constexpr (FROM != FROM_PACKED) {
+      if (g.from != FROM_PACKED) planes_pair_kernel<FROM, PLANES, FROM, PLANES><<<dim3(all), 256, 0, s>>>(g.g, h.g, blocks);
+      else if (g.planes == 1) planes_pair_kernel<FROM_PACKED, 1, FROM, PLANES><<<dim3(all), 256, 0, s>>>(g.g, h.g, blocks);
+      else planes_pair_kernel<FROM_PACKED, 3, FROM, PLANES><<<dim3(all), 256, 0, s>>>(g.g, h.g, blocks);
+    }
+  });
+  HIP_TRY(hipGetLastError());
+  return SHAMPOO_OK;
 }
 
 // outputs[o][j] = sum of the parts of each of `count` entries of g
@@ -228,12 +253,15 @@ struct Source {
   int planes() const { return dtype == SHAMPOO_GRAD_F32 ? 3 : 1; }
   int64_t ldp() const { return round_up(cols, 64); }
   uint16_t *take(Arena &a) const { return copy() ? a.take<uint16_t>((size_t)planes() * rows * ldp()) : nullptr; }
-  int operand(const void *p, uint16_t *scratch, int lie, Operand &o, hipStream_t s) const {
-    if (!copy()) { o = {static_cast<const uint16_t *>(p), ld, 0, 1, lie}; return SHAMPOO_OK; }
-    o = {scratch, ldp(), rows * ldp(), planes(), lie};
-    PlanesArgs g = {};
-    g.rows = rows; g.x = p; g.ldx = ld; g.out = scratch; g.plane = o.plane; g.ld = o.ld; g.cols = (int32_t)cols;
-    return dtype == SHAMPOO_GRAD_F32 ? launch_planes<FROM_F32>(g, 3, rows, s) : launch_planes<FROM_BF16>(g, 1, rows, s);
+  Operand operand(const void *p, const uint16_t *scratch, int lie) const {
+    if (!copy()) return {static_cast<const uint16_t *>(p), ld, 0, 1, lie};
+    return {scratch, ldp(), rows * ldp(), planes(), lie};
+  }
+  PlanesTask task(const void *p, uint16_t *scratch) const {
+    PlanesTask t = {};
+    t.from = dtype == SHAMPOO_GRAD_F32 ? FROM_F32 : FROM_BF16; t.planes = planes(); t.rows = rows;
+    t.g.rows = rows; t.g.x = p; t.g.ldx = ld; t.g.out = scratch; t.g.plane = rows * ldp(); t.g.ld = ldp(); t.g.cols = (int32_t)cols;
+    return t;
   }
 };
 
@@ -329,13 +357,13 @@ int weight_grad_plan(int64_t rows, int32_t in, int32_t out, int32_t activation, 
                               std::max<int64_t>(PIECE_ROWS, (int64_t)(PLANE_BYTES / ((size_t)p.ldp * 2 * p.planes)) / PIECE_ROWS * PIECE_ROWS));
   p.pieces = (rows + p.piece - 1) / p.piece;
   p.sum = p.pieces > 1 && grad_dtype == SHAMPOO_GRAD_BF16;
-  p.part_rows = std::max<int64_t>(64, (rows + 63) / 64);
+  p.part_rows = rows <= 512 ? 512 : std::max<int64_t>(64, (rows + 63) / 64);      // 512 rows: one part, no second launch
   p.parts = std::max<int64_t>(1, (rows + p.part_rows - 1) / p.part_rows);
   Arena a(workspace);
   p.xp = a.take<uint16_t>((size_t)p.planes * p.piece * p.ldp);
   p.dyp = p.dy.take(a);
   if (p.sum) p.acc = a.take<float>((size_t)in * out);
-  if (bias) p.sums = a.take<float>((size_t)p.parts * out);
+  if (bias && p.parts > 1) p.sums = a.take<float>((size_t)p.parts * out);
   size_t part = 0;
   for (int64_t n : {p.piece, rows - std::max<int64_t>(0, p.pieces - 1) * p.piece, rows}) {
     if (n < 1 || n > p.piece) continue;
@@ -471,9 +499,10 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
     if (dbias) TRY(launch_zero(dbias, 1, v, v, 4, s));
     return SHAMPOO_OK;
   }
-  Operand xo, wo;
-  TRY(p.x.operand(x, p.xp, LIE_K, xo, s));
-  TRY(p.w.operand(w, p.wp, out_in ? LIE_K : LIE_ROWS, wo, s));
+  const Operand xo = p.x.operand(x, p.xp, LIE_K), wo = p.w.operand(w, p.wp, out_in ? LIE_K : LIE_ROWS);
+  if (p.x.copy() && p.w.copy()) TRY(launch_planes(p.x.task(x, p.xp), p.w.task(w, p.wp), s));
+  else if (p.x.copy()) TRY(launch_planes(p.x.task(x, p.xp), s));
+  else if (p.w.copy()) TRY(launch_planes(p.w.task(w, p.wp), s));
   for (int64_t k = 0; k < p.pieces; ++k) {
     const int64_t i0 = k * p.piece, n = std::min(p.piece, c->rows - i0);
     Operand xk = xo;
@@ -498,16 +527,18 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
     HIP_TRY(hipGetLastError());
     const RowLossArgs r = {p.stats, p.piece, p.target_z, targets + i0, weight ? weight + i0 : nullptr, scale, p.lse, p.coef, loss + i0,
                            (int32_t)n, (int32_t)v, (int32_t)((v + span - 1) / span)};
-    row_loss_kernel<<<dim3((unsigned)((n + 15) / 16)), 1024, 0, s>>>(r);
-    HIP_TRY(hipGetLastError());
-    if (!dx && !dw && !dbias) continue;
+    const dim3 grid((unsigned)((p.ldz / 8 + 255) / 256), (unsigned)((round_up(n, TG_BK) + p.range_rows - 1) / p.range_rows));   // zeros behind the last row
+    const bool wanted = dx || dw || dbias;
+    if (!wanted || p.twice || grid.x > 1) {                   // otherwise softmax_grad_kernel ends the rows
+      row_loss_kernel<<<dim3((unsigned)((n + 15) / 16)), 1024, 0, s>>>(r);
+      HIP_TRY(hipGetLastError());
+    }
+    if (!wanted) continue;
     if (p.twice) {
       z.c = p.g; z.lse = p.lse; z.coef = p.coef; z.c_plane = p.piece * p.ldz; z.c_planes = p.planes;
       gemm_launch<END_GRAD>(z, cut, xk.lie, wo.lie, s);
     } else {
-      const SoftmaxGradArgs q = {p.z, p.ldz, p.stats, p.piece, span, p.lse, p.coef, targets + i0, p.g, p.piece * p.ldz,
-                                 dbias ? p.sums + k * p.ranges * v : nullptr, (int32_t)n, (int32_t)v, (int32_t)p.range_rows};
-      const dim3 grid((unsigned)((p.ldz / 8 + 255) / 256), (unsigned)((round_up(n, TG_BK) + p.range_rows - 1) / p.range_rows));   // zeros behind the last row
+      const SoftmaxGradArgs q = {r, p.z, p.ldz, span, p.g, p.piece * p.ldz, dbias ? p.sums + k * p.ranges * v : nullptr, (int32_t)p.range_rows};
       switch (p.planes) {
         case 0: softmax_grad_kernel<0><<<grid, 256, 0, s>>>(q); break;
         case 1: softmax_grad_kernel<1><<<grid, 256, 0, s>>>(q); break;
@@ -616,29 +647,31 @@ int shampoo_checkpoint_weight_grad(const void *packed, size_t packed_bytes, int6
     if (db) TRY(launch_zero(db, 1, out, out, 4, s));
     return SHAMPOO_OK;
   }
-  Operand dyo;
-  TRY(p.dy.operand(dy, p.dyp, LIE_ROWS, dyo, s));
-  PlanesArgs g = {};
-  g.out = p.xp; g.ld = p.ldp; g.cols = in; g.activation = activation;
+  const Operand dyo = p.dy.operand(dy, p.dyp, LIE_ROWS);
+  const bool both = p.dy.copy() && p.pieces == 1;
+  if (p.dy.copy() && !both) TRY(launch_planes(p.dy.task(dy, p.dyp), s));
+  PlanesTask t = {};
+  t.from = FROM_PACKED; t.planes = p.planes;
+  t.g.out = p.xp; t.g.ld = p.ldp; t.g.plane = p.piece * p.ldp; t.g.cols = in; t.g.activation = activation;
   for (int64_t k = 0; k < p.pieces; ++k) {
     const int64_t i0 = k * p.piece, n = std::min(p.piece, rows - i0);
     const Operand xo = {p.xp, p.ldp, p.piece * p.ldp, p.planes, LIE_ROWS, true};
     Operand dk = dyo;
     dk.p += i0 * dyo.ld;
-    g.p = packed_view(packed, rows, in);
-    g.p.codes += i0 * g.p.pitch; g.p.exps += i0 * (g.p.pitch / 32);
-    g.plane = xo.plane;
-    g.rows = n;
-    TRY(launch_planes<FROM_PACKED>(g, p.planes, round_up(n, TG_BK), s));     // zeros behind the last row
+    t.g.p = packed_view(packed, rows, in);
+    t.g.p.codes += i0 * t.g.p.pitch; t.g.p.exps += i0 * (t.g.p.pitch / 32);
+    t.g.rows = n; t.rows = round_up(n, TG_BK);              // zeros behind the last row
+    if (both) TRY(launch_planes(t, p.dy.task(dy, p.dyp), s)); else TRY(launch_planes(t, s));
     const Result r = piece_result(dw, lddw, grad_dtype, p.acc, out_in ? in : out, k == 0, k == p.pieces - 1);
     TRY(out_in ? gemm(dk, xo, out, in, n, r, p.part, s) : gemm(xo, dk, in, out, n, r, p.part, s));
   }
   if (db) {
     const dim3 grid((out + 63) / 64, (unsigned)p.parts);
-    if (dtype == SHAMPOO_GRAD_F32) column_sums_kernel<float><<<grid, 1024, 0, s>>>(static_cast<const float *>(dy), lddy, rows, out, p.part_rows, p.sums);
-    else column_sums_kernel<uint16_t><<<grid, 1024, 0, s>>>(static_cast<const uint16_t *>(dy), lddy, rows, out, p.part_rows, p.sums);
+    float *const sums = p.parts > 1 ? p.sums : db;
+    if (dtype == SHAMPOO_GRAD_F32) column_sums_kernel<float><<<grid, 1024, 0, s>>>(static_cast<const float *>(dy), lddy, rows, out, p.part_rows, sums);
+    else column_sums_kernel<uint16_t><<<grid, 1024, 0, s>>>(static_cast<const uint16_t *>(dy), lddy, rows, out, p.part_rows, sums);
     HIP_TRY(hipGetLastError());
-    TRY(launch_join_rows(p.sums, p.parts, out, db, s));
+    if (p.parts > 1) TRY(launch_join_rows(p.sums, p.parts, out, db, s));
   }
   return SHAMPOO_OK;
 }
