@@ -80,20 +80,25 @@ __device__ __forceinline__ void packed_store8(const Packed &p, int64_t i, int c,
   if ((c & 31) == 0) p.exps[i * (p.pitch >> 5) + (c >> 5)] = (uint8_t)byte;
 }
 
-__device__ __forceinline__ float activate(float z, int kind) {
+// a(z) and a'(z) of eight values.  The choice lies outside the loops: a wavefront fetches the code of one function only.
+template <typename F> __device__ __forceinline__ void each8(f32x8 &z, F &&f) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) z.v[e] = f(z.v[e]);
+}
+__device__ __forceinline__ void activate8(f32x8 &z, int kind) {
   switch (kind) {
-    case ACT_RELU: return z > 0.f ? z : z != z ? z : 0.f;
-    case ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-    case ACT_SILU: return z / (1.f + expf(-z));
-    default: return z;
+    case ACT_RELU: each8(z, [](float x) { return x > 0.f ? x : x != x ? x : 0.f; }); break;
+    case ACT_GELU: each8(z, [](float x) { return 0.5f * x * (1.f + erff(x * 0.70710678118654752f)); }); break;
+    case ACT_SILU: each8(z, [](float x) { return x / (1.f + expf(-x)); }); break;
+    default: break;
   }
 }
-__device__ __forceinline__ float slope(float z, int kind) {
+__device__ __forceinline__ void slope8(f32x8 &z, int kind) {
   switch (kind) {
-    case ACT_RELU: return z > 0.f ? 1.f : z != z ? z : 0.f;
-    case ACT_GELU: return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
-    case ACT_SILU: { const float s = 1.f / (1.f + expf(-z)); return s * (1.f + z * (1.f - s)); }
-    default: return 1.f;
+    case ACT_RELU: each8(z, [](float x) { return x > 0.f ? 1.f : x != x ? x : 0.f; }); break;
+    case ACT_GELU: each8(z, [](float x) { return 0.5f * (1.f + erff(x * 0.70710678118654752f)) + x * expf(-0.5f * x * x) * 0.39894228040143268f; }); break;
+    case ACT_SILU: each8(z, [](float x) { const float s = 1.f / (1.f + expf(-x)); return s * (1.f + x * (1.f - s)); }); break;
+    default: each8(z, [](float) { return 1.f; });
   }
 }
 
@@ -135,11 +140,11 @@ template <typename T, bool GRAD> __global__ __launch_bounds__(256) void checkpoi
   f32x8 x = packed_load8(g.p, row, c);
   if constexpr (GRAD) {
     const f32x8 d = load8(static_cast<const T *>(g.dy) + row * g.lddy, c, g.p.cols);
+    slope8(x, g.activation);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x.v[e] = d.v[e] * slope(x.v[e], g.activation);
-  } else if (g.activation != ACT_NONE) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x.v[e] = activate(x.v[e], g.activation);
+    for (int e = 0; e < 8; ++e) x.v[e] *= d.v[e];
+  } else {
+    activate8(x, g.activation);
   }
   store8(static_cast<T *>(g.y) + row * g.ldy, c, g.p.cols, x);
 }
@@ -162,10 +167,8 @@ template <int FROM, int PLANES> __device__ __forceinline__ void planes_piece(con
   if (row >= g.rows) {
   } else if constexpr (FROM == FROM_PACKED) {
     if (c < g.p.pitch) x = packed_load8(g.p, row, c);
-    if (g.activation != ACT_NONE) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x.v[e] = c + e < g.cols ? activate(x.v[e], g.activation) : 0.f;
-    } else {                                     // a group that is not finite reads NaN in the padding too
+    activate8(x, g.activation);
+    if (c + 8 > g.cols) {                          // a group that is not finite reads NaN in the padding too
 #pragma unroll
       for (int e = 0; e < 8; ++e) if (c + e >= g.cols) x.v[e] = 0.f;
     }

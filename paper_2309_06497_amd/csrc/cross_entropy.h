@@ -20,7 +20,8 @@
 namespace shampoo {
 
 // Logits from the float32 results of several splits of their product, where that has too few tiles to fill the GPU otherwise: what
-// the logits' product leaves (train_gemm.h), in spans of 64 classes.  A thread has eight classes of a row, eight threads a span.
+// the logits' product leaves (train_gemm.h), in spans of 64 classes.  A thread has eight classes of a row and
+// every fourth split.
 struct LogitsJoinArgs {
   const float *part; int64_t stride, pitch; int32_t splits;
   void *z; int64_t ldz; int32_t end, store;
@@ -30,15 +31,20 @@ struct LogitsJoinArgs {
   uint32_t pieces, per_row;          // ldz / 8, a multiple of 8
 };
 __global__ __launch_bounds__(256) void logits_join_kernel(const LogitsJoinArgs g) {
-  const uint32_t at = min(blockIdx.x * 256u + threadIdx.x, g.pieces - 1);       // the last one again: whole spans, whole wavefronts
-  const int i = at / g.per_row, c = (at - i * g.per_row) * 8;
-  f32x8 z = load8(g.part + (int64_t)i * g.pitch, c, (int)g.pitch);
+  // lanes 8 l ... 8 l + 7 of a span's 32: splits l, l + 4, ...
+  const uint32_t piece = (blockIdx.x * 256u + threadIdx.x) / 32 * 8 + (threadIdx.x & 7), at = min(piece, g.pieces - 1);   // the last one again: whole wavefronts
+  const int i = at / g.per_row, c = (at - i * g.per_row) * 8, lane = (threadIdx.x >> 3) & 3;
+  f32x8 z = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
 #pragma unroll 4
-  for (int k = 1; k < g.splits; ++k) {
+  for (int k = lane; k < g.splits; k += 4) {
     const f32x8 x = load8(g.part + k * g.stride + (int64_t)i * g.pitch, c, (int)g.pitch);
 #pragma unroll
     for (int e = 0; e < 8; ++e) z.v[e] += x.v[e];
   }
+#pragma unroll
+  for (int o = 8; o < 32; o <<= 1)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z.v[e] += __shfl_xor(z.v[e], o, 64);
   if (g.bias) {
     const f32x8 b = load8(g.bias, c, g.classes);
 #pragma unroll
@@ -64,7 +70,7 @@ __global__ __launch_bounds__(256) void logits_join_kernel(const LogitsJoinArgs g
   }
 #pragma unroll
   for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor(sum, o, 64);
-  if (blockIdx.x * 256u + threadIdx.x >= g.pieces) return;
+  if (piece >= g.pieces || lane != 0) return;
 #pragma unroll
   for (int e = 0; e < 8; ++e)
     if (t == e && c + e < g.classes) g.target_z[i] = z.v[e];

@@ -518,7 +518,7 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
       HIP_TRY(hipGetLastError());
       LogitsJoinArgs j = {p.part, z.c_split, z.ldc, cut.splits, logits, p.ldz, end, store, bias, targets + i0, p.stats, p.piece, p.target_z,
                           (int32_t)n, (int32_t)v, (uint32_t)(n * (p.ldz / 8)), (uint32_t)(p.ldz / 8)};
-      logits_join_kernel<<<dim3((j.pieces + 255) / 256), 256, 0, s>>>(j);
+      logits_join_kernel<<<dim3((j.pieces + 63) / 64), 256, 0, s>>>(j);
     } else {
       z.c = logits; z.ldc = p.ldz; z.store = store;
       z.bias = bias; z.targets = targets + i0; z.stats = p.stats; z.stats_ld = p.piece; z.target_z = p.target_z;
