@@ -47,6 +47,8 @@ struct TrainGemmArgs {
   int32_t padded;                          // both along rows: 1 where A, 2 where B has the zeros
   uint32_t plane_a, plane_b;               // four bits each: the planes of product i
   int32_t tiles_m, tiles_n, splits, per_split;   // slabs of the whole sequence (products x ceil(K / 64)) per split
+  int32_t tile0, tiles;                    // this launch's: tile0 ... tile0 + tiles - 1
+  int32_t by_tile;                         // c holds this launch's tiles one behind the other, 64 TI x 64 TI each, per split
   void *c; int64_t ldc, c_split;           // c_split: from the result of a split to the next
   const float *add; int64_t ldadd;         // C += add (float32; may be c itself) or nullptr
   int32_t store;
@@ -69,6 +71,13 @@ constexpr float LOGIT_STEPS = 1024.f, LOG2_E = 1.4426950408889634f;
 __device__ __forceinline__ uint32_t logit_pair(float d, float e) {
   constexpr float C = -LOG2_E * LOGIT_STEPS / 65535.f;
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(d * C, e * C));
+}
+
+// Where a tile lies: columns of eight tiles, so that neighbours in number share operands.
+__device__ __forceinline__ void tile_place(int tile, int tiles_m, int tiles_n, int &tm, int &tn) {
+  const int group = tile / (8 * tiles_n), in_group = tile - group * 8 * tiles_n, rows = min(8, tiles_m - 8 * group);
+  tm = 8 * group + in_group % rows;
+  tn = in_group / rows;
 }
 
 // LDS accesses of one wavefront that depend on one another: LDS keeps their order, the compiler must
@@ -143,13 +152,13 @@ __global__ __launch_bounds__(256, TI == 2 && STAGES == 2 ? 2 : 1) void train_gem
   typedef SlabSide<BLIE, TI> SideB;
   constexpr int TILE = 64 * TI, SPAN = 32 * TI, STAGE = SideA::BYTES + SideB::BYTES, PIECES = SideA::PIECES, NMM = TI * TI;
   __shared__ __align__(256) unsigned char smem[STAGES * STAGE];
-  const int tiles = g.tiles_m * g.tiles_n, total = tiles * g.splits;
-  // an XCD (workgroup index modulo 8) has neighbouring tiles, in columns of eight
+  const int total = g.tiles * g.splits;
+  // an XCD (workgroup index modulo 8) has neighbouring tiles
   const int per = (total + 7) / 8, logical = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
   if (logical >= total || (int)(blockIdx.x >> 3) >= per) return;
-  const int split = logical / tiles, tile = logical - split * tiles;
-  const int group = tile / (8 * g.tiles_n), in_group = tile - group * 8 * g.tiles_n, rows_of = min(8, g.tiles_m - 8 * group);
-  const int tm = 8 * group + in_group % rows_of, tn = in_group / rows_of;
+  const int split = logical / g.tiles, tile = g.tile0 + logical - split * g.tiles;
+  int tm, tn;
+  tile_place(tile, g.tiles_m, g.tiles_n, tm, tn);
   const int row0 = tm * TILE, col0 = tn * TILE;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
   const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)smem;
@@ -304,6 +313,7 @@ __global__ __launch_bounds__(256, TI == 2 && STAGES == 2 ? 2 : 1) void train_gem
   auto staged = [&](int r) { return load8(buf + r * PITCH + c, 0, 8); };
 
   if constexpr (END == END_PLAIN) {
+    const int64_t from = split * g.c_split + (g.by_tile ? (int64_t)(tile - g.tile0) * TILE * TILE - (int64_t)row0 * TILE - col0 : 0);
 #pragma unroll
     for (int i = 0; i < TI; ++i) {
       stage(i);
@@ -315,7 +325,7 @@ __global__ __launch_bounds__(256, TI == 2 && STAGES == 2 ? 2 : 1) void train_gem
           for (int e = 0; e < 8; ++e) z.v[e] += old.v[e];
         }
         if (g.store == STORE_BF16) store8(static_cast<uint16_t *>(g.c) + out * g.ldc, col, limit, z);
-        else store8(static_cast<float *>(g.c) + split * g.c_split + out * g.ldc, col, limit, z);
+        else store8(static_cast<float *>(g.c) + from + out * g.ldc, col, limit, z);
       });
     }
   } else {
@@ -452,6 +462,37 @@ template <int LANES> __global__ __launch_bounds__(256) void train_join_kernel(co
   }
   if (g.store == STORE_BF16) store8(static_cast<uint16_t *>(g.c) + row * g.ldc, c, g.cols, s);
   else store8(static_cast<float *>(g.c) + row * g.ldc, c, g.cols, s);
+}
+
+// The tiles of a product's last round, which its splits left one behind the other (by_tile), added up in order.
+struct JoinTilesArgs {
+  const float *part; int64_t stride; int32_t splits;
+  void *c; int64_t ldc; const float *add; int64_t ldadd;
+  int32_t M, N, tiles_m, tiles_n, tile0, tile, store;       // tile: rows of one
+};
+__global__ __launch_bounds__(256) void train_join_tiles_kernel(const JoinTilesArgs g) {
+  const int pieces = g.tile * g.tile / 8, per = pieces / 256;           // workgroups of a tile
+  const int t = blockIdx.x / per, i = (blockIdx.x - t * per) * 256 + threadIdx.x, r = i / (g.tile / 8), c = (i - r * (g.tile / 8)) * 8;
+  int tm, tn;
+  tile_place(g.tile0 + t, g.tiles_m, g.tiles_n, tm, tn);
+  const int64_t row = (int64_t)tm * g.tile + r;
+  const int col = tn * g.tile + c;
+  if (row >= g.M || col >= g.N) return;
+  const float *p = g.part + (int64_t)t * g.tile * g.tile + (int64_t)i * 8;
+  f32x8 s = load8(p, 0, 8);
+#pragma unroll 4
+  for (int k = 1; k < g.splits; ++k) {
+    const f32x8 x = load8(p + k * g.stride, 0, 8);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s.v[e] += x.v[e];
+  }
+  if (g.add) {
+    const f32x8 x = load8(g.add + row * g.ldadd, col, g.N);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s.v[e] += x.v[e];
+  }
+  if (g.store == STORE_BF16) store8(static_cast<uint16_t *>(g.c) + row * g.ldc, col, g.N, s);
+  else store8(static_cast<float *>(g.c) + row * g.ldc, col, g.N, s);
 }
 
 }  // namespace shampoo

@@ -175,12 +175,24 @@ int plane_pairs(int na, int nb, uint32_t &pa, uint32_t &pb) {
 // Against all cuts of 19 shapes between 256 x 256 x 512 and 8192 x 2048 x 8192 the choice is within 15 % of the best.  For example
 // 2000 x 1000 x 50000: 186 (256, 8 splits), 206 (128, 4), 637 (128, 1); 2048 x 2048 x 2048: 21 (128, 1; two stages 29), 41 (128, 2),
 // 47 (256, 1); 256 x 256 x 4096: 11 (128, 16), 26 (128, 1).
-struct GemmCut { int ti, splits, per_split; size_t bytes; int stages; };
+// tail: splits of the last round's tiles, where the others fill the GPU a whole number of times and these leave much of it idle for as long
+// again: 1000 x 50001 x 1999 with three pairs of planes, 784 tiles of 256
+// in four rounds, 665 us; in three and the 16 left over in 16 splits each, 602 with their join.
+struct GemmCut { int ti, splits, per_split; size_t bytes; int stages, tail; };
+constexpr int64_t CUS = 256, BIG_TILE = 256;
 GemmCut gemm_cut(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, int most = 512) {
   uint32_t unused_a, unused_b;
   const int64_t all = (K + TG_BK - 1) / TG_BK * plane_pairs(planes_a, planes_b, unused_a, unused_b);
-  GemmCut best = {2, 1, (int)all, 0, 2};
+  GemmCut best = {2, 1, (int)all, 0, 2, 1};
   double shortest = INFINITY;
+  const int64_t big = ((M + BIG_TILE - 1) / BIG_TILE) * ((N + BIG_TILE - 1) / BIG_TILE), rest = big % CUS;
+  int tail = 1;
+  double saved = 0.0;
+  if (big > CUS && rest > 0 && most > LOGIT_SPLITS) {
+    tail = (int)std::max<int64_t>(1, std::min(CUS / rest, all / 2));
+    saved = 6.0 + 1.7 * (double)all - (8.0 + 1.7 * (double)((all + tail - 1) / tail) + 3.0 + (double)(rest * tail) * 0.13);
+    if (tail < 2 || saved < 5.0) { tail = 1; saved = 0.0; }
+  }
   for (int ti : {2, 4})
     for (int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256, 384, 512}) {
       if (splits > 1 && (splits > all / 2 || splits > most)) break;
@@ -188,16 +200,19 @@ GemmCut gemm_cut(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, in
       const double each = (double)((tiles * splits + 255) / 256);       // workgroups per CU
       double us = ti == 4 ? 5.0 + each * (6.0 + 1.7 * (double)per) : 4.0 + (double)per * (each <= 1.0 ? 0.55 : each <= 2.0 ? 1.0 : 0.58 * each);
       if (splits > 1) us += 3.0 + (double)splits * (double)M * (double)N * 2e-6;
+      const bool with_tail = ti == 4 && splits == 1 && tail > 1;
+      if (with_tail) us -= saved;
       if (us < shortest) {
         shortest = us;
-        best = {ti, (int)((all + per - 1) / per), (int)per, 0, ti == 2 && each <= 1.0 ? 4 : 2};
+        best = {ti, (int)((all + per - 1) / per), (int)per, 0, ti == 2 && each <= 1.0 ? 4 : 2, with_tail ? tail : 1};
       }
     }
   if (best.splits > 1) best.bytes = align_up((size_t)best.splits * M * round_up(N, 8) * sizeof(float));
+  if (best.tail > 1) best.bytes = align_up((size_t)best.tail * rest * BIG_TILE * BIG_TILE * sizeof(float));
   return best;
 }
 template <int TI, int STAGES, int END> void gemm_launch(const TrainGemmArgs &g, int alie, int blie, hipStream_t s) {
-  const int64_t total = (int64_t)g.tiles_m * g.tiles_n * g.splits;
+  const int64_t total = (int64_t)g.tiles * g.splits;
   const dim3 grid((unsigned)((total + 7) / 8 * 8));
   if (alie == LIE_K && blie == LIE_K) train_gemm_kernel<TI, STAGES, LIE_K, LIE_K, END><<<grid, 256, 0, s>>>(g);
   else if (alie == LIE_K) train_gemm_kernel<TI, STAGES, LIE_K, LIE_ROWS, END><<<grid, 256, 0, s>>>(g);
@@ -215,6 +230,7 @@ void gemm_args(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t
   g.products = plane_pairs(a.planes, b.planes, g.plane_a, g.plane_b);
   g.tiles_m = (int32_t)((M + 64 * cut.ti - 1) / (64 * cut.ti)); g.tiles_n = (int32_t)((N + 64 * cut.ti - 1) / (64 * cut.ti));
   g.splits = cut.splits; g.per_split = cut.per_split;
+  g.tiles = g.tiles_m * g.tiles_n;
   g.padded = a.padded ? 1 : b.padded ? 2 : 0;
 }
 // the splits' results one behind the other in `part`
@@ -229,7 +245,18 @@ int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, co
   gemm_args(a, b, M, N, K, cut, g);
   if (cut.splits == 1) {
     g.c = c.c; g.ldc = c.ldc; g.add = c.add; g.ldadd = c.ldadd; g.store = c.store;
+    const int32_t all = g.per_split, rest = cut.tail > 1 ? (int32_t)(g.tiles % CUS) : 0;
+    g.tiles -= rest;
     gemm_launch<END_PLAIN>(g, cut, a.lie, b.lie, s);
+    HIP_TRY(hipGetLastError());
+    if (rest == 0) return SHAMPOO_OK;
+    g.tile0 = g.tiles; g.tiles = rest; g.by_tile = 1;
+    g.per_split = (all + cut.tail - 1) / cut.tail; g.splits = (all + g.per_split - 1) / g.per_split;
+    g.c = part; g.ldc = BIG_TILE; g.c_split = rest * BIG_TILE * BIG_TILE; g.add = nullptr; g.store = STORE_F32;
+    gemm_launch<END_PLAIN>(g, cut, a.lie, b.lie, s);
+    HIP_TRY(hipGetLastError());
+    const JoinTilesArgs j = {part, g.c_split, g.splits, c.c, c.ldc, c.add, c.ldadd, g.M, g.N, g.tiles_m, g.tiles_n, g.tile0, (int32_t)BIG_TILE, c.store};
+    train_join_tiles_kernel<<<dim3((unsigned)(rest * (BIG_TILE * BIG_TILE / 8 / 256))), 256, 0, s>>>(j);
     HIP_TRY(hipGetLastError());
     return SHAMPOO_OK;
   }

@@ -392,6 +392,26 @@ def test_weight_gradient_from_a_checkpoint(n, i, o, how, act, out_in, kinds):
     assert rel(db, dy.double().sum(0)) <= 2.0 ** -18
 
 
+@pytest.mark.parametrize("out_in", [False, True])
+def test_weight_gradient_whose_last_round_of_tiles_is_split(out_in):
+    """4 x 67 tiles of 256: 256 of them, and twelve that are split along the tokens."""
+    torch = torch_()
+    g = gen(21)
+    n, i, o = 2500, 1000, 17000
+    for dt, grad, bar in ((torch.bfloat16, torch.bfloat16, U), (torch.bfloat16, torch.float32, 2.0 ** -18), (torch.float32, torch.float32, 2.0 ** -18)):
+        x, dy = activations(g, n, i).to(dt), normal(g, n, o).to(dt)
+        c = B.shampoo_checkpoint_pack(x)
+        want = held(x).t() @ dy.double()
+        got = B.shampoo_checkpoint_weight_grad(c, dy, grad_dtype=grad, out_in=out_in)
+        got = got.t() if out_in else got
+        assert rel(got, want) <= bar
+        # each tile of the last round by itself, and the one before
+        for k in range(o - 13 * 256, o, 128):
+            assert rel(got[:, k:k + 128], want[:, k:k + 128]) <= 2 * bar
+        for k in range(0, i, 128):
+            assert rel(got[k:k + 128, -3000:], want[k:k + 128, -3000:]) <= 2 * bar
+
+
 def test_weight_gradient_in_several_pieces_of_rows():
     torch = torch_()
     g = gen(3)
