@@ -103,7 +103,8 @@ __device__ __forceinline__ void slope8(f32x8 &z, int kind) {
 }
 
 // Pieces of eight in row order: a thread takes one piece, a grid at most 2^30 of them; row0: the grid's first row.
-// One pass, 16 bytes (8 for codes) per lane: bound by memory.
+// One pass, 16 bytes (8 for codes) per lane: bound by memory.  8192 x 8192 in bf16: packed in 39 us, read back in 33 (203 MB each,
+// 5.2 and 6.2 TB/s, part of it from the cache behind the L2); the GELU gradient of 3001 x 4001 in float32 22 us (108 MB, 4.9 TB/s).
 struct PackArgs {
   const void *x; int64_t ldx;
   Packed p;
@@ -150,7 +151,7 @@ template <typename T, bool GRAD> __global__ __launch_bounds__(256) void checkpoi
 }
 
 // a(x) of a checkpoint, or a matrix in memory (float32 or bf16, any alignment), as PLANES bf16 planes [plane][rows][ld], ld a
-// multiple of 8, zeros from cols to ld and in rows from `rows` on.
+// multiple of 8, zeros from cols to ld and in rows from `rows` on.  Bound by memory: one plane of 8192 x 8192 codes 36 us (5.6 TB/s).
 struct PlanesArgs {
   Packed p; const void *x; int64_t ldx;        // one of the two
   uint16_t *out; int64_t plane, ld;

@@ -12,9 +12,10 @@
 // written once: bound by memory, beside about 35 vector operations per element.  Forward a team is one wavefront up to
 // 2048 features: its sums need no barrier, and other wavefronts hide its latency.  Backward a team has several rows, the next one on its way
 // while one is worked on, and keeps weights and the sums for their gradients in registers, so a thread has one piece
-// (up to 4096 features): 16384 x 2048 in bf16 from checkpoints 90 us, 223 with a wavefront per row and four pieces a thread (477 registers), 141 with the
-// weights read for every row; 768 teams of 256 threads, three per CU, and 111 us with 1024.  The teams' sums are joined in order by a second launch.
-// 16384 x 2048, bf16: forward with checkpoints 68 us (337 MB, 5.0 TB/s), backward 90 + 7 us (337 MB, 3.7 TB/s).
+// (up to 4096 features): 16384 x 2048 in bf16 from checkpoints 84 us, where a wavefront per row with four pieces a thread (477 registers) took 223 and
+// weights read for every row 141; 768 teams of 256 threads, three per CU (with 1024 teams a fifth more).  The teams' sums are joined in order by a second launch.
+// 16384 x 2048, bf16: forward with checkpoints 72 us (337 MB, 4.7 TB/s), backward 84 + 7 us (337 MB, 3.7 TB/s: 57 vector
+// operations per element beside them).  3003 x 1001, float32, layer norms: 14 and 22 + 6 us.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

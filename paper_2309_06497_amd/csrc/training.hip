@@ -176,8 +176,8 @@ int plane_pairs(int na, int nb, uint32_t &pa, uint32_t &pb) {
 // 2000 x 1000 x 50000: 186 (256, 8 splits), 206 (128, 4), 637 (128, 1); 2048 x 2048 x 2048: 21 (128, 1; two stages 29), 41 (128, 2),
 // 47 (256, 1); 256 x 256 x 4096: 11 (128, 16), 26 (128, 1).
 // tail: splits of the last round's tiles, where the others fill the GPU a whole number of times and these leave much of it idle for as long
-// again: 1000 x 50001 x 1999 with three pairs of planes, 784 tiles of 256
-// in four rounds, 665 us; in three and the 16 left over in 16 splits each, 602 with their join.
+// again: 1000 x 50001 x 1999 with three planes a side, 784 tiles of 256 in four rounds, 665 us; in three and the 16 left over in
+// 16 splits each, 602 with their join.
 struct GemmCut { int ti, splits, per_split; size_t bytes; int stages, tail; };
 constexpr int64_t CUS = 256, BIG_TILE = 256;
 GemmCut gemm_cut(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, int most = 512) {
