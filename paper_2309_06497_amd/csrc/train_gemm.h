@@ -150,16 +150,17 @@ template <int LIE, int TI> struct SlabRegs {
   }
 };
 
+// One tile; smem: GEMM_LDS bytes.
+template <int TI, int STAGES> constexpr int GEMM_LDS = STAGES * 64 * TI * TG_BK * 2 * 2;
 template <int TI, int STAGES, int ALIE, int BLIE, int END>
-__global__ __launch_bounds__(256, TI == 2 && STAGES == 2 ? 2 : 1) void train_gemm_kernel(const TrainGemmArgs g) {
+__device__ __forceinline__ void train_gemm_tile(const TrainGemmArgs &g, int block, unsigned char *smem) {
   typedef SlabSide<ALIE, TI> SideA;
   typedef SlabSide<BLIE, TI> SideB;
   constexpr int TILE = 64 * TI, SPAN = 32 * TI, STAGE = SideA::BYTES + SideB::BYTES, PIECES = SideA::PIECES, NMM = TI * TI;
-  __shared__ __align__(256) unsigned char smem[STAGES * STAGE];
   const int total = g.tiles * g.splits;
   // an XCD (workgroup index modulo 8) has neighbouring tiles
-  const int per = (total + 7) / 8, logical = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
-  if (logical >= total || (int)(blockIdx.x >> 3) >= per) return;
+  const int per = (total + 7) / 8, logical = (block & 7) * per + (block >> 3);
+  if (logical >= total || (block >> 3) >= per) return;
   const int split = logical / g.tiles, tile = g.tile0 + logical - split * g.tiles;
   int tm, tn;
   tile_place(tile, g.tiles_m, g.tiles_n, tm, tn);
@@ -431,6 +432,21 @@ __global__ __launch_bounds__(256, TI == 2 && STAGES == 2 ? 2 : 1) void train_gem
       }
     }
   }
+}
+
+template <int TI, int STAGES, int ALIE, int BLIE, int END>
+__global__ __launch_bounds__(256, TI == 2 && STAGES == 2 ? 2 : 1) void train_gemm_kernel(const TrainGemmArgs g) {
+  __shared__ __align__(256) unsigned char smem[GEMM_LDS<TI, STAGES>];
+  train_gemm_tile<TI, STAGES, ALIE, BLIE, END>(g, (int)blockIdx.x, smem);
+}
+
+// Two small products that do not depend on one another, in one launch: the first `blocks` workgroups (a multiple of 8) have g, whose A
+// lies along k, the others h, whose operands both lie along rows.
+template <int BLIE> __global__ __launch_bounds__(256, 1) void train_gemm_pair_kernel(const TrainGemmArgs g, const TrainGemmArgs h, int blocks) {
+  __shared__ __align__(256) unsigned char smem[GEMM_LDS<2, 4>];
+  const int block = (int)blockIdx.x;
+  if (block < blocks) train_gemm_tile<2, 4, LIE_K, BLIE, END_PLAIN>(g, block, smem);
+  else train_gemm_tile<2, 4, LIE_ROWS, LIE_ROWS, END_PLAIN>(h, block - blocks, smem);
 }
 
 // The results of several splits, float32 [split][rows][cols], added up in an order that does not depend on the launch.  LANES

@@ -178,13 +178,15 @@ int plane_pairs(int na, int nb, uint32_t &pa, uint32_t &pb) {
 // tail: splits of the last round's tiles, where the others fill the GPU a whole number of times and these leave much of it idle for as long
 // again: 1000 x 50001 x 1999 with three planes a side, 784 tiles of 256 in four rounds, 665 us; in three and the 16 left over in
 // 16 splits each, 602 with their join.
-struct GemmCut { int ti, splits, per_split; size_t bytes; int stages, tail; };
+struct GemmCut { int ti, splits, per_split; size_t bytes; int stages, tail; double us; };
 constexpr int64_t CUS = 256, BIG_TILE = 256;
+constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256, 384, 512};
+inline double join_us(int64_t M, int64_t N, int splits) { return splits > 1 ? 3.0 + (double)splits * (double)M * (double)N * 2e-6 : 0.0; }
+inline size_t part_bytes(int64_t M, int64_t N, int splits) { return splits > 1 ? align_up((size_t)splits * M * round_up(N, 8) * sizeof(float)) : 0; }
 GemmCut gemm_cut(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, int most = 512) {
   uint32_t unused_a, unused_b;
   const int64_t all = (K + TG_BK - 1) / TG_BK * plane_pairs(planes_a, planes_b, unused_a, unused_b);
-  GemmCut best = {2, 1, (int)all, 0, 2, 1};
-  double shortest = INFINITY;
+  GemmCut best = {2, 1, (int)all, 0, 2, 1, INFINITY};
   const int64_t big = ((M + BIG_TILE - 1) / BIG_TILE) * ((N + BIG_TILE - 1) / BIG_TILE), rest = big % CUS;
   int tail = 1;
   double saved = 0.0;
@@ -194,20 +196,17 @@ GemmCut gemm_cut(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, in
     if (tail < 2 || saved < 5.0) { tail = 1; saved = 0.0; }
   }
   for (int ti : {2, 4})
-    for (int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256, 384, 512}) {
+    for (int splits : SPLITS) {
       if (splits > 1 && (splits > all / 2 || splits > most)) break;
       const int64_t tile = 64 * ti, tiles = ((M + tile - 1) / tile) * ((N + tile - 1) / tile), per = (all + splits - 1) / splits;
       const double each = (double)((tiles * splits + 255) / 256);       // workgroups per CU
       double us = ti == 4 ? 5.0 + each * (6.0 + 1.7 * (double)per) : 4.0 + (double)per * (each <= 1.0 ? 0.55 : each <= 2.0 ? 1.0 : 0.58 * each);
-      if (splits > 1) us += 3.0 + (double)splits * (double)M * (double)N * 2e-6;
+      us += join_us(M, N, splits);
       const bool with_tail = ti == 4 && splits == 1 && tail > 1;
       if (with_tail) us -= saved;
-      if (us < shortest) {
-        shortest = us;
-        best = {ti, (int)((all + per - 1) / per), (int)per, 0, ti == 2 && each <= 1.0 ? 4 : 2, with_tail ? tail : 1};
-      }
+      if (us < best.us) best = {ti, (int)((all + per - 1) / per), (int)per, 0, ti == 2 && each <= 1.0 ? 4 : 2, with_tail ? tail : 1, us};
     }
-  if (best.splits > 1) best.bytes = align_up((size_t)best.splits * M * round_up(N, 8) * sizeof(float));
+  best.bytes = part_bytes(M, N, best.splits);
   if (best.tail > 1) best.bytes = align_up((size_t)best.tail * rest * BIG_TILE * BIG_TILE * sizeof(float));
   return best;
 }
@@ -233,18 +232,28 @@ void gemm_args(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t
   g.tiles = g.tiles_m * g.tiles_n;
   g.padded = a.padded ? 1 : b.padded ? 2 : 0;
 }
-// the splits' results one behind the other in `part`
-void gemm_partial(TrainGemmArgs &g, const GemmCut &cut, int alie, int blie, float *part, hipStream_t s) {
-  g.c = part; g.ldc = round_up(g.N, 8); g.c_split = g.M * g.ldc; g.store = STORE_F32;
-  gemm_launch<END_PLAIN>(g, cut, alie, blie, s);
+// where C goes: with several splits their results lie one behind the other in `part`
+void gemm_result(TrainGemmArgs &g, const Result &c, float *part) {
+  if (g.splits > 1) { g.c = part; g.ldc = round_up(g.N, 8); g.c_split = g.M * g.ldc; g.store = STORE_F32; }
+  else { g.c = c.c; g.ldc = c.ldc; g.add = c.add; g.ldadd = c.ldadd; g.store = c.store; }
+}
+int gemm_join(const TrainGemmArgs &g, const Result &c, hipStream_t s) {
+  JoinArgs j = {};
+  j.part = static_cast<const float *>(g.c); j.stride = g.c_split; j.splits = g.splits; j.c = c.c; j.ldc = c.ldc; j.add = c.add; j.ldadd = c.ldadd;
+  j.cols = g.N; j.pitch = (int32_t)g.ldc; j.store = c.store; j.per_row = (uint32_t)(g.ldc / 8);
+  return by_rows(g.M, j.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
+    j.row0 = r; j.pieces = pieces;
+    if (g.splits >= 16 && pieces < (1u << 24)) train_join_kernel<8><<<dim3((pieces + 31) / 32), 256, 0, s>>>(j);
+    else train_join_kernel<1><<<grid, 256, 0, s>>>(j);
+  });
 }
 // C = A B^T; `part`: scratch of gemm_cut's size
 int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const Result &c, float *part, hipStream_t s) {
   const GemmCut cut = gemm_cut(M, N, K, a.planes, b.planes);
   TrainGemmArgs g;
   gemm_args(a, b, M, N, K, cut, g);
+  gemm_result(g, c, part);
   if (cut.splits == 1) {
-    g.c = c.c; g.ldc = c.ldc; g.add = c.add; g.ldadd = c.ldadd; g.store = c.store;
     const int32_t all = g.per_split, rest = cut.tail > 1 ? (int32_t)(g.tiles % CUS) : 0;
     g.tiles -= rest;
     gemm_launch<END_PLAIN>(g, cut, a.lie, b.lie, s);
@@ -260,16 +269,57 @@ int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, co
     HIP_TRY(hipGetLastError());
     return SHAMPOO_OK;
   }
-  gemm_partial(g, cut, a.lie, b.lie, part, s);
+  gemm_launch<END_PLAIN>(g, cut, a.lie, b.lie, s);
   HIP_TRY(hipGetLastError());
-  JoinArgs j = {};
-  j.part = part; j.stride = g.c_split; j.splits = cut.splits; j.c = c.c; j.ldc = c.ldc; j.add = c.add; j.ldadd = c.ldadd;
-  j.cols = (int32_t)N; j.pitch = (int32_t)g.ldc; j.store = c.store; j.per_row = (uint32_t)(g.ldc / 8);
-  return by_rows(M, j.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
-    j.row0 = r; j.pieces = pieces;
-    if (cut.splits >= 16 && pieces < (1u << 24)) train_join_kernel<8><<<dim3((pieces + 31) / 32), 256, 0, s>>>(j);
-    else train_join_kernel<1><<<grid, 256, 0, s>>>(j);
-  });
+  return gemm_join(g, c, s);
+}
+
+// Two products, the second with both operands along rows: in one launch of tiles of 128, a workgroup per CU at most, where that is
+// shorter by gemm_cut's model and 2 us for a launch.  The gradients of 256 x 2048 x 1000 in float32: 15 + 18 us, together 21.5; of
+// 32 x 256 x 1000 in bf16 5.4 + 6.1, together 6.4.
+struct PairCut { GemmCut first, second; bool together; size_t bytes; };
+struct Product { int64_t M, N, K; int planes_a, planes_b; };
+PairCut pair_cut(const Product &f, const Product &g) {
+  const GemmCut one = gemm_cut(f.M, f.N, f.K, f.planes_a, f.planes_b), two = gemm_cut(g.M, g.N, g.K, g.planes_a, g.planes_b);
+  PairCut best = {one, two, false, std::max(one.bytes, two.bytes)};
+  double shortest = one.us + two.us + 2.0;
+  uint32_t unused_a, unused_b;
+  const auto tiles = [](const Product &p) { return (p.M + 127) / 128 * ((p.N + 127) / 128); };
+  const auto slabs = [&](const Product &p) { return (p.K + TG_BK - 1) / TG_BK * plane_pairs(p.planes_a, p.planes_b, unused_a, unused_b); };
+  const int64_t tiles_f = tiles(f), tiles_g = tiles(g), all_f = slabs(f), all_g = slabs(g);
+  for (int sf : SPLITS) {
+    if (round_up(tiles_f * sf, 8) + tiles_g > CUS || (sf > 1 && sf > all_f / 2)) break;
+    for (int sg : SPLITS) {
+      if (round_up(tiles_f * sf, 8) + round_up(tiles_g * sg, 8) > CUS || (sg > 1 && sg > all_g / 2)) break;
+      const int64_t per_f = (all_f + sf - 1) / sf, per_g = (all_g + sg - 1) / sg;
+      const double us = 4.0 + 0.55 * (double)std::max(per_f, per_g) + join_us(f.M, f.N, sf) + join_us(g.M, g.N, sg);
+      if (us < shortest) {
+        shortest = us;
+        best.first = {2, (int)((all_f + per_f - 1) / per_f), (int)per_f, 0, 4, 1, us};
+        best.second = {2, (int)((all_g + per_g - 1) / per_g), (int)per_g, 0, 4, 1, us};
+        best.first.bytes = part_bytes(f.M, f.N, best.first.splits); best.second.bytes = part_bytes(g.M, g.N, best.second.splits);
+        best.together = true; best.bytes = best.first.bytes + best.second.bytes;
+      }
+    }
+  }
+  return best;
+}
+// C = A B^T and E = D F^T in one launch, cut by pair_cut
+int gemm_pair(const Operand &a, const Operand &b, const Product &f, const Result &c, const Operand &d, const Operand &e, const Product &g,
+              const Result &r, const PairCut &cut, float *part, hipStream_t s) {
+  TrainGemmArgs x, y;
+  gemm_args(a, b, f.M, f.N, f.K, cut.first, x);
+  gemm_args(d, e, g.M, g.N, g.K, cut.second, y);
+  gemm_result(x, c, part);
+  gemm_result(y, r, part + cut.first.bytes / sizeof(float));
+  const int blocks = (int)round_up(x.tiles * x.splits, 8);
+  const dim3 grid((unsigned)(blocks + round_up(y.tiles * y.splits, 8)));
+  if (b.lie == LIE_K) train_gemm_pair_kernel<LIE_K><<<grid, 256, 0, s>>>(x, y, blocks);
+  else train_gemm_pair_kernel<LIE_ROWS><<<grid, 256, 0, s>>>(x, y, blocks);
+  HIP_TRY(hipGetLastError());
+  if (x.splits > 1) TRY(gemm_join(x, c, s));
+  if (y.splits > 1) TRY(gemm_join(y, r, s));
+  return SHAMPOO_OK;
 }
 
 // A matrix of the caller as an operand: as it lies, or as planes in scratch (float32; rows that the products cannot read to their
@@ -306,6 +356,12 @@ struct CrossEntropyPlan {
   float *z, *lse, *coef, *target_z, *acc, *sums, *part;
   float2 *stats;
   int grad_planes() const { return std::max(planes, 1); }
+  // the gradients' products over n rows
+  Product for_dx(const shampoo_cross_entropy &c, int64_t n) const { return {n, c.features, c.classes, x.planes(), w.planes()}; }
+  Product for_dw(const shampoo_cross_entropy &c, int64_t n) const {
+    if (c.w_layout == SHAMPOO_OUT_IN) return {c.classes, c.features, n, grad_planes(), x.planes()};
+    return {c.features, c.classes, n, x.planes(), grad_planes()};
+  }
 };
 int cross_entropy_plan(const shampoo_cross_entropy &c, void *workspace, CrossEntropyPlan &p) {
   if (c.rows < 0 || c.features < 1 || c.classes < 1) return SHAMPOO_ERR_SHAPE;
@@ -350,8 +406,9 @@ int cross_entropy_plan(const shampoo_cross_entropy &c, void *workspace, CrossEnt
     if (n < 1 || n > p.piece) continue;
     part = std::max(part, gemm_cut(n, v, d, p.x.planes(), p.w.planes(), p.twice ? 1 : LOGIT_SPLITS).bytes);
     if (!c.gradients) continue;
-    part = std::max(part, gemm_cut(n, d, v, c.dtype == SHAMPOO_GRAD_F32 ? 3 : 1, p.w.planes()).bytes);
-    part = std::max(part, out_in ? gemm_cut(v, d, n, p.grad_planes(), p.x.planes()).bytes : gemm_cut(d, v, n, p.x.planes(), p.grad_planes()).bytes);
+    const Product fx = p.for_dx(c, n), fw = p.for_dw(c, n);
+    for (const Product &f : {fx, fw}) part = std::max(part, gemm_cut(f.M, f.N, f.K, f.planes_a, f.planes_b).bytes);
+    part = std::max(part, pair_cut(fx, fw).bytes);
   }
   if (part) p.part = a.take<float>(part / sizeof(float));
   p.bytes = a.used;
@@ -541,7 +598,8 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
     TrainGemmArgs z;
     gemm_args(xk, wo, n, v, d, cut, z);
     if (cut.splits > 1) {
-      gemm_partial(z, cut, xk.lie, wo.lie, p.part, s);
+      gemm_result(z, {}, p.part);
+      gemm_launch<END_PLAIN>(z, cut, xk.lie, wo.lie, s);
       HIP_TRY(hipGetLastError());
       LogitsJoinArgs j = {p.part, z.c_split, z.ldc, cut.splits, logits, p.ldz, end, store, bias, targets + i0, p.stats, p.piece, p.target_z,
                           (int32_t)n, (int32_t)v, (uint32_t)(n * (p.ldz / 8)), (uint32_t)(p.ldz / 8)};
@@ -573,18 +631,22 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
       }
     }
     HIP_TRY(hipGetLastError());
-    if (dx) {
-      const Operand go = {p.g, p.ldz, p.piece * p.ldz, c->dtype == SHAMPOO_GRAD_F32 ? 3 : 1, LIE_K};
-      Operand wt = wo;
-      wt.lie = out_in ? LIE_ROWS : LIE_K;
-      TRY(gemm(go, wt, n, d, v, {static_cast<char *>(dx) + i0 * c->lddx * size_of(c->dtype), c->lddx, c->dtype == SHAMPOO_GRAD_F32 ? STORE_F32 : STORE_BF16, nullptr, 0}, p.part, s));
+    // dx = g w, dw = g^T x (or its transpose)
+    const Operand go = {p.g, p.ldz, p.piece * p.ldz, p.x.planes(), LIE_K}, gt = {p.g, p.ldz, p.piece * p.ldz, p.grad_planes(), LIE_ROWS, true};
+    Operand wt = wo;
+    wt.lie = out_in ? LIE_ROWS : LIE_K;
+    xk.lie = LIE_ROWS;
+    const Operand &left = out_in ? gt : xk, &right = out_in ? xk : gt;
+    const Product fx = p.for_dx(*c, n), fw = p.for_dw(*c, n);
+    const Result to_dx = {!dx ? nullptr : static_cast<char *>(dx) + i0 * c->lddx * size_of(c->dtype), c->lddx, c->dtype == SHAMPOO_GRAD_F32 ? STORE_F32 : STORE_BF16, nullptr, 0};
+    const Result to_dw = piece_result(dw, c->lddw, c->grad_dtype, p.acc, p.w.cols, k == 0, k == p.pieces - 1);
+    const PairCut pair = dx && dw ? pair_cut(fx, fw) : PairCut();
+    if (pair.together) {
+      TRY(gemm_pair(go, wt, fx, to_dx, left, right, fw, to_dw, pair, p.part, s));
+      continue;
     }
-    if (dw) {
-      const Operand gt = {p.g, p.ldz, p.piece * p.ldz, p.grad_planes(), LIE_ROWS, true};
-      xk.lie = LIE_ROWS;
-      const Result out = piece_result(dw, c->lddw, c->grad_dtype, p.acc, p.w.cols, k == 0, k == p.pieces - 1);
-      TRY(out_in ? gemm(gt, xk, v, d, n, out, p.part, s) : gemm(xk, gt, d, v, n, out, p.part, s));
-    }
+    if (dx) TRY(gemm(go, wt, n, d, v, to_dx, p.part, s));
+    if (dw) TRY(gemm(left, right, fw.M, fw.N, fw.K, to_dw, p.part, s));
   }
   if (dbias) {
     const int64_t last = c->rows - (p.pieces - 1) * p.piece, parts = (p.pieces - 1) * p.ranges + (round_up(last, TG_BK) + p.range_rows - 1) / p.range_rows;
