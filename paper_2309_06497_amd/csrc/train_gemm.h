@@ -279,6 +279,19 @@ __device__ __forceinline__ void train_gemm_tile(const TrainGemmArgs &g, int bloc
     step(std::integral_constant<int, 3>(), st, next, st);
     st = next;
   }
+  // the rows' targets in this span (-1: elsewhere), all asked for at once
+  [[maybe_unused]] const int colw = col0 + wn * SPAN, roww = row0 + wm * SPAN;
+  [[maybe_unused]] int target_at[TI];
+  [[maybe_unused]] float row_lse[TI], row_coef[TI];
+  if constexpr (END != END_PLAIN) {
+#pragma unroll
+    for (int i = 0; i < TI; ++i) {
+      const int row = min(roww + 32 * i + (lane & 31), g.M - 1);
+      const int64_t t = g.targets[row] - colw;
+      target_at[i] = t >= 0 && t < SPAN && colw + t < g.N ? (int)t : -1;
+      if constexpr (END == END_GRAD) { row_lse[i] = g.lse[row]; row_coef[i] = g.coef[row]; }
+    }
+  }
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   ra[0].arrived(); rb[0].arrived();
   LDS_DMA_WAIT_VM(0);
@@ -289,7 +302,7 @@ __device__ __forceinline__ void train_gemm_tile(const TrainGemmArgs &g, int bloc
   constexpr int PITCH = SPAN + 4, PITCH16 = SPAN + 8;      // floats, 16-bit logits: rows are 16-byte aligned and four banks apart
   static_assert(4 * 32 * PITCH * 4 + 4 * SPAN * 4 <= STAGES * STAGE, "LDS");
   float *buf = reinterpret_cast<float *>(smem) + wave * 32 * PITCH;
-  const int half = lane >> 5, colw = col0 + wn * SPAN, roww = row0 + wm * SPAN;
+  const int half = lane >> 5;
   [[maybe_unused]] float *bias = reinterpret_cast<float *>(smem) + 4 * 32 * PITCH + wave * SPAN;
   if constexpr (END == END_LOGITS || END == END_GRAD) {
     for (int j = lane; j < SPAN; j += 64) bias[j] = colw + j >= g.N ? -INFINITY : g.bias ? g.bias[colw + j] : 0.f;   // no class there: probability 0
@@ -338,7 +351,6 @@ __device__ __forceinline__ void train_gemm_tile(const TrainGemmArgs &g, int bloc
 #pragma unroll
     for (int i = 0; i < TI; ++i) {
       const int row = roww + 32 * i + (lane & 31);
-      const int64_t target = row < g.M ? g.targets[row] - colw : -1;
       if constexpr (END == END_LOGITS || END == END_GRAD) {
 #pragma unroll
         for (int j = 0; j < TI; ++j)
@@ -349,8 +361,8 @@ __device__ __forceinline__ void train_gemm_tile(const TrainGemmArgs &g, int bloc
           }
       }
       if constexpr (END == END_GRAD) {
-        const float lse = row < g.M ? g.lse[row] : 0.f, k = row < g.M && lse != -INFINITY ? g.coef[row] : 0.f;
-        const int at = target >= 0 && target < SPAN ? (int)target - 4 * half : -1;
+        const float lse = row_lse[i], k = row < g.M && lse != -INFINITY ? row_coef[i] : 0.f;
+        const int at = target_at[i] - 4 * half;
 #pragma unroll
         for (int j = 0; j < TI; ++j)
 #pragma unroll
@@ -387,14 +399,15 @@ __device__ __forceinline__ void train_gemm_tile(const TrainGemmArgs &g, int bloc
             for (int v = 0; v < 16; v += 2) largest = fmaxf(largest, fmaxf(z(j, v), z(j, v + 1)));
           largest = fmaxf(largest, __shfl_xor(largest, 32, 64));
           const float base = largest == -INFINITY ? 0.f : largest;
-          const bool here = target >= 0 && target < SPAN && colw + target < g.N;
+          const int target = target_at[i];
+          const bool here = target >= 0 && row < g.M;
           if (__any(here)) {
             float zt = 0.f;
 #pragma unroll
             for (int j = 0; j < TI; ++j)
 #pragma unroll
-              for (int v = 0; v < 16; ++v) zt = (int)target == 32 * j + 8 * (v >> 2) + 4 * half + (v & 3) ? acc[i][j][v] : zt;
-            if (here && (((int)target >> 2) & 1) == half) g.target_z[row] = zt;
+              for (int v = 0; v < 16; ++v) zt = target == 32 * j + 8 * (v >> 2) + 4 * half + (v & 3) ? acc[i][j][v] : zt;
+            if (here && ((target >> 2) & 1) == half) g.target_z[row] = zt;
           }
           // exp of the distance from the largest, and that in 16 bits, one conversion for two
           float sum = 0.f;
