@@ -464,13 +464,38 @@ template <int BLIE> __global__ __launch_bounds__(256, 1) void train_gemm_pair_ke
 
 // The results of several splits, float32 [split][rows][cols], added up in an order that does not depend on the launch.  LANES
 // threads share a piece of eight columns where there are many splits, so that their loads are on their way together.
+// Workgroups from `blocks` on add up the rows of `sums` (16 columns each, 16 threads a column), which saves a launch of their own.
+struct RowSums { const float *in; float *out; int32_t parts, cols; };      // [parts][cols]
 struct JoinArgs {
   const float *part; int64_t stride; int32_t splits;
   void *c; int64_t ldc; const float *add; int64_t ldadd;
   int64_t row0; uint32_t pieces, per_row;
   int32_t cols, pitch, store;
+  uint32_t blocks; RowSums sums;
 };
+__device__ __forceinline__ void row_sums(const RowSums &g, int block) {
+  __shared__ float part[16][16];
+  const int c = threadIdx.x & 15, k = threadIdx.x >> 4, j = block * 16 + c;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (j < g.cols) {
+    const float *p = g.in + j;
+    int i = k;
+    for (; i + 48 < g.parts; i += 64) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) s[q] += p[(int64_t)(i + 16 * q) * g.cols];
+    }
+    for (; i < g.parts; i += 16) s[0] += p[(int64_t)i * g.cols];
+  }
+  part[k][c] = (s[0] + s[1]) + (s[2] + s[3]);
+  __syncthreads();
+  if (k != 0 || j >= g.cols) return;
+  float t = 0.f;
+#pragma unroll
+  for (int q = 0; q < 16; ++q) t += part[q][c];
+  g.out[j] = t;
+}
 template <int LANES> __global__ __launch_bounds__(256) void train_join_kernel(const JoinArgs g) {
+  if (blockIdx.x >= g.blocks) { row_sums(g.sums, blockIdx.x - g.blocks); return; }
   const uint32_t at = blockIdx.x * (256u / LANES) + threadIdx.x / LANES, i = min(at, g.pieces - 1);
   const int lane = threadIdx.x % LANES;
   const uint32_t r = i / g.per_row;

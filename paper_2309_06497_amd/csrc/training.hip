@@ -127,11 +127,11 @@ int launch_join_sums(JoinSumsArgs g, int count, int64_t outputs, hipStream_t s) 
   }
   return SHAMPOO_OK;
 }
-// out[j] = sum of `parts` rows of in
-int launch_join_rows(const float *in, int64_t parts, int32_t cols, float *out, hipStream_t s) {
+// nothing where `out` is null: a join before it has done it
+int launch_row_sums(const RowSums &r, hipStream_t s) {
   JoinSumsArgs g = {};
-  g.in[0] = in; g.out[0] = out; g.parts[0] = (int32_t)parts; g.part_stride = cols; g.cols = cols;
-  return launch_join_sums(g, 1, 1, s);
+  g.in[0] = r.in; g.out[0] = r.out; g.parts[0] = r.parts; g.part_stride = r.cols; g.cols = r.cols;
+  return launch_join_sums(g, r.out ? 1 : 0, 1, s);
 }
 
 __global__ __launch_bounds__(256) void zero_rows_kernel(unsigned char *p, int64_t row_bytes, int64_t ld_bytes) {
@@ -237,18 +237,23 @@ void gemm_result(TrainGemmArgs &g, const Result &c, float *part) {
   if (g.splits > 1) { g.c = part; g.ldc = round_up(g.N, 8); g.c_split = g.M * g.ldc; g.store = STORE_F32; }
   else { g.c = c.c; g.ldc = c.ldc; g.add = c.add; g.ldadd = c.ldadd; g.store = c.store; }
 }
-int gemm_join(const TrainGemmArgs &g, const Result &c, hipStream_t s) {
+// sums: go along, and are struck out there
+int gemm_join(const TrainGemmArgs &g, const Result &c, RowSums &sums, hipStream_t s) {
   JoinArgs j = {};
   j.part = static_cast<const float *>(g.c); j.stride = g.c_split; j.splits = g.splits; j.c = c.c; j.ldc = c.ldc; j.add = c.add; j.ldadd = c.ldadd;
   j.cols = g.N; j.pitch = (int32_t)g.ldc; j.store = c.store; j.per_row = (uint32_t)(g.ldc / 8);
   return by_rows(g.M, j.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
     j.row0 = r; j.pieces = pieces;
-    if (g.splits >= 16 && pieces < (1u << 24)) train_join_kernel<8><<<dim3((pieces + 31) / 32), 256, 0, s>>>(j);
-    else train_join_kernel<1><<<grid, 256, 0, s>>>(j);
+    const bool eight = g.splits >= 16 && pieces < (1u << 24);
+    j.blocks = eight ? (pieces + 31) / 32 : grid.x;
+    j.sums = sums;
+    sums.out = nullptr;
+    const dim3 all(j.blocks + (j.sums.out ? (j.sums.cols + 15) / 16 : 0));
+    if (eight) train_join_kernel<8><<<all, 256, 0, s>>>(j); else train_join_kernel<1><<<all, 256, 0, s>>>(j);
   });
 }
 // C = A B^T; `part`: scratch of gemm_cut's size
-int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const Result &c, float *part, hipStream_t s) {
+int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const Result &c, float *part, RowSums &sums, hipStream_t s) {
   const GemmCut cut = gemm_cut(M, N, K, a.planes, b.planes);
   TrainGemmArgs g;
   gemm_args(a, b, M, N, K, cut, g);
@@ -271,7 +276,7 @@ int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, co
   }
   gemm_launch<END_PLAIN>(g, cut, a.lie, b.lie, s);
   HIP_TRY(hipGetLastError());
-  return gemm_join(g, c, s);
+  return gemm_join(g, c, sums, s);
 }
 
 // Two products, the second with both operands along rows: in one launch of tiles of 128, a workgroup per CU at most, where that is
@@ -306,7 +311,7 @@ PairCut pair_cut(const Product &f, const Product &g) {
 }
 // C = A B^T and E = D F^T in one launch, cut by pair_cut
 int gemm_pair(const Operand &a, const Operand &b, const Product &f, const Result &c, const Operand &d, const Operand &e, const Product &g,
-              const Result &r, const PairCut &cut, float *part, hipStream_t s) {
+              const Result &r, const PairCut &cut, float *part, RowSums &sums, hipStream_t s) {
   TrainGemmArgs x, y;
   gemm_args(a, b, f.M, f.N, f.K, cut.first, x);
   gemm_args(d, e, g.M, g.N, g.K, cut.second, y);
@@ -317,8 +322,8 @@ int gemm_pair(const Operand &a, const Operand &b, const Product &f, const Result
   if (b.lie == LIE_K) train_gemm_pair_kernel<LIE_K><<<grid, 256, 0, s>>>(x, y, blocks);
   else train_gemm_pair_kernel<LIE_ROWS><<<grid, 256, 0, s>>>(x, y, blocks);
   HIP_TRY(hipGetLastError());
-  if (x.splits > 1) TRY(gemm_join(x, c, s));
-  if (y.splits > 1) TRY(gemm_join(y, r, s));
+  if (x.splits > 1) TRY(gemm_join(x, c, sums, s));
+  if (y.splits > 1) TRY(gemm_join(y, r, sums, s));
   return SHAMPOO_OK;
 }
 
@@ -587,8 +592,11 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
   if (p.x.copy() && p.w.copy()) TRY(launch_planes(p.x.task(x, p.xp), p.w.task(w, p.wp), s));
   else if (p.x.copy()) TRY(launch_planes(p.x.task(x, p.xp), s));
   else if (p.w.copy()) TRY(launch_planes(p.w.task(w, p.wp), s));
+  const int64_t last = c->rows - (p.pieces - 1) * p.piece;
+  RowSums bias_sums = {dbias ? p.sums : nullptr, dbias, (int32_t)((p.pieces - 1) * p.ranges + (round_up(last, TG_BK) + p.range_rows - 1) / p.range_rows), (int32_t)v}, none = {};
   for (int64_t k = 0; k < p.pieces; ++k) {
     const int64_t i0 = k * p.piece, n = std::min(p.piece, c->rows - i0);
+    RowSums &sums = k == p.pieces - 1 ? bias_sums : none;      // once all pieces have left theirs
     Operand xk = xo;
     xk.p += i0 * xo.ld;
     const GemmCut cut = gemm_cut(n, v, d, xk.planes, wo.planes, p.twice ? 1 : LOGIT_SPLITS);
@@ -642,17 +650,13 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
     const Result to_dw = piece_result(dw, c->lddw, c->grad_dtype, p.acc, p.w.cols, k == 0, k == p.pieces - 1);
     const PairCut pair = dx && dw ? pair_cut(fx, fw) : PairCut();
     if (pair.together) {
-      TRY(gemm_pair(go, wt, fx, to_dx, left, right, fw, to_dw, pair, p.part, s));
+      TRY(gemm_pair(go, wt, fx, to_dx, left, right, fw, to_dw, pair, p.part, sums, s));
       continue;
     }
-    if (dx) TRY(gemm(go, wt, n, d, v, to_dx, p.part, s));
-    if (dw) TRY(gemm(left, right, fw.M, fw.N, fw.K, to_dw, p.part, s));
+    if (dx) TRY(gemm(go, wt, n, d, v, to_dx, p.part, sums, s));
+    if (dw) TRY(gemm(left, right, fw.M, fw.N, fw.K, to_dw, p.part, sums, s));
   }
-  if (dbias) {
-    const int64_t last = c->rows - (p.pieces - 1) * p.piece, parts = (p.pieces - 1) * p.ranges + (round_up(last, TG_BK) + p.range_rows - 1) / p.range_rows;
-    TRY(launch_join_rows(p.sums, parts, (int32_t)v, dbias, s));
-  }
-  return SHAMPOO_OK;
+  return launch_row_sums(bias_sums, s);
 }
 
 size_t shampoo_checkpoint_bytes(int64_t rows, int32_t cols) {
@@ -736,6 +740,15 @@ int shampoo_checkpoint_weight_grad(const void *packed, size_t packed_bytes, int6
     if (db) TRY(launch_zero(db, 1, out, out, 4, s));
     return SHAMPOO_OK;
   }
+  RowSums sums = {};
+  if (db && p.parts > 1) sums = {p.sums, db, (int32_t)p.parts, out};
+  if (db) {
+    const dim3 grid((out + 63) / 64, (unsigned)p.parts);
+    float *const to = p.parts > 1 ? p.sums : db;
+    if (dtype == SHAMPOO_GRAD_F32) column_sums_kernel<float><<<grid, 1024, 0, s>>>(static_cast<const float *>(dy), lddy, rows, out, p.part_rows, to);
+    else column_sums_kernel<uint16_t><<<grid, 1024, 0, s>>>(static_cast<const uint16_t *>(dy), lddy, rows, out, p.part_rows, to);
+    HIP_TRY(hipGetLastError());
+  }
   const Operand dyo = p.dy.operand(dy, p.dyp, LIE_ROWS);
   const bool both = p.dy.copy() && p.pieces == 1;
   if (p.dy.copy() && !both) TRY(launch_planes(p.dy.task(dy, p.dyp), s));
@@ -752,17 +765,9 @@ int shampoo_checkpoint_weight_grad(const void *packed, size_t packed_bytes, int6
     t.g.rows = n; t.rows = round_up(n, TG_BK);              // zeros behind the last row
     if (both) TRY(launch_planes(t, p.dy.task(dy, p.dyp), s)); else TRY(launch_planes(t, s));
     const Result r = piece_result(dw, lddw, grad_dtype, p.acc, out_in ? in : out, k == 0, k == p.pieces - 1);
-    TRY(out_in ? gemm(dk, xo, out, in, n, r, p.part, s) : gemm(xo, dk, in, out, n, r, p.part, s));
+    TRY(out_in ? gemm(dk, xo, out, in, n, r, p.part, sums, s) : gemm(xo, dk, in, out, n, r, p.part, sums, s));
   }
-  if (db) {
-    const dim3 grid((out + 63) / 64, (unsigned)p.parts);
-    float *const sums = p.parts > 1 ? p.sums : db;
-    if (dtype == SHAMPOO_GRAD_F32) column_sums_kernel<float><<<grid, 1024, 0, s>>>(static_cast<const float *>(dy), lddy, rows, out, p.part_rows, sums);
-    else column_sums_kernel<uint16_t><<<grid, 1024, 0, s>>>(static_cast<const uint16_t *>(dy), lddy, rows, out, p.part_rows, sums);
-    HIP_TRY(hipGetLastError());
-    if (p.parts > 1) TRY(launch_join_rows(p.sums, p.parts, out, db, s));
-  }
-  return SHAMPOO_OK;
+  return launch_row_sums(sums, s);
 }
 
 int shampoo_residual_norm_forward(const shampoo_residual_norm *c, const void *r, int64_t ldr, const void *f, int64_t ldf, void *r_out,
