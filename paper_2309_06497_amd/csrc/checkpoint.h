@@ -189,37 +189,46 @@ template <int FROM, int PLANES> __device__ __forceinline__ void planes_piece(con
     *reinterpret_cast<uint4 *>(g.out + t * g.plane + row * g.ld + c) = w;
   }
 }
-template <int FROM, int PLANES> __global__ __launch_bounds__(256) void planes_kernel(const PlanesArgs g) { planes_piece<FROM, PLANES>(g, blockIdx.x * 256u + threadIdx.x); }
-// Both operands of a product in one launch: the first `blocks` workgroups have g, the others h.
-template <int FROM_G, int PLANES_G, int FROM_H, int PLANES_H>
-__global__ __launch_bounds__(256) void planes_pair_kernel(const PlanesArgs g, const PlanesArgs h, uint32_t blocks) {
-  if (blockIdx.x < blocks) planes_piece<FROM_G, PLANES_G>(g, blockIdx.x * 256u + threadIdx.x);
-  else planes_piece<FROM_H, PLANES_H>(h, (blockIdx.x - blocks) * 256u + threadIdx.x);
+// Column sums of x (float32 or bf16) by parts of its rows, in an order that does not depend on the launch: 64 columns of one part a
+// workgroup, four threads a column.  They go along with the planes of a product's operands: a launch of their own took 4 us.
+struct ColumnSumsArgs { const void *x; int64_t ldx, rows, per_part; float *out; int32_t cols, bf16; };      // out: [parts][cols]
+__device__ __forceinline__ void column_sums(const ColumnSumsArgs &g, uint32_t block) {
+  __shared__ float part[4][64];
+  const uint32_t across = (uint32_t)(g.cols + 63) / 64, p = block / across;
+  const int c = threadIdx.x & 63, k = threadIdx.x >> 6, j = (int)(block - p * across) * 64 + c;
+  const int64_t i0 = p * g.per_part, i1 = min(g.rows, i0 + g.per_part);
+  auto rows = [&](auto value) {
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    int64_t i = i0 + k;
+    for (; i + 28 < i1; i += 32) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) s[q] += value(i + 4 * q);
+    }
+    for (; i < i1; i += 4) s[0] += value(i);
+    return ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+  };
+  float s = 0.f;
+  if (j < g.cols) {
+    if (g.bf16) s = rows([&](int64_t i) { return bf16_value(static_cast<const uint16_t *>(g.x)[i * g.ldx + j]); });
+    else s = rows([&](int64_t i) { return static_cast<const float *>(g.x)[i * g.ldx + j]; });
+  }
+  part[k][c] = s;
+  __syncthreads();
+  if (k == 0 && j < g.cols) g.out[(int64_t)p * g.cols + j] = (part[0][c] + part[1][c]) + (part[2][c] + part[3][c]);
 }
 
-// Column sums of x, in an order that does not depend on the launch: workgroup (j / 64, part) sums its rows, 16 threads a column, and
-// join_sums_kernel the parts.
-template <typename T> __global__ __launch_bounds__(1024) void column_sums_kernel(const T *x, int64_t ldx, int64_t rows, int32_t cols, int64_t per_part, float *out) {
-  __shared__ float part[16][64];
-  const int c = threadIdx.x & 63, k = threadIdx.x >> 6, j = blockIdx.x * 64 + c;
-  const int64_t i1 = min(rows, (int64_t)(blockIdx.y + 1) * per_part);
-  auto value = [&](int64_t i) { if constexpr (sizeof(T) == 4) return x[i * ldx + j]; else return bf16_value(x[i * ldx + j]); };
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
-  if (j < cols) {
-    int64_t i = blockIdx.y * per_part + k;
-    for (; i + 48 < i1; i += 64) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) s[q] += value(i + 16 * q);
-    }
-    for (; i < i1; i += 16) s[0] += value(i);
-  }
-  part[k][c] = (s[0] + s[1]) + (s[2] + s[3]);
-  __syncthreads();
-  if (k != 0 || j >= cols) return;
-  float t = 0.f;
-#pragma unroll
-  for (int q = 0; q < 16; ++q) t += part[q][c];
-  out[(int64_t)blockIdx.y * cols + j] = t;
+// SUMS: workgroups from `blocks` on have column sums.
+template <int FROM, int PLANES, bool SUMS>
+__global__ __launch_bounds__(256) void planes_kernel(const PlanesArgs g, uint32_t blocks, const ColumnSumsArgs sums) {
+  if (SUMS && blockIdx.x >= blocks) column_sums(sums, blockIdx.x - blocks);
+  else planes_piece<FROM, PLANES>(g, blockIdx.x * 256u + threadIdx.x);
+}
+// Both operands of a product in one launch: the first `blocks` workgroups have g, those up to `sums_from` h.
+template <int FROM_G, int PLANES_G, int FROM_H, int PLANES_H>
+__global__ __launch_bounds__(256) void planes_pair_kernel(const PlanesArgs g, const PlanesArgs h, uint32_t blocks, uint32_t sums_from, const ColumnSumsArgs sums) {
+  if (blockIdx.x < blocks) planes_piece<FROM_G, PLANES_G>(g, blockIdx.x * 256u + threadIdx.x);
+  else if (blockIdx.x < sums_from) planes_piece<FROM_H, PLANES_H>(h, (blockIdx.x - blocks) * 256u + threadIdx.x);
+  else column_sums(sums, blockIdx.x - sums_from);
 }
 
 }  // namespace shampoo

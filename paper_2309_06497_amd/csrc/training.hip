@@ -91,27 +91,41 @@ template <typename F> void planes_variant(const PlanesTask &t, F &&f) {
   else if (t.planes == 1) f(std::integral_constant<int, FROM_PACKED>(), std::integral_constant<int, 1>());
   else f(std::integral_constant<int, FROM_PACKED>(), std::integral_constant<int, 3>());
 }
-int launch_planes(PlanesTask t, hipStream_t s) {
+struct ColumnSums {                    // none: parts = 0
+  ColumnSumsArgs g; int64_t parts;
+  uint32_t blocks() const { return (uint32_t)(parts * ((g.cols + 63) / 64)); }
+};
+// sums: go along with the first launch
+int launch_planes(PlanesTask t, hipStream_t s, ColumnSums sums = {}) {
   t.g.per_row = (uint32_t)(t.g.ld / 8);
   return by_rows(t.rows, t.g.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
     t.g.row0 = r; t.g.pieces = pieces;
-    planes_variant(t, [&](auto from, auto planes) { planes_kernel<decltype(from)::value, decltype(planes)::value><<<grid, 256, 0, s>>>(t.g); });
+    const uint32_t more = sums.blocks();
+    sums.parts = 0;
+    planes_variant(t, [&](auto from, auto planes) {
+      constexpr int FROM = decltype(from)::value, PLANES = decltype(planes)::value;
+      if constexpr (FROM == FROM_PACKED) {
+        if (more) { planes_kernel<FROM, PLANES, true><<<dim3(grid.x + more), 256, 0, s>>>(t.g, grid.x, sums.g); return; }
+      }
+      planes_kernel<FROM, PLANES, false><<<grid, 256, 0, s>>>(t.g, grid.x, {});
+    });
   });
 }
 // Two of them, in one launch where both are small: up to 2^22 pieces of eight together a launch's latency counts.  g of FROM_F32 with h of the same,
 // FROM_BF16 likewise, or g of FROM_PACKED with either.
-int launch_planes(PlanesTask g, PlanesTask h, hipStream_t s) {
+int launch_planes(PlanesTask g, PlanesTask h, hipStream_t s, const ColumnSums &sums = {}) {
   g.g.per_row = (uint32_t)(g.g.ld / 8); h.g.per_row = (uint32_t)(h.g.ld / 8);
   const int64_t pg = g.rows * g.g.per_row, ph = h.rows * h.g.per_row;
-  if (pg + ph > (1 << 22)) { TRY(launch_planes(g, s)); return launch_planes(h, s); }
+  if (pg + ph > (1 << 22)) { TRY(launch_planes(h, s)); return launch_planes(g, s, sums); }
   g.g.pieces = (uint32_t)pg; h.g.pieces = (uint32_t)ph;
-  const uint32_t blocks = (uint32_t)((pg + 255) / 256), all = blocks + (uint32_t)((ph + 255) / 256);
+  const uint32_t blocks = (uint32_t)((pg + 255) / 256), from_here = blocks + (uint32_t)((ph + 255) / 256);
+  const dim3 all(from_here + sums.blocks());
   planes_variant(h, [&](auto from, auto planes) {
     constexpr int FROM = decltype(from)::value, PLANES = decltype(planes)::value;
     if constexpr (FROM != FROM_PACKED) {
-      if (g.from != FROM_PACKED) planes_pair_kernel<FROM, PLANES, FROM, PLANES><<<dim3(all), 256, 0, s>>>(g.g, h.g, blocks);
-      else if (g.planes == 1) planes_pair_kernel<FROM_PACKED, 1, FROM, PLANES><<<dim3(all), 256, 0, s>>>(g.g, h.g, blocks);
-      else planes_pair_kernel<FROM_PACKED, 3, FROM, PLANES><<<dim3(all), 256, 0, s>>>(g.g, h.g, blocks);
+      if (g.from != FROM_PACKED) planes_pair_kernel<FROM, PLANES, FROM, PLANES><<<all, 256, 0, s>>>(g.g, h.g, blocks, from_here, sums.g);
+      else if (g.planes == 1) planes_pair_kernel<FROM_PACKED, 1, FROM, PLANES><<<all, 256, 0, s>>>(g.g, h.g, blocks, from_here, sums.g);
+      else planes_pair_kernel<FROM_PACKED, 3, FROM, PLANES><<<all, 256, 0, s>>>(g.g, h.g, blocks, from_here, sums.g);
     }
   });
   HIP_TRY(hipGetLastError());
@@ -446,7 +460,7 @@ int weight_grad_plan(int64_t rows, int32_t in, int32_t out, int32_t activation, 
                               std::max<int64_t>(PIECE_ROWS, (int64_t)(PLANE_BYTES / ((size_t)p.ldp * 2 * p.planes)) / PIECE_ROWS * PIECE_ROWS));
   p.pieces = (rows + p.piece - 1) / p.piece;
   p.sum = p.pieces > 1 && grad_dtype == SHAMPOO_GRAD_BF16;
-  p.part_rows = rows <= 512 ? 512 : std::max<int64_t>(64, (rows + 63) / 64);      // 512 rows: one part, no second launch
+  p.part_rows = rows <= 128 ? 128 : std::max<int64_t>(64, (rows + 255) / 256);
   p.parts = std::max<int64_t>(1, (rows + p.part_rows - 1) / p.part_rows);
   Arena a(workspace);
   p.xp = a.take<uint16_t>((size_t)p.planes * p.piece * p.ldp);
@@ -740,15 +754,10 @@ int shampoo_checkpoint_weight_grad(const void *packed, size_t packed_bytes, int6
     if (db) TRY(launch_zero(db, 1, out, out, 4, s));
     return SHAMPOO_OK;
   }
+  ColumnSums columns = {};
   RowSums sums = {};
+  if (db) columns = {{dy, lddy, rows, p.part_rows, p.parts > 1 ? p.sums : db, out, dtype == SHAMPOO_GRAD_BF16}, p.parts};
   if (db && p.parts > 1) sums = {p.sums, db, (int32_t)p.parts, out};
-  if (db) {
-    const dim3 grid((out + 63) / 64, (unsigned)p.parts);
-    float *const to = p.parts > 1 ? p.sums : db;
-    if (dtype == SHAMPOO_GRAD_F32) column_sums_kernel<float><<<grid, 1024, 0, s>>>(static_cast<const float *>(dy), lddy, rows, out, p.part_rows, to);
-    else column_sums_kernel<uint16_t><<<grid, 1024, 0, s>>>(static_cast<const uint16_t *>(dy), lddy, rows, out, p.part_rows, to);
-    HIP_TRY(hipGetLastError());
-  }
   const Operand dyo = p.dy.operand(dy, p.dyp, LIE_ROWS);
   const bool both = p.dy.copy() && p.pieces == 1;
   if (p.dy.copy() && !both) TRY(launch_planes(p.dy.task(dy, p.dyp), s));
@@ -763,7 +772,8 @@ int shampoo_checkpoint_weight_grad(const void *packed, size_t packed_bytes, int6
     t.g.p = packed_view(packed, rows, in);
     t.g.p.codes += i0 * t.g.p.pitch; t.g.p.exps += i0 * (t.g.p.pitch / 32);
     t.g.rows = n; t.rows = round_up(n, TG_BK);              // zeros behind the last row
-    if (both) TRY(launch_planes(t, p.dy.task(dy, p.dyp), s)); else TRY(launch_planes(t, s));
+    if (both) TRY(launch_planes(t, p.dy.task(dy, p.dyp), s, columns)); else TRY(launch_planes(t, s, columns));
+    columns.parts = 0;
     const Result r = piece_result(dw, lddw, grad_dtype, p.acc, out_in ? in : out, k == 0, k == p.pieces - 1);
     TRY(out_in ? gemm(dk, xo, out, in, n, r, p.part, sums, s) : gemm(xo, dk, in, out, n, r, p.part, sums, s));
   }
