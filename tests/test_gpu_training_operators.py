@@ -412,6 +412,31 @@ def test_weight_gradient_whose_last_round_of_tiles_is_split(out_in):
             assert rel(got[k:k + 128, -3000:], want[k:k + 128, -3000:]) <= 2 * bar
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("n,i,o", [(64, 40, 63), (128, 40, 64), (129, 200, 65), (192, 40, 300), (1000, 8, 1), (16385, 40, 130), (20001, 33, 7)])
+def test_bias_gradients_by_parts_of_the_rows(n, i, o, dt):
+    """Every column by itself: a term goes through less than 40 float32 additions, so 40 e of the sum of |dy|."""
+    torch = torch_()
+    g = gen(n + o)
+    dt = torch.bfloat16 if dt == "bf16" else torch.float32
+    x, dy = activations(g, n, i).to(dt), normal(g, n, o).to(dt)
+    dy[:, ::3] += 1.0
+    c = B.shampoo_checkpoint_pack(x)
+    for grad in {dt, torch.float32}:
+        dw, db = B.shampoo_checkpoint_weight_grad(c, dy, grad_dtype=grad, bias=True)
+        assert ((db.double() - dy.double().sum(0)).abs() <= 40 * 2.0 ** -24 * dy.double().abs().sum(0)).all()
+        alone = B.shampoo_checkpoint_weight_grad(c, dy, grad_dtype=grad)
+        assert torch.equal(dw, alone)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("in_out", [False, True])
+@pytest.mark.parametrize("n,d,v", [(40, 300, 1100), (250, 520, 700), (32, 2048, 1000), (700, 1100, 900)])
+def test_head_whose_small_gradients_share_a_launch(n, d, v, in_out, kind):
+    test_head_and_its_gradients(n, d, v, True, in_out, kind)
+    test_head_and_its_gradients(n, d, v, False, in_out, kind)
+
+
 def test_weight_gradient_in_several_pieces_of_rows():
     torch = torch_()
     g = gen(3)
