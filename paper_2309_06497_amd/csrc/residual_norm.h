@@ -427,6 +427,13 @@ __global__ __launch_bounds__(1024) void join_sums_kernel(const JoinSumsArgs g) {
   if (j < g.cols) {
     const float *p = g.in[blockIdx.z] + blockIdx.y * g.output_stride + j;
     int i = k;
+    for (; i + 240 < parts; i += 256) {
+      float x[16];
+#pragma unroll
+      for (int q = 0; q < 16; ++q) x[q] = p[(i + 16 * q) * g.part_stride];
+#pragma unroll
+      for (int q = 0; q < 16; ++q) s[q & 3] += x[q];
+    }
     for (; i + 48 < parts; i += 64) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) s[q] += p[(i + 16 * q) * g.part_stride];
