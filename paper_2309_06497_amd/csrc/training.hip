@@ -189,6 +189,7 @@ int plane_pairs(int na, int nb, uint32_t &pa, uint32_t &pb) {
 // Against all cuts of 19 shapes between 256 x 256 x 512 and 8192 x 2048 x 8192 the choice is within 15 % of the best.  For example
 // 2000 x 1000 x 50000: 186 (256, 8 splits), 206 (128, 4), 637 (128, 1); 2048 x 2048 x 2048: 21 (128, 1; two stages 29), 41 (128, 2),
 // 47 (256, 1); 256 x 256 x 4096: 11 (128, 16), 26 (128, 1).
+// tile_end: what a tile of 128 has to do behind its products beyond a plain store.
 // tail: splits of the last round's tiles, where the others fill the GPU a whole number of times and these leave much of it idle for as long
 // again: 1000 x 50001 x 1999 with three planes a side, 784 tiles of 256 in four rounds, 665 us; in three and the 16 left over in
 // 16 splits each, 602 with their join.
@@ -197,7 +198,7 @@ constexpr int64_t CUS = 256, BIG_TILE = 256;
 constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256, 384, 512};
 inline double join_us(int64_t M, int64_t N, int splits) { return splits > 1 ? 3.0 + (double)splits * (double)M * (double)N * 2e-6 : 0.0; }
 inline size_t part_bytes(int64_t M, int64_t N, int splits) { return splits > 1 ? align_up((size_t)splits * M * round_up(N, 8) * sizeof(float)) : 0; }
-GemmCut gemm_cut(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, int most = 512) {
+GemmCut gemm_cut(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, int most = 512, double tile_end = 0.0) {
   uint32_t unused_a, unused_b;
   const int64_t all = (K + TG_BK - 1) / TG_BK * plane_pairs(planes_a, planes_b, unused_a, unused_b);
   GemmCut best = {2, 1, (int)all, 0, 2, 1, INFINITY};
@@ -214,7 +215,7 @@ GemmCut gemm_cut(int64_t M, int64_t N, int64_t K, int planes_a, int planes_b, in
       if (splits > 1 && (splits > all / 2 || splits > most)) break;
       const int64_t tile = 64 * ti, tiles = ((M + tile - 1) / tile) * ((N + tile - 1) / tile), per = (all + splits - 1) / splits;
       const double each = (double)((tiles * splits + 255) / 256);       // workgroups per CU
-      double us = ti == 4 ? 5.0 + each * (6.0 + 1.7 * (double)per) : 4.0 + (double)per * (each <= 1.0 ? 0.55 : each <= 2.0 ? 1.0 : 0.58 * each);
+      double us = ti == 4 ? 5.0 + each * (6.0 + 1.7 * (double)per) : 4.0 + (double)per * (each <= 1.0 ? 0.55 : each <= 2.0 ? 1.0 : 0.58 * each) + tile_end * each;
       us += join_us(M, N, splits);
       const bool with_tail = ti == 4 && splits == 1 && tail > 1;
       if (with_tail) us -= saved;
@@ -375,6 +376,11 @@ struct CrossEntropyPlan {
   float *z, *lse, *coef, *target_z, *acc, *sums, *part;
   float2 *stats;
   int grad_planes() const { return std::max(planes, 1); }
+  // the logits' product over n rows: where it stores float32 ones, 0.4 us more for the end of a tile of 128 (1999 x 1000 x 50001: 354 us
+  // in 25 tiles of 128 a CU, 330 in seven rounds of tiles of 256; 512 x 512 x 32000 in float32 dw 159 us in all, 168)
+  GemmCut for_logits(const shampoo_cross_entropy &c, int64_t n) const {
+    return gemm_cut(n, c.classes, c.features, x.planes(), w.planes(), twice ? 1 : LOGIT_SPLITS, c.gradients && !twice && planes ? 0.4 : 0.0);
+  }
   // the gradients' products over n rows
   Product for_dx(const shampoo_cross_entropy &c, int64_t n) const { return {n, c.features, c.classes, x.planes(), w.planes()}; }
   Product for_dw(const shampoo_cross_entropy &c, int64_t n) const {
@@ -423,7 +429,7 @@ int cross_entropy_plan(const shampoo_cross_entropy &c, void *workspace, CrossEnt
   size_t part = 0;
   for (int64_t n : {p.piece, c.rows - std::max<int64_t>(0, p.pieces - 1) * p.piece, c.rows}) {      // all pieces, the last one, a single one
     if (n < 1 || n > p.piece) continue;
-    part = std::max(part, gemm_cut(n, v, d, p.x.planes(), p.w.planes(), p.twice ? 1 : LOGIT_SPLITS).bytes);
+    part = std::max(part, p.for_logits(c, n).bytes);
     if (!c.gradients) continue;
     const Product fx = p.for_dx(c, n), fw = p.for_dw(c, n);
     for (const Product &f : {fx, fw}) part = std::max(part, gemm_cut(f.M, f.N, f.K, f.planes_a, f.planes_b).bytes);
@@ -613,7 +619,7 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
     RowSums &sums = k == p.pieces - 1 ? bias_sums : none;      // once all pieces have left theirs
     Operand xk = xo;
     xk.p += i0 * xo.ld;
-    const GemmCut cut = gemm_cut(n, v, d, xk.planes, wo.planes, p.twice ? 1 : LOGIT_SPLITS);
+    const GemmCut cut = p.for_logits(*c, n);
     const int32_t span = cut.splits > 1 ? 64 : 32 * cut.ti;
     const int store = !c->gradients || p.twice ? STORE_NOTHING : STORE_F32, end = store == STORE_NOTHING || p.planes ? END_LOGITS : END_LOGITS_U16;
     void *const logits = p.planes ? static_cast<void *>(p.z) : p.g;
