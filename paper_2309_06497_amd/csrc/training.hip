@@ -460,7 +460,8 @@ int weight_grad_plan(int64_t rows, int32_t in, int32_t out, int32_t activation, 
   if (!dtype_ok(dtype) || !dtype_ok(grad_dtype) || activation < ACT_NONE || activation > ACT_SILU) return SHAMPOO_ERR_HYPER;
   if (dtype == SHAMPOO_GRAD_F32 && grad_dtype != SHAMPOO_GRAD_F32) return SHAMPOO_ERR_HYPER;
   p.dy = {dtype, rows, out, lddy, 8};
-  p.planes = activation == ACT_NONE ? 1 : grad_dtype == SHAMPOO_GRAD_F32 ? 3 : 1;
+  // a code times its scale is a bf16 value, and so is its ReLU; other activations take three planes for a float32 result
+  p.planes = activation == ACT_NONE || activation == ACT_RELU || grad_dtype != SHAMPOO_GRAD_F32 ? 1 : 3;
   p.ldp = round_up(in, 64);
   p.piece = std::min<int64_t>(round_up(std::max<int64_t>(rows, 1), PIECE_ROWS),
                               std::max<int64_t>(PIECE_ROWS, (int64_t)(PLANE_BYTES / ((size_t)p.ldp * 2 * p.planes)) / PIECE_ROWS * PIECE_ROWS));

@@ -413,6 +413,19 @@ def test_weight_gradient_whose_last_round_of_tiles_is_split(out_in):
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("n,i,o", [(1, 40, 9), (257, 256, 128), (999, 130, 331)])
+def test_weight_gradient_of_relu_is_exact_up_to_sums(n, i, o, dt):
+    """relu(x) of a checkpoint is a bf16 value: as without an activation, nothing but float32 sums of n terms."""
+    torch = torch_()
+    g = gen(n + 7)
+    dt = torch.bfloat16 if dt == "bf16" else torch.float32
+    x, dy = activations(g, n, i).to(dt), normal(g, n, o).to(dt)
+    c = B.shampoo_checkpoint_pack(x)
+    want = held(x).clamp_min(0.0).t() @ dy.double()
+    assert rel(B.shampoo_checkpoint_weight_grad(c, dy, B.ACT_RELU, torch.float32), want) <= 2.0 ** -18
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("n,i,o", [(64, 40, 63), (128, 40, 64), (129, 200, 65), (192, 40, 300), (1000, 8, 1), (16385, 40, 130), (20001, 33, 7)])
 def test_bias_gradients_by_parts_of_the_rows(n, i, o, dt):
     """Every column by itself: a term goes through less than 40 float32 additions, so 40 e of the sum of |dy|."""
