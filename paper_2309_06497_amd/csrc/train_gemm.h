@@ -455,11 +455,11 @@ __global__ __launch_bounds__(256, TI == 2 && STAGES == 2 ? 2 : 1) void train_gem
 
 // Two small products that do not depend on one another, in one launch: the first `blocks` workgroups (a multiple of 8) have g, whose A
 // lies along k, the others h, whose operands both lie along rows.
-template <int BLIE> __global__ __launch_bounds__(256, 1) void train_gemm_pair_kernel(const TrainGemmArgs g, const TrainGemmArgs h, int blocks) {
-  __shared__ __align__(256) unsigned char smem[GEMM_LDS<2, 4>];
+template <int STAGES, int BLIE> __global__ __launch_bounds__(256, STAGES == 2 ? 2 : 1) void train_gemm_pair_kernel(const TrainGemmArgs g, const TrainGemmArgs h, int blocks) {
+  __shared__ __align__(256) unsigned char smem[GEMM_LDS<2, STAGES>];
   const int block = (int)blockIdx.x;
-  if (block < blocks) train_gemm_tile<2, 4, LIE_K, BLIE, END_PLAIN>(g, block, smem);
-  else train_gemm_tile<2, 4, LIE_ROWS, LIE_ROWS, END_PLAIN>(h, block - blocks, smem);
+  if (block < blocks) train_gemm_tile<2, STAGES, LIE_K, BLIE, END_PLAIN>(g, block, smem);
+  else train_gemm_tile<2, STAGES, LIE_ROWS, LIE_ROWS, END_PLAIN>(h, block - blocks, smem);
 }
 
 // The results of several splits, float32 [split][rows][cols], added up in an order that does not depend on the launch.  LANES

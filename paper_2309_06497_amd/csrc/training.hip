@@ -294,9 +294,10 @@ int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, co
   return gemm_join(g, c, sums, s);
 }
 
-// Two products, the second with both operands along rows: in one launch of tiles of 128, a workgroup per CU at most, where that is
+// Two products, the second with both operands along rows: in one launch of tiles of 128, four workgroups per CU at most, where that is
 // shorter by gemm_cut's model and 2 us for a launch.  The gradients of 256 x 2048 x 1000 in float32: 15 + 18 us, together 21.5; of
-// 32 x 256 x 1000 in bf16 5.4 + 6.1, together 6.4.
+// 32 x 256 x 1000 in bf16 5.4 + 6.1, together 6.4; with more than one workgroup per CU the whole of 100 x 1024 x 10000 in bf16
+// 45.8, 39.0 together.  Of 18 shapes in both types one was longer together (by 2 %, 700 x 700 x 7000 in float32).
 struct PairCut { GemmCut first, second; bool together; size_t bytes; };
 struct Product { int64_t M, N, K; int planes_a, planes_b; };
 PairCut pair_cut(const Product &f, const Product &g) {
@@ -308,15 +309,17 @@ PairCut pair_cut(const Product &f, const Product &g) {
   const auto slabs = [&](const Product &p) { return (p.K + TG_BK - 1) / TG_BK * plane_pairs(p.planes_a, p.planes_b, unused_a, unused_b); };
   const int64_t tiles_f = tiles(f), tiles_g = tiles(g), all_f = slabs(f), all_g = slabs(g);
   for (int sf : SPLITS) {
-    if (round_up(tiles_f * sf, 8) + tiles_g > CUS || (sf > 1 && sf > all_f / 2)) break;
+    if (tiles_f * sf + tiles_g > 4 * CUS || (sf > 1 && sf > all_f / 2)) break;
     for (int sg : SPLITS) {
-      if (round_up(tiles_f * sf, 8) + round_up(tiles_g * sg, 8) > CUS || (sg > 1 && sg > all_g / 2)) break;
-      const int64_t per_f = (all_f + sf - 1) / sf, per_g = (all_g + sg - 1) / sg;
-      const double us = 4.0 + 0.55 * (double)std::max(per_f, per_g) + join_us(f.M, f.N, sf) + join_us(g.M, g.N, sg);
+      if (tiles_f * sf + tiles_g * sg > 4 * CUS || (sg > 1 && sg > all_g / 2)) break;
+      const int64_t per_f = (all_f + sf - 1) / sf, per_g = (all_g + sg - 1) / sg, longest = std::max(per_f, per_g);
+      const bool alone = round_up(tiles_f * sf, 8) + round_up(tiles_g * sg, 8) <= CUS;        // on its CU
+      const double work = (double)(tiles_f * sf * per_f + tiles_g * sg * per_g) / (double)CUS;
+      const double us = 4.0 + (alone ? 0.55 * (double)longest : std::max((double)longest, 0.58 * work)) + join_us(f.M, f.N, sf) + join_us(g.M, g.N, sg);
       if (us < shortest) {
         shortest = us;
-        best.first = {2, (int)((all_f + per_f - 1) / per_f), (int)per_f, 0, 4, 1, us};
-        best.second = {2, (int)((all_g + per_g - 1) / per_g), (int)per_g, 0, 4, 1, us};
+        best.first = {2, (int)((all_f + per_f - 1) / per_f), (int)per_f, 0, alone ? 4 : 2, 1, us};
+        best.second = {2, (int)((all_g + per_g - 1) / per_g), (int)per_g, 0, best.first.stages, 1, us};
         best.first.bytes = part_bytes(f.M, f.N, best.first.splits); best.second.bytes = part_bytes(g.M, g.N, best.second.splits);
         best.together = true; best.bytes = best.first.bytes + best.second.bytes;
       }
@@ -334,8 +337,13 @@ int gemm_pair(const Operand &a, const Operand &b, const Product &f, const Result
   gemm_result(y, r, part + cut.first.bytes / sizeof(float));
   const int blocks = (int)round_up(x.tiles * x.splits, 8);
   const dim3 grid((unsigned)(blocks + round_up(y.tiles * y.splits, 8)));
-  if (b.lie == LIE_K) train_gemm_pair_kernel<LIE_K><<<grid, 256, 0, s>>>(x, y, blocks);
-  else train_gemm_pair_kernel<LIE_ROWS><<<grid, 256, 0, s>>>(x, y, blocks);
+  if (cut.first.stages == 4) {
+    if (b.lie == LIE_K) train_gemm_pair_kernel<4, LIE_K><<<grid, 256, 0, s>>>(x, y, blocks);
+    else train_gemm_pair_kernel<4, LIE_ROWS><<<grid, 256, 0, s>>>(x, y, blocks);
+  } else {
+    if (b.lie == LIE_K) train_gemm_pair_kernel<2, LIE_K><<<grid, 256, 0, s>>>(x, y, blocks);
+    else train_gemm_pair_kernel<2, LIE_ROWS><<<grid, 256, 0, s>>>(x, y, blocks);
+  }
   HIP_TRY(hipGetLastError());
   if (x.splits > 1) TRY(gemm_join(x, c, sums, s));
   if (y.splits > 1) TRY(gemm_join(y, r, sums, s));

@@ -125,6 +125,13 @@ def test_head_and_its_gradients(n, d, v, bias, in_out, kind):
     assert torch.allclose(loss, out[0], rtol=1e-5, atol=1e-5)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("in_out", [False, True])
+@pytest.mark.parametrize("n,d,v", [(200, 300, 8000), (17, 2048, 1500), (520, 1000, 4001)])
+def test_head_whose_gradients_share_a_launch_of_more_workgroups_than_cus(n, d, v, in_out, kind):
+    test_head_and_its_gradients(n, d, v, True, in_out, kind)
+
+
 @pytest.mark.parametrize("how", ["rows", "odd"])
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_head_on_strided_views(how, dt):
