@@ -3,7 +3,11 @@
 //   lse_i = log sum_v exp z_iv        loss_i = lse_i - z_{i,t_i}        g_iv = c_i (exp(z_iv - lse_i) - [v = t_i])
 //   dx = g w        dw = g^T x        db = column sums of g
 //
-// c_i = scale weight_i, zero where the target is ignored.  The product that makes z (train_gemm.h) leaves, for every row
+// c_i = scale weight_i, zero where the target is ignored.  g is kept with the power of two of `scale` alone, and the products' results are
+// multiplied by the rest in float32: g of the target is about -c_i in every row, and its rounding to bf16 would be the same error of up
+// to 3.9e-3 in all rows, while 1 - p rounds exactly or nearly so (255 x 256 x 20000 at a scale of 1/255: gradients 4.2e-3 off the definition's
+// with the scale in g, 1.7 ... 2.0e-3 so, of which 1.7e-3 is the rounding of the result).
+// The product that makes z (train_gemm.h) leaves, for every row
 // and span of 64 or 128 classes, the largest z and the sum of exp(z - largest), and of a piece of the rows
 //   bf16 x, bf16 dw, no bias: the distance of z from the largest of its span in 16 bits, steps of 2^-10 in the exponent of 2
 //     (2 bytes per logit; exp(z) is off by 3.4e-4 of itself at most where the rounding of g to bf16 is 3.9e-3; what is further than 64
@@ -132,8 +136,9 @@ struct SoftmaxGradArgs {
   const float *z; int64_t ldg;       // float32 logits
   int32_t span;
   uint16_t *out; int64_t plane;      // [plane][rows][ldg]; 16-bit logits are read here
-  float *sums;                       // [ranges][classes] column sums of g, or nullptr
+  float *sums;                       // [ranges][classes] column sums of g, or nullptr; times `alpha`
   int32_t per_range;                 // at most 64
+  float alpha;
 };
 // PLANES = 0: one plane, in the place of 16-bit logits.  Four rows are on their way together.  Where a workgroup has the rows' whole
 // width (up to 2048 classes) it ends the rows' sums too: one launch instead of two.
@@ -215,7 +220,7 @@ template <int PLANES> __global__ __launch_bounds__(256) void softmax_grad_kernel
   if (!g.sums) return;
 #pragma unroll
   for (int e = 0; e < 8; ++e)
-    if (c + e < classes) g.sums[(int64_t)blockIdx.y * classes + c + e] = sum.v[e];
+    if (c + e < classes) g.sums[(int64_t)blockIdx.y * classes + c + e] = g.alpha * sum.v[e];
 }
 
 }  // namespace shampoo

@@ -55,6 +55,7 @@ struct TrainGemmArgs {
   int32_t by_tile;                         // c holds this launch's tiles one behind the other, 64 TI x 64 TI each, per split
   void *c; int64_t ldc, c_split;           // c_split: from the result of a split to the next
   const float *add; int64_t ldadd;         // C += add (float32; may be c itself) or nullptr
+  float alpha;                             // C = alpha A B^T + add
   int32_t store;
   // END_LOGITS...: z = C + bias (16 bits: no bias); per row and span (32 TI columns): the largest z and sum of exp(z - largest); the target's z
   const float *bias; const int64_t *targets;
@@ -337,6 +338,8 @@ __device__ __forceinline__ void train_gemm_tile(const TrainGemmArgs &g, int bloc
       stage(i);
       put(i, [&](int r, int64_t out) {
         f32x8 z = staged(r);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z.v[e] *= g.alpha;
         if (g.add) {
           const f32x8 old = load8(g.add + out * g.ldadd, col, g.N);
 #pragma unroll
@@ -471,6 +474,7 @@ struct JoinArgs {
   void *c; int64_t ldc; const float *add; int64_t ldadd;
   int64_t row0; uint32_t pieces, per_row;
   int32_t cols, pitch, store;
+  float alpha;
   uint32_t blocks; RowSums sums;
 };
 __device__ __forceinline__ void row_sums(const RowSums &g, int block) {
@@ -513,6 +517,8 @@ template <int LANES> __global__ __launch_bounds__(256) void train_join_kernel(co
 #pragma unroll
     for (int e = 0; e < 8; ++e) s.v[e] += __shfl_xor(s.v[e], o, 64);
   if (at >= g.pieces || lane != 0) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s.v[e] *= g.alpha;
   if (g.add) {
     const f32x8 x = load8(g.add + row * g.ldadd, c, g.cols);
 #pragma unroll
@@ -527,6 +533,7 @@ struct JoinTilesArgs {
   const float *part; int64_t stride; int32_t splits;
   void *c; int64_t ldc; const float *add; int64_t ldadd;
   int32_t M, N, tiles_m, tiles_n, tile0, tile, store;       // tile: rows of one
+  float alpha;
 };
 __global__ __launch_bounds__(256) void train_join_tiles_kernel(const JoinTilesArgs g) {
   const int pieces = g.tile * g.tile / 8, per = pieces / 256;           // workgroups of a tile
@@ -544,6 +551,8 @@ __global__ __launch_bounds__(256) void train_join_tiles_kernel(const JoinTilesAr
 #pragma unroll
     for (int e = 0; e < 8; ++e) s.v[e] += x.v[e];
   }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s.v[e] *= g.alpha;
   if (g.add) {
     const f32x8 x = load8(g.add + row * g.ldadd, col, g.N);
 #pragma unroll

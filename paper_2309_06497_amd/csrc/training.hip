@@ -170,6 +170,7 @@ struct Operand {
 };
 struct Result {
   void *c; int64_t ldc; int store; const float *add; int64_t ldadd;
+  float alpha = 1.f;
 };
 
 // the pairs of planes that a product needs, smallest first: of terms of 8 bits each, those that reach 24 bits
@@ -246,17 +247,18 @@ void gemm_args(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t
   g.splits = cut.splits; g.per_split = cut.per_split;
   g.tiles = g.tiles_m * g.tiles_n;
   g.padded = a.padded ? 1 : b.padded ? 2 : 0;
+  g.alpha = 1.f;
 }
 // where C goes: with several splits their results lie one behind the other in `part`
 void gemm_result(TrainGemmArgs &g, const Result &c, float *part) {
   if (g.splits > 1) { g.c = part; g.ldc = round_up(g.N, 8); g.c_split = g.M * g.ldc; g.store = STORE_F32; }
-  else { g.c = c.c; g.ldc = c.ldc; g.add = c.add; g.ldadd = c.ldadd; g.store = c.store; }
+  else { g.c = c.c; g.ldc = c.ldc; g.add = c.add; g.ldadd = c.ldadd; g.store = c.store; g.alpha = c.alpha; }
 }
 // sums: go along, and are struck out there
 int gemm_join(const TrainGemmArgs &g, const Result &c, RowSums &sums, hipStream_t s) {
   JoinArgs j = {};
   j.part = static_cast<const float *>(g.c); j.stride = g.c_split; j.splits = g.splits; j.c = c.c; j.ldc = c.ldc; j.add = c.add; j.ldadd = c.ldadd;
-  j.cols = g.N; j.pitch = (int32_t)g.ldc; j.store = c.store; j.per_row = (uint32_t)(g.ldc / 8);
+  j.alpha = c.alpha; j.cols = g.N; j.pitch = (int32_t)g.ldc; j.store = c.store; j.per_row = (uint32_t)(g.ldc / 8);
   return by_rows(g.M, j.per_row, [&](int64_t r, uint32_t pieces, dim3 grid) {
     j.row0 = r; j.pieces = pieces;
     const bool eight = g.splits >= 16 && pieces < (1u << 24);
@@ -281,10 +283,10 @@ int gemm(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, co
     if (rest == 0) return SHAMPOO_OK;
     g.tile0 = g.tiles; g.tiles = rest; g.by_tile = 1;
     g.per_split = (all + cut.tail - 1) / cut.tail; g.splits = (all + g.per_split - 1) / g.per_split;
-    g.c = part; g.ldc = BIG_TILE; g.c_split = rest * BIG_TILE * BIG_TILE; g.add = nullptr; g.store = STORE_F32;
+    g.c = part; g.ldc = BIG_TILE; g.c_split = rest * BIG_TILE * BIG_TILE; g.add = nullptr; g.alpha = 1.f; g.store = STORE_F32;
     gemm_launch<END_PLAIN>(g, cut, a.lie, b.lie, s);
     HIP_TRY(hipGetLastError());
-    const JoinTilesArgs j = {part, g.c_split, g.splits, c.c, c.ldc, c.add, c.ldadd, g.M, g.N, g.tiles_m, g.tiles_n, g.tile0, (int32_t)BIG_TILE, c.store};
+    const JoinTilesArgs j = {part, g.c_split, g.splits, c.c, c.ldc, c.add, c.ldadd, g.M, g.N, g.tiles_m, g.tiles_n, g.tile0, (int32_t)BIG_TILE, c.store, c.alpha};
     train_join_tiles_kernel<<<dim3((unsigned)(rest * (BIG_TILE * BIG_TILE / 8 / 256))), 256, 0, s>>>(j);
     HIP_TRY(hipGetLastError());
     return SHAMPOO_OK;
@@ -623,6 +625,9 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
   else if (p.w.copy()) TRY(launch_planes(p.w.task(w, p.wp), s));
   const int64_t last = c->rows - (p.pieces - 1) * p.piece;
   RowSums bias_sums = {dbias ? p.sums : nullptr, dbias, (int32_t)((p.pieces - 1) * p.ranges + (round_up(last, TG_BK) + p.range_rows - 1) / p.range_rows), (int32_t)v}, none = {};
+  // scale = power alpha, alpha in [1, 2); very small ones as they are
+  const float power = std::fabs(scale) < 0x1p-100f ? scale : std::copysign(std::ldexp(1.f, std::ilogb(scale)), scale);
+  const float alpha = std::fabs(scale) < 0x1p-100f ? 1.f : scale / power;
   for (int64_t k = 0; k < p.pieces; ++k) {
     const int64_t i0 = k * p.piece, n = std::min(p.piece, c->rows - i0);
     RowSums &sums = k == p.pieces - 1 ? bias_sums : none;      // once all pieces have left theirs
@@ -647,7 +652,7 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
       if (end == END_LOGITS_U16) gemm_launch<END_LOGITS_U16>(z, cut, xk.lie, wo.lie, s); else gemm_launch<END_LOGITS>(z, cut, xk.lie, wo.lie, s);
     }
     HIP_TRY(hipGetLastError());
-    const RowLossArgs r = {p.stats, p.piece, p.target_z, targets + i0, weight ? weight + i0 : nullptr, scale, p.lse, p.coef, loss + i0,
+    const RowLossArgs r = {p.stats, p.piece, p.target_z, targets + i0, weight ? weight + i0 : nullptr, power, p.lse, p.coef, loss + i0,
                            (int32_t)n, (int32_t)v, (int32_t)((v + span - 1) / span)};
     const dim3 grid((unsigned)((p.ldz / 8 + 255) / 256), (unsigned)((round_up(n, TG_BK) + p.range_rows - 1) / p.range_rows));   // zeros behind the last row
     const bool wanted = dx || dw || dbias;
@@ -660,7 +665,7 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
       z.c = p.g; z.lse = p.lse; z.coef = p.coef; z.c_plane = p.piece * p.ldz; z.c_planes = p.planes;
       gemm_launch<END_GRAD>(z, cut, xk.lie, wo.lie, s);
     } else {
-      const SoftmaxGradArgs q = {r, p.z, p.ldz, span, p.g, p.piece * p.ldz, dbias ? p.sums + k * p.ranges * v : nullptr, (int32_t)p.range_rows};
+      const SoftmaxGradArgs q = {r, p.z, p.ldz, span, p.g, p.piece * p.ldz, dbias ? p.sums + k * p.ranges * v : nullptr, (int32_t)p.range_rows, alpha};
       switch (p.planes) {
         case 0: softmax_grad_kernel<0><<<grid, 256, 0, s>>>(q); break;
         case 1: softmax_grad_kernel<1><<<grid, 256, 0, s>>>(q); break;
@@ -675,8 +680,9 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
     xk.lie = LIE_ROWS;
     const Operand &left = out_in ? gt : xk, &right = out_in ? xk : gt;
     const Product fx = p.for_dx(*c, n), fw = p.for_dw(*c, n);
-    const Result to_dx = {!dx ? nullptr : static_cast<char *>(dx) + i0 * c->lddx * size_of(c->dtype), c->lddx, c->dtype == SHAMPOO_GRAD_F32 ? STORE_F32 : STORE_BF16, nullptr, 0};
-    const Result to_dw = piece_result(dw, c->lddw, c->grad_dtype, p.acc, p.w.cols, k == 0, k == p.pieces - 1);
+    const Result to_dx = {!dx ? nullptr : static_cast<char *>(dx) + i0 * c->lddx * size_of(c->dtype), c->lddx, c->dtype == SHAMPOO_GRAD_F32 ? STORE_F32 : STORE_BF16, nullptr, 0, alpha};
+    Result to_dw = piece_result(dw, c->lddw, c->grad_dtype, p.acc, p.w.cols, k == 0, k == p.pieces - 1);
+    to_dw.alpha = alpha;
     const PairCut pair = dx && dw ? pair_cut(fx, fw) : PairCut();
     if (pair.together) {
       TRY(gemm_pair(go, wt, fx, to_dx, left, right, fw, to_dw, pair, p.part, sums, s));

@@ -132,6 +132,31 @@ def test_head_whose_gradients_share_a_launch_of_more_workgroups_than_cus(n, d, v
     test_head_and_its_gradients(n, d, v, True, in_out, kind)
 
 
+@pytest.mark.parametrize("d", [64, 256])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("scale", [1.0 / 255, 1.0 / 509, -3.02, 1.0])
+def test_head_gradients_in_bf16_are_not_scaled_as_a_whole(scale, bias, d):
+    """Against the definition's gradients rounded once (one product of a bf16 x and the scale is many a dw's only term, so that roundings
+    of the result all go one way): roundings of single elements of g average out in <got, want> / <want, want> (over 255 d of them, and
+    more); one of the scale, which every row shares, would not: 2^-11, of which 2^-13 is the largest probability, which 1 - p may lose."""
+    torch = torch_()
+    g = gen(31)
+    n, v = 255, 20000
+    x, w = normal(g, n, d, sigma=0.1).bfloat16(), normal(g, v, d, sigma=0.1).bfloat16()
+    t = torch.randint(0, v, (n,), generator=g, device="cuda")
+    b = normal(g, v, sigma=0.01) if bias else None
+    out = B.shampoo_linear_cross_entropy(x, w, t, bias=b, scale=scale)
+    want = head_reference(x, w, t, b, None, scale)
+    want = [want[0], want[1].bfloat16().double(), want[2].bfloat16().double(), want[3]]
+    for k in (1, 2) + ((3,) if bias else ()):
+        dot = float((out[k].double() * want[k]).sum() / (want[k] * want[k]).sum())
+        assert abs(dot - 1.0) <= 2.0 ** -11
+    none = B.shampoo_linear_cross_entropy(x, w, t, bias=b, scale=0.0)
+    assert not none[1].any() and not none[2].any()
+    tiny = B.shampoo_linear_cross_entropy(x, w, t, bias=b, scale=1.7e-38, grad_dtype=torch.float32)
+    assert torch.isfinite(tiny[2]).all() and torch.isfinite(tiny[1].float()).all()
+
+
 @pytest.mark.parametrize("how", ["rows", "odd"])
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_head_on_strided_views(how, dt):
