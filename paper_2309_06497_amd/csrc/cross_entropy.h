@@ -1,7 +1,10 @@
 // Softmax cross entropy of a linear layer z = x w^T + b over many classes, with its gradients.
 //
-//   lse_i = log sum_v exp z_iv        loss_i = lse_i - z_{i,t_i}        g_iv = c_i (exp(z_iv - lse_i) - [v = t_i])
+//   m_i = max_v z_iv        s_i = sum_v exp(z_iv - m_i)        loss_i = (m_i - z_{i,t_i}) + log s_i        g_iv = c_i (exp(z_iv - m_i) / s_i - [v = t_i])
 //   dx = g w        dw = g^T x        db = column sums of g
+//
+// m and log s are never added: beside an m of 1e4 a float32 keeps log s to 5e-4, and that would be the relative error of every p of the row (300 equal
+// logits of 1e6: the sum of p 1.016).  z - m is exact where p matters.  A row is kept as m_i, c_i and c_i / s_i, so that g is one fused multiply-add.
 //
 // c_i = scale weight_i, zero where the target is ignored.  g is kept with the power of two of `scale` alone, and the products' results are
 // multiplied by the rest in float32: g of the target is about -c_i in every row, and its rounding to bf16 would be the same error of up
@@ -84,12 +87,12 @@ __global__ __launch_bounds__(256) void logits_join_kernel(const LogitsJoinArgs g
   else if (g.store != STORE_NOTHING) store8(static_cast<float *>(g.z) + (int64_t)i * g.ldz, c, (int)g.ldz, z);
 }
 
-// lse, loss and c of every row from the largest logits and sums of its spans: 16 rows per workgroup, 64 threads a row.
+// m, c, c / s and the loss of every row from the largest logits and sums of its spans: 16 rows per workgroup, 64 threads a row.
 struct RowLossArgs {
   const float2 *stats; int64_t stats_ld;
   const float *target_z; const int64_t *targets; const float *weight;
   float scale;
-  float *lse, *coef, *loss;
+  float *top, *coef, *share, *loss;  // m, c, c / s
   int32_t rows, classes, spans;
 };
 // exp sums (m, s) and (n, t) together; s is 0 or NaN where m is -infinity
@@ -98,14 +101,15 @@ __device__ __forceinline__ void join_exp(float &m, float &s, float n, float t) {
   const float a = m == -INFINITY ? s : s * __builtin_amdgcn_exp2f((m - top) * LOG2_E), b = n == -INFINITY ? t : t * __builtin_amdgcn_exp2f((n - top) * LOG2_E);
   m = top; s = a + b;
 }
-__device__ __forceinline__ void row_end(const RowLossArgs &g, int i, float m, float s, float &lse, float &coef) {
-  const float l = (m == -INFINITY ? 0.f : m) + logf(s);         // no class left: -infinity
+// No class left (s = 0): c = 0.
+__device__ __forceinline__ void row_end(const RowLossArgs &g, int i, float m, float s, float &top, float &coef, float &share) {
   const int64_t t = g.targets[i];
   const bool valid = t >= 0 && t < g.classes;
-  lse = l;
-  coef = valid ? g.scale * (g.weight ? g.weight[i] : 1.f) : 0.f;
+  top = m == -INFINITY ? 0.f : m;
+  coef = valid && s != 0.f ? g.scale * (g.weight ? g.weight[i] : 1.f) : 0.f;
+  share = coef / s;
   const float zt = valid ? g.target_z[i] : 0.f;
-  g.loss[i] = !valid ? 0.f : zt == -INFINITY ? INFINITY : l - zt;
+  g.loss[i] = !valid ? 0.f : zt == -INFINITY ? INFINITY : (m - zt) + logf(s);
 }
 __global__ __launch_bounds__(1024) void row_loss_kernel(const RowLossArgs g) {
   __shared__ float2 part[16][16];
@@ -127,7 +131,7 @@ __global__ __launch_bounds__(1024) void row_loss_kernel(const RowLossArgs g) {
   __syncthreads();
   if (k != 0 || i >= g.rows) return;
   for (int p = 1; p < 16; ++p) join_exp(m, s, part[p][r].x, part[p][r].y);
-  row_end(g, i, m, s, g.lse[i], g.coef[i]);
+  row_end(g, i, m, s, g.top[i], g.coef[i], g.share[i]);
 }
 
 // g of a piece of the rows, zeros from classes to ldg and in the rows from `rows` to the next multiple of 64.  A thread has eight columns of the rows of its range.
@@ -144,12 +148,12 @@ struct SoftmaxGradArgs {
 // width (up to 2048 classes) it ends the rows' sums too: one launch instead of two.
 template <int PLANES> __global__ __launch_bounds__(256) void softmax_grad_kernel(const SoftmaxGradArgs g) {
   constexpr int OUT = PLANES ? PLANES : 1, AHEAD = 4;
-  __shared__ float row_lse[64], row_coef[64];
+  __shared__ float row_top[64], row_coef[64], row_share[64];
   const int c = (blockIdx.x * 256 + threadIdx.x) * 8, rows = g.row.rows, classes = g.row.classes;
   const int end = (rows + 63) & ~63, i0 = blockIdx.y * g.per_range, i1 = min(end, i0 + g.per_range);
   {
     const int r = threadIdx.x >> 2, i = i0 + r;                 // four threads a row
-    float lse = 0.f, coef = 0.f;                                // nothing behind the last row
+    float top = 0.f, coef = 0.f, share = 0.f;                   // nothing behind the last row
     if (gridDim.x == 1) {
       float m = -INFINITY, s = 0.f;
       if (i < min(i1, rows))
@@ -162,9 +166,9 @@ template <int PLANES> __global__ __launch_bounds__(256) void softmax_grad_kernel
         const float n = __shfl_xor(m, o, 64), t = __shfl_xor(s, o, 64);
         join_exp(m, s, n, t);
       }
-      if ((threadIdx.x & 3) == 0 && i < min(i1, rows)) row_end(g.row, i, m, s, lse, coef);
-    } else if (i < min(i1, rows)) { lse = g.row.lse[i]; coef = g.row.coef[i]; }
-    if ((threadIdx.x & 3) == 0) { row_lse[r] = lse; row_coef[r] = coef; }
+      if ((threadIdx.x & 3) == 0 && i < min(i1, rows)) row_end(g.row, i, m, s, top, coef, share);
+    } else if (i < min(i1, rows)) { top = g.row.top[i]; coef = g.row.coef[i]; share = g.row.share[i]; }
+    if ((threadIdx.x & 3) == 0) { row_top[r] = top; row_coef[r] = coef; row_share[r] = share; }
   }
   __syncthreads();
   if (c >= g.ldg) return;
@@ -173,14 +177,14 @@ template <int PLANES> __global__ __launch_bounds__(256) void softmax_grad_kernel
   for (int first = i0; first < i1; first += AHEAD) {
     Raw8<float> z[PLANES ? AHEAD : 1];
     Raw8<uint16_t> q16[PLANES ? 1 : AHEAD];
-    float lse[AHEAD], k[AHEAD], top[AHEAD];
+    float m[AHEAD], k[AHEAD], share[AHEAD], top[AHEAD];      // top: of the span
     int64_t t[AHEAD];
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
       const int i = min(first + a, i1 - 1);
       const int64_t at = (int64_t)i * g.ldg + c;
       const bool there = i < rows;
-      lse[a] = row_lse[i - i0]; k[a] = row_coef[i - i0]; t[a] = (there ? g.row.targets[i] : 0) - c;
+      m[a] = row_top[i - i0]; k[a] = row_coef[i - i0]; share[a] = row_share[i - i0]; t[a] = (there ? g.row.targets[i] : 0) - c;
       if constexpr (PLANES == 0) { q16[a] = raw_load8(g.out + at, 0, 8); top[a] = there ? g.row.stats[span + i].x : 0.f; }
       else z[a] = raw_load8(g.z + at, 0, 8);
     }
@@ -189,7 +193,7 @@ template <int PLANES> __global__ __launch_bounds__(256) void softmax_grad_kernel
       if (first + a >= i1) break;
       f32x8 p;
       if constexpr (PLANES == 0) {
-        const float from = (top[a] - lse[a]) * LOG2_E;
+        const float from = (top[a] - m[a]) * LOG2_E;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const uint32_t q = (q16[a].u[0][e >> 1] >> (16 * (e & 1))) & 0xffffu;
@@ -198,13 +202,13 @@ template <int PLANES> __global__ __launch_bounds__(256) void softmax_grad_kernel
       } else {
         p = expand8(z[a]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p.v[e] = expf(p.v[e] - lse[a]);
+        for (int e = 0; e < 8; ++e) p.v[e] = expf(p.v[e] - m[a]);
       }
       uint16_t q[8][OUT];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float x = 0.f;
-        if (k[a] != 0.f && c + e < classes && lse[a] != -INFINITY) x = k[a] * (p.v[e] - (t[a] == e ? 1.f : 0.f));
+        if (k[a] != 0.f && c + e < classes) x = fmaf(share[a], p.v[e], t[a] == e ? -k[a] : 0.f);
         sum.v[e] += x;
         bf16_planes_of<OUT>(x, q[e]);
       }

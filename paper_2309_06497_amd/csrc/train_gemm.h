@@ -61,8 +61,8 @@ struct TrainGemmArgs {
   const float *bias; const int64_t *targets;
   float2 *stats; int64_t stats_ld;         // [span][row]
   float *target_z;
-  // END_GRAD, from the statistics of a first product: coef (exp(z - lse) - [target]) as bf16 planes
-  const float *lse, *coef; int64_t c_plane; int32_t c_planes;
+  // END_GRAD, from the statistics of a first product: share exp(z - top) - coef [target] as bf16 planes
+  const float *top, *coef, *share; int64_t c_plane; int32_t c_planes;
 };
 
 typedef float train_f32x16 __attribute__((ext_vector_type(16)));
@@ -283,14 +283,14 @@ __device__ __forceinline__ void train_gemm_tile(const TrainGemmArgs &g, int bloc
   // the rows' targets in this span (-1: elsewhere), all asked for at once
   [[maybe_unused]] const int colw = col0 + wn * SPAN, roww = row0 + wm * SPAN;
   [[maybe_unused]] int target_at[TI];
-  [[maybe_unused]] float row_lse[TI], row_coef[TI];
+  [[maybe_unused]] float row_top[TI], row_coef[TI], row_share[TI];
   if constexpr (END != END_PLAIN) {
 #pragma unroll
     for (int i = 0; i < TI; ++i) {
       const int row = min(roww + 32 * i + (lane & 31), g.M - 1);
       const int64_t t = g.targets[row] - colw;
       target_at[i] = t >= 0 && t < SPAN && colw + t < g.N ? (int)t : -1;
-      if constexpr (END == END_GRAD) { row_lse[i] = g.lse[row]; row_coef[i] = g.coef[row]; }
+      if constexpr (END == END_GRAD) { row_top[i] = g.top[row]; row_coef[i] = g.coef[row]; row_share[i] = g.share[row]; }
     }
   }
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -364,14 +364,14 @@ __device__ __forceinline__ void train_gemm_tile(const TrainGemmArgs &g, int bloc
           }
       }
       if constexpr (END == END_GRAD) {
-        const float lse = row_lse[i], k = row < g.M && lse != -INFINITY ? row_coef[i] : 0.f;
+        const float top = row_top[i], share = row_share[i], k = row < g.M ? row_coef[i] : 0.f;
         const int at = target_at[i] - 4 * half;
 #pragma unroll
         for (int j = 0; j < TI; ++j)
 #pragma unroll
           for (int v = 0; v < 16; ++v) {
-            const float p = __builtin_amdgcn_exp2f((acc[i][j][v] - lse) * LOG2_E);
-            acc[i][j][v] = k != 0.f ? k * (at == 32 * j + 8 * (v >> 2) + (v & 3) ? p - 1.f : p) : 0.f;
+            const float p = __builtin_amdgcn_exp2f((acc[i][j][v] - top) * LOG2_E);
+            acc[i][j][v] = k != 0.f ? fmaf(share, p, at == 32 * j + 8 * (v >> 2) + (v & 3) ? -k : 0.f) : 0.f;
           }
         stage(i);
         put(i, [&](int r, int64_t out) {

@@ -383,7 +383,7 @@ struct CrossEntropyPlan {
   bool sum = false;          // bf16 dw of several pieces: summed in scratch
   size_t bytes = 0;
   uint16_t *xp, *wp, *g;
-  float *z, *lse, *coef, *target_z, *acc, *sums, *part;
+  float *z, *top, *coef, *share, *target_z, *acc, *sums, *part;
   float2 *stats;
   int grad_planes() const { return std::max(planes, 1); }
   // the logits' product over n rows: where it stores float32 ones, 0.4 us more for the end of a tile of 128 (1999 x 1000 x 50001: 354 us
@@ -428,7 +428,7 @@ int cross_entropy_plan(const shampoo_cross_entropy &c, void *workspace, CrossEnt
   p.ranges = (p.piece + p.range_rows - 1) / p.range_rows;
   Arena a(workspace);
   p.xp = p.x.take(a); p.wp = p.w.take(a);
-  p.lse = a.take<float>(p.piece); p.coef = a.take<float>(p.piece); p.target_z = a.take<float>(p.piece);
+  p.top = a.take<float>(p.piece); p.coef = a.take<float>(p.piece); p.share = a.take<float>(p.piece); p.target_z = a.take<float>(p.piece);
   p.stats = a.take<float2>((size_t)p.spans * p.piece);
   if (c.gradients) {
     if (p.planes && !p.twice) p.z = a.take<float>((size_t)p.piece * p.ldz);
@@ -652,7 +652,7 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
       if (end == END_LOGITS_U16) gemm_launch<END_LOGITS_U16>(z, cut, xk.lie, wo.lie, s); else gemm_launch<END_LOGITS>(z, cut, xk.lie, wo.lie, s);
     }
     HIP_TRY(hipGetLastError());
-    const RowLossArgs r = {p.stats, p.piece, p.target_z, targets + i0, weight ? weight + i0 : nullptr, power, p.lse, p.coef, loss + i0,
+    const RowLossArgs r = {p.stats, p.piece, p.target_z, targets + i0, weight ? weight + i0 : nullptr, power, p.top, p.coef, p.share, loss + i0,
                            (int32_t)n, (int32_t)v, (int32_t)((v + span - 1) / span)};
     const dim3 grid((unsigned)((p.ldz / 8 + 255) / 256), (unsigned)((round_up(n, TG_BK) + p.range_rows - 1) / p.range_rows));   // zeros behind the last row
     const bool wanted = dx || dw || dbias;
@@ -662,7 +662,7 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
     }
     if (!wanted) continue;
     if (p.twice) {
-      z.c = p.g; z.lse = p.lse; z.coef = p.coef; z.c_plane = p.piece * p.ldz; z.c_planes = p.planes;
+      z.c = p.g; z.top = p.top; z.coef = p.coef; z.share = p.share; z.c_plane = p.piece * p.ldz; z.c_planes = p.planes;
       gemm_launch<END_GRAD>(z, cut, xk.lie, wo.lie, s);
     } else {
       const SoftmaxGradArgs q = {r, p.z, p.ldz, span, p.g, p.piece * p.ldz, dbias ? p.sums + k * p.ranges * v : nullptr, (int32_t)p.range_rows, alpha};

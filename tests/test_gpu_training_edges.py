@@ -1,0 +1,105 @@
+"""The operators of a training pass at the ends of their ranges, against float64: logits far from zero, values that bf16 does not reach,
+rows in several pieces, strided outputs, results in place.
+
+e = 2^-24 is the rounding of float32, u = 2^-8 that of bf16.  Bars are derived at each test."""
+import math
+
+import pytest
+
+from paper_2309_06497_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -8
+KINDS = [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")]
+
+
+def torch_():
+    import torch
+    return torch
+
+
+def gen(seed):
+    g = torch_().Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def types(kind):
+    torch = torch_()
+    return [{"bf16": torch.bfloat16, "f32": torch.float32}[k] for k in kind]
+
+
+def rel(got, want):
+    torch = torch_()
+    return float(torch.linalg.vector_norm(got.double() - want) / torch.linalg.vector_norm(want))
+
+
+# ----------------------------------------------------------------------------
+# Logits far from zero
+# ----------------------------------------------------------------------------
+def quarters(g, *shape):
+    """-2/4 ... 2/4: products are sixteenths, which a float32 sum holds exactly beside 2^18"""
+    torch = torch_()
+    return torch.randint(-2, 3, shape, generator=g, device="cuda") * 0.25
+
+
+def softmax_gradients(z, x, w, t):
+    torch = torch_()
+    z = z - z.amax(1, keepdim=True)
+    total = torch.exp(z).sum(1, keepdim=True)
+    i = torch.arange(z.shape[0], device="cuda")
+    loss = torch.log(total)[:, 0] - z[i, t]
+    g = torch.exp(z) / total
+    g[i, t] -= 1.0
+    return loss, g @ w, g.t() @ x, g.sum(0)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("by_bias", [False, True])
+@pytest.mark.parametrize("offset", [2.0 ** 13, -2.0 ** 13, 2.0 ** 18])
+@pytest.mark.parametrize("n,d,v", [(40, 64, 300), (200, 1024, 300), (70, 256, 2500), (600, 712, 16500)])
+def test_a_common_offset_of_the_logits_changes_nothing(n, d, v, offset, by_bias, kind):
+    """Logits are exact here (sixteenths beside at most 2^18: 23 bits), so what separates the result from the definition is what it is without an
+    offset: exponents of |z - largest| < 64 off by 64 e, sums of exponentials by less than that again: 2^-17 in a loss and
+    in float32 gradients; 3 u in bf16 ones."""
+    torch = torch_()
+    dt, grad = types(kind)
+    g = gen(n + v)
+    x, w = quarters(g, n, d), quarters(g, v, d)
+    bias = None
+    if by_bias:
+        bias = torch.full((v,), offset, device="cuda")
+    else:
+        x[:, 0], w[:, 0] = math.copysign(2.0 ** 7, offset), abs(offset) / 2.0 ** 7
+    t = torch.randint(0, v, (n,), generator=g, device="cuda")
+    z = x.double() @ w.double().t() + (offset if by_bias else 0.0)
+    loss64, dx64, dw64, db64 = softmax_gradients(z, x.double(), w.double(), t)
+    loss, dx, dw, db = B.shampoo_linear_cross_entropy(x.to(dt), w.to(dt), t, bias=bias, grad_dtype=grad)
+    alone = B.shampoo_linear_cross_entropy(x.to(dt), w.to(dt), t, bias=bias, gradients=False)
+    for l in (loss, alone):
+        assert float((l.double() - loss64).abs().max()) <= 2.0 ** -17 * max(1.0, float(loss64.max()))
+    if not by_bias:        # the common feature's gradient: a sum of p - [t] over the classes, 0, times the offset
+        dx, dx64 = dx[:, 1:], dx64[:, 1:]
+    assert rel(dx, dx64) <= (3 * U if kind[0] == "bf16" else 2.0 ** -16)
+    assert rel(dw, dw64) <= (3 * U if kind[1] == "bf16" else 2.0 ** -16)
+    if by_bias:
+        assert rel(db, db64) <= 2.0 ** -16
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,d,v", [(40, 64, 300), (200, 1024, 300), (600, 64, 16500)])
+def test_the_softmax_of_equal_logits_however_low(n, d, v, kind):
+    """A bias of the type's lowest value leaves nothing of x w^T: probabilities of 1 / classes, a loss of log(classes)."""
+    torch = torch_()
+    dt, grad = types(kind)
+    g = gen(12)
+    x, w = torch.randn((n, d), generator=g, device="cuda").to(dt), (torch.randn((v, d), generator=g, device="cuda") * 0.1).to(dt)
+    t = torch.randint(0, v, (n,), generator=g, device="cuda")
+    for low in (torch.finfo(torch.float32).min, -3.0e20):
+        bias = torch.full((v,), low, device="cuda")
+        loss64, dx64, dw64, db64 = softmax_gradients(torch.zeros((n, v), dtype=torch.float64, device="cuda"), x.double(), w.double(), t)
+        loss, dx, dw, db = B.shampoo_linear_cross_entropy(x, w, t, bias=bias, grad_dtype=grad)
+        assert float((loss.double() - loss64).abs().max()) <= 2.0 ** -20 * math.log(v)
+        assert rel(dx, dx64) <= (3 * U if kind[0] == "bf16" else 2.0 ** -16)
+        assert rel(dw, dw64) <= (3 * U if kind[1] == "bf16" else 2.0 ** -16)
+        assert rel(db, db64) <= 2.0 ** -16
