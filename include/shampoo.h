@@ -442,7 +442,8 @@ int shampoo_checkpoint_activation_grad(const void *packed, size_t packed_bytes, 
  *   dW = a(x)^T dy (SHAMPOO_IN_OUT; SHAMPOO_OUT_IN: transposed),  db = column sums of dy (float32; NULL: not wanted).
  * dtype: of dy (16-byte aligned, else SHAMPOO_ERR_UNSUPPORTED).  Float32 dy: products to float32 accuracy, dw float32.
  * bf16 dy: x and dy enter as they are; a(x), where an activation is given, rounded to bf16 for bf16 dw, with float32 accuracy for
- * float32 dw.  in <= 65536, out <= 4194304.
+ * float32 dw.  An infinity in float32 dy reaches its results as in the sum; in bf16 dy it makes them infinite or NaN.
+ * in <= 65536, out <= 4194304.
  */
 size_t shampoo_checkpoint_weight_grad_workspace_bytes(int64_t rows, int32_t in, int32_t out, int32_t activation, int32_t dtype,
                                                       int64_t lddy, int32_t grad_dtype, int32_t want_bias);

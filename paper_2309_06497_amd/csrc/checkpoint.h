@@ -180,7 +180,9 @@ template <int FROM, int PLANES> __device__ __forceinline__ void planes_piece(con
   }
   uint16_t q[8][PLANES];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) bf16_planes_of<PLANES>(x.v[e], q[e]);
+  for (int e = 0; e < 8; ++e) {
+    if constexpr (FROM == FROM_F32) bf16_planes_of_any(x.v[e], q[e]); else bf16_planes_of<PLANES>(x.v[e], q[e]);
+  }
 #pragma unroll
   for (int t = 0; t < PLANES; ++t) {
     uint4 w;

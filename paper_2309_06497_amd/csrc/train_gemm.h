@@ -6,7 +6,7 @@
 // products (s, t) are all that float32 accuracy needs, smallest first: one loop over k behind the other.  An operand lies along
 // k (ptr[row * ld + k]) or along rows (ptr[k * ld + row]).  Contract, which the host keeps: 16-byte aligned, ld % 8 == 0; along k
 // readable up to the next multiple of 64 of K and zero there, along rows readable up to a multiple of 8 of the rows; and where both
-// lie along rows, one of them has zeros for k from K to the next multiple of 64.
+// lie along rows, one of them has zeros for k from K to the next multiple of 64 (both: an infinity in the other's last k meets no zero).
 //
 // Tile of 64 TI x 64 TI per workgroup of four wavefronts, 32 TI x 32 TI each as TI x TI tiles of v_mfma_f32_32x32x16_bf16.  TI = 4:
 // 256 accumulator registers, one wavefront per SIMD; 8 KB of operands from LDS per 16 products of 32 cycles, half of what LDS
@@ -48,7 +48,7 @@ struct TrainGemmArgs {
   int64_t lda, ldb, a_plane, b_plane;      // elements
   int32_t M, N, K;
   int32_t products;                        // pairs of planes
-  int32_t padded;                          // both along rows: 1 where A, 2 where B has the zeros
+  int32_t padded;                          // both along rows: 1: A has the zeros, 2: B
   uint32_t plane_a, plane_b;               // four bits each: the planes of product i
   int32_t tiles_m, tiles_n, splits, per_split;   // slabs of the whole sequence (products x ceil(K / 64)) per split
   int32_t tile0, tiles;                    // this launch's: tile0 ... tile0 + tiles - 1
@@ -185,8 +185,8 @@ __device__ __forceinline__ void train_gemm_tile(const TrainGemmArgs &g, int bloc
     in_a = uniform_ptr(corner_a + pa * g.a_plane + in_s * step_a);
     in_b = uniform_ptr(corner_b + pb * g.b_plane + in_s * step_b);
     in_k = g.K - in_s * TG_BK;
-    sa.offsets(g.lda, g.M - row0, g.padded == 1 ? TG_BK : in_k, wave, lane);
-    sb.offsets(g.ldb, g.N - col0, g.padded == 2 ? TG_BK : in_k, wave, lane);
+    sa.offsets(g.lda, g.M - row0, g.padded & 1 ? TG_BK : in_k, wave, lane);
+    sb.offsets(g.ldb, g.N - col0, g.padded & 2 ? TG_BK : in_k, wave, lane);
   };
   auto next_slab = [&]() {
     if (--in_left > 0) {

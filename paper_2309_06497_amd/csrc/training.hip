@@ -246,7 +246,7 @@ void gemm_args(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t
   g.tiles_m = (int32_t)((M + 64 * cut.ti - 1) / (64 * cut.ti)); g.tiles_n = (int32_t)((N + 64 * cut.ti - 1) / (64 * cut.ti));
   g.splits = cut.splits; g.per_split = cut.per_split;
   g.tiles = g.tiles_m * g.tiles_n;
-  g.padded = a.padded ? 1 : b.padded ? 2 : 0;
+  g.padded = (a.padded ? 1 : 0) | (b.padded ? 2 : 0);
   g.alpha = 1.f;
 }
 // where C goes: with several splits their results lie one behind the other in `part`
@@ -356,18 +356,20 @@ int gemm_pair(const Operand &a, const Operand &b, const Product &f, const Result
 // slabs' end: `along`, 64 where the columns are k in some product, otherwise 8).
 struct Source {
   int32_t dtype; int64_t rows, cols, ld; int along;
+  bool zeros = false;        // a copy has them behind its last row, to the next multiple of 64
   bool copy() const { return dtype != SHAMPOO_GRAD_BF16 || cols % along != 0 || ld % 8 != 0 || ld > MAX_LD; }
   int planes() const { return dtype == SHAMPOO_GRAD_F32 ? 3 : 1; }
   int64_t ldp() const { return round_up(cols, 64); }
-  uint16_t *take(Arena &a) const { return copy() ? a.take<uint16_t>((size_t)planes() * rows * ldp()) : nullptr; }
+  int64_t held() const { return zeros ? round_up(rows, TG_BK) : rows; }
+  uint16_t *take(Arena &a) const { return copy() ? a.take<uint16_t>((size_t)planes() * held() * ldp()) : nullptr; }
   Operand operand(const void *p, const uint16_t *scratch, int lie) const {
     if (!copy()) return {static_cast<const uint16_t *>(p), ld, 0, 1, lie};
-    return {scratch, ldp(), rows * ldp(), planes(), lie};
+    return {scratch, ldp(), held() * ldp(), planes(), lie, zeros};
   }
   PlanesTask task(const void *p, uint16_t *scratch) const {
     PlanesTask t = {};
-    t.from = dtype == SHAMPOO_GRAD_F32 ? FROM_F32 : FROM_BF16; t.planes = planes(); t.rows = rows;
-    t.g.rows = rows; t.g.x = p; t.g.ldx = ld; t.g.out = scratch; t.g.plane = rows * ldp(); t.g.ld = ldp(); t.g.cols = (int32_t)cols;
+    t.from = dtype == SHAMPOO_GRAD_F32 ? FROM_F32 : FROM_BF16; t.planes = planes(); t.rows = held();
+    t.g.rows = rows; t.g.x = p; t.g.ldx = ld; t.g.out = scratch; t.g.plane = held() * ldp(); t.g.ld = ldp(); t.g.cols = (int32_t)cols;
     return t;
   }
 };
@@ -469,7 +471,7 @@ int weight_grad_plan(int64_t rows, int32_t in, int32_t out, int32_t activation, 
     return SHAMPOO_ERR_UNSUPPORTED;
   if (!dtype_ok(dtype) || !dtype_ok(grad_dtype) || activation < ACT_NONE || activation > ACT_SILU) return SHAMPOO_ERR_HYPER;
   if (dtype == SHAMPOO_GRAD_F32 && grad_dtype != SHAMPOO_GRAD_F32) return SHAMPOO_ERR_HYPER;
-  p.dy = {dtype, rows, out, lddy, 8};
+  p.dy = {dtype, rows, out, lddy, 8, true};
   // a code times its scale is a bf16 value, and so is its ReLU; other activations take three planes for a float32 result
   p.planes = activation == ACT_NONE || activation == ACT_RELU || grad_dtype != SHAMPOO_GRAD_F32 ? 1 : 3;
   p.ldp = round_up(in, 64);

@@ -72,13 +72,27 @@ template <typename T> __device__ __forceinline__ void store8(T *row, int c, int 
   }
 }
 
-// x = sum of planes, each bf16: the first rounds x, the others what that leaves (three hold all 24 bits)
+// x = sum of planes, each bf16: the first rounds x, the others what that leaves (three hold all 24 bits).  |x| < 3.396e38, from where on
+// bf16 rounds to infinity.
 template <int PLANES> __device__ __forceinline__ void bf16_planes_of(float x, uint16_t (&p)[PLANES]) {
 #pragma unroll
   for (int t = 0; t < PLANES; ++t) {
     p[t] = bf16_bits(x);
     if (t + 1 < PLANES) x -= bf16_value(p[t]);
   }
+}
+
+// The same of any float32.  The largest ones begin with bf16's largest.  An infinity is the third plane, behind a one of its sign: it meets the
+// other operand's first plane alone (plane_pairs), so that a product is infinite with the sign of the two, where infinity in the first plane would meet
+// zeros, and second planes of either sign.
+__device__ __forceinline__ void bf16_planes_of_any(float x, uint16_t (&p)[3]) {
+  constexpr float MOST = 3.3895313892515355e38f;
+  const bool infinite = fabsf(x) == INFINITY;
+  float rest = infinite ? copysignf(1.f, x) : x;
+  p[0] = bf16_bits(fminf(fmaxf(rest, -MOST), MOST));
+  rest -= bf16_value(p[0]);                        // NaN: there from here on
+  p[1] = bf16_bits(rest);
+  p[2] = bf16_bits(infinite ? x : rest - bf16_value(p[1]));
 }
 
 }  // namespace shampoo

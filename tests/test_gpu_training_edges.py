@@ -103,3 +103,55 @@ def test_the_softmax_of_equal_logits_however_low(n, d, v, kind):
         assert rel(dx, dx64) <= (3 * U if kind[0] == "bf16" else 2.0 ** -16)
         assert rel(dw, dw64) <= (3 * U if kind[1] == "bf16" else 2.0 ** -16)
         assert rel(db, db64) <= 2.0 ** -16
+
+
+# ----------------------------------------------------------------------------
+# Float32 values that bf16 does not reach
+# ----------------------------------------------------------------------------
+LARGEST = 3.4028234663852886e38
+
+
+@pytest.mark.parametrize("out_in", [False, True])
+@pytest.mark.parametrize("act", [B.ACT_NONE, B.ACT_SILU])
+@pytest.mark.parametrize("n", [1, 64, 70, 999])
+def test_weight_gradient_of_the_largest_and_of_infinite_float32_values(n, act, out_in):
+    """dy's columns: ordinary, the largest float32, an infinity, two of one sign, two of different sign; in the last row too.  A
+    result is what the sum is: within 2^-18 of the sum of its terms' sizes (float32 sums of n terms), infinite, or NaN."""
+    torch = torch_()
+    g = gen(n)
+    x = torch.randint(0, 2, (n, 40), generator=g, device="cuda") * 0.25 + 0.25
+    x *= torch.randint(0, 2, (n, 40), generator=g, device="cuda") * 2 - 1              # codes of 32 and 64 steps, or 64 and 128: held exactly
+    dy = torch.randn((n, 9), generator=g, device="cuda")
+    k = torch.tensor(sorted({0, n // 2, n - 1}), device="cuda")
+    dy[k[-1], 1], dy[k[0], 2], dy[k[-1], 3], dy[k[0], 4], dy[k[-1], 5] = LARGEST, -LARGEST, math.inf, -math.inf, -math.inf
+    dy[k[0], 6] = dy[k[-1], 6] = math.inf
+    dy[k[0], 7], dy[k[-1], 7] = -math.inf, math.inf
+    dy[k[-1], 8] = 3.397e38                                                           # rounds to an infinity of bf16
+    c = B.shampoo_checkpoint_pack(x)
+    assert torch.equal(B.shampoo_checkpoint_unpack(c), x)
+    a = x.double() if act == B.ACT_NONE else x.double() * torch.sigmoid(x.double())
+    want = (a[:, :, None] * dy.double()[:, None, :]).sum(0)
+    size = (a[:, :, None] * dy.double()[:, None, :]).abs().sum(0)
+    dw, db = B.shampoo_checkpoint_weight_grad(c, dy, act, out_in=out_in, bias=True)
+    dw = dw.t() if out_in else dw
+    fin = torch.isfinite(want)
+    assert torch.equal(torch.isnan(dw), torch.isnan(want))
+    assert torch.equal(dw[torch.isinf(want)].double(), want[torch.isinf(want)])
+    assert bool(((dw.double() - want).abs()[fin] <= 2.0 ** -18 * size[fin]).all())
+    want = dy.double().sum(0)
+    assert torch.equal(torch.isnan(db), torch.isnan(want)) and torch.equal(db[torch.isinf(want)].double(), want[torch.isinf(want)])
+
+
+def test_head_with_the_largest_float32_weight():
+    torch = torch_()
+    g = gen(4)
+    for n, d, v in ((40, 64, 300), (90, 200, 2500)):
+        x, w = torch.randn((n, d), generator=g, device="cuda"), torch.randn((v, d), generator=g, device="cuda") * 0.1
+        x[:, 0], w[5, 0] = 2.0 ** -126, LARGEST                                         # 4 in a logit
+        t = torch.randint(0, v, (n,), generator=g, device="cuda")
+        loss64, dx64, dw64, _ = softmax_gradients(x.double() @ w.double().t(), x.double(), w.double(), t)
+        loss, dx, dw, _ = B.shampoo_linear_cross_entropy(x, w, t)
+        assert float((loss.double() - loss64).abs().max()) <= 2.0 ** -17 * float(loss64.max())
+        assert rel(dw, dw64) <= 2.0 ** -16
+        for part in (slice(0, 1), slice(1, d)):
+            assert rel(dx[:, part], dx64[:, part]) <= 2.0 ** -16
