@@ -36,6 +36,7 @@ struct ResidualNormArgs {
   float *dgate;                                        // written here where a team has whole groups
   float *partial;                                      // [teams][5][cols]: dgate, dw_post, dw_pre, db_post, db_pre
   int64_t rows, group_rows, chunk_rows, teams;         // rows per gate, per team of the backward pass
+  int64_t row0;                                        // forward: this launch's first row
   int32_t chunks_per_group;                            // 0: a team has whole groups
   int32_t cols, post, pre;
   float epsilon, alpha;
@@ -114,7 +115,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void residual_norm_forward_k
   constexpr int TEAMS = TPR > 256 ? 1 : 256 / TPR;
   __shared__ float red[4 * NORM_SLOT];
   const RowPieces<TPR, NJ> at = {(int)threadIdx.x % TPR, g.cols};
-  const int64_t i = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TPR;
+  const int64_t i = g.row0 + (int64_t)blockIdx.x * TEAMS + threadIdx.x / TPR;
   if (i >= g.rows) return;                             // a whole team
   f32x8 f[NJ], r[NJ];
   const T *pr = static_cast<const T *>(g.r) + i * g.ldr, *pf = static_cast<const T *>(g.f) + i * g.ldf;

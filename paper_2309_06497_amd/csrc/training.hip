@@ -564,13 +564,19 @@ template <typename F> void norm_backward_variant(int32_t cols, F &&launch) {
   else VARIANT(512, 4);
 #undef VARIANT
 }
-template <typename T> int launch_norm_forward(const ResidualNormArgs &g, hipStream_t s) {
+// at most 2^22 workgroups in a launch, whose threads have 32 bits
+template <typename T> int launch_norm_forward(ResidualNormArgs g, hipStream_t s) {
+  int rc = SHAMPOO_OK;
   norm_forward_variant(g.cols, [&](auto tpr, auto nj) {
-    constexpr int TPR = decltype(tpr)::value, TEAMS = TPR > 256 ? 1 : 256 / TPR;
-    residual_norm_forward_kernel<T, TPR, decltype(nj)::value><<<dim3((unsigned)((g.rows + TEAMS - 1) / TEAMS)), TEAMS * TPR, 0, s>>>(g);
+    constexpr int TPR = decltype(tpr)::value;
+    constexpr int64_t TEAMS = TPR > 256 ? 1 : 256 / TPR, AT_ONCE = TEAMS << 22;
+    for (; g.row0 < g.rows && rc == SHAMPOO_OK; g.row0 += AT_ONCE) {
+      const int64_t rows = std::min(AT_ONCE, g.rows - g.row0);
+      residual_norm_forward_kernel<T, TPR, decltype(nj)::value><<<dim3((unsigned)((rows + TEAMS - 1) / TEAMS)), TEAMS * TPR, 0, s>>>(g);
+      if (hipGetLastError() != hipSuccess) rc = SHAMPOO_ERR_HIP;
+    }
   });
-  HIP_TRY(hipGetLastError());
-  return SHAMPOO_OK;
+  return rc;
 }
 template <typename T> int launch_norm_backward(const ResidualNormArgs &g, bool bias, hipStream_t s) {
   norm_backward_variant(g.cols, [&](auto tpr, auto nj) {

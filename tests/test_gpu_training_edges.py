@@ -155,3 +155,25 @@ def test_head_with_the_largest_float32_weight():
         assert rel(dw, dw64) <= 2.0 ** -16
         for part in (slice(0, 1), slice(1, d)):
             assert rel(dx[:, part], dx64[:, part]) <= 2.0 ** -16
+
+
+# ----------------------------------------------------------------------------
+# Many rows
+# ----------------------------------------------------------------------------
+def test_residual_norm_forward_in_several_launches():
+    """2^22 workgroups of four rows a launch: the rows around each of their ends, and the last ones."""
+    torch = torch_()
+    g = gen(5)
+    n, d = 2 * (1 << 24) + 5, 8
+    r, f = torch.randn((n, d), generator=g, device="cuda").bfloat16(), torch.randn((n, d), generator=g, device="cuda").bfloat16()
+    w = torch.rand((d,), generator=g, device="cuda") + 0.5
+    r_out, h, r8, f8 = B.shampoo_residual_norm_forward(r, f, post=B.NORM_NONE, pre=B.NORM_RMS, w_pre=w, scale=0.5, checkpoint=True)
+    held = [B.shampoo_checkpoint_unpack(c) for c in (r8, f8)]
+    for k in range(0, n, 1 << 22):
+        part = slice(k, min(n, k + (1 << 22)))
+        out = r[part].double() + 0.5 * f[part].double()
+        norm = out / torch.sqrt(out.square().mean(1, keepdim=True) + 1e-5) * w.double()
+        assert float((r_out[part].double() - out).abs().max()) <= U * float(out.abs().max())
+        assert float((h[part].double() - norm).abs().max()) <= U * float(norm.abs().max())
+        for x, y in zip((r, f), held):
+            assert float((x[part].double() - y[part].double()).abs().max()) <= float(x[part].abs().max()) / 127.5

@@ -1,0 +1,33 @@
+"""The operators of a training pass at the largest sizes that their argument checks admit, against a runtime that launches nothing (and
+refuses launches of 2^32 threads and more along a dimension, as HIP does), and their workspaces there."""
+import ctypes
+
+import pytest
+
+import host_hip
+from paper_2309_06497_amd import binding as B
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    return host_hip.build(str(tmp_path_factory.mktemp("hip")))
+
+
+ROWS = r"""
+P = ctypes.c_void_p(1 << 40)
+S = ctypes.c_void_p(STREAM)
+for rows, cols in ((1, 1), (1 << 26, 64), ((1 << 24) + 1, 1500), (1 << 24, 4096), ((1 << 23) + 3, 16384), ((1 << 31) - 1, 1), ((1 << 31) - 1, 16384)):
+    k = B.ResidualNorm(rows, cols, 1, 1, 1, 0, 1e-5, 1.0, 1 << 40, None, None, 1 << 40, None)
+    reset()
+    rc = L.shampoo_residual_norm_forward(ctypes.byref(k), P, cols, P, cols, P, cols, P, cols, None, None, 0, S)
+    each = 4 if cols <= 2048 else 1                # rows of a workgroup
+    print(rows, cols, rc, sum(e.a for e in launches("residual_norm_forward")) * each)
+"""
+
+
+def test_residual_norm_forward_of_as_many_rows_as_it_admits(lib):
+    seen = [list(map(int, line.split())) for line in host_hip.run(lib, ROWS) if line]
+    assert len(seen) == 7
+    for rows, cols, rc, covered in seen:
+        assert rc == 0, (rows, cols, rc)
+        assert rows <= covered < rows + 4, (rows, cols, covered)
