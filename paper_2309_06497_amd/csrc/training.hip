@@ -27,6 +27,7 @@ constexpr size_t PLANE_BYTES = (size_t)1 << 30;
 constexpr int LOGIT_SPLITS = 64;
 constexpr int64_t PIECE_ROWS = 256, MAX_PIECE_ROWS = 1 << 21;   // rows of a piece are a multiple of the first (grids: at most 65535 ranges of 64)
 constexpr int64_t MAX_TILES = 1 << 23;                     // of a product: threads of a launch have 32 bits
+constexpr int64_t MAX_SUM_BLOCKS = 1 << 22;                // workgroups of column sums, beside as many for planes
 
 inline size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
 inline int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
@@ -479,7 +480,9 @@ int weight_grad_plan(int64_t rows, int32_t in, int32_t out, int32_t activation, 
                               std::max<int64_t>(PIECE_ROWS, (int64_t)(PLANE_BYTES / ((size_t)p.ldp * 2 * p.planes)) / PIECE_ROWS * PIECE_ROWS));
   p.pieces = (rows + p.piece - 1) / p.piece;
   p.sum = p.pieces > 1 && grad_dtype == SHAMPOO_GRAD_BF16;
-  p.part_rows = rows <= 128 ? 128 : std::max<int64_t>(64, (rows + 255) / 256);
+  // parts of the rows for the column sums: 256, fewer where those were more than 2^22 workgroups of 64 columns
+  const int64_t most = std::min<int64_t>(256, MAX_SUM_BLOCKS / (((int64_t)out + 63) / 64));
+  p.part_rows = rows <= 128 ? 128 : std::max<int64_t>(64, (rows + most - 1) / most);
   p.parts = std::max<int64_t>(1, (rows + p.part_rows - 1) / p.part_rows);
   Arena a(workspace);
   p.xp = a.take<uint16_t>((size_t)p.planes * p.piece * p.ldp);

@@ -31,3 +31,21 @@ def test_residual_norm_forward_of_as_many_rows_as_it_admits(lib):
     for rows, cols, rc, covered in seen:
         assert rc == 0, (rows, cols, rc)
         assert rows <= covered < rows + 4, (rows, cols, covered)
+
+
+BIAS = r"""
+P = ctypes.c_void_p(1 << 40)
+S = ctypes.c_void_p(STREAM)
+for rows, n, out, act, dtype in ((16384, 8, 1 << 22, 0, 1), (16384, 40, (1 << 22) - 3, 3, 0), (1 << 20, 8, 1 << 22, 0, 1), (1 << 20, 8, 1 << 20, 0, 1), (16384, 8, 3000000, 2, 1),
+                                  ((1 << 31) - 1, 1, 1, 0, 1), (8192, 8192, 2048, 0, 1)):
+    b = L.shampoo_checkpoint_bytes(rows, n)
+    ws = L.shampoo_checkpoint_weight_grad_workspace_bytes(rows, n, out, act, dtype, out, dtype, 1)
+    reset()
+    rc = L.shampoo_checkpoint_weight_grad(P, b, rows, n, act, P, dtype, out, out, P, dtype, 0, n, P, P, ws, S)
+    print(rows, out, rc)
+"""
+
+
+def test_bias_gradients_of_as_many_outputs_as_it_admits(lib):
+    seen = [list(map(int, line.split())) for line in host_hip.run(lib, BIAS) if line]
+    assert len(seen) == 7 and all(rc == 0 for _, _, rc in seen), seen
