@@ -413,13 +413,13 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR, NJ == 1 && TPR <= 256 && siz
   }
 }
 
-// Sums over teams or parts: out_k[o][j] = sum over p < parts_k of in_k[o][p][j], k = blockIdx.z, o = blockIdx.y, in an order that
+// Sums over teams or parts: out_k[o][j] = (add: out_k[o][j] +) sum over p < parts_k of in_k[o][p][j], k = blockIdx.z, o = blockIdx.y, in an order that
 // does not depend on the launch.  A workgroup has 64 columns and 16 threads for each.
 constexpr int JOIN_SUMS = 8;
 struct JoinSumsArgs {
   const float *in[JOIN_SUMS]; float *out[JOIN_SUMS]; int32_t parts[JOIN_SUMS];
   int64_t output_stride, part_stride, out_stride;
-  int32_t cols;
+  int32_t cols, add;
 };
 __global__ __launch_bounds__(1024) void join_sums_kernel(const JoinSumsArgs g) {
   __shared__ float part[16][64];
@@ -447,7 +447,8 @@ __global__ __launch_bounds__(1024) void join_sums_kernel(const JoinSumsArgs g) {
   float t = 0.f;
 #pragma unroll
   for (int q = 0; q < 16; ++q) t += part[q][c];
-  g.out[blockIdx.z][blockIdx.y * g.out_stride + j] = t;
+  float *out = g.out[blockIdx.z] + blockIdx.y * g.out_stride + j;
+  *out = g.add ? *out + t : t;
 }
 
 }  // namespace shampoo

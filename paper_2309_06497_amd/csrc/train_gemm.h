@@ -468,7 +468,7 @@ template <int STAGES, int BLIE> __global__ __launch_bounds__(256, STAGES == 2 ? 
 // The results of several splits, float32 [split][rows][cols], added up in an order that does not depend on the launch.  LANES
 // threads share a piece of eight columns where there are many splits, so that their loads are on their way together.
 // Workgroups from `blocks` on add up the rows of `sums` (16 columns each, 16 threads a column), which saves a launch of their own.
-struct RowSums { const float *in; float *out; int32_t parts, cols; };      // [parts][cols]
+struct RowSums { const float *in; float *out; int32_t parts, cols, add; };      // [parts][cols]; add: to what is there
 struct JoinArgs {
   const float *part; int64_t stride; int32_t splits;
   void *c; int64_t ldc; const float *add; int64_t ldadd;
@@ -496,7 +496,7 @@ __device__ __forceinline__ void row_sums(const RowSums &g, int block) {
   float t = 0.f;
 #pragma unroll
   for (int q = 0; q < 16; ++q) t += part[q][c];
-  g.out[j] = t;
+  g.out[j] = g.add ? g.out[j] + t : t;
 }
 template <int LANES> __global__ __launch_bounds__(256) void train_join_kernel(const JoinArgs g) {
   if (blockIdx.x >= g.blocks) { row_sums(g.sums, blockIdx.x - g.blocks); return; }

@@ -145,7 +145,7 @@ int launch_join_sums(JoinSumsArgs g, int count, int64_t outputs, hipStream_t s) 
 // nothing where `out` is null: a join before it has done it
 int launch_row_sums(const RowSums &r, hipStream_t s) {
   JoinSumsArgs g = {};
-  g.in[0] = r.in; g.out[0] = r.out; g.parts[0] = r.parts; g.part_stride = r.cols; g.cols = r.cols;
+  g.in[0] = r.in; g.out[0] = r.out; g.parts[0] = r.parts; g.part_stride = r.cols; g.cols = r.cols; g.add = r.add;
   return launch_join_sums(g, r.out ? 1 : 0, 1, s);
 }
 
@@ -437,7 +437,7 @@ int cross_entropy_plan(const shampoo_cross_entropy &c, void *workspace, CrossEnt
     if (p.planes && !p.twice) p.z = a.take<float>((size_t)p.piece * p.ldz);
     p.g = a.take<uint16_t>((size_t)p.grad_planes() * p.piece * p.ldz);
     if (p.sum) p.acc = a.take<float>((size_t)p.w.rows * p.w.cols);
-    if (c.has_bias) p.sums = a.take<float>((size_t)p.ranges * p.pieces * v);
+    if (c.has_bias) p.sums = a.take<float>((size_t)p.ranges * v);
   }
   size_t part = 0;
   for (int64_t n : {p.piece, c.rows - std::max<int64_t>(0, p.pieces - 1) * p.piece, c.rows}) {      // all pieces, the last one, a single one
@@ -634,14 +634,11 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
   if (p.x.copy() && p.w.copy()) TRY(launch_planes(p.x.task(x, p.xp), p.w.task(w, p.wp), s));
   else if (p.x.copy()) TRY(launch_planes(p.x.task(x, p.xp), s));
   else if (p.w.copy()) TRY(launch_planes(p.w.task(w, p.wp), s));
-  const int64_t last = c->rows - (p.pieces - 1) * p.piece;
-  RowSums bias_sums = {dbias ? p.sums : nullptr, dbias, (int32_t)((p.pieces - 1) * p.ranges + (round_up(last, TG_BK) + p.range_rows - 1) / p.range_rows), (int32_t)v}, none = {};
   // scale = power alpha, alpha in [1, 2); very small ones as they are
   const float power = std::fabs(scale) < 0x1p-100f ? scale : std::copysign(std::ldexp(1.f, std::ilogb(scale)), scale);
   const float alpha = std::fabs(scale) < 0x1p-100f ? 1.f : scale / power;
   for (int64_t k = 0; k < p.pieces; ++k) {
     const int64_t i0 = k * p.piece, n = std::min(p.piece, c->rows - i0);
-    RowSums &sums = k == p.pieces - 1 ? bias_sums : none;      // once all pieces have left theirs
     Operand xk = xo;
     xk.p += i0 * xo.ld;
     const GemmCut cut = p.for_logits(*c, n);
@@ -666,6 +663,7 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
     const RowLossArgs r = {p.stats, p.piece, p.target_z, targets + i0, weight ? weight + i0 : nullptr, power, p.top, p.coef, p.share, loss + i0,
                            (int32_t)n, (int32_t)v, (int32_t)((v + span - 1) / span)};
     const dim3 grid((unsigned)((p.ldz / 8 + 255) / 256), (unsigned)((round_up(n, TG_BK) + p.range_rows - 1) / p.range_rows));   // zeros behind the last row
+    RowSums sums = {p.sums, dbias, (int32_t)grid.y, (int32_t)v, k > 0};      // later pieces add to dbias
     const bool wanted = dx || dw || dbias;
     if (!wanted || p.twice || grid.x > 1) {                   // otherwise softmax_grad_kernel ends the rows
       row_loss_kernel<<<dim3((unsigned)((n + 15) / 16)), 1024, 0, s>>>(r);
@@ -676,7 +674,7 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
       z.c = p.g; z.top = p.top; z.coef = p.coef; z.share = p.share; z.c_plane = p.piece * p.ldz; z.c_planes = p.planes;
       gemm_launch<END_GRAD>(z, cut, xk.lie, wo.lie, s);
     } else {
-      const SoftmaxGradArgs q = {r, p.z, p.ldz, span, p.g, p.piece * p.ldz, dbias ? p.sums + k * p.ranges * v : nullptr, (int32_t)p.range_rows, alpha};
+      const SoftmaxGradArgs q = {r, p.z, p.ldz, span, p.g, p.piece * p.ldz, dbias ? p.sums : nullptr, (int32_t)p.range_rows, alpha};
       switch (p.planes) {
         case 0: softmax_grad_kernel<0><<<grid, 256, 0, s>>>(q); break;
         case 1: softmax_grad_kernel<1><<<grid, 256, 0, s>>>(q); break;
@@ -697,12 +695,13 @@ int shampoo_linear_cross_entropy(const shampoo_cross_entropy *c, const void *x, 
     const PairCut pair = dx && dw ? pair_cut(fx, fw) : PairCut();
     if (pair.together) {
       TRY(gemm_pair(go, wt, fx, to_dx, left, right, fw, to_dw, pair, p.part, sums, s));
-      continue;
+    } else {
+      if (dx) TRY(gemm(go, wt, n, d, v, to_dx, p.part, sums, s));
+      if (dw) TRY(gemm(left, right, fw.M, fw.N, fw.K, to_dw, p.part, sums, s));
     }
-    if (dx) TRY(gemm(go, wt, n, d, v, to_dx, p.part, sums, s));
-    if (dw) TRY(gemm(left, right, fw.M, fw.N, fw.K, to_dw, p.part, sums, s));
+    TRY(launch_row_sums(sums, s));
   }
-  return launch_row_sums(bias_sums, s);
+  return SHAMPOO_OK;
 }
 
 size_t shampoo_checkpoint_bytes(int64_t rows, int32_t cols) {
@@ -789,7 +788,7 @@ int shampoo_checkpoint_weight_grad(const void *packed, size_t packed_bytes, int6
   ColumnSums columns = {};
   RowSums sums = {};
   if (db) columns = {{dy, lddy, rows, p.part_rows, p.parts > 1 ? p.sums : db, out, dtype == SHAMPOO_GRAD_BF16}, p.parts};
-  if (db && p.parts > 1) sums = {p.sums, db, (int32_t)p.parts, out};
+  if (db && p.parts > 1) sums = {p.sums, db, (int32_t)p.parts, out, 0};
   const Operand dyo = p.dy.operand(dy, p.dyp, LIE_ROWS);
   const bool both = p.dy.copy() && p.pieces == 1;
   if (p.dy.copy() && !both) TRY(launch_planes(p.dy.task(dy, p.dyp), s));

@@ -177,3 +177,40 @@ def test_residual_norm_forward_in_several_launches():
         assert float((h[part].double() - norm).abs().max()) <= U * float(norm.abs().max())
         for x, y in zip((r, f), held):
             assert float((x[part].double() - y[part].double()).abs().max()) <= float(x[part].abs().max()) / 127.5
+
+
+@pytest.mark.parametrize("kind,n,d,bias,in_out", [
+    (("bf16", "bf16"), 300, 200, False, False), (("bf16", "bf16"), 530, 40, True, True), (("bf16", "f32"), 300, 648, False, False),
+    (("bf16", "f32"), 300, 40, True, False), (("f32", "f32"), 300, 104, False, True), (("f32", "f32"), 530, 24, True, False)])
+def test_head_in_several_pieces_of_rows_whose_logits_are_kept(kind, n, d, bias, in_out):
+    """256 rows of 4194301 classes are a piece: 16-bit logits, float32 ones, and a bias gradient that later pieces add to.  |z| < 16: exponents
+    off by 2^-19, float32 gradients by less than 2^-16 of their norm; bf16 ones 3 u."""
+    torch = torch_()
+    dt, grad = types(kind)
+    g = gen(n + d)
+    v = 4194301
+    x, w = torch.randn((n, d), generator=g, device="cuda").to(dt), (torch.randn((v, d), generator=g, device="cuda") * (2 / math.sqrt(d))).to(dt)
+    t = torch.randint(0, v, (n,), generator=g, device="cuda")
+    b = torch.randn((v,), generator=g, device="cuda") if bias else None
+    wv = w.t().contiguous().t() if in_out else w
+    loss, dx, dw, db = B.shampoo_linear_cross_entropy(x, wv, t, bias=b, scale=1.0 / n, grad_dtype=grad)
+    x64, w64, b64 = x.double(), w.double(), b.double() if bias else 0.0
+    loss64, dx64 = torch.zeros(n, dtype=torch.float64, device="cuda"), torch.zeros_like(x64)
+    dw64, db64, largest = torch.zeros_like(w64), torch.zeros(v, dtype=torch.float64, device="cuda"), 0.0
+    for k in range(0, n, 100):                 # 2^31 elements and more in one float64 product came out wrong in places
+        z, tk = x64[k:k + 100] @ w64.t() + b64, t[k:k + 100]
+        largest = max(largest, float(z.abs().max()))
+        i = torch.arange(z.shape[0], device="cuda")
+        lse = torch.logsumexp(z, 1)
+        loss64[k:k + 100] = lse - z[i, tk]
+        p = z.sub_(lse[:, None]).exp_()
+        p[i, tk] -= 1.0
+        p /= n
+        dx64[k:k + 100] = p @ w64
+        dw64 += p.t() @ x64[k:k + 100]
+        db64 += p.sum(0)
+    assert float((loss.double() - loss64).abs().max()) <= 2.0 ** -23 * (math.sqrt(d) + 16) * largest
+    assert rel(dx, dx64) <= (3 * U if kind[0] == "bf16" else 2.0 ** -16)
+    assert rel(dw, dw64) <= (3 * U if kind[1] == "bf16" else 2.0 ** -16)
+    if bias:
+        assert rel(db, db64) <= 2.0 ** -16

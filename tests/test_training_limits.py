@@ -49,3 +49,19 @@ for rows, n, out, act, dtype in ((16384, 8, 1 << 22, 0, 1), (16384, 40, (1 << 22
 def test_bias_gradients_of_as_many_outputs_as_it_admits(lib):
     seen = [list(map(int, line.split())) for line in host_hip.run(lib, BIAS) if line]
     assert len(seen) == 7 and all(rc == 0 for _, _, rc in seen), seen
+
+
+def test_cross_entropy_workspace_does_not_grow_with_the_rows_of_a_bias_gradient():
+    """A piece of the rows takes the same memory whatever their number: logits, and partial sums of the bias's gradient.  From the first size on
+    which is one piece of its own (2^14 rows of 131072 classes)."""
+    L = B.lib()
+    for dtype, grad in ((1, 1), (1, 0), (0, 0)):
+        for bias in (0, 1):
+            need = []
+            for rows in (1 << 16, 1 << 20, (1 << 31) - 1):
+                c = B.CrossEntropy(rows, 2048, 131072, dtype, grad, 0, bias, 1, 2048, 2048, 2048, 2048)
+                need.append(L.shampoo_linear_cross_entropy_workspace_bytes(ctypes.byref(c)))
+                if dtype == 0:         # planes of all of x
+                    need[-1] -= 3 * rows * 2048 * 2
+            assert 0 < min(need) and max(need) - min(need) < 64 << 20, (dtype, grad, bias, need)
+            assert max(need) < 10 << 30
