@@ -487,6 +487,7 @@ class Checkpoint:
     @property
     def dtype(self):
         """That of the packed matrix"""
+        _ops or _load_ops()
         return _DTYPES[self.code]
 
 
@@ -497,18 +498,20 @@ def shampoo_checkpoint_pack(x):
 
 def shampoo_checkpoint_unpack(c, activation=ACT_NONE, dtype=None):
     """activation(x) [rows, cols] of what a checkpoint holds, in `dtype` (default: that of the packed matrix)."""
-    return _result(_ops.unpack(c.packed, c.rows, c.cols, activation, c.code if dtype is None else _code(dtype)))
+    ops = _ops or _load_ops()
+    return _result(ops.unpack(c.packed, c.rows, c.cols, activation, c.code if dtype is None else _code(dtype)))
 
 
 def shampoo_checkpoint_activation_grad(c, dy, activation):
     """dy * activation'(x) for the x that a checkpoint holds."""
-    return _result(_ops.activation_grad(c.packed, c.rows, c.cols, dy, activation))
+    return _result((_ops or _load_ops()).activation_grad(c.packed, c.rows, c.cols, dy, activation))
 
 
 def shampoo_checkpoint_weight_grad(c, dy, activation=ACT_NONE, grad_dtype=None, out_in=False, bias=False):
     """Gradient of the weight of y = activation(x) W from a checkpoint of x [rows, in] and dy [rows, out]: [in, out], or [out, in]
     with out_in; of grad_dtype (default: the type of dy).  With bias also the column sums of dy, float32."""
-    r = _result(_ops.weight_grad(c.packed, c.rows, c.cols, dy, activation, None if grad_dtype is None else _code(grad_dtype), out_in, bias))
+    ops = _ops or _load_ops()
+    r = _result(ops.weight_grad(c.packed, c.rows, c.cols, dy, activation, None if grad_dtype is None else _code(grad_dtype), out_in, bias))
     return r if bias else r[0]
 
 
@@ -535,7 +538,8 @@ def shampoo_residual_norm_backward(r, f, dr_out, dh, post=NORM_RMS, pre=NORM_RMS
     dw_pre, db_pre, None for those of what is not there."""
     ops = _ops or _load_ops()
     if isinstance(r, Checkpoint):
-        assert (f.rows, f.cols, f.code) == (r.rows, r.cols, r.code), "checkpoints of one shape and type are needed"
+        if not isinstance(f, Checkpoint) or (f.rows, f.cols, f.code) != (r.rows, r.cols, r.code):
+            raise AssertionError("checkpoints of one shape and type are needed")
         out = ops.norm_backward(r.packed, f.packed, r.rows, r.cols, r.code, dr_out, dh, post, pre, w_post, b_post, gate, w_pre, b_pre, epsilon, scale)
     else:
         out = ops.norm_backward(r, f, 0, 0, None, dr_out, dh, post, pre, w_post, b_post, gate, w_pre, b_pre, epsilon, scale)

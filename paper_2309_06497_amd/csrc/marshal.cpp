@@ -266,6 +266,20 @@ at::Tensor packed_for(const at::Tensor &x) {
 }
 size_t size_of(const at::Tensor &x) { return static_cast<size_t>(x.numel()); }
 
+// An int32 argument of the library
+int32_t integer32(PyObject *o) {
+  const int64_t v = integer(o);
+  if (v < INT32_MIN || v > INT32_MAX) throw Refused{"an integer of 32 bits is needed"};
+  return static_cast<int32_t>(v);
+}
+// The memory of a checkpoint of this shape: the library reads as much of it as the shape says.
+const at::Tensor &checkpoint(PyObject *o, int64_t rows, int32_t cols) {
+  const at::Tensor &p = tensor(o);
+  if (!p.is_cuda() || p.scalar_type() != at::kByte || !p.is_contiguous()) throw Refused{"a checkpoint is contiguous bytes on a CUDA device"};
+  if (rows < 0 || cols < 1 || size_of(p) < library.checkpoint_bytes(rows, cols)) throw Refused{"the checkpoint's memory does not hold its shape"};
+  return p;
+}
+
 // (x) -> packed
 PyObject *pack(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
   return guarded(n_args, 1, [&]() -> PyObject * {
@@ -281,13 +295,12 @@ PyObject *pack(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
 // (packed, rows, cols, activation, code of the type) -> y
 PyObject *unpack(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
   return guarded(n_args, 5, [&]() -> PyObject * {
-    const at::Tensor &p = tensor(a[0]);
-    const int64_t rows = integer(a[1]), cols = integer(a[2]), code = integer(a[4]);
-    const int32_t activation = static_cast<int32_t>(integer(a[3]));
+    const int64_t rows = integer(a[1]), code = integer(a[4]);
+    const int32_t cols = integer32(a[2]), activation = integer32(a[3]);
+    const at::Tensor &p = checkpoint(a[0], rows, cols);
     const at::Tensor y = empty(p, {rows, cols}, dtype_of(code));
     const int rc = call(p, [&](void *stream) {
-      return library.unpack(p.data_ptr(), size_of(p), rows, static_cast<int32_t>(cols), activation, y.data_ptr(),
-                            static_cast<int32_t>(code), cols, stream);
+      return library.unpack(p.data_ptr(), size_of(p), rows, cols, activation, y.data_ptr(), static_cast<int32_t>(code), cols, stream);
     });
     return rc != 0 ? PyLong_FromLong(rc) : THPVariable_Wrap(y);
   });
@@ -296,15 +309,15 @@ PyObject *unpack(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
 // (packed, rows, cols, dy, activation) -> dx
 PyObject *activation_grad(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
   return guarded(n_args, 5, [&]() -> PyObject * {
-    const at::Tensor &p = tensor(a[0]);
-    const int64_t rows = integer(a[1]), cols = integer(a[2]);
-    const int32_t activation = static_cast<int32_t>(integer(a[4]));
+    const int64_t rows = integer(a[1]);
+    const int32_t cols = integer32(a[2]), activation = integer32(a[4]);
+    const at::Tensor &p = checkpoint(a[0], rows, cols);
     const at::Tensor dy = rows_of(tensor(a[3]));
     if (dy.size(0) != rows || dy.size(1) != cols || dy.device() != p.device()) throw Refused{"dy is not of the checkpoint's shape and device"};
     const int code = dtype_code(dy.scalar_type());
     const at::Tensor dx = empty(dy, {rows, cols}, dy.scalar_type());
     const int rc = call(dy, [&](void *stream) {
-      return library.activation_grad(p.data_ptr(), size_of(p), rows, static_cast<int32_t>(cols), activation, dy.data_ptr(), code, ld(dy), dx.data_ptr(), cols, stream);
+      return library.activation_grad(p.data_ptr(), size_of(p), rows, cols, activation, dy.data_ptr(), code, ld(dy), dx.data_ptr(), cols, stream);
     });
     return rc != 0 ? PyLong_FromLong(rc) : THPVariable_Wrap(dx);
   });
@@ -313,9 +326,9 @@ PyObject *activation_grad(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
 // (packed, rows, cols, dy, activation, code of dw's type or None, out_in, bias) -> (dw, db)
 PyObject *weight_grad(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
   return guarded(n_args, 8, [&]() -> PyObject * {
-    const at::Tensor &p = tensor(a[0]);
-    const int64_t rows = integer(a[1]), in = integer(a[2]);
-    const int32_t activation = static_cast<int32_t>(integer(a[4]));
+    const int64_t rows = integer(a[1]);
+    const int32_t in = integer32(a[2]), activation = integer32(a[4]);
+    const at::Tensor &p = checkpoint(a[0], rows, in);
     const at::Tensor dy = rows_of(tensor(a[3]), 16);
     if (dy.size(0) != rows || dy.device() != p.device()) throw Refused{"dy is not of the checkpoint's rows and device"};
     const int64_t out = dy.size(1);
@@ -326,10 +339,10 @@ PyObject *weight_grad(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
     const at::Tensor dw = out_in ? empty(dy, {out, in}, grad) : empty(dy, {in, out}, grad);
     std::optional<at::Tensor> db;
     if (PyObject_IsTrue(a[7]) != 0) db = empty(dy, {out}, at::kFloat);
-    const int32_t in32 = static_cast<int32_t>(in), out32 = static_cast<int32_t>(out);
-    const at::Tensor ws = bytes(dy, library.weight_grad_bytes(rows, in32, out32, activation, code, ld(dy), dtype_code(grad), db ? 1 : 0));
+    const int32_t out32 = static_cast<int32_t>(out);
+    const at::Tensor ws = bytes(dy, library.weight_grad_bytes(rows, in, out32, activation, code, ld(dy), dtype_code(grad), db ? 1 : 0));
     const int rc = call(dy, [&](void *stream) {
-      return library.weight_grad(p.data_ptr(), size_of(p), rows, in32, activation, dy.data_ptr(), code, out32, ld(dy), dw.data_ptr(), dtype_code(grad),
+      return library.weight_grad(p.data_ptr(), size_of(p), rows, in, activation, dy.data_ptr(), code, out32, ld(dy), dw.data_ptr(), dtype_code(grad),
                                  out_in ? SHAMPOO_OUT_IN : SHAMPOO_IN_OUT, dw.size(1), static_cast<float *>(address(db)), ws.data_ptr(), size_of(ws), stream);
     });
     return rc != 0 ? PyLong_FromLong(rc) : tuple({dw, db});
@@ -379,7 +392,8 @@ PyObject *norm_forward(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
 PyObject *norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
   return guarded(n_args, 16, [&]() -> PyObject * {
     const bool packed = a[4] != Py_None;
-    const at::Tensor r = packed ? tensor(a[0]) : rows_of(tensor(a[0])), f = packed ? tensor(a[1]) : rows_of(tensor(a[1]));
+    const auto matrix = [&](PyObject *o) { return packed ? checkpoint(o, integer(a[2]), integer32(a[3])) : rows_of(tensor(o)); };
+    const at::Tensor r = matrix(a[0]), f = matrix(a[1]);
     const int64_t rows = packed ? integer(a[2]) : r.size(0), cols = packed ? integer(a[3]) : r.size(1);
     const at::ScalarType type = packed ? dtype_of(integer(a[4])) : r.scalar_type();
     const at::Device device = r.device();
