@@ -214,3 +214,216 @@ def test_head_in_several_pieces_of_rows_whose_logits_are_kept(kind, n, d, bias, 
     assert rel(dw, dw64) <= (3 * U if kind[1] == "bf16" else 2.0 ** -16)
     if bias:
         assert rel(db, db64) <= 2.0 ** -16
+
+
+# ----------------------------------------------------------------------------
+# Float32 accuracy takes all three bf16 terms
+# ----------------------------------------------------------------------------
+def two_terms(x):
+    """What two bf16 terms hold of float32 x"""
+    h = x.bfloat16().float()
+    return h + (x - h).bfloat16().float()
+
+
+@pytest.mark.parametrize("d,bias", [(8, False), (704, False), (8, True)])
+@pytest.mark.parametrize("v", [251, 2 * 1190 + 1])
+def test_float32_weight_gradient_of_bf16_rows_has_24_bits_of_g(v, d, bias):
+    """One row, x = 1, w = 0: every logit is 0, p = 1 / v and dw is g itself, 1 / v and 1 / v - 1.  1 / v and the product with it are off by 2 e,
+    three terms by less than e, their sum by 2 e: 2^-21 of each element.  Two terms of 1 / v are further off (2^-17.0 of it for 251)."""
+    torch = torch_()
+    x, w = torch.ones((1, d), device="cuda").bfloat16(), torch.zeros((v, d), device="cuda").bfloat16()
+    t = torch.tensor([v // 2], device="cuda")
+    want = torch.full((v,), 1.0 / v, dtype=torch.float64, device="cuda")
+    want[v // 2] -= 1.0
+    bar = 2.0 ** -21
+    if v == 251:
+        assert float(((two_terms(want.float()).double() - want) / want).abs().max()) > 8 * bar
+    _, _, dw, db = B.shampoo_linear_cross_entropy(x, w, t, bias=torch.zeros(v, device="cuda") if bias else None, grad_dtype=torch.float32)
+    assert float(((dw.double() - want[:, None]) / want[:, None]).abs().max()) <= bar
+    if bias:
+        assert float(((db.double() - want) / want).abs().max()) <= bar
+
+
+@pytest.mark.parametrize("kind", [("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("act", [B.ACT_GELU, B.ACT_SILU])
+def test_float32_weight_gradient_has_24_bits_of_the_activation(act, kind):
+    """One row, dy = 1: dw is a(x) itself.  x > 0, where erf and exp do not cancel: a few 2^-23 of each, three terms less than e: 2^-20.  Two
+    terms are off by up to 2^-17."""
+    torch = torch_()
+    dt, grad = types(kind)
+    x = torch.arange(1, 4096, device="cuda").float()[None] * 2.0 ** -10
+    c = B.shampoo_checkpoint_pack(x.to(dt))
+    z = B.shampoo_checkpoint_unpack(c, dtype=torch.float32).double()
+    want = z * torch.sigmoid(z) if act == B.ACT_SILU else z * 0.5 * torch.special.erfc(-z / math.sqrt(2))
+    some = want[0] > 0
+    assert int(some.sum()) > 4000
+    bar = 2.0 ** -20
+    assert float(((two_terms(want.float()).double() - want) / want)[0, some].abs().max()) > 4 * bar
+    dw = B.shampoo_checkpoint_weight_grad(c, torch.ones((1, 1), device="cuda").to(dt), act, grad, out_in=True)
+    assert float(((dw.double() - want) / want)[0, some].abs().max()) <= bar
+
+
+# ----------------------------------------------------------------------------
+# Results in place and in rows further apart, by the C interface
+# ----------------------------------------------------------------------------
+class Rows:
+    """A matrix inside a buffer of one value: its rows `ld` apart, from an element on that is not aligned (aligned: on 256 bytes)"""
+    FILL = 77.0
+
+    def __init__(self, rows, cols, dtype, gap=5, values=None, aligned=False):
+        torch = torch_()
+        self.ld = -(-(cols + gap) // 8) * 8 if aligned else cols + gap
+        first = 256 if aligned else self.ld + 3
+        self.all = torch.full((first + (rows + 2) * self.ld,), self.FILL, dtype=dtype, device="cuda")
+        self.view = torch.as_strided(self.all, (rows, cols), (self.ld, 1), first)
+        if values is not None:
+            self.view.copy_(values)
+
+    def p(self):
+        return self.view.data_ptr()
+
+    def check(self, want):
+        """The matrix as wanted, bit by bit, and nothing else touched"""
+        torch = torch_()
+        assert torch.equal(self.view, want)
+        self.view.fill_(self.FILL)
+        assert bool((self.all == self.FILL).all())
+
+
+def done(rc):
+    torch_().cuda.synchronize()
+    assert rc == 0, rc
+
+
+def stream():
+    return torch_().cuda.current_stream().cuda_stream
+
+
+def code(dt):
+    return B.GRAD_F32 if dt == torch_().float32 else B.GRAD_BF16
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("in_out", [False, True])
+@pytest.mark.parametrize("n,d,v,bias", [(3, 7, 5, False), (130, 201, 257, True), (65, 777, 1001, False), (600, 130, 16501, False), (1000, 257, 20003, True)])
+def test_gradients_of_the_head_in_rows_further_apart(n, d, v, bias, in_out, kind):
+    import ctypes
+    torch = torch_()
+    dt, grad = types(kind)
+    g = gen(n)
+    x, w = torch.randn((n, d), generator=g, device="cuda").to(dt), (torch.randn((v, d), generator=g, device="cuda") * 0.1).to(dt)
+    t = torch.randint(0, v, (n,), generator=g, device="cuda")
+    b = torch.randn((v,), generator=g, device="cuda") if bias else None
+    wv = w.t().contiguous().t() if in_out else w
+    loss, dx, dw, db = B.shampoo_linear_cross_entropy(x, wv, t, bias=b, grad_dtype=grad)
+    dw = dw.t() if in_out else dw
+    x2, w2 = Rows(n, d, dt, values=x, aligned=True), Rows(*dw.shape, dt, values=w.t() if in_out else w, aligned=True)
+    dx2, dw2, loss2 = Rows(n, d, dt), Rows(*dw.shape, grad), Rows(1, n, torch.float32)
+    db2 = Rows(1, v, torch.float32)
+    c = B.CrossEntropy(n, d, v, code(dt), code(grad), B.IN_OUT if in_out else B.OUT_IN, int(bias), 1, x2.ld, w2.ld, dx2.ld, dw2.ld)
+    need = B.lib().shampoo_linear_cross_entropy_workspace_bytes(ctypes.byref(c))
+    ws = torch.full((need + 4096,), 255, dtype=torch.uint8, device="cuda")       # NaN, whatever is read of it
+    done(B.lib().shampoo_linear_cross_entropy(ctypes.byref(c), x2.p(), w2.p(), b.data_ptr() if bias else None, t.data_ptr(), None, 1.0, loss2.p(), dx2.p(),
+                                              dw2.p(), db2.p() if bias else None, ws.data_ptr(), need, stream()))
+    assert bool((ws[need:] == 255).all())
+    loss2.check(loss[None])
+    dx2.check(dx)
+    dw2.check(dw)
+    x2.check(x)
+    w2.check(w.t() if in_out else w)
+    if bias:
+        db2.check(db[None])
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("n,d", [(1, 1), (3, 7), (5, 33), (70, 200), (33, 1001)])
+def test_checkpoints_of_rows_further_apart_and_gradients_in_place(n, d, dt):
+    torch = torch_()
+    dt, = types((dt,))
+    L, g = B.lib(), gen(d)
+    x, dy = torch.randn((n, d), generator=g, device="cuda").to(dt), torch.randn((n, d), generator=g, device="cuda").to(dt)
+    c = B.shampoo_checkpoint_pack(x)
+    need = L.shampoo_checkpoint_bytes(n, d)
+    x2, packed = Rows(n, d, dt, values=x), torch.full((need + 512,), 77, dtype=torch.uint8, device="cuda")
+    done(L.shampoo_checkpoint_pack(x2.p(), code(dt), n, d, x2.ld, packed.data_ptr(), need, stream()))
+    x2.check(x)
+    assert bool((packed[need:] == 77).all())
+    for act in (B.ACT_NONE, B.ACT_SILU):
+        y = Rows(n, d, dt)
+        done(L.shampoo_checkpoint_unpack(packed.data_ptr(), need, n, d, act, y.p(), code(dt), y.ld, stream()))
+        y.check(B.shampoo_checkpoint_unpack(c, act))
+    want = B.shampoo_checkpoint_activation_grad(c, dy, B.ACT_GELU)
+    dy2, dx2 = Rows(n, d, dt, values=dy), Rows(n, d, dt, gap=9)
+    done(L.shampoo_checkpoint_activation_grad(packed.data_ptr(), need, n, d, B.ACT_GELU, dy2.p(), code(dt), dy2.ld, dx2.p(), dx2.ld, stream()))
+    dx2.check(want)
+    done(L.shampoo_checkpoint_activation_grad(packed.data_ptr(), need, n, d, B.ACT_GELU, dy2.p(), code(dt), dy2.ld, dy2.p(), dy2.ld, stream()))
+    dy2.check(want)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("out_in", [False, True])
+@pytest.mark.parametrize("n,i,o", [(1, 1, 1), (70, 33, 65), (999, 130, 331), (2500, 1000, 17001)])
+def test_weight_gradient_in_rows_further_apart(n, i, o, out_in, kind):
+    """The last size: tiles of 256 of which a last round is split"""
+    torch = torch_()
+    dt, grad = types(kind)
+    L, g = B.lib(), gen(o)
+    x, dy = torch.randn((n, i), generator=g, device="cuda").to(dt), torch.randn((n, o), generator=g, device="cuda").to(dt)
+    c = B.shampoo_checkpoint_pack(x)
+    dy2 = Rows(n, o, dt, values=dy, aligned=True)
+    dw, db = B.shampoo_checkpoint_weight_grad(c, dy2.view, B.ACT_SILU, grad, out_in, True)
+    dw2, db2 = Rows(*dw.shape, grad), Rows(1, o, torch.float32)
+    need = L.shampoo_checkpoint_weight_grad_workspace_bytes(n, i, o, B.ACT_SILU, code(dt), dy2.ld, code(grad), 1)
+    ws = torch.full((need + 4096,), 255, dtype=torch.uint8, device="cuda")       # NaN, whatever is read of it
+    done(L.shampoo_checkpoint_weight_grad(c.packed.data_ptr(), c.packed.numel(), n, i, B.ACT_SILU, dy2.p(), code(dt), o, dy2.ld, dw2.p(), code(grad),
+                                          B.OUT_IN if out_in else B.IN_OUT, dw2.ld, db2.p(), ws.data_ptr(), need, stream()))
+    assert bool((ws[need:] == 255).all())
+    dw2.check(dw)
+    db2.check(db[None])
+    dy2.check(dy)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("n,d,gates", [(1, 1, 1), (6, 33, 3), (40, 520, 0), (300, 1001, 1), (24, 2049, 4), (9, 4100, 1), (6, 8201, 2)])
+def test_residual_norms_in_place_in_rows_further_apart(n, d, gates, packed, dt):
+    """r_out in the place of r, dr in that of dr_out, df in that of dh"""
+    import ctypes
+    torch = torch_()
+    dt, = types((dt,))
+    L, g = B.lib(), gen(d)
+    r, f, dr_out, dh = (torch.randn((n, d), generator=g, device="cuda").to(dt) for _ in range(4))
+    w_post, b_post, w_pre, b_pre = (torch.randn((d,), generator=g, device="cuda") for _ in range(4))
+    gate = torch.randn((gates, d), generator=g, device="cuda") if gates else None
+    kw = dict(post=B.NORM_LAYER, pre=B.NORM_LAYER, w_post=w_post, b_post=b_post, gate=gate, w_pre=w_pre, b_pre=b_pre, epsilon=1e-5, scale=0.5)
+    out = B.shampoo_residual_norm_forward(r, f, checkpoint=packed, **kw)
+    want = B.shampoo_residual_norm_backward(*(out[2:] if packed else (r, f)), dr_out, dh, **kw)
+    c = B.ResidualNorm(n, d, code(dt), B.NORM_LAYER, B.NORM_LAYER, gates, 1e-5, 0.5, w_post.data_ptr(), b_post.data_ptr(), gate.data_ptr() if gates else None,
+                       w_pre.data_ptr(), b_pre.data_ptr())
+    size = L.shampoo_checkpoint_bytes(n, d)
+    memory = [torch.full((size + 512,), 77, dtype=torch.uint8, device="cuda") for _ in range(2)] if packed else None
+    r2, f2, h2 = Rows(n, d, dt, values=r), Rows(n, d, dt, gap=9, values=f), Rows(n, d, dt, gap=1)
+    done(L.shampoo_residual_norm_forward(ctypes.byref(c), r2.p(), r2.ld, f2.p(), f2.ld, r2.p(), r2.ld, h2.p(), h2.ld,
+                                         *((m.data_ptr() for m in memory) if packed else (None, None)), size, stream()))
+    r2.check(out[0])
+    h2.check(out[1])
+    if packed:
+        for m, have in zip(memory, out[2:]):
+            again = B.Checkpoint(m[:size], (n, d), code(dt))
+            assert torch.equal(B.shampoo_checkpoint_unpack(again), B.shampoo_checkpoint_unpack(have)) and bool((m[size:] == 77).all())
+    r2.view.copy_(r)
+    a2, b2 = Rows(n, d, dt, values=dr_out), Rows(n, d, dt, gap=2, values=dh)
+    sums = {k: Rows(gates if k == "dgate" else 1, d, torch.float32, gap=0) for k in ("dgate", "dw_post", "db_post", "dw_pre", "db_pre")}
+    need = L.shampoo_residual_norm_backward_workspace_bytes(ctypes.byref(c))
+    ws = torch.full((need + 4096,), 255, dtype=torch.uint8, device="cuda")       # NaN, whatever is read of it
+    rf = [(m.data_ptr(), 0) for m in memory] if packed else [(r2.p(), r2.ld), (f2.p(), f2.ld)]
+    done(L.shampoo_residual_norm_backward(ctypes.byref(c), int(packed), *rf[0], *rf[1], a2.p(), a2.ld, b2.p(), b2.ld, a2.p(), a2.ld, b2.p(), b2.ld,
+                                          *(sums[k].p() if gates or k != "dgate" else None for k in sums), ws.data_ptr(), need, stream()))
+    assert bool((ws[need:] == 255).all())
+    a2.check(want["dr"])
+    b2.check(want["df"])
+    r2.check(r)
+    f2.check(f)
+    for k, s in sums.items():
+        if want[k] is not None:
+            s.check(want[k].view(-1, d))
