@@ -388,16 +388,18 @@ enum { SHAMPOO_OUT_IN = 0, SHAMPOO_IN_OUT = 1 };
  * Softmax cross entropy of a linear layer over many classes, and its gradients:
  *   z = x w^T + bias,  lse_i = log sum_v exp z_iv,  loss_i = lse_i - z_{i,t_i},
  *   g_iv = scale weight_i (exp(z_iv - lse_i) - [v = t_i]),  dx = g w,  dw = g^T x,  dbias_v = sum_i g_iv
- * (the gradients of scale sum_i weight_i loss_i).  The logits of a piece of the rows at a time lie in the workspace,
- * at most 4 GiB of them (or 256 rows), never all of them.
+ * (the gradients of scale sum_i weight_i loss_i).  For gradients the logits of a piece of the rows at a time lie in the workspace,
+ * with what is made of them 2 to 10 bytes each: as many rows as fit in 4 GiB, at least 256, so all logits of a call that fits.
+ * The loss alone keeps none of them.
  * A row whose target is outside 0 ... classes - 1 is ignored: loss 0 and g_i = 0 whatever its logits are (its row of x
  * still is a factor of dw: 0 times a value that is not finite is not 0).  bias may mask classes by -infinity: their
- * probability and gradient are 0; a masked target has loss +infinity; a row with every class masked has g_i = 0.
+ * probability is 0 and so is their gradient; a masked target has loss +infinity and, as p = 0, the gradient -scale weight_i; a row with every class
+ * masked has g_i = 0.  The loss and p are those of z - max z: a common offset of the logits takes nothing but the bits that it takes of z.
  */
 typedef struct {
   int64_t rows;           /* >= 0                                                              */
   int32_t features;       /* 1 ... 65536                                                       */
-  int32_t classes;        /* 1 ... 4194304                                                     */
+  int32_t classes;        /* 1 ... 4194304; at most 2^23 blocks of 128 features by 128 classes  */
   int32_t dtype;          /* of x, w and dx.  bf16: z from exact products; g is rounded to bf16 for the products of dx
                              and bf16 dw, and has float32 accuracy (three bf16 terms) for float32 dw.  float32: all
                              products to float32 accuracy (three terms per value, six products) */
@@ -443,7 +445,7 @@ int shampoo_checkpoint_activation_grad(const void *packed, size_t packed_bytes, 
  * dtype: of dy (16-byte aligned, else SHAMPOO_ERR_UNSUPPORTED).  Float32 dy: products to float32 accuracy, dw float32.
  * bf16 dy: x and dy enter as they are; a(x), where an activation is given, rounded to bf16 for bf16 dw, with float32 accuracy for
  * float32 dw.  An infinity in float32 dy reaches its results as in the sum; in bf16 dy it makes them infinite or NaN.
- * in <= 65536, out <= 4194304.
+ * in <= 65536, out <= 4194304, at most 2^23 blocks of 128 by 128.
  */
 size_t shampoo_checkpoint_weight_grad_workspace_bytes(int64_t rows, int32_t in, int32_t out, int32_t activation, int32_t dtype,
                                                       int64_t lddy, int32_t grad_dtype, int32_t want_bias);
@@ -474,7 +476,7 @@ int shampoo_residual_norm_forward(const shampoo_residual_norm *c, const void *r,
                                   void *packed_r, void *packed_f, size_t packed_bytes, void *stream);
 /*
  * Gradients from those of r_out (dr_out, NULL: 0) and of h (dh; NULL where there is no h).  r and f as the forward call had them: packed != 0:
- * their checkpoints (ldr, ldf ignored), otherwise the matrices.  dr may be dr_out, df may be dh.  dgate [gates][cols], dw_post, db_post,
+ * their checkpoints, shampoo_checkpoint_bytes(rows, cols) bytes each (ldr, ldf ignored), otherwise the matrices.  dr may be dr_out, df may be dh.  dgate [gates][cols], dw_post, db_post,
  * dw_pre, db_pre [cols]: float32, each NULL where it is not wanted.
  */
 size_t shampoo_residual_norm_backward_workspace_bytes(const shampoo_residual_norm *c);

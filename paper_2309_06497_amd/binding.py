@@ -432,7 +432,8 @@ def shampoo_root_inverse_newton(a, epsilon, p, tolerance=1e-6, max_iterations=10
 
 
 # ----------------------------------------------------------------------------
-# Operators of a training pass: checks of tensors, outputs and workspaces are csrc/marshal.cpp's
+# Operators of a training pass: checks of tensors, outputs and workspaces are csrc/marshal.cpp's.  Like the step they take tensors that
+# require gradients and record nothing for automatic differentiation: their results are not part of any graph.
 # ----------------------------------------------------------------------------
 _ops = None
 _codes = {}            # torch's types and the library's

@@ -151,7 +151,7 @@ template <typename T, bool GRAD> __global__ __launch_bounds__(256) void checkpoi
 }
 
 // a(x) of a checkpoint, or a matrix in memory (float32 or bf16, any alignment), as PLANES bf16 planes [plane][rows][ld], ld a
-// multiple of 8, zeros from cols to ld and in rows from `rows` on.  Bound by memory: one plane of 8192 x 8192 codes 36 us (5.6 TB/s).
+// multiple of 8, zeros from cols to ld and in rows from `rows` on.  Bound by memory: one plane of 8192 x 8192 codes 37 us (5.5 TB/s).
 struct PlanesArgs {
   Packed p; const void *x; int64_t ldx;        // one of the two
   uint16_t *out; int64_t plane, ld;

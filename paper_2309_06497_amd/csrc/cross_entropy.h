@@ -18,7 +18,7 @@
 //   float32 x or dw, or a bias: z in float32, beside it g as the bf16 planes that float32 results need.
 // Few features (and no sums for a bias): neither; the product runs a second time, once the rows' sums are known, and leaves g itself.
 // The three products are 6 rows features classes operations; what lies between them is bound by memory.  8192 x 2048 x 131072 in bf16:
-// products 4.00, 3.46 (dx) and 3.47 ms (dw), 16-bit logits to g 0.88 (4.3 GB, 4.9 TB/s), the rows' sums 0.03.
+// products 4.24, 3.62 (dx) and 3.75 ms (dw), 16-bit logits to g 0.87 (4.3 GB, 4.9 TB/s), the rows' sums 0.03.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

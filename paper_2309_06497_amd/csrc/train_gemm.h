@@ -25,9 +25,9 @@
 // The MFMA operands are handed over swapped, so that a lane has one row of C and runs of four columns: softmax statistics are sums over
 // registers, and stores go through LDS in whole rows.
 //
-// Bound by the matrix cores and the clock that they leave: of 8192 x 2048 x 131072 in bf16, dw runs at 1.27 PFLOP/s with them busy for
-// 71 % of the cycles at 1.61 GHz, no bank conflicts, and dx at the same rate; the logits at 1.10, since a tile ends with 13 vector
-// operations per logit.  8192 x 2048 x 8192 (dw) 1.30.  Small: 256 x 2048 x 1000, six products of planes, 15 ... 18 us a product.
+// Bound by the matrix cores and the clock that they leave: of 8192 x 2048 x 131072 in bf16, dw runs at 1.17 PFLOP/s (1.24 on a card with a higher clock) with them busy for
+// 72 % of the cycles at 1.50 GHz, no bank conflicts, dx at 1.22; the logits at 1.04, since a tile ends with 13 vector
+// operations per logit.  8192 x 2048 x 8192 (dw) 1.16.  Small: 256 x 2048 x 1000, six products of planes, 15 ... 19 us a product.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
