@@ -485,6 +485,98 @@ int shampoo_residual_norm_backward(const shampoo_residual_norm *c, int32_t packe
                                    void *dr, int64_t ld_dr, void *df, int64_t ld_df, float *dgate, float *dw_post, float *db_post,
                                    float *dw_pre, float *db_pre, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Operators on given logits: what a program learns from, scores with or answers with where a product has made them.  Conventions as above.
+ * ------------------------------------------------------------------------------------------ */
+
+/*
+ * Of every row of logits z, with x = (z - max z) / T and log p = x - log sum exp x:
+ *   log_probs_j = log p of given token j,  entropy = -sum_v p_v log p_v,  and the `top` most probable tokens with their log p.
+ * The order of tokens is that of the logits as they are given; of equal ones the lower token comes first.
+ * A given token outside 0 ... classes - 1 is ignored: log_probs 0, no gradient.  -infinity masks a token: its log p is -infinity, it adds nothing to the
+ * entropy and is none of the most probable; where fewer than `top` are left, the rest of top_tokens is -1 and of top_log_probs -infinity.  A row with nothing
+ * left has entropy 0.  A NaN or +infinity makes all log p of its row and its entropy NaN; top_tokens are in the order of what is not NaN.
+ */
+typedef struct {
+  int64_t rows;               /* 0 ... 2^31 - 1                                                   */
+  int32_t classes;            /* 1 ... 4194304                                                    */
+  int32_t tokens;             /* given tokens of a row, 0 ... 64; the same one may be given twice */
+  int32_t top;                /* 0 ... 64                                                         */
+  int32_t dtype;              /* of the logits and of their gradient                              */
+  float inverse_temperature;  /* 1 / T, > 0 and finite                                            */
+  int64_t ld;                 /* of the logits, >= classes                                        */
+} shampoo_logits;
+size_t shampoo_log_probs_workspace_bytes(const shampoo_logits *c);  /* 0 also if c is invalid */
+/* tokens [rows][c->tokens] int64 (log_probs alike, float32; both may be NULL where there are none), entropy [rows] float32, top_tokens [rows][top] int64,
+ * top_log_probs [rows][top] float32 (NULL where top is 0), statistics [rows][4] float32, 16-byte aligned: what the gradient needs of a row.
+ * workspace: 256-byte aligned, may be NULL where none is needed. */
+int shampoo_log_probs(const shampoo_logits *c, const void *logits, const int64_t *tokens, float *log_probs, float *entropy, int64_t *top_tokens,
+                      float *top_log_probs, float *statistics, void *workspace, size_t workspace_bytes, void *stream);
+/*
+ * Gradient of the logits from those of log_probs (a, [rows][c->tokens] float32, or NULL: none) and of the entropy (b, [rows] float32, or NULL):
+ *   dz_v = (sum_j a_j [v = t_j] - p_v (sum_j a_j + b (log p_v + entropy))) / T
+ * logits, tokens and statistics as the forward call had and left them; c->top is ignored.  d_logits [rows][classes] may be the logits themselves (the same
+ * leading dimension then).  A given token that is masked has p = 0 and the gradient a / T; a row with nothing left, or whose coefficients are all zero,
+ * has the gradient 0.
+ */
+int shampoo_log_probs_grad(const shampoo_logits *c, const void *logits, const int64_t *tokens, const float *statistics, const float *d_log_probs,
+                           const float *d_entropy, void *d_logits, int64_t ld_d_logits, void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * All tensors of a model at once: the norm of the gradients, and an AdamW step (for parameters that have no factors worth keeping: vectors, embeddings).
+ * ------------------------------------------------------------------------------------------ */
+
+/*
+ * norm = sqrt of the sum of the squares of all elements of n gradients, norms[i] (or NULL) that of gradient i; sums in 64 bits.
+ * grads: host array [n] of device pointers, contiguous; numel: host array [n], >= 0 each, at most 2^39 together (NULL is a pointer for none).  norm, norms: float32 device
+ * pointers.  NaN and infinities reach the results, and so does a norm that float32 does not hold.
+ */
+size_t shampoo_gradient_norm_workspace_bytes(int32_t n, const int64_t *numel);
+int shampoo_gradient_norm(int32_t n, const void *const *grads, const int64_t *numel, int32_t dtype, float *norm, float *norms, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
+/*
+ * AdamW (decoupled weight decay, bias correction):
+ *   g <- g min(1, max_norm / norm)  (where a norm is given)
+ *   m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) g^2,  t = step + 1
+ *   w <- (1 - lr weight_decay) w - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + epsilon)
+ * in float32.  bf16 parameters are rounded up with the probability of what is left over (an update is mostly less than half a step of theirs); the
+ * random numbers are a mix of the element's index and the step's number, so that the same call gives the same bits.
+ * state_bits = 8: 128 neighbouring elements of a tensor share a power of two; m has a sign, 4 bits of exponent and 3 of mantissa, v 5 and 3, rounded the same way (v > 0
+ * never to 0).  Groups whose largest is below 2^-100 are kept as zeros; one with an infinity, a NaN or a value from 2^127 on reads NaN as a whole.
+ */
+typedef struct shampoo_adamw shampoo_adamw; /* opaque, owned by the library */
+typedef struct {
+  int32_t n_params;        /* 1 ... 2^20                                            */
+  const int64_t *numel;    /* host [n_params]: elements, >= 0 each, at most 2^39 together */
+  const int32_t *decay;    /* host [n_params]: != 0 where weight_decay applies; NULL: everywhere */
+  int32_t state_bits;      /* 32 or 8                                               */
+  int32_t param_dtype;     /* SHAMPOO_GRAD_F32 or SHAMPOO_GRAD_BF16                 */
+  int32_t grad_dtype;
+  int32_t device;          /* HIP device ordinal: the current one in every call     */
+  double beta1, beta2;     /* in [0, 1)                                             */
+  double epsilon;          /* 1e-30 ... 1e30                                        */
+  double weight_decay;     /* >= 0                                                  */
+} shampoo_adamw_config;
+/* 0 if cfg is invalid.  With 32 bits the workspace begins with m, [all elements] float32, one parameter behind the other; v follows at the next multiple of 256 bytes. */
+size_t shampoo_adamw_workspace_bytes(const shampoo_adamw_config *cfg);
+/* workspace: 256-byte aligned; holds all state and stays allocated until shampoo_adamw_destroy.  m = v = 0; `stream` is synchronised before returning. */
+int shampoo_adamw_create(const shampoo_adamw_config *cfg, void *workspace, size_t workspace_bytes, void *stream, shampoo_adamw **out);
+/*
+ * params, grads: host arrays [n_params] of device pointers, contiguous, aligned to their elements; params are updated in place.  copies: NULL, or bf16 tensors [n_params]
+ * that get the updated float32 parameters, rounded to the nearest.  step: 0-based, strictly increasing.  norm: NULL, or a device pointer to the norm of these gradients
+ * (max_norm > 0, may be infinite); where it is not finite the call changes nothing on the device, and the step counts as taken.
+ * Recorded into a graph, a step keeps the pointers, lr and step number that it was given.
+ */
+int shampoo_adamw_step(shampoo_adamw *opt, void *const *params, const void *const *grads, void *const *copies, double lr, int64_t step,
+                       const float *norm, float max_norm, void *stream);
+/* m and v of all parameters, one behind the other without gaps ([all elements] each, of `dtype`; bf16 holds what 8 bits hold), and the other way round from float32 (8 bits: rounded to
+ * the nearest). */
+int shampoo_adamw_get(shampoo_adamw *opt, void *m, void *v, int32_t dtype, void *stream);
+int shampoo_adamw_set(shampoo_adamw *opt, const float *m, const float *v, void *stream);
+/* Frees the host-side handle only. */
+int shampoo_adamw_destroy(shampoo_adamw *opt);
+
 /* Static, NUL-terminated description of a return code. */
 const char *shampoo_strerror(int code);
 

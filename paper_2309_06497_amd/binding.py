@@ -37,6 +37,9 @@ EXPORTS = (
     "shampoo_checkpoint_bytes", "shampoo_checkpoint_pack", "shampoo_checkpoint_unpack", "shampoo_checkpoint_activation_grad",
     "shampoo_checkpoint_weight_grad_workspace_bytes", "shampoo_checkpoint_weight_grad",
     "shampoo_residual_norm_forward", "shampoo_residual_norm_backward_workspace_bytes", "shampoo_residual_norm_backward",
+    "shampoo_log_probs_workspace_bytes", "shampoo_log_probs", "shampoo_log_probs_grad",
+    "shampoo_gradient_norm_workspace_bytes", "shampoo_gradient_norm",
+    "shampoo_adamw_workspace_bytes", "shampoo_adamw_create", "shampoo_adamw_step", "shampoo_adamw_get", "shampoo_adamw_set", "shampoo_adamw_destroy",
     "shampoo_strerror",
 )
 
@@ -82,6 +85,17 @@ class ResidualNorm(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("cols", "dtype", "post", "pre")] + [
         ("gates", ctypes.c_int64), ("epsilon", ctypes.c_float), ("scale", ctypes.c_float)] + [
         (n, ctypes.c_void_p) for n in ("w_post", "b_post", "gate", "w_pre", "b_pre")]
+
+
+class Logits(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("classes", "tokens", "top", "dtype")] + [
+        ("inverse_temperature", ctypes.c_float), ("ld", ctypes.c_int64)]
+
+
+class AdamWConfig(ctypes.Structure):
+    _fields_ = [("n_params", ctypes.c_int32), ("numel", ctypes.POINTER(ctypes.c_int64)), ("decay", ctypes.POINTER(ctypes.c_int32))] + [
+        (n, ctypes.c_int32) for n in ("state_bits", "param_dtype", "grad_dtype", "device")] + [
+        (n, ctypes.c_double) for n in ("beta1", "beta2", "epsilon", "weight_decay")]
 
 
 _lib = None
@@ -154,6 +168,29 @@ def lib():
     L.shampoo_residual_norm_backward_workspace_bytes.restype = sz
     L.shampoo_residual_norm_backward.argtypes = [rnp, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64] + [vp] * 5 + [vp, sz, vp]
     L.shampoo_residual_norm_backward.restype = ctypes.c_int
+    lgp, awp, f64 = ctypes.POINTER(Logits), ctypes.POINTER(AdamWConfig), ctypes.c_double
+    L.shampoo_log_probs_workspace_bytes.argtypes = [lgp]
+    L.shampoo_log_probs_workspace_bytes.restype = sz
+    L.shampoo_log_probs.argtypes = [lgp] + [vp] * 8 + [sz, vp]
+    L.shampoo_log_probs.restype = ctypes.c_int
+    L.shampoo_log_probs_grad.argtypes = [lgp] + [vp] * 6 + [i64, vp]
+    L.shampoo_log_probs_grad.restype = ctypes.c_int
+    L.shampoo_gradient_norm_workspace_bytes.argtypes = [i32, ctypes.POINTER(i64)]
+    L.shampoo_gradient_norm_workspace_bytes.restype = sz
+    L.shampoo_gradient_norm.argtypes = [i32, ctypes.POINTER(vp), ctypes.POINTER(i64), i32, vp, vp, vp, sz, vp]
+    L.shampoo_gradient_norm.restype = ctypes.c_int
+    L.shampoo_adamw_workspace_bytes.argtypes = [awp]
+    L.shampoo_adamw_workspace_bytes.restype = sz
+    L.shampoo_adamw_create.argtypes = [awp, vp, sz, vp, ctypes.POINTER(vp)]
+    L.shampoo_adamw_create.restype = ctypes.c_int
+    L.shampoo_adamw_step.argtypes = [vp, ctypes.POINTER(vp), ctypes.POINTER(vp), ctypes.POINTER(vp), f64, i64, vp, f32, vp]
+    L.shampoo_adamw_step.restype = ctypes.c_int
+    L.shampoo_adamw_get.argtypes = [vp, vp, vp, i32, vp]
+    L.shampoo_adamw_get.restype = ctypes.c_int
+    L.shampoo_adamw_set.argtypes = [vp, vp, vp, vp]
+    L.shampoo_adamw_set.restype = ctypes.c_int
+    L.shampoo_adamw_destroy.argtypes = [vp]
+    L.shampoo_adamw_destroy.restype = ctypes.c_int
     L.shampoo_strerror.argtypes = [ctypes.c_int]
     L.shampoo_strerror.restype = ctypes.c_char_p
     _lib = L
@@ -448,7 +485,8 @@ def _load_ops():
     _marshal.use([ctypes.cast(getattr(L, "shampoo_" + name), ctypes.c_void_p).value for name in (
         "linear_cross_entropy_workspace_bytes", "linear_cross_entropy", "checkpoint_bytes", "checkpoint_pack", "checkpoint_unpack",
         "checkpoint_activation_grad", "checkpoint_weight_grad_workspace_bytes", "checkpoint_weight_grad", "residual_norm_forward",
-        "residual_norm_backward_workspace_bytes", "residual_norm_backward")])
+        "residual_norm_backward_workspace_bytes", "residual_norm_backward", "log_probs_workspace_bytes", "log_probs", "log_probs_grad",
+        "gradient_norm_workspace_bytes", "gradient_norm", "adamw_step")])
     _codes = {torch.float32: GRAD_F32, torch.bfloat16: GRAD_BF16}
     _DTYPES = (torch.float32, torch.bfloat16)
     _ops = _marshal
@@ -545,3 +583,113 @@ def shampoo_residual_norm_backward(r, f, dr_out, dh, post=NORM_RMS, pre=NORM_RMS
     else:
         out = ops.norm_backward(r, f, 0, 0, None, dr_out, dh, post, pre, w_post, b_post, gate, w_pre, b_pre, epsilon, scale)
     return dict(zip(_NORM_GRADIENTS, _result(out)))
+
+
+# ----------------------------------------------------------------------------
+# Operators on given logits
+# ----------------------------------------------------------------------------
+class LogProbs:
+    """What shampoo_log_probs returns: log_probs (of the given tokens, in their shape), entropy [n], and where alternatives were asked
+    for top_tokens [n, top] int64 and top_log_probs [n, top]; statistics [n, 4] and temperature are the backward pass's."""
+    __slots__ = ("log_probs", "entropy", "top_tokens", "top_log_probs", "statistics", "temperature")
+
+    def __init__(self, log_probs, entropy, top_tokens, top_log_probs, statistics, temperature):
+        self.log_probs, self.entropy, self.top_tokens, self.top_log_probs = log_probs, entropy, top_tokens, top_log_probs
+        self.statistics, self.temperature = statistics, temperature
+
+
+def shampoo_log_probs(logits, tokens, top=0, temperature=1.0):
+    """Log probabilities of given tokens under softmax(logits / temperature), the entropy of every row and its `top` most probable tokens.
+
+    logits [n, v]: CUDA, float32 or bfloat16.  tokens [n] or [n, m] int64, m at most 64 (outside 0 ... v - 1: ignored, log probability 0).  -inf masks a
+    token.  Of equal logits the lower token is the more probable one; where fewer than top (at most 64) are left the rest is -1."""
+    return LogProbs(*_result((_ops or _load_ops()).log_probs(logits, tokens, top, temperature)), temperature)
+
+
+def shampoo_log_probs_grad(logits, tokens, forward, d_log_probs, d_entropy=None, out=None):
+    """Gradient of the logits from those of `forward`'s log_probs (or None) and entropy (or None); logits and tokens as shampoo_log_probs had them.
+    out: where it is written, the logits themselves where they are no longer needed."""
+    return _result((_ops or _load_ops()).log_probs_grad(logits, tokens, forward.statistics, forward.temperature, d_log_probs, d_entropy, out))
+
+
+# ----------------------------------------------------------------------------
+# All tensors of a model
+# ----------------------------------------------------------------------------
+def shampoo_gradient_norm(grads):
+    """(norm of all gradients together, norms [n] of each) on their device, float32, from sums in 64 bits.  grads: contiguous CUDA tensors, all float32 or
+    all bfloat16."""
+    return _result((_ops or _load_ops()).gradient_norm(grads))
+
+
+class AdamW:
+    """AdamW over one list of parameters: owns the workspace tensor, which holds all state, and the library handle.  decay: for every parameter
+    whether weight_decay applies to it (default: to all)."""
+
+    def __init__(self, shapes, beta1=0.9, beta2=0.999, epsilon=1e-8, weight_decay=0.01, decay=None, state_bits=32, param_dtype=GRAD_F32,
+                 grad_dtype=GRAD_F32, device=0):
+        import torch
+        self.shapes = [tuple(int(d) for d in s) for s in shapes]
+        n = len(self.shapes)
+        sizes = [int(np.prod(s, dtype=object)) for s in self.shapes]
+        self.total = sum(sizes)
+        numel = (ctypes.c_int64 * max(n, 1))(*sizes)
+        flags = None
+        if decay is not None:
+            if len(decay) != n:
+                raise ValueError("one entry of decay per parameter")
+            flags = (ctypes.c_int32 * max(n, 1))(*[1 if d else 0 for d in decay])
+        self.cfg = AdamWConfig(n, numel, flags, state_bits, param_dtype, grad_dtype, device, beta1, beta2, epsilon, weight_decay)
+        self.device, self.param_dtype, self.state_bits = torch.device("cuda", device), param_dtype, state_bits
+        self.handle = ctypes.c_void_p()
+        nbytes = lib().shampoo_adamw_workspace_bytes(ctypes.byref(self.cfg))
+        if nbytes == 0:
+            raise ShampooError(lib().shampoo_adamw_create(ctypes.byref(self.cfg), None, 0, None, ctypes.byref(self.handle)))
+        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        with torch.cuda.device(self.device):
+            _check(lib().shampoo_adamw_create(ctypes.byref(self.cfg), ctypes.c_void_p(self.workspace.data_ptr()), nbytes, _stream_ptr(),
+                                              ctypes.byref(self.handle)))
+        ops = _ops or _load_ops()
+        self._step = ops.adamw_step
+        self._stepper = ops.make(0, self.handle.value, device, grad_dtype == GRAD_BF16, self.shapes)
+
+    def step(self, params, grads, lr, step, copies=None, norm=None, max_norm=float("inf")):
+        """One step, 0-based and strictly increasing.  params, grads: lists of contiguous CUDA tensors of the types given; params are updated in place, each
+        tensor stands there once.  copies: bfloat16 tensors that get the updated float32 parameters.  norm: that of these gradients, as shampoo_gradient_norm
+        returns it: they count as scaled down to max_norm, and nothing changes where it is not finite."""
+        _check(self._step(self._stepper, params, grads, copies, lr, step, norm, max_norm, self.param_dtype) if self.handle else -1)
+
+    def state(self):
+        """(m, v) of all parameters, one behind the other: with 32 bits views of the optimizer's memory, with 8 bits the values that it holds, as
+        bfloat16 (which holds them exactly)."""
+        import torch
+        if not self.handle:
+            raise ShampooError(-1)
+        if self.state_bits == 32:
+            size = 4 * self.total
+            return tuple(self.workspace[at:at + size].view(torch.float32) for at in (0, (size + 255) // 256 * 256))
+        m, v = (torch.empty(self.total, dtype=torch.bfloat16, device=self.device) for _ in range(2))
+        with torch.cuda.device(self.device):
+            _check(lib().shampoo_adamw_get(self.handle, ctypes.c_void_p(m.data_ptr()), ctypes.c_void_p(v.data_ptr()), GRAD_BF16, _stream_ptr()))
+        return m, v
+
+    def load(self, m, v):
+        """The states of another optimizer, as state() gives them (any floating type)."""
+        import torch
+        if not self.handle:
+            raise ShampooError(-1)
+        assert all(x.is_cuda and x.device == self.device and x.numel() == self.total for x in (m, v)), "states of all elements on the optimizer's device"
+        m, v = (x.reshape(-1).to(torch.float32).contiguous() for x in (m, v))
+        with torch.cuda.device(self.device):
+            _check(lib().shampoo_adamw_set(self.handle, ctypes.c_void_p(m.data_ptr()), ctypes.c_void_p(v.data_ptr()), _stream_ptr()))
+
+    def destroy(self):
+        if self.handle:
+            self._stepper = None
+            lib().shampoo_adamw_destroy(self.handle)
+            self.handle = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass

@@ -11,7 +11,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB = os.path.join(HERE, "libshampoo.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
-SOURCES = [os.path.join(HERE, "csrc", f) for f in ("shampoo.hip", "training.hip")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("shampoo.hip", "training.hip", "logits.hip", "adamw.hip")]
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
     # packed fp32 instructions are kept out of the generated code

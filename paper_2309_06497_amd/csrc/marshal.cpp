@@ -133,8 +133,14 @@ struct Library {
   decltype(&shampoo_residual_norm_forward) norm_forward;
   decltype(&shampoo_residual_norm_backward_workspace_bytes) norm_backward_bytes;
   decltype(&shampoo_residual_norm_backward) norm_backward;
+  decltype(&shampoo_log_probs_workspace_bytes) log_probs_bytes;
+  decltype(&shampoo_log_probs) log_probs;
+  decltype(&shampoo_log_probs_grad) log_probs_grad;
+  decltype(&shampoo_gradient_norm_workspace_bytes) gradient_norm_bytes;
+  decltype(&shampoo_gradient_norm) gradient_norm;
+  decltype(&shampoo_adamw_step) adamw_step;
 } library;
-static_assert(sizeof(Library) == 11 * sizeof(void *), "addresses only");
+static_assert(sizeof(Library) == 17 * sizeof(void *), "addresses only");
 
 // use([addresses of the entry points in the order above])
 PyObject *use(PyObject *, PyObject *list) {
@@ -424,10 +430,175 @@ PyObject *norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
   });
 }
 
+// ---------------------------------------------------------------------------
+// Operators on given logits
+// ---------------------------------------------------------------------------
+// logits [n, v], tokens [n] or [n, m] int64 on the same device, temperature
+struct Logits {
+  at::Tensor z, tokens;
+  shampoo_logits c;
+  Logits(PyObject *logits, PyObject *given, PyObject *temperature) {
+    const at::Tensor &t = tensor(given);
+    const int code = dtype_code(tensor(logits).scalar_type());
+    z = rows_of(tensor(logits));
+    if (t.scalar_type() != at::kLong || t.device() != z.device() || t.dim() < 1 || t.dim() > 2 || t.size(0) != z.size(0)) throw Refused{"tokens are int64 [n] or [n, m] beside logits [n, v]"};
+    const int64_t m = t.dim() == 2 ? t.size(1) : 1;
+    if (z.size(1) > INT32_MAX || m > INT32_MAX) throw Refused{"too many classes or tokens"};
+    tokens = t.contiguous();
+    c = {z.size(0), static_cast<int32_t>(z.size(1)), static_cast<int32_t>(m), 0, code, static_cast<float>(1.0 / PyFloat_AsDouble(temperature)), ld(z)};
+    if (PyErr_Occurred()) throw python_error();
+  }
+  const int64_t *given() const { return static_cast<const int64_t *>(tokens.data_ptr()); }
+};
+
+// (logits, tokens, top, temperature) -> (log_probs, entropy, top_tokens, top_log_probs, statistics)
+PyObject *log_probs(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
+  return guarded(n_args, 4, [&]() -> PyObject * {
+    Logits k(a[0], a[1], a[3]);
+    k.c.top = integer32(a[2]);
+    const int64_t n = k.c.rows;
+    const at::Tensor lp = empty(k.z, k.tokens.sizes(), at::kFloat), entropy = empty(k.z, {n}, at::kFloat), stats = empty(k.z, {n, 4}, at::kFloat);
+    std::optional<at::Tensor> top, top_lp;
+    if (k.c.top > 0) { top = empty(k.z, {n, k.c.top}, at::kLong); top_lp = empty(k.z, {n, k.c.top}, at::kFloat); }
+    const size_t need = library.log_probs_bytes(&k.c);
+    std::optional<at::Tensor> ws;
+    if (need > 0) ws = bytes(k.z, need);
+    const int rc = call(k.z, [&](void *stream) {
+      return library.log_probs(&k.c, k.z.data_ptr(), k.given(), static_cast<float *>(lp.data_ptr()), static_cast<float *>(entropy.data_ptr()),
+                               static_cast<int64_t *>(address(top)), static_cast<float *>(address(top_lp)), static_cast<float *>(stats.data_ptr()), address(ws), need, stream);
+    });
+    return rc != 0 ? PyLong_FromLong(rc) : tuple({lp, entropy, top, top_lp, stats});
+  });
+}
+
+// Whether rows of `y` may be written while those of `x` are read: the same rows, or none in common
+bool rows_fit(const at::Tensor &x, const at::Tensor &y) {
+  const int64_t n = x.size(0), d = x.size(1), size = static_cast<int64_t>(x.element_size());
+  const intptr_t p = reinterpret_cast<intptr_t>(x.data_ptr()), q = reinterpret_cast<intptr_t>(y.data_ptr());
+  if (n == 0 || d == 0 || (p == q && ld(x) == ld(y))) return true;
+  if (p + ((n - 1) * ld(x) + d) * size <= q || q + ((n - 1) * ld(y) + d) * size <= p) return true;
+  if (ld(x) != ld(y)) return false;
+  const int64_t pitch = ld(x) * size, off = ((q - p) % pitch + pitch) % pitch;      // columns of one matrix side by side
+  return off >= d * size && pitch - off >= d * size;
+}
+
+// (logits, tokens, statistics, temperature, d_log_probs, d_entropy, out) -> d_logits
+PyObject *log_probs_grad(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
+  return guarded(n_args, 7, [&]() -> PyObject * {
+    const Logits k(a[0], a[1], a[3]);
+    const int64_t n = k.c.rows, d = k.c.classes;
+    const auto stats = vector(a[2], {n, 4}, k.z.device()), dlp = vector(a[4], k.tokens.sizes(), k.z.device()), dh = vector(a[5], {n}, k.z.device());
+    if (!stats) throw Refused{"the forward call's statistics are needed"};
+    at::Tensor out;
+    if (a[6] == Py_None) {
+      out = empty(k.z, {n, d}, k.z.scalar_type());
+    } else {
+      out = tensor(a[6]);
+      if (out.sizes() != k.z.sizes() || out.scalar_type() != k.z.scalar_type() || out.device() != k.z.device() || (d > 1 && out.stride(1) != 1) ||
+          (n > 1 && out.stride(0) < d))
+        throw Refused{"out is of the logits' shape, type and device, with contiguous rows"};
+      if (!rows_fit(k.z, out)) throw Refused{"out is the logits' memory or has none of it"};
+    }
+    const int rc = call(k.z, [&](void *stream) {
+      return library.log_probs_grad(&k.c, k.z.data_ptr(), k.given(), floats(stats), floats(dlp), floats(dh), out.data_ptr(), ld(out), stream);
+    });
+    return rc != 0 ? PyLong_FromLong(rc) : THPVariable_Wrap(out);
+  });
+}
+
+// ---------------------------------------------------------------------------
+// All tensors of a model
+// ---------------------------------------------------------------------------
+// (sequence of gradients) -> (norm, norms)
+PyObject *gradient_norm(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
+  return guarded(n_args, 1, [&]() -> PyObject * {
+    THPObjectPtr list(PySequence_Fast(a[0], "a sequence of tensors is needed"));
+    if (!list) return nullptr;
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(list.get());
+    if (n < 1 || n > INT32_MAX) throw Refused{"one gradient at least is needed"};
+    std::vector<const void *> g(n);
+    std::vector<int64_t> numel(n);
+    const at::Tensor &first = tensor(PySequence_Fast_GET_ITEM(list.get(), 0));
+    const at::ScalarType type = first.scalar_type();
+    const int code = dtype_code(type);
+    if (!first.is_cuda()) throw Refused{"gradients on a CUDA device are needed"};
+    for (Py_ssize_t i = 0; i < n; ++i) {
+      const at::Tensor &x = tensor(PySequence_Fast_GET_ITEM(list.get(), i));
+      if (x.device() != first.device() || x.scalar_type() != type) throw Refused{"gradients of one type on one device are needed"};
+      if (!x.is_contiguous()) throw Refused{"gradients must be contiguous"};
+      g[i] = x.data_ptr(); numel[i] = x.numel();
+    }
+    const int32_t count = static_cast<int32_t>(n);
+    const at::Tensor norm = empty(first, {}, at::kFloat), norms = empty(first, {static_cast<int64_t>(n)}, at::kFloat);
+    const at::Tensor ws = bytes(first, library.gradient_norm_bytes(count, numel.data()));
+    const int rc = call(first, [&](void *stream) {
+      return library.gradient_norm(count, g.data(), numel.data(), code, static_cast<float *>(norm.data_ptr()), static_cast<float *>(norms.data_ptr()), ws.data_ptr(),
+                                   size_of(ws), stream);
+    });
+    return rc != 0 ? PyLong_FromLong(rc) : tuple({norm, norms});
+  });
+}
+
+// (stepper, params, grads, copies, lr, step number, norm, max_norm, code of the parameters' type) -> return code of shampoo_adamw_step; the stepper is make's, whose shapes may be of any rank
+PyObject *adamw_step(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
+  return guarded(n_args, 9, [&]() -> PyObject * {
+    auto *s = static_cast<Stepper *>(PyCapsule_GetPointer(a[0], CAPSULE));
+    if (!s) return nullptr;
+    const at::ScalarType type = dtype_of(integer(a[8]));
+    const size_t n = s->shapes.size();
+    THPObjectPtr lists[3];
+    const bool copies = a[3] != Py_None;
+    for (int k = 0; k < 2 + copies; ++k) {
+      lists[k] = PySequence_Fast(a[1 + k], "params, grads and copies are sequences of tensors");
+      if (!lists[k]) return nullptr;
+      if (static_cast<size_t>(PySequence_Fast_GET_SIZE(lists[k].get())) != n) {
+        PyErr_SetString(PyExc_ValueError, "one tensor per declared parameter");
+        return nullptr;
+      }
+    }
+    std::vector<void *> c(copies ? n : 0);
+    for (size_t i = 0; i < n; ++i) {
+      const char *bad = nullptr;
+      for (int k = 0; k < 2 + copies && !bad; ++k) {
+        PyObject *o = PySequence_Fast_GET_ITEM(lists[k].get(), static_cast<Py_ssize_t>(i));
+        if (!THPVariable_Check(o)) { bad = "parameters, gradients and copies are tensors"; break; }
+        const at::Tensor &x = THPVariable_Unpack(o);
+        if (x.device() != s->device) bad = "tensors must live on the optimizer's device";
+        else if (x.scalar_type() != (k == 0 ? type : k == 1 ? s->grad_dtype : at::kBFloat16)) bad = "parameters and gradients are of the types given at creation, copies are bfloat16";
+        else if (!x.is_contiguous()) bad = "tensors must be contiguous";
+        else if (x.sizes() != c10::IntArrayRef(s->shapes[i])) bad = "shape differs from the one given at creation";
+        else if (k == 0) s->w[i] = x.data_ptr();
+        else if (k == 1) s->g[i] = x.data_ptr();
+        else c[i] = x.data_ptr();
+      }
+      if (bad) { PyErr_Format(PyExc_ValueError, "parameter %zu: %s", i, bad); return nullptr; }
+    }
+    const double lr = PyFloat_AsDouble(a[4]);
+    const int64_t t = integer(a[5]);
+    const float max_norm = real(a[7]);
+    if (PyErr_Occurred()) throw python_error();
+    const float *norm = nullptr;
+    if (a[6] != Py_None) {
+      const at::Tensor &x = tensor(a[6]);
+      if (x.device() != s->device || x.scalar_type() != at::kFloat || x.numel() != 1) throw Refused{"norm is one float32 value on the optimizer's device"};
+      norm = static_cast<const float *>(x.data_ptr());
+    }
+    const c10::hip::HIPGuard guard(s->device.index());
+    void *stream = c10::hip::getCurrentHIPStream(s->device.index()).stream();
+    int rc;
+    {
+      pybind11::gil_scoped_release no_gil;
+      rc = library.adamw_step(static_cast<shampoo_adamw *>(s->handle), s->w.data(), s->g.data(), copies ? c.data() : nullptr, lr, t, norm, max_norm, stream);
+    }
+    return PyLong_FromLong(rc);
+  });
+}
+
 #define OPERATOR(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"make", make, METH_VARARGS, nullptr}, {"step", step, METH_VARARGS, nullptr}, {"use", use, METH_O, nullptr},
                          OPERATOR(cross_entropy), OPERATOR(pack), OPERATOR(unpack), OPERATOR(activation_grad), OPERATOR(weight_grad),
-                         OPERATOR(norm_forward), OPERATOR(norm_backward), {nullptr, nullptr, 0, nullptr}};
+                         OPERATOR(norm_forward), OPERATOR(norm_backward), OPERATOR(log_probs), OPERATOR(log_probs_grad),
+                         OPERATOR(gradient_norm), OPERATOR(adamw_step), {nullptr, nullptr, 0, nullptr}};
 #undef OPERATOR
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -7,9 +7,9 @@
 #include <cstdint>
 #include <type_traits>
 
-#include "../../include/shampoo.h"
 #include "checkpoint.h"
 #include "cross_entropy.h"
+#include "host_checks.h"
 #include "residual_norm.h"
 #include "train_gemm.h"
 #include "vectors.h"
@@ -18,7 +18,6 @@ using namespace shampoo;
 
 namespace {
 
-constexpr size_t ALIGN = 256;
 constexpr int64_t MAX_ROWS = 0x7fffffff;
 constexpr int32_t MAX_FEATURES = 65536, MAX_OUT = 1 << 22, MAX_PACKED_COLS = 1 << 20, MAX_NORM_COLS = 16384;
 constexpr int64_t MAX_LD = 1 << 22;                        // of an operand as it lies: offsets inside a tile have 32 bits
@@ -28,39 +27,6 @@ constexpr int LOGIT_SPLITS = 64;
 constexpr int64_t PIECE_ROWS = 256, MAX_PIECE_ROWS = 1 << 21;   // rows of a piece are a multiple of the first (grids: at most 65535 ranges of 64)
 constexpr int64_t MAX_TILES = 1 << 23;                     // of a product: threads of a launch have 32 bits
 constexpr int64_t MAX_SUM_BLOCKS = 1 << 22;                // workgroups of column sums, beside as many for planes
-
-inline size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
-inline int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
-inline bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
-inline bool dtype_ok(int32_t d) { return d == SHAMPOO_GRAD_F32 || d == SHAMPOO_GRAD_BF16; }
-inline int64_t size_of(int32_t d) { return d == SHAMPOO_GRAD_F32 ? 4 : 2; }
-
-#define HIP_TRY(expr)                          \
-  do {                                         \
-    hipError_t e_ = (expr);                    \
-    if (e_ != hipSuccess) return SHAMPOO_ERR_HIP; \
-  } while (0)
-#define TRY(...)                               \
-  do {                                         \
-    const int rc_ = (__VA_ARGS__);             \
-    if (rc_ != SHAMPOO_OK) return rc_;         \
-  } while (0)
-
-// ---------------------------------------------------------------------------
-// Workspaces: arrays one behind the other
-// ---------------------------------------------------------------------------
-struct Arena {
-  unsigned char *base; size_t used = 0;
-  explicit Arena(void *p) : base(static_cast<unsigned char *>(p)) {}
-  template <typename T> T *take(size_t count) {
-    T *p = reinterpret_cast<T *>(base + used);
-    used += align_up(count * sizeof(T));
-    return p;
-  }
-};
-inline int workspace_ok(const void *p, size_t have, size_t want) {
-  return want > 0 && (!p || !aligned(p, ALIGN) || have < want) ? SHAMPOO_ERR_WORKSPACE : SHAMPOO_OK;
-}
 
 // ---------------------------------------------------------------------------
 // Elementwise launches

@@ -1,0 +1,460 @@
+"""The AdamW step over many tensors, its 8-bit states and the norm of all gradients against the definitions in 64 bits.
+
+u = 2^-24 is half a step of float32.  m is a sum of two products, each rounded and the weights too: 2 u of both products and u of the sum, 4 u (|b1 m| + |(1 - b1) g|) with
+the limited gradient's own u.  v: one product more, 5 u of v.  The update: sqrt, its scale, epsilon, quotient and lr: 8 u of the update and half the error of v (2.5 u) and that of m, which
+is not relative to m; the result: 2 u of what is left of w, u of the sum.
+A state of 8 bits is the value's code after floor(value / step + offset), with an offset in 2^-20 steps: the kernel's value is the one above, and where
+value / step + offset is nearer to a whole number than that error, either neighbour is right."""
+import math
+
+import numpy as np
+import pytest
+
+from paper_2309_06497_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+GROUP = 128
+M32 = 0xFFFFFFFF
+
+
+def offsets(first, n, step):
+    """Of elements first ... first + n - 1, in steps: of m, v and a bf16 parameter"""
+    i = np.arange(first, first + n, dtype=np.uint64)
+    k = lambda x: np.uint64(x)
+    x = ((i & k(M32)) * k(0x9E3779B9) + (i >> k(32)) * k(0xBB67AE85) + k((step * 0x6A09E667) & M32)) & k(M32)
+    x = ((x ^ (x >> k(16))) * k(0xBB67AE85)) & k(M32)
+    x = ((x ^ (x >> k(15))) * k(0xA54FF53B)) & k(M32)
+    x ^= x >> k(16)
+    y = (x * k(0x9E3779B9) + k(0x6A09E667)) & k(M32)
+    y ^= y >> k(15)
+    return (x >> k(12)).astype(np.float64) / 2 ** 20, (y >> k(12)).astype(np.float64) / 2 ** 20, (y & k(0xFFFF)).astype(np.float64) / 2 ** 16
+
+
+def held(x, binades, offset, largest=None):
+    """What 8 bits hold of one tensor's values, and the step of each; largest: of the groups, where they are not to be seen by the values"""
+    n = len(x)
+    v = np.pad(x, (0, -n % GROUP)).reshape(-1, GROUP)
+    o = np.pad(offset, (0, -n % GROUP)).reshape(-1, GROUP)
+    with np.errstate(invalid="ignore", over="ignore"):
+        largest = np.abs(v).max(1, keepdims=True) if largest is None else largest
+        bad = ~(largest < 2.0 ** 127)
+        top = np.where(bad, 0, np.frexp(largest)[1] - 1)
+        zero = largest < 2.0 ** -100
+        unit = np.ldexp(1.0, np.maximum(np.frexp(v)[1] - 1, top - binades + 1) - 3)
+        q = np.floor(np.abs(v) / unit + o)
+        if binades == 30:
+            q = np.where((q == 0) & (v != 0), 1.0, q)
+        out = np.where(bad, np.nan, np.where(zero, 0.0, np.copysign(q * unit, v)))
+    return out.reshape(-1)[:n], unit.reshape(-1)[:n]
+
+
+def rounded8(got, value, off, binades, offset, what):
+    """got: what 8 bits hold of a value that is off by `off` at most.  The largest of a group is off as well: beside a power of two (a tenth of a bf16 value can be one) either
+    side of it is right.  A v below 1.2e-38 may be zero in float32, and its code then."""
+    want, _ = held(value, binades, offset)
+    assert np.array_equal(np.isnan(got), np.isnan(want)), what
+    pad = lambda x: np.pad(x, (0, -len(x) % GROUP)).reshape(-1, GROUP)
+    ok = (np.abs(value) < 1.2e-38) & (got == 0)
+    for side in (-1, 1):
+        with np.errstate(invalid="ignore"):
+            _, unit = held(value, binades, offset, np.maximum(pad(np.abs(value)) + side * pad(off), 0.0).max(1, keepdims=True))
+        low, high = (np.floor(np.maximum(np.abs(value) + s * off, 0.0) / unit + offset) * unit for s in (-1, 1))
+        if binades == 30:
+            high = np.maximum(high, unit)
+        ok |= (np.abs(got) >= low * (1 - 1e-15)) & (np.abs(got) <= high * (1 + 1e-15))
+    differ = (got != want) & ~np.isnan(want)
+    assert ok[differ].all(), (what, got[differ & ~ok][:3], value[differ & ~ok][:3])
+
+
+def held_range(value, off, unit, offset, sign):
+    x = np.maximum(np.abs(value) + sign * off, 0.0)
+    return np.floor(x / unit + offset) * unit, unit
+
+
+class Model:
+    """The definition in 64 bits over a list of tensors; states are what the optimizer held before each step"""
+
+    def __init__(self, shapes, beta1=0.9, beta2=0.999, epsilon=1e-8, weight_decay=0.01, decay=None):
+        self.sizes = [int(np.prod(s)) for s in shapes]
+        self.beta1, self.beta2, self.epsilon, self.weight_decay = beta1, beta2, epsilon, weight_decay
+        self.decay = decay or [True] * len(shapes)
+
+    def step(self, i, w, g, m, v, lr, t):
+        wd = self.weight_decay if self.decay[i] else 0.0
+        m1 = self.beta1 * m + (1 - self.beta1) * g
+        v1 = self.beta2 * v + (1 - self.beta2) * g * g
+        root = np.sqrt(v1 / (1 - self.beta2 ** (t + 1))) + self.epsilon
+        c = lr / (1 - self.beta1 ** (t + 1))
+        w1 = w * (1 - lr * wd) - c * m1 / root
+        off_m = 5 * U * (np.abs(self.beta1 * m) + np.abs((1 - self.beta1) * g)) + 1e-44
+        off_v = 6 * U * v1 + 4e-38 * U          # squares of float32 may be subnormal
+        off_w = 3 * U * np.abs(w) + abs(c) * (11 * U * np.abs(m1) + off_m) / root + abs(c) * np.abs(m1) / root ** 2 * np.sqrt(3e-45) + U * np.abs(w1)
+        return m1, v1, w1, off_m, off_v, off_w
+
+
+def flat(x):
+    return x.double().cpu().numpy().reshape(-1)
+
+
+def run(shapes, bits, param, grad, steps=3, copies=False, clip=None, views=False, seed=0, lr=1e-2, first=0, decay=None, gradients=None, **kw):
+    """Steps of the kernels, each checked against the definition from the states and parameters before it"""
+    import torch
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    dtypes = {"f32": torch.float32, "bf16": torch.bfloat16}
+    total = sum(int(np.prod(s)) for s in shapes)
+
+    def tensors(dtype, sigma):
+        size = torch.randn((total + 3,), generator=gen, device="cuda").mul_(1.5).exp_()
+        x = torch.randn((total + 3,), generator=gen, device="cuda").mul_(size * sigma).to(dtype)
+        out, at = [], 3 if views else 0
+        for s in shapes:
+            n = int(np.prod(s))
+            out.append(x[at:at + n].view(s) if views else x[at:at + n].clone().view(s))
+            at += n
+        return out
+
+    w = tensors(dtypes[param], 0.05)
+    c = [torch.zeros(s, device="cuda", dtype=torch.bfloat16) for s in shapes] if copies else None
+    opt = B.AdamW(shapes, decay=decay, state_bits=bits, param_dtype=B.GRAD_F32 if param == "f32" else B.GRAD_BF16,
+                  grad_dtype=B.GRAD_F32 if grad == "f32" else B.GRAD_BF16, **kw)
+    model = Model(shapes, decay=decay, **kw)
+    starts = np.cumsum([0] + model.sizes)
+    for k in range(steps):
+        t = first + 2 * k
+        g = gradients(k, shapes) if gradients else tensors(dtypes[grad], 1e-3 * 10 ** k)
+        m0, v0 = (flat(x) for x in opt.state())
+        w0 = [flat(x) for x in w]
+        g0 = [flat(x) for x in g]
+        norm, limit = None, math.inf
+        if clip:
+            norm, limit = B.shampoo_gradient_norm(g)[0], clip
+            size = math.sqrt(sum(float((x * x).sum()) for x in g0))
+            assert abs(float(norm) - size) <= U * size * 1.01
+            g0 = [x * min(1.0, limit / size) for x in g0]
+        opt.step(w, g, lr, t, copies=c, norm=norm, max_norm=limit)
+        m1, v1 = (flat(x) for x in opt.state())
+        for i, n in enumerate(model.sizes):
+            if n == 0:
+                continue
+            at = slice(starts[i], starts[i + 1])
+            wm, wv, ww, em, ev, ew = model.step(i, w0[i], g0[i], m0[at], v0[at], lr, t)
+            if clip:
+                em, ev, ew = em + 2 * U * np.abs(0.1 * g0[i]), ev + 4 * U * wv, ew + lr * 8 * U * 40
+            om, ov, ow = offsets(starts[i], n, t)
+            what = (shapes[i], bits, param, grad, k)
+            if bits == 32:
+                assert (np.abs(m1[at] - wm) <= em).all() and (np.abs(v1[at] - wv) <= ev).all(), what
+            else:
+                rounded8(m1[at], wm, em, 14, om, what)
+                rounded8(v1[at], wv, ev, 30, ov, what)
+            got = flat(w[i])
+            if param == "f32":
+                assert (np.abs(got - ww) <= ew).all(), (what, (np.abs(got - ww) / ew).max())
+                if copies:
+                    assert torch.equal(c[i], w[i].bfloat16()), what
+            else:
+                with np.errstate(divide="ignore"):
+                    unit = np.ldexp(1.0, np.maximum(np.frexp(ww)[1] - 8, -133))
+                low, high = (held_range(ww, ew, unit, ow, s)[0] for s in (-1, 1))
+                ok = (np.abs(got) >= low * (1 - 1e-15)) & (np.abs(got) <= high * (1 + 1e-15)) & ((got == 0) | (np.sign(got) == np.sign(ww)) | (np.abs(ww) <= ew))
+                assert ok.all(), (what, got[~ok][:3], ww[~ok][:3])
+    return opt, w
+
+
+ODD = [(1,), (3, 5), (0,), (128,), (129,), (2, 64), (4096,), (4097,), (1000, 33), (7,), (8,), (9,), (2049, 3), (16385,), (1, 1, 1, 2), ()]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("param,grad,copies", [("f32", "f32", False), ("f32", "bf16", True), ("bf16", "bf16", False), ("bf16", "f32", False), ("f32", "bf16", False)])
+@pytest.mark.parametrize("views", [False, True])
+def test_steps(bits, param, grad, copies, views):
+    run(ODD, bits, param, grad, copies=copies, views=views)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("count", [159, 160, 161, 500])
+def test_many_tensors(bits, count):
+    shapes = [((k * 37) % 300 + 1,) if k % 3 else ((k % 11) + 1, 130) for k in range(count)]
+    run(shapes, bits, "f32", "bf16", steps=2, copies=True, views=True, clip=0.5)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_options(bits):
+    run([(300,), (20, 30)], bits, "f32", "f32", decay=[False, True], weight_decay=0.3, clip=1e-3)
+    run([(300,), (20, 30)], bits, "f32", "f32", clip=1e6, first=1000)
+    run([(300,), (20, 30)], bits, "f32", "f32", beta1=0.0, beta2=0.0, weight_decay=0.0)
+    run([(300,), (20, 30)], bits, "f32", "f32", epsilon=1e-3, lr=-1e-2, first=(1 << 40) + 1)
+    run([(300,), (20, 30)], bits, "f32", "f32", lr=0.0)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_gradients_of_all_sizes(bits):
+    """Groups of zeros, of one value among zeros, of values whose squares float32 does not hold, 2^-100 and below"""
+    import torch
+
+    def gradients(k, shapes):
+        g = torch.zeros((8, 128), device="cuda")
+        g[1, 5] = 1e-3
+        g[2] = 1e-30
+        g[3] = torch.logspace(-20, 15, 128, device="cuda")
+        g[4] = torch.randn((128,), device="cuda") * 1e-13
+        g[5, :64], g[5, 64:] = 1e-22, 1e-3
+        g[6] = -torch.logspace(-6, 0, 128, device="cuda")
+        g[7, 127] = 1e17
+        return [g]
+
+    run([(8, 128)], bits, "f32", "f32", gradients=gradients, steps=4)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_a_norm_that_is_not_finite_changes_nothing(bits, bad):
+    import torch
+    opt, w = run([(300,), (20, 30)], bits, "f32", "bf16", copies=True)
+    before = [x.clone() for x in w] + [x.clone() for x in opt.state()]
+    g = [torch.ones_like(x, dtype=torch.bfloat16) for x in w]
+    g[1][3, 4] = bad
+    c = [torch.full_like(x, 7.0, dtype=torch.bfloat16) for x in w]
+    norm, norms = B.shampoo_gradient_norm(g)
+    assert not math.isfinite(float(norm)) and math.isfinite(float(norms[0])) and not math.isfinite(float(norms[1]))
+    opt.step(w, g, 1e-2, 100, copies=c, norm=norm, max_norm=1.0)
+    assert all(torch.equal(x, y) for x, y in zip(before, w + list(opt.state()))) and all((x == 7).all() for x in c)
+    opt.step(w, g, 1e-2, 101)                       # without the norm it reaches what it touches: its element, and with 8 bits its group
+    assert not torch.isfinite(w[1][3, 4]) and torch.isfinite(w[0]).all() and int((~torch.isfinite(w[1])).sum()) == 1
+    g[1][3, 4] = 1.0
+    opt.step(w, g, 1e-2, 102)
+    assert torch.isfinite(w[0]).all() and int((~torch.isfinite(w[1])).sum()) == (1 if bits == 32 else 128)
+
+
+def test_a_norm_of_zero_and_one_that_float32_rounds():
+    run([(300,)], 32, "f32", "f32", gradients=lambda k, s: [__import__("torch").zeros((300,), device="cuda")], clip=None)
+    import torch
+    opt = B.AdamW([(300,)])
+    w, g = [torch.ones((300,), device="cuda")], [torch.zeros((300,), device="cuda")]
+    opt.step(w, g, 1e-2, 0, norm=B.shampoo_gradient_norm(g)[0], max_norm=1.0)
+    assert torch.isfinite(w[0]).all()
+
+
+def test_states_of_8_bits_move_as_their_mean_does():
+    """Without a gradient v falls by beta2 a step, which is a 60th of half a step of its code.  After 700 steps the mean over 2^16 elements is beta2^700 = 0.496 of what it was: a code
+    moves by a step of at most 1/8 of its value at a time, and the variance of a sum of such moves is at most the sum of step x move = 1/8 x 0.7 in squares of the value; the mean of
+    2^16: 0.3 / 256 = 1.2e-3, five times that is the bar.  All elements begin at the same value, so that nothing but the offsets tells them apart."""
+    import torch
+    n = 1 << 16
+    opt = B.AdamW([(n,)], state_bits=8, beta1=0.999)
+    opt.load(torch.full((n,), 1.0, device="cuda"), torch.full((n,), 1.0, device="cuda"))
+    w, g = [torch.zeros((n,), device="cuda")], [torch.zeros((n,), device="cuda")]
+    for t in range(700):
+        opt.step(w, g, 0.0, t)
+    for x in opt.state():
+        assert abs(float(x.double().mean()) - 0.999 ** 700) < 6e-3
+        assert float(x.min()) > 0 and len(torch.unique(x)) > 3
+
+
+def test_bf16_parameters_move_by_less_than_half_a_step():
+    """An update of 1e-3 (gradients of one size: m / sqrt(v) = 1) of parameters of 1 whose step is 2^-8 below and 2^-7 above: after 200 steps their mean is 0.8.
+    Variance of a rounding at most step^2 / 4, 200 of them, 2^16 elements: 2^-8 x 0.5 x 14 / 256 = 1.1e-4, five times that; m and v begin at nothing and are corrected: float32."""
+    import torch
+    n = 1 << 16
+    opt = B.AdamW([(n,)], param_dtype=B.GRAD_BF16, weight_decay=0.0)
+    w, g = [torch.full((n,), 1.0, device="cuda", dtype=torch.bfloat16)], [torch.full((n,), 0.5, device="cuda")]
+    for t in range(200):
+        opt.step(w, g, 1e-3, t)
+    assert abs(float(w[0].double().mean()) - 0.8) < 6e-4
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_states_saved_and_loaded(bits):
+    """What state() gives is what load() takes: the next steps are the same bits"""
+    import torch
+    opt, w = run(ODD, bits, "bf16", "f32")
+    other = B.AdamW(ODD, state_bits=bits, param_dtype=B.GRAD_BF16)
+    other.load(*[x.clone() for x in opt.state()])
+    assert all(torch.equal(x, y) for x, y in zip(opt.state(), other.state()))
+    u = [x.clone() for x in w]
+    for t in (50, 60):
+        g = [torch.randn(x.shape, device="cuda") for x in w]
+        opt.step(w, g, 1e-2, t)
+        other.step(u, g, 1e-2, t)
+    assert all(torch.equal(x, y) for x, y in zip(w, u)) and all(torch.equal(x, y) for x, y in zip(opt.state(), other.state()))
+
+
+def test_loading_rounds_to_the_nearest():
+    import torch
+    n = 5000
+    m, v = torch.randn((n,), device="cuda") * torch.logspace(-3, 3, n, device="cuda"), torch.rand((n,), device="cuda") * torch.logspace(-8, 2, n, device="cuda")
+    opt = B.AdamW([(n,)], state_bits=8)
+    opt.load(m, v)
+    for got, x, binades in zip(opt.state(), (m, v), (14, 30)):
+        want, _ = held(flat(x), binades, np.full(n, 0.5))
+        assert np.array_equal(flat(got), want)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_other_streams_and_replayed_graphs(bits):
+    """Two recorded steps of two optimizers, replayed between eager steps on other tensors: each works on the tensors that it was recorded with"""
+    import torch
+    shapes = [(300, 5), (77,)] * 90
+    make = lambda: [torch.randn(s, device="cuda") for s in shapes]
+    opts, want = [B.AdamW(shapes, state_bits=bits) for _ in range(2)], [B.AdamW(shapes, state_bits=bits) for _ in range(2)]
+    w, g = [make() for _ in range(2)], [make() for _ in range(2)]
+    u = [[x.clone() for x in y] for y in w]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for k in range(2):
+            opts[k].step(w[k], g[k], 1e-2, 3, norm=B.shampoo_gradient_norm(g[k])[0], max_norm=1.0)
+    torch.cuda.synchronize()
+    graphs = []
+    for k in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            opts[k].step(w[k], g[k], 1e-2, 10, norm=B.shampoo_gradient_norm(g[k])[0], max_norm=1.0)
+        graphs.append(graph)
+    for k in range(2):
+        want[k].step(u[k], g[k], 1e-2, 3, norm=B.shampoo_gradient_norm(g[k])[0], max_norm=1.0)
+    for r in range(3):
+        for k in range(2):
+            other = make()
+            graphs[k].replay()
+            opts[k].step(other, g[1 - k], 1e-2, 20 + r)
+            again = B.AdamW(shapes, state_bits=bits)              # a step number again is a new optimizer with the old states
+            again.load(*want[k].state())
+            again.step(u[k], g[k], 1e-2, 10, norm=B.shampoo_gradient_norm(g[k])[0], max_norm=1.0)
+            want[k] = again
+            again = B.AdamW(shapes, state_bits=bits)
+            again.load(*want[k].state())
+            again.step(make(), g[1 - k], 1e-2, 20 + r)
+            want[k] = again
+            torch.cuda.synchronize()
+            assert all(torch.equal(x, y) for x, y in zip(w[k], u[k])), (r, k)
+            assert all(torch.equal(x, y) for x, y in zip(opts[k].state(), want[k].state())), (r, k)
+
+
+def test_refusals():
+    import torch
+    shapes = [(4, 5), (7,)]
+    opt = B.AdamW(shapes)
+    w, g = [torch.zeros(s, device="cuda") for s in shapes], [torch.ones(s, device="cuda") for s in shapes]
+    c = [torch.zeros(s, device="cuda", dtype=torch.bfloat16) for s in shapes]
+    norm = torch.ones((), device="cuda")
+    opt.step(w, g, 1e-3, 5)
+    for call in (lambda: opt.step(w[:1], g, 1e-3, 6), lambda: opt.step(w, [x.bfloat16() for x in g], 1e-3, 6), lambda: opt.step([x.cpu() for x in w], g, 1e-3, 6),
+                 lambda: opt.step([w[0].t(), w[1]], g, 1e-3, 6), lambda: opt.step(w, [g[0][:, :4], g[1]], 1e-3, 6), lambda: opt.step(w, g, 1e-3, 6, copies=w),
+                 lambda: opt.step([torch.zeros((10, 4), device="cuda")[::2].t(), w[1]], g, 1e-3, 6), lambda: opt.step([1, 2], g, 1e-3, 6)):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: opt.step(w, g, 1e-3, 6, norm=norm.cpu()), lambda: opt.step(w, g, 1e-3, 6, norm=norm.double()), lambda: opt.step(w, g, 1e-3, 6, norm=torch.ones((2,), device="cuda")),
+                 lambda: B.shampoo_gradient_norm([]), lambda: B.shampoo_gradient_norm([g[0], c[0]]), lambda: B.shampoo_gradient_norm([g[0].t()]), lambda: B.shampoo_gradient_norm([x.cpu() for x in g]),
+                 lambda: opt.load(torch.zeros((26,), device="cuda"), torch.zeros((27,), device="cuda"))):
+        with pytest.raises(AssertionError):
+            call()
+    for call, code in ((lambda: opt.step(w, g, 1e-3, 5), -5), (lambda: opt.step(w, g, 1e-3, -1), -5), (lambda: opt.step(w, g, math.nan, 6), -3),
+                       (lambda: opt.step(w, g, 1e-3, 6, norm=norm, max_norm=0.0), -3), (lambda: opt.step(w, g, 1e-3, 6, norm=norm, max_norm=math.nan), -3),
+                       (lambda: B.AdamW(shapes, beta1=1.0), -3), (lambda: B.AdamW(shapes, state_bits=16), -3), (lambda: B.AdamW(shapes, epsilon=0.0), -3), (lambda: B.AdamW([]), -2)):
+        with pytest.raises(B.ShampooError) as e:
+            call()
+        assert e.value.code == code
+    half = B.AdamW(shapes, param_dtype=B.GRAD_BF16)
+    with pytest.raises(B.ShampooError):
+        half.step(c, g, 1e-3, 0, copies=[x.clone() for x in c])
+    moved = 1e-3 * (0.1 / (1 - 0.9 ** 6)) / math.sqrt(0.001 / (1 - 0.999 ** 6))       # by the one step that was taken
+    assert all(float(x.abs().max()) == pytest.approx(moved, rel=1e-4) for x in w)
+    opt.step(w, g, 1e-3, 6, norm=norm, max_norm=math.inf)
+    opt.destroy()
+    with pytest.raises(B.ShampooError):
+        opt.step(w, g, 1e-3, 7)
+
+
+def test_indices_beyond_32_bits():
+    """A tensor of 2^32 + 300 elements behind a small one; what lies at its ends and around 2^31 and 2^32 against the definition"""
+    import torch
+    n = (1 << 32) + 300
+    shapes = [(5,), (n,)]
+    w = [torch.zeros(s, device="cuda", dtype=torch.bfloat16) for s in shapes]
+    g = [torch.zeros(s, device="cuda", dtype=torch.bfloat16) for s in shapes]
+    opt = B.AdamW(shapes, state_bits=8, param_dtype=B.GRAD_BF16, grad_dtype=B.GRAD_BF16)
+    spots = [(0, 1024), ((1 << 31) - 512, 1024), ((1 << 32) - 1024, 1024), ((1 << 32), 300)]
+    for at, k in spots:
+        w[1][at:at + k] = torch.randn((k,), device="cuda").bfloat16()
+        g[1][at:at + k] = torch.randn((k,), device="cuda").bfloat16()
+    w0 = [flat(w[1][at:at + k]) for at, k in spots]
+    opt.step(w, g, 1e-2, 9)
+    m, v = opt.state()
+    model = Model([(1,)])
+    square = 0.0
+    for (at, k), x0 in zip(spots, w0):
+        gs = flat(g[1][at:at + k])
+        square += float((gs * gs).sum())
+        wm, wv, ww, em, ev, ew = model.step(0, x0, gs, 0 * gs, 0 * gs, 1e-2, 9)
+        om, ov, ow = offsets(5 + at, k, 9)
+        rounded8(flat(m[5 + at:5 + at + k]), wm, em, 14, om, at)
+        rounded8(flat(v[5 + at:5 + at + k]), wv, ev, 30, ov, at)
+        unit = np.ldexp(1.0, np.frexp(ww)[1] - 8)
+        got = flat(w[1][at:at + k])
+        low, high = (held_range(ww, ew, unit, ow, s)[0] for s in (-1, 1))
+        assert ((np.abs(got) >= low * (1 - 1e-15)) & (np.abs(got) <= high * (1 + 1e-15))).all()
+    norm, norms = B.shampoo_gradient_norm(g)
+    assert abs(float(norm) - math.sqrt(square)) <= 2 * U * math.sqrt(square) and float(norms[0]) == 0 and float(norms[1]) == float(norm)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("shapes", [[(1,)], [(0,), (3, 5), (0,)], [(129,)] * 191 + [(0,)], [(77,)] * 192, [(0,)] * 200 + [(5,)], [(k % 50 + 1, 41) for k in range(577)],
+                                    [(65536 * 3 + 1,), (2048,), (2049,)], [(3000001,), (7,)], [(0,)]])
+def test_norms(shapes, dtype):
+    """Products are exact in 64 bits, sums off by 2^-53 each: the float32 result is the rounded one (u, and a little for what is next to a border)"""
+    import torch
+    dtype = getattr(torch, dtype)
+    total = sum(int(np.prod(s)) for s in shapes)
+    x = (torch.randn((total + 1,), device="cuda") * torch.randn((total + 1,), device="cuda").mul_(3).exp_()).to(dtype)
+    g, at = [], 1
+    for s in shapes:
+        g.append(x[at:at + int(np.prod(s))].view(s))
+        at += int(np.prod(s))
+    norm, norms = B.shampoo_gradient_norm(g)
+    assert norm.shape == () and norms.shape == (len(shapes),) and norm.dtype == norms.dtype == torch.float32
+    each = [float(y.double().square().sum()) for y in g]
+    for got, want in zip([norm] + list(norms.cpu()), [math.sqrt(sum(each))] + [math.sqrt(y) for y in each]):
+        assert abs(float(got) - want) <= U * 1.001 * want
+    again = B.shampoo_gradient_norm(g)
+    assert torch.equal(norm, again[0]) and torch.equal(norms, again[1])
+
+
+def test_norms_at_the_ends_of_float32():
+    import torch
+    for value, want in ((1e30, 1e32), (1e-30, 1e-28), (3e38, math.inf), (1e-44, None), (math.nan, math.nan), (-math.inf, math.inf)):
+        g = torch.full((10000,), value, device="cuda")
+        got = float(B.shampoo_gradient_norm([g])[0])
+        want = float(g[0].double()) * 100.0 if want is None else want
+        assert (math.isnan(got) and math.isnan(want)) or got == want or abs(got - want) <= 2e-7 * want
+
+
+def test_a_training_step_of_all_together():
+    """Logits of a linear head; log probabilities with their gradient; gradients of head and input; their norm; AdamW.  Against the same in 64 bits from the
+    same bf16 tensors: products of 256 bf16 values in float32 (torch's), the logits' gradient rounded to float32: 1e-4 of the norm covers sums of 256 and 4096
+    terms (4096 u = 2.4e-4 at worst, a tenth of it as it comes); the update m / sqrt(v) of a first step is sign(g) (lr), which small gradients' errors
+    do not turn: what is compared is m, linear in the gradient."""
+    import torch
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(4)
+    n, d, v = 512, 256, 4096
+    x = torch.randn((n, d), generator=gen, device="cuda")
+    w = torch.randn((v, d), generator=gen, device="cuda") * 0.1
+    tokens = torch.randint(0, v, (n,), generator=gen, device="cuda")
+    advantage = torch.randn((n,), generator=gen, device="cuda") / n
+    opt = B.AdamW([(v, d)], state_bits=32)
+    z = x @ w.t()
+    r = B.shampoo_log_probs(z, tokens, top=4)
+    dz = B.shampoo_log_probs_grad(z, tokens, r, -advantage, torch.full((n,), -0.01 / n, device="cuda"), out=z)
+    dw = dz.t() @ x
+    norm, _ = B.shampoo_gradient_norm([dw])
+    w0 = w.double().clone().requires_grad_()
+    lp = torch.log_softmax(x.double() @ w0.t(), 1)
+    loss = -(advantage.double() * lp.gather(1, tokens[:, None])[:, 0]).sum() - 0.01 / n * torch.special.entr(torch.exp(lp)).sum()
+    want = torch.autograd.grad(loss, w0)[0]
+    assert float((dw.double() - want).norm() / want.norm()) < 1e-4
+    opt.step([w], [dw], 1e-3, 0, norm=norm, max_norm=float(want.norm()) / 2)
+    m, _ = opt.state()
+    assert float((m.view(v, d).double() - 0.05 * want).norm() / (0.05 * want).norm()) < 1.1e-4
