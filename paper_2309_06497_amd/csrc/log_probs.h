@@ -67,51 +67,245 @@ __device__ __forceinline__ RowStatistics row_statistics(const SoftSums &t) {
   return r;
 }
 
-// A workgroup per row.
-template <typename T> __global__ __launch_bounds__(256) void log_probs_kernel(const LogProbsArgs g) {
-  __shared__ SoftSums part[4];
-  __shared__ uint64_t best[4];
-  const int64_t i = g.row0 + blockIdx.x;
-  const T *z = static_cast<const T *>(g.z) + i * g.ld;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  SoftSums t = {-INFINITY, 0.f, 0.f};
-  for (int v = threadIdx.x; v < g.classes; v += 256) {
-    const float x = load8(z, v, v + 1).v[0];
-    t = join_soft(t, {x, 1.f, 0.f}, g.c);
-    if (x != x) t.s = x;
-    if (x == INFINITY) t.s = NAN;
+// Keys of which every thread of a workgroup has N (0: none; no two others alike): a bound that `top` to chosen_of(top) of them reach, or all where there are
+// no more.  A search by halves below `above`, which none reaches; counts: two sets of four.
+constexpr int LP_CHOSEN = 2 * LP_MAX_TOP + 16, LP_CANDIDATES = 1024;
+__device__ __forceinline__ int chosen_of(int top) { return 2 * top + 16; }
+__device__ __forceinline__ int count_256(int mine, int (*counts)[4], int &turn) {
+  if ((threadIdx.x & 63) == 0) counts[turn][threadIdx.x >> 6] = mine;
+  __syncthreads();
+  const int all = counts[turn][0] + counts[turn][1] + counts[turn][2] + counts[turn][3];
+  turn ^= 1;
+  return all;
+}
+template <typename Count> __device__ __forceinline__ uint64_t bound_of(uint64_t lowest, uint64_t above, int least, int most, Count &&count) {
+  if (count(lowest) <= most) return lowest;
+  // from the largest on, in steps that grow: an eighth of a binade first
+  uint64_t lo = lowest, hi = above, step = (uint64_t)1 << 52;
+  while (hi - lo > 1) {
+    const uint64_t mid = step != 0 && hi - lo > step ? hi - step : lo + (hi - lo) / 2;
+    const int n = count(mid);
+    if (n < least) { hi = mid; step <<= 1; }
+    else if (n > most) { lo = mid; step = 0; }
+    else return mid;
   }
+  return lo;
+}
+template <int N> __device__ __forceinline__ uint64_t bound_of_keys(const uint64_t (&key)[N], uint64_t above, int top, int (*counts)[4], int &turn) {
+  return bound_of(1, above, top, chosen_of(top), [&](uint64_t bound) {
+    int mine = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) mine += __popcll(__ballot(key[e] >= bound));
+    return count_256(mine, counts, turn);
+  });
+}
+// Candidates in LDS in their order: by how many are larger.  put(rank, key) for the first `top` of them, key 0 where there are fewer.
+template <typename Put> __device__ __forceinline__ void put_in_order(const uint64_t *candidate, int n, int top, Put &&put) {
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const uint64_t key = candidate[i];
+    int rank = 0;
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) rank += candidate[j] > key ? 1 : 0;
+    if (rank < top) put(rank, key);
+  }
+  for (int i = n + threadIdx.x; i < top; i += 256) put(i, (uint64_t)0);
+}
+
+// A part of a row, one behind the other: `pieces` of eight logits for each thread, 2048 logits apart.
+constexpr int LP_STRIPS = 4, LP_MAX_PIECES = 64, LP_MAX_PARTS = 64, LP_STEP = 2048;
+constexpr float LP_SLACK = 8.f;            // x may be that far above its reference
+
+// One workgroup per part.  One pass: sums about a reference that follows the largest at a distance, so that it hardly ever moves; and of every strip of pieces that a
+// thread reads the largest logit and the first piece that has it.  The k largest strips hold the k most probable tokens (the first `top` keys of strips
+// are tokens of their own, and no token of another strip comes before any of them), so that these strips alone are read again, and what reaches the bound is put in order.
+// parts > 1: sums and keys of the part go to `sums` and `keys`, and log_probs_join_kernel ends the row.
+struct LogPartArgs { LogProbsArgs g; int32_t parts, pieces; SoftSums *sums; uint64_t *keys; };
+
+__device__ __forceinline__ void put_row(const LogProbsArgs &g, int64_t i, const RowStatistics &r) {
+  if (threadIdx.x == 0) { g.stats[i] = r; g.entropy[i] = r.entropy; }
+}
+template <typename T> __device__ __forceinline__ void put_given(const LogProbsArgs &g, int64_t i, const RowStatistics &r, int j) {
+  const int64_t tok = g.tokens[i * g.m + j];
+  const T *z = static_cast<const T *>(g.z) + i * g.ld;
+  g.log_probs[i * g.m + j] = tok >= 0 && tok < g.classes ? log_prob_of(load8(z, (int)tok, (int)tok + 1).v[0], r, g.tau) : 0.f;
+}
+__device__ __forceinline__ void put_top(const LogProbsArgs &g, int64_t i, const RowStatistics &r, int rank, uint64_t key) {
+  g.top_tokens[i * g.top + rank] = key ? key_token(key) : -1;
+  g.top_log_probs[i * g.top + rank] = log_prob_of(key ? key_logit(key) : -INFINITY, r, g.tau);
+}
+
+template <typename T, bool TOP> __global__ __launch_bounds__(256) void log_probs_kernel(const LogPartArgs a) {
+  constexpr int AHEAD = 4;
+  __shared__ SoftSums part_sums[4];
+  const LogProbsArgs &g = a.g;
+  const int64_t unit = g.row0 + blockIdx.x / (uint32_t)a.parts;
+  const int part = (int)(blockIdx.x % (uint32_t)a.parts), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const T *z = static_cast<const T *>(g.z) + unit * g.ld;
+  const int begin = part * a.pieces * LP_STEP, end = min(g.classes, begin + a.pieces * LP_STEP);
+  const int per_strip = (a.pieces + LP_STRIPS - 1) / LP_STRIPS;
+
+  float ref = -INFINITY, from = 0.f, s = 0.f, w = 0.f;         // from: ref, or 0 while there is none
+  float largest[LP_STRIPS];
+  int at[LP_STRIPS];
+#pragma unroll
+  for (int k = 0; k < LP_STRIPS; ++k) { largest[k] = -INFINITY; at[k] = 0; }
+  const auto take = [&](const f32x8 &x, int piece, float &top, int &top_at) {
+    float m = fmaxf(fmaxf(fmaxf(x.v[0], x.v[1]), fmaxf(x.v[2], x.v[3])), fmaxf(fmaxf(x.v[4], x.v[5]), fmaxf(x.v[6], x.v[7])));
+    if (m > top) { top = m; top_at = piece; }
+    if (__any((m - ref) * g.c > LP_SLACK)) {
+      const float next = fmaxf(ref, m);
+      if (ref != -INFINITY) {
+        const float d = fmaxf((ref - next) * g.c, LP_NOTHING), f = __builtin_amdgcn_exp2f(d);
+        w = f * fmaf(d, s, w);
+        s *= f;
+      }
+      ref = next;
+      from = next == -INFINITY ? 0.f : next;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float d = (x.v[e] - from) * g.c, p = __builtin_amdgcn_exp2f(d);
+      s += p;
+      w = fmaf(p, fmaxf(d, LP_NOTHING), w);
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < LP_STRIPS; ++k) {
+    const int first = k * per_strip, last = min(a.pieces, first + per_strip);
+    for (int q = first; q < last; q += AHEAD) {
+      const int c = begin + q * LP_STEP + tid * 8;
+      if (begin + q * LP_STEP >= end) break;
+      Raw8<T> raw[AHEAD];
+      if (q + AHEAD <= last && begin + (q + AHEAD) * LP_STEP <= end) {
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) raw[e] = raw_load8(z, c + e * LP_STEP, 0x7fffffff);
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) take(expand8(raw[e]), q + e, largest[k], at[k]);
+      } else {
+        for (int e = 0; e < AHEAD && q + e < last; ++e) {
+          const int o = c + e * LP_STEP;
+          if (o >= end) break;
+          f32x8 x = load8(z, o, end);
+#pragma unroll
+          for (int v = 0; v < 8; ++v)
+            if (o + v >= end) x.v[v] = -INFINITY;
+          take(x, q + e, largest[k], at[k]);
+        }
+      }
+    }
+  }
+  SoftSums t = {ref, s, w};
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) t = join_soft(t, {__shfl_xor(t.m, o, 64), __shfl_xor(t.s, o, 64), __shfl_xor(t.w, o, 64)}, g.c);
-  if (lane == 0) part[wave] = t;
+  if (lane == 0) part_sums[wave] = t;
   __syncthreads();
-  t = part[0];
-  for (int k = 1; k < 4; ++k) t = join_soft(t, part[k], g.c);
-  const RowStatistics r = row_statistics(t);
-  if (threadIdx.x == 0) { g.stats[i] = r; g.entropy[i] = r.entropy; }
-  if ((int)threadIdx.x < g.m) {
-    const int64_t tok = g.tokens[i * g.m + threadIdx.x];
-    g.log_probs[i * g.m + threadIdx.x] = tok >= 0 && tok < g.classes ? log_prob_of(load8(z, (int)tok, (int)tok + 1).v[0], r, g.tau) : 0.f;
-  }
-  uint64_t last = ~0ull;
-  for (int k = 0; k < g.top; ++k) {
-    uint64_t key = 0;
-    for (int v = threadIdx.x; v < g.classes; v += 256) {
-      const uint64_t q = logit_key(load8(z, v, v + 1).v[0], v);
-      if (q < last && q > key) key = q;
-    }
+  t = part_sums[0];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) { const uint64_t q = __shfl_xor((unsigned long long)key, o, 64); key = q > key ? q : key; }
+  for (int k = 1; k < 4; ++k) t = join_soft(t, part_sums[k], g.c);
+  const RowStatistics r = row_statistics(t);
+  const int64_t out = unit * a.parts + part;
+  if (a.parts == 1) {
+    put_row(g, unit, r);
+    if (tid < g.m) put_given<T>(g, unit, r, tid);
+  } else if (tid == 0) a.sums[out] = t;
+
+  if constexpr (TOP) {
+    __shared__ int counts[2][4], chosen[LP_CHOSEN], n_chosen, n_candidates;
+    __shared__ uint64_t candidate[LP_CANDIDATES];
+    int turn = 0;
+    uint64_t key[LP_STRIPS];
+    float most = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < LP_STRIPS; ++k) { key[k] = logit_key(largest[k], begin + at[k] * LP_STEP + tid * 8); most = fmaxf(most, largest[k]); }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
+    __syncthreads();                       // part_sums have been read
+    if (lane == 0) part_sums[wave].m = most;
+    if (tid == 0) n_chosen = n_candidates = 0;
     __syncthreads();
-    if (lane == 0) best[wave] = key;
+    most = fmaxf(fmaxf(part_sums[0].m, part_sums[1].m), fmaxf(part_sums[2].m, part_sums[3].m));
+    const uint64_t above = logit_key(most, 0) + 1;
+    uint64_t bound = bound_of_keys(key, above, g.top, counts, turn);
+#pragma unroll
+    for (int k = 0; k < LP_STRIPS; ++k)
+      if (key[k] >= bound) { const int n = atomicAdd(&n_chosen, 1); if (n < LP_CHOSEN) chosen[n] = k * 256 + tid; }
     __syncthreads();
-    for (int w = 0; w < 4; ++w) key = best[w] > key ? best[w] : key;
-    if (threadIdx.x == 0) {
-      g.top_tokens[i * g.top + k] = key ? key_token(key) : -1;
-      g.top_log_probs[i * g.top + k] = log_prob_of(key ? key_logit(key) : -INFINITY, r, g.tau);
+    const int strips = min(n_chosen, LP_CHOSEN), again = strips * per_strip;
+    // the chosen strips' logits
+    const auto each = [&](auto &&f) {
+      for (int i = tid; i < again; i += 256) {
+        const int u = i / strips, strip = chosen[i - u * strips], q = (strip >> 8) * per_strip + u, o = begin + q * LP_STEP + (strip & 255) * 8;
+        if (q >= min(a.pieces, ((strip >> 8) + 1) * per_strip) || o >= end) continue;
+        const f32x8 x = load8(z, o, end);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (o + e < end) f(logit_key(x.v[e], o + e));
+      }
+    };
+    // a bound that is a strip's counts its whole piece: its other tokens may come before the next strip's
+    each([&](uint64_t k) {
+      if (k && (k | 7) >= bound) { const int n = atomicAdd(&n_candidates, 1); if (n < LP_CANDIDATES) candidate[n] = k; }
+    });
+    __syncthreads();
+    if (n_candidates > LP_CANDIDATES) {    // many tokens of one strip: a bound among the tokens themselves
+      bound = bound_of(max(bound & ~(uint64_t)7, (uint64_t)1), above, g.top, LP_CANDIDATES, [&](uint64_t b) {
+        int mine = 0;
+        each([&](uint64_t k) { mine += k >= b ? 1 : 0; });
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) mine += __shfl_xor(mine, o, 64);
+        return count_256(mine, counts, turn);
+      });
+      __syncthreads();
+      if (tid == 0) n_candidates = 0;
+      __syncthreads();
+      each([&](uint64_t k) {
+        if (k >= bound) { const int n = atomicAdd(&n_candidates, 1); if (n < LP_CANDIDATES) candidate[n] = k; }
+      });
+      __syncthreads();
     }
-    last = key;
+    put_in_order(candidate, min(n_candidates, LP_CANDIDATES), g.top, [&](int rank, uint64_t k) {
+      if (a.parts == 1) put_top(g, unit, r, rank, k); else a.keys[out * g.top + rank] = k;
+    });
   }
+}
+
+// The parts of a row together: sums in order, and of the keys those that reach a bound.
+template <typename T> __global__ __launch_bounds__(256) void log_probs_join_kernel(const LogPartArgs a) {
+  constexpr int N = LP_MAX_PARTS * LP_MAX_TOP / 256;
+  __shared__ int counts[2][4], n_candidates;
+  __shared__ uint64_t candidate[LP_CHOSEN];
+  const LogProbsArgs &g = a.g;
+  const int64_t i = g.row0 + blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63;
+  SoftSums t = {-INFINITY, 0.f, 0.f};
+  if (lane < a.parts) t = a.sums[i * a.parts + lane];
+  uint64_t key[N];
+  const int n = a.parts * g.top;
+#pragma unroll
+  for (int e = 0; e < N; ++e) key[e] = e * 256 + tid < n ? a.keys[i * n + e * 256 + tid] : 0;
+  if (tid == 0) n_candidates = 0;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) t = join_soft(t, {__shfl_xor(t.m, o, 64), __shfl_xor(t.s, o, 64), __shfl_xor(t.w, o, 64)}, g.c);
+  const RowStatistics r = row_statistics(t);
+  put_row(g, i, r);
+  if (tid < g.m) put_given<T>(g, i, r, tid);
+  if (g.top == 0) return;
+  __shared__ uint64_t part_most[4];
+  uint64_t most = 0;
+#pragma unroll
+  for (int e = 0; e < N; ++e) most = max(most, key[e]);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) most = max(most, (uint64_t)__shfl_xor((unsigned long long)most, o, 64));
+  if (lane == 0) part_most[tid >> 6] = most;
+  __syncthreads();
+  most = max(max(part_most[0], part_most[1]), max(part_most[2], part_most[3]));
+  int turn = 0;
+  const uint64_t bound = bound_of_keys(key, most + 1, g.top, counts, turn);
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (key[e] >= bound) { const int k = atomicAdd(&n_candidates, 1); if (k < LP_CHOSEN) candidate[k] = key[e]; }
+  __syncthreads();
+  put_in_order(candidate, min(n_candidates, LP_CHOSEN), g.top, [&](int rank, uint64_t k) { put_top(g, i, r, rank, k); });
 }
 
 struct LogProbsGradArgs {
@@ -120,16 +314,18 @@ struct LogProbsGradArgs {
   const float *a, *b;                      // gradients of the log probabilities [rows][m] and of the entropy [rows]; each may be null
   void *dz; int64_t ld_dz;                 // may be z
   float c, tau;
-  int32_t classes, m;
+  int32_t classes, m, parts, part_len;     // part_len: classes of a part, a multiple of LP_STEP
   int64_t row0;
 };
-// A workgroup per row.  A token's own part is added by the thread of its first appearance, with those of all others, behind the row's other values.
+// A workgroup per part of a row.  A token's own part is added by the thread of its first appearance, with those of all others, behind the row's other values.
 template <typename T> __global__ __launch_bounds__(256) void log_probs_grad_kernel(const LogProbsGradArgs g) {
   __shared__ int32_t token[LP_MAX_TOKENS];
   __shared__ float a[LP_MAX_TOKENS];
-  const int64_t i = g.row0 + blockIdx.x;
+  const int64_t i = g.row0 + blockIdx.x / (uint32_t)g.parts;
+  const int begin = (int)(blockIdx.x % (uint32_t)g.parts) * g.part_len, end = min(g.classes, begin + g.part_len);
   const T *z = static_cast<const T *>(g.z) + i * g.ld;
   T *dz = static_cast<T *>(g.dz) + i * g.ld_dz;
+  if (begin >= end) return;
   const RowStatistics r = g.stats[i];
   const int j = threadIdx.x;
   if (j < LP_MAX_TOKENS) {
@@ -140,7 +336,7 @@ template <typename T> __global__ __launch_bounds__(256) void log_probs_grad_kern
   }
   __syncthreads();
   float all = 0.f, own = 0.f;
-  bool first = j < LP_MAX_TOKENS && token[j] >= 0;
+  bool first = j < LP_MAX_TOKENS && token[j] >= begin && token[j] < end;
   for (int k = 0; k < g.m; ++k) {
     all += a[k];
     if (first && token[k] == token[j]) { own += a[k]; if (k < j) first = false; }
@@ -155,7 +351,7 @@ template <typename T> __global__ __launch_bounds__(256) void log_probs_grad_kern
   float at_token = 0.f;
   if (first) at_token = value(load8(z, token[j], token[j] + 1).v[0]) + (r.inv_s != 0.f ? g.tau * own : 0.f);
   __syncthreads();
-  for (int v = threadIdx.x * 8; v < g.classes; v += 2048) {
+  for (int v = begin + threadIdx.x * 8; v < end; v += LP_STEP) {
     f32x8 x = load8(z, v, g.classes);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x.v[e] = value(x.v[e]);

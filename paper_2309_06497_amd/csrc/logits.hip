@@ -25,13 +25,43 @@ int check(const shampoo_logits &c) {
 // 1 / T over log 2, of a T whose reciprocal float32 holds
 float exponent_scale(float inverse_temperature) { return (float)((double)inverse_temperature * 1.4426950408889634); }
 
-// rows at a time
-template <typename Launch> int by_rows(int64_t rows, Launch &&launch) {
-  for (int64_t r = 0; r < rows; r += MAX_BLOCKS) {
-    launch(r, dim3((unsigned)std::min(MAX_BLOCKS, rows - r)));
+// Parts of a row: what one workgroup takes at most, and where there are few rows as many as give four workgroups to every CU, of 2048 classes at least
+constexpr int64_t WORKGROUPS = 1024;
+int32_t parts_of(int64_t rows, int32_t classes, int64_t most_pieces, int64_t most_parts, int32_t &pieces) {
+  const int64_t all = (classes + LP_STEP - 1) / LP_STEP;
+  const int64_t wanted = std::max((all + most_pieces - 1) / most_pieces, std::min(most_parts, (WORKGROUPS + rows - 1) / std::max<int64_t>(rows, 1)));
+  pieces = (int32_t)((all + wanted - 1) / wanted);
+  return (int32_t)((all + pieces - 1) / pieces);
+}
+size_t layout(const shampoo_logits &c, void *workspace, LogPartArgs &a) {
+  a.parts = parts_of(c.rows, c.classes, LP_MAX_PIECES, LP_MAX_PARTS, a.pieces);
+  Arena at(workspace);
+  if (a.parts > 1) {
+    a.sums = at.take<SoftSums>((size_t)(c.rows * a.parts));
+    a.keys = at.take<uint64_t>((size_t)(c.rows * a.parts * c.top));
+  }
+  return at.used;
+}
+
+// rows at a time, `parts` workgroups each
+template <typename Launch> int by_rows(int64_t rows, int32_t parts, Launch &&launch) {
+  const int64_t at_once = MAX_BLOCKS / parts;
+  for (int64_t r = 0; r < rows; r += at_once) {
+    launch(r, (unsigned)std::min(at_once, rows - r));
     HIP_TRY(hipGetLastError());
   }
   return SHAMPOO_OK;
+}
+template <typename T> int launch_log_probs(LogPartArgs a, int64_t rows, hipStream_t s) {
+  TRY(by_rows(rows, a.parts, [&](int64_t r, unsigned n) {
+    a.g.row0 = r;
+    if (a.g.top > 0) log_probs_kernel<T, true><<<dim3(n * a.parts), 256, 0, s>>>(a); else log_probs_kernel<T, false><<<dim3(n * a.parts), 256, 0, s>>>(a);
+  }));
+  if (a.parts == 1) return SHAMPOO_OK;
+  return by_rows(rows, 1, [&](int64_t r, unsigned n) {
+    a.g.row0 = r;
+    log_probs_join_kernel<T><<<dim3(n), 256, 0, s>>>(a);
+  });
 }
 
 }  // namespace
@@ -39,7 +69,8 @@ template <typename Launch> int by_rows(int64_t rows, Launch &&launch) {
 extern "C" {
 
 size_t shampoo_log_probs_workspace_bytes(const shampoo_logits *c) {
-  return 0;
+  LogPartArgs a = {};
+  return c && check(*c) == SHAMPOO_OK ? layout(*c, nullptr, a) : 0;
 }
 
 int shampoo_log_probs(const shampoo_logits *c, const void *logits, const int64_t *tokens, float *log_probs, float *entropy, int64_t *top_tokens,
@@ -49,16 +80,14 @@ int shampoo_log_probs(const shampoo_logits *c, const void *logits, const int64_t
   if (c->rows == 0) return SHAMPOO_OK;
   if (!logits || !entropy || !statistics || (c->tokens > 0 && (!tokens || !log_probs)) || (c->top > 0 && (!top_tokens || !top_log_probs))) return SHAMPOO_ERR_NULL;
   if (!aligned(statistics, 16)) return SHAMPOO_ERR_UNSUPPORTED;
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  LogProbsArgs g = {};
+  LogPartArgs a = {};
+  TRY(workspace_ok(workspace, workspace_bytes, layout(*c, workspace, a)));
+  LogProbsArgs &g = a.g;
   g.z = logits; g.ld = c->ld; g.tokens = tokens; g.c = exponent_scale(c->inverse_temperature); g.tau = c->inverse_temperature;
   g.classes = c->classes; g.m = c->tokens; g.top = c->top; g.log_probs = log_probs; g.entropy = entropy; g.top_tokens = top_tokens; g.top_log_probs = top_log_probs;
   g.stats = reinterpret_cast<RowStatistics *>(statistics);
-  return by_rows(c->rows, [&](int64_t r, dim3 grid) {
-    g.row0 = r;
-    if (c->dtype == SHAMPOO_GRAD_F32) log_probs_kernel<float><<<grid, 256, 0, s>>>(g);
-    else log_probs_kernel<uint16_t><<<grid, 256, 0, s>>>(g);
-  });
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return c->dtype == SHAMPOO_GRAD_F32 ? launch_log_probs<float>(a, c->rows, s) : launch_log_probs<uint16_t>(a, c->rows, s);
 }
 
 int shampoo_log_probs_grad(const shampoo_logits *c, const void *logits, const int64_t *tokens, const float *statistics, const float *d_log_probs,
@@ -74,10 +103,13 @@ int shampoo_log_probs_grad(const shampoo_logits *c, const void *logits, const in
   g.z = logits; g.ld = c->ld; g.tokens = tokens; g.stats = reinterpret_cast<const RowStatistics *>(statistics); g.a = d_log_probs; g.b = d_entropy;
   g.dz = d_logits; g.ld_dz = ld_d_logits; g.c = exponent_scale(c->inverse_temperature); g.tau = c->inverse_temperature;
   g.classes = c->classes; g.m = d_log_probs ? c->tokens : 0;
-  return by_rows(c->rows, [&](int64_t r, dim3 grid) {
+  int32_t pieces;
+  g.parts = parts_of(c->rows, c->classes, MAX_CLASSES, MAX_CLASSES, pieces);
+  g.part_len = pieces * LP_STEP;
+  return by_rows(c->rows, g.parts, [&](int64_t r, unsigned n) {
     g.row0 = r;
-    if (c->dtype == SHAMPOO_GRAD_F32) log_probs_grad_kernel<float><<<grid, 256, 0, s>>>(g);
-    else log_probs_grad_kernel<uint16_t><<<grid, 256, 0, s>>>(g);
+    if (c->dtype == SHAMPOO_GRAD_F32) log_probs_grad_kernel<float><<<dim3(n * g.parts), 256, 0, s>>>(g);
+    else log_probs_grad_kernel<uint16_t><<<dim3(n * g.parts), 256, 0, s>>>(g);
   });
 }
 

@@ -121,11 +121,11 @@ def gradient(z, t, a, b, temperature):
     return dz / temperature, (off + spot) / temperature
 
 
-def check_gradient(z, t, a, b, temperature, out=None):
+def check_gradient(z, t, a, b, temperature, got=None):
     import torch
-    r = B.shampoo_log_probs(z, t, temperature=temperature)
     want, off = gradient(z, t, a if a is not None else torch.zeros(t.shape, device=z.device), b, temperature)
-    got = B.shampoo_log_probs_grad(z, t, r, a, b, out=out)
+    if got is None:
+        got = B.shampoo_log_probs_grad(z, t, B.shampoo_log_probs(z, t, temperature=temperature), a, b)
     assert got.dtype == z.dtype and got.shape == z.shape
     half = torch.finfo(z.dtype).eps / 2
     near(got, want, off * (1 + half) + half * want.abs() + 1.2e-38, "gradient")
@@ -393,12 +393,11 @@ def test_offsets_beyond_32_bits():
     tokens = torch.full((n, 1), 3, device="cuda")
     tokens[some] = t
     r = B.shampoo_log_probs(z, tokens, top=5)
-    want = check(y, t, 5, 1.0)
-    assert torch.equal(r.log_probs[some], want.log_probs) and torch.equal(r.top_tokens[some], want.top_tokens) and torch.equal(r.entropy[some], want.entropy)
+    check(y, t, 5, 1.0, B.LogProbs(*(x[some] for x in (r.log_probs, r.entropy, r.top_tokens, r.top_log_probs, r.statistics)), 1.0))
     assert (r.top_tokens[60000] == torch.arange(5, device="cuda")).all()
     a, b = torch.ones((n, 1), device="cuda"), torch.ones((n,), device="cuda")
-    dy = B.shampoo_log_probs_grad(y, t, want, a[:len(some)], b[:len(some)])
-    assert torch.equal(B.shampoo_log_probs_grad(z, tokens, r, a, b, out=z)[some], dy)
+    got = B.shampoo_log_probs_grad(z, tokens, r, a, b, out=z)
+    check_gradient(y, t, a[some], b[some], 1.0, got[some])
 
 
 def test_the_same_call_gives_the_same_bits():
