@@ -9,6 +9,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include "group.h"
 #include "vectors.h"
 
 namespace shampoo {
@@ -30,14 +31,30 @@ struct LogProbsArgs {
   int64_t row0;
 };
 
-// Sums of a part of a row: the largest z, sum of 2^x, sum of x 2^x (x from that z, in units of log 2).  m = -infinity: nothing there.
+// Sums of a part of a row: sum of 2^x and sum of x 2^x, x from z = m in units of log 2.  m = -infinity: nothing there.
 struct SoftSums { float m, s, w; };
-__device__ __forceinline__ SoftSums join_soft(const SoftSums a, const SoftSums b, float c) {
-  const SoftSums hi = a.m >= b.m ? a : b, lo = a.m >= b.m ? b : a;
-  if (lo.m == -INFINITY) return {hi.m, hi.s + (lo.s != lo.s ? lo.s : 0.f), hi.w};
-  const float d = fmaxf((lo.m - hi.m) * c, LP_NOTHING), f = __builtin_amdgcn_exp2f(d);
-  return {hi.m, fmaf(f, lo.s, hi.s), fmaf(f, fmaf(d, lo.s, lo.w), hi.w)};
+// the same about another m, no smaller
+__device__ __forceinline__ SoftSums about(const SoftSums t, float m, float c) {
+  const float d = fmaxf((t.m - m) * c, LP_NOTHING), f = __builtin_amdgcn_exp2f(d);
+  return {m, f * t.s, f * fmaf(d, t.s, t.w)};
 }
+
+// Over the lanes of a wavefront, by moves between lanes that need no LDS; the result in all of them.
+#define LP_DPP(x, ctrl, old) __builtin_amdgcn_update_dpp(old, x, ctrl, 0xf, 0xf, false)
+template <typename F> __device__ __forceinline__ float wave_all(float x, float none, F &&f) {
+  const int o = __float_as_int(none);
+  x = f(x, __int_as_float(LP_DPP(__float_as_int(x), 0x111, o)));          // from 1, 2, 4, 8 lanes before in a row of 16
+  x = f(x, __int_as_float(LP_DPP(__float_as_int(x), 0x112, o)));
+  x = f(x, __int_as_float(LP_DPP(__float_as_int(x), 0x114, o)));
+  x = f(x, __int_as_float(LP_DPP(__float_as_int(x), 0x118, o)));
+  x = f(x, __int_as_float(__builtin_amdgcn_update_dpp(o, __float_as_int(x), 0x142, 0xa, 0xf, false)));   // the last of a row to the next one
+  x = f(x, __int_as_float(__builtin_amdgcn_update_dpp(o, __float_as_int(x), 0x143, 0xc, 0xf, false)));   // of the first half to the second
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+__device__ __forceinline__ float wave_max(float x) { return wave_all(x, -INFINITY, [](float p, float q) { return fmaxf(p, q); }); }
+__device__ __forceinline__ float wave_sum(float x) { return wave_all(x, 0.f, [](float p, float q) { return p + q; }); }
+// how many lanes before this one are in a mask
+__device__ __forceinline__ int lanes_before(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); }
 
 // The order of logits: larger first, of equal ones the lower token.  0: none (masked by -infinity, or NaN).
 __device__ __forceinline__ uint64_t logit_key(float z, uint32_t v) {
@@ -67,63 +84,81 @@ __device__ __forceinline__ RowStatistics row_statistics(const SoftSums &t) {
   return r;
 }
 
-// Keys of which every thread of a workgroup has N (0: none; no two others alike): a bound that `top` to chosen_of(top) of them reach, or all where there are
-// no more.  A search by halves below `above`, which none reaches; counts: two sets of four.
-constexpr int LP_CHOSEN = 2 * LP_MAX_TOP + 16, LP_CANDIDATES = 1024;
-__device__ __forceinline__ int chosen_of(int top) { return 2 * top + 16; }
-__device__ __forceinline__ int count_256(int mine, int (*counts)[4], int &turn) {
-  if ((threadIdx.x & 63) == 0) counts[turn][threadIdx.x >> 6] = mine;
-  __syncthreads();
-  const int all = counts[turn][0] + counts[turn][1] + counts[turn][2] + counts[turn][3];
-  turn ^= 1;
-  return all;
-}
-template <typename Count> __device__ __forceinline__ uint64_t bound_of(uint64_t lowest, uint64_t above, int least, int most, Count &&count) {
+// The k largest keys of many, of which no two are alike: a bound that `top` to at_most(top) of them reach (all, where there are no more), and what reaches it in
+// order.  count(b): how many are >= b.  The search goes from `above`, which none reaches, in steps that grow until enough do (an eighth of a
+// binade first), and by halves from there.
+__device__ __forceinline__ int at_most(int top) { return top + max(16, top / 2); }
+constexpr int LP_CHOSEN = LP_MAX_TOP + LP_MAX_TOP / 2, LP_CANDIDATES = 1024;
+template <typename Key, typename Count> __device__ __forceinline__ Key bound_of(Key lowest, Key above, Key step, int least, int most, Count &&count) {
   if (count(lowest) <= most) return lowest;
-  // from the largest on, in steps that grow: an eighth of a binade first
-  uint64_t lo = lowest, hi = above, step = (uint64_t)1 << 52;
+  Key lo = lowest, hi = above;
   while (hi - lo > 1) {
-    const uint64_t mid = step != 0 && hi - lo > step ? hi - step : lo + (hi - lo) / 2;
+    const Key mid = step != 0 && hi - lo > step ? hi - step : lo + (hi - lo) / 2;
     const int n = count(mid);
     if (n < least) { hi = mid; step <<= 1; }
     else if (n > most) { lo = mid; step = 0; }
     else return mid;
   }
-  return lo;
+  return lo;                             // more than `most` equal ones, where keys are values alone
 }
-template <int N> __device__ __forceinline__ uint64_t bound_of_keys(const uint64_t (&key)[N], uint64_t above, int top, int (*counts)[4], int &turn) {
-  return bound_of(1, above, top, chosen_of(top), [&](uint64_t bound) {
+constexpr uint64_t LP_STEP64 = (uint64_t)1 << 52;
+
+// What a workgroup of W wavefronts needs for that
+template <int W> struct Selection {
+  int counts[2][W], n_chosen, n_candidates;
+  int chosen[LP_CHOSEN];
+  uint64_t candidate[LP_CANDIDATES], last[LP_CHOSEN];
+};
+template <int W> __device__ __forceinline__ int count_all(int mine, Selection<W> &l, int &turn) {
+  if ((threadIdx.x & 63) == 0) l.counts[turn][threadIdx.x >> 6] = mine;
+  __syncthreads();
+  int all = 0;
+#pragma unroll
+  for (int k = 0; k < W; ++k) all += l.counts[turn][k];
+  turn ^= 1;                             // the next count writes elsewhere: one barrier each
+  return all;
+}
+template <int W, int N> __device__ __forceinline__ uint64_t bound_of_keys(const uint64_t (&key)[N], uint64_t above, int top, Selection<W> &l, int &turn) {
+  return bound_of<uint64_t>(1, above, LP_STEP64, top, at_most(top), [&](uint64_t bound) {
     int mine = 0;
 #pragma unroll
     for (int e = 0; e < N; ++e) mine += __popcll(__ballot(key[e] >= bound));
-    return count_256(mine, counts, turn);
+    return count_all(mine, l, turn);
   });
 }
-// Candidates in LDS in their order: by how many are larger.  put(rank, key) for the first `top` of them, key 0 where there are fewer.
-template <typename Put> __device__ __forceinline__ void put_in_order(const uint64_t *candidate, int n, int top, Put &&put) {
-  for (int i = threadIdx.x; i < n; i += 256) {
-    const uint64_t key = candidate[i];
+// put(rank, key) for the first `top` of n keys in LDS, key 0 where there are fewer: four lanes count how many are larger than one of them
+template <int THREADS, typename Put> __device__ __forceinline__ void put_in_order(const uint64_t *keys, int n, int top, int tid, Put &&put) {
+  for (int i0 = 0; i0 < n; i0 += THREADS / 4) {
+    const int i = i0 + (tid >> 2);
+    const uint64_t key = keys[min(i, n - 1)];
     int rank = 0;
 #pragma unroll 4
-    for (int j = 0; j < n; ++j) rank += candidate[j] > key ? 1 : 0;
-    if (rank < top) put(rank, key);
+    for (int j = tid & 3; j < n; j += 4) rank += keys[j] > key ? 1 : 0;
+    rank += __shfl_xor(rank, 1, 64);
+    rank += __shfl_xor(rank, 2, 64);
+    if (i < n && rank < top && (tid & 3) == 0) put(rank, key);
   }
-  for (int i = n + threadIdx.x; i < top; i += 256) put(i, (uint64_t)0);
+  for (int i = n + tid; i < top; i += THREADS) put(i, (uint64_t)0);
+}
+// n candidates in LDS, in order
+template <int W, typename Put> __device__ __forceinline__ void put_candidates(Selection<W> &l, int n, int top, uint64_t above, int &turn, Put &&put) {
+  constexpr int THREADS = 64 * W, N = LP_CANDIDATES / THREADS;
+  const int tid = threadIdx.x;
+  if (n <= LP_CHOSEN) { put_in_order<THREADS>(l.candidate, n, top, tid, put); return; }
+  uint64_t key[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) key[e] = e * THREADS + tid < n ? l.candidate[e * THREADS + tid] : 0;
+  const uint64_t bound = bound_of_keys(key, above, top, l, turn);
+  if (tid == 0) l.n_chosen = 0;
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (key[e] >= bound) { const int k = atomicAdd(&l.n_chosen, 1); if (k < LP_CHOSEN) l.last[k] = key[e]; }
+  __syncthreads();
+  put_in_order<THREADS>(l.last, min(l.n_chosen, LP_CHOSEN), top, tid, put);
 }
 
-// A part of a row, one behind the other: `pieces` of eight logits for each thread, 2048 logits apart.
-constexpr int LP_STRIPS = 4, LP_MAX_PIECES = 64, LP_MAX_PARTS = 64, LP_STEP = 2048;
-constexpr float LP_SLACK = 8.f;            // x may be that far above its reference
-
-// One workgroup per part.  One pass: sums about a reference that follows the largest at a distance, so that it hardly ever moves; and of every strip of pieces that a
-// thread reads the largest logit and the first piece that has it.  The k largest strips hold the k most probable tokens (the first `top` keys of strips
-// are tokens of their own, and no token of another strip comes before any of them), so that these strips alone are read again, and what reaches the bound is put in order.
-// parts > 1: sums and keys of the part go to `sums` and `keys`, and log_probs_join_kernel ends the row.
-struct LogPartArgs { LogProbsArgs g; int32_t parts, pieces; SoftSums *sums; uint64_t *keys; };
-
-__device__ __forceinline__ void put_row(const LogProbsArgs &g, int64_t i, const RowStatistics &r) {
-  if (threadIdx.x == 0) { g.stats[i] = r; g.entropy[i] = r.entropy; }
-}
+__device__ __forceinline__ void put_row(const LogProbsArgs &g, int64_t i, const RowStatistics &r) { g.stats[i] = r; g.entropy[i] = r.entropy; }
 template <typename T> __device__ __forceinline__ void put_given(const LogProbsArgs &g, int64_t i, const RowStatistics &r, int j) {
   const int64_t tok = g.tokens[i * g.m + j];
   const T *z = static_cast<const T *>(g.z) + i * g.ld;
@@ -133,15 +168,115 @@ __device__ __forceinline__ void put_top(const LogProbsArgs &g, int64_t i, const 
   g.top_tokens[i * g.top + rank] = key ? key_token(key) : -1;
   g.top_log_probs[i * g.top + rank] = log_prob_of(key ? key_logit(key) : -INFINITY, r, g.tau);
 }
+// of eight, NaN is passed over
+__device__ __forceinline__ float largest_of(const f32x8 &x) {
+  return fmaxf(fmaxf(fmaxf(x.v[0], x.v[1]), fmaxf(x.v[2], x.v[3])), fmaxf(fmaxf(x.v[4], x.v[5]), fmaxf(x.v[6], x.v[7])));
+}
+// 2^x and x 2^x of eight logits from z = from
+__device__ __forceinline__ void add_soft(const f32x8 &x, float from, float c, float &s, float &w) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float d = (x.v[e] - from) * c, p = __builtin_amdgcn_exp2f(d);
+    s += p;
+    w = fmaf(p, fmaxf(d, LP_NOTHING), w);
+  }
+}
 
-template <typename T, bool TOP> __global__ __launch_bounds__(256) void log_probs_kernel(const LogPartArgs a) {
-  constexpr int AHEAD = 4;
-  __shared__ SoftSums part_sums[4];
+// Up to 512 PIECES classes: a wavefront per row, which stays in registers.
+template <typename T, int PIECES, bool TOP> __global__ __launch_bounds__(256) void log_probs_row_kernel(const LogProbsArgs g, int64_t rows) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t i = g.row0 + (int64_t)blockIdx.x * 4 + wave;
+  if (i >= rows) return;
+  const T *z = static_cast<const T *>(g.z) + i * g.ld;
+  f32x8 x[PIECES];
+  SoftSums t = {-INFINITY, 0.f, 0.f};
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+    x[p] = load8(z, p * 512 + lane * 8, g.classes);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (p * 512 + lane * 8 + e >= g.classes) x[p].v[e] = -INFINITY;
+    t.m = fmaxf(t.m, largest_of(x[p]));
+  }
+  t.m = wave_max(t.m);
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) add_soft(x[p], t.m == -INFINITY ? 0.f : t.m, g.c, t.s, t.w);
+  t.s = wave_sum(t.s); t.w = wave_sum(t.w);
+  const RowStatistics r = row_statistics(t);
+  if (lane == 0) put_row(g, i, r);
+  if (lane < g.m) put_given<T>(g, i, r, lane);
+
+  if constexpr (TOP) {
+    __shared__ uint64_t keys[4][LP_CHOSEN];
+    uint64_t *const candidate = keys[wave];
+    uint32_t order[8 * PIECES];
+#pragma unroll
+    for (int e = 0; e < 8 * PIECES; ++e) order[e] = (uint32_t)(logit_key(x[e >> 3].v[e & 7], 0) >> 32);
+    const auto count = [&](uint32_t bound) {
+      int n = 0;
+#pragma unroll
+      for (int e = 0; e < 8 * PIECES; ++e) n += __popcll(__ballot(order[e] >= bound));
+      return n;
+    };
+    const int most = at_most(g.top);
+    const uint32_t above = (uint32_t)(logit_key(t.m, 0) >> 32) + 1;
+    uint32_t bound = bound_of<uint32_t>(1, above, 1u << 20, g.top, most, count);
+    // more than `most` reach it: those above, and of equal ones the first
+    const bool ties = count(bound) > most;
+    if (ties) ++bound;
+    int n = 0;
+    const auto key = [&](int e) { return (uint64_t)order[e] << 32 | (0xffffffffu - (uint32_t)((e >> 3) * 512 + lane * 8 + (e & 7))); };
+#pragma unroll
+    for (int e = 0; e < 8 * PIECES; ++e) {
+      const bool in = order[e] >= bound;
+      const uint64_t mask = __ballot(in);
+      if (in) candidate[n + lanes_before(mask)] = key(e);
+      n += __popcll(mask);
+    }
+    if (ties) {
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) {
+        int mine = 0, before = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mine += order[8 * p + e] == bound - 1 ? 1 : 0;
+        int all = 0;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const uint64_t mask = __ballot((mine >> b) & 1);
+          before += lanes_before(mask) << b; all += __popcll(mask) << b;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (order[8 * p + e] == bound - 1) {
+            if (n + before < g.top) candidate[n + before] = key(8 * p + e);
+            ++before;
+          }
+        n = min(n + all, g.top);
+      }
+    }
+    wavefront_order();
+    put_in_order<64>(candidate, n, g.top, lane, [&](int rank, uint64_t k) { put_top(g, i, r, rank, k); });
+  }
+}
+
+// A part of a row, one behind the other: `pieces` of eight logits for each thread, one of the workgroup's pieces behind the other.
+constexpr int LP_STRIPS = 4, LP_MAX_PART = 131072, LP_MAX_PARTS = 64, LP_STEP = 2048;
+constexpr float LP_SLACK = 8.f;            // x may be that far above its reference
+
+// One workgroup per part.  One pass: sums about a reference that follows the largest at a distance, so that it hardly ever moves; and of every strip of pieces that a
+// thread reads the largest logit and the first piece that has it.  The k largest strips hold the k most probable tokens (the first `top` keys of strips
+// are tokens of their own, and no token of another strip comes before any of them), so that these strips alone are read again, and what reaches the bound is put in order.
+// parts > 1: sums and keys of the part go to `sums` and `keys`, and log_probs_join_kernel ends the row.
+struct LogPartArgs { LogProbsArgs g; int32_t parts, pieces; SoftSums *sums; uint64_t *keys; };
+
+template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void log_probs_kernel(const LogPartArgs a) {
+  constexpr int AHEAD = 4, STEP = 512 * W;
+  __shared__ float part_m[W], part_most[W], part_s[W], part_w[W];
   const LogProbsArgs &g = a.g;
   const int64_t unit = g.row0 + blockIdx.x / (uint32_t)a.parts;
   const int part = (int)(blockIdx.x % (uint32_t)a.parts), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const T *z = static_cast<const T *>(g.z) + unit * g.ld;
-  const int begin = part * a.pieces * LP_STEP, end = min(g.classes, begin + a.pieces * LP_STEP);
+  const int begin = part * a.pieces * STEP, end = min(g.classes, begin + a.pieces * STEP);
   const int per_strip = (a.pieces + LP_STRIPS - 1) / LP_STRIPS;
 
   float ref = -INFINITY, from = 0.f, s = 0.f, w = 0.f;         // from: ref, or 0 while there is none
@@ -150,40 +285,31 @@ template <typename T, bool TOP> __global__ __launch_bounds__(256) void log_probs
 #pragma unroll
   for (int k = 0; k < LP_STRIPS; ++k) { largest[k] = -INFINITY; at[k] = 0; }
   const auto take = [&](const f32x8 &x, int piece, float &top, int &top_at) {
-    float m = fmaxf(fmaxf(fmaxf(x.v[0], x.v[1]), fmaxf(x.v[2], x.v[3])), fmaxf(fmaxf(x.v[4], x.v[5]), fmaxf(x.v[6], x.v[7])));
+    const float m = largest_of(x);
     if (m > top) { top = m; top_at = piece; }
     if (__any((m - ref) * g.c > LP_SLACK)) {
       const float next = fmaxf(ref, m);
-      if (ref != -INFINITY) {
-        const float d = fmaxf((ref - next) * g.c, LP_NOTHING), f = __builtin_amdgcn_exp2f(d);
-        w = f * fmaf(d, s, w);
-        s *= f;
-      }
+      if (ref != -INFINITY) { const SoftSums t = about({ref, s, w}, next, g.c); s = t.s; w = t.w; }
       ref = next;
       from = next == -INFINITY ? 0.f : next;
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float d = (x.v[e] - from) * g.c, p = __builtin_amdgcn_exp2f(d);
-      s += p;
-      w = fmaf(p, fmaxf(d, LP_NOTHING), w);
-    }
+    add_soft(x, from, g.c, s, w);
   };
 #pragma unroll
   for (int k = 0; k < LP_STRIPS; ++k) {
     const int first = k * per_strip, last = min(a.pieces, first + per_strip);
     for (int q = first; q < last; q += AHEAD) {
-      const int c = begin + q * LP_STEP + tid * 8;
-      if (begin + q * LP_STEP >= end) break;
-      Raw8<T> raw[AHEAD];
-      if (q + AHEAD <= last && begin + (q + AHEAD) * LP_STEP <= end) {
+      const int c = begin + q * STEP + tid * 8;
+      if (begin + q * STEP >= end) break;
+      if (q + AHEAD <= last && begin + (q + AHEAD) * STEP <= end) {
+        Raw8<T> raw[AHEAD];
 #pragma unroll
-        for (int e = 0; e < AHEAD; ++e) raw[e] = raw_load8(z, c + e * LP_STEP, 0x7fffffff);
+        for (int e = 0; e < AHEAD; ++e) raw[e] = raw_load8(z, c + e * STEP, 0x7fffffff);
 #pragma unroll
         for (int e = 0; e < AHEAD; ++e) take(expand8(raw[e]), q + e, largest[k], at[k]);
       } else {
         for (int e = 0; e < AHEAD && q + e < last; ++e) {
-          const int o = c + e * LP_STEP;
+          const int o = c + e * STEP;
           if (o >= end) break;
           f32x8 x = load8(z, o, end);
 #pragma unroll
@@ -194,76 +320,98 @@ template <typename T, bool TOP> __global__ __launch_bounds__(256) void log_probs
       }
     }
   }
-  SoftSums t = {ref, s, w};
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) t = join_soft(t, {__shfl_xor(t.m, o, 64), __shfl_xor(t.s, o, 64), __shfl_xor(t.w, o, 64)}, g.c);
-  if (lane == 0) part_sums[wave] = t;
+  float most = fmaxf(fmaxf(largest[0], largest[1]), fmaxf(largest[2], largest[3]));
+  SoftSums t = {wave_max(ref), 0.f, 0.f};
+  if constexpr (TOP) most = wave_max(most);
+  if (lane == 0) { part_m[wave] = t.m; part_most[wave] = most; }
   __syncthreads();
-  t = part_sums[0];
 #pragma unroll
-  for (int k = 1; k < 4; ++k) t = join_soft(t, part_sums[k], g.c);
+  for (int k = 0; k < W; ++k) { t.m = fmaxf(t.m, part_m[k]); most = fmaxf(most, part_most[k]); }
+  {
+    const SoftSums u = about({ref, s, w}, t.m, g.c);
+    t.s = wave_sum(u.s); t.w = wave_sum(u.w);
+  }
+  if (lane == 0) { part_s[wave] = t.s; part_w[wave] = t.w; }
+  __syncthreads();
+  t.s = t.w = 0.f;
+#pragma unroll
+  for (int k = 0; k < W; ++k) { t.s += part_s[k]; t.w += part_w[k]; }
   const RowStatistics r = row_statistics(t);
   const int64_t out = unit * a.parts + part;
   if (a.parts == 1) {
-    put_row(g, unit, r);
+    if (tid == 0) put_row(g, unit, r);
     if (tid < g.m) put_given<T>(g, unit, r, tid);
   } else if (tid == 0) a.sums[out] = t;
 
   if constexpr (TOP) {
-    __shared__ int counts[2][4], chosen[LP_CHOSEN], n_chosen, n_candidates;
-    __shared__ uint64_t candidate[LP_CANDIDATES];
+    __shared__ Selection<W> l;
     int turn = 0;
+    if (tid == 0) l.n_chosen = l.n_candidates = 0;
     uint64_t key[LP_STRIPS];
-    float most = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < LP_STRIPS; ++k) { key[k] = logit_key(largest[k], begin + at[k] * LP_STEP + tid * 8); most = fmaxf(most, largest[k]); }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
-    __syncthreads();                       // part_sums have been read
-    if (lane == 0) part_sums[wave].m = most;
-    if (tid == 0) n_chosen = n_candidates = 0;
-    __syncthreads();
-    most = fmaxf(fmaxf(part_sums[0].m, part_sums[1].m), fmaxf(part_sums[2].m, part_sums[3].m));
+    for (int k = 0; k < LP_STRIPS; ++k) key[k] = logit_key(largest[k], begin + at[k] * STEP + tid * 8);
     const uint64_t above = logit_key(most, 0) + 1;
-    uint64_t bound = bound_of_keys(key, above, g.top, counts, turn);
+    uint64_t bound = bound_of_keys(key, above, g.top, l, turn);
+    // a wavefront's strips one behind the other
+    uint64_t mask[LP_STRIPS];
+    int mine = 0, place = 0;
 #pragma unroll
-    for (int k = 0; k < LP_STRIPS; ++k)
-      if (key[k] >= bound) { const int n = atomicAdd(&n_chosen, 1); if (n < LP_CHOSEN) chosen[n] = k * 256 + tid; }
+    for (int k = 0; k < LP_STRIPS; ++k) { mask[k] = __ballot(key[k] >= bound); mine += __popcll(mask[k]); }
+    if (lane == 0 && mine > 0) place = atomicAdd(&l.n_chosen, mine);
+    place = __builtin_amdgcn_readfirstlane(place);
+#pragma unroll
+    for (int k = 0; k < LP_STRIPS; ++k) {
+      const int n = place + lanes_before(mask[k]);
+      if (key[k] >= bound && n < LP_CHOSEN) l.chosen[n] = k * 64 * W + tid;
+      place += __popcll(mask[k]);
+    }
     __syncthreads();
-    const int strips = min(n_chosen, LP_CHOSEN), again = strips * per_strip;
-    // the chosen strips' logits
+    const int strips = min(l.n_chosen, LP_CHOSEN), again = strips * per_strip;
+    // eight logits of a chosen strip at a time
     const auto each = [&](auto &&f) {
-      for (int i = tid; i < again; i += 256) {
-        const int u = i / strips, strip = chosen[i - u * strips], q = (strip >> 8) * per_strip + u, o = begin + q * LP_STEP + (strip & 255) * 8;
-        if (q >= min(a.pieces, ((strip >> 8) + 1) * per_strip) || o >= end) continue;
+      for (int i = tid; i < again; i += 64 * W) {
+        const int u = i / strips, strip = l.chosen[i - u * strips], k = strip / (64 * W), q = k * per_strip + u, o = begin + q * STEP + (strip - k * 64 * W) * 8;
+        if (q >= min(a.pieces, (k + 1) * per_strip) || o >= end) continue;
         const f32x8 x = load8(z, o, end);
+        uint64_t keys[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (o + e < end) f(logit_key(x.v[e], o + e));
+        for (int e = 0; e < 8; ++e) keys[e] = o + e < end ? logit_key(x.v[e], o + e) : 0;
+        f(keys);
       }
     };
-    // a bound that is a strip's counts its whole piece: its other tokens may come before the next strip's
-    each([&](uint64_t k) {
-      if (k && (k | 7) >= bound) { const int n = atomicAdd(&n_candidates, 1); if (n < LP_CANDIDATES) candidate[n] = k; }
-    });
-    __syncthreads();
-    if (n_candidates > LP_CANDIDATES) {    // many tokens of one strip: a bound among the tokens themselves
-      bound = bound_of(max(bound & ~(uint64_t)7, (uint64_t)1), above, g.top, LP_CANDIDATES, [&](uint64_t b) {
-        int mine = 0;
-        each([&](uint64_t k) { mine += k >= b ? 1 : 0; });
+    const auto gather = [&](uint64_t b) {
+      each([&](const uint64_t (&k)[8]) {
+        int n = 0;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) mine += __shfl_xor(mine, o, 64);
-        return count_256(mine, counts, turn);
+        for (int e = 0; e < 8; ++e) n += k[e] >= b ? 1 : 0;
+        if (n == 0) return;
+        int to = atomicAdd(&l.n_candidates, n);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (k[e] >= b) { if (to < LP_CANDIDATES) l.candidate[to] = k[e]; ++to; }
       });
       __syncthreads();
-      if (tid == 0) n_candidates = 0;
-      __syncthreads();
-      each([&](uint64_t k) {
-        if (k >= bound) { const int n = atomicAdd(&n_candidates, 1); if (n < LP_CANDIDATES) candidate[n] = k; }
+    };
+    // a strip's key is that of the first token of its piece: the others may come before the next strip's
+    bound = max(bound & ~(uint64_t)7, (uint64_t)1);
+    gather(bound);
+    if (l.n_candidates > LP_CANDIDATES) {  // many tokens of one strip: a bound among the tokens themselves
+      bound = bound_of<uint64_t>(bound, above, LP_STEP64, g.top, LP_CANDIDATES, [&](uint64_t b) {
+        int n = 0;
+        each([&](const uint64_t (&k)[8]) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) n += k[e] >= b ? 1 : 0;
+        });
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) n += __shfl_xor(n, o, 64);
+        return count_all(n, l, turn);
       });
       __syncthreads();
+      if (tid == 0) l.n_candidates = 0;
+      __syncthreads();
+      gather(bound);
     }
-    put_in_order(candidate, min(n_candidates, LP_CANDIDATES), g.top, [&](int rank, uint64_t k) {
+    put_candidates(l, min(l.n_candidates, LP_CANDIDATES), g.top, above, turn, [&](int rank, uint64_t k) {
       if (a.parts == 1) put_top(g, unit, r, rank, k); else a.keys[out * g.top + rank] = k;
     });
   }
@@ -272,40 +420,38 @@ template <typename T, bool TOP> __global__ __launch_bounds__(256) void log_probs
 // The parts of a row together: sums in order, and of the keys those that reach a bound.
 template <typename T> __global__ __launch_bounds__(256) void log_probs_join_kernel(const LogPartArgs a) {
   constexpr int N = LP_MAX_PARTS * LP_MAX_TOP / 256;
-  __shared__ int counts[2][4], n_candidates;
-  __shared__ uint64_t candidate[LP_CHOSEN];
+  __shared__ Selection<4> l;
+  __shared__ float part_most[4];
   const LogProbsArgs &g = a.g;
   const int64_t i = g.row0 + blockIdx.x;
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x, lane = tid & 63, n = a.parts * g.top;
   SoftSums t = {-INFINITY, 0.f, 0.f};
   if (lane < a.parts) t = a.sums[i * a.parts + lane];
   uint64_t key[N];
-  const int n = a.parts * g.top;
+  float most = -INFINITY;
 #pragma unroll
-  for (int e = 0; e < N; ++e) key[e] = e * 256 + tid < n ? a.keys[i * n + e * 256 + tid] : 0;
-  if (tid == 0) n_candidates = 0;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) t = join_soft(t, {__shfl_xor(t.m, o, 64), __shfl_xor(t.s, o, 64), __shfl_xor(t.w, o, 64)}, g.c);
+  for (int e = 0; e < N; ++e) {
+    key[e] = e * 256 + tid < n ? a.keys[i * n + e * 256 + tid] : 0;
+    most = fmaxf(most, key[e] ? key_logit(key[e]) : -INFINITY);
+  }
+  t = about(t, wave_max(t.m), g.c);
+  t.s = wave_sum(t.s); t.w = wave_sum(t.w);
   const RowStatistics r = row_statistics(t);
-  put_row(g, i, r);
+  if (tid == 0) put_row(g, i, r);
   if (tid < g.m) put_given<T>(g, i, r, tid);
   if (g.top == 0) return;
-  __shared__ uint64_t part_most[4];
-  uint64_t most = 0;
-#pragma unroll
-  for (int e = 0; e < N; ++e) most = max(most, key[e]);
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) most = max(most, (uint64_t)__shfl_xor((unsigned long long)most, o, 64));
+  most = wave_max(most);
   if (lane == 0) part_most[tid >> 6] = most;
+  if (tid == 0) l.n_candidates = 0;
   __syncthreads();
-  most = max(max(part_most[0], part_most[1]), max(part_most[2], part_most[3]));
+  most = fmaxf(fmaxf(part_most[0], part_most[1]), fmaxf(part_most[2], part_most[3]));
   int turn = 0;
-  const uint64_t bound = bound_of_keys(key, most + 1, g.top, counts, turn);
+  const uint64_t above = logit_key(most, 0) + 1, bound = bound_of_keys(key, above, g.top, l, turn);
 #pragma unroll
   for (int e = 0; e < N; ++e)
-    if (key[e] >= bound) { const int k = atomicAdd(&n_candidates, 1); if (k < LP_CHOSEN) candidate[k] = key[e]; }
+    if (key[e] >= bound) { const int k = atomicAdd(&l.n_candidates, 1); if (k < LP_CANDIDATES) l.candidate[k] = key[e]; }
   __syncthreads();
-  put_in_order(candidate, min(n_candidates, LP_CHOSEN), g.top, [&](int rank, uint64_t k) { put_top(g, i, r, rank, k); });
+  put_candidates(l, min(l.n_candidates, LP_CANDIDATES), g.top, above, turn, [&](int rank, uint64_t k) { put_top(g, i, r, rank, k); });
 }
 
 struct LogProbsGradArgs {

@@ -25,16 +25,21 @@ int check(const shampoo_logits &c) {
 // 1 / T over log 2, of a T whose reciprocal float32 holds
 float exponent_scale(float inverse_temperature) { return (float)((double)inverse_temperature * 1.4426950408889634); }
 
-// Parts of a row: what one workgroup takes at most, and where there are few rows as many as give four workgroups to every CU, of 2048 classes at least
+// Parts of a row, in steps of `step` classes: what one workgroup takes at most, and where there are few rows as many as give four workgroups to every CU.
 constexpr int64_t WORKGROUPS = 1024;
-int32_t parts_of(int64_t rows, int32_t classes, int64_t most_pieces, int64_t most_parts, int32_t &pieces) {
-  const int64_t all = (classes + LP_STEP - 1) / LP_STEP;
-  const int64_t wanted = std::max((all + most_pieces - 1) / most_pieces, std::min(most_parts, (WORKGROUPS + rows - 1) / std::max<int64_t>(rows, 1)));
+int32_t parts_of(int64_t rows, int32_t classes, int64_t step, int64_t longest, int64_t most_parts, int32_t &pieces) {
+  const int64_t all = (classes + step - 1) / step;
+  const int64_t wanted = std::max((classes + longest - 1) / longest, std::min(most_parts, (WORKGROUPS + rows - 1) / std::max<int64_t>(rows, 1)));
   pieces = (int32_t)((all + wanted - 1) / wanted);
   return (int32_t)((all + pieces - 1) / pieces);
 }
+// Rows that one wavefront keeps in registers; otherwise wavefronts of a workgroup: a row stays whole, without a second launch, from 512 rows on.
+constexpr int32_t SMALL_CLASSES = 2048;
+int wavefronts(int64_t rows) { return rows >= 2048 || rows < 512 ? 4 : rows >= 1024 ? 8 : 16; }
 size_t layout(const shampoo_logits &c, void *workspace, LogPartArgs &a) {
-  a.parts = parts_of(c.rows, c.classes, LP_MAX_PIECES, LP_MAX_PARTS, a.pieces);
+  a.parts = 1;
+  if (c.classes <= SMALL_CLASSES) return 0;
+  a.parts = parts_of(c.rows, c.classes, 512 * wavefronts(c.rows), LP_MAX_PART, c.rows >= 512 ? 1 : LP_MAX_PARTS, a.pieces);
   Arena at(workspace);
   if (a.parts > 1) {
     a.sums = at.take<SoftSums>((size_t)(c.rows * a.parts));
@@ -52,14 +57,29 @@ template <typename Launch> int by_rows(int64_t rows, int32_t parts, Launch &&lau
   }
   return SHAMPOO_OK;
 }
+template <typename T, int W> void launch_parts(const LogPartArgs &a, unsigned n, hipStream_t s) {
+  if (a.g.top > 0) log_probs_kernel<T, W, true><<<dim3(n * a.parts), 64 * W, 0, s>>>(a); else log_probs_kernel<T, W, false><<<dim3(n * a.parts), 64 * W, 0, s>>>(a);
+}
+template <typename T, int PIECES> void launch_rows(const LogProbsArgs &g, unsigned n, hipStream_t s) {
+  const dim3 grid((n + 3) / 4);
+  if (g.top > 0) log_probs_row_kernel<T, PIECES, true><<<grid, 256, 0, s>>>(g, g.row0 + n); else log_probs_row_kernel<T, PIECES, false><<<grid, 256, 0, s>>>(g, g.row0 + n);
+}
 template <typename T> int launch_log_probs(LogPartArgs a, int64_t rows, hipStream_t s) {
+  LogProbsArgs &g = a.g;
   TRY(by_rows(rows, a.parts, [&](int64_t r, unsigned n) {
-    a.g.row0 = r;
-    if (a.g.top > 0) log_probs_kernel<T, true><<<dim3(n * a.parts), 256, 0, s>>>(a); else log_probs_kernel<T, false><<<dim3(n * a.parts), 256, 0, s>>>(a);
+    g.row0 = r;
+    if (g.classes <= 512) launch_rows<T, 1>(g, n, s);
+    else if (g.classes <= 1024) launch_rows<T, 2>(g, n, s);
+    else if (g.classes <= SMALL_CLASSES) launch_rows<T, 4>(g, n, s);
+    else switch (wavefronts(rows)) {
+      case 4: launch_parts<T, 4>(a, n, s); break;
+      case 8: launch_parts<T, 8>(a, n, s); break;
+      default: launch_parts<T, 16>(a, n, s);
+    }
   }));
   if (a.parts == 1) return SHAMPOO_OK;
   return by_rows(rows, 1, [&](int64_t r, unsigned n) {
-    a.g.row0 = r;
+    g.row0 = r;
     log_probs_join_kernel<T><<<dim3(n), 256, 0, s>>>(a);
   });
 }
@@ -104,7 +124,7 @@ int shampoo_log_probs_grad(const shampoo_logits *c, const void *logits, const in
   g.dz = d_logits; g.ld_dz = ld_d_logits; g.c = exponent_scale(c->inverse_temperature); g.tau = c->inverse_temperature;
   g.classes = c->classes; g.m = d_log_probs ? c->tokens : 0;
   int32_t pieces;
-  g.parts = parts_of(c->rows, c->classes, MAX_CLASSES, MAX_CLASSES, pieces);
+  g.parts = parts_of(c->rows, c->classes, LP_STEP, MAX_CLASSES, MAX_CLASSES, pieces);
   g.part_len = pieces * LP_STEP;
   return by_rows(c->rows, g.parts, [&](int64_t r, unsigned n) {
     g.row0 = r;
