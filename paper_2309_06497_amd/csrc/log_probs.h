@@ -88,7 +88,7 @@ __device__ __forceinline__ RowStatistics row_statistics(const SoftSums &t) {
 // order.  count(b): how many are >= b.  The search goes from `above`, which none reaches, in steps that grow until enough do (an eighth of a
 // binade first), and by halves from there.
 __device__ __forceinline__ int at_most(int top) { return top + max(16, top / 2); }
-constexpr int LP_CHOSEN = LP_MAX_TOP + LP_MAX_TOP / 2, LP_CANDIDATES = 1024;
+constexpr int LP_CHOSEN = LP_MAX_TOP + LP_MAX_TOP / 2, LP_CANDIDATES = 512;
 template <typename Key, typename Count> __device__ __forceinline__ Key bound_of(Key lowest, Key above, Key step, int least, int most, Count &&count) {
   if (count(lowest) <= most) return lowest;
   Key lo = lowest, hi = above;
@@ -101,30 +101,68 @@ template <typename Key, typename Count> __device__ __forceinline__ Key bound_of(
   }
   return lo;                             // more than `most` equal ones, where keys are values alone
 }
-constexpr uint64_t LP_STEP64 = (uint64_t)1 << 52;
-
 // What a workgroup of W wavefronts needs for that
 template <int W> struct Selection {
-  int counts[2][W], n_chosen, n_candidates;
-  int chosen[LP_CHOSEN];
+  uint64_t counts[2][W];
+  int n_chosen, n_candidates, chosen[LP_CHOSEN];
   uint64_t candidate[LP_CANDIDATES], last[LP_CHOSEN];
 };
-template <int W> __device__ __forceinline__ int count_all(int mine, Selection<W> &l, int &turn) {
-  if ((threadIdx.x & 63) == 0) l.counts[turn][threadIdx.x >> 6] = mine;
-  __syncthreads();
-  int all = 0;
+// The same by a workgroup, which needs a barrier for every count: four bounds at a time.  mine(b): how many keys of this wavefront are >= b; turn: of the two
+// places for counts, so that one barrier is enough.
+// Key is the value alone (32 bits, compared four times as fast) or all of a key.  False: more than `most` equal ones, of value `found`.
+template <typename Key, int W, typename Mine>
+__device__ __forceinline__ bool bound_of_all(Key lowest, Key above, int least, int most, Selection<W> &l, int &turn, Key &found, Mine &&mine) {
+  Key lo = lowest, hi = above;
+  for (bool first = true;; first = false) {
+    const Key width = hi - lo;
+    if (!first && width <= 1) { found = lo; return false; }
+    Key bound[4];                          // an eighth of a binade below, one, eight, and all; then fifths
 #pragma unroll
-  for (int k = 0; k < W; ++k) all += l.counts[turn][k];
-  turn ^= 1;                             // the next count writes elsewhere: one barrier each
-  return all;
+    for (int j = 0; j < 4; ++j) {
+      const Key down = first ? (j < 3 ? (Key)1 << (8 * sizeof(Key) - 12 + 3 * j) : width) : width > 5 ? width / 5 * (j + 1) : (Key)(j + 1);
+      bound[j] = down < width ? hi - down : first ? lo : lo + 1;
+    }
+    uint64_t packed = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) packed |= (uint64_t)mine(bound[j]) << (16 * j);
+    if ((threadIdx.x & 63) == 0) l.counts[turn][threadIdx.x >> 6] = packed;
+    __syncthreads();
+    packed = 0;
+#pragma unroll
+    for (int k = 0; k < W; ++k) packed += l.counts[turn][k];
+    turn ^= 1;
+    if (first && (int)(packed >> 48) <= most) { found = lo; return true; }
+    bool enough = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int n = (int)(packed >> (16 * j)) & 0xffff;
+      if (enough) continue;
+      if (n < least) { hi = bound[j]; continue; }
+      if (n <= most) { found = bound[j]; return true; }
+      enough = true;
+      lo = bound[j];
+    }
+  }
 }
-template <int W, int N> __device__ __forceinline__ uint64_t bound_of_keys(const uint64_t (&key)[N], uint64_t above, int top, Selection<W> &l, int &turn) {
-  return bound_of<uint64_t>(1, above, LP_STEP64, top, at_most(top), [&](uint64_t bound) {
-    int mine = 0;
+template <int W, int N> __device__ __forceinline__ uint64_t bound_of_keys(const uint64_t (&key)[N], int used, uint64_t above, int top, Selection<W> &l, int &turn) {
+  uint32_t value;
+  const bool done = bound_of_all<uint32_t>(1, (uint32_t)(above >> 32) + 1, top, at_most(top), l, turn, value, [&](uint32_t bound) {
+    int n = 0;
 #pragma unroll
-    for (int e = 0; e < N; ++e) mine += __popcll(__ballot(key[e] >= bound));
-    return count_all(mine, l, turn);
+    for (int e = 0; e < N; ++e)
+      if (e < used) n += __popcll(__ballot((uint32_t)(key[e] >> 32) >= bound));
+    return n;
   });
+  if (done) return (uint64_t)value << 32;
+  uint64_t found;
+  bound_of_all<uint64_t>((uint64_t)value << 32, ((uint64_t)value << 32) + ((uint64_t)1 << 32), top, at_most(top), l, turn, found, [&](uint64_t bound) {
+    int n = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (e < used) n += __popcll(__ballot(key[e] >= bound));
+    return n;
+  });
+  return found;
 }
 // put(rank, key) for the first `top` of n keys in LDS, key 0 where there are fewer: four lanes count how many are larger than one of them
 template <int THREADS, typename Put> __device__ __forceinline__ void put_in_order(const uint64_t *keys, int n, int top, int tid, Put &&put) {
@@ -148,7 +186,7 @@ template <int W, typename Put> __device__ __forceinline__ void put_candidates(Se
   uint64_t key[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) key[e] = e * THREADS + tid < n ? l.candidate[e * THREADS + tid] : 0;
-  const uint64_t bound = bound_of_keys(key, above, top, l, turn);
+  const uint64_t bound = bound_of_keys(key, (n + THREADS - 1) / THREADS, above, top, l, turn);
   if (tid == 0) l.n_chosen = 0;
   __syncthreads();
 #pragma unroll
@@ -164,13 +202,25 @@ template <typename T> __device__ __forceinline__ void put_given(const LogProbsAr
   const T *z = static_cast<const T *>(g.z) + i * g.ld;
   g.log_probs[i * g.m + j] = tok >= 0 && tok < g.classes ? log_prob_of(load8(z, (int)tok, (int)tok + 1).v[0], r, g.tau) : 0.f;
 }
-__device__ __forceinline__ void put_top(const LogProbsArgs &g, int64_t i, const RowStatistics &r, int rank, uint64_t key) {
-  g.top_tokens[i * g.top + rank] = key ? key_token(key) : -1;
+// pad: the key's token is that much too large
+__device__ __forceinline__ void put_top(const LogProbsArgs &g, int64_t i, const RowStatistics &r, int rank, uint64_t key, int pad = 0) {
+  g.top_tokens[i * g.top + rank] = key ? key_token(key) - pad : -1;
   g.top_log_probs[i * g.top + rank] = log_prob_of(key ? key_logit(key) : -INFINITY, r, g.tau);
 }
 // of eight, NaN is passed over
 __device__ __forceinline__ float largest_of(const f32x8 &x) {
   return fmaxf(fmaxf(fmaxf(x.v[0], x.v[1]), fmaxf(x.v[2], x.v[3])), fmaxf(fmaxf(x.v[4], x.v[5]), fmaxf(x.v[6], x.v[7])));
+}
+// Logits that lie before the first of a row up to a multiple of 16 bytes: a row is read from there on, in aligned pieces of eight, of which the first begins with `pad` masked
+// ones.  (Pieces at odd addresses: 2048 x 50001 bf16 in 49.3 us, so in PAD_US.)
+template <typename T> __device__ __forceinline__ int row_pad(const T *z) { return (int)((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T)); }
+// eight logits from o on, -infinity for what is not there
+template <typename T> __device__ __forceinline__ f32x8 load_logits(const T *z, int o, int pad, int end) {
+  f32x8 x;
+  if (o >= pad && o + 8 <= end) return load8(z, o, 0x7fffffff);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x.v[e] = o + e >= pad && o + e < end ? load8(z, o + e, o + e + 1).v[0] : -INFINITY;
+  return x;
 }
 // 2^x and x 2^x of eight logits from z = from
 __device__ __forceinline__ void add_soft(const f32x8 &x, float from, float c, float &s, float &w) {
@@ -276,7 +326,9 @@ template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void
   const int64_t unit = g.row0 + blockIdx.x / (uint32_t)a.parts;
   const int part = (int)(blockIdx.x % (uint32_t)a.parts), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const T *z = static_cast<const T *>(g.z) + unit * g.ld;
-  const int begin = part * a.pieces * STEP, end = min(g.classes, begin + a.pieces * STEP);
+  const int pad = row_pad(z);
+  z -= pad;
+  const int begin = part * a.pieces * STEP, end = min(g.classes + pad, begin + a.pieces * STEP);
   const int per_strip = (a.pieces + LP_STRIPS - 1) / LP_STRIPS;
 
   float ref = -INFINITY, from = 0.f, s = 0.f, w = 0.f;         // from: ref, or 0 while there is none
@@ -301,7 +353,7 @@ template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void
     for (int q = first; q < last; q += AHEAD) {
       const int c = begin + q * STEP + tid * 8;
       if (begin + q * STEP >= end) break;
-      if (q + AHEAD <= last && begin + (q + AHEAD) * STEP <= end) {
+      if (q + AHEAD <= last && begin + (q + AHEAD) * STEP <= end && begin + q * STEP >= pad) {
         Raw8<T> raw[AHEAD];
 #pragma unroll
         for (int e = 0; e < AHEAD; ++e) raw[e] = raw_load8(z, c + e * STEP, 0x7fffffff);
@@ -311,11 +363,7 @@ template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void
         for (int e = 0; e < AHEAD && q + e < last; ++e) {
           const int o = c + e * STEP;
           if (o >= end) break;
-          f32x8 x = load8(z, o, end);
-#pragma unroll
-          for (int v = 0; v < 8; ++v)
-            if (o + v >= end) x.v[v] = -INFINITY;
-          take(x, q + e, largest[k], at[k]);
+          take(load_logits(z, o, pad, end), q + e, largest[k], at[k]);
         }
       }
     }
@@ -351,7 +399,7 @@ template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void
 #pragma unroll
     for (int k = 0; k < LP_STRIPS; ++k) key[k] = logit_key(largest[k], begin + at[k] * STEP + tid * 8);
     const uint64_t above = logit_key(most, 0) + 1;
-    uint64_t bound = bound_of_keys(key, above, g.top, l, turn);
+    uint64_t bound = bound_of_keys(key, LP_STRIPS, above, g.top, l, turn);
     // a wavefront's strips one behind the other
     uint64_t mask[LP_STRIPS];
     int mine = 0, place = 0;
@@ -372,10 +420,10 @@ template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void
       for (int i = tid; i < again; i += 64 * W) {
         const int u = i / strips, strip = l.chosen[i - u * strips], k = strip / (64 * W), q = k * per_strip + u, o = begin + q * STEP + (strip - k * 64 * W) * 8;
         if (q >= min(a.pieces, (k + 1) * per_strip) || o >= end) continue;
-        const f32x8 x = load8(z, o, end);
+        const f32x8 x = load_logits(z, o, pad, end);
         uint64_t keys[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) keys[e] = o + e < end ? logit_key(x.v[e], o + e) : 0;
+        for (int e = 0; e < 8; ++e) keys[e] = logit_key(x.v[e], o + e);
         f(keys);
       }
     };
@@ -396,7 +444,8 @@ template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void
     bound = max(bound & ~(uint64_t)7, (uint64_t)1);
     gather(bound);
     if (l.n_candidates > LP_CANDIDATES) {  // many tokens of one strip: a bound among the tokens themselves
-      bound = bound_of<uint64_t>(bound, above, LP_STEP64, g.top, LP_CANDIDATES, [&](uint64_t b) {
+      const uint64_t from_strips = bound;
+      bound_of_all<uint64_t>(from_strips, above, g.top, LP_CANDIDATES, l, turn, bound, [&](uint64_t b) {
         int n = 0;
         each([&](const uint64_t (&k)[8]) {
 #pragma unroll
@@ -404,7 +453,7 @@ template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void
         });
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) n += __shfl_xor(n, o, 64);
-        return count_all(n, l, turn);
+        return n;
       });
       __syncthreads();
       if (tid == 0) l.n_candidates = 0;
@@ -412,7 +461,7 @@ template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void
       gather(bound);
     }
     put_candidates(l, min(l.n_candidates, LP_CANDIDATES), g.top, above, turn, [&](int rank, uint64_t k) {
-      if (a.parts == 1) put_top(g, unit, r, rank, k); else a.keys[out * g.top + rank] = k;
+      if (a.parts == 1) put_top(g, unit, r, rank, k, pad); else a.keys[out * g.top + rank] = k;
     });
   }
 }
@@ -424,7 +473,7 @@ template <typename T> __global__ __launch_bounds__(256) void log_probs_join_kern
   __shared__ float part_most[4];
   const LogProbsArgs &g = a.g;
   const int64_t i = g.row0 + blockIdx.x;
-  const int tid = threadIdx.x, lane = tid & 63, n = a.parts * g.top;
+  const int tid = threadIdx.x, lane = tid & 63, n = a.parts * g.top, pad = row_pad(static_cast<const T *>(g.z) + i * g.ld);
   SoftSums t = {-INFINITY, 0.f, 0.f};
   if (lane < a.parts) t = a.sums[i * a.parts + lane];
   uint64_t key[N];
@@ -446,12 +495,12 @@ template <typename T> __global__ __launch_bounds__(256) void log_probs_join_kern
   __syncthreads();
   most = fmaxf(fmaxf(part_most[0], part_most[1]), fmaxf(part_most[2], part_most[3]));
   int turn = 0;
-  const uint64_t above = logit_key(most, 0) + 1, bound = bound_of_keys(key, above, g.top, l, turn);
+  const uint64_t above = logit_key(most, 0) + 1, bound = bound_of_keys(key, (n + 255) / 256, above, g.top, l, turn);
 #pragma unroll
   for (int e = 0; e < N; ++e)
     if (key[e] >= bound) { const int k = atomicAdd(&l.n_candidates, 1); if (k < LP_CANDIDATES) l.candidate[k] = key[e]; }
   __syncthreads();
-  put_candidates(l, min(l.n_candidates, LP_CANDIDATES), g.top, above, turn, [&](int rank, uint64_t k) { put_top(g, i, r, rank, k); });
+  put_candidates(l, min(l.n_candidates, LP_CANDIDATES), g.top, above, turn, [&](int rank, uint64_t k) { put_top(g, i, r, rank, k, pad); });
 }
 
 struct LogProbsGradArgs {
@@ -463,24 +512,32 @@ struct LogProbsGradArgs {
   int32_t classes, m, parts, part_len;     // part_len: classes of a part, a multiple of LP_STEP
   int64_t row0;
 };
-// A workgroup per part of a row.  A token's own part is added by the thread of its first appearance, with those of all others, behind the row's other values.
-template <typename T> __global__ __launch_bounds__(256) void log_probs_grad_kernel(const LogProbsGradArgs g) {
-  __shared__ int32_t token[LP_MAX_TOKENS];
-  __shared__ float a[LP_MAX_TOKENS];
-  const int64_t i = g.row0 + blockIdx.x / (uint32_t)g.parts;
-  const int begin = (int)(blockIdx.x % (uint32_t)g.parts) * g.part_len, end = min(g.classes, begin + g.part_len);
+// W = 4: a workgroup per part of a row; W = 1: a wavefront per row, four rows a workgroup, for up to 2048 classes.  A token's own part is added by the thread of its
+// first appearance, with those of all others, behind the row's other values.
+template <typename T, int W> __global__ __launch_bounds__(256) void log_probs_grad_kernel(const LogProbsGradArgs g, int64_t rows) {
+  constexpr int STEP = 512 * W, AHEAD = 2;
+  __shared__ int32_t tokens[4 / W][LP_MAX_TOKENS];
+  __shared__ float coefs[4 / W][LP_MAX_TOKENS];
+  const int which = W == 1 ? threadIdx.x >> 6 : 0, j = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+  const int64_t i = g.row0 + (W == 1 ? (int64_t)blockIdx.x * 4 + which : blockIdx.x / (uint32_t)g.parts);
+  if (i >= rows) return;
+  int32_t *const token = tokens[which];
+  float *const a = coefs[which];
   const T *z = static_cast<const T *>(g.z) + i * g.ld;
   T *dz = static_cast<T *>(g.dz) + i * g.ld_dz;
+  const int pad = row_pad(z);
+  z -= pad; dz -= pad;
+  const int begin = W == 1 ? 0 : (int)(blockIdx.x % (uint32_t)g.parts) * g.part_len, end = min(g.classes + pad, W == 1 ? 0x7fffffff : begin + g.part_len);
   if (begin >= end) return;
   const RowStatistics r = g.stats[i];
-  const int j = threadIdx.x;
+  const auto meet = [&]() { if constexpr (W == 1) { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup"); __builtin_amdgcn_wave_barrier(); } else __syncthreads(); };
   if (j < LP_MAX_TOKENS) {
     const int64_t t = j < g.m && g.a ? g.tokens[i * g.m + j] : -1;
     const bool valid = t >= 0 && t < g.classes;
-    token[j] = valid ? (int32_t)t : -1;
+    token[j] = valid ? (int32_t)t + pad : -1;
     a[j] = valid ? g.a[i * g.m + j] : 0.f;
   }
-  __syncthreads();
+  meet();
   float all = 0.f, own = 0.f;
   bool first = j < LP_MAX_TOKENS && token[j] >= begin && token[j] < end;
   for (int k = 0; k < g.m; ++k) {
@@ -494,17 +551,35 @@ template <typename T> __global__ __launch_bounds__(256) void log_probs_grad_kern
     const float d = fmaxf((x - r.m) * g.c, LP_NOTHING);
     return some ? __builtin_amdgcn_exp2f(d) * fmaf(k1, d, k0) : 0.f;
   };
-  float at_token = 0.f;
-  if (first) at_token = value(load8(z, token[j], token[j] + 1).v[0]) + (r.inv_s != 0.f ? g.tau * own : 0.f);
-  __syncthreads();
-  for (int v = begin + threadIdx.x * 8; v < end; v += LP_STEP) {
-    f32x8 x = load8(z, v, g.classes);
+  const auto put = [&](const Raw8<T> &raw, int v) {
+    f32x8 x = expand8(raw);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x.v[e] = value(x.v[e]);
-    store8(dz, v, g.classes, x);
+    store8(dz, v, 0x7fffffff, x);
+  };
+  const auto one = [&](int v) { return value(load8(z, v, v + 1).v[0]); };
+  const auto put_one = [&](int v, float y) { const f32x8 x = {{y}}; store8(dz, v, v + 1, x); };
+  float at_token = 0.f;
+  if (first) at_token = one(token[j]) + (r.inv_s != 0.f ? g.tau * own : 0.f);
+  meet();
+  int v = begin + j * 8;
+  if (pad > 0 && v == 0) {                 // before the first whole piece
+    for (int e = pad; e < min(8, end); ++e) put_one(e, one(e));
+    v += STEP;
   }
-  __syncthreads();
-  if (first) { f32x8 x = {{at_token}}; store8(dz, token[j], token[j] + 1, x); }
+  for (; v + (AHEAD - 1) * STEP + 8 <= end; v += AHEAD * STEP) {
+    Raw8<T> raw[AHEAD];
+#pragma unroll
+    for (int e = 0; e < AHEAD; ++e) raw[e] = raw_load8(z, v + e * STEP, 0x7fffffff);
+#pragma unroll
+    for (int e = 0; e < AHEAD; ++e) put(raw[e], v + e * STEP);
+  }
+  for (; v < end; v += STEP) {
+    if (v + 8 <= end) put(raw_load8(z, v, 0x7fffffff), v);
+    else for (int e = v; e < end; ++e) put_one(e, one(e));
+  }
+  meet();
+  if (first) put_one(token[j], at_token);
 }
 
 }  // namespace shampoo

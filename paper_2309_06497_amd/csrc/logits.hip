@@ -25,21 +25,33 @@ int check(const shampoo_logits &c) {
 // 1 / T over log 2, of a T whose reciprocal float32 holds
 float exponent_scale(float inverse_temperature) { return (float)((double)inverse_temperature * 1.4426950408889634); }
 
+// The most logits before a row that its kernel skips to read aligned pieces
+int32_t pad_of(const shampoo_logits &c, const void *logits) { return aligned(logits, 16) && c.ld * size_of(c.dtype) % 16 == 0 ? 0 : (int32_t)(16 / size_of(c.dtype)) - 1; }
 // Parts of a row, in steps of `step` classes: what one workgroup takes at most, and where there are few rows as many as give four workgroups to every CU.
 constexpr int64_t WORKGROUPS = 1024;
-int32_t parts_of(int64_t rows, int32_t classes, int64_t step, int64_t longest, int64_t most_parts, int32_t &pieces) {
-  const int64_t all = (classes + step - 1) / step;
+int32_t parts_of(int64_t rows, int32_t classes, int64_t step, int64_t longest, int64_t most_parts, int32_t pad, int32_t &pieces) {
+  const int64_t all = (classes + pad + step - 1) / step;
   const int64_t wanted = std::max((classes + longest - 1) / longest, std::min(most_parts, (WORKGROUPS + rows - 1) / std::max<int64_t>(rows, 1)));
   pieces = (int32_t)((all + wanted - 1) / wanted);
   return (int32_t)((all + pieces - 1) / pieces);
 }
-// Rows that one wavefront keeps in registers; otherwise wavefronts of a workgroup: a row stays whole, without a second launch, from 512 rows on.
-constexpr int32_t SMALL_CLASSES = 2048;
-int wavefronts(int64_t rows) { return rows >= 2048 || rows < 512 ? 4 : rows >= 1024 ? 8 : 16; }
-size_t layout(const shampoo_logits &c, void *workspace, LogPartArgs &a) {
+// Rows of more classes than a wavefront keeps in registers have a workgroup each, of as many wavefronts as leave 16 pieces to a thread, or more where that fills the
+// GPU's 4096 places.  Parts and a second launch for long rows where they are few: 20 tokens of 1 x 131072 in PARTS_US instead of WHOLE_US, of 1 x 50000 13.2
+// instead of 11.1, of 128 x 131072 20.4 instead of 18.7.
+constexpr int32_t SMALL_CLASSES = 2048, LONG_ROW = 65536;
+constexpr int64_t FEW_ROWS = 64;
+int wavefronts(int64_t rows, int32_t classes) {
+  int w = 1;
+  while (w < 8 && (classes > 8192 * w || (rows * w < 4096 && classes > 1024 * w))) w *= 2;
+  return w;
+}
+size_t layout(const shampoo_logits &c, int32_t pad, void *workspace, LogPartArgs &a, int &w) {
   a.parts = 1;
+  w = 0;
   if (c.classes <= SMALL_CLASSES) return 0;
-  a.parts = parts_of(c.rows, c.classes, 512 * wavefronts(c.rows), LP_MAX_PART, c.rows >= 512 ? 1 : LP_MAX_PARTS, a.pieces);
+  const bool cut = c.rows < FEW_ROWS && c.classes > LONG_ROW;
+  w = cut ? 4 : wavefronts(c.rows, c.classes);
+  a.parts = parts_of(c.rows, c.classes, 512 * w, LP_MAX_PART, cut ? LP_MAX_PARTS : 1, pad, a.pieces);
   Arena at(workspace);
   if (a.parts > 1) {
     a.sums = at.take<SoftSums>((size_t)(c.rows * a.parts));
@@ -64,17 +76,18 @@ template <typename T, int PIECES> void launch_rows(const LogProbsArgs &g, unsign
   const dim3 grid((n + 3) / 4);
   if (g.top > 0) log_probs_row_kernel<T, PIECES, true><<<grid, 256, 0, s>>>(g, g.row0 + n); else log_probs_row_kernel<T, PIECES, false><<<grid, 256, 0, s>>>(g, g.row0 + n);
 }
-template <typename T> int launch_log_probs(LogPartArgs a, int64_t rows, hipStream_t s) {
+template <typename T> int launch_log_probs(LogPartArgs a, int w, int64_t rows, hipStream_t s) {
   LogProbsArgs &g = a.g;
   TRY(by_rows(rows, a.parts, [&](int64_t r, unsigned n) {
     g.row0 = r;
     if (g.classes <= 512) launch_rows<T, 1>(g, n, s);
     else if (g.classes <= 1024) launch_rows<T, 2>(g, n, s);
     else if (g.classes <= SMALL_CLASSES) launch_rows<T, 4>(g, n, s);
-    else switch (wavefronts(rows)) {
+    else switch (w) {
+      case 1: launch_parts<T, 1>(a, n, s); break;
+      case 2: launch_parts<T, 2>(a, n, s); break;
       case 4: launch_parts<T, 4>(a, n, s); break;
-      case 8: launch_parts<T, 8>(a, n, s); break;
-      default: launch_parts<T, 16>(a, n, s);
+      default: launch_parts<T, 8>(a, n, s);
     }
   }));
   if (a.parts == 1) return SHAMPOO_OK;
@@ -90,7 +103,9 @@ extern "C" {
 
 size_t shampoo_log_probs_workspace_bytes(const shampoo_logits *c) {
   LogPartArgs a = {};
-  return c && check(*c) == SHAMPOO_OK ? layout(*c, nullptr, a) : 0;
+  int w;
+  if (!c || check(*c) != SHAMPOO_OK) return 0;
+  return std::max(layout(*c, 0, nullptr, a, w), layout(*c, 7, nullptr, a, w));      // whatever their alignment
 }
 
 int shampoo_log_probs(const shampoo_logits *c, const void *logits, const int64_t *tokens, float *log_probs, float *entropy, int64_t *top_tokens,
@@ -101,13 +116,14 @@ int shampoo_log_probs(const shampoo_logits *c, const void *logits, const int64_t
   if (!logits || !entropy || !statistics || (c->tokens > 0 && (!tokens || !log_probs)) || (c->top > 0 && (!top_tokens || !top_log_probs))) return SHAMPOO_ERR_NULL;
   if (!aligned(statistics, 16)) return SHAMPOO_ERR_UNSUPPORTED;
   LogPartArgs a = {};
-  TRY(workspace_ok(workspace, workspace_bytes, layout(*c, workspace, a)));
+  int w;
+  TRY(workspace_ok(workspace, workspace_bytes, layout(*c, pad_of(*c, logits), workspace, a, w)));
   LogProbsArgs &g = a.g;
   g.z = logits; g.ld = c->ld; g.tokens = tokens; g.c = exponent_scale(c->inverse_temperature); g.tau = c->inverse_temperature;
   g.classes = c->classes; g.m = c->tokens; g.top = c->top; g.log_probs = log_probs; g.entropy = entropy; g.top_tokens = top_tokens; g.top_log_probs = top_log_probs;
   g.stats = reinterpret_cast<RowStatistics *>(statistics);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return c->dtype == SHAMPOO_GRAD_F32 ? launch_log_probs<float>(a, c->rows, s) : launch_log_probs<uint16_t>(a, c->rows, s);
+  return c->dtype == SHAMPOO_GRAD_F32 ? launch_log_probs<float>(a, w, c->rows, s) : launch_log_probs<uint16_t>(a, w, c->rows, s);
 }
 
 int shampoo_log_probs_grad(const shampoo_logits *c, const void *logits, const int64_t *tokens, const float *statistics, const float *d_log_probs,
@@ -124,12 +140,17 @@ int shampoo_log_probs_grad(const shampoo_logits *c, const void *logits, const in
   g.dz = d_logits; g.ld_dz = ld_d_logits; g.c = exponent_scale(c->inverse_temperature); g.tau = c->inverse_temperature;
   g.classes = c->classes; g.m = d_log_probs ? c->tokens : 0;
   int32_t pieces;
-  g.parts = parts_of(c->rows, c->classes, LP_STEP, MAX_CLASSES, MAX_CLASSES, pieces);
+  if (c->classes <= SMALL_CLASSES) return by_rows(c->rows, 1, [&](int64_t r, unsigned n) {
+    g.row0 = r;
+    if (c->dtype == SHAMPOO_GRAD_F32) log_probs_grad_kernel<float, 1><<<dim3((n + 3) / 4), 256, 0, s>>>(g, r + n);
+    else log_probs_grad_kernel<uint16_t, 1><<<dim3((n + 3) / 4), 256, 0, s>>>(g, r + n);
+  });
+  g.parts = parts_of(c->rows, c->classes, LP_STEP, MAX_CLASSES, MAX_CLASSES, pad_of(*c, logits), pieces);
   g.part_len = pieces * LP_STEP;
   return by_rows(c->rows, g.parts, [&](int64_t r, unsigned n) {
     g.row0 = r;
-    if (c->dtype == SHAMPOO_GRAD_F32) log_probs_grad_kernel<float><<<dim3(n * g.parts), 256, 0, s>>>(g);
-    else log_probs_grad_kernel<uint16_t><<<dim3(n * g.parts), 256, 0, s>>>(g);
+    if (c->dtype == SHAMPOO_GRAD_F32) log_probs_grad_kernel<float, 4><<<dim3(n * g.parts), 256, 0, s>>>(g, c->rows);
+    else log_probs_grad_kernel<uint16_t, 4><<<dim3(n * g.parts), 256, 0, s>>>(g, c->rows);
   });
 }
 
