@@ -53,6 +53,15 @@ template <typename F> __device__ __forceinline__ float wave_all(float x, float n
 }
 __device__ __forceinline__ float wave_max(float x) { return wave_all(x, -INFINITY, [](float p, float q) { return fmaxf(p, q); }); }
 __device__ __forceinline__ float wave_sum(float x) { return wave_all(x, 0.f, [](float p, float q) { return p + q; }); }
+__device__ __forceinline__ int wave_scan(int x) {            // of this lane and those before it
+  x += LP_DPP(x, 0x111, 0);
+  x += LP_DPP(x, 0x112, 0);
+  x += LP_DPP(x, 0x114, 0);
+  x += LP_DPP(x, 0x118, 0);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
 // how many lanes before this one are in a mask
 __device__ __forceinline__ int lanes_before(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); }
 
@@ -101,8 +110,28 @@ template <typename Key, typename Count> __device__ __forceinline__ Key bound_of(
   }
   return lo;                             // more than `most` equal ones, where keys are values alone
 }
+// What that search is for when a table does not do.  Bins of x from the largest logit down, a sixteenth of a unit of log 2 each: what reaches bin b holds the `top`
+// largest if `top` values do, since equal ones share a bin and larger ones have no higher one.
+constexpr int LP_BINS = 256;
+__device__ __forceinline__ int bin_of(float z, float largest, float c) { return (int)fminf((largest - z) * c * 16.f, (float)LP_BINS); }   // LP_BINS: none, and NaN
+// the first bin by which `top` values are there, or LP_BINS: there are not so many, or more than LP_CHOSEN
+__device__ __forceinline__ int bin_bound(const int *bins, int top, int lane) {
+  const int4 b = reinterpret_cast<const int4 *>(bins)[lane];
+  const int upto = wave_scan(b.x + b.y + b.z + b.w);
+  const uint64_t enough = __ballot(upto >= top);
+  if (enough == 0) return LP_BINS;
+  const int at = __builtin_ctzll(enough);
+  const int x = __builtin_amdgcn_readlane(b.x, at), y = __builtin_amdgcn_readlane(b.y, at), z = __builtin_amdgcn_readlane(b.z, at), w = __builtin_amdgcn_readlane(b.w, at);
+  int n = __builtin_amdgcn_readlane(upto, at) - (x + y + z + w) + x, bin = 4 * at;
+  if (n < top) { n += y; ++bin; }
+  if (n < top) { n += z; ++bin; }
+  if (n < top) { n += w; ++bin; }
+  return n <= LP_CHOSEN ? bin : LP_BINS;
+}
+
 // What a workgroup of W wavefronts needs for that
 template <int W> struct Selection {
+  alignas(16) int bins[LP_BINS];
   uint64_t counts[2][W];
   int n_chosen, n_candidates, chosen[LP_CHOSEN];
   uint64_t candidate[LP_CANDIDATES], last[LP_CHOSEN];
@@ -258,22 +287,40 @@ template <typename T, int PIECES, bool TOP> __global__ __launch_bounds__(256) vo
 
   if constexpr (TOP) {
     __shared__ uint64_t keys[4][LP_CHOSEN];
+    __shared__ int4 table[4][LP_BINS / 4];
     uint64_t *const candidate = keys[wave];
+    int *const bins = reinterpret_cast<int *>(table[wave]);
+    table[wave][lane] = make_int4(0, 0, 0, 0);
     uint32_t order[8 * PIECES];
+    wavefront_order();
 #pragma unroll
-    for (int e = 0; e < 8 * PIECES; ++e) order[e] = (uint32_t)(logit_key(x[e >> 3].v[e & 7], 0) >> 32);
-    const auto count = [&](uint32_t bound) {
-      int n = 0;
+    for (int e = 0; e < 8 * PIECES; ++e) {
+      const int bin = bin_of(x[e >> 3].v[e & 7], t.m, g.c);
+      if (bin < LP_BINS) atomicAdd(&bins[bin], 1);
+    }
+    wavefront_order();
+    const int by_bin = bin_bound(bins, g.top, lane);
+    uint32_t bound = 1;
+    bool ties = false;
+    if (by_bin < LP_BINS) {
 #pragma unroll
-      for (int e = 0; e < 8 * PIECES; ++e) n += __popcll(__ballot(order[e] >= bound));
-      return n;
-    };
-    const int most = at_most(g.top);
-    const uint32_t above = (uint32_t)(logit_key(t.m, 0) >> 32) + 1;
-    uint32_t bound = bound_of<uint32_t>(1, above, 1u << 20, g.top, most, count);
-    // more than `most` reach it: those above, and of equal ones the first
-    const bool ties = count(bound) > most;
-    if (ties) ++bound;
+      for (int e = 0; e < 8 * PIECES; ++e)
+        order[e] = bin_of(x[e >> 3].v[e & 7], t.m, g.c) <= by_bin ? (uint32_t)(logit_key(x[e >> 3].v[e & 7], 0) >> 32) : 0u;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8 * PIECES; ++e) order[e] = (uint32_t)(logit_key(x[e >> 3].v[e & 7], 0) >> 32);
+      const auto count = [&](uint32_t from) {
+        int n = 0;
+#pragma unroll
+        for (int e = 0; e < 8 * PIECES; ++e) n += __popcll(__ballot(order[e] >= from));
+        return n;
+      };
+      const int most = at_most(g.top);
+      const uint32_t above = (uint32_t)(logit_key(t.m, 0) >> 32) + 1;
+      bound = bound_of<uint32_t>(1, above, 1u << 20, g.top, most, count);
+      ties = count(bound) > most;          // those above, and of equal ones the first
+      if (ties) ++bound;
+    }
     int n = 0;
     const auto key = [&](int e) { return (uint64_t)order[e] << 32 | (0xffffffffu - (uint32_t)((e >> 3) * 512 + lane * 8 + (e & 7))); };
 #pragma unroll
@@ -322,6 +369,7 @@ struct LogPartArgs { LogProbsArgs g; int32_t parts, pieces; SoftSums *sums; uint
 template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void log_probs_kernel(const LogPartArgs a) {
   constexpr int AHEAD = 4, STEP = 512 * W;
   __shared__ float part_m[W], part_most[W], part_s[W], part_w[W];
+  [[maybe_unused]] __shared__ Selection<W> l;
   const LogProbsArgs &g = a.g;
   const int64_t unit = g.row0 + blockIdx.x / (uint32_t)a.parts;
   const int part = (int)(blockIdx.x % (uint32_t)a.parts), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -370,7 +418,11 @@ template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void
   }
   float most = fmaxf(fmaxf(largest[0], largest[1]), fmaxf(largest[2], largest[3]));
   SoftSums t = {wave_max(ref), 0.f, 0.f};
-  if constexpr (TOP) most = wave_max(most);
+  if constexpr (TOP) {
+    most = wave_max(most);
+    for (int k = tid; k < LP_BINS; k += 64 * W) l.bins[k] = 0;
+    if (tid == 0) l.n_chosen = l.n_candidates = 0;
+  }
   if (lane == 0) { part_m[wave] = t.m; part_most[wave] = most; }
   __syncthreads();
 #pragma unroll
@@ -380,6 +432,13 @@ template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void
     t.s = wave_sum(u.s); t.w = wave_sum(u.w);
   }
   if (lane == 0) { part_s[wave] = t.s; part_w[wave] = t.w; }
+  if constexpr (TOP) {
+#pragma unroll
+    for (int k = 0; k < LP_STRIPS; ++k) {
+      const int bin = bin_of(largest[k], most, g.c);
+      if (bin < LP_BINS) atomicAdd(&l.bins[bin], 1);
+    }
+  }
   __syncthreads();
   t.s = t.w = 0.f;
 #pragma unroll
@@ -392,25 +451,35 @@ template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void
   } else if (tid == 0) a.sums[out] = t;
 
   if constexpr (TOP) {
-    __shared__ Selection<W> l;
     int turn = 0;
-    if (tid == 0) l.n_chosen = l.n_candidates = 0;
-    uint64_t key[LP_STRIPS];
-#pragma unroll
-    for (int k = 0; k < LP_STRIPS; ++k) key[k] = logit_key(largest[k], begin + at[k] * STEP + tid * 8);
     const uint64_t above = logit_key(most, 0) + 1;
-    uint64_t bound = bound_of_keys(key, LP_STRIPS, above, g.top, l, turn);
+    const int by_bin = bin_bound(l.bins, g.top, lane);
+    uint64_t bound = 1;
+    bool chosen[LP_STRIPS];
+    if (by_bin < LP_BINS) {
+#pragma unroll
+      for (int k = 0; k < LP_STRIPS; ++k) chosen[k] = bin_of(largest[k], most, g.c) <= by_bin;
+    } else {
+      uint64_t key[LP_STRIPS];
+#pragma unroll
+      for (int k = 0; k < LP_STRIPS; ++k) key[k] = logit_key(largest[k], begin + at[k] * STEP + tid * 8);
+      bound = bound_of_keys(key, LP_STRIPS, above, g.top, l, turn);
+#pragma unroll
+      for (int k = 0; k < LP_STRIPS; ++k) chosen[k] = key[k] >= bound;
+      // a strip's key is that of the first token of its piece: the others may come before the next strip's
+      bound = max(bound & ~(uint64_t)7, (uint64_t)1);
+    }
     // a wavefront's strips one behind the other
     uint64_t mask[LP_STRIPS];
     int mine = 0, place = 0;
 #pragma unroll
-    for (int k = 0; k < LP_STRIPS; ++k) { mask[k] = __ballot(key[k] >= bound); mine += __popcll(mask[k]); }
+    for (int k = 0; k < LP_STRIPS; ++k) { mask[k] = __ballot(chosen[k]); mine += __popcll(mask[k]); }
     if (lane == 0 && mine > 0) place = atomicAdd(&l.n_chosen, mine);
     place = __builtin_amdgcn_readfirstlane(place);
 #pragma unroll
     for (int k = 0; k < LP_STRIPS; ++k) {
       const int n = place + lanes_before(mask[k]);
-      if (key[k] >= bound && n < LP_CHOSEN) l.chosen[n] = k * 64 * W + tid;
+      if (chosen[k] && n < LP_CHOSEN) l.chosen[n] = k * 64 * W + tid;
       place += __popcll(mask[k]);
     }
     __syncthreads();
@@ -423,7 +492,7 @@ template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void
         const f32x8 x = load_logits(z, o, pad, end);
         uint64_t keys[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) keys[e] = logit_key(x.v[e], o + e);
+        for (int e = 0; e < 8; ++e) keys[e] = by_bin == LP_BINS || bin_of(x.v[e], most, g.c) <= by_bin ? logit_key(x.v[e], o + e) : 0;
         f(keys);
       }
     };
@@ -440,8 +509,6 @@ template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void
       });
       __syncthreads();
     };
-    // a strip's key is that of the first token of its piece: the others may come before the next strip's
-    bound = max(bound & ~(uint64_t)7, (uint64_t)1);
     gather(bound);
     if (l.n_candidates > LP_CANDIDATES) {  // many tokens of one strip: a bound among the tokens themselves
       const uint64_t from_strips = bound;
@@ -491,14 +558,23 @@ template <typename T> __global__ __launch_bounds__(256) void log_probs_join_kern
   if (g.top == 0) return;
   most = wave_max(most);
   if (lane == 0) part_most[tid >> 6] = most;
+  l.bins[tid] = 0;
   if (tid == 0) l.n_candidates = 0;
   __syncthreads();
   most = fmaxf(fmaxf(part_most[0], part_most[1]), fmaxf(part_most[2], part_most[3]));
-  int turn = 0;
-  const uint64_t above = logit_key(most, 0) + 1, bound = bound_of_keys(key, (n + 255) / 256, above, g.top, l, turn);
+  const int used = (n + 255) / 256;
+  const auto bin = [&](uint64_t k) { return k ? bin_of(key_logit(k), most, g.c) : LP_BINS; };
 #pragma unroll
   for (int e = 0; e < N; ++e)
-    if (key[e] >= bound) { const int k = atomicAdd(&l.n_candidates, 1); if (k < LP_CANDIDATES) l.candidate[k] = key[e]; }
+    if (e < used && bin(key[e]) < LP_BINS) atomicAdd(&l.bins[bin(key[e])], 1);
+  __syncthreads();
+  int turn = 0;
+  const uint64_t above = logit_key(most, 0) + 1;
+  const int by_bin = bin_bound(l.bins, g.top, lane);
+  const uint64_t bound = by_bin < LP_BINS ? 1 : bound_of_keys(key, used, above, g.top, l, turn);
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (e < used && key[e] >= bound && (by_bin == LP_BINS || bin(key[e]) <= by_bin)) { const int k = atomicAdd(&l.n_candidates, 1); if (k < LP_CANDIDATES) l.candidate[k] = key[e]; }
   __syncthreads();
   put_candidates(l, min(l.n_candidates, LP_CANDIDATES), g.top, above, turn, [&](int rank, uint64_t k) { put_top(g, i, r, rank, k, pad); });
 }
