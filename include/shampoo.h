@@ -555,7 +555,7 @@ typedef struct {
   int32_t grad_dtype;
   int32_t device;          /* HIP device ordinal: the current one in every call     */
   double beta1, beta2;     /* in [0, 1)                                             */
-  double epsilon;          /* 1e-30 ... 1e30                                        */
+  double epsilon;          /* 1e-12 ... 1e12                                        */
   double weight_decay;     /* >= 0                                                  */
 } shampoo_adamw_config;
 /* 0 if cfg is invalid.  With 32 bits the workspace begins with m, [all elements] float32, one parameter behind the other; v follows at the next multiple of 256 bytes. */

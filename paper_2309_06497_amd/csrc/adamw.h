@@ -21,7 +21,7 @@
 
 namespace shampoo {
 
-constexpr int AW_GROUP = 128, AW_CHUNK = 4096, AW_TENSORS = 160;
+constexpr int AW_GROUP = 128, AW_CHUNK = 2048, AW_POINTERS = 480;       // of a launch: 240 tensors, 160 with copies
 constexpr uint32_t AW_MIX1 = 0x9E3779B9u, AW_MIX2 = 0x6A09E667u, AW_MIX3 = 0xBB67AE85u, AW_MIX4 = 0xA54FF53Bu;
 constexpr uint32_t AW_EXP_NAN = 254, AW_EXP_ZERO = 27;         // groups from 2^127 on read NaN, below 2^-100 zero
 
@@ -38,8 +38,8 @@ struct AdamArgs {
   const float *norm;                              // or nullptr
   float max_norm, b1, b1c, b2, b2c, inv_sqrt, epsilon, keep, lr;     // keep: 1 - lr wd; lr over the first correction, inv_sqrt: one over the root of the second
   uint32_t mix;                                   // of the step's number
-  int32_t has_copies;
-  void *p[AW_TENSORS]; const void *g[AW_TENSORS]; uint16_t *copy[AW_TENSORS];
+  int32_t tensor0, tensors, has_copies;
+  const void *tensor[AW_POINTERS];                // parameters, gradients, copies
 };
 static_assert(sizeof(AdamArgs) <= 4096, "arguments of a kernel");
 
@@ -53,73 +53,82 @@ __device__ __forceinline__ float sum(float x, float y) {
   return x + y;
 }
 
-// 2^E and 2^-E of an exponent byte
-__device__ __forceinline__ float exp_value(uint32_t byte) { return __uint_as_float(byte << 23); }
-__device__ __forceinline__ float exp_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
-
-// what a code (without sign) stands for, times 2^-E
-template <int SHIFT> __device__ __forceinline__ float code_value(uint32_t code) { return __uint_as_float(code << 20) * __uint_as_float((uint32_t)(127 + SHIFT) << 23); }
-template <int SHIFT> __device__ __forceinline__ uint32_t code_of(float magnitude, float inverse, uint32_t add) {
-  return (__float_as_uint(magnitude * inverse * __uint_as_float((uint32_t)(127 - SHIFT) << 23)) + add) >> 20;
-}
-// eight neighbouring codes, the sign of m in bit 7
+// Eight neighbouring codes of a group whose exponent byte is `byte`, and back; the sign of m in bit 7.  A code's bits, 20 places up, are those of a float32 that is
+// 2^-(SHIFT + E) of the value; scaling by that power of two is one exact instruction (and one rounding, of what is below the lowest binade's last bit but 20).
+constexpr int AW_SHIFT_M = 113, AW_SHIFT_V = 97;
 __device__ __forceinline__ void decode_m(uint2 q, uint32_t byte, f32x8 &x) {
-  const float scale = byte == 255 ? NAN : exp_value(byte);
+  const int power = (int)byte - 127 + AW_SHIFT_M;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const uint32_t c = ((e < 4 ? q.x : q.y) >> (8 * (e & 3))) & 255u;
-    x.v[e] = __uint_as_float(__float_as_uint(code_value<113>(c & 127u) * scale) | (c >> 7) << 31);
+    const uint32_t c = (e < 4 ? q.x : q.y) << (24 - 8 * (e & 3));
+    x.v[e] = __builtin_amdgcn_ldexpf(__uint_as_float((c >> 4 & 0x07f00000u) | (c & 0x80000000u)), power);
+  }
+  if (__any(byte == 255)) {                // hardly ever
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x.v[e] = byte == 255 ? NAN : x.v[e];
   }
 }
 __device__ __forceinline__ void decode_v(uint2 q, uint32_t byte, f32x8 &x) {
-  const float scale = byte == 255 ? NAN : exp_value(byte);
+  const int power = (int)byte - 127 + AW_SHIFT_V;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x.v[e] = code_value<97>(((e < 4 ? q.x : q.y) >> (8 * (e & 3))) & 255u) * scale;
+  for (int e = 0; e < 8; ++e) x.v[e] = __builtin_amdgcn_ldexpf(__uint_as_float(((e < 4 ? q.x : q.y) >> (8 * (e & 3)) & 255u) << 20), power);
+  if (__any(byte == 255)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x.v[e] = byte == 255 ? NAN : x.v[e];
+  }
 }
-// the exponent byte of a group, 16 lanes with eight values each
-__device__ __forceinline__ uint32_t group_exponent(const f32x8 &x) {
+// Bits of the largest magnitude of a group, 16 lanes with eight values each
+__device__ __forceinline__ uint32_t group_largest(const f32x8 &x) {
   uint32_t top = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x.v[e]) & 0x7fffffffu);
+  for (int e = 0; e < 8; e += 2) top = max(top, max(__float_as_uint(x.v[e]) & 0x7fffffffu, __float_as_uint(x.v[e + 1]) & 0x7fffffffu));
 #pragma unroll
   for (int o = 1; o < 16; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
-  return top >> 23 >= AW_EXP_NAN ? 255u : top >> 23;
+  return top;
+}
+// its exponent byte
+__device__ __forceinline__ uint32_t group_exponent(const f32x8 &x) {
+  const uint32_t byte = group_largest(x) >> 23;
+  return byte >= AW_EXP_NAN ? 255u : byte;
 }
 __device__ __forceinline__ uint2 encode_m(const f32x8 &x, uint32_t byte, const uint32_t (&add)[8]) {
   uint32_t w[2] = {0u, 0u};
-  if (byte >= AW_EXP_ZERO && byte != 255) {
-    const float inverse = exp_inverse(byte);
+  const int power = 127 - AW_SHIFT_M - (int)byte;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t u = __float_as_uint(x.v[e]), c = code_of<113>(fabsf(x.v[e]), inverse, add[e]) | (u >> 31) << 7;
-      w[e >> 2] |= c << (8 * (e & 3));
-    }
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t c = (__float_as_uint(__builtin_amdgcn_ldexpf(fabsf(x.v[e]), power)) + add[e]) >> 20;
+    w[e >> 2] |= (c | (__float_as_uint(x.v[e]) >> 24 & 128u)) << (8 * (e & 3));
   }
-  return make_uint2(w[0], w[1]);
+  const bool some = byte >= AW_EXP_ZERO && byte != 255;
+  return make_uint2(some ? w[0] : 0u, some ? w[1] : 0u);
 }
 __device__ __forceinline__ uint2 encode_v(const f32x8 &x, uint32_t byte, const uint32_t (&add)[8]) {
   uint32_t w[2] = {0u, 0u};
-  if (byte >= AW_EXP_ZERO && byte != 255) {
-    const float inverse = exp_inverse(byte);
+  const int power = 127 - AW_SHIFT_V - (int)byte;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      uint32_t c = code_of<97>(fabsf(x.v[e]), inverse, add[e]);
-      c = c == 0 && x.v[e] != 0.f ? 1u : c;
-      w[e >> 2] |= c << (8 * (e & 3));
-    }
+  for (int e = 0; e < 8; ++e) {
+    const float v = fabsf(x.v[e]);
+    const uint32_t c = (__float_as_uint(__builtin_amdgcn_ldexpf(v, power)) + add[e]) >> 20;
+    w[e >> 2] |= max(c, min(__float_as_uint(v), 1u)) << (8 * (e & 3));        // only zero is zero
   }
-  return make_uint2(w[0], w[1]);
+  const bool some = byte >= AW_EXP_ZERO && byte != 255;
+  return make_uint2(some ? w[0] : 0u, some ? w[1] : 0u);
 }
 
-// Offsets of the roundings of element i in a step: of m and v in 2^-20, of a bf16 parameter in 2^-16
-__device__ __forceinline__ void rounding_offsets(uint32_t seed, uint32_t &m, uint32_t &v, uint32_t &p) {
-  uint32_t x = seed;
-  x = (x ^ x >> 16) * AW_MIX3;
-  x = (x ^ x >> 15) * AW_MIX4;
-  x ^= x >> 16;
-  uint32_t y = x * AW_MIX1 + AW_MIX2;
-  y ^= y >> 15;
-  m = x >> 12; v = y >> 12; p = y & 0xffffu;
+// Offsets of the roundings of elements i ... i + 7 in a step: of m and v in 2^-20, of a bf16 parameter in 2^-16
+__device__ __forceinline__ void rounding_offsets(uint64_t i, uint32_t mix, uint32_t (&m)[8], uint32_t (&v)[8], uint32_t (&p)[8]) {
+  const uint32_t low = (uint32_t)i, seed = low * AW_MIX1 + (uint32_t)(i >> 32) * AW_MIX3 + mix;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    uint32_t x = seed + (uint32_t)e * AW_MIX1;
+    if (low > 0xfffffff8u && low + e < low) x += AW_MIX3;      // over 2^32
+    x = (x ^ x >> 16) * AW_MIX3;
+    x = (x ^ x >> 15) * AW_MIX4;
+    x ^= x >> 16;
+    uint32_t y = x * AW_MIX1 + AW_MIX2;
+    y ^= y >> 15;
+    m[e] = x >> 12; v[e] = y >> 12; p[e] = y & 0xffffu;
+  }
 }
 
 // P, G: types of parameters and gradients (float or uint16_t, bf16 bits).  A thread has eight neighbouring elements.
@@ -131,9 +140,10 @@ template <typename P, typename G, int BITS> __global__ __launch_bounds__(256) vo
     if (!(fabsf(norm) < INFINITY)) return;                     // nothing is touched
     clip = norm > g.max_norm ? g.max_norm / norm : 1.f;
   }
-  P *p = global_ptr<P>(g.p[c.tensor]) + c.start;
-  const G *grad = global_ptr<const G>(g.g[c.tensor]) + c.start;
-  uint16_t *copy = g.has_copies ? global_ptr<uint16_t>(g.copy[c.tensor]) + c.start : nullptr;
+  const int t = c.tensor - g.tensor0;
+  P *p = global_ptr<P>(g.tensor[t]) + c.start;
+  const G *grad = global_ptr<const G>(g.tensor[g.tensors + t]) + c.start;
+  uint16_t *copy = g.has_copies ? global_ptr<uint16_t>(g.tensor[2 * g.tensors + t]) + c.start : nullptr;
   const float keep = c.decayed ? g.keep : 1.f;
   for (int at = threadIdx.x * 8; at < ((c.len + AW_GROUP - 1) & ~(AW_GROUP - 1)); at += 2048) {
     const f32x8 x = load8(grad, at, c.len);
@@ -151,14 +161,13 @@ template <typename P, typename G, int BITS> __global__ __launch_bounds__(256) vo
       const float k = product(x.v[e], clip);
       m.v[e] = sum(product(m.v[e], g.b1), product(k, g.b1c));
       v.v[e] = sum(product(v.v[e], g.b2), product(product(k, g.b2c), k));
-      const float u = m.v[e] / fmaf(sqrtf(v.v[e]), g.inv_sqrt, g.epsilon);
+      // root and reciprocal of the GPU's instructions: within one step; a v below 1.2e-38 has the root 0, a millionth of epsilon
+      const float u = m.v[e] * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v.v[e]), g.inv_sqrt, g.epsilon));
       w.v[e] = fmaf(-g.lr, u, w.v[e] * keep);
     }
     [[maybe_unused]] uint32_t rm[8], rv[8], rp[8];
     if constexpr (BITS == 8 || sizeof(P) == 2) {
-      const uint64_t i = (uint64_t)c.flat + (uint32_t)at;       // eight neighbours may reach over 2^32
-#pragma unroll
-      for (int e = 0; e < 8; ++e) rounding_offsets((uint32_t)(i + e) * AW_MIX1 + (uint32_t)((i + e) >> 32) * AW_MIX3 + g.mix, rm[e], rv[e], rp[e]);
+      rounding_offsets((uint64_t)c.flat + (uint32_t)at, g.mix, rm, rv, rp);
     }
     if constexpr (BITS == 32) {
       store8(g.state.m + c.flat, at, c.len, m);
@@ -173,9 +182,8 @@ template <typename P, typename G, int BITS> __global__ __launch_bounds__(256) vo
     if constexpr (sizeof(P) == 2) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const uint32_t u = __float_as_uint(w.v[e]);
-        // infinities and NaN as they are (a NaN keeps a bit)
-        w.v[e] = __uint_as_float((u & 0x7f800000u) == 0x7f800000u ? (u & 0x7fffffu ? u | 0x400000u : u) & 0xffff0000u : (u + rp[e]) & 0xffff0000u);
+        const float up = __uint_as_float((__float_as_uint(w.v[e]) + rp[e]) & 0xffff0000u);      // an infinity stays one
+        w.v[e] = w.v[e] != w.v[e] ? NAN : up;
       }
     }
     store8(p, at, c.len, w);
@@ -205,12 +213,7 @@ template <typename T, int BITS> __global__ __launch_bounds__(256) void adamw_get
 // Codes to the nearest; m or v null: zeros.  A largest of just a power of two counts as the top of the binade below it, as which a step may have left it: what an
 // optimizer held is held again.
 __device__ __forceinline__ uint32_t loaded_exponent(const f32x8 &x) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x.v[e]) & 0x7fffffffu);
-#pragma unroll
-  for (int o = 1; o < 16; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
-  const uint32_t byte = top >> 23 >= AW_EXP_NAN ? 255u : top >> 23;
+  const uint32_t top = group_largest(x), byte = top >> 23 >= AW_EXP_NAN ? 255u : top >> 23;
   return byte != 255 && byte > AW_EXP_ZERO && (top & 0x7fffffu) == 0 ? byte - 1 : byte;
 }
 template <int BITS> __global__ __launch_bounds__(256) void adamw_set_kernel(const AdamValuesArgs g) {
@@ -245,13 +248,16 @@ struct NormArgs {
   const void *g[GN_TENSORS]; int64_t len[GN_TENSORS];
 };
 static_assert(sizeof(NormArgs) <= 4096, "arguments of a kernel");
-__device__ __forceinline__ double sum_256(double s) {
-  __shared__ double part[4];
+template <int THREADS> __device__ __forceinline__ double sum_of(double s) {
+  __shared__ double part[THREADS / 64];
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o, 64);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
   __syncthreads();
-  return (part[0] + part[1]) + (part[2] + part[3]);
+  s = part[0];
+#pragma unroll
+  for (int k = 1; k < THREADS / 64; ++k) s += part[k];
+  return s;
 }
 template <typename G> __global__ __launch_bounds__(256) void square_sums_kernel(const NormArgs g) {
   const int block = blockIdx.x;
@@ -268,25 +274,39 @@ template <typename G> __global__ __launch_bounds__(256) void square_sums_kernel(
   const int64_t start = (int64_t)(block - g.at[lo]) * g.chunk;
   const G *x = global_ptr<const G>(g.g[lo]) + start;
   const int n = (int)min((int64_t)g.chunk, g.len[lo] - start);
-  double s = 0.0;
-  for (int c = threadIdx.x * 8; c < n; c += 2048) {
-    const f32x8 v = load8(x, c, n);
+  constexpr int AHEAD = 4;
+  double part[AHEAD] = {0.0, 0.0, 0.0, 0.0};
+  const auto add = [](double &s, const f32x8 &v) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) s = fma((double)v.v[e], (double)v.v[e], s);
+  };
+  int c = threadIdx.x * 8;
+  for (; c + (AHEAD - 1) * 2048 + 8 <= n; c += AHEAD * 2048) {
+    Raw8<G> raw[AHEAD];
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) raw[a] = raw_load8(x, c + a * 2048, 0x7fffffff);
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) add(part[a], expand8(raw[a]));
   }
-  s = sum_256(s);
+  for (; c < n; c += 2048) add(part[0], load8(x, c, n));
+  const double s = sum_of<256>((part[0] + part[1]) + (part[2] + part[3]));
   if (threadIdx.x == 0) g.part[g.block0 + block] = s;
 }
 // a workgroup per tensor, and the last one for all
-__global__ __launch_bounds__(256) void norms_kernel(const double *part, const int32_t *first, int32_t tensors, float *norm, float *norms) {
+__global__ __launch_bounds__(1024) void norms_kernel(const double *part, const int32_t *first, int32_t tensors, float *norm, float *norms) {
   const int t = blockIdx.x;
   const int from = t < tensors ? first[t] : 0, to = t < tensors ? first[t + 1] : first[tensors];
-  double s = 0.0;
-  for (int i = from + threadIdx.x; i < to; i += 256) s += part[i];
-  s = sum_256(s);
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
+  int i = from + (int)threadIdx.x;
+  for (; i + 3 * 1024 < to; i += 4 * 1024) {
+#pragma unroll
+    for (int a = 0; a < 4; ++a) s[a] += part[i + a * 1024];
+  }
+  for (; i < to; i += 1024) s[0] += part[i];
+  const double all = sum_of<1024>((s[0] + s[1]) + (s[2] + s[3]));
   if (threadIdx.x != 0) return;
-  if (t < tensors) { if (norms) norms[t] = (float)sqrt(s); }
-  else *norm = (float)sqrt(s);
+  if (t < tensors) { if (norms) norms[t] = (float)sqrt(all); }
+  else *norm = (float)sqrt(all);
 }
 
 }  // namespace shampoo

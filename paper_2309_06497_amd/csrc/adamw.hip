@@ -47,7 +47,7 @@ int check(const shampoo_adamw_config *c) {
   if (total < 0) return (int)total;
   if (!dtype_ok(c->param_dtype) || !dtype_ok(c->grad_dtype) || (c->state_bits != 32 && c->state_bits != 8)) return SHAMPOO_ERR_HYPER;
   if (!(c->beta1 >= 0.0 && c->beta1 < 1.0 && c->beta2 >= 0.0 && c->beta2 < 1.0)) return SHAMPOO_ERR_HYPER;
-  if (!(c->epsilon >= 1e-30 && c->epsilon <= 1e30 && c->weight_decay >= 0.0 && std::isfinite(c->weight_decay))) return SHAMPOO_ERR_HYPER;
+  if (!(c->epsilon >= 1e-12 && c->epsilon <= 1e12 && c->weight_decay >= 0.0 && std::isfinite(c->weight_decay))) return SHAMPOO_ERR_HYPER;
   return SHAMPOO_OK;
 }
 int64_t groups_of(int64_t n) { return (n + AW_GROUP - 1) / AW_GROUP; }
@@ -138,7 +138,7 @@ int shampoo_adamw_create(const shampoo_adamw_config *cfg, void *workspace, size_
   for (int32_t i = 0; i < cfg->n_params; ++i) {
     o->first.push_back((int64_t)chunks.size());
     for (int64_t at = 0; at < o->numel[i]; at += AW_CHUNK)
-      chunks.push_back({at, flat + at, slot + at, (int32_t)std::min<int64_t>(AW_CHUNK, o->numel[i] - at), i % AW_TENSORS, !cfg->decay || cfg->decay[i] ? 1 : 0, 0});
+      chunks.push_back({at, flat + at, slot + at, (int32_t)std::min<int64_t>(AW_CHUNK, o->numel[i] - at), i, !cfg->decay || cfg->decay[i] ? 1 : 0, 0});
     flat += o->numel[i];
     slot += groups_of(o->numel[i]) * AW_GROUP;
   }
@@ -173,10 +173,13 @@ int shampoo_adamw_step(shampoo_adamw *o, void *const *params, const void *const 
   g.epsilon = (float)c.epsilon; g.keep = (float)(1.0 - lr * c.weight_decay); g.lr = (float)(lr / (1.0 - std::pow(c.beta1, t)));
   g.mix = (uint32_t)(uint64_t)step * AW_MIX2;
   g.has_copies = copies ? 1 : 0;
-  for (int32_t i0 = 0; i0 < c.n_params; i0 += AW_TENSORS) {
-    const int32_t n = std::min(AW_TENSORS, c.n_params - i0);
+  const int32_t at_once = AW_POINTERS / (copies ? 3 : 2);
+  for (int32_t i0 = 0; i0 < c.n_params; i0 += at_once) {
+    const int32_t n = std::min(at_once, c.n_params - i0);
+    g.tensor0 = i0; g.tensors = n;
     for (int32_t k = 0; k < n; ++k) {
-      g.p[k] = params[i0 + k]; g.g[k] = grads[i0 + k]; g.copy[k] = copies ? static_cast<uint16_t *>(copies[i0 + k]) : nullptr;
+      g.tensor[k] = params[i0 + k]; g.tensor[n + k] = grads[i0 + k];
+      if (copies) g.tensor[2 * n + k] = copies[i0 + k];
     }
     TRY(by_chunks(o->first[i0], o->first[i0 + n], [&](int64_t at, dim3 grid) {
       g.chunks = o->chunks + at;
@@ -246,7 +249,7 @@ int shampoo_gradient_norm(int32_t n, const void *const *grads, const int64_t *nu
     HIP_TRY(hipGetLastError());
     block0 += blocks;
   }
-  norms_kernel<<<dim3((unsigned)n + 1), 256, 0, s>>>(part, first, n, norm, norms);
+  norms_kernel<<<dim3((unsigned)n + 1), 1024, 0, s>>>(part, first, n, norm, norms);
   HIP_TRY(hipGetLastError());
   return SHAMPOO_OK;
 }

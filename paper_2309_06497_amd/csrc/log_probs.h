@@ -591,7 +591,7 @@ struct LogProbsGradArgs {
 // W = 4: a workgroup per part of a row; W = 1: a wavefront per row, four rows a workgroup, for up to 2048 classes.  A token's own part is added by the thread of its
 // first appearance, with those of all others, behind the row's other values.
 template <typename T, int W> __global__ __launch_bounds__(256) void log_probs_grad_kernel(const LogProbsGradArgs g, int64_t rows) {
-  constexpr int STEP = 512 * W, AHEAD = 2;
+  constexpr int STEP = 512 * W, AHEAD = W == 1 ? 2 : 4;
   __shared__ int32_t tokens[4 / W][LP_MAX_TOKENS];
   __shared__ float coefs[4 / W][LP_MAX_TOKENS];
   const int which = W == 1 ? threadIdx.x >> 6 : 0, j = W == 1 ? threadIdx.x & 63 : threadIdx.x;
