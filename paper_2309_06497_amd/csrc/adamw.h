@@ -28,6 +28,21 @@ constexpr uint32_t AW_EXP_NAN = 254, AW_EXP_ZERO = 27;         // groups from 2^
 // A piece of a tensor: where it begins there, among all elements, and among the 8-bit states (whose tensors begin with whole groups)
 struct AdamChunk { int64_t start, flat, slot; int32_t len, tensor, decayed, unused; };
 
+// and what it is made from: first: the tensor's first piece
+struct AdamTensor { int64_t first, numel, flat, slot; int32_t decayed, unused; };
+__global__ __launch_bounds__(256) void adamw_chunks_kernel(const AdamTensor *tensors, int32_t n, AdamChunk *chunks, int64_t count) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= count) return;
+  int lo = 0, hi = n;                             // the last tensor that begins here or before: empty ones begin where the next one does
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (tensors[mid].first <= i) lo = mid; else hi = mid;
+  }
+  const AdamTensor t = tensors[lo];
+  const int64_t at = (i - t.first) * AW_CHUNK;
+  chunks[i] = {at, t.flat + at, t.slot + at, (int32_t)min((int64_t)AW_CHUNK, t.numel - at), lo, t.decayed, 0};
+}
+
 struct AdamState {
   float *m, *v;                                   // 32 bits: [all elements]
   uint8_t *m8, *v8, *m_exp, *v_exp;               // 8 bits: [slots], [slots / 128]

@@ -52,7 +52,7 @@ int check(const shampoo_adamw_config *c) {
 }
 int64_t groups_of(int64_t n) { return (n + AW_GROUP - 1) / AW_GROUP; }
 
-size_t layout(const shampoo_adamw_config &c, void *workspace, AdamState &st, AdamChunk *&chunks) {
+size_t layout(const shampoo_adamw_config &c, void *workspace, AdamState &st, AdamChunk *&chunks, AdamTensor *&tensors) {
   int64_t total = 0, groups = 0, pieces = 0;
   for (int32_t i = 0; i < c.n_params; ++i) { total += c.numel[i]; groups += groups_of(c.numel[i]); pieces += (c.numel[i] + AW_CHUNK - 1) / AW_CHUNK; }
   Arena a(workspace);
@@ -67,7 +67,8 @@ size_t layout(const shampoo_adamw_config &c, void *workspace, AdamState &st, Ada
     st.v_exp = a.take<uint8_t>((size_t)groups);
   }
   chunks = a.take<AdamChunk>((size_t)pieces);
-  return std::max(a.used, ALIGN);
+  tensors = a.take<AdamTensor>((size_t)c.n_params);
+  return a.used;
 }
 
 // chunks c0 ... c1 - 1, at most MAX_BLOCKS in a launch
@@ -121,7 +122,8 @@ size_t shampoo_adamw_workspace_bytes(const shampoo_adamw_config *cfg) {
   if (check(cfg) != SHAMPOO_OK) return 0;
   AdamState st;
   AdamChunk *chunks;
-  return layout(*cfg, nullptr, st, chunks);
+  AdamTensor *tensors;
+  return layout(*cfg, nullptr, st, chunks, tensors);
 }
 
 int shampoo_adamw_create(const shampoo_adamw_config *cfg, void *workspace, size_t workspace_bytes, void *stream, shampoo_adamw **out) try {
@@ -132,21 +134,27 @@ int shampoo_adamw_create(const shampoo_adamw_config *cfg, void *workspace, size_
   o->cfg = *cfg;
   o->numel.assign(cfg->numel, cfg->numel + cfg->n_params);
   o->cfg.numel = o->numel.data();
-  TRY(workspace_ok(workspace, workspace_bytes, layout(o->cfg, workspace, o->state, o->chunks)));
-  std::vector<AdamChunk> chunks;
-  int64_t flat = 0, slot = 0;
+  AdamTensor *table;
+  TRY(workspace_ok(workspace, workspace_bytes, layout(o->cfg, workspace, o->state, o->chunks, table)));
+  std::vector<AdamTensor> tensors;
+  int64_t pieces = 0, flat = 0, slot = 0;
   for (int32_t i = 0; i < cfg->n_params; ++i) {
-    o->first.push_back((int64_t)chunks.size());
-    for (int64_t at = 0; at < o->numel[i]; at += AW_CHUNK)
-      chunks.push_back({at, flat + at, slot + at, (int32_t)std::min<int64_t>(AW_CHUNK, o->numel[i] - at), i, !cfg->decay || cfg->decay[i] ? 1 : 0, 0});
-    flat += o->numel[i];
-    slot += groups_of(o->numel[i]) * AW_GROUP;
+    const int64_t n = o->numel[i];
+    o->first.push_back(pieces);
+    tensors.push_back({pieces, n, flat, slot, !cfg->decay || cfg->decay[i] ? 1 : 0, 0});
+    pieces += (n + AW_CHUNK - 1) / AW_CHUNK;
+    flat += n;
+    slot += groups_of(n) * AW_GROUP;
   }
-  o->first.push_back((int64_t)chunks.size());
+  o->first.push_back(pieces);
   o->cfg.decay = nullptr;
   hipStream_t s = static_cast<hipStream_t>(stream);
   HIP_TRY(hipSetDevice(cfg->device));
-  if (!chunks.empty()) HIP_TRY(hipMemcpyAsync(o->chunks, chunks.data(), chunks.size() * sizeof(AdamChunk), hipMemcpyHostToDevice, s));
+  HIP_TRY(hipMemcpyAsync(table, tensors.data(), tensors.size() * sizeof(AdamTensor), hipMemcpyHostToDevice, s));
+  if (pieces > 0) {
+    adamw_chunks_kernel<<<dim3((unsigned)((pieces + 255) / 256)), 256, 0, s>>>(table, cfg->n_params, o->chunks, pieces);
+    HIP_TRY(hipGetLastError());
+  }
   TRY(set_states(o.get(), nullptr, nullptr, s));
   HIP_TRY(hipStreamSynchronize(s));
   *out = o.release();
