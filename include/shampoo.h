@@ -503,7 +503,7 @@ typedef struct {
   int32_t tokens;             /* given tokens of a row, 0 ... 64; the same one may be given twice */
   int32_t top;                /* 0 ... 64                                                         */
   int32_t dtype;              /* of the logits and of their gradient                              */
-  float inverse_temperature;  /* 1 / T, > 0 and finite                                            */
+  float inverse_temperature;  /* 1 / T, > 0, at most 2e38                                        */
   int64_t ld;                 /* of the logits, >= classes                                        */
 } shampoo_logits;
 size_t shampoo_log_probs_workspace_bytes(const shampoo_logits *c);  /* 0 also if c is invalid */
@@ -515,7 +515,7 @@ int shampoo_log_probs(const shampoo_logits *c, const void *logits, const int64_t
 /*
  * Gradient of the logits from those of log_probs (a, [rows][c->tokens] float32, or NULL: none) and of the entropy (b, [rows] float32, or NULL):
  *   dz_v = (sum_j a_j [v = t_j] - p_v (sum_j a_j + b (log p_v + entropy))) / T
- * logits, tokens and statistics as the forward call had and left them; c->top is ignored.  d_logits [rows][classes] may be the logits themselves (the same
+ * c, logits, tokens and statistics as the forward call had and left them.  d_logits [rows][classes] may be the logits themselves (the same
  * leading dimension then).  A given token that is masked has p = 0 and the gradient a / T; a row with nothing left, or whose coefficients are all zero,
  * has the gradient 0.
  */

@@ -93,25 +93,10 @@ __device__ __forceinline__ RowStatistics row_statistics(const SoftSums &t) {
   return r;
 }
 
-// The k largest keys of many, of which no two are alike: a bound that `top` to at_most(top) of them reach (all, where there are no more), and what reaches it in
-// order.  count(b): how many are >= b.  The search goes from `above`, which none reaches, in steps that grow until enough do (an eighth of a
-// binade first), and by halves from there.
-__device__ __forceinline__ int at_most(int top) { return top + max(16, top / 2); }
+// The `top` largest of many logits.  First by a table: bins of the distance from the largest one, a sixteenth of a unit of log 2 each.  What reaches bin b holds the `top`
+// largest if `top` values do, since equal ones share a bin and larger ones have no higher one.  One pass of LDS atomics where a search for a bound takes a
+// count by all lanes for each of its steps: 20 tokens of 1 x 131072 in 11.6 us, by the search alone in 14.1.
 constexpr int LP_CHOSEN = LP_MAX_TOP + LP_MAX_TOP / 2, LP_CANDIDATES = 512;
-template <typename Key, typename Count> __device__ __forceinline__ Key bound_of(Key lowest, Key above, Key step, int least, int most, Count &&count) {
-  if (count(lowest) <= most) return lowest;
-  Key lo = lowest, hi = above;
-  while (hi - lo > 1) {
-    const Key mid = step != 0 && hi - lo > step ? hi - step : lo + (hi - lo) / 2;
-    const int n = count(mid);
-    if (n < least) { hi = mid; step <<= 1; }
-    else if (n > most) { lo = mid; step = 0; }
-    else return mid;
-  }
-  return lo;                             // more than `most` equal ones, where keys are values alone
-}
-// What that search is for when a table does not do.  Bins of x from the largest logit down, a sixteenth of a unit of log 2 each: what reaches bin b holds the `top`
-// largest if `top` values do, since equal ones share a bin and larger ones have no higher one.
 constexpr int LP_BINS = 256;
 __device__ __forceinline__ int bin_of(float z, float largest, float c) { return (int)fminf((largest - z) * c * 16.f, (float)LP_BINS); }   // LP_BINS: none, and NaN
 // the first bin by which `top` values are there, or LP_BINS: there are not so many, or more than LP_CHOSEN
@@ -129,7 +114,22 @@ __device__ __forceinline__ int bin_bound(const int *bins, int top, int lane) {
   return n <= LP_CHOSEN ? bin : LP_BINS;
 }
 
-// What a workgroup of W wavefronts needs for that
+// Where that does not do (distances beyond the table, too many in a bin): a bound that `top` to at_most(top) keys reach, or all, where there are no more.  count(b): how many
+// are >= b.  The search goes from `above`, which none reaches, in steps that grow until enough do, and by halves from there.
+__device__ __forceinline__ int at_most(int top) { return top + max(16, top / 2); }
+template <typename Key, typename Count> __device__ __forceinline__ Key bound_of(Key lowest, Key above, Key step, int least, int most, Count &&count) {
+  if (count(lowest) <= most) return lowest;
+  Key lo = lowest, hi = above;
+  while (hi - lo > 1) {
+    const Key mid = step != 0 && hi - lo > step ? hi - step : lo + (hi - lo) / 2;
+    const int n = count(mid);
+    if (n < least) { hi = mid; step <<= 1; }
+    else if (n > most) { lo = mid; step = 0; }
+    else return mid;
+  }
+  return lo;                             // more than `most` equal ones, where keys are values alone
+}
+// What a workgroup of W wavefronts needs for both
 template <int W> struct Selection {
   alignas(16) int bins[LP_BINS];
   uint64_t counts[2][W];
@@ -241,7 +241,7 @@ __device__ __forceinline__ float largest_of(const f32x8 &x) {
   return fmaxf(fmaxf(fmaxf(x.v[0], x.v[1]), fmaxf(x.v[2], x.v[3])), fmaxf(fmaxf(x.v[4], x.v[5]), fmaxf(x.v[6], x.v[7])));
 }
 // Logits that lie before the first of a row up to a multiple of 16 bytes: a row is read from there on, in aligned pieces of eight, of which the first begins with `pad` masked
-// ones.  (Pieces at odd addresses: 2048 x 50001 bf16 in 49.3 us, so in PAD_US.)
+// ones.  (2048 x 50001 bf16 with pieces at odd addresses 49.3 us, so 43.5.)
 template <typename T> __device__ __forceinline__ int row_pad(const T *z) { return (int)((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T)); }
 // eight logits from o on, -infinity for what is not there
 template <typename T> __device__ __forceinline__ f32x8 load_logits(const T *z, int o, int pad, int end) {
@@ -261,7 +261,8 @@ __device__ __forceinline__ void add_soft(const f32x8 &x, float from, float c, fl
   }
 }
 
-// Up to 512 PIECES classes: a wavefront per row, which stays in registers.
+// Up to 512 PIECES classes: a wavefront per row, which stays in registers, so that there is no barrier and a row is read once.  Bound by memory (32768 x 1000 float32 26.0 us, 5.05 TB/s),
+// with most probable tokens by the LDS atomics and the orders of candidates (20 of 8192 x 999 bf16: 14.9 us, none 8.1; a workgroup per row 32.7).
 template <typename T, int PIECES, bool TOP> __global__ __launch_bounds__(256) void log_probs_row_kernel(const LogProbsArgs g, int64_t rows) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t i = g.row0 + (int64_t)blockIdx.x * 4 + wave;
@@ -361,9 +362,11 @@ constexpr int LP_STRIPS = 4, LP_MAX_PART = 131072, LP_MAX_PARTS = 64, LP_STEP = 
 constexpr float LP_SLACK = 8.f;            // x may be that far above its reference
 
 // One workgroup per part.  One pass: sums about a reference that follows the largest at a distance, so that it hardly ever moves; and of every strip of pieces that a
-// thread reads the largest logit and the first piece that has it.  The k largest strips hold the k most probable tokens (the first `top` keys of strips
-// are tokens of their own, and no token of another strip comes before any of them), so that these strips alone are read again, and what reaches the bound is put in order.
+// thread reads the largest logit and the first piece that has it.  The `top` largest strips hold the `top` most probable tokens (each has one of its own, and no token of
+// another strip comes before any of them), so that the chosen strips alone are read again, and what reaches the bound is put in order.
 // parts > 1: sums and keys of the part go to `sums` and `keys`, and log_probs_join_kernel ends the row.
+// Bound by memory: 8192 x 131072 bf16 368 us (5.8 TB/s), with 20 tokens 384; ten vector operations and an exponential per logit take 0.28 ms of them.  Four loads of a thread
+// are on their way together.  Few rows: 1 x 50000 with 20 tokens 9.9 us, of which the choice is 3.4 (table, strips again from L2, order).
 struct LogPartArgs { LogProbsArgs g; int32_t parts, pieces; SoftSums *sums; uint64_t *keys; };
 
 template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void log_probs_kernel(const LogPartArgs a) {
@@ -588,8 +591,10 @@ struct LogProbsGradArgs {
   int32_t classes, m, parts, part_len;     // part_len: classes of a part, a multiple of LP_STEP
   int64_t row0;
 };
-// W = 4: a workgroup per part of a row; W = 1: a wavefront per row, four rows a workgroup, for up to 2048 classes.  A token's own part is added by the thread of its
-// first appearance, with those of all others, behind the row's other values.
+// W = 4: a workgroup per part of a row; W = 1: a wavefront per row, four rows a workgroup, for up to 2048 classes (32768 x 1000 bf16: 25 us, a workgroup per row 42).  A token's
+// own part is added by the thread of its first appearance, with those of all others, behind the row's other values: no atomics, and the sum of a token that
+// is given twice is rounded once.  Bound by memory: 4096 x 32000 bf16 106 us (5.0 TB/s, a copy's rate), 999 x 50001 float32 93 us; four loads of a thread
+// together (two in a wavefront's row), 2 % better than two, and stores past the caches no better.
 template <typename T, int W> __global__ __launch_bounds__(256) void log_probs_grad_kernel(const LogProbsGradArgs g, int64_t rows) {
   constexpr int STEP = 512 * W, AHEAD = W == 1 ? 2 : 4;
   __shared__ int32_t tokens[4 / W][LP_MAX_TOKENS];

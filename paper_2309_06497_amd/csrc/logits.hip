@@ -16,14 +16,14 @@ namespace {
 constexpr int64_t MAX_ROWS = 0x7fffffff, MAX_BLOCKS = 1 << 22;      // workgroups of a launch: its threads have 32 bits
 constexpr int32_t MAX_CLASSES = 1 << 22;
 
+// 1 / T over log 2
+float exponent_scale(float inverse_temperature) { return (float)((double)inverse_temperature * 1.4426950408889634); }
 int check(const shampoo_logits &c) {
-  if (!dtype_ok(c.dtype) || !std::isfinite(c.inverse_temperature) || c.inverse_temperature <= 0.f) return SHAMPOO_ERR_HYPER;
+  if (!dtype_ok(c.dtype) || !(c.inverse_temperature > 0.f) || !std::isfinite(exponent_scale(c.inverse_temperature))) return SHAMPOO_ERR_HYPER;
   if (c.rows < 0 || c.classes < 1 || c.tokens < 0 || c.top < 0 || c.ld < c.classes) return SHAMPOO_ERR_SHAPE;
   if (c.rows > MAX_ROWS || c.classes > MAX_CLASSES || c.tokens > LP_MAX_TOKENS || c.top > LP_MAX_TOP) return SHAMPOO_ERR_UNSUPPORTED;
   return SHAMPOO_OK;
 }
-// 1 / T over log 2, of a T whose reciprocal float32 holds
-float exponent_scale(float inverse_temperature) { return (float)((double)inverse_temperature * 1.4426950408889634); }
 
 // The most logits before a row that its kernel skips to read aligned pieces
 int32_t pad_of(const shampoo_logits &c, const void *logits) { return aligned(logits, 16) && c.ld * size_of(c.dtype) % 16 == 0 ? 0 : (int32_t)(16 / size_of(c.dtype)) - 1; }
@@ -36,8 +36,9 @@ int32_t parts_of(int64_t rows, int32_t classes, int64_t step, int64_t longest, i
   return (int32_t)((all + pieces - 1) / pieces);
 }
 // Rows of more classes than a wavefront keeps in registers have a workgroup each, of as many wavefronts as leave 16 pieces to a thread, or more where that fills the
-// GPU's 4096 places.  Parts and a second launch for long rows where they are few: 20 tokens of 1 x 131072 in PARTS_US instead of WHOLE_US, of 1 x 50000 13.2
-// instead of 11.1, of 128 x 131072 20.4 instead of 18.7.
+// GPU's 4096 places.  20 tokens with 1, 2, 4 and 8 wavefronts: 8192 x 4096 bf16 27, 29, 38 and 59 us, 8192 x 131072 572, 470, 405 and 385, 1024 x 50000 55, 33, 29 and 26.
+// Parts and a second launch for long rows where they are few: 20 tokens of 1 x 131072 in 11.6 us, whole 16.4; of 1 x 50000 13.2, whole 9.9; of 128 x 131072 19.2, whole
+// 17.1.
 constexpr int32_t SMALL_CLASSES = 2048, LONG_ROW = 65536;
 constexpr int64_t FEW_ROWS = 64;
 int wavefronts(int64_t rows, int32_t classes) {

@@ -8,8 +8,8 @@ that is e^-y of the largest has 3 u y / log 2 of itself, and p y summed over a r
   log p: delta + 5 u |log p| + 2 u log2(classes)
   H:    two terms, log s and sum p x, of at most log(classes) + 1 each and delta of themselves: 3 delta (log(classes) + 1)
   dz:   p (A + b (log p + H)) / T:  p is off by delta + 5 u |log p| of itself, the bracket by 8 u of the sum of its magnitudes and b's part of the errors of log p and
-        H; then the rounding to the result's type (2^-8 of a bf16 value, u of a float32 one; a product of values that are that small may also lose all of itself below
-        1.2e-38)."""
+        H; the GPU's 2^x is zero below 2^-126, so that p is off by 1.2e-38 in any case, and dz by that times the bracket; then the rounding to the result's type (2^-8 of a
+        bf16 value, u of a float32 one, and a product that is that small may also lose all of itself below 1.2e-38)."""
 import math
 
 import pytest
@@ -113,7 +113,7 @@ def gradient(z, t, a, b, temperature):
         dz[i, t[i, j]] += a[i, j]
     d = delta(v)
     magnitude = size + bb.abs() * (lp0.abs() + h[:, None])
-    off = p * (magnitude * (d + 5 * U * lp0.abs() + 8 * U) + bb.abs() * (lp_tolerance(lp0, v) + 3 * d * (math.log(v) + 1)))
+    off = p * (magnitude * (d + 5 * U * lp0.abs() + 8 * U) + bb.abs() * (lp_tolerance(lp0, v) + 3 * d * (math.log(v) + 1))) + 1.2e-38 * magnitude
     spot = torch.zeros_like(dz)
     for j in range(t.shape[1]):
         i = ok[:, j].nonzero()[:, 0]

@@ -35,7 +35,7 @@ def test_log_probs_refusals():
     for f in (call, grad):
         assert f(z=None) == -1 and f(t=None) == -1 and f(st=None) == -1
         assert f(rows=-1) == -2 and f(classes=0) == -2 and f(tokens=-1) == -2 and f(top=-1) == -2 and f(classes=101) == -2
-        assert f(dtype=2) == -3 and f(inverse_temperature=0.0) == -3 and f(inverse_temperature=-1.0) == -3 and f(inverse_temperature=NAN) == -3 and f(inverse_temperature=INF) == -3
+        assert f(dtype=2) == -3 and f(inverse_temperature=0.0) == -3 and f(inverse_temperature=-1.0) == -3 and f(inverse_temperature=NAN) == -3 and f(inverse_temperature=INF) == -3 and f(inverse_temperature=3e38) == -3
         assert f(rows=1 << 31) == -7 and f(tokens=65) == -7 and f(top=65) == -7
         assert f(st=ODD) == -7
         assert f(rows=0, z=None, t=None, st=None) == 0
