@@ -1,7 +1,7 @@
 """The AdamW step over many tensors, its 8-bit states and the norm of all gradients against the definitions in 64 bits.
 
 u = 2^-24 is half a step of float32.  m is a sum of two products, each rounded and the weights too: 2 u of both products and u of the sum, 4 u (|b1 m| + |(1 - b1) g|) with
-the limited gradient's own u.  v: one product more, 5 u of v.  The update: sqrt, its scale, epsilon, quotient and lr: 8 u of the update and half the error of v (2.5 u) and that of m, which
+a limited gradient's own 2 u more.  v: one product more, 5 u of v.  The update: sqrt, its scale, epsilon, quotient and lr: 8 u of the update and half the error of v (2.5 u) and that of m, which
 is not relative to m; the result: 2 u of what is left of w, u of the sum.
 A state of 8 bits is the value's code after floor(value / step + offset), with an offset in 2^-20 steps: the kernel's value is the one above, and where
 value / step + offset is nearer to a whole number than that error, either neighbour is right."""
@@ -50,26 +50,32 @@ def held(x, binades, offset, largest=None):
 
 
 def rounded8(got, value, off, binades, offset, what):
-    """got: what 8 bits hold of a value that is off by `off` at most.  The largest of a group is off as well: beside a power of two (a tenth of a bf16 value can be one) either
+    """got: what 8 bits hold of a value that is off by `off` at most, and below the lowest binade by 2^-21 of a step more: there the value is first rounded to whole 2^-20 steps.
+    The largest of a group is off as well: beside a power of two (a tenth of a bf16 value can be one) either
     side of it is right.  A v below 1.2e-38 may be zero in float32, and its code then."""
-    want, _ = held(value, binades, offset)
+    want, unit = held(value, binades, offset)
+    off = off + unit * 2.0 ** -21
     assert np.array_equal(np.isnan(got), np.isnan(want)), what
     pad = lambda x: np.pad(x, (0, -len(x) % GROUP)).reshape(-1, GROUP)
     ok = (np.abs(value) < 1.2e-38) & (got == 0)
     for side in (-1, 1):
         with np.errstate(invalid="ignore"):
-            _, unit = held(value, binades, offset, np.maximum(pad(np.abs(value)) + side * pad(off), 0.0).max(1, keepdims=True))
-        low, high = (np.floor(np.maximum(np.abs(value) + s * off, 0.0) / unit + offset) * unit for s in (-1, 1))
-        if binades == 30:
-            high = np.maximum(high, unit)
+            largest = np.maximum(pad(np.abs(value)) + side * pad(off), 0.0).max(1, keepdims=True)
+            low, high = (np.abs(held(np.maximum(np.abs(value) + s * off, 0.0), binades, offset, largest)[0]) for s in (-1, 1))     # rounding keeps the order of values
         ok |= (np.abs(got) >= low * (1 - 1e-15)) & (np.abs(got) <= high * (1 + 1e-15))
     differ = (got != want) & ~np.isnan(want)
     assert ok[differ].all(), (what, got[differ & ~ok][:3], value[differ & ~ok][:3])
 
 
-def held_range(value, off, unit, offset, sign):
-    x = np.maximum(np.abs(value) + sign * off, 0.0)
-    return np.floor(x / unit + offset) * unit, unit
+def rounded16(got, value, off, offset):
+    """The same for bf16 parameters"""
+    ends = []
+    for sign in (-1, 1):
+        x = np.maximum(np.abs(value) + sign * off, 0.0)
+        unit = np.ldexp(1.0, np.maximum(np.frexp(x)[1] - 8, -133))
+        ends.append(np.floor(x / unit + offset) * unit)
+    ok = (np.abs(got) >= ends[0] * (1 - 1e-15)) & (np.abs(got) <= ends[1] * (1 + 1e-15))
+    return ok & ((got == 0) | (np.sign(got) == np.sign(value)) | (np.abs(value) <= off))
 
 
 class Model:
@@ -80,16 +86,17 @@ class Model:
         self.beta1, self.beta2, self.epsilon, self.weight_decay = beta1, beta2, epsilon, weight_decay
         self.decay = decay or [True] * len(shapes)
 
-    def step(self, i, w, g, m, v, lr, t):
+    def step(self, i, w, g, m, v, lr, t, limited=0):
         wd = self.weight_decay if self.decay[i] else 0.0
         m1 = self.beta1 * m + (1 - self.beta1) * g
         v1 = self.beta2 * v + (1 - self.beta2) * g * g
         root = np.sqrt(v1 / (1 - self.beta2 ** (t + 1))) + self.epsilon
         c = lr / (1 - self.beta1 ** (t + 1))
         w1 = w * (1 - lr * wd) - c * m1 / root
-        off_m = 5 * U * (np.abs(self.beta1 * m) + np.abs((1 - self.beta1) * g)) + 1e-44
-        off_v = 6 * U * v1 + 4e-38 * U          # squares of float32 may be subnormal
-        off_w = 3 * U * np.abs(w) + abs(c) * (11 * U * np.abs(m1) + off_m) / root + abs(c) * np.abs(m1) / root ** 2 * np.sqrt(3e-45) + U * np.abs(w1)
+        k = 2 * limited                         # a gradient that was limited: the norm's rounding and the quotient's
+        off_m = (5 + k) * U * (np.abs(self.beta1 * m) + np.abs((1 - self.beta1) * g)) + 1e-44
+        off_v = (6 + 2 * k) * U * v1 + 4e-38 * U          # squares of float32 may be subnormal
+        off_w = 3 * U * np.abs(w) + abs(c) * ((11 + k) * U * np.abs(m1) + off_m) / root + abs(c) * np.abs(m1) / root ** 2 * np.sqrt(3e-45) + U * np.abs(w1)
         return m1, v1, w1, off_m, off_v, off_w
 
 
@@ -132,16 +139,14 @@ def run(shapes, bits, param, grad, steps=3, copies=False, clip=None, views=False
             norm, limit = B.shampoo_gradient_norm(g)[0], clip
             size = math.sqrt(sum(float((x * x).sum()) for x in g0))
             assert abs(float(norm) - size) <= U * size * 1.01
-            g0 = [x * min(1.0, limit / size) for x in g0]
+            g0 = [x * (limit / size if size > limit else 1.0) for x in g0]
         opt.step(w, g, lr, t, copies=c, norm=norm, max_norm=limit)
         m1, v1 = (flat(x) for x in opt.state())
         for i, n in enumerate(model.sizes):
             if n == 0:
                 continue
             at = slice(starts[i], starts[i + 1])
-            wm, wv, ww, em, ev, ew = model.step(i, w0[i], g0[i], m0[at], v0[at], lr, t)
-            if clip:
-                em, ev, ew = em + 2 * U * np.abs(0.1 * g0[i]), ev + 4 * U * wv, ew + lr * 8 * U * 40
+            wm, wv, ww, em, ev, ew = model.step(i, w0[i], g0[i], m0[at], v0[at], lr, t, 1 if clip else 0)
             om, ov, ow = offsets(starts[i], n, t)
             what = (shapes[i], bits, param, grad, k)
             if bits == 32:
@@ -155,10 +160,7 @@ def run(shapes, bits, param, grad, steps=3, copies=False, clip=None, views=False
                 if copies:
                     assert torch.equal(c[i], w[i].bfloat16()), what
             else:
-                with np.errstate(divide="ignore"):
-                    unit = np.ldexp(1.0, np.maximum(np.frexp(ww)[1] - 8, -133))
-                low, high = (held_range(ww, ew, unit, ow, s)[0] for s in (-1, 1))
-                ok = (np.abs(got) >= low * (1 - 1e-15)) & (np.abs(got) <= high * (1 + 1e-15)) & ((got == 0) | (np.sign(got) == np.sign(ww)) | (np.abs(ww) <= ew))
+                ok = rounded16(got, ww, ew, ow)
                 assert ok.all(), (what, got[~ok][:3], ww[~ok][:3])
     return opt, w
 
@@ -392,10 +394,7 @@ def test_indices_beyond_32_bits():
         om, ov, ow = offsets(5 + at, k, 9)
         rounded8(flat(m[5 + at:5 + at + k]), wm, em, 14, om, at)
         rounded8(flat(v[5 + at:5 + at + k]), wv, ev, 30, ov, at)
-        unit = np.ldexp(1.0, np.frexp(ww)[1] - 8)
-        got = flat(w[1][at:at + k])
-        low, high = (held_range(ww, ew, unit, ow, s)[0] for s in (-1, 1))
-        assert ((np.abs(got) >= low * (1 - 1e-15)) & (np.abs(got) <= high * (1 + 1e-15))).all()
+        assert rounded16(flat(w[1][at:at + k]), ww, ew, ow).all()
     norm, norms = B.shampoo_gradient_norm(g)
     assert abs(float(norm) - math.sqrt(square)) <= 2 * U * math.sqrt(square) and float(norms[0]) == 0 and float(norms[1]) == float(norm)
 
