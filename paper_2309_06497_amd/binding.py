@@ -648,6 +648,8 @@ class AdamW:
         with torch.cuda.device(self.device):
             _check(lib().shampoo_adamw_create(ctypes.byref(self.cfg), ctypes.c_void_p(self.workspace.data_ptr()), nbytes, _stream_ptr(),
                                               ctypes.byref(self.handle)))
+        size = 4 * self.total
+        self._views = tuple(self.workspace[at:at + size].view(torch.float32) for at in (0, (size + 255) // 256 * 256)) if state_bits == 32 else None
         ops = _ops or _load_ops()
         self._step = ops.adamw_step
         self._stepper = ops.make(0, self.handle.value, device, grad_dtype == GRAD_BF16, self.shapes)
@@ -665,8 +667,7 @@ class AdamW:
         if not self.handle:
             raise ShampooError(-1)
         if self.state_bits == 32:
-            size = 4 * self.total
-            return tuple(self.workspace[at:at + size].view(torch.float32) for at in (0, (size + 255) // 256 * 256))
+            return self._views
         m, v = (torch.empty(self.total, dtype=torch.bfloat16, device=self.device) for _ in range(2))
         with torch.cuda.device(self.device):
             _check(lib().shampoo_adamw_get(self.handle, ctypes.c_void_p(m.data_ptr()), ctypes.c_void_p(v.data_ptr()), GRAD_BF16, _stream_ptr()))

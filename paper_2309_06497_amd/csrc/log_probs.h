@@ -98,7 +98,8 @@ __device__ __forceinline__ RowStatistics row_statistics(const SoftSums &t) {
 // count by all lanes for each of its steps: 20 tokens of 1 x 131072 in 11.6 us, by the search alone in 14.1.
 constexpr int LP_CHOSEN = LP_MAX_TOP + LP_MAX_TOP / 2, LP_CANDIDATES = 512;
 constexpr int LP_BINS = 256;
-__device__ __forceinline__ int bin_of(float z, float largest, float c) { return (int)fminf((largest - z) * c * 16.f, (float)LP_BINS); }   // LP_BINS: none, and NaN
+__device__ __forceinline__ float bin_distance(float z, float largest, float c) { return (largest - z) * c * 16.f; }
+__device__ __forceinline__ int bin_of(float z, float largest, float c) { return (int)fminf(bin_distance(z, largest, c), (float)LP_BINS); }   // LP_BINS: none, and NaN
 // the first bin by which `top` values are there, or LP_BINS: there are not so many, or more than LP_CHOSEN
 __device__ __forceinline__ int bin_bound(const int *bins, int top, int lane) {
   const int4 b = reinterpret_cast<const int4 *>(bins)[lane];
@@ -269,6 +270,7 @@ template <typename T, int PIECES, bool TOP> __global__ __launch_bounds__(256) vo
   if (i >= rows) return;
   const T *z = static_cast<const T *>(g.z) + i * g.ld;
   f32x8 x[PIECES];
+  float largest[PIECES];
   SoftSums t = {-INFINITY, 0.f, 0.f};
 #pragma unroll
   for (int p = 0; p < PIECES; ++p) {
@@ -276,7 +278,8 @@ template <typename T, int PIECES, bool TOP> __global__ __launch_bounds__(256) vo
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (p * 512 + lane * 8 + e >= g.classes) x[p].v[e] = -INFINITY;
-    t.m = fmaxf(t.m, largest_of(x[p]));
+    largest[p] = largest_of(x[p]);
+    t.m = fmaxf(t.m, largest[p]);
   }
   t.m = wave_max(t.m);
 #pragma unroll
@@ -291,65 +294,83 @@ template <typename T, int PIECES, bool TOP> __global__ __launch_bounds__(256) vo
     __shared__ int4 table[4][LP_BINS / 4];
     uint64_t *const candidate = keys[wave];
     int *const bins = reinterpret_cast<int *>(table[wave]);
-    table[wave][lane] = make_int4(0, 0, 0, 0);
-    uint32_t order[8 * PIECES];
-    wavefront_order();
+    // Pieces of eight first: as many as `top` of them within a bin hold the `top` largest, and an eighth of the atomics tells which bin.  Then the logits themselves.
+    int n = LP_CHOSEN + 1;
+    const auto choose = [&](auto &&add) {
+      table[wave][lane] = make_int4(0, 0, 0, 0);
+      wavefront_order();
+      add();
+      wavefront_order();
+      const int by_bin = bin_bound(bins, g.top, lane);
+      wavefront_order();
+      if (by_bin == LP_BINS) return;
+      n = 0;
 #pragma unroll
-    for (int e = 0; e < 8 * PIECES; ++e) {
-      const int bin = bin_of(x[e >> 3].v[e & 7], t.m, g.c);
+      for (int e = 0; e < 8 * PIECES; ++e) {
+        const float z = x[e >> 3].v[e & 7];
+        const bool in = bin_distance(z, t.m, g.c) < (float)(by_bin + 1);
+        const uint64_t mask = __ballot(in);
+        if (mask == 0) continue;
+        const int to = n + lanes_before(mask);
+        if (in && to < LP_CHOSEN) candidate[to] = logit_key(z, (e >> 3) * 512 + lane * 8 + (e & 7));
+        n += __popcll(mask);
+      }
+    };
+    const auto count_in = [&](float z) {
+      const int bin = bin_of(z, t.m, g.c);
       if (bin < LP_BINS) atomicAdd(&bins[bin], 1);
-    }
-    wavefront_order();
-    const int by_bin = bin_bound(bins, g.top, lane);
-    uint32_t bound = 1;
-    bool ties = false;
-    if (by_bin < LP_BINS) {
+    };
+    choose([&]() {
 #pragma unroll
-      for (int e = 0; e < 8 * PIECES; ++e)
-        order[e] = bin_of(x[e >> 3].v[e & 7], t.m, g.c) <= by_bin ? (uint32_t)(logit_key(x[e >> 3].v[e & 7], 0) >> 32) : 0u;
-    } else {
+      for (int p = 0; p < PIECES; ++p) count_in(largest[p]);
+    });
+    if (n > LP_CHOSEN) choose([&]() {
+#pragma unroll
+      for (int e = 0; e < 8 * PIECES; ++e) count_in(x[e >> 3].v[e & 7]);
+    });
+    if (n > LP_CHOSEN) {
+      uint32_t order[8 * PIECES];
 #pragma unroll
       for (int e = 0; e < 8 * PIECES; ++e) order[e] = (uint32_t)(logit_key(x[e >> 3].v[e & 7], 0) >> 32);
       const auto count = [&](uint32_t from) {
-        int n = 0;
-#pragma unroll
-        for (int e = 0; e < 8 * PIECES; ++e) n += __popcll(__ballot(order[e] >= from));
-        return n;
-      };
-      const int most = at_most(g.top);
-      const uint32_t above = (uint32_t)(logit_key(t.m, 0) >> 32) + 1;
-      bound = bound_of<uint32_t>(1, above, 1u << 20, g.top, most, count);
-      ties = count(bound) > most;          // those above, and of equal ones the first
-      if (ties) ++bound;
-    }
-    int n = 0;
-    const auto key = [&](int e) { return (uint64_t)order[e] << 32 | (0xffffffffu - (uint32_t)((e >> 3) * 512 + lane * 8 + (e & 7))); };
-#pragma unroll
-    for (int e = 0; e < 8 * PIECES; ++e) {
-      const bool in = order[e] >= bound;
-      const uint64_t mask = __ballot(in);
-      if (in) candidate[n + lanes_before(mask)] = key(e);
-      n += __popcll(mask);
-    }
-    if (ties) {
-#pragma unroll
-      for (int p = 0; p < PIECES; ++p) {
-        int mine = 0, before = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) mine += order[8 * p + e] == bound - 1 ? 1 : 0;
         int all = 0;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const uint64_t mask = __ballot((mine >> b) & 1);
-          before += lanes_before(mask) << b; all += __popcll(mask) << b;
-        }
+        for (int e = 0; e < 8 * PIECES; ++e) all += __popcll(__ballot(order[e] >= from));
+        return all;
+      };
+      const int most = at_most(g.top);
+      uint32_t bound = bound_of<uint32_t>(1, (uint32_t)(logit_key(t.m, 0) >> 32) + 1, 1u << 20, g.top, most, count);
+      const bool ties = count(bound) > most;      // those above, and of equal ones the first
+      if (ties) ++bound;
+      const auto key = [&](int e) { return (uint64_t)order[e] << 32 | (0xffffffffu - (uint32_t)((e >> 3) * 512 + lane * 8 + (e & 7))); };
+      n = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (order[8 * p + e] == bound - 1) {
-            if (n + before < g.top) candidate[n + before] = key(8 * p + e);
-            ++before;
+      for (int e = 0; e < 8 * PIECES; ++e) {
+        const bool in = order[e] >= bound;
+        const uint64_t mask = __ballot(in);
+        if (in) candidate[n + lanes_before(mask)] = key(e);
+        n += __popcll(mask);
+      }
+      if (ties) {
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+          int mine = 0, before = 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) mine += order[8 * p + e] == bound - 1 ? 1 : 0;
+          int all = 0;
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            const uint64_t mask = __ballot((mine >> b) & 1);
+            before += lanes_before(mask) << b; all += __popcll(mask) << b;
           }
-        n = min(n + all, g.top);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (order[8 * p + e] == bound - 1) {
+              if (n + before < g.top) candidate[n + before] = key(8 * p + e);
+              ++before;
+            }
+          n = min(n + all, g.top);
+        }
       }
     }
     wavefront_order();

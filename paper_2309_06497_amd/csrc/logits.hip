@@ -141,7 +141,8 @@ int shampoo_log_probs_grad(const shampoo_logits *c, const void *logits, const in
   g.dz = d_logits; g.ld_dz = ld_d_logits; g.c = exponent_scale(c->inverse_temperature); g.tau = c->inverse_temperature;
   g.classes = c->classes; g.m = d_log_probs ? c->tokens : 0;
   int32_t pieces;
-  if (c->classes <= SMALL_CLASSES) return by_rows(c->rows, 1, [&](int64_t r, unsigned n) {
+  // A wavefront per row: 32768 x 2100 bf16 52 us, a workgroup per row 96; 8192 x 4096 bf16 22.6, 23.4; 4096 x 4096 float32 26.8, 24.8; 4096 x 2100 float32 14.3, 16.4.
+  if (c->classes <= (c->dtype == SHAMPOO_GRAD_F32 ? 3584 : 4096)) return by_rows(c->rows, 1, [&](int64_t r, unsigned n) {
     g.row0 = r;
     if (c->dtype == SHAMPOO_GRAD_F32) log_probs_grad_kernel<float, 1><<<dim3((n + 3) / 4), 256, 0, s>>>(g, r + n);
     else log_probs_grad_kernel<uint16_t, 1><<<dim3((n + 3) / 4), 256, 0, s>>>(g, r + n);
