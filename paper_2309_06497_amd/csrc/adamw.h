@@ -146,7 +146,9 @@ __device__ __forceinline__ void rounding_offsets(uint64_t i, uint32_t mix, uint3
   }
 }
 
-// P, G: types of parameters and gradients (float or uint16_t, bf16 bits).  A thread has eight neighbouring elements.
+// P, G: types of parameters and gradients (float or uint16_t, bf16 bits).  A thread has eight neighbouring elements, a workgroup 2048 (4096 and 8192: 4 and 5 % longer with float32
+// parameters).  Bound by memory: 200 M float32 parameters with bf16 gradients and copies, 32 bits 1.03 ms (28 bytes each, 5.4 TB/s), 671 M with 8 bits 1.99 ms (16 bytes, 5.4 TB/s);
+// bf16 parameters with 8 bits (10 bytes) by 72 vector operations an element, three of them products of 32 bits for the random numbers: 67 M in 160 us, 4.2 TB/s.
 template <typename P, typename G, int BITS> __global__ __launch_bounds__(256) void adamw_kernel(const AdamArgs g) {
   const AdamChunk c = g.chunks[blockIdx.x];
   float clip = 1.f;
@@ -176,7 +178,7 @@ template <typename P, typename G, int BITS> __global__ __launch_bounds__(256) vo
       const float k = product(x.v[e], clip);
       m.v[e] = sum(product(m.v[e], g.b1), product(k, g.b1c));
       v.v[e] = sum(product(v.v[e], g.b2), product(product(k, g.b2c), k));
-      // root and reciprocal of the GPU's instructions: within one step; a v below 1.2e-38 has the root 0, a millionth of epsilon
+      // root and reciprocal of the GPU's instructions: within one step; a v below 1.2e-38 has the root 0, not 1.1e-19 or less: epsilon is 1e-12 at least
       const float u = m.v[e] * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v.v[e]), g.inv_sqrt, g.epsilon));
       w.v[e] = fmaf(-g.lr, u, w.v[e] * keep);
     }
@@ -252,7 +254,8 @@ template <int BITS> __global__ __launch_bounds__(256) void adamw_set_kernel(cons
 }
 
 // ---------------------------------------------------------------------------
-// Norms: sums of squares in 64 bits (no float32 gradient's square leaves their range), one per piece of a tensor, added up in order.
+// Norms: sums of squares in 64 bits (no float32 gradient's square leaves their range), one per piece of a tensor, added up in order.  Bound by memory: 671 M bf16 gradients 222 us,
+// 6.0 TB/s, four loads of a thread on their way together (one: 273).
 // ---------------------------------------------------------------------------
 constexpr int GN_TENSORS = 192;
 struct NormArgs {

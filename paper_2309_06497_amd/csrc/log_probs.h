@@ -387,7 +387,8 @@ constexpr float LP_SLACK = 8.f;            // x may be that far above its refere
 // another strip comes before any of them), so that the chosen strips alone are read again, and what reaches the bound is put in order.
 // parts > 1: sums and keys of the part go to `sums` and `keys`, and log_probs_join_kernel ends the row.
 // Bound by memory: 8192 x 131072 bf16 368 us (5.8 TB/s), with 20 tokens 384; ten vector operations and an exponential per logit take 0.28 ms of them.  Four loads of a thread
-// are on their way together.  Few rows: 1 x 50000 with 20 tokens 9.9 us, of which the choice is 3.4 (table, strips again from L2, order).
+// are on their way together.  Four strips a thread: with 20 tokens 7 % more is read; two cost as much, eight (fewer logits again, more of everything else) 396 and, for 8192 x 32000, 139
+// instead of 114.  Few rows: 1 x 50000 with 20 tokens 9.9 us, of which the choice is 3.4 (table, strips again from L2, order).
 struct LogPartArgs { LogProbsArgs g; int32_t parts, pieces; SoftSums *sums; uint64_t *keys; };
 
 template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void log_probs_kernel(const LogPartArgs a) {
