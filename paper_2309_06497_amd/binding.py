@@ -486,7 +486,7 @@ def _load_ops():
         "linear_cross_entropy_workspace_bytes", "linear_cross_entropy", "checkpoint_bytes", "checkpoint_pack", "checkpoint_unpack",
         "checkpoint_activation_grad", "checkpoint_weight_grad_workspace_bytes", "checkpoint_weight_grad", "residual_norm_forward",
         "residual_norm_backward_workspace_bytes", "residual_norm_backward", "log_probs_workspace_bytes", "log_probs", "log_probs_grad",
-        "gradient_norm_workspace_bytes", "gradient_norm", "adamw_step")])
+        "gradient_norm_workspace_bytes", "gradient_norm", "adamw_step", "adamw_get")])
     _codes = {torch.float32: GRAD_F32, torch.bfloat16: GRAD_BF16}
     _DTYPES = (torch.float32, torch.bfloat16)
     _ops = _marshal
@@ -623,7 +623,7 @@ def shampoo_gradient_norm(grads):
 
 class AdamW:
     """AdamW over one list of parameters: owns the workspace tensor, which holds all state, and the library handle.  decay: for every parameter
-    whether weight_decay applies to it (default: to all)."""
+    whether weight_decay applies to it (default: to all).  Calls on several streams are ordered by the caller."""
 
     def __init__(self, shapes, beta1=0.9, beta2=0.999, epsilon=1e-8, weight_decay=0.01, decay=None, state_bits=32, param_dtype=GRAD_F32,
                  grad_dtype=GRAD_F32, device=0):
@@ -651,7 +651,7 @@ class AdamW:
         size = 4 * self.total
         self._views = tuple(self.workspace[at:at + size].view(torch.float32) for at in (0, (size + 255) // 256 * 256)) if state_bits == 32 else None
         ops = _ops or _load_ops()
-        self._step = ops.adamw_step
+        self._step, self._state = ops.adamw_step, ops.adamw_state
         self._stepper = ops.make(0, self.handle.value, device, grad_dtype == GRAD_BF16, self.shapes)
 
     def step(self, params, grads, lr, step, copies=None, norm=None, max_norm=float("inf")):
@@ -663,15 +663,11 @@ class AdamW:
     def state(self):
         """(m, v) of all parameters, one behind the other: with 32 bits views of the optimizer's memory, with 8 bits the values that it holds, as
         bfloat16 (which holds them exactly)."""
-        import torch
         if not self.handle:
             raise ShampooError(-1)
         if self.state_bits == 32:
             return self._views
-        m, v = (torch.empty(self.total, dtype=torch.bfloat16, device=self.device) for _ in range(2))
-        with torch.cuda.device(self.device):
-            _check(lib().shampoo_adamw_get(self.handle, ctypes.c_void_p(m.data_ptr()), ctypes.c_void_p(v.data_ptr()), GRAD_BF16, _stream_ptr()))
-        return m, v
+        return _result(self._state(self._stepper, self.total))
 
     def load(self, m, v):
         """The states of another optimizer, as state() gives them (any floating type)."""

@@ -93,29 +93,32 @@ __device__ __forceinline__ RowStatistics row_statistics(const SoftSums &t) {
   return r;
 }
 
-// The `top` largest of many logits.  First by a table: bins of the distance from the largest one, a sixteenth of a unit of log 2 each.  What reaches bin b holds the `top`
-// largest if `top` values do, since equal ones share a bin and larger ones have no higher one.  One pass of LDS atomics where a search for a bound takes a
-// count by all lanes for each of its steps: 20 tokens of 1 x 131072 in 11.6 us, by the search alone in 14.1.
+// The `top` largest of many logits.  First by a table: bins of the distance from the largest one, 64 to each doubling of 1 + that distance in units of log 2, up to 255 units (a row that is
+// sure of one token has its others far away).  What reaches bin b holds the `top` largest if `top` values do, since equal ones share a bin and larger ones have
+// no higher one.  One pass of LDS atomics where a search for a bound takes a count by all lanes for each of its steps: 20 tokens of 1 x 131072 in 11.6 us, by the
+// search alone in 14.1.
 constexpr int LP_CHOSEN = LP_MAX_TOP + LP_MAX_TOP / 2, LP_CANDIDATES = 512;
-constexpr int LP_BINS = 256;
-__device__ __forceinline__ float bin_distance(float z, float largest, float c) { return (largest - z) * c * 16.f; }
-__device__ __forceinline__ int bin_of(float z, float largest, float c) { return (int)fminf(bin_distance(z, largest, c), (float)LP_BINS); }   // LP_BINS: none, and NaN
+constexpr int LP_BINS = 512;
+constexpr uint32_t LP_BIN_SHIFT = 17, LP_BIN_FIRST = 0x3f800000u >> LP_BIN_SHIFT;      // the upper bits of a float32 are the bin
+__device__ __forceinline__ uint32_t bin_bits(float z, float largest, float c) { return __float_as_uint(fmaf(largest - z, c, 1.f)); }
+__device__ __forceinline__ int bin_of(float z, float largest, float c) { return (int)min((bin_bits(z, largest, c) >> LP_BIN_SHIFT) - LP_BIN_FIRST, (uint32_t)LP_BINS); }   // LP_BINS: none, and NaN
+__device__ __forceinline__ bool within_bin(float z, float largest, float c, int bin) { return bin_bits(z, largest, c) < (uint32_t)(bin + 1 + (int)LP_BIN_FIRST) << LP_BIN_SHIFT; }
 // the first bin by which `top` values are there, or LP_BINS: there are not so many, or more than LP_CHOSEN
 __device__ __forceinline__ int bin_bound(const int *bins, int top, int lane) {
-  const int4 b = reinterpret_cast<const int4 *>(bins)[lane];
-  const int upto = wave_scan(b.x + b.y + b.z + b.w);
+  const int4 p = reinterpret_cast<const int4 *>(bins)[2 * lane], q = reinterpret_cast<const int4 *>(bins)[2 * lane + 1];
+  const int here[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+  const int all = ((p.x + p.y) + (p.z + p.w)) + ((q.x + q.y) + (q.z + q.w)), upto = wave_scan(all);
   const uint64_t enough = __ballot(upto >= top);
   if (enough == 0) return LP_BINS;
+  int n = upto - all, bin = 8 * lane - 1;
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (n < top) { n += here[k]; ++bin; }
   const int at = __builtin_ctzll(enough);
-  const int x = __builtin_amdgcn_readlane(b.x, at), y = __builtin_amdgcn_readlane(b.y, at), z = __builtin_amdgcn_readlane(b.z, at), w = __builtin_amdgcn_readlane(b.w, at);
-  int n = __builtin_amdgcn_readlane(upto, at) - (x + y + z + w) + x, bin = 4 * at;
-  if (n < top) { n += y; ++bin; }
-  if (n < top) { n += z; ++bin; }
-  if (n < top) { n += w; ++bin; }
-  return n <= LP_CHOSEN ? bin : LP_BINS;
+  return __builtin_amdgcn_readlane(n, at) <= LP_CHOSEN ? __builtin_amdgcn_readlane(bin, at) : LP_BINS;
 }
 
-// Where that does not do (distances beyond the table, too many in a bin): a bound that `top` to at_most(top) keys reach, or all, where there are no more.  count(b): how many
+// Where that does not do (tiny spreads, too many in a bin): a bound that `top` to at_most(top) keys reach, or all, where there are no more.  count(b): how many
 // are >= b.  The search goes from `above`, which none reaches, in steps that grow until enough do, and by halves from there.
 __device__ __forceinline__ int at_most(int top) { return top + max(16, top / 2); }
 template <typename Key, typename Count> __device__ __forceinline__ Key bound_of(Key lowest, Key above, Key step, int least, int most, Count &&count) {
@@ -297,7 +300,7 @@ template <typename T, int PIECES, bool TOP> __global__ __launch_bounds__(256) vo
     // Pieces of eight first: as many as `top` of them within a bin hold the `top` largest, and an eighth of the atomics tells which bin.  Then the logits themselves.
     int n = LP_CHOSEN + 1;
     const auto choose = [&](auto &&add) {
-      table[wave][lane] = make_int4(0, 0, 0, 0);
+      table[wave][lane] = table[wave][64 + lane] = make_int4(0, 0, 0, 0);
       wavefront_order();
       add();
       wavefront_order();
@@ -308,7 +311,7 @@ template <typename T, int PIECES, bool TOP> __global__ __launch_bounds__(256) vo
 #pragma unroll
       for (int e = 0; e < 8 * PIECES; ++e) {
         const float z = x[e >> 3].v[e & 7];
-        const bool in = bin_distance(z, t.m, g.c) < (float)(by_bin + 1);
+        const bool in = within_bin(z, t.m, g.c, by_bin);
         const uint64_t mask = __ballot(in);
         if (mask == 0) continue;
         const int to = n + lanes_before(mask);
@@ -483,7 +486,7 @@ template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void
     bool chosen[LP_STRIPS];
     if (by_bin < LP_BINS) {
 #pragma unroll
-      for (int k = 0; k < LP_STRIPS; ++k) chosen[k] = bin_of(largest[k], most, g.c) <= by_bin;
+      for (int k = 0; k < LP_STRIPS; ++k) chosen[k] = within_bin(largest[k], most, g.c, by_bin);
     } else {
       uint64_t key[LP_STRIPS];
 #pragma unroll
@@ -517,7 +520,7 @@ template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void
         const f32x8 x = load_logits(z, o, pad, end);
         uint64_t keys[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) keys[e] = by_bin == LP_BINS || bin_of(x.v[e], most, g.c) <= by_bin ? logit_key(x.v[e], o + e) : 0;
+        for (int e = 0; e < 8; ++e) keys[e] = by_bin == LP_BINS || within_bin(x.v[e], most, g.c, by_bin) ? logit_key(x.v[e], o + e) : 0;
         f(keys);
       }
     };
@@ -583,7 +586,7 @@ template <typename T> __global__ __launch_bounds__(256) void log_probs_join_kern
   if (g.top == 0) return;
   most = wave_max(most);
   if (lane == 0) part_most[tid >> 6] = most;
-  l.bins[tid] = 0;
+  l.bins[tid] = l.bins[256 + tid] = 0;
   if (tid == 0) l.n_candidates = 0;
   __syncthreads();
   most = fmaxf(fmaxf(part_most[0], part_most[1]), fmaxf(part_most[2], part_most[3]));

@@ -139,8 +139,9 @@ struct Library {
   decltype(&shampoo_gradient_norm_workspace_bytes) gradient_norm_bytes;
   decltype(&shampoo_gradient_norm) gradient_norm;
   decltype(&shampoo_adamw_step) adamw_step;
+  decltype(&shampoo_adamw_get) adamw_get;
 } library;
-static_assert(sizeof(Library) == 17 * sizeof(void *), "addresses only");
+static_assert(sizeof(Library) == 18 * sizeof(void *), "addresses only");
 
 // use([addresses of the entry points in the order above])
 PyObject *use(PyObject *, PyObject *list) {
@@ -594,11 +595,25 @@ PyObject *adamw_step(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
   });
 }
 
+// (stepper, elements of all parameters) -> (m, v), bfloat16
+PyObject *adamw_state(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
+  return guarded(n_args, 2, [&]() -> PyObject * {
+    auto *s = static_cast<Stepper *>(PyCapsule_GetPointer(a[0], CAPSULE));
+    if (!s) return nullptr;
+    const int64_t total = integer(a[1]);
+    const auto options = at::TensorOptions().dtype(at::kBFloat16).device(s->device);
+    const at::Tensor m = at::empty({total}, options), v = at::empty({total}, options);
+    const c10::hip::HIPGuard guard(s->device.index());
+    const int rc = library.adamw_get(static_cast<shampoo_adamw *>(s->handle), m.data_ptr(), v.data_ptr(), SHAMPOO_GRAD_BF16, c10::hip::getCurrentHIPStream(s->device.index()).stream());
+    return rc != 0 ? PyLong_FromLong(rc) : tuple({m, v});
+  });
+}
+
 #define OPERATOR(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"make", make, METH_VARARGS, nullptr}, {"step", step, METH_VARARGS, nullptr}, {"use", use, METH_O, nullptr},
                          OPERATOR(cross_entropy), OPERATOR(pack), OPERATOR(unpack), OPERATOR(activation_grad), OPERATOR(weight_grad),
                          OPERATOR(norm_forward), OPERATOR(norm_backward), OPERATOR(log_probs), OPERATOR(log_probs_grad),
-                         OPERATOR(gradient_norm), OPERATOR(adamw_step), {nullptr, nullptr, 0, nullptr}};
+                         OPERATOR(gradient_norm), OPERATOR(adamw_step), OPERATOR(adamw_state), {nullptr, nullptr, 0, nullptr}};
 #undef OPERATOR
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

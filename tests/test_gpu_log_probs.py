@@ -68,6 +68,7 @@ def lp_tolerance(lp, v):
 def near(got, want, tolerance, what):
     import torch
     got, want = got.double(), want.double()
+    want = torch.where(want.abs() > 3.4028235677973366e38, torch.copysign(torch.full_like(want, math.inf), want), want)      # what float32 rounds to infinity
     assert torch.equal(torch.isfinite(got), torch.isfinite(want)), what
     assert torch.equal(torch.isnan(got), torch.isnan(want)), what
     same = (got == want) | torch.isnan(want)
@@ -207,6 +208,20 @@ def test_rows_in_order(v, dtype):
     t = torch.tensor([[0, v - 1]] * 6, device="cuda")
     for top in (3, 64):
         check(z, t, top, 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("v", [100, 1500, 5000, 40000, 150000])
+def test_rows_that_are_sure_of_one_token(v, dtype):
+    """The others far behind: 10 ... 300, and more than any exponent holds; spreads that are next to nothing"""
+    import torch
+    z, t, _ = make(7, v, 2, getattr(torch, dtype), v)
+    for i, (lead, spread) in enumerate(((10.0, 1.0), (60.0, 1.0), (300.0, 3.0), (1e4, 1.0), (20.0, 1e-3), (0.0, 1e-30), (3e38, 1.0))):
+        z[i] *= spread
+        z[i, (v * i) // 7] = lead
+    for top in (1, 20, 64):
+        for temperature in (1.0, 0.1, 30.0):
+            check(z, t, top, temperature)
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
