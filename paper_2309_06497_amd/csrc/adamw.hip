@@ -179,6 +179,7 @@ int shampoo_adamw_step(shampoo_adamw *o, void *const *params, const void *const 
   g.b1 = (float)c.beta1; g.b1c = (float)(1.0 - c.beta1); g.b2 = (float)c.beta2; g.b2c = (float)(1.0 - c.beta2);
   g.inv_sqrt = (float)(1.0 / std::sqrt(1.0 - std::pow(c.beta2, t)));
   g.epsilon = (float)c.epsilon; g.keep = (float)(1.0 - lr * c.weight_decay); g.lr = (float)(lr / (1.0 - std::pow(c.beta1, t)));
+  if (!std::isfinite(g.lr) || !std::isfinite(g.keep)) return SHAMPOO_ERR_HYPER;
   g.mix = (uint32_t)(uint64_t)step * AW_MIX2;
   g.has_copies = copies ? 1 : 0;
   const int32_t at_once = AW_POINTERS / (copies ? 3 : 2);

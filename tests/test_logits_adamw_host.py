@@ -174,7 +174,7 @@ for sizes, copies in (([5, 0, 4096], False), ([7] * 240, False), ([7] * 241, Fal
     k = launches("adamw_kernel")
     print(n, rc, rs, len(k), sum(e.a for e in k), sum(-(-s // 2048) for s in sizes), all(e.stream == STREAM for e in entries()))
     reset()
-    assert step(h, n, 3) == -5 and step(h, n, -1) == -5 and step(h, n, 4, lr=float("nan")) == -3 and step(h, n, 4, norm=P, most=0.0) == -3 and step(h, n, 4, norm=P, most=float("nan")) == -3
+    assert step(h, n, 3) == -5 and step(h, n, -1) == -5 and step(h, n, 4, lr=float("nan")) == -3 and step(h, n, 4, lr=1e39) == -3 and step(h, n, 4, norm=P, most=0.0) == -3 and step(h, n, 4, norm=P, most=float("nan")) == -3
     if sizes[0]:
         assert step(h, n, 4, hole=0) == -1 and L.shampoo_adamw_get(h, None, P, 0, S) == -1 and L.shampoo_adamw_set(h, P, None, S) == -1
     assert L.shampoo_adamw_get(h, P, P, 3, S) == -3 and not entries()
