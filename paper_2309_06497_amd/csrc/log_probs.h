@@ -389,7 +389,7 @@ constexpr float LP_SLACK = 8.f;            // x may be that far above its refere
 // thread reads the largest logit and the first piece that has it.  The `top` largest strips hold the `top` most probable tokens (each has one of its own, and no token of
 // another strip comes before any of them), so that the chosen strips alone are read again, and what reaches the bound is put in order.
 // parts > 1: sums and keys of the part go to `sums` and `keys`, and log_probs_join_kernel ends the row.
-// Bound by memory: 8192 x 131072 bf16 368 us (5.8 TB/s), with 20 tokens 384; ten vector operations and an exponential per logit take 0.28 ms of them.  Four loads of a thread
+// Bound by memory: 8192 x 131072 bf16 368 us (5.8 TB/s), with 20 tokens 379; ten vector operations and an exponential per logit take 0.28 ms of them.  Four loads of a thread
 // are on their way together.  Four strips a thread: with 20 tokens 7 % more is read; two cost as much, eight (fewer logits again, more of everything else) 396 and, for 8192 x 32000, 139
 // instead of 114.  Few rows: 1 x 50000 with 20 tokens 9.9 us, of which the choice is 3.4 (table, strips again from L2, order).
 struct LogPartArgs { LogProbsArgs g; int32_t parts, pieces; SoftSums *sums; uint64_t *keys; };
@@ -616,7 +616,7 @@ struct LogProbsGradArgs {
   int32_t classes, m, parts, part_len;     // part_len: classes of a part, a multiple of LP_STEP
   int64_t row0;
 };
-// W = 4: a workgroup per part of a row; W = 1: a wavefront per row, four rows a workgroup, for up to 2048 classes (32768 x 1000 bf16: 25 us, a workgroup per row 42).  A token's
+// W = 4: a workgroup per part of a row; W = 1: a wavefront per row, four rows a workgroup, for up to 4096 (bf16) or 3584 classes (32768 x 1000 bf16: 25 us, a workgroup per row 42).  A token's
 // own part is added by the thread of its first appearance, with those of all others, behind the row's other values: no atomics, and the sum of a token that
 // is given twice is rounded once.  Bound by memory: 4096 x 32000 bf16 106 us (5.0 TB/s, a copy's rate), 999 x 50001 float32 93 us; four loads of a thread
 // together (two in a wavefront's row), 2 % better than two, and stores past the caches no better.
