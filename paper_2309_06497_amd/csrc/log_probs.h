@@ -396,7 +396,7 @@ struct LogPartArgs { LogProbsArgs g; int32_t parts, pieces; SoftSums *sums; uint
 
 template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void log_probs_kernel(const LogPartArgs a) {
   constexpr int AHEAD = 4, STEP = 512 * W;
-  __shared__ float part_m[W], part_most[W], part_s[W], part_w[W];
+  __shared__ float part_m[W], part_s[W], part_w[W];
   [[maybe_unused]] __shared__ Selection<W> l;
   const LogProbsArgs &g = a.g;
   const int64_t unit = g.row0 + blockIdx.x / (uint32_t)a.parts;
@@ -444,19 +444,19 @@ template <typename T, int W, bool TOP> __global__ __launch_bounds__(64 * W) void
       }
     }
   }
-  float most = fmaxf(fmaxf(largest[0], largest[1]), fmaxf(largest[2], largest[3]));
-  SoftSums t = {wave_max(ref), 0.f, 0.f};
+  // From here on about the largest logit: about a reference 8 below it log p of a sure token would be the difference of two numbers of 8, three bits less exact.
+  SoftSums t = {wave_max(fmaxf(fmaxf(largest[0], largest[1]), fmaxf(largest[2], largest[3]))), 0.f, 0.f};
   if constexpr (TOP) {
-    most = wave_max(most);
     for (int k = tid; k < LP_BINS; k += 64 * W) l.bins[k] = 0;
     if (tid == 0) l.n_chosen = l.n_candidates = 0;
   }
-  if (lane == 0) { part_m[wave] = t.m; part_most[wave] = most; }
+  if (lane == 0) part_m[wave] = t.m;
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < W; ++k) { t.m = fmaxf(t.m, part_m[k]); most = fmaxf(most, part_most[k]); }
+  for (int k = 0; k < W; ++k) t.m = fmaxf(t.m, part_m[k]);
+  const float most = t.m;
   {
-    const SoftSums u = about({ref, s, w}, t.m, g.c);
+    const SoftSums u = about({ref, s, w}, most, g.c);
     t.s = wave_sum(u.s); t.w = wave_sum(u.w);
   }
   if (lane == 0) { part_s[wave] = t.s; part_w[wave] = t.w; }
