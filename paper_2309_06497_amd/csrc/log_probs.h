@@ -620,7 +620,9 @@ struct LogProbsGradArgs {
 // own part is added by the thread of its first appearance, with those of all others, behind the row's other values: no atomics, and the sum of a token that
 // is given twice is rounded once.  Bound by memory: 4096 x 32000 bf16 106 us (5.0 TB/s, a copy's rate), 999 x 50001 float32 93 us; four loads of a thread
 // together (two in a wavefront's row), 2 % better than two, and stores past the caches no better.
-template <typename T, int W> __global__ __launch_bounds__(256) void log_probs_grad_kernel(const LogProbsGradArgs g, int64_t rows) {
+// LATE (1 / T above 2^64): 1 / T is a factor of the results and not of the coefficients: 0 times a coefficient over T that float32 does not hold would be no number.  (In one kernel for both:
+// 999 x 50001 float32 1 % longer.)
+template <typename T, int W, bool LATE> __global__ __launch_bounds__(256) void log_probs_grad_kernel(const LogProbsGradArgs g, int64_t rows) {
   constexpr int STEP = 512 * W, AHEAD = W == 1 ? 2 : 4;
   __shared__ int32_t tokens[4 / W][LP_MAX_TOKENS];
   __shared__ float coefs[4 / W][LP_MAX_TOKENS];
@@ -650,7 +652,8 @@ template <typename T, int W> __global__ __launch_bounds__(256) void log_probs_gr
     all += a[k];
     if (first && token[k] == token[j]) { own += a[k]; if (k < j) first = false; }
   }
-  const float b = g.b ? g.b[i] : 0.f, scale = -g.tau * r.inv_s;
+  const float before = LATE ? 1.f : g.tau, after = LATE ? g.tau : 1.f;
+  const float b = g.b ? g.b[i] : 0.f, scale = -before * r.inv_s;
   const bool some = r.inv_s != 0.f && (all != 0.f || b != 0.f);
   const float k1 = some ? scale * b * LP_LN2 : 0.f, k0 = some ? scale * (all + b * (r.entropy - r.log2_s * LP_LN2)) : 0.f;
   const auto value = [&](float x) {
@@ -660,17 +663,17 @@ template <typename T, int W> __global__ __launch_bounds__(256) void log_probs_gr
   const auto put = [&](const Raw8<T> &raw, int v) {
     f32x8 x = expand8(raw);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x.v[e] = value(x.v[e]);
+    for (int e = 0; e < 8; ++e) x.v[e] = value(x.v[e]) * after;
     store8(dz, v, 0x7fffffff, x);
   };
   const auto one = [&](int v) { return value(load8(z, v, v + 1).v[0]); };
   const auto put_one = [&](int v, float y) { const f32x8 x = {{y}}; store8(dz, v, v + 1, x); };
   float at_token = 0.f;
-  if (first) at_token = one(token[j]) + (r.inv_s != 0.f ? g.tau * own : 0.f);
+  if (first) at_token = (one(token[j]) + (r.inv_s != 0.f ? before * own : 0.f)) * after;
   meet();
   int v = begin + j * 8;
   if (pad > 0 && v == 0) {                 // before the first whole piece
-    for (int e = pad; e < min(8, end); ++e) put_one(e, one(e));
+    for (int e = pad; e < min(8, end); ++e) put_one(e, one(e) * after);
     v += STEP;
   }
   for (; v + (AHEAD - 1) * STEP + 8 <= end; v += AHEAD * STEP) {
@@ -682,7 +685,7 @@ template <typename T, int W> __global__ __launch_bounds__(256) void log_probs_gr
   }
   for (; v < end; v += STEP) {
     if (v + 8 <= end) put(raw_load8(z, v, 0x7fffffff), v);
-    else for (int e = v; e < end; ++e) put_one(e, one(e));
+    else for (int e = v; e < end; ++e) put_one(e, one(e) * after);
   }
   meet();
   if (first) put_one(token[j], at_token);

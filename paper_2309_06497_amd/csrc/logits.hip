@@ -97,6 +97,12 @@ template <typename T> int launch_log_probs(LogPartArgs a, int w, int64_t rows, h
     log_probs_join_kernel<T><<<dim3(n), 256, 0, s>>>(a);
   });
 }
+template <typename T, int W> void launch_grad_of(dim3 grid, const LogProbsGradArgs &g, int64_t rows, hipStream_t s) {
+  if (g.tau > 0x1p64f) log_probs_grad_kernel<T, W, true><<<grid, 256, 0, s>>>(g, rows); else log_probs_grad_kernel<T, W, false><<<grid, 256, 0, s>>>(g, rows);
+}
+template <int W> void launch_grad(int32_t dtype, dim3 grid, const LogProbsGradArgs &g, int64_t rows, hipStream_t s) {
+  if (dtype == SHAMPOO_GRAD_F32) launch_grad_of<float, W>(grid, g, rows, s); else launch_grad_of<uint16_t, W>(grid, g, rows, s);
+}
 
 }  // namespace
 
@@ -144,15 +150,13 @@ int shampoo_log_probs_grad(const shampoo_logits *c, const void *logits, const in
   // A wavefront per row: 32768 x 2100 bf16 52 us, a workgroup per row 96; 8192 x 4096 bf16 22.6, 23.4; 4096 x 4096 float32 26.8, 24.8; 4096 x 2100 float32 14.3, 16.4.
   if (c->classes <= (c->dtype == SHAMPOO_GRAD_F32 ? 3584 : 4096)) return by_rows(c->rows, 1, [&](int64_t r, unsigned n) {
     g.row0 = r;
-    if (c->dtype == SHAMPOO_GRAD_F32) log_probs_grad_kernel<float, 1><<<dim3((n + 3) / 4), 256, 0, s>>>(g, r + n);
-    else log_probs_grad_kernel<uint16_t, 1><<<dim3((n + 3) / 4), 256, 0, s>>>(g, r + n);
+    launch_grad<1>(c->dtype, dim3((n + 3) / 4), g, r + n, s);
   });
   g.parts = parts_of(c->rows, c->classes, LP_STEP, MAX_CLASSES, MAX_CLASSES, pad_of(*c, logits), pieces);
   g.part_len = pieces * LP_STEP;
   return by_rows(c->rows, g.parts, [&](int64_t r, unsigned n) {
     g.row0 = r;
-    if (c->dtype == SHAMPOO_GRAD_F32) log_probs_grad_kernel<float, 4><<<dim3(n * g.parts), 256, 0, s>>>(g, c->rows);
-    else log_probs_grad_kernel<uint16_t, 4><<<dim3(n * g.parts), 256, 0, s>>>(g, c->rows);
+    launch_grad<4>(c->dtype, dim3(n * g.parts), g, c->rows, s);
   });
 }
 

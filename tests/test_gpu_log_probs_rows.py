@@ -107,3 +107,46 @@ def test_a_sure_token_read_behind_a_less_probable_one(n, v, dtype):
     off = (r.log_probs.double() - want).abs() / (9 * U + torch.tensor([0.0, 5 * U], device="cuda") * want.abs())
     worst = float(off.max())
     assert worst <= 1, worst
+
+
+def check_gradient(z, t, a, b, temperature, r, row):
+    """a [n, m] or None, b [n] or None"""
+    import torch
+    n, v = z.shape
+    got = B.shampoo_log_probs_grad(z, t, r, a, b)
+    assert got.dtype == z.dtype and got.shape == z.shape
+    ok, at, _, _ = given(row, t, v)
+    ok = ok & row.some
+    coef = torch.where(ok, a.double(), 0.0) if a is not None else torch.zeros(t.shape, device=z.device, dtype=torch.float64)
+    bb = b.double()[:, None] if b is not None else torch.zeros((n, 1), device=z.device, dtype=torch.float64)
+    total, size = coef.sum(1, keepdim=True), coef.abs().sum(1, keepdim=True)
+    want = -row.p * (total + bb * (row.near_lp + row.h))
+    magnitude = size + bb.abs() * (row.near_lp.abs() + row.h)
+    bar = row.p_bar * magnitude + row.p * (12 * U * magnitude + bb.abs() * (torch.where(row.p == 0, 0.0, row.lp_bar) + row.h_bar)) + 1.2e-38 * magnitude
+    want.scatter_add_(1, at, coef)
+    bar.scatter_add_(1, at, torch.where(ok, size * (t.shape[1] + 4) * U, 0.0))
+    half = torch.finfo(z.dtype).eps / 2
+    want, bar = want / temperature, bar / temperature
+    within(got, want, bar * (1 + half) + half * want.abs() + 1.2e-38, "gradient")
+    return got
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("v", [50, 3000, 9000])
+@pytest.mark.parametrize("temperature", [1e-38, 1e-30, 1e-12])
+def test_gradients_of_small_temperatures(v, dtype, temperature):
+    """Coefficients over T that float32 does not hold: nothing for tokens of no probability, and for a token that has all of it"""
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(v)
+    z = torch.randn((40, v), generator=g, device="cuda").to(getattr(torch, dtype))
+    z[:, 1] = torch.where(torch.arange(40, device="cuda") % 2 == 0, -math.inf, 8.0)
+    t = torch.randint(0, v, (40, 2), generator=g, device="cuda")
+    t[:, 0] = torch.where(torch.arange(40, device="cuda") % 3 == 0, z.float().argmax(1), 1)
+    t[::5, 1] = -100
+    a = torch.randn((40, 2), generator=g, device="cuda") * 8
+    b = torch.randn((40,), generator=g, device="cuda") * 8
+    r, row = check(z, t, 5, temperature)
+    for x, y in ((a, None), (a, b), (None, b)):
+        got = check_gradient(z, t, x, y, temperature, r, row)
+        assert not bool(torch.isnan(got).any())
