@@ -150,3 +150,77 @@ def test_gradients_of_small_temperatures(v, dtype, temperature):
     for x, y in ((a, None), (a, b), (None, b)):
         got = check_gradient(z, t, x, y, temperature, r, row)
         assert not bool(torch.isnan(got).any())
+
+
+# Rows in a workgroup of one, two, four and eight wavefronts, and rows in parts of eight that a second launch joins (test_logits_adamw_rows_host.py holds that they are)
+BATCHES = [(4100, 2049), (4099, 8191), (2050, 2500), (4097, 16381), (4097, 16393), (2100, 33000), (65, 131075), (64, 262147), (63, 131077)]
+
+
+def many_kinds(n, v, dtype, seed):
+    """Rows of sixteen kinds by turns, the last rows too: what makes the choice of tokens easy, and what sends it through each of its searches"""
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    z = torch.randn((n, v), generator=g, device="cuda").mul_(2.0)
+    rand = lambda *shape: torch.rand(shape, generator=g, device="cuda")
+    up = torch.arange(v, device="cuda", dtype=torch.float32)
+    kinds = [None,
+             lambda i: torch.floor(rand(v) * 3),                                         # few values
+             lambda i: torch.full((v,), -2.5, device="cuda"),                            # one
+             lambda i: torch.where(rand(v) < 0.5, 0.0, -0.0),
+             lambda i: torch.full((v,), torch.finfo(dtype).min, device="cuda").index_fill_(0, torch.tensor([v // 2, v - 1], device="cuda"), 1.0),
+             lambda i: up * 0.01, lambda i: up * -0.01,                                  # in order
+             lambda i: (up // 8) % 70 * 0.01,
+             lambda i: up // 512 % 40,                                                   # the largest side by side
+             lambda i: z[i].clone().index_fill_(0, (rand(1) * v).long(), 14.0),          # sure of one
+             lambda i: (z[i] * 0.1).index_fill_(0, (rand(1) * v).long(), 300.0),
+             lambda i: torch.where(rand(v) < 0.98, -math.inf, z[i]),                     # few left
+             lambda i: torch.full((v,), -math.inf, device="cuda").index_fill_(0, (rand(1) * v).long(), -3.0),
+             lambda i: torch.full((v,), -math.inf, device="cuda"),
+             lambda i: z[i] * 1e-30,                                                     # spreads next to nothing
+             lambda i: torch.where(up < v - 9, -1.0, 1.0)]                               # the largest last
+    for i in list(range(64 if n > 64 else n)) + list(range(max(n - 16, 64), n)):
+        if kinds[i % 16]:
+            z[i] = kinds[i % 16](i)
+    t = torch.randint(0, v, (n, 3), generator=g, device="cuda")
+    t[:, 2] = z.argmax(1)
+    t[rand(n, 3) < 0.1] = -100
+    a, b = torch.randn((n, 3), generator=g, device="cuda"), torch.randn((n,), generator=g, device="cuda")
+    return z.to(dtype), t, a, b
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,v", BATCHES)
+def test_batches_of_every_kind_of_row(n, v, dtype):
+    import torch
+    z, t, a, b = many_kinds(n, v, getattr(torch, dtype), v)
+    for temperature, tops in ((1.0, (0, 20, 64)), (0.6, (5,))):
+        row = Row(z, temperature)
+        for top in tops:
+            r, _ = check(z, t, top, temperature, row)
+    check_gradient(z, t, a, b, temperature, r, row)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,v", [(4100, 2050), (2050, 4100), (65, 131076)])
+def test_batches_between_the_columns_of_a_matrix(n, v, dtype):
+    """Rows that begin anywhere"""
+    import torch
+    z, t, a, b = many_kinds(n, v, getattr(torch, dtype), v + 1)
+    wide = torch.full((n, v + 3), math.inf, device="cuda", dtype=z.dtype)
+    for first in (1, 2):
+        view = wide[:, first:first + v]
+        view.copy_(z)
+        r, row = check(view, t, 20, 1.0)
+        check_gradient(view, t, a, b, 1.0, r, row)
+        view.fill_(math.inf)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("v", [37, 500, 700, 1025, 2048])
+def test_short_rows_of_every_kind(v, dtype):
+    import torch
+    z, t, a, b = many_kinds(300, v, getattr(torch, dtype), v)
+    for top in (0, 1, 20, 64):
+        r, row = check(z, t, top, 1.0)
+    check_gradient(z, t, a, b, 1.0, r, row)
