@@ -545,7 +545,7 @@ int shampoo_gradient_norm(int32_t n, const void *const *grads, const int64_t *nu
  * state_bits = 8: 128 neighbouring elements of a tensor share a power of two; m has a sign, 4 bits of exponent and 3 of mantissa, v 5 and 3, rounded the same way (v > 0
  * never to 0).  Groups whose largest is below 2^-100 are kept as zeros; one with an infinity, a NaN or a value from 2^127 on reads NaN as a whole.
  */
-typedef struct shampoo_adamw shampoo_adamw; /* opaque, owned by the library */
+typedef struct shampoo_adamw shampoo_adamw; /* opaque, owned by the library; no two calls on the same one at once */
 typedef struct {
   int32_t n_params;        /* 1 ... 2^20                                            */
   const int64_t *numel;    /* host [n_params]: elements, >= 0 each, at most 2^39 together */
@@ -567,6 +567,8 @@ int shampoo_adamw_create(const shampoo_adamw_config *cfg, void *workspace, size_
  * that get the updated float32 parameters, rounded to the nearest.  step: 0-based, strictly increasing.  norm: NULL, or a device pointer to the norm of these gradients
  * (max_norm > 0, may be infinite); where it is not finite the call changes nothing on the device, and the step counts as taken.
  * Recorded into a graph, a step keeps the pointers, lr and step number that it was given.
+ * A step of many tensors is several launches.  If one fails (SHAMPOO_ERR_HIP) the step does not count as taken, but tensors of earlier launches have had it: their parameters, states and
+ * copies are to be restored before it is tried again, which would otherwise apply it to them twice.
  */
 int shampoo_adamw_step(shampoo_adamw *opt, void *const *params, const void *const *grads, void *const *copies, double lr, int64_t step,
                        const float *norm, float max_norm, void *stream);

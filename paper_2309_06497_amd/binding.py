@@ -657,7 +657,8 @@ class AdamW:
     def step(self, params, grads, lr, step, copies=None, norm=None, max_norm=float("inf")):
         """One step, 0-based and strictly increasing.  params, grads: lists of contiguous CUDA tensors of the types given; params are updated in place, each
         tensor stands there once.  copies: bfloat16 tensors that get the updated float32 parameters.  norm: that of these gradients, as shampoo_gradient_norm
-        returns it: they count as scaled down to max_norm, and nothing changes where it is not finite."""
+        returns it: they count as scaled down to max_norm, and nothing changes where it is not finite.  After a launch that failed (code -6) the step does not
+        count, but some tensors may have had it: restore them and the state before it is tried again."""
         _check(self._step(self._stepper, params, grads, copies, lr, step, norm, max_norm, self.param_dtype) if self.handle else -1)
 
     def state(self):
