@@ -95,8 +95,8 @@ __device__ __forceinline__ RowStatistics row_statistics(const SoftSums &t) {
 
 // The `top` largest of many logits.  First by a table: bins of the distance from the largest one, 64 to each doubling of 1 + that distance in units of log 2, up to 255 units (a row that is
 // sure of one token has its others far away).  What reaches bin b holds the `top` largest if `top` values do, since equal ones share a bin and larger ones have
-// no higher one.  One pass of LDS atomics where a search for a bound takes a count by all lanes for each of its steps: 20 tokens of 1 x 131072 in 11.6 us, by the
-// search alone in 14.1.
+// no higher one.  One pass of LDS atomics where a search for a bound takes a count by all lanes for each of its steps: 20 tokens of 1 x 131072 in 11.7 us, by the
+// search alone 2.5 more.
 constexpr int LP_CHOSEN = LP_MAX_TOP + LP_MAX_TOP / 2, LP_CANDIDATES = 512;
 constexpr int LP_BINS = 512;
 constexpr uint32_t LP_BIN_SHIFT = 17, LP_BIN_FIRST = 0x3f800000u >> LP_BIN_SHIFT;      // the upper bits of a float32 are the bin
@@ -389,7 +389,8 @@ constexpr float LP_SLACK = 8.f;            // x may be that far above its refere
 // thread reads the largest logit and the first piece that has it.  The `top` largest strips hold the `top` most probable tokens (each has one of its own, and no token of
 // another strip comes before any of them), so that the chosen strips alone are read again, and what reaches the bound is put in order.
 // parts > 1: sums and keys of the part go to `sums` and `keys`, and log_probs_join_kernel ends the row.
-// Bound by memory: 8192 x 131072 bf16 368 us (5.8 TB/s), with 20 tokens 379; ten vector operations and an exponential per logit take 0.28 ms of them.  Four loads of a thread
+// Bound by memory: 8192 x 131072 bf16 362 us (5.9 TB/s), with 20 tokens 376; ten vector operations and an exponential per logit take 0.28 ms of them.  (The first some 80 passes of a load
+// that has just begun take up to 570.)  Four loads of a thread
 // are on their way together.  Four strips a thread: with 20 tokens 7 % more is read; two cost as much, eight (fewer logits again, more of everything else) 396 and, for 8192 x 32000, 139
 // instead of 114.  Few rows: 1 x 50000 with 20 tokens 9.9 us, of which the choice is 3.4 (table, strips again from L2, order).
 struct LogPartArgs { LogProbsArgs g; int32_t parts, pieces; SoftSums *sums; uint64_t *keys; };

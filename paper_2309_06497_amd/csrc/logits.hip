@@ -36,9 +36,11 @@ int32_t parts_of(int64_t rows, int32_t classes, int64_t step, int64_t longest, i
   return (int32_t)((all + pieces - 1) / pieces);
 }
 // Rows of more classes than a wavefront keeps in registers have a workgroup each, of as many wavefronts as leave 16 pieces to a thread, or more where that fills the
-// GPU's 4096 places.  20 tokens with 1, 2, 4 and 8 wavefronts: 8192 x 4096 bf16 27, 29, 38 and 59 us, 8192 x 131072 572, 470, 405 and 385, 1024 x 50000 55, 33, 29 and 26.
-// Parts and a second launch for long rows where they are few: 20 tokens of 1 x 131072 in 11.6 us, whole 16.4; of 1 x 50000 13.2, whole 9.9; of 128 x 131072 19.2, whole
-// 17.1.
+// GPU's 4096 places.  20 tokens with 1, 2, 4 and 8 wavefronts: 8192 x 4096 bf16 28, 29, 38 and 59 us, 8192 x 131072 566, 466, 402 and 380, 1024 x 50000 51, 33, 29 and 26.
+// Parts and a second launch for long rows where they are few.  Rows of 131072 bf16 classes in parts and whole, us: one 11.7 and 16.2 with 20 tokens, 8.1 and 12.3 with
+// none; 63 rows 16.0 and 17.7, 9.0 and 14.1; 128 rows 19.2 and 18.1, 12.3 and 14.5; 256 rows 23.8 and 19.5, 16.3 and 15.7.  float32: one 11.5 and 15.3, 8.3 and 11.8; 63 rows
+// 17.4 and 17.3, 10.5 and 13.8; 128 rows 21.7 and 18.6, 14.8 and 15.0.  50000 classes are faster whole in both types, for any number of rows: one 9.7 to 11.4.  So without
+// alternatives parts would still pay at 128 rows, which this rule does not use.
 constexpr int32_t SMALL_CLASSES = 2048, LONG_ROW = 65536;
 constexpr int64_t FEW_ROWS = 64;
 int wavefronts(int64_t rows, int32_t classes) {
