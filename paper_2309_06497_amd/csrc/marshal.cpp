@@ -460,7 +460,7 @@ PyObject *log_probs(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
     const int64_t n = k.c.rows;
     const at::Tensor lp = empty(k.z, k.tokens.sizes(), at::kFloat), entropy = empty(k.z, {n}, at::kFloat), stats = empty(k.z, {n, 4}, at::kFloat);
     std::optional<at::Tensor> top, top_lp;
-    if (k.c.top > 0) { top = empty(k.z, {n, k.c.top}, at::kLong); top_lp = empty(k.z, {n, k.c.top}, at::kFloat); }
+    if (const int64_t most = std::min(k.c.top, 64); most > 0) { top = empty(k.z, {n, most}, at::kLong); top_lp = empty(k.z, {n, most}, at::kFloat); }      // more is refused below
     const size_t need = library.log_probs_bytes(&k.c);
     std::optional<at::Tensor> ws;
     if (need > 0) ws = bytes(k.z, need);

@@ -224,3 +224,14 @@ def test_short_rows_of_every_kind(v, dtype):
     for top in (0, 1, 20, 64):
         r, row = check(z, t, top, 1.0)
     check_gradient(z, t, a, b, 1.0, r, row)
+
+
+@pytest.mark.parametrize("top", [65, 1 << 20, (1 << 31) - 1])
+def test_more_tokens_than_are_ordered_are_refused_before_their_memory_is_asked_for(top):
+    import torch
+    z, t = torch.zeros((1 << 15, 8), device="cuda"), torch.zeros((1 << 15,), dtype=torch.int64, device="cuda")
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_reserved()
+    with pytest.raises(B.ShampooError) as e:
+        B.shampoo_log_probs(z, t, top=top)
+    assert e.value.code == -7 and torch.cuda.memory_reserved() - before < 1 << 28
